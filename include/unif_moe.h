@@ -416,6 +416,82 @@ UNIF_MOE_API int unif_moe_group_noalloc(int T, int n_experts, int n_blocks,
                                         int32_t* row_token_dev, float* row_weight_dev,
                                         int64_t row_capacity, void* stream);
 
+/* ---- Operators round the layer ----
+ * They need no handle, allocate nothing and keep no state between calls: all
+ * memory is the caller's, on the current device. Row strides (ld_*) count
+ * elements and are at least the width; rows that are 16-byte aligned and a
+ * multiple of 8 elements wide and apart are moved in 16-byte accesses, others
+ * element by element. The paper has no counterpart of them; its backbones hold
+ * the layer in Transformer blocks, which need them beside it. */
+
+enum { UNIF_MOE_NORM_NONE = 0, UNIF_MOE_NORM_LAYER = 1, UNIF_MOE_NORM_RMS = 2 };
+#define UNIF_MOE_NORM_MAX_WIDTH 8192
+
+/* The step between two blocks of a Transformer: the norm after a block, the
+ * block's gate, the scaled residual sum and the norm before the next block. For
+ * each token, with y the block's output and x the residual stream:
+ *   z   = w_post N_post(y) + b_post     (z = y without post norm)
+ *   out = res_scale x + gate z          (gate 1 where there is none)
+ *   u   = w_pre N_pre(out) + b_pre      (no u without pre norm)
+ * N(v) = (v - mean) / sqrt(var + eps) (LAYER, biased variance) or
+ * v / sqrt(mean(v^2) + eps) (RMS) over the token's `width` features. x and out
+ * have the stream's dtype, y, u and all parameters the branch's: both fp32, both
+ * bf16, or an fp32 stream with a bf16 branch. Arithmetic is fp32, and u is taken
+ * from the fp32 sum, not from the rounded out. */
+typedef struct {
+  int tokens, width;              /* T >= 0, 1 <= width <= UNIF_MOE_NORM_MAX_WIDTH */
+  int stream_dtype, branch_dtype; /* unif_moe_dtype */
+  int post_norm, pre_norm;        /* UNIF_MOE_NORM_* */
+  int gate_rows;                  /* consecutive tokens that share a row of the gate: token t
+                                     uses row t / gate_rows; 0: one row for all */
+  float res_scale, eps;
+} unif_moe_block_norm;
+
+/* Forward.
+ *   x_dev [T][width], y_dev [T][width] or NULL: without y this is the norm
+ *     before a stack's first block, u = w_pre N_pre(x) + b_pre (no post norm,
+ *     gate or out then, and res_scale is not used)
+ *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose rows are not read
+ *     and give 0 in out, u and the statistics
+ *   w_*, b_* [width], gate_dev [ceil(T / gate_rows) or 1][width]; biases and the
+ *     gate may be NULL
+ *   out_dev [T][width] (NULL: not stored), u_dev [T][width]; out may be x and u
+ *     may be y, with the same strides
+ *   *_mean_dev, *_rstd_dev [T] fp32 or NULL: mean and 1 / sqrt(...) of y and of
+ *     out, which the backward reads
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (width), ERR_CUDA. */
+UNIF_MOE_API int unif_moe_block_norm_forward(
+    const unif_moe_block_norm* p, const void* x_dev, int64_t ld_x, const void* y_dev, int64_t ld_y,
+    const uint8_t* token_mask_dev, const void* w_post_dev, const void* b_post_dev,
+    const void* gate_dev, const void* w_pre_dev, const void* b_pre_dev, void* out_dev,
+    int64_t ld_out, void* u_dev, int64_t ld_u, float* post_mean_dev, float* post_rstd_dev,
+    float* pre_mean_dev, float* pre_rstd_dev, void* stream);
+
+/* Bytes of device workspace of unif_moe_block_norm_backward for this
+ * description, with or without a gate; -1 on a bad description. */
+UNIF_MOE_API int64_t unif_moe_block_norm_workspace(const unif_moe_block_norm* p, int gate);
+
+/* Backward: from out, y and the statistics of the forward and the gradients of
+ * out (dout_dev, stream dtype, or NULL: none) and u (du_dev, branch dtype; needed
+ * with a pre norm), the gradients of the inputs and parameters. In the form without y, out_dev is that
+ * forward's x. out_dev and du_dev are not read without a pre norm; the means are
+ * not read for RMS.
+ *   dx_dev [T][width] stream dtype, dy_dev [T][width] branch dtype, each or NULL
+ *   dw_post, db_post, dw_pre, db_pre [width], d_gate [rows of the gate][width]
+ *     fp32, overwritten, each or NULL
+ * dx may be dout and dy may be y or du, with the same strides. Padding rows give 0 and take no part in any sum.
+ * Sums over tokens are added in a fixed order. Enqueued on `stream`, no sync.
+ * Errors: as the forward, and ERR_CAPACITY (workspace_bytes). */
+UNIF_MOE_API int unif_moe_block_norm_backward(
+    const unif_moe_block_norm* p, const void* out_dev, int64_t ld_out, const void* y_dev,
+    int64_t ld_y, const uint8_t* token_mask_dev, const void* w_post_dev, const void* b_post_dev,
+    const void* gate_dev, const void* w_pre_dev, const float* post_mean_dev,
+    const float* post_rstd_dev, const float* pre_mean_dev, const float* pre_rstd_dev,
+    const void* dout_dev, int64_t ld_dout, const void* du_dev, int64_t ld_du, void* dx_dev,
+    int64_t ld_dx, void* dy_dev, int64_t ld_dy, float* dw_post_dev, float* db_post_dev,
+    float* d_gate_dev, float* dw_pre_dev, float* db_pre_dev, void* workspace_dev,
+    int64_t workspace_bytes, void* stream);
+
 /* Frees the handle and its device memory (synchronises the device first).
  * NULL is ignored. */
 UNIF_MOE_API void unif_moe_destroy(unif_moe_t h);

@@ -19,9 +19,12 @@ from typing import Optional
 
 import torch
 
+from . import operators as _operators
+from .operators import BlockNorm
+
 __all__ = ["Layer", "lib", "UnifMoeError", "ERR", "EXPORTS", "Options", "FEATURE_NORM_FIRST",
            "FEATURE_HOST_IO", "FEATURE_BACKWARD", "FEATURE_DIAGNOSTICS", "FEATURES_DEFAULT",
-           "FEATURES_ALL"]
+           "FEATURES_ALL", "BlockNorm"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libunif_moe.so")
@@ -40,7 +43,7 @@ EXPORTS = ["unif_moe_default_thresholds", "unif_moe_default_options", "unif_moe_
            "unif_moe_kernels_per_forward",
            "unif_moe_set_stage_events",
            "unif_moe_sync_status", "unif_moe_selftest_timeout", "unif_moe_group_noalloc",
-           "unif_moe_destroy", "unif_moe_last_error"]
+           "unif_moe_destroy", "unif_moe_last_error"] + _operators.EXPORTS
 
 
 class UnifMoeError(RuntimeError):
@@ -104,10 +107,12 @@ def lib(path: str = LIB_PATH) -> C.CDLL:
         L.unif_moe_destroy.argtypes = [P]
         L.unif_moe_destroy.restype = None
         L.unif_moe_last_error.restype = C.c_char_p
+        _operators.declare(L)
         for name in EXPORTS:
             if name not in ("unif_moe_default_thresholds", "unif_moe_default_options",
                             "unif_moe_destroy",
-                            "unif_moe_last_error", "unif_moe_max_rows"):
+                            "unif_moe_last_error", "unif_moe_max_rows") \
+                    and name not in _operators.EXPORTS:
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib

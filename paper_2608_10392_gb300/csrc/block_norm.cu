@@ -1,0 +1,808 @@
+// The norms round a block, fused with the block's gate and the scaled residual
+// sum, forward and backward (unif_moe_block_norm_forward / _backward).
+//
+//   yn = (y - mean) rstd,  z = w_post yn + b_post      (or z = y)
+//   out = s x + g z,  u = w_pre (out - mean) rstd + b_pre
+//
+// Both passes are bound by memory: a row is read once, held in registers while
+// its sums are taken, and its results written once. A row belongs to a group of
+// threads, eight values to a thread: 8, 16 or 32 lanes of a warp where d <= 64,
+// 128 or 256, else a CTA of ceil(d / 256) warps. Values and sums are fp32; a result is
+// rounded once, to the type it is stored in.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "internal.cuh"
+
+namespace unif {
+namespace norm {
+
+constexpr int kE = 8;            // values per thread and row
+constexpr int kThreads = 128;    // threads per CTA of the forms with several rows per warp or CTA
+constexpr int kMaxWarps = 32;
+
+// ---- eight values of a row ----
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 a, b;
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 a;
+};
+
+// VEC: thread j of a group holds columns 8 j .. 8 j + 7 (16-byte accesses);
+// otherwise columns j, j + n, j + 2 n, ... of n threads.
+template <bool VEC>
+__device__ __forceinline__ int column(int j, int n, int i) {
+  return VEC ? j * kE + i : i * n + j;
+}
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void from_float(float v, float* p) { *p = v; }
+__device__ __forceinline__ void from_float(float v, __nv_bfloat16* p) { *p = __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ void unpack(const uint4& r, float (&v)[kE]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void load(const float* p, int j, int n, int d, float (&v)[kE]) {
+  if (VEC) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (j * kE < d) {
+      a = *reinterpret_cast<const float4*>(p + j * kE);
+      b = *reinterpret_cast<const float4*>(p + j * kE + 4);
+    }
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const int c = column<false>(j, n, i);
+      v[i] = c < d ? p[c] : 0.f;
+    }
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load(const __nv_bfloat16* p, int j, int n, int d, float (&v)[kE]) {
+  if (VEC) {
+    uint4 a = make_uint4(0u, 0u, 0u, 0u);
+    if (j * kE < d) a = *reinterpret_cast<const uint4*>(p + j * kE);
+    unpack(a, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const int c = column<false>(j, n, i);
+      v[i] = c < d ? __bfloat162float(p[c]) : 0.f;
+    }
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store(float* p, int j, int n, int d, const float (&v)[kE]) {
+  if (VEC) {
+    if (j * kE < d) {
+      *reinterpret_cast<float4*>(p + j * kE) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(p + j * kE + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const int c = column<false>(j, n, i);
+      if (c < d) p[c] = v[i];
+    }
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store(__nv_bfloat16* p, int j, int n, int d, const float (&v)[kE]) {
+  if (VEC) {
+    if (j * kE < d) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<uint32_t*>(&t);
+      }
+      *reinterpret_cast<uint4*>(p + j * kE) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const int c = column<false>(j, n, i);
+      if (c < d) p[c] = __float2bfloat16_rn(v[i]);
+    }
+  }
+}
+
+// The sums of N values over the threads of a row's group. GL: lanes per group
+// within a warp, or 0 for the whole CTA; the warps of a CTA meet in `red` (two
+// buffers in turn: the next sum writes the other one, so one barrier is enough).
+template <int GL, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float* red, int& turn) {
+#pragma unroll
+  for (int o = (GL ? GL : 32) / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  if (GL) return;
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return;
+  float* buf = red + (turn & 1) * (2 * kMaxWarps);
+  turn ^= 1;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) buf[(threadIdx.x >> 5) * N + i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.f;
+  for (int w = 0; w < warps; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += buf[w * N + i];
+}
+
+// ---- forward ----
+template <typename TX, typename TB>
+struct ForwardArgs {
+  int T, d, post, pre, gate_rows;
+  float scale, eps;
+  const TX* x;
+  const TB* y;
+  long long ld_x, ld_y, ld_out, ld_u;
+  const uint8_t* mask;
+  const TB *w_post, *b_post, *gate, *w_pre, *b_pre;
+  TX* out;
+  TB* u;
+  float *m_post, *r_post, *m_pre, *r_pre;
+};
+
+// Standardises v (the columns past d hold 0 and stay 0).
+template <bool VEC, int GL>
+__device__ __forceinline__ void standardise(float (&v)[kE], int kind, int j, int n, int d, float eps,
+                                            float* red, int& turn, float& mean, float& rstd) {
+  const float inv = 1.f / (float)d;
+  mean = 0.f;
+  if (kind == UNIF_MOE_NORM_LAYER) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < kE; ++i) s[0] += v[i];
+    group_sum<GL>(s, red, turn);
+    mean = s[0] * inv;
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (column<VEC>(j, n, i) < d) v[i] -= mean;
+  }
+  float q[1] = {0.f};
+#pragma unroll
+  for (int i = 0; i < kE; ++i) q[0] = fmaf(v[i], v[i], q[0]);
+  group_sum<GL>(q, red, turn);
+  rstd = rsqrtf(q[0] * inv + eps);
+#pragma unroll
+  for (int i = 0; i < kE; ++i) v[i] *= rstd;
+}
+
+template <bool VEC, typename TB>
+__device__ __forceinline__ void scale_shift(float (&v)[kE], const TB* w, const TB* b, int j, int n,
+                                            int d) {
+  float t[kE];
+  load<VEC>(w, j, n, d, t);
+#pragma unroll
+  for (int i = 0; i < kE; ++i) v[i] *= t[i];
+  if (b) {
+    load<VEC>(b, j, n, d, t);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] += t[i];
+  }
+}
+
+template <typename TX, typename TB, bool VEC, int GL>
+__global__ void __launch_bounds__(GL ? kThreads : 1024)
+    forward_kernel(const ForwardArgs<TX, TB> a) {
+  __shared__ float red[2 * 2 * kMaxWarps];
+  int turn = 0;
+  const int n = GL ? GL : (int)blockDim.x;
+  const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
+  const int rows = GL ? kThreads / (GL ? GL : 1) : 1;
+  const int d = a.d;
+  // every lane of a warp takes part in the shuffles, also past the last row
+  const int row = blockIdx.x * rows + (GL ? (int)threadIdx.x / (GL ? GL : 1) : 0);
+  const bool in = row < a.T;
+  const bool valid = in && (!a.mask || a.mask[row]);
+  float o[kE], z[kE];
+#pragma unroll
+  for (int i = 0; i < kE; ++i) o[i] = z[i] = 0.f;
+  if (valid) load<VEC>(a.x + row * a.ld_x, j, n, d, o);
+  if (a.y) {
+    if (valid) load<VEC>(a.y + row * a.ld_y, j, n, d, z);
+    if (a.post) {
+      float mean, rstd;
+      standardise<VEC, GL>(z, a.post, j, n, d, a.eps, red, turn, mean, rstd);
+      scale_shift<VEC>(z, a.w_post, a.b_post, j, n, d);
+      if (j == 0 && in) {
+        if (a.m_post) a.m_post[row] = valid ? mean : 0.f;
+        if (a.r_post) a.r_post[row] = valid ? rstd : 0.f;
+      }
+    }
+    if (a.gate && in) {
+      float g[kE];
+      const long long at = a.gate_rows ? row / a.gate_rows : 0;
+      load<VEC>(a.gate + at * d, j, n, d, g);
+#pragma unroll
+      for (int i = 0; i < kE; ++i) z[i] *= g[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i) o[i] = valid ? fmaf(a.scale, o[i], z[i]) : 0.f;
+    if (a.out && in) store<VEC>(a.out + row * a.ld_out, j, n, d, o);
+  }
+  if (a.pre) {
+    float mean, rstd;
+    standardise<VEC, GL>(o, a.pre, j, n, d, a.eps, red, turn, mean, rstd);
+    scale_shift<VEC>(o, a.w_pre, a.b_pre, j, n, d);
+    if (!valid)
+#pragma unroll
+      for (int i = 0; i < kE; ++i) o[i] = 0.f;
+    if (in) {
+      store<VEC>(a.u + row * a.ld_u, j, n, d, o);
+      if (j == 0) {
+        if (a.m_pre) a.m_pre[row] = valid ? mean : 0.f;
+        if (a.r_pre) a.r_pre[row] = valid ? rstd : 0.f;
+      }
+    }
+  }
+}
+
+// ---- backward ----
+// With o^ = (out - m) r, a = du w_pre:
+//   D = dout + r (a - mean(a) - o^ mean(a o^)),  dx = s D
+//   e = D g,  f = e w_post,  dy = r_y (f - mean(f) - yn mean(f yn))
+// (no mean(a), mean(f) terms for rms), and the column sums
+//   dw_pre = sum du o^, db_pre = sum du, dw_post = sum e yn, db_post = sum e,
+//   dg = sum D z over the rows of a gate row.
+// A CTA walks a run of consecutive rows that share a gate row (or holds whole
+// gate rows), keeps the column sums of its columns in registers and writes
+// them once; finish_kernel adds the CTAs' sums in a fixed order, so results
+// do not change from run to run.
+template <typename TX, typename TB>
+struct BackwardArgs {
+  int T, d, post, pre, gate_rows;
+  float scale;
+  const TX* o;
+  const TB* y;
+  const TX* dout;
+  const TB* du;
+  long long ld_o, ld_y, ld_dout, ld_du, ld_dx, ld_dy;
+  const uint8_t* mask;
+  const TB *w_post, *b_post, *gate, *w_pre;
+  const float *m_post, *r_post, *m_pre, *r_pre;
+  TX* dx;
+  TB* dy;
+  float* d_gate;       // written here where a CTA holds whole gate rows (pieces == 1)
+  float* part;         // [CTAs][4][d]: dw_post, db_post, dw_pre, db_pre
+  float* part_gate;    // [CTAs][d] where pieces > 1
+  int wanted;          // bits 0-3: the sums of part; bit 4: dg
+  int pieces;          // CTAs per gate row, or 1
+  int run;             // rows per CTA
+};
+
+// MT: most threads of a CTA (its registers: 128 a thread up to 512 threads).
+template <typename TX, typename TB, bool VEC, int GL, int MT>
+__global__ void __launch_bounds__(MT)
+    backward_kernel(const BackwardArgs<TX, TB> a) {
+  __shared__ float red[2 * 2 * kMaxWarps];
+  __shared__ float fold[GL ? kThreads * kE : 1];
+  int turn = 0;
+  const int n = GL ? GL : (int)blockDim.x;
+  const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
+  const int groups = GL ? kThreads / (GL ? GL : 1) : 1;
+  const int grp = GL ? (int)threadIdx.x / (GL ? GL : 1) : 0;
+  const int d = a.d;
+  const float inv = 1.f / (float)d;
+  const int period = a.gate_rows ? a.gate_rows : a.T;
+  int r0, r1;
+  if (a.pieces > 1) {  // piece of a gate row
+    const int g = blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
+    const long long g0 = (long long)g * period, g1 = min((long long)a.T, g0 + period);
+    r0 = (int)min(g1, g0 + (long long)p * a.run);
+    r1 = (int)min(g1, (long long)r0 + a.run);
+  } else {
+    r0 = (int)min((long long)a.T, (long long)blockIdx.x * a.run);
+    r1 = (int)min((long long)a.T, (long long)r0 + a.run);
+  }
+  float s_wpost[kE], s_bpost[kE], s_wpre[kE], s_bpre[kE], s_gate[kE];
+#pragma unroll
+  for (int i = 0; i < kE; ++i)
+    s_wpost[i] = s_bpost[i] = s_wpre[i] = s_bpre[i] = s_gate[i] = 0.f;
+
+  // Adds the groups' sums of a column in order of the groups and stores them.
+  auto flush = [&](float (&s)[kE], float* to) {
+    if (GL) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kE; ++i) fold[i * kThreads + threadIdx.x] = s[i];
+      __syncthreads();
+      if (grp == 0)
+#pragma unroll
+        for (int i = 0; i < kE; ++i) {
+          float t = 0.f;
+          for (int g = 0; g < groups; ++g) t += fold[i * kThreads + g * n + j];
+          s[i] = t;
+        }
+    }
+    if (grp == 0) store<VEC>(to, j, n, d, s);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) s[i] = 0.f;
+  };
+
+  // the rows of one gate row after another (of all the CTA's rows, without a gate)
+  const bool sum_gate = (a.wanted & 16) != 0;
+  for (int g0 = r0; g0 < r1;) {
+    const int gi = g0 / period;
+    const int g1 = sum_gate && a.pieces == 1 ? (int)min((long long)r1, (long long)(gi + 1) * period) : r1;
+    for (int base = g0; base < g1; base += groups) {
+      const int row = base + grp;
+      const bool in = row < g1;
+      const bool valid = in && (!a.mask || a.mask[row]);
+      float D[kE], oh[kE], yn[kE];
+#pragma unroll
+      for (int i = 0; i < kE; ++i) D[i] = oh[i] = yn[i] = 0.f;
+      if (valid && a.dout) load<VEC>(a.dout + row * a.ld_dout, j, n, d, D);
+      if (valid && a.y) load<VEC>(a.y + row * a.ld_y, j, n, d, yn);
+      if (a.pre) {
+        float w[kE], du[kE], s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kE; ++i) du[i] = 0.f;
+        float m = 0.f, r = 0.f;
+        if (valid) {
+          load<VEC>(a.o + row * a.ld_o, j, n, d, oh);
+          load<VEC>(a.du + row * a.ld_du, j, n, d, du);
+          m = a.pre == UNIF_MOE_NORM_LAYER ? a.m_pre[row] : 0.f;
+          r = a.r_pre[row];
+        }
+        load<VEC>(a.w_pre, j, n, d, w);
+#pragma unroll
+        for (int i = 0; i < kE; ++i) {
+          oh[i] = column<VEC>(j, n, i) < d ? (oh[i] - m) * r : 0.f;
+          s_wpre[i] = fmaf(du[i], oh[i], s_wpre[i]);
+          s_bpre[i] += du[i];
+          w[i] *= du[i];
+          s[0] += w[i];
+          s[1] = fmaf(w[i], oh[i], s[1]);
+        }
+        group_sum<GL>(s, red, turn);
+        const float c0 = a.pre == UNIF_MOE_NORM_LAYER ? s[0] * inv : 0.f, c1 = s[1] * inv;
+#pragma unroll
+        for (int i = 0; i < kE; ++i) D[i] = fmaf(r, w[i] - c0 - oh[i] * c1, D[i]);
+      }
+      if (a.dx && in) {
+        float t[kE];
+#pragma unroll
+        for (int i = 0; i < kE; ++i) t[i] = valid ? a.scale * D[i] : 0.f;
+        store<VEC>(a.dx + row * a.ld_dx, j, n, d, t);
+      }
+      if (a.dy || sum_gate) {
+        float w[kE], m = 0.f, r = 1.f;
+        if (a.post) {
+          if (valid) {
+            m = a.post == UNIF_MOE_NORM_LAYER ? a.m_post[row] : 0.f;
+            r = a.r_post[row];
+          }
+          load<VEC>(a.w_post, j, n, d, w);
+#pragma unroll
+          for (int i = 0; i < kE; ++i) yn[i] = valid && column<VEC>(j, n, i) < d ? (yn[i] - m) * r : 0.f;
+        }
+        if (sum_gate) {
+          float b[kE];
+#pragma unroll
+          for (int i = 0; i < kE; ++i) b[i] = 0.f;
+          if (a.post && a.b_post) load<VEC>(a.b_post, j, n, d, b);
+#pragma unroll
+          for (int i = 0; i < kE; ++i)
+            s_gate[i] = fmaf(D[i], a.post ? fmaf(w[i], yn[i], b[i]) : yn[i], s_gate[i]);
+        }
+        if (a.gate && in) {
+          float g[kE];
+          load<VEC>(a.gate + (long long)(a.gate_rows ? row / period : 0) * d, j, n, d, g);
+#pragma unroll
+          for (int i = 0; i < kE; ++i) D[i] *= g[i];
+        }
+        if (a.post) {
+          float s[2] = {0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < kE; ++i) {
+            s_wpost[i] = fmaf(D[i], yn[i], s_wpost[i]);
+            s_bpost[i] += D[i];
+            D[i] *= w[i];
+            s[0] += D[i];
+            s[1] = fmaf(D[i], yn[i], s[1]);
+          }
+          group_sum<GL>(s, red, turn);
+          const float c0 = a.post == UNIF_MOE_NORM_LAYER ? s[0] * inv : 0.f, c1 = s[1] * inv;
+#pragma unroll
+          for (int i = 0; i < kE; ++i) D[i] = r * (D[i] - c0 - yn[i] * c1);
+        }
+        if (a.dy && in) {
+          if (!valid)
+#pragma unroll
+            for (int i = 0; i < kE; ++i) D[i] = 0.f;
+          store<VEC>(a.dy + row * a.ld_dy, j, n, d, D);
+        }
+      }
+    }
+    if (sum_gate && a.pieces == 1) flush(s_gate, a.d_gate + (long long)gi * d);
+    g0 = g1;
+  }
+  float* part = a.part + (long long)blockIdx.x * 4 * d;
+  if (a.wanted & 1) flush(s_wpost, part);
+  if (a.wanted & 2) flush(s_bpost, part + d);
+  if (a.wanted & 4) flush(s_wpre, part + 2 * (long long)d);
+  if (a.wanted & 8) flush(s_bpre, part + 3 * (long long)d);
+  if (sum_gate && a.pieces > 1) flush(s_gate, a.part_gate + (long long)blockIdx.x * d);
+}
+
+struct FinishArgs {
+  int d, ctas, pieces;
+  const float* part;
+  const float* part_gate;
+  float* to[4];   // dw_post, db_post, dw_pre, db_pre
+  float* d_gate;
+};
+
+// One CTA per 32 columns of one sum: 32 threads per column add every 32nd
+// CTA's share, a tree adds those.
+__global__ void __launch_bounds__(1024) finish_kernel(const FinishArgs a) {
+  __shared__ float t[32][33];
+  grid_dep_wait();
+  const int c = blockIdx.x * 32 + threadIdx.x, k = blockIdx.y;
+  const float* from;
+  float* to;
+  long long step;
+  int count;
+  if (k < 4) {
+    to = a.to[k];
+    if (!to) return;
+    from = a.part + (long long)k * a.d;
+    step = 4ll * a.d;
+    count = a.ctas;
+  } else {
+    to = a.d_gate + (long long)(k - 4) * a.d;
+    from = a.part_gate + (long long)(k - 4) * a.pieces * a.d;
+    step = a.d;
+    count = a.pieces;
+  }
+  float s = 0.f;
+  if (c < a.d)
+#pragma unroll 4
+    for (int i = threadIdx.y; i < count; i += 32) s += from[i * step + c];
+  t[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  s = t[threadIdx.x][threadIdx.y];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const int cc = blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && cc < a.d) to[cc] = s;
+}
+
+// ---- host ----
+// Lanes of a row's group within a warp, or 0 where a row takes a CTA.
+inline int group_lanes(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : d <= 256 ? 32 : 0; }
+inline int cta_threads(int d) {
+  return group_lanes(d) ? kThreads : (d + 32 * kE - 1) / (32 * kE) * 32;
+}
+
+struct Plan {
+  int run, pieces, ctas;
+};
+
+// How the backward's rows are split: about `slots` runs of rows. Where a gate
+// row's rows are many, every gate row is cut into the same number of pieces;
+// where they are few, a run holds whole gate rows.
+Plan plan_backward(const unif_moe_block_norm* p, bool gate, int sms) {
+  const int warps = cta_threads(p->width) / 32;
+  const int groups = group_lanes(p->width) ? kThreads / group_lanes(p->width) : 1;
+  const int slots = sms * (warps >= 16 ? 1 : 16 / warps);
+  const long long T = p->tokens;
+  const long long period = gate && p->gate_rows && p->gate_rows < T ? p->gate_rows : T;
+  const long long G = (T + period - 1) / period;
+  // a run has at least a few rows for each group, so that its column sums are worth writing
+  const long long least = 4ll * groups;
+  long long want = (T + slots - 1) / slots;
+  if (want < least) want = least;
+  Plan r;
+  if (period > want) {
+    long long pieces = slots / G < 1 ? 1 : slots / G;
+    const long long most = (period + least - 1) / least;
+    if (pieces > most) pieces = most;
+    r.pieces = (int)pieces;
+    r.run = (int)((period + pieces - 1) / pieces);
+    r.pieces = (int)((period + r.run - 1) / r.run);
+    r.ctas = (int)(G * r.pieces);
+  } else {
+    r.pieces = 1;
+    r.run = (int)(want / period * period);
+    r.ctas = (int)((T + r.run - 1) / r.run);
+  }
+  return r;
+}
+
+template <typename T>
+bool vec_ok(const T* p, long long ld) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % kE == 0;
+}
+
+template <typename TX, typename TB, bool VEC>
+cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, cudaStream_t s) {
+  const int threads = cta_threads(a.d);
+  switch (group_lanes(a.d)) {
+    case 8: forward_kernel<TX, TB, VEC, 8><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
+    case 16: forward_kernel<TX, TB, VEC, 16><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
+    case 32: forward_kernel<TX, TB, VEC, 32><<<(a.T + 3) / 4, threads, 0, s>>>(a); break;
+    default: forward_kernel<TX, TB, VEC, 0><<<a.T, threads, 0, s>>>(a); break;
+  }
+  return cudaGetLastError();
+}
+
+template <typename TX, typename TB, bool VEC>
+cudaError_t launch_bwd(const BackwardArgs<TX, TB>& a, int ctas, cudaStream_t s) {
+  const int threads = cta_threads(a.d);
+  switch (group_lanes(a.d)) {
+    case 8: backward_kernel<TX, TB, VEC, 8, kThreads><<<ctas, threads, 0, s>>>(a); break;
+    case 16: backward_kernel<TX, TB, VEC, 16, kThreads><<<ctas, threads, 0, s>>>(a); break;
+    case 32: backward_kernel<TX, TB, VEC, 32, kThreads><<<ctas, threads, 0, s>>>(a); break;
+    default:
+      if (threads <= 256) backward_kernel<TX, TB, VEC, 0, 256><<<ctas, threads, 0, s>>>(a);
+      else if (threads <= 512) backward_kernel<TX, TB, VEC, 0, 512><<<ctas, threads, 0, s>>>(a);
+      else backward_kernel<TX, TB, VEC, 0, 1024><<<ctas, threads, 0, s>>>(a);
+      break;
+  }
+  return cudaGetLastError();
+}
+
+int check_desc(const unif_moe_block_norm* p) {
+  if (!p) { set_error("the description is NULL"); return UNIF_MOE_ERR_ARG; }
+  if (p->tokens < 0 || p->width < 1 || p->gate_rows < 0) {
+    set_error("bad sizes: tokens=%d width=%d gate_rows=%d", p->tokens, p->width, p->gate_rows);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (p->width > UNIF_MOE_NORM_MAX_WIDTH) {
+    set_error("width=%d above %d", p->width, UNIF_MOE_NORM_MAX_WIDTH);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  auto type = [](int t) { return t == UNIF_MOE_F32 || t == UNIF_MOE_BF16; };
+  if (!type(p->stream_dtype) || !type(p->branch_dtype) ||
+      (p->stream_dtype == UNIF_MOE_BF16 && p->branch_dtype == UNIF_MOE_F32)) {
+    set_error("bad dtypes: stream %d, branch %d (a bf16 stream takes a bf16 branch)",
+              p->stream_dtype, p->branch_dtype);
+    return UNIF_MOE_ERR_ARG;
+  }
+  auto kind = [](int k) { return k >= UNIF_MOE_NORM_NONE && k <= UNIF_MOE_NORM_RMS; };
+  if (!kind(p->post_norm) || !kind(p->pre_norm)) {
+    set_error("bad norms: post %d, pre %d", p->post_norm, p->pre_norm);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (!(p->eps >= 0.f) || !isfinite(p->eps) || !isfinite(p->res_scale)) {
+    set_error("eps must be finite and >= 0, res_scale finite");
+    return UNIF_MOE_ERR_ARG;
+  }
+  return UNIF_MOE_OK;
+}
+
+bool ld_bad(const void* p, long long ld, int d) { return p && ld < d; }
+
+template <typename TX, typename TB>
+cudaError_t forward_as(const unif_moe_block_norm* p, const void* x, long long ld_x, const void* y,
+                       long long ld_y, const uint8_t* mask, const void* w_post, const void* b_post,
+                       const void* gate, const void* w_pre, const void* b_pre, void* out,
+                       long long ld_out, void* u, long long ld_u, float* m_post, float* r_post,
+                       float* m_pre, float* r_pre, cudaStream_t s) {
+  ForwardArgs<TX, TB> a{p->tokens, p->width, p->post_norm, p->pre_norm, p->gate_rows,
+                        p->res_scale, p->eps,
+                        static_cast<const TX*>(x), static_cast<const TB*>(y),
+                        ld_x, ld_y, ld_out, ld_u, mask,
+                        static_cast<const TB*>(w_post), static_cast<const TB*>(b_post),
+                        static_cast<const TB*>(gate), static_cast<const TB*>(w_pre),
+                        static_cast<const TB*>(b_pre), static_cast<TX*>(out),
+                        static_cast<TB*>(u), m_post, r_post, m_pre, r_pre};
+  const bool vec = p->width % kE == 0 && vec_ok(a.x, ld_x) && (!y || vec_ok(a.y, ld_y)) &&
+                   (!out || vec_ok(a.out, ld_out)) && (!u || vec_ok(a.u, ld_u)) &&
+                   vec_ok(a.w_post, 0) && vec_ok(a.b_post, 0) && vec_ok(a.gate, 0) &&
+                   vec_ok(a.w_pre, 0) && vec_ok(a.b_pre, 0);
+  return vec ? launch_fwd<TX, TB, true>(a, s) : launch_fwd<TX, TB, false>(a, s);
+}
+
+int sm_count(int* n) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    set_error("no CUDA device");
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+int64_t workspace_floats(const Plan& pl, int d) {
+  return (int64_t)pl.ctas * d * (pl.pieces > 1 ? 5 : 4);
+}
+
+template <typename TX, typename TB>
+cudaError_t backward_as(const unif_moe_block_norm* p, const Plan& pl, const void* o, long long ld_o,
+                        const void* y, long long ld_y, const uint8_t* mask, const void* w_post,
+                        const void* b_post, const void* gate, const void* w_pre,
+                        const float* m_post, const float* r_post, const float* m_pre,
+                        const float* r_pre, const void* dout, long long ld_dout, const void* du,
+                        long long ld_du, void* dx, long long ld_dx, void* dy, long long ld_dy,
+                        float* const (&to)[4], float* d_gate, float* ws, cudaStream_t s) {
+  BackwardArgs<TX, TB> a{};
+  a.T = p->tokens; a.d = p->width; a.post = p->post_norm; a.pre = p->pre_norm;
+  a.gate_rows = gate ? p->gate_rows : 0;
+  a.scale = y ? p->res_scale : 1.f;
+  a.o = static_cast<const TX*>(o); a.y = static_cast<const TB*>(y);
+  a.dout = static_cast<const TX*>(dout); a.du = static_cast<const TB*>(du);
+  a.ld_o = ld_o; a.ld_y = ld_y; a.ld_dout = ld_dout; a.ld_du = ld_du; a.ld_dx = ld_dx; a.ld_dy = ld_dy;
+  a.mask = mask;
+  a.w_post = static_cast<const TB*>(w_post); a.b_post = static_cast<const TB*>(b_post);
+  a.gate = static_cast<const TB*>(gate); a.w_pre = static_cast<const TB*>(w_pre);
+  a.m_post = m_post; a.r_post = r_post; a.m_pre = m_pre; a.r_pre = r_pre;
+  a.dx = static_cast<TX*>(dx); a.dy = static_cast<TB*>(dy); a.d_gate = d_gate;
+  a.part = ws;
+  a.part_gate = ws + (int64_t)pl.ctas * 4 * a.d;
+  for (int i = 0; i < 4; ++i) a.wanted |= to[i] ? 1 << i : 0;
+  a.wanted |= d_gate ? 16 : 0;
+  a.pieces = pl.pieces; a.run = pl.run;
+  auto ok = [](const void* q, long long ld) { return !q || vec_ok(static_cast<const char*>(q), ld); };
+  // d_gate is written a gate row at a time by the CTA that holds it
+  const bool vec = a.d % kE == 0 && ok(o, ld_o) && ok(y, ld_y) && ok(dout, ld_dout) &&
+                   ok(du, ld_du) && ok(dx, ld_dx) && ok(dy, ld_dy) && ok(w_post, 0) &&
+                   ok(b_post, 0) && ok(gate, 0) && ok(w_pre, 0) && ok(d_gate, 0) && ok(ws, 0);
+  cudaError_t e = vec ? launch_bwd<TX, TB, true>(a, pl.ctas, s)
+                      : launch_bwd<TX, TB, false>(a, pl.ctas, s);
+  const bool gates = d_gate && pl.pieces > 1;
+  if (e != cudaSuccess || !((a.wanted & 15) || gates)) return e;
+  FinishArgs f{a.d, pl.ctas, pl.pieces, a.part, a.part_gate, {to[0], to[1], to[2], to[3]}, d_gate};
+  return launch_dependent(finish_kernel,
+                          dim3((a.d + 31) / 32, 4 + (gates ? pl.ctas / pl.pieces : 0)),
+                          dim3(32, 32), 0, s, f);
+}
+
+}  // namespace norm
+}  // namespace unif
+
+using unif::set_error;
+namespace nm = unif::norm;
+
+extern "C" {
+
+int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
+                                const void* y, int64_t ld_y, const uint8_t* mask,
+                                const void* w_post, const void* b_post, const void* gate,
+                                const void* w_pre, const void* b_pre, void* out, int64_t ld_out,
+                                void* u, int64_t ld_u, float* m_post, float* r_post, float* m_pre,
+                                float* r_pre, void* stream) {
+  set_error("%s", "");
+  const int rc = nm::check_desc(p);
+  if (rc != UNIF_MOE_OK) return rc;
+  if (p->tokens == 0) return UNIF_MOE_OK;
+  if (!y && (p->post_norm || gate || out)) {
+    set_error("without y there is no post norm, no gate and no out");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if ((p->post_norm && !w_post) || (p->pre_norm && !w_pre)) {
+    set_error("a norm's weight is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (!x || (y && !out && !p->pre_norm) || (p->pre_norm && !u) || (!y && !p->pre_norm)) {
+    set_error("x, out or u is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (nm::ld_bad(x, ld_x, p->width) || nm::ld_bad(y, ld_y, p->width) ||
+      nm::ld_bad(out, ld_out, p->width) || nm::ld_bad(p->pre_norm ? u : nullptr, ld_u, p->width)) {
+    set_error("a row stride is below the width");
+    return UNIF_MOE_ERR_ARG;
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+#define UNIF_ARGS p, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u, \
+                  ld_u, m_post, r_post, m_pre, r_pre, s
+  if (p->branch_dtype == UNIF_MOE_F32) e = nm::forward_as<float, float>(UNIF_ARGS);
+  else if (p->stream_dtype == UNIF_MOE_F32) e = nm::forward_as<float, __nv_bfloat16>(UNIF_ARGS);
+  else e = nm::forward_as<__nv_bfloat16, __nv_bfloat16>(UNIF_ARGS);
+#undef UNIF_ARGS
+  if (e != cudaSuccess) {
+    set_error("block norm forward: %s", cudaGetErrorString(e));
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+int64_t unif_moe_block_norm_workspace(const unif_moe_block_norm* p, int gate) {
+  set_error("%s", "");
+  int sms = 0;
+  if (nm::check_desc(p) != UNIF_MOE_OK || nm::sm_count(&sms) != UNIF_MOE_OK) return -1;
+  if (p->tokens == 0) return 0;
+  return nm::workspace_floats(nm::plan_backward(p, gate != 0, sms), p->width) * (int64_t)sizeof(float);
+}
+
+int unif_moe_block_norm_backward(const unif_moe_block_norm* p, const void* out, int64_t ld_out,
+                                 const void* y, int64_t ld_y, const uint8_t* mask,
+                                 const void* w_post, const void* b_post, const void* gate,
+                                 const void* w_pre, const float* m_post, const float* r_post,
+                                 const float* m_pre, const float* r_pre, const void* dout,
+                                 int64_t ld_dout, const void* du, int64_t ld_du, void* dx,
+                                 int64_t ld_dx, void* dy, int64_t ld_dy, float* dw_post,
+                                 float* db_post, float* d_gate, float* dw_pre, float* db_pre,
+                                 void* workspace, int64_t workspace_bytes, void* stream) {
+  set_error("%s", "");
+  const int rc = nm::check_desc(p);
+  if (rc != UNIF_MOE_OK) return rc;
+  const int d = p->width;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  float* const to[4] = {dw_post, db_post, dw_pre, db_pre};
+  if (p->tokens == 0) {
+    for (float* t : to)
+      if (t && cudaMemsetAsync(t, 0, sizeof(float) * d, s) != cudaSuccess) {
+        set_error("block norm backward: clearing the gradients failed");
+        return UNIF_MOE_ERR_CUDA;
+      }
+    // one gate row where all tokens share it; none where each has its own
+    if (d_gate && p->gate_rows == 0 && cudaMemsetAsync(d_gate, 0, sizeof(float) * d, s) != cudaSuccess) {
+      set_error("block norm backward: clearing the gradients failed");
+      return UNIF_MOE_ERR_CUDA;
+    }
+    return UNIF_MOE_OK;
+  }
+  if (!y && (p->post_norm || gate || dy || d_gate)) {
+    set_error("without y there is no post norm, no gate and no dy");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if ((p->post_norm && !w_post) || (p->pre_norm && !w_pre) || (d_gate && !gate) ||
+      ((dw_post || db_post) && !p->post_norm) || ((dw_pre || db_pre) && !p->pre_norm)) {
+    set_error("a norm's weight or the gate is NULL, or a gradient of a norm that is not there is asked for");
+    return UNIF_MOE_ERR_ARG;
+  }
+  const bool layer_post = p->post_norm == UNIF_MOE_NORM_LAYER;
+  const bool layer_pre = p->pre_norm == UNIF_MOE_NORM_LAYER;
+  if ((p->pre_norm && (!out || !du || !r_pre)) || (layer_pre && !m_pre) ||
+      (p->post_norm && !r_post) || (layer_post && !m_post) || !(dout || du)) {
+    set_error("out, du, dout or a statistic that the norms need is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (nm::ld_bad(p->pre_norm ? out : nullptr, ld_out, d) || nm::ld_bad(y, ld_y, d) ||
+      nm::ld_bad(dout, ld_dout, d) || nm::ld_bad(p->pre_norm ? du : nullptr, ld_du, d) ||
+      nm::ld_bad(dx, ld_dx, d) || nm::ld_bad(dy, ld_dy, d)) {
+    set_error("a row stride is below the width");
+    return UNIF_MOE_ERR_ARG;
+  }
+  int sms = 0;
+  const int rs = nm::sm_count(&sms);
+  if (rs != UNIF_MOE_OK) return rs;
+  const nm::Plan pl = nm::plan_backward(p, gate != nullptr, sms);
+  const int64_t need = nm::workspace_floats(pl, d) * (int64_t)sizeof(float);
+  if (need > workspace_bytes || !workspace) {
+    set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    return UNIF_MOE_ERR_CAPACITY;
+  }
+  if (reinterpret_cast<uintptr_t>(workspace) & 15u) {
+    set_error("the workspace must be 16-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  cudaError_t e;
+#define UNIF_ARGS p, pl, p->pre_norm ? out : nullptr, ld_out, y, ld_y, mask, w_post, b_post, gate, \
+                  w_pre, m_post, r_post, m_pre, r_pre, dout, ld_dout, p->pre_norm ? du : nullptr, \
+                  ld_du, dx, ld_dx, dy, ld_dy, to, d_gate, static_cast<float*>(workspace), s
+  if (p->branch_dtype == UNIF_MOE_F32) e = nm::backward_as<float, float>(UNIF_ARGS);
+  else if (p->stream_dtype == UNIF_MOE_F32) e = nm::backward_as<float, __nv_bfloat16>(UNIF_ARGS);
+  else e = nm::backward_as<__nv_bfloat16, __nv_bfloat16>(UNIF_ARGS);
+#undef UNIF_ARGS
+  if (e != cudaSuccess) {
+    set_error("block norm backward: %s", cudaGetErrorString(e));
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+}  // extern "C"

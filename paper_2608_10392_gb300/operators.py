@@ -1,0 +1,200 @@
+"""Operators round the layer: thin ctypes binding of the handle-free entry points
+of include/unif_moe.h, on torch tensors of the current device.
+
+    norm = BlockNorm(1024, stream_dtype="f32", branch_dtype="bf16", post_norm="rms", pre_norm="rms")
+    r = norm.forward(x, y, post_weight=g1, pre_weight=g2)   # r["out"], r["u"], statistics
+    g = norm.backward(r["out"], y, r, dout=dout, du=du, post_weight=g1, pre_weight=g2)
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+__all__ = ["BlockNorm"]
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+_CODES = {torch.float32: 0, torch.bfloat16: 1}
+_NORMS = {"none": 0, "layer": 1, "rms": 2}
+
+
+class _BlockNormDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("width", C.c_int), ("stream_dtype", C.c_int),
+                ("branch_dtype", C.c_int), ("post_norm", C.c_int), ("pre_norm", C.c_int),
+                ("gate_rows", C.c_int), ("res_scale", C.c_float), ("eps", C.c_float)]
+
+
+EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
+           "unif_moe_block_norm_backward"]
+
+
+def declare(L: C.CDLL) -> None:
+    """Argument and result types of the entry points."""
+    P, I, I64 = C.c_void_p, C.c_int, C.c_int64
+    D = C.POINTER(_BlockNormDesc)
+    L.unif_moe_block_norm_forward.argtypes = ([D, P, I64, P, I64] + [P] * 6 + [P, I64, P, I64]
+                                              + [P] * 5)
+    L.unif_moe_block_norm_workspace.argtypes = [D, I]
+    L.unif_moe_block_norm_backward.argtypes = ([D, P, I64, P, I64] + [P] * 9 + [P, I64] * 4
+                                               + [P] * 6 + [I64, P])
+    for name in EXPORTS:
+        getattr(L, name).restype = C.c_int
+    L.unif_moe_block_norm_workspace.restype = I64
+
+
+def _lib():
+    from . import lib
+    return lib()
+
+
+def _check(rc: int):
+    if rc != 0:
+        from . import _check as check
+        check(rc)
+
+
+def _stream(stream):
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+def _rows(t: Optional[torch.Tensor], name: str, rows: int, width: int, dtype: torch.dtype):
+    """(pointer, row stride) of a [rows][width] CUDA tensor whose rows are dense."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows \
+            or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError("%s: need a CUDA tensor [%d][%d] of %s with dense rows, got %s %s"
+                         % (name, rows, width, dtype, tuple(t.shape), t.dtype))
+    ld = t.stride(0)
+    return t.data_ptr(), (ld if rows > 1 else max(ld, width))
+
+
+def _dense(t: Optional[torch.Tensor], name: str, count: int, dtype: torch.dtype):
+    """Pointer of a contiguous CUDA tensor of `count` elements."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s: need a contiguous CUDA tensor of %d elements of %s, got %s %s"
+                         % (name, count, dtype, tuple(t.shape), t.dtype))
+    return t.data_ptr()
+
+
+def _mask(mask: Optional[torch.Tensor], T: int):
+    if mask is not None and mask.dtype == torch.bool:
+        mask = mask.view(torch.uint8)
+    return _dense(mask, "mask", T, torch.uint8)
+
+
+class BlockNorm:
+    """The step between two blocks of a Transformer: the norm after a block, the
+    block's gate, the scaled residual sum and the norm before the next block.
+
+        z = N_post(y),  out = res_scale x + gate z,  u = N_pre(out)
+
+    x, out: the residual stream [T][width] (stream_dtype "f32" or "bf16"); y, u and
+    all parameters: branch_dtype. post_norm and pre_norm: "none", "layer" or
+    "rms". gate_rows consecutive tokens share a row of the gate (0: all of them).
+    Rows of the tensors may be strided; masked rows (mask 0) are not read and
+    give 0."""
+
+    def __init__(self, width: int, stream_dtype: str = "bf16", branch_dtype: str = "bf16",
+                 post_norm: str = "none", pre_norm: str = "rms", gate_rows: int = 0,
+                 res_scale: float = 1.0, eps: float = 1e-6):
+        self.width, self.gate_rows = width, gate_rows
+        self.stream, self.branch = DTYPES[stream_dtype], DTYPES[branch_dtype]
+        self.post, self.pre = _NORMS[post_norm], _NORMS[pre_norm]
+        self._args = (width, _CODES[self.stream], _CODES[self.branch], self.post, self.pre,
+                      gate_rows, res_scale, eps)
+
+    def _params(self, T, post_weight, post_bias, gate, pre_weight, pre_bias=None):
+        d, tb = self.width, self.branch
+        rows = 1 if self.gate_rows == 0 else -(-T // self.gate_rows)
+        return (_dense(post_weight, "post_weight", d, tb), _dense(post_bias, "post_bias", d, tb),
+                _dense(gate, "gate", rows * d, tb), _dense(pre_weight, "pre_weight", d, tb),
+                _dense(pre_bias, "pre_bias", d, tb))
+
+    def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
+                post_weight: Optional[torch.Tensor] = None,
+                post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                pre_weight: Optional[torch.Tensor] = None,
+                pre_bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None,
+                stream=None) -> dict:
+        """dict of out (x itself without y), u (None without pre norm) and the
+        statistics post_mean, post_rstd, pre_mean, pre_rstd [T] that backward
+        takes. Without y: the norm before a stack's first block."""
+        T, d = x.shape[0], self.width
+        dev = x.device
+        if y is not None and out is None:
+            out = torch.empty(T, d, dtype=self.stream, device=dev)
+        if self.pre and u is None:
+            u = torch.empty(T, d, dtype=self.branch, device=dev)
+        stats = torch.empty(4, T, dtype=torch.float32, device=dev)
+        px, ldx = _rows(x, "x", T, d, self.stream)
+        py, ldy = _rows(y, "y", T, d, self.branch)
+        po, ldo = _rows(out, "out", T, d, self.stream)
+        pu, ldu = _rows(u, "u", T, d, self.branch)
+        s0, step = stats.data_ptr(), 4 * T
+        _check(_lib().unif_moe_block_norm_forward(
+            _BlockNormDesc(T, *self._args), px, ldx, py, ldy, _mask(mask, T),
+            *self._params(T, post_weight, post_bias, gate, pre_weight, pre_bias), po, ldo, pu, ldu,
+            s0, s0 + step, s0 + 2 * step, s0 + 3 * step, _stream(stream)))
+        m1, r1, m2, r2 = stats.unbind(0)
+        return dict(out=x if y is None else out, u=u, post_mean=m1, post_rstd=r1, pre_mean=m2,
+                    pre_rstd=r2)
+
+    def backward(self, out: Optional[torch.Tensor], y: Optional[torch.Tensor], stats: dict, *,
+                 dout: Optional[torch.Tensor] = None, du: Optional[torch.Tensor] = None,
+                 post_weight: Optional[torch.Tensor] = None,
+                 post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                 pre_weight: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                 stream=None) -> dict:
+        """Gradients from those of out (None: none) and u, and the forward's out
+        (x in the form without y), y and statistics: dict of dx (stream_dtype), dy
+        (branch_dtype; None without y) and, in fp32, those of the parameters that
+        there are: d_post_weight, d_post_bias, d_gate, d_pre_weight, d_pre_bias."""
+        ref = du if dout is None else dout
+        if ref is None:
+            raise ValueError("dout and du are both None")
+        T, d = ref.shape[0], self.width
+        dev = ref.device
+        L, desc = _lib(), _BlockNormDesc(T, *self._args)
+        dx = torch.empty(T, d, dtype=self.stream, device=dev)
+        dy = None if y is None else torch.empty(T, d, dtype=self.branch, device=dev)
+        need = L.unif_moe_block_norm_workspace(desc, int(gate is not None))
+        if need < 0:
+            _check(-1)
+        # one allocation: the parameters' gradients, each at 16 bytes, and the workspace
+        names = (["d_post_weight", "d_post_bias"] if self.post else []) \
+            + (["d_pre_weight", "d_pre_bias"] if self.pre else [])
+        step = -(-d // 4) * 4
+        gates = 0 if gate is None else gate.numel()
+        g0 = len(names) * step
+        w0 = g0 + -(-gates // 4) * 4
+        flat = torch.empty(w0 + need // 4, dtype=torch.float32, device=dev)
+        base = flat.data_ptr()
+        at = {n: base + 4 * step * i for i, n in enumerate(names)}
+        po, ldo = _rows(out, "out", T, d, self.stream) if self.pre else (None, 0)
+        py, ldy = _rows(y, "y", T, d, self.branch)
+        pdo, lddo = _rows(dout, "dout", T, d, self.stream)
+        pdu, lddu = _rows(du, "du", T, d, self.branch)
+        F = torch.float32
+        m1, r1, m2, r2 = (
+            _dense(stats.get(k), k, T, F) if used else None for k, used in
+            (("post_mean", self.post), ("post_rstd", self.post), ("pre_mean", self.pre),
+             ("pre_rstd", self.pre)))
+        _check(L.unif_moe_block_norm_backward(
+            desc, po, ldo, py, ldy, _mask(mask, T),
+            *self._params(T, post_weight, post_bias, gate, pre_weight)[:4], m1, r1, m2, r2,
+            pdo, lddo, pdu, lddu, dx.data_ptr(), d, None if dy is None else dy.data_ptr(), d,
+            at.get("d_post_weight"), at.get("d_post_bias"),
+            None if gate is None else base + 4 * g0, at.get("d_pre_weight"), at.get("d_pre_bias"),
+            base + 4 * w0, need, _stream(stream)))
+        r = {n: flat[i * step:i * step + d] for i, n in enumerate(names)}
+        r["dx"], r["dy"] = dx, dy
+        if gate is not None:
+            r["d_gate"] = flat[g0:w0][:gates].view(-1, d)
+        return r
