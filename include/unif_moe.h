@@ -492,6 +492,39 @@ UNIF_MOE_API int unif_moe_block_norm_backward(
     float* d_gate_dev, float* dw_pre_dev, float* db_pre_dev, void* workspace_dev,
     int64_t workspace_bytes, void* stream);
 
+#define UNIF_MOE_BALANCE_MAX_EXPERTS 512
+
+/* Bytes of device workspace of unif_moe_balance_loss; -1 on bad sizes. */
+UNIF_MOE_API int64_t unif_moe_balance_workspace(int T, int K);
+
+/* Losses that keep a router's experts in use, with per-expert counts and the
+ * gradient of the router's logits. Over the n tokens that are not padding, with
+ * p_t = softmax(z_t) over the K experts, c_j how often expert j is selected:
+ *   f_j = c_j / sum_i c_i,  P_j = sum_t p_tj / n
+ *   balance = K sum_j f_j P_j (1 where both are uniform)
+ *   zloss   = sum_t logsumexp(z_t)^2 / n
+ *   loss    = w_balance balance + w_z zloss
+ * The selections are held fixed in the gradient (they are whole numbers):
+ *   dloss/dz_tj = p_tj / n (w_balance K (f_j - sum_i f_i p_ti) + 2 w_z logsumexp(z_t))
+ *   logits_dev [T][K] fp32 or bf16, rows ld apart (the residual experts' columns of a
+ *     router's product [T][K + 1] are such rows); no alignment needed
+ *   q_dev [T][n_q] int32, rows ld_q apart: the experts of a token; k_dev [T] int32 or
+ *     NULL: only the first k_t of them count (unif_moe_get_routing's q with the
+ *     forward's residual_counts). Entries outside [0, K) are skipped
+ *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose logits are not read
+ * A token whose logits are all -inf counts as padding. With no token left, losses, counts and prob
+ * are 0. Outputs (device, overwritten): loss_dev [3] = loss, balance, zloss;
+ * counts_dev [K] = c; prob_dev [K] = P; dlogits_dev [T][K] fp32 or NULL (0 for
+ * padding). Sums over tokens are added in a fixed order.
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (K above
+ * UNIF_MOE_BALANCE_MAX_EXPERTS), ERR_CAPACITY (workspace), ERR_CUDA. */
+UNIF_MOE_API int unif_moe_balance_loss(int T, int K, const void* logits_dev, unif_moe_dtype dtype,
+                                       int64_t ld, const int32_t* q_dev, int n_q, int64_t ld_q,
+                                       const int32_t* k_dev, const uint8_t* token_mask_dev,
+                                       float w_balance, float w_z, float* loss_dev,
+                                       int32_t* counts_dev, float* prob_dev, float* dlogits_dev,
+                                       void* workspace_dev, int64_t workspace_bytes, void* stream);
+
 /* Frees the handle and its device memory (synchronises the device first).
  * NULL is ignored. */
 UNIF_MOE_API void unif_moe_destroy(unif_moe_t h);

@@ -20,11 +20,11 @@ from typing import Optional
 import torch
 
 from . import operators as _operators
-from .operators import BlockNorm
+from .operators import BlockNorm, balance_loss
 
 __all__ = ["Layer", "lib", "UnifMoeError", "ERR", "EXPORTS", "Options", "FEATURE_NORM_FIRST",
            "FEATURE_HOST_IO", "FEATURE_BACKWARD", "FEATURE_DIAGNOSTICS", "FEATURES_DEFAULT",
-           "FEATURES_ALL", "BlockNorm"]
+           "FEATURES_ALL", "BlockNorm", "balance_loss"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libunif_moe.so")

@@ -615,16 +615,6 @@ cudaError_t forward_as(const unif_moe_block_norm* p, const void* x, long long ld
   return vec ? launch_fwd<TX, TB, true>(a, s) : launch_fwd<TX, TB, false>(a, s);
 }
 
-int sm_count(int* n) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-    set_error("no CUDA device");
-    return UNIF_MOE_ERR_CUDA;
-  }
-  return UNIF_MOE_OK;
-}
-
 int64_t workspace_floats(const Plan& pl, int d) {
   return (int64_t)pl.ctas * d * (pl.pieces > 1 ? 5 : 4);
 }
@@ -722,7 +712,7 @@ int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int
 int64_t unif_moe_block_norm_workspace(const unif_moe_block_norm* p, int gate) {
   set_error("%s", "");
   int sms = 0;
-  if (nm::check_desc(p) != UNIF_MOE_OK || nm::sm_count(&sms) != UNIF_MOE_OK) return -1;
+  if (nm::check_desc(p) != UNIF_MOE_OK || unif::sm_count(&sms) != UNIF_MOE_OK) return -1;
   if (p->tokens == 0) return 0;
   return nm::workspace_floats(nm::plan_backward(p, gate != 0, sms), p->width) * (int64_t)sizeof(float);
 }
@@ -778,7 +768,7 @@ int unif_moe_block_norm_backward(const unif_moe_block_norm* p, const void* out, 
     return UNIF_MOE_ERR_ARG;
   }
   int sms = 0;
-  const int rs = nm::sm_count(&sms);
+  const int rs = unif::sm_count(&sms);
   if (rs != UNIF_MOE_OK) return rs;
   const nm::Plan pl = nm::plan_backward(p, gate != nullptr, sms);
   const int64_t need = nm::workspace_floats(pl, d) * (int64_t)sizeof(float);

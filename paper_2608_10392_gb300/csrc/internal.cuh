@@ -235,6 +235,9 @@ bool pick_split(int n, int* bn, int* nsub);  // N sub-tiles of the tensor-core G
 
 void set_error(const char* fmt, ...);
 
+// SMs of the current device; a UNIF_MOE_* code.
+int sm_count(int* n);
+
 // Lets kernel `fn` be launched with `need` bytes of dynamic shared memory. The
 // limit belongs to the kernel, not to a handle, and the value set last holds
 // for all launches: it is always the most that the device allows beside the

@@ -2,7 +2,7 @@
 of include/unif_moe.h, on torch tensors of the current device.
 
     norm = BlockNorm(1024, stream_dtype="f32", branch_dtype="bf16", post_norm="rms", pre_norm="rms")
-    r = norm.forward(x, y, post_weight=g1, pre_weight=g2)   # r["out"], r["u"], statistics
+    r = norm.forward(x, y, post_weight=g1, pre_weight=g2, stats=True)   # r["out"], r["u"], ...
     g = norm.backward(r["out"], y, r, dout=dout, du=du, post_weight=g1, pre_weight=g2)
 """
 from __future__ import annotations
@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-__all__ = ["BlockNorm"]
+__all__ = ["BlockNorm", "balance_loss"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
@@ -26,7 +26,7 @@ class _BlockNormDesc(C.Structure):
 
 
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
-           "unif_moe_block_norm_backward"]
+           "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss"]
 
 
 def declare(L: C.CDLL) -> None:
@@ -38,14 +38,22 @@ def declare(L: C.CDLL) -> None:
     L.unif_moe_block_norm_workspace.argtypes = [D, I]
     L.unif_moe_block_norm_backward.argtypes = ([D, P, I64, P, I64] + [P] * 9 + [P, I64] * 4
                                                + [P] * 6 + [I64, P])
+    L.unif_moe_balance_workspace.argtypes = [I, I]
+    L.unif_moe_balance_loss.argtypes = ([I, I, P, I, I64, P, I, I64, P, P, C.c_float, C.c_float]
+                                        + [P] * 5 + [I64, P])
     for name in EXPORTS:
-        getattr(L, name).restype = C.c_int
-    L.unif_moe_block_norm_workspace.restype = I64
+        getattr(L, name).restype = I64 if name.endswith("_workspace") else C.c_int
 
 
-def _lib():
-    from . import lib
-    return lib()
+_loaded = None
+
+
+def _lib() -> C.CDLL:
+    global _loaded
+    if _loaded is None:
+        from . import lib
+        _loaded = lib()
+    return _loaded
 
 
 def _check(rc: int):
@@ -55,8 +63,8 @@ def _check(rc: int):
 
 
 def _stream(stream):
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # the current stream's handle, without making a Stream object (3 us)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -64,19 +72,19 @@ def _rows(t: Optional[torch.Tensor], name: str, rows: int, width: int, dtype: to
     """(pointer, row stride) of a [rows][width] CUDA tensor whose rows are dense."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows \
-            or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+    at = t.stride()
+    if t.dtype is not dtype or t.shape != (rows, width) or not t.is_cuda \
+            or (at[1] != 1 and width > 1):
         raise ValueError("%s: need a CUDA tensor [%d][%d] of %s with dense rows, got %s %s"
                          % (name, rows, width, dtype, tuple(t.shape), t.dtype))
-    ld = t.stride(0)
-    return t.data_ptr(), (ld if rows > 1 else max(ld, width))
+    return t.data_ptr(), (at[0] if rows > 1 else max(at[0], width))
 
 
 def _dense(t: Optional[torch.Tensor], name: str, count: int, dtype: torch.dtype):
     """Pointer of a contiguous CUDA tensor of `count` elements."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != count or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s: need a contiguous CUDA tensor of %d elements of %s, got %s %s"
                          % (name, count, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
@@ -122,29 +130,34 @@ class BlockNorm:
                 pre_weight: Optional[torch.Tensor] = None,
                 pre_bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None,
-                stream=None) -> dict:
-        """dict of out (x itself without y), u (None without pre norm) and the
-        statistics post_mean, post_rstd, pre_mean, pre_rstd [T] that backward
-        takes. Without y: the norm before a stack's first block."""
+                stats: bool = False, stream=None) -> dict:
+        """dict of out (x itself without y), u (None without pre norm) and, where
+        `stats` asks for them, the statistics post_mean, post_rstd, pre_mean,
+        pre_rstd [T] that backward takes. Without y: the norm before a stack's
+        first block."""
         T, d = x.shape[0], self.width
         dev = x.device
         if y is not None and out is None:
             out = torch.empty(T, d, dtype=self.stream, device=dev)
         if self.pre and u is None:
             u = torch.empty(T, d, dtype=self.branch, device=dev)
-        stats = torch.empty(4, T, dtype=torch.float32, device=dev)
+        saved = torch.empty(4, T, dtype=torch.float32, device=dev) if stats else None
         px, ldx = _rows(x, "x", T, d, self.stream)
         py, ldy = _rows(y, "y", T, d, self.branch)
         po, ldo = _rows(out, "out", T, d, self.stream)
         pu, ldu = _rows(u, "u", T, d, self.branch)
-        s0, step = stats.data_ptr(), 4 * T
+        at = (None,) * 4
+        if stats:
+            s0 = saved.data_ptr()
+            at = (s0, s0 + 4 * T, s0 + 8 * T, s0 + 12 * T)
         _check(_lib().unif_moe_block_norm_forward(
             _BlockNormDesc(T, *self._args), px, ldx, py, ldy, _mask(mask, T),
             *self._params(T, post_weight, post_bias, gate, pre_weight, pre_bias), po, ldo, pu, ldu,
-            s0, s0 + step, s0 + 2 * step, s0 + 3 * step, _stream(stream)))
-        m1, r1, m2, r2 = stats.unbind(0)
-        return dict(out=x if y is None else out, u=u, post_mean=m1, post_rstd=r1, pre_mean=m2,
-                    pre_rstd=r2)
+            *at, _stream(stream)))
+        r = dict(out=x if y is None else out, u=u)
+        if stats:
+            r.update(zip(("post_mean", "post_rstd", "pre_mean", "pre_rstd"), saved.unbind(0)))
+        return r
 
     def backward(self, out: Optional[torch.Tensor], y: Optional[torch.Tensor], stats: dict, *,
                  dout: Optional[torch.Tensor] = None, du: Optional[torch.Tensor] = None,
@@ -198,3 +211,38 @@ class BlockNorm:
         if gate is not None:
             r["d_gate"] = flat[g0:w0][:gates].view(-1, d)
         return r
+
+
+def balance_loss(logits: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, *,
+                 mask: Optional[torch.Tensor] = None, balance_weight: float = 0.01,
+                 z_weight: float = 0.0, grad: bool = True, stream=None) -> dict:
+    """Balance and z losses of a router and the gradient of its logits: dict of
+    loss [3] (weighted sum, balance, z), counts [K] (how often each expert was
+    selected, int32), prob [K] (mean probabilities) and dlogits [T][K] (fp32; None
+    without grad).
+
+    logits [T][K] fp32 or bf16, rows may be strided; q [T][n] int32: the experts of
+    a token, of which the first k[t] count (all without k): Layer.routing()'s q
+    with the forward's residual_counts; mask [T]: 0 marks padding."""
+    T, K = logits.shape
+    dev = logits.device
+    if logits.dtype not in _CODES:
+        raise ValueError("logits: fp32 or bf16, got %s" % logits.dtype)
+    pz, ld = _rows(logits, "logits", T, K, logits.dtype)
+    n_q = q.shape[1]
+    pq, ld_q = _rows(q, "q", T, n_q, torch.int32)
+    L = _lib()
+    need = L.unif_moe_balance_workspace(T, K)
+    if need < 0:
+        _check(-1)
+    # one allocation: loss, counts and prob, each at 16 bytes, and the workspace
+    step = -(-K // 4) * 4
+    flat = torch.empty(4 + 2 * step + need // 4, dtype=torch.float32, device=dev)
+    at = flat.data_ptr()
+    d = torch.empty(T, K, dtype=torch.float32, device=dev) if grad else None
+    _check(L.unif_moe_balance_loss(
+        T, K, pz, _CODES[logits.dtype], ld, pq, n_q, ld_q, _dense(k, "k", T, torch.int32),
+        _mask(mask, T), balance_weight, z_weight, at, at + 16, at + 16 + 4 * step,
+        None if d is None else d.data_ptr(), at + 16 + 8 * step, need, _stream(stream)))
+    return dict(loss=flat[:3], counts=flat[4:4 + K].view(torch.int32),
+                prob=flat[4 + step:4 + step + K], dlogits=d)

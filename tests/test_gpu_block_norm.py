@@ -130,7 +130,7 @@ def test_forward_against_64_bits(case):
     T, d, stream, branch = case[:4]
     cfg, v, e = make(*case, seed=3, dev="cuda")
     r = layer_of(cfg, stream, branch).forward(v["x"], v["y"], mask=v["mask"],
-                                              pre_bias=v["pre_bias"],
+                                              pre_bias=v["pre_bias"], stats=True,
                                               **{k: v[k] for k in PARAMS})
     keep = keep_of(cfg, e)
     rows = torch.arange(T)[keep]
@@ -252,7 +252,7 @@ def test_gradients_against_differences(post, pre):
     cfg, v, e = make(T, d, "f32", "f32", post, pre, 10, True, None, seed=9, dev="cuda")
     from paper_2608_10392_gb300 import BlockNorm
     norm = layer_of(cfg, "f32", "f32")
-    fwd = norm.forward(v["x"], v["y"], pre_bias=v["pre_bias"], **{k: v[k] for k in PARAMS})
+    fwd = norm.forward(v["x"], v["y"], pre_bias=v["pre_bias"], stats=True, **{k: v[k] for k in PARAMS})
     r = norm.backward(fwd["out"], v["y"], fwd, dout=v["dout"], du=v["du"],
                       **{k: v[k] for k in PARAMS})
     rows = torch.arange(T)
@@ -279,7 +279,8 @@ def test_opening_form():
         cfg, v, e = make(70, d, stream, branch, "none", "layer", None, True, "some", seed=2,
                          dev="cuda", scale=1.0)
         norm = layer_of(cfg, stream, branch)
-        r = norm.forward(v["x"], pre_weight=v["pre_weight"], pre_bias=v["pre_bias"], mask=v["mask"])
+        r = norm.forward(v["x"], pre_weight=v["pre_weight"], pre_bias=v["pre_bias"], mask=v["mask"],
+                         stats=True)
         assert r["out"] is v["x"]
         keep = keep_of(cfg, e)
         n, _, rstd = norm64(e["x"][keep], "layer")
