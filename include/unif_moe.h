@@ -525,6 +525,32 @@ UNIF_MOE_API int unif_moe_balance_loss(int T, int K, const void* logits_dev, uni
                                        int32_t* counts_dev, float* prob_dev, float* dlogits_dev,
                                        void* workspace_dev, int64_t workspace_bytes, void* stream);
 
+/* Microscaled 4-bit floating point (MXFP4, E2M1 elements and E8M0 scales). A row
+ * of `cols` columns is held as
+ *   codes  ceil(cols / 32) * 16 bytes: two elements a byte, the even column in
+ *          the low half; sign, two exponent bits, one mantissa bit, the values
+ *          0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives
+ *   scales ceil(cols / 256) * 8 bytes: byte b scales columns 32 b .. 32 b + 31 by
+ *          2^(byte - 127); 255 makes all of them NaN
+ * Elements past cols and the scale bytes past the last block are 0. Rows are
+ * densely packed, codes 16-byte aligned and scales 8-byte. */
+#define UNIF_MOE_MXFP4_MAX_COLS (1 << 24)
+
+/* Rows to MXFP4: a block's scale is 2^e, e = floor(log2 max |x|) - 2 (at least
+ * -127), an element x 2^-e rounded to nearest even among the values above, and
+ * to 6 beyond 6. A block with a NaN or an infinity gets the scale 255 and codes 0.
+ *   x_dev [rows][cols] fp32 or bf16, rows ld apart
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_CUDA. */
+UNIF_MOE_API int unif_moe_mxfp4_quantize(const void* x_dev, unif_moe_dtype dtype, int64_t rows,
+                                         int cols, int64_t ld, uint8_t* codes_dev,
+                                         uint8_t* scales_dev, void* stream);
+
+/* MXFP4 back to rows of fp32 or bf16 (exact but for values beyond bf16's or
+ * fp32's range), rows ld apart. Enqueued on `stream`, no sync. Errors as above. */
+UNIF_MOE_API int unif_moe_mxfp4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                           int64_t rows, int cols, void* x_dev,
+                                           unif_moe_dtype dtype, int64_t ld, void* stream);
+
 /* Frees the handle and its device memory (synchronises the device first).
  * NULL is ignored. */
 UNIF_MOE_API void unif_moe_destroy(unif_moe_t h);

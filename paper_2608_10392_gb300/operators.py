@@ -8,11 +8,11 @@ of include/unif_moe.h, on torch tensors of the current device.
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
-__all__ = ["BlockNorm", "balance_loss"]
+__all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
@@ -26,7 +26,8 @@ class _BlockNormDesc(C.Structure):
 
 
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
-           "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss"]
+           "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss",
+           "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize"]
 
 
 def declare(L: C.CDLL) -> None:
@@ -41,6 +42,8 @@ def declare(L: C.CDLL) -> None:
     L.unif_moe_balance_workspace.argtypes = [I, I]
     L.unif_moe_balance_loss.argtypes = ([I, I, P, I, I64, P, I, I64, P, P, C.c_float, C.c_float]
                                         + [P] * 5 + [I64, P])
+    L.unif_moe_mxfp4_quantize.argtypes = [P, I, I64, I, I64, P, P, P]
+    L.unif_moe_mxfp4_dequantize.argtypes = [P, P, I64, I, P, I, I64, P]
     for name in EXPORTS:
         getattr(L, name).restype = I64 if name.endswith("_workspace") else C.c_int
 
@@ -246,3 +249,68 @@ def balance_loss(logits: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor
         None if d is None else d.data_ptr(), at + 16 + 8 * step, need, _stream(stream)))
     return dict(loss=flat[:3], counts=flat[4:4 + K].view(torch.int32),
                 prob=flat[4 + step:4 + step + K], dlogits=d)
+
+
+class Mxfp4(NamedTuple):
+    """Rows in microscaled 4-bit floating point: codes [...][16 ceil(cols / 32)] uint8
+    (two elements a byte, the even column in the low half), scales
+    [...][8 ceil(cols / 256)] uint8 (byte b: columns 32 b .. 32 b + 31 by 2^(byte - 127)),
+    both contiguous."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+
+
+def _mxfp4(t: Mxfp4, name: str):
+    """(codes' pointer, scales' pointer, rows) of rows in 4 bits."""
+    codes, scales, cols = t
+    per, pitch = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
+    if cols < 1 or codes.dim() < 1 or codes.shape[-1] != per:
+        raise ValueError("%s: codes of %d columns are %d bytes a row, got %s"
+                         % (name, cols, per, tuple(codes.shape)))
+    rows = codes.numel() // per
+    return (_dense(codes, name + ".codes", rows * per, torch.uint8),
+            _dense(scales, name + ".scales", rows * pitch, torch.uint8), rows)
+
+
+def mxfp4_quantize(x: torch.Tensor, out: Optional[Mxfp4] = None, stream=None) -> Mxfp4:
+    """Rows x [...][cols] (fp32 or bf16; a 2-d x may have strided rows) to 4 bits: a
+    block of 32 columns shares the scale 2^e, e = floor(log2 max |x|) - 2, elements
+    round to nearest even and saturate at 6 2^e."""
+    lead, cols = x.shape[:-1], x.shape[-1]
+    if x.dim() != 2:
+        if not x.is_contiguous():
+            raise ValueError("x: more than two dimensions need a contiguous tensor")
+        x = x.view(-1, cols)
+    rows = x.shape[0]
+    if x.dtype not in _CODES:
+        raise ValueError("x: fp32 or bf16, got %s" % x.dtype)
+    px, ld = _rows(x, "x", rows, cols, x.dtype)
+    per, pitch = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
+    if out is None:
+        codes = torch.empty(*lead, per, dtype=torch.uint8, device=x.device)
+        scales = torch.empty(*lead, pitch, dtype=torch.uint8, device=x.device)
+        out = Mxfp4(codes, scales, cols)
+        pc, ps = codes.data_ptr(), scales.data_ptr()
+    else:
+        pc, ps, n = _mxfp4(out, "out")
+        if out.cols != cols or n != rows:
+            raise ValueError("out: %d rows of %d columns, need %d of %d" % (n, out.cols, rows, cols))
+    _check(_lib().unif_moe_mxfp4_quantize(px, _CODES[x.dtype], rows, cols, ld, pc, ps,
+                                          _stream(stream)))
+    return out
+
+
+def mxfp4_dequantize(q: Mxfp4, dtype: str = "bf16", out: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """The values of rows in 4 bits, [...][cols] ("bf16" or "f32"); a 2-d out may have
+    strided rows."""
+    pc, ps, rows = _mxfp4(q, "q")
+    if out is None:
+        out = torch.empty(*q.codes.shape[:-1], q.cols, dtype=DTYPES[dtype], device=q.codes.device)
+        po, ld = out.data_ptr(), q.cols
+    else:
+        po, ld = _rows(out, "out", rows, q.cols, DTYPES[dtype])
+    _check(_lib().unif_moe_mxfp4_dequantize(pc, ps, rows, q.cols, po, _CODES[DTYPES[dtype]], ld,
+                                            _stream(stream)))
+    return out
