@@ -551,6 +551,36 @@ UNIF_MOE_API int unif_moe_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
                                            int64_t rows, int cols, void* x_dev,
                                            unif_moe_dtype dtype, int64_t ld, void* stream);
 
+enum { UNIF_MOE_ACTIVATION_NONE = 0, UNIF_MOE_ACTIVATION_GELU = 1 };
+#define UNIF_MOE_MXFP4_MAX_GROUPS 1024
+
+/* Product of rows in MXFP4 with the weights of their group, also in MXFP4:
+ *   out[r][j] = act(sum_c A[r][c] W[g][j][c]) for the rows r of group g, those in
+ *   [offsets[g], offsets[g + 1])
+ * Elements and scales are multiplied exactly and summed in fp32; a result is
+ * rounded once. With the rows of a layer's group table (unif_moe_get_groups,
+ * unif_moe_group_noalloc) a group is an (expert, block) pair and its offsets are
+ * the table's.
+ *   a_codes_dev, a_scales_dev   [rows] rows of cols columns
+ *   w_codes_dev, w_scales_dev   [groups][n] rows of cols columns
+ *   offsets_dev [groups + 1] int32; NULL with one group: all rows. Offsets outside
+ *     [0, rows] are taken as the nearest bound; a group whose end is not above its
+ *     start has no rows, and groups that together have more than `rows` rows lose the
+ *     last ones. Rows of no group are not written
+ *   activation  UNIF_MOE_ACTIVATION_*: GELU is 0.5 v (1 + erf(v / sqrt 2)), for bf16
+ *     output within 3e-4 |v| of it before the rounding
+ *   out_dev [rows][n] fp32 or bf16, rows ld apart
+ *   status_dev [1] int32: a kernel that gives up a wait sets it non-zero (zero it
+ *     before the first call); the output is then incomplete
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (groups, or more than
+ * 2^31 tiles), ERR_CUDA. */
+UNIF_MOE_API int unif_moe_mxfp4_product(const uint8_t* a_codes_dev, const uint8_t* a_scales_dev,
+                                        int64_t rows, int cols, const uint8_t* w_codes_dev,
+                                        const uint8_t* w_scales_dev, int n, int groups,
+                                        const int32_t* offsets_dev, int activation, void* out_dev,
+                                        unif_moe_dtype dtype, int64_t ld, int32_t* status_dev,
+                                        void* stream);
+
 /* Frees the handle and its device memory (synchronises the device first).
  * NULL is ignored. */
 UNIF_MOE_API void unif_moe_destroy(unif_moe_t h);

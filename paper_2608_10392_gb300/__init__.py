@@ -20,12 +20,13 @@ from typing import Optional
 import torch
 
 from . import operators as _operators
-from .operators import BlockNorm, Mxfp4, balance_loss, mxfp4_dequantize, mxfp4_quantize
+from .operators import (BlockNorm, Mxfp4, balance_loss, mxfp4_dequantize, mxfp4_product,
+                        mxfp4_quantize, mxfp4_status)
 
 __all__ = ["Layer", "lib", "UnifMoeError", "ERR", "EXPORTS", "Options", "FEATURE_NORM_FIRST",
            "FEATURE_HOST_IO", "FEATURE_BACKWARD", "FEATURE_DIAGNOSTICS", "FEATURES_DEFAULT",
            "FEATURES_ALL", "BlockNorm", "balance_loss", "Mxfp4",
-           "mxfp4_quantize", "mxfp4_dequantize"]
+           "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_product", "mxfp4_status"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libunif_moe.so")

@@ -1,0 +1,491 @@
+// Product of rows in MXFP4 with the weights of their group, also in MXFP4
+// (unif_moe_mxfp4_product): out[r][n] = act(sum_c A[r][c] W[g(r)][n][c]).
+//
+// tcgen05 block-scaled MMAs (kind mxf4: products of 4-bit elements and 8-bit
+// scales exact, sums in fp32 in TMEM). The weights are the M operand, 128 output
+// channels to a tile, and the rows the N operand, up to 192 to a tile: a tile
+// of few rows then costs few columns, whatever a group's size, and a lane of
+// the accumulator is a channel, so that 32 lanes store consecutive channels of
+// one row.
+//
+// One CTA per SM walks (row tile, channel tile) items, steps of 256 columns
+// through a ring of stages. Roles of the warps: 8 store accumulators, one loads
+// codes by TMA, one issues MMAs, 4 bring the scales: eight bytes a row and step,
+// read from row-major storage into registers and written as the 512-byte blocks
+// that tcgen05.cp spreads over TMEM (byte 16 (r % 32) + 4 (r / 32) + b of a block
+// is scale b of row r).
+#include <math.h>
+
+#include "tc_common.cuh"
+
+namespace unif {
+namespace fp4p {
+
+using namespace tc;
+
+constexpr int kTN = 192;         // rows of a tile (MMA N)
+constexpr int kStep = 256;       // columns of a step: 128 bytes of codes, 8 scales
+constexpr int kStages = 5;
+constexpr uint32_t kBytesW = 128 * 128, kBytesA = kTN * 128;
+constexpr uint32_t kBytesSW = 1024, kBytesSA = 2048;  // scale blocks of a stage
+constexpr uint32_t kStageBytes = kBytesW + kBytesA + kBytesSW + kBytesSA;
+constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 4;
+constexpr int kThreads = 32 * (kScaleWarp + kScaleWarps);
+constexpr int kBoxRows = 32;     // rows of one TMA box of A
+// TMEM columns: two accumulators, then the scales of each stage.
+constexpr uint32_t kAcc = kTN, kScaleCol = 2 * kTN, kScaleCols = 24, kTmemCols = 512;
+static_assert(kScaleCol + kStages * kScaleCols <= kTmemCols, "TMEM");
+constexpr int kBars = 2 * kStages + 5;
+
+struct Params {
+  int rows, N, G, num_kb, ch_tiles;
+  const int32_t* offsets;   // [G + 1], or NULL: one group of all rows
+  const uint8_t* a_scales;
+  const uint8_t* w_scales;
+  int pitch;                // scale bytes of a row
+  void* out;
+  long long ld;
+  bool pairs;               // out and ld allow stores of two bf16
+  int* status;
+  long long wait_limit;
+};
+
+__host__ __device__ constexpr uint32_t smem_bytes(int G) {
+  return 1024u + kStages * kStageBytes + (kBars + 1) * 8u + (uint32_t)(2 * G + 1) * 4u + 16u;
+}
+
+__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                         uint32_t sa, uint32_t sb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::
+          "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+      : "memory");
+}
+// A 512-byte block of scales (32 x 16 bytes) to four TMEM columns, in all four
+// lane quarters.
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// Descriptor of such a block: no swizzle, 8-row groups of 16-byte rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) |
+         ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+// Instruction descriptor of kind mxf4: A and B E2M1 (bits 7-9, 10-12 = 1), N >> 3
+// at bits 17-22, scales E8M0 (bit 23), M >> 7 at bits 27-28; bits 4-5 and 29-30
+// pick the byte of a TMEM word at which B's and A's scales start (0 or 2).
+__device__ __forceinline__ uint32_t idesc_mxf4(int n, int scale_byte) {
+  return ((uint32_t)scale_byte << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
+         (1u << 23) | (1u << 27) | ((uint32_t)scale_byte << 29);
+}
+
+__device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > limit) return;
+}
+
+// Items of the walk: a run of a group's rows and 128 of its channels.
+struct Item {
+  int g, ch0, row0, rows;  // rows >= 1
+};
+
+template <typename TO, bool GELU>
+__device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int row0, int rows, int ch,
+                                            int lane) {
+  if constexpr (sizeof(TO) == 4) {
+    float* o = static_cast<float*>(p.out) + (long long)row0 * p.ld + ch;
+    if (ch < p.N)
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        if (j < rows) {
+          float y = v[j];
+          if (GELU) y = 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
+          *o = y;
+        }
+        o += p.ld;
+      }
+  } else {
+    uint32_t h[16];  // rows 2 i and 2 i + 1 of this lane's channel
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (GELU) {
+        h[i] = gelu2_bf16x2(v[2 * i], v[2 * i + 1]);
+      } else {
+        __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        h[i] = *reinterpret_cast<uint32_t*>(&t);
+      }
+    }
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + (long long)row0 * p.ld;
+    if (p.pairs) {
+      // an even lane stores its and the next lane's channel of row 2 i, the odd one of row 2 i + 1
+      const bool odd = lane & 1;
+      o += (odd ? p.ld : 0) + (ch & ~1);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, h[i], 1);
+        const uint32_t w = odd ? __byte_perm(other, h[i], 0x7632) : __byte_perm(h[i], other, 0x5410);
+        if (2 * i + (odd ? 1 : 0) < rows && ch < p.N) *reinterpret_cast<uint32_t*>(o) = w;
+        o += 2 * p.ld;
+      }
+    } else if (ch < p.N) {
+      o += ch;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const __nv_bfloat162 t = *reinterpret_cast<__nv_bfloat162*>(&h[i]);
+        if (2 * i < rows) *o = t.x;
+        o += p.ld;
+        if (2 * i + 1 < rows) *o = t.y;
+        o += p.ld;
+      }
+    }
+  }
+}
+
+template <typename TO, bool GELU>
+__global__ void __launch_bounds__(kThreads, 1)
+    product_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+                   const Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t s0 = smem_u32(smem);
+  // stage s: weight codes, row codes, weight scales, row scales
+  auto stage = [&](int s) { return s0 + (uint32_t)s * kStageBytes; };
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto accf_bar = [&](int a) { return bar0 + 8u * (2 * kStages + a); };
+  auto acce_bar = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); };
+  const uint32_t mma_done = bar0 + 8u * (2 * kStages + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int32_t* first_s = reinterpret_cast<int32_t*>(bars + kBars + 1);  // [G + 1]
+  int32_t* len_s = first_s + p.G + 1;                               // [G]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 2);  // the loader and the scales' warp
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(accf_bar(a), 1);
+      mbar_init(acce_bar(a), kEpiWarps);
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  grid_dep_wait();
+  if (warp == 0) {
+    // row tiles before each group; whatever the offsets hold, rows stay in [0, rows)
+    // and the groups have no more than `rows` rows together
+    int sum = 0, left = p.rows;
+    for (int g0 = 0; g0 < p.G; g0 += 32) {
+      const int g = g0 + lane;
+      int n = 0;
+      if (g < p.G) {
+        const int lo = p.offsets ? min(max(p.offsets[g], 0), p.rows) : 0;
+        const int hi = p.offsets ? min(max(p.offsets[g + 1], 0), p.rows) : p.rows;
+        n = max(hi - lo, 0);
+      }
+      long long before = n;  // rows of the groups up to this one
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long t = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += t;
+      }
+      const long long all = __shfl_sync(0xffffffffu, before, 31);
+      n = (int)max(0ll, min((long long)n, left - (before - n)));
+      left = (int)max(0ll, left - all);
+      if (g < p.G) len_s[g] = n;
+      const int tiles = (n + kTN - 1) / kTN;
+      int inc = tiles;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (g < p.G) first_s[g] = sum + inc - tiles;
+      sum += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) first_s[p.G] = sum;
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int n_items = first_s[p.G] * p.ch_tiles;
+  auto item_of = [&](int i) {
+    const int tile = i / p.ch_tiles;
+    int lo = 0, hi = p.G - 1;  // the last group whose first tile is <= tile
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first_s[mid] <= tile) lo = mid; else hi = mid - 1;
+    }
+    Item it;
+    it.g = lo;
+    it.ch0 = (i - tile * p.ch_tiles) * 128;
+    const int tiles = first_s[lo + 1] - first_s[lo], rows = len_s[lo];
+    const int part = ((rows + tiles - 1) / tiles + 15) & ~15;
+    const int at = (tile - first_s[lo]) * part;
+    it.row0 = (p.offsets ? min(max(p.offsets[lo], 0), p.rows) : 0) + at;
+    it.rows = min(part, rows - at);
+    return it;
+  };
+
+  if (warp < kEpiWarps) {
+    // ---------------- accumulators to the output ----------------------------
+    const int q = warp & 3, half = warp >> 2;
+    int acc = 0;
+    uint32_t ph = 0;
+    for (int i = blockIdx.x; i < n_items; i += gridDim.x) {
+      const Item it = item_of(i);
+      if (!wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit)) break;
+      tc_fence_after();
+      const int chunks = (it.rows + 31) / 32;
+      const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16);
+      float v[32];
+      for (int c = half; c < chunks; c += 2) {
+        tmem_ld32(from + c * 32, v);
+        if (c + 2 >= chunks) {
+          tc_fence_before();
+          if (lane == 0) mbar_arrive(acce_bar(acc));
+        }
+        store_chunk<TO, GELU>(p, v, it.row0 + c * 32, it.rows - c * 32, it.ch0 + q * 32 + lane, lane);
+      }
+      if (half >= chunks && lane == 0) mbar_arrive(acce_bar(acc));
+      if (++acc == 2) { acc = 0; ph ^= 1u; }
+    }
+  } else if (warp == kTmaWarp) {
+    // ---------------- codes of both operands --------------------------------
+    bool ok = true;
+    int s = 0;
+    uint32_t ph = 0;
+    long long issued = 0;
+    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
+      const Item it = item_of(i);
+      const int boxes = (it.rows + kBoxRows - 1) / kBoxRows;
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        ok = wait_warp(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t bar = full_bar(s);
+          mbar_expect_tx(bar, kBytesW + (uint32_t)boxes * kBoxRows * 128u);
+          tma_load_2d(stage(s), &tmW, bar, kb * 64, it.g * p.N + it.ch0);
+          for (int b = 0; b < boxes; ++b)
+            tma_load_2d(stage(s) + kBytesW + (uint32_t)b * kBoxRows * 128u, &tmA, bar, kb * 64,
+                        it.row0 + b * kBoxRows);
+        }
+        __syncwarp();
+        ++issued;
+        if (++s == kStages) { s = 0; ph ^= 1u; }
+      }
+    }
+    // loads still in flight land before the CTA exits
+    if (lane == 0)
+      for (long long j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
+        wait_settle(full_bar((int)(j % kStages)), (uint32_t)((j / kStages) & 1), p.wait_limit / 16);
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    // ---------------- scales to TMEM, MMAs ----------------------------------
+    int s = 0, acc = 0;
+    uint32_t ph = 0, acc_ph = 0;
+    bool ok = true, any = false;
+    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
+      const Item it = item_of(i);
+      ok = wait_warp(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
+      if (!ok) break;
+      tc_fence_after();
+      const int n = (it.rows + 15) & ~15;
+      const uint32_t d = tmem + acc * kAcc;
+      const uint32_t id0 = idesc_mxf4(n, 0), id2 = idesc_mxf4(n, 2);
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        ok = wait_warp(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t sc = stage(s) + kBytesW + kBytesA;
+          const uint32_t tw = tmem + kScaleCol + s * kScaleCols, ta = tw + 8;
+          const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW);
+          copy_scales(tw, dw);
+          copy_scales(tw + 4, dw + (512 >> 4));
+          copy_scales(ta, da);
+          copy_scales(ta + 8, da + (1024 >> 4));
+          if (n > 128) {
+            copy_scales(ta + 4, da + (512 >> 4));
+            copy_scales(ta + 12, da + (1536 >> 4));
+          }
+          const uint64_t w = sw128_desc(stage(s)), a = sw128_desc(stage(s) + kBytesW);
+          // 64 columns (32 bytes, two scales) at a time
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            mma_mxf4(d, w + 2 * k, a + 2 * k, (k & 1) ? id2 : id0, tw + 4 * (k >> 1),
+                     ta + 8 * (k >> 1), (kb | k) != 0 ? 1u : 0u);
+          umma_commit(empty_bar(s));
+          if (kb == p.num_kb - 1) umma_commit(accf_bar(acc));
+        }
+        __syncwarp();
+        any = true;
+        if (++s == kStages) { s = 0; ph ^= 1u; }
+      }
+      if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+    }
+    // every MMA issued has completed before TMEM is released
+    if (any) {
+      if (elect_one()) umma_commit(mma_done);
+      __syncwarp();
+      wait_settle(mma_done, 0u, p.wait_limit);
+    }
+  } else {
+    // ---------------- scales ------------------------------------------------
+    const int mine = warp - kScaleWarp;
+    long long c = 0;  // steps so far
+    bool ok = true;
+    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
+      const Item it = item_of(i);
+      const uint8_t* ws = p.w_scales + ((long long)it.g * p.N + it.ch0 + lane) * p.pitch;
+      const uint8_t* as = p.a_scales + ((long long)it.row0 + lane) * p.pitch;
+      for (int kb = 0; kb < p.num_kb; ++kb, ++c) {
+        if ((int)(c % kScaleWarps) != mine) continue;
+        uint2 w[4], a[6];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          w[r] = make_uint2(0u, 0u);
+          if (it.ch0 + 32 * r + lane < p.N)
+            w[r] = __ldg(reinterpret_cast<const uint2*>(ws + (long long)(32 * r) * p.pitch + kb * 8));
+        }
+#pragma unroll
+        for (int r = 0; r < 6; ++r) {
+          a[r] = make_uint2(0u, 0u);
+          if (32 * r + lane < it.rows)
+            a[r] = __ldg(reinterpret_cast<const uint2*>(as + (long long)(32 * r) * p.pitch + kb * 8));
+        }
+        const int s = (int)(c % kStages);
+        const uint32_t ph = (uint32_t)((c / kStages) & 1);
+        ok = wait_warp(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        uint8_t* at = smem + (size_t)s * kStageBytes + kBytesW + kBytesA + lane * 16;
+        *reinterpret_cast<uint4*>(at) = make_uint4(w[0].x, w[1].x, w[2].x, w[3].x);
+        *reinterpret_cast<uint4*>(at + 512) = make_uint4(w[0].y, w[1].y, w[2].y, w[3].y);
+        at += kBytesSW;
+        *reinterpret_cast<uint4*>(at) = make_uint4(a[0].x, a[1].x, a[2].x, a[3].x);
+        *reinterpret_cast<uint4*>(at + 512) = make_uint4(a[4].x, a[5].x, 0u, 0u);
+        *reinterpret_cast<uint4*>(at + 1024) = make_uint4(a[0].y, a[1].y, a[2].y, a[3].y);
+        *reinterpret_cast<uint4*>(at + 1536) = make_uint4(a[4].y, a[5].y, 0u, 0u);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full_bar(s));
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+}
+
+template <typename TO, bool GELU>
+cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmA, const Params& p, int grid,
+                   cudaStream_t s) {
+  const uint32_t smem = smem_bytes(p.G);
+  cudaError_t e = allow_smem(product_kernel<TO, GELU>, smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(product_kernel<TO, GELU>, dim3(grid), dim3(kThreads), smem, s, tmW, tmA, p);
+}
+
+}  // namespace fp4p
+}  // namespace unif
+
+using unif::set_error;
+namespace fpp = unif::fp4p;
+
+extern "C" {
+
+int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int64_t rows, int cols,
+                           const uint8_t* w_codes, const uint8_t* w_scales, int n, int groups,
+                           const int32_t* offsets, int activation, void* out, unif_moe_dtype dtype,
+                           int64_t ld, int32_t* status, void* stream) {
+  set_error("%s", "");
+  if (rows < 0 || rows > 0x7fffffff - 1024 || n < 1 || groups < 1 || cols < 1 ||
+      cols > UNIF_MOE_MXFP4_MAX_COLS || (int64_t)n * groups > 0x7fffffff - 1024) {
+    set_error("bad sizes: rows=%lld cols=%d n=%d groups=%d", (long long)rows, cols, n, groups);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (groups > UNIF_MOE_MXFP4_MAX_GROUPS) {
+    set_error("groups=%d above %d", groups, UNIF_MOE_MXFP4_MAX_GROUPS);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  if ((dtype != UNIF_MOE_F32 && dtype != UNIF_MOE_BF16) || activation < 0 ||
+      activation > UNIF_MOE_ACTIVATION_GELU) {
+    set_error("bad dtype %d or activation %d", (int)dtype, activation);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (rows == 0) return UNIF_MOE_OK;
+  if (!a_codes || !a_scales || !w_codes || !w_scales || !out || !status || (groups > 1 && !offsets)) {
+    set_error("codes, scales, offsets, out or status is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  const uintptr_t codes = reinterpret_cast<uintptr_t>(a_codes) | reinterpret_cast<uintptr_t>(w_codes);
+  const uintptr_t scales = reinterpret_cast<uintptr_t>(a_scales) | reinterpret_cast<uintptr_t>(w_scales);
+  if ((codes & 15u) || (scales & 7u)) {
+    set_error("codes must be 16-byte aligned, scales 8-byte");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (ld < n) {
+    set_error("the output's row stride %lld is below n=%d", (long long)ld, n);
+    return UNIF_MOE_ERR_ARG;
+  }
+  int sms = 0;
+  const int rc = unif::sm_count(&sms);
+  if (rc != UNIF_MOE_OK) return rc;
+  const uint64_t pitch = (uint64_t)(cols + 31) / 32 * 16;
+  CUtensorMap tmW, tmA;  // 128-byte pieces of code rows, counted in 2-byte units
+  if (!unif::encode_bf16_map(&tmW, w_codes, pitch / 2, (uint64_t)n * groups, 64, 128, 128) ||
+      !unif::encode_bf16_map(&tmA, a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxRows, 128)) {
+    set_error("cuTensorMapEncodeTiled failed for the codes");
+    return UNIF_MOE_ERR_CUDA;
+  }
+  fpp::Params p{};
+  p.rows = (int)rows; p.N = n; p.G = groups;
+  p.num_kb = (cols + fpp::kStep - 1) / fpp::kStep;
+  p.ch_tiles = (n + 127) / 128;
+  p.offsets = offsets;
+  p.a_scales = a_scales; p.w_scales = w_scales;
+  p.pitch = (cols + 255) / 256 * 8;
+  p.out = out; p.ld = ld;
+  p.pairs = (reinterpret_cast<uintptr_t>(out) & 3u) == 0 && ld % 2 == 0 && n % 2 == 0;
+  p.status = status;
+  p.wait_limit = unif::gemm_wait_limit();
+  // at most one part-filled row tile per group beside the full ones
+  const int64_t most = ((int64_t)rows / fpp::kTN + (groups < rows ? groups : rows)) * p.ch_tiles;
+  if (most > 0x7fffffff) {
+    set_error("too many tiles: rows=%lld n=%d groups=%d", (long long)rows, n, groups);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  const int grid = (int)(most < sms ? most : sms);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  const bool gelu = activation == UNIF_MOE_ACTIVATION_GELU;
+  if (dtype == UNIF_MOE_F32)
+    e = gelu ? fpp::launch<float, true>(tmW, tmA, p, grid, s) : fpp::launch<float, false>(tmW, tmA, p, grid, s);
+  else
+    e = gelu ? fpp::launch<__nv_bfloat16, true>(tmW, tmA, p, grid, s)
+             : fpp::launch<__nv_bfloat16, false>(tmW, tmA, p, grid, s);
+  if (e != cudaSuccess) {
+    set_error("mxfp4 product: %s", cudaGetErrorString(e));
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+}  // extern "C"

@@ -12,10 +12,12 @@ from typing import NamedTuple, Optional
 
 import torch
 
-__all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize"]
+__all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize",
+           "mxfp4_product", "mxfp4_status"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
+_ACTIVATIONS = {"none": 0, "gelu": 1}
 _NORMS = {"none": 0, "layer": 1, "rms": 2}
 
 
@@ -27,7 +29,7 @@ class _BlockNormDesc(C.Structure):
 
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
            "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss",
-           "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize"]
+           "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize", "unif_moe_mxfp4_product"]
 
 
 def declare(L: C.CDLL) -> None:
@@ -44,6 +46,7 @@ def declare(L: C.CDLL) -> None:
                                         + [P] * 5 + [I64, P])
     L.unif_moe_mxfp4_quantize.argtypes = [P, I, I64, I, I64, P, P, P]
     L.unif_moe_mxfp4_dequantize.argtypes = [P, P, I64, I, P, I, I64, P]
+    L.unif_moe_mxfp4_product.argtypes = [P, P, I64, I, P, P, I, I, P, I, P, I, I64, P, P]
     for name in EXPORTS:
         getattr(L, name).restype = I64 if name.endswith("_workspace") else C.c_int
 
@@ -313,4 +316,56 @@ def mxfp4_dequantize(q: Mxfp4, dtype: str = "bf16", out: Optional[torch.Tensor] 
         po, ld = _rows(out, "out", rows, q.cols, DTYPES[dtype])
     _check(_lib().unif_moe_mxfp4_dequantize(pc, ps, rows, q.cols, po, _CODES[DTYPES[dtype]], ld,
                                             _stream(stream)))
+    return out
+
+
+_status_words = {}  # per device: set by a product whose kernel gave up a wait
+
+
+def _status_word(device: torch.device) -> torch.Tensor:
+    t = _status_words.get(device)
+    if t is None:
+        t = _status_words[device] = torch.zeros(1, dtype=torch.int32, device=device)
+    return t
+
+
+def mxfp4_status(device=None) -> int:
+    """Waits for the device and returns ERR_TIMEOUT (-5) if a product's kernel gave up a
+    wait since the last call (its output is incomplete), else 0."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None \
+        else torch.device(device)
+    torch.cuda.synchronize(device)
+    word = _status_word(device)
+    bad = int(word.item()) != 0
+    word.zero_()
+    return -5 if bad else 0
+
+
+def mxfp4_product(a: Mxfp4, w: Mxfp4, offsets: Optional[torch.Tensor] = None, *,
+                  activation: str = "none", dtype: str = "bf16",
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[r] = act(W_g a[r]) for the rows r of group g, [rows][n] ("bf16" or "f32").
+
+    a: rows in 4 bits; w: codes [groups][n][...] or [n][...] (one group); offsets
+    [groups + 1] int32 on the GPU: group g has the rows offsets[g] .. offsets[g + 1] - 1
+    (None with one group: all rows; e.g. the offsets of Layer.groups()). Rows of no group
+    are not written. activation: "none" or "gelu"."""
+    pa, psa, rows = _mxfp4(a, "a")
+    pw, psw, wn = _mxfp4(w, "w")
+    if a.cols != w.cols:
+        raise ValueError("a has %d columns, w %d" % (a.cols, w.cols))
+    n = w.codes.shape[-2] if w.codes.dim() > 1 else 1
+    groups = wn // n if n else 0
+    if offsets is None and groups != 1:
+        raise ValueError("offsets: needed with %d groups" % groups)
+    dev = a.codes.device
+    if out is None:
+        out = torch.empty(rows, n, dtype=DTYPES[dtype], device=dev)
+        po, ld = out.data_ptr(), n
+    else:
+        po, ld = _rows(out, "out", rows, n, DTYPES[dtype])
+    _check(_lib().unif_moe_mxfp4_product(
+        pa, psa, rows, a.cols, pw, psw, n, groups, _dense(offsets, "offsets", groups + 1, torch.int32),
+        _ACTIVATIONS[activation], po, _CODES[DTYPES[dtype]], ld, _status_word(dev).data_ptr(),
+        _stream(stream)))
     return out

@@ -1,0 +1,229 @@
+"""The product of MXFP4 rows with their group's MXFP4 weights (mxfp4_product) against
+64 bits: groups of every size (empty ones too), odd channel counts and columns,
+output types and strides, the layer's own group table; refusals.
+
+Tolerances. Products of elements and scales are exact; sums are fp32. With S the
+sum of the absolute values of a result's terms, each of the at most 64 steps of
+64 columns (4,096 columns) may lose 2^-22 S (sums of a step aligned and cut at fp32's
+last bits): 1.6e-5 S. f32 results: 2e-5 S. bf16 results: one rounding (2^-8 with a
+neighbour) more. GELU has a slope of at most 1.13, in bf16 output 3e-4 |v| more, in
+f32 output 2e-6 |v| + 2e-7 (erff, and 1 + erff where they cancel)."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+LEVELS = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def codes(rows, cols, g, lo=118, hi=130):
+    """Random rows in 4 bits, as the operator takes them."""
+    from paper_2608_10392_gb300 import Mxfp4
+    blocks = (cols + 31) // 32
+    c = torch.randint(0, 16, (rows, blocks * 32), generator=g, dtype=torch.uint8)
+    c[:, cols:] = 0
+    s = torch.zeros(rows, (blocks + 7) // 8 * 8, dtype=torch.uint8)
+    s[:, :blocks] = torch.randint(lo, hi, (rows, blocks), generator=g, dtype=torch.uint8)
+    return Mxfp4((c[:, 0::2] | c[:, 1::2] << 4).cuda(), s.cuda(), cols)
+
+
+def values(q):
+    """What the codes stand for, in 64 bits."""
+    c, s = q.codes.cpu(), q.scales.cpu()
+    c, s = c.reshape(-1, c.shape[-1]), s.reshape(-1, s.shape[-1])
+    table = torch.tensor(LEVELS + [-v for v in LEVELS], dtype=torch.float64)
+    v = torch.stack([table[(c & 15).long()], table[(c >> 4).long()]], -1).reshape(len(c), -1)
+    size = torch.exp2(s.double() - 127)
+    size[s == 255] = math.nan
+    return (v * size.repeat_interleave(32, 1)[:, :v.shape[1]])[:, :q.cols]
+
+
+def reference(a, w, n, offsets, act):
+    av, wv = values(a), values(w)
+    out = torch.full((len(av), n), math.nan, dtype=torch.float64)
+    size = torch.zeros_like(out)
+    for g in range(len(offsets) - 1):
+        lo, hi = offsets[g], offsets[g + 1]
+        m = wv[g * n:(g + 1) * n]
+        out[lo:hi] = av[lo:hi] @ m.T
+        size[lo:hi] = av[lo:hi].abs() @ m.abs().T
+    pre = out.clone()
+    if act == "gelu":
+        out = out * 0.5 * (1 + torch.erf(out / math.sqrt(2)))
+    return out, size, pre
+
+
+def check(sizes, n, cols, act="none", dtype="bf16", seed=0, out=None, offsets=None):
+    from paper_2608_10392_gb300 import Mxfp4, mxfp4_product, mxfp4_status
+    g = torch.Generator().manual_seed(seed)
+    rows, G = sum(sizes), len(sizes)
+    a, w = codes(rows, cols, g), codes(G * n, cols, g)
+    off = [0]
+    for s in sizes:
+        off.append(off[-1] + s)
+    wg = Mxfp4(w.codes.view(G, n, -1), w.scales.view(G, n, -1), cols)
+    # about unit results: rows come out around sqrt(cols) 2.4^2 2^-6
+    got = mxfp4_product(a, wg, torch.tensor(off, dtype=torch.int32, device="cuda"),
+                        activation=act, dtype=dtype, out=out)
+    assert mxfp4_status() == 0
+    want, size, pre = reference(a, w, n, off, act)
+    tol = 2e-5 * size
+    if act == "gelu":
+        tol = 1.13 * tol + (3e-4 * pre.abs() if dtype == "bf16" else 2e-6 * pre.abs() + 2e-7)
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * want.abs()
+    err = (got.double().cpu() - want).abs()
+    assert got.shape == want.shape and not torch.isnan(got).any()
+    assert (err <= tol).all(), (float((err / tol.clamp(min=1e-30)).max()), int((err > tol).sum()))
+    return a, wg, got
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes,n,cols", [
+    ([1], 1, 1), ([1], 128, 256), ([5], 64, 32), ([16], 130, 64), ([17], 257, 96),
+    ([31, 1, 0, 33], 128, 384), ([0, 0, 7, 0], 200, 100), ([192, 193, 191], 128, 768),
+    ([385, 12], 192, 2048), ([1000], 1000, 1024), ([127, 128, 129, 65, 64, 63], 96, 4096),
+    ([3] * 40, 72, 320), ([2, 0, 300], 33, 31), ([500], 7, 257)])
+def test_against_64_bits(sizes, n, cols, dtype):
+    check(sizes, n, cols, dtype=dtype, seed=n + cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gelu(dtype):
+    check([70, 0, 200, 3], 160, 640, act="gelu", dtype=dtype, seed=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [33, 272, 1024])
+def test_many_groups(G):
+    g = torch.Generator().manual_seed(G)
+    sizes = torch.randint(0, 9, (G,), generator=g).tolist()
+    check(sizes, 64, 128, seed=G)
+
+
+@pytest.mark.gpu
+def test_more_items_than_sms():
+    """Several items per CTA with few and many steps: the ring and the accumulators
+    come round, in groups of unequal size."""
+    check([700, 0, 1500, 9, 333], 1200, 512, seed=1, dtype="f32")
+    check([50] * 30, 1500, 300, seed=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,pad,shift", [(128, 8, 0), (96, 1, 0), (64, 7, 1), (63, 0, 0), (64, 2, 1)])
+def test_strided_output(n, pad, shift, dtype):
+    wide = torch.full((150, n + pad + shift), 3.0, device="cuda",
+                      dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    check([100, 50], n, 256, dtype=dtype, out=wide[:, shift:shift + n])
+    assert (wide[:, :shift] == 3).all() and (wide[:, shift + n:] == 3).all()
+
+
+@pytest.mark.gpu
+def test_scales_of_every_size():
+    """Scales from 2^-127 to 2^63 and the NaN byte: a NaN spoils its row of the output
+    (of its channel, in the weights) and nothing else."""
+    from paper_2608_10392_gb300 import Mxfp4, mxfp4_product
+    g = torch.Generator().manual_seed(3)
+    for lo, hi in ((0, 1), (60, 70), (180, 191)):
+        a, w = codes(40, 128, g, lo, hi), codes(64, 128, g, 127, 130)
+        got = mxfp4_product(a, w, dtype="f32").double().cpu()
+        av, wv = values(a), values(w)
+        assert ((got - av @ wv.T).abs() <= 2e-5 * (av.abs() @ wv.abs().T) + 2.0 ** -140).all()
+    a, w = codes(40, 128, g), codes(64, 128, g)
+    a.scales[7, 2], w.scales[9, 0] = 255, 255
+    got = mxfp4_product(a, w, dtype="f32").cpu()
+    nan = torch.zeros(40, 64, dtype=torch.bool)
+    nan[7], nan[:, 9] = True, True
+    assert torch.equal(torch.isnan(got), nan)
+
+
+@pytest.mark.gpu
+def test_offsets_that_leave_rows_out_or_are_out_of_range():
+    """Rows of no group keep what the output held; offsets beyond the rows, below 0 or
+    falling are taken as the documentation says, and nothing else is written."""
+    from paper_2608_10392_gb300 import Mxfp4, mxfp4_product
+    g = torch.Generator().manual_seed(4)
+    a, w = codes(60, 96, g), codes(3 * 40, 96, g)
+    wg = Mxfp4(w.codes.view(3, 40, -1), w.scales.view(3, 40, -1), 96)
+    av, wv = values(a), values(w).view(3, 40, 96)
+
+    def run(off, rows_of):
+        wide = torch.full((62, 40), 3.0, device="cuda")
+        mxfp4_product(a, wg, torch.tensor(off, dtype=torch.int32, device="cuda"), dtype="f32",
+                      out=wide[1:61])
+        want = torch.full((62, 40), 3.0, dtype=torch.float64)
+        for k, (lo, hi) in enumerate(rows_of):
+            want[1 + lo:1 + hi] = av[lo:hi] @ wv[k].T
+        assert ((wide.double().cpu() - want).abs() <= 1e-4 * (1 + want.abs())).all()
+
+    run([5, 10, 30, 50], [(5, 10), (10, 30), (30, 50)])
+    run([-100, 20, 20, 2000000000], [(0, 20), (20, 20), (20, 60)])
+    run([40, 60, 20, 30], [(40, 60), (0, 0), (20, 30)])
+    run([0, 60, 0, 60], [(0, 60), (0, 0), (0, 0)])  # the third group's rows are over the count
+
+
+@pytest.mark.gpu
+def test_repeatable_streams_and_no_rows():
+    from paper_2608_10392_gb300 import mxfp4_product
+    a, wg, got = check([300, 200], 256, 1024, seed=8)
+    off = torch.tensor([0, 300, 500], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = mxfp4_product(a, wg, off)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, again)
+    none = type(a)(a.codes[:0], a.scales[:0], a.cols)
+    assert mxfp4_product(none, wg, torch.zeros_like(off)).shape == (0, 256)
+
+
+@pytest.mark.gpu
+def test_graph_capture():
+    """The call can be captured and replayed."""
+    from paper_2608_10392_gb300 import mxfp4_product
+    a, wg, got = check([90, 30], 128, 512, seed=9)
+    off = torch.tensor([0, 90, 120], dtype=torch.int32, device="cuda")
+    out = torch.zeros_like(got)
+    mxfp4_product(a, wg, off, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mxfp4_product(a, wg, off, out=out)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, got)
+
+
+def test_refusals():
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    L = pkg.lib()
+    p = C.c_void_p(4096)
+
+    def call(**k):
+        v = dict(a=p, sa=p, rows=4, cols=64, w=p, sw=p, n=8, groups=2, off=p, act=0, out=p, dt=1, ld=8,
+                 status=p)
+        v.update(k)
+        return L.unif_moe_mxfp4_product(v["a"], v["sa"], v["rows"], v["cols"], v["w"], v["sw"], v["n"],
+                                        v["groups"], v["off"], v["act"], v["out"], v["dt"], v["ld"],
+                                        v["status"], None)
+
+    for k in (dict(a=None), dict(sa=None), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(w=None),
+              dict(sw=None), dict(n=0), dict(groups=0), dict(off=None), dict(act=2), dict(act=-1),
+              dict(out=None), dict(dt=2), dict(ld=7), dict(status=None), dict(a=C.c_void_p(4104)),
+              dict(sw=C.c_void_p(4100)), dict(n=1 << 30)):
+        assert call(**k) == -1, k
+    assert call(groups=1025) == -2
+    assert call(rows=0, a=None) == 0
+    z = torch.zeros(4, 32, dtype=torch.uint8)
+    s = torch.zeros(4, 8, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="a.codes"):
+        pkg.mxfp4_product(pkg.Mxfp4(z, s, 64), pkg.Mxfp4(z, s, 64))
+    with pytest.raises(ValueError, match="codes"):
+        pkg.mxfp4_product(pkg.Mxfp4(z, s, 65), pkg.Mxfp4(z, s, 64))
