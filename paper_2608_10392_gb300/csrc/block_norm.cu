@@ -257,6 +257,134 @@ __global__ void __launch_bounds__(GL ? kThreads : 1024)
   }
 }
 
+// ---- pairs of fp32 values (one instruction for two) ----
+struct F8 {
+  uint64_t p[kE / 2];
+};
+__device__ __forceinline__ uint64_t pk(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 upk(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ F8 pairs(const float (&v)[kE]) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < kE / 2; ++i) r.p[i] = pk(v[2 * i], v[2 * i + 1]);
+  return r;
+}
+__device__ __forceinline__ void singles(const F8& a, float (&v)[kE]) {
+#pragma unroll
+  for (int i = 0; i < kE / 2; ++i) {
+    const float2 f = upk(a.p[i]);
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ F8 zero8() {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < kE / 2; ++i) r.p[i] = 0ull;
+  return r;
+}
+
+// Sums over the threads of a row's group of two values for each of R rows, each
+// given as a pair of partial sums. N = 2 R values are halved among the lanes at
+// every exchange until a lane carries one: N - 1 + log2(lanes / N) shuffles. The
+// warps of a CTA meet in `red` (two buffers in turn), of which they read all
+// `W` warps' slots, those without a warp being 0.
+template <int GL, int R, int W>
+__device__ __forceinline__ void group_sums(const uint64_t (&s)[R][2], float* red, int& turn,
+                                           float2 (&out)[R]) {
+  constexpr int N = 2 * R, kLanes = GL ? GL : 32;
+  float v[N];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float2 a = upk(s[r][0]), b = upk(s[r][1]);
+    v[2 * r] = a.x + a.y;
+    v[2 * r + 1] = b.x + b.y;
+  }
+  // after the exchanges lane l carries value (l / (kLanes / N)) of its group
+  int half = kLanes / 2;
+#pragma unroll
+  for (int m = N / 2; m > 0; m >>= 1, half >>= 1) {
+    const bool upper = threadIdx.x & half;
+#pragma unroll
+    for (int i = 0; i < m; ++i)
+      v[i] = (upper ? v[m + i] : v[i]) + __shfl_xor_sync(0xffffffffu, upper ? v[i] : v[m + i], half);
+  }
+#pragma unroll
+  for (; half > 0; half >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], half);
+  constexpr int kStep = kLanes / N;
+  if (GL) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int at = (threadIdx.x & 31 & ~(kLanes - 1)) + 2 * r * kStep;
+      out[r].x = __shfl_sync(0xffffffffu, v[0], at);
+      out[r].y = __shfl_sync(0xffffffffu, v[0], at + kStep);
+    }
+    return;
+  }
+  float* buf = red + (turn & 1) * (N * W);
+  turn ^= 1;
+  if ((threadIdx.x & (kStep - 1)) == 0) buf[threadIdx.x / kStep] = v[0];  // warp w: N w ...
+  __syncthreads();
+  uint64_t t[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) t[r] = reinterpret_cast<const uint64_t*>(buf)[r];
+#pragma unroll
+  for (int w = 1; w < W; ++w)
+#pragma unroll
+    for (int r = 0; r < R; ++r) t[r] = add2(t[r], reinterpret_cast<const uint64_t*>(buf)[w * R + r]);
+#pragma unroll
+  for (int r = 0; r < R; ++r) out[r] = upk(t[r]);
+}
+
+// A parameter's values of this thread's columns: bf16 ones stay in registers from
+// row to row as they were read, fp32 ones are read again.
+template <typename TB, bool VEC>
+struct Param {
+  const TB* p = nullptr;
+  __device__ __forceinline__ void set(const TB* q, int, int, int) { p = q; }
+  __device__ __forceinline__ F8 get(int j, int n, int d) const {
+    if (!p) return zero8();
+    float v[kE];
+    load<VEC>(p, j, n, d, v);
+    return pairs(v);
+  }
+};
+template <>
+struct Param<__nv_bfloat16, true> {
+  uint4 raw = {0u, 0u, 0u, 0u};
+  __device__ __forceinline__ void set(const __nv_bfloat16* q, int j, int, int d) {
+    if (q && j * kE < d) raw = *reinterpret_cast<const uint4*>(q + j * kE);
+  }
+  __device__ __forceinline__ F8 get(int, int, int) const {
+    float v[kE];
+    unpack(raw, v);
+    return pairs(v);
+  }
+};
+
 // ---- backward ----
 // With o^ = (out - m) r, a = du w_pre:
 //   D = dout + r (a - mean(a) - o^ mean(a o^)),  dx = s D
@@ -290,152 +418,379 @@ struct BackwardArgs {
   int run;             // rows per CTA
 };
 
-// MT: most threads of a CTA (its registers: 128 a thread up to 512 threads).
+// A step of the backward takes R rows of a group at a time (two, where the threads
+// are few enough to have the registers); the next steps' rows are on their way to
+// shared memory meanwhile, in a ring of as many steps as the SM's shared memory
+// holds for 384 or 512 threads.
+__host__ __device__ constexpr int step_rows(bool vec, int mt) { return vec && mt <= 384 ? 2 : 1; }
+template <typename TX, typename TB>
+__host__ __device__ constexpr int row_bytes() {  // of a thread: dout, out, y, du
+  return 2 * kE * (int)(sizeof(TX) + sizeof(TB));
+}
+template <typename TX, typename TB>
+__host__ __device__ constexpr int ring_steps(int mt) {
+  return (mt <= 384 ? 512 : 384) / (step_rows(true, mt) * row_bytes<TX, TB>());
+}
+
+// This thread's eight values of a row, global to shared (16-byte planes of
+// `threads` slots each) and back: a thread reads only what it copied itself, so
+// waiting for its own copies is enough.
+template <typename T>
+__device__ __forceinline__ void ring_copy(uint4* slot, const T* p, int threads) {
+  constexpr int n = kE * sizeof(T) / 16;
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(slot + i * threads));
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst),
+                 "l"(reinterpret_cast<const uint4*>(p) + i)
+                 : "memory");
+  }
+}
+__device__ __forceinline__ void ring_read(const uint4* slot, int threads, const float*, float (&v)[kE]) {
+  const uint4 a = slot[0], b = slot[threads];
+  v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y);
+  v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+  v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y);
+  v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+}
+__device__ __forceinline__ void ring_read(const uint4* slot, int, const __nv_bfloat16*, float (&v)[kE]) {
+  unpack(slot[0], v);
+}
+
+// The rows of a CTA, `step` at a time. With `cut` a step never holds rows of two
+// gate rows, and `gate` is the one it is in.
+struct Walk {
+  int base, end, last, period, gate;
+  bool cut;
+  __device__ __forceinline__ bool more() const { return base < last; }
+  __device__ __forceinline__ void next(int step) {
+    base += step;
+    if (cut && base >= end) {
+      base = end;
+      end = min(last - end, period) + end;
+      ++gate;
+    }
+  }
+};
+
+// MT: most threads of a CTA. Two rows at a time take about 160 registers, so 12
+// warps are on an SM; with one row and 16 warps the chains of a row (two sums over
+// the CTA) left half of the issue slots empty.
 template <typename TX, typename TB, bool VEC, int GL, int MT>
-__global__ void __launch_bounds__(MT)
+__global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     backward_kernel(const BackwardArgs<TX, TB> a) {
-  __shared__ float red[2 * 2 * kMaxWarps];
-  __shared__ float fold[GL ? kThreads * kE : 1];
+  constexpr int R = step_rows(VEC, MT), W = MT / 32;
+  constexpr int kRing = ring_steps<TX, TB>(MT);
+  constexpr int kPX = kE * sizeof(TX) / 16, kPB = kE * sizeof(TB) / 16;  // planes of an array
+  constexpr int kPlanes = 2 * kPX + 2 * kPB;
+  constexpr int kGroups = GL ? MT / (GL ? GL : 1) : 1;
+  constexpr int kStep = kGroups * R;
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float red[GL ? 4 : 2 * 2 * R * W];
+  __shared__ float fold[GL ? MT * kE : 1];
+  const int threads = (int)blockDim.x;
   int turn = 0;
-  const int n = GL ? GL : (int)blockDim.x;
+  const int n = GL ? GL : threads;
   const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
-  const int groups = GL ? kThreads / (GL ? GL : 1) : 1;
   const int grp = GL ? (int)threadIdx.x / (GL ? GL : 1) : 0;
   const int d = a.d;
   const float inv = 1.f / (float)d;
+  const bool layer_pre = a.pre == UNIF_MOE_NORM_LAYER, layer_post = a.post == UNIF_MOE_NORM_LAYER;
+  const bool act = !VEC || j * kE < d;  // VEC: this thread has columns
   const int period = a.gate_rows ? a.gate_rows : a.T;
-  int r0, r1;
+  int r0, r1, gate0 = 0;
   if (a.pieces > 1) {  // piece of a gate row
-    const int g = blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
-    const long long g0 = (long long)g * period, g1 = min((long long)a.T, g0 + period);
+    gate0 = blockIdx.x / a.pieces;
+    const int p = blockIdx.x % a.pieces;
+    const long long g0 = (long long)gate0 * period, g1 = min((long long)a.T, g0 + period);
     r0 = (int)min(g1, g0 + (long long)p * a.run);
     r1 = (int)min(g1, (long long)r0 + a.run);
   } else {
     r0 = (int)min((long long)a.T, (long long)blockIdx.x * a.run);
     r1 = (int)min((long long)a.T, (long long)r0 + a.run);
+    gate0 = r0 / period;
   }
-  float s_wpost[kE], s_bpost[kE], s_wpre[kE], s_bpre[kE], s_gate[kE];
-#pragma unroll
-  for (int i = 0; i < kE; ++i)
-    s_wpost[i] = s_bpost[i] = s_wpre[i] = s_bpre[i] = s_gate[i] = 0.f;
+  const bool sum_gate = (a.wanted & 16) != 0;
+  const bool each = a.gate_rows == 1;  // a gate row for each row
+  const bool cut = a.gate && a.pieces == 1 && !each;
+  const bool with_y = a.dy || (a.wanted & 19);
+  F8 s_wpost = zero8(), s_bpost = zero8(), s_wpre = zero8(), s_bpre = zero8(), s_gate = zero8();
 
   // Adds the groups' sums of a column in order of the groups and stores them.
-  auto flush = [&](float (&s)[kE], float* to) {
+  auto flush = [&](F8& sum, float* to) {
+    float s[kE];
+    singles(sum, s);
     if (GL) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kE; ++i) fold[i * kThreads + threadIdx.x] = s[i];
+      for (int i = 0; i < kE; ++i) fold[i * MT + threadIdx.x] = s[i];
       __syncthreads();
       if (grp == 0)
 #pragma unroll
         for (int i = 0; i < kE; ++i) {
           float t = 0.f;
-          for (int g = 0; g < groups; ++g) t += fold[i * kThreads + g * n + j];
+          for (int g = 0; g < kGroups; ++g) t += fold[i * MT + g * n + j];
           s[i] = t;
         }
     }
     if (grp == 0) store<VEC>(to, j, n, d, s);
-#pragma unroll
-    for (int i = 0; i < kE; ++i) s[i] = 0.f;
+    sum = zero8();
   };
+  Param<TB, VEC> w_pre, w_post, b_post, gate;
+  w_pre.set(a.w_pre, j, n, d);
+  w_post.set(a.w_post, j, n, d);
+  b_post.set(a.b_post, j, n, d);
+  if (a.gate && !each) gate.set(a.gate + (long long)gate0 * d, j, n, d);
 
-  // the rows of one gate row after another (of all the CTA's rows, without a gate)
-  const bool sum_gate = (a.wanted & 16) != 0;
-  for (int g0 = r0; g0 < r1;) {
-    const int gi = g0 / period;
-    const int g1 = sum_gate && a.pieces == 1 ? (int)min((long long)r1, (long long)(gi + 1) * period) : r1;
-    for (int base = g0; base < g1; base += groups) {
-      const int row = base + grp;
-      const bool in = row < g1;
-      const bool valid = in && (!a.mask || a.mask[row]);
-      float D[kE], oh[kE], yn[kE];
+  // planes of dout, out, y, du of each row of a step
+  auto slot = [&](int k, int r) { return ring + (k * R + r) * (kPlanes * threads) + threadIdx.x; };
+  if (VEC && !act)  // threads without columns read zeros
+    for (int k = 0; k < kRing * R; ++k)
 #pragma unroll
-      for (int i = 0; i < kE; ++i) D[i] = oh[i] = yn[i] = 0.f;
-      if (valid && a.dout) load<VEC>(a.dout + row * a.ld_dout, j, n, d, D);
-      if (valid && a.y) load<VEC>(a.y + row * a.ld_y, j, n, d, yn);
-      if (a.pre) {
-        float w[kE], du[kE], s[2] = {0.f, 0.f};
+      for (int i = 0; i < kPlanes; ++i) slot(0, k)[i * threads] = make_uint4(0u, 0u, 0u, 0u);
+  if (!GL && threadIdx.x < 2 * 2 * R * W) red[threadIdx.x] = 0.f;
+  if (!GL) __syncthreads();
+
+  Walk at;
+  at.base = r0; at.last = r1; at.period = period; at.gate = gate0; at.cut = cut;
+  at.end = cut ? (int)min((long long)r1, (long long)(gate0 + 1) * period) : r1;
+  Walk ahead = at;
+  auto row_of = [&](const Walk& w, int r) { return w.base + r * kGroups + grp; };
+  // bit r: row r of the step is there and no padding
+  auto validity = [&](const Walk& w) {
+    uint32_t v = 0;
 #pragma unroll
-        for (int i = 0; i < kE; ++i) du[i] = 0.f;
-        float m = 0.f, r = 0.f;
-        if (valid) {
-          load<VEC>(a.o + row * a.ld_o, j, n, d, oh);
-          load<VEC>(a.du + row * a.ld_du, j, n, d, du);
-          m = a.pre == UNIF_MOE_NORM_LAYER ? a.m_pre[row] : 0.f;
-          r = a.r_pre[row];
-        }
-        load<VEC>(a.w_pre, j, n, d, w);
+    for (int r = 0; r < R; ++r) {
+      const int row = row_of(w, r);
+      if (w.more() && row < w.end && (!a.mask || a.mask[row])) v |= 1u << r;
+    }
+    return v;
+  };
+  uint32_t valids = 0;  // R bits for each step from the current one on
+  uint32_t next_valid = VEC ? validity(ahead) : 0u;
+  int put = 0, get = 0;
+  auto fetch = [&](int k) {  // the step `ahead` stands at, the k-th to be worked on
+    if (ahead.more()) {
+      valids |= next_valid << (k * R);
+      if (act)
 #pragma unroll
-        for (int i = 0; i < kE; ++i) {
-          oh[i] = column<VEC>(j, n, i) < d ? (oh[i] - m) * r : 0.f;
-          s_wpre[i] = fmaf(du[i], oh[i], s_wpre[i]);
-          s_bpre[i] += du[i];
-          w[i] *= du[i];
-          s[0] += w[i];
-          s[1] = fmaf(w[i], oh[i], s[1]);
-        }
-        group_sum<GL>(s, red, turn);
-        const float c0 = a.pre == UNIF_MOE_NORM_LAYER ? s[0] * inv : 0.f, c1 = s[1] * inv;
-#pragma unroll
-        for (int i = 0; i < kE; ++i) D[i] = fmaf(r, w[i] - c0 - oh[i] * c1, D[i]);
-      }
-      if (a.dx && in) {
-        float t[kE];
-#pragma unroll
-        for (int i = 0; i < kE; ++i) t[i] = valid ? a.scale * D[i] : 0.f;
-        store<VEC>(a.dx + row * a.ld_dx, j, n, d, t);
-      }
-      if (a.dy || sum_gate) {
-        float w[kE], m = 0.f, r = 1.f;
-        if (a.post) {
-          if (valid) {
-            m = a.post == UNIF_MOE_NORM_LAYER ? a.m_post[row] : 0.f;
-            r = a.r_post[row];
+        for (int r = 0; r < R; ++r)
+          if (next_valid >> r & 1u) {
+            const long long row = row_of(ahead, r);
+            uint4* to = slot(put, r);
+            if (a.dout) ring_copy(to, a.dout + row * a.ld_dout + j * kE, threads);
+            if (a.pre) {
+              ring_copy(to + kPX * threads, a.o + row * a.ld_o + j * kE, threads);
+              ring_copy(to + (2 * kPX + kPB) * threads, a.du + row * a.ld_du + j * kE, threads);
+            }
+            if (with_y) ring_copy(to + 2 * kPX * threads, a.y + row * a.ld_y + j * kE, threads);
           }
-          load<VEC>(a.w_post, j, n, d, w);
+      ahead.next(kStep);
+      next_valid = validity(ahead);
+      if (++put == kRing) put = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (VEC)
 #pragma unroll
-          for (int i = 0; i < kE; ++i) yn[i] = valid && column<VEC>(j, n, i) < d ? (yn[i] - m) * r : 0.f;
-        }
-        if (sum_gate) {
-          float b[kE];
+    for (int k = 0; k < kRing - 1; ++k) fetch(k);
+
+  // the statistics of the step that `at` stands at
+  float mp[R], rp[R], my[R], ry[R];
+  auto statistics = [&](const Walk& w) {
 #pragma unroll
-          for (int i = 0; i < kE; ++i) b[i] = 0.f;
-          if (a.post && a.b_post) load<VEC>(a.b_post, j, n, d, b);
-#pragma unroll
-          for (int i = 0; i < kE; ++i)
-            s_gate[i] = fmaf(D[i], a.post ? fmaf(w[i], yn[i], b[i]) : yn[i], s_gate[i]);
-        }
-        if (a.gate && in) {
-          float g[kE];
-          load<VEC>(a.gate + (long long)(a.gate_rows ? row / period : 0) * d, j, n, d, g);
-#pragma unroll
-          for (int i = 0; i < kE; ++i) D[i] *= g[i];
-        }
-        if (a.post) {
-          float s[2] = {0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < kE; ++i) {
-            s_wpost[i] = fmaf(D[i], yn[i], s_wpost[i]);
-            s_bpost[i] += D[i];
-            D[i] *= w[i];
-            s[0] += D[i];
-            s[1] = fmaf(D[i], yn[i], s[1]);
-          }
-          group_sum<GL>(s, red, turn);
-          const float c0 = a.post == UNIF_MOE_NORM_LAYER ? s[0] * inv : 0.f, c1 = s[1] * inv;
-#pragma unroll
-          for (int i = 0; i < kE; ++i) D[i] = r * (D[i] - c0 - yn[i] * c1);
-        }
-        if (a.dy && in) {
-          if (!valid)
-#pragma unroll
-            for (int i = 0; i < kE; ++i) D[i] = 0.f;
-          store<VEC>(a.dy + row * a.ld_dy, j, n, d, D);
-        }
+    for (int r = 0; r < R; ++r) {
+      const int row = row_of(w, r);
+      mp[r] = rp[r] = my[r] = ry[r] = 0.f;
+      if (w.more() && row < w.end) {
+        if (layer_pre) mp[r] = a.m_pre[row];
+        if (a.pre) rp[r] = a.r_pre[row];
+        if (layer_post) my[r] = a.m_post[row];
+        if (a.post) ry[r] = a.r_post[row];
       }
     }
-    if (sum_gate && a.pieces == 1) flush(s_gate, a.d_gate + (long long)gi * d);
-    g0 = g1;
+  };
+  statistics(at);
+  while (at.more()) {
+    const int gate_row = at.gate;
+    const Walk here = at;
+    uint32_t valid;
+    if (VEC) {
+      fetch(kRing - 1);
+      valid = valids & ((1u << R) - 1u);
+      valids >>= R;
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+    } else {
+      valid = validity(at);
+    }
+    const int ring_at = get;
+    if (++get == kRing) get = 0;
+    float m0[R], q0[R], m1[R], q1[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool v = valid >> r & 1u;
+      q0[r] = v ? rp[r] : 0.f;
+      q1[r] = v ? ry[r] : 0.f;
+      m0[r] = -mp[r] * q0[r];
+      m1[r] = -my[r] * q1[r];
+    }
+    at.next(kStep);
+    statistics(at);
+    const bool ends = cut && at.gate != here.gate;  // the last step of a gate row
+    const uint32_t present = (row_of(here, R - 1) < here.end ? 1u << (R - 1) : 0u) |
+                             (row_of(here, 0) < here.end ? 1u : 0u);
+    if (GL || valid) {  // (without groups in warps the whole CTA agrees)
+      auto values = [&](auto* base, long long ld, int plane, int r) {
+        float v[kE];
+        const bool ok = valid >> r & 1u;
+        if (VEC) {
+          ring_read(slot(ring_at, r) + plane * threads, threads, base, v);
+#pragma unroll
+          for (int i = 0; i < kE; ++i) v[i] = ok ? v[i] : 0.f;
+        } else {
+#pragma unroll
+          for (int i = 0; i < kE; ++i) v[i] = 0.f;
+          if (ok) load<false>(base + row_of(here, r) * ld, j, n, d, v);
+        }
+        return pairs(v);
+      };
+      F8 D[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) D[r] = a.dout ? values(a.dout, a.ld_dout, 0, r) : zero8();
+      // columns past d hold 0 in every parameter and input, so that no sum sees what
+      // the rest of the arithmetic makes of them
+      if (a.pre) {
+        F8 oh[R], w[R];
+        uint64_t s[R][2];
+        float2 c[R];
+        const F8 wp = w_pre.get(j, n, d);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          oh[r] = values(a.o, a.ld_o, kPX, r);
+          w[r] = values(a.du, a.ld_du, 2 * kPX + kPB, r);
+          const uint64_t q = pk(q0[r], q0[r]), mq = pk(m0[r], m0[r]);
+          s[r][0] = s[r][1] = 0ull;
+#pragma unroll
+          for (int i = 0; i < kE / 2; ++i) {
+            oh[r].p[i] = fma2(oh[r].p[i], q, mq);
+            s_wpre.p[i] = fma2(w[r].p[i], oh[r].p[i], s_wpre.p[i]);
+            s_bpre.p[i] = add2(s_bpre.p[i], w[r].p[i]);
+            w[r].p[i] = mul2(wp.p[i], w[r].p[i]);
+            s[r][0] = add2(s[r][0], w[r].p[i]);
+            s[r][1] = fma2(w[r].p[i], oh[r].p[i], s[r][1]);
+          }
+        }
+        group_sums<GL, R, W>(s, red, turn, c);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float c0 = layer_pre ? -c[r].x * inv * q0[r] : 0.f, c1 = -c[r].y * inv * q0[r];
+          const uint64_t q = pk(q0[r], q0[r]), k0 = pk(c0, c0), k1 = pk(c1, c1);
+#pragma unroll
+          for (int i = 0; i < kE / 2; ++i)
+            D[r].p[i] = add2(D[r].p[i], fma2(w[r].p[i], q, fma2(oh[r].p[i], k1, k0)));
+        }
+      }
+      if (a.dx) {
+        const uint64_t sc = pk(a.scale, a.scale);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float t[kE];
+          F8 x;
+#pragma unroll
+          for (int i = 0; i < kE / 2; ++i) x.p[i] = mul2(D[r].p[i], sc);
+          singles(x, t);
+          if (present >> r & 1u) store<VEC>(a.dx + row_of(here, r) * a.ld_dx, j, n, d, t);
+        }
+      }
+      if (with_y) {
+        F8 yn[R], w;
+        if (a.post) w = w_post.get(j, n, d);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          yn[r] = values(a.y, a.ld_y, 2 * kPX, r);
+          if (a.post) {
+            const uint64_t q = pk(q1[r], q1[r]), mq = pk(m1[r], m1[r]);
+#pragma unroll
+            for (int i = 0; i < kE / 2; ++i) yn[r].p[i] = fma2(yn[r].p[i], q, mq);
+          }
+        }
+        if (sum_gate) {
+          F8 b = zero8();
+          if (a.post && a.b_post) b = b_post.get(j, n, d);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            F8 z = yn[r];
+            if (a.post)
+#pragma unroll
+              for (int i = 0; i < kE / 2; ++i) z.p[i] = fma2(w.p[i], yn[r].p[i], b.p[i]);
+            if (each) {
+              float t[kE];
+#pragma unroll
+              for (int i = 0; i < kE / 2; ++i) z.p[i] = mul2(D[r].p[i], z.p[i]);
+              singles(z, t);
+              if (present >> r & 1u) store<VEC>(a.d_gate + (long long)row_of(here, r) * d, j, n, d, t);
+            } else {
+#pragma unroll
+              for (int i = 0; i < kE / 2; ++i) s_gate.p[i] = fma2(D[r].p[i], z.p[i], s_gate.p[i]);
+            }
+          }
+        }
+        if (a.gate)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (each && (present >> r & 1u)) gate.set(a.gate + (long long)row_of(here, r) * d, j, n, d);
+            const F8 t = gate.get(j, n, d);
+#pragma unroll
+            for (int i = 0; i < kE / 2; ++i) D[r].p[i] = mul2(D[r].p[i], t.p[i]);
+          }
+        if (a.post) {
+          uint64_t s[R][2];
+          float2 c[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            s[r][0] = s[r][1] = 0ull;
+#pragma unroll
+            for (int i = 0; i < kE / 2; ++i) {
+              s_wpost.p[i] = fma2(D[r].p[i], yn[r].p[i], s_wpost.p[i]);
+              s_bpost.p[i] = add2(s_bpost.p[i], D[r].p[i]);
+              D[r].p[i] = mul2(D[r].p[i], w.p[i]);
+              s[r][0] = add2(s[r][0], D[r].p[i]);
+              s[r][1] = fma2(D[r].p[i], yn[r].p[i], s[r][1]);
+            }
+          }
+          group_sums<GL, R, W>(s, red, turn, c);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float c0 = layer_post ? -c[r].x * inv * q1[r] : 0.f, c1 = -c[r].y * inv * q1[r];
+            const uint64_t q = pk(q1[r], q1[r]), k0 = pk(c0, c0), k1 = pk(c1, c1);
+#pragma unroll
+            for (int i = 0; i < kE / 2; ++i) D[r].p[i] = fma2(D[r].p[i], q, fma2(yn[r].p[i], k1, k0));
+          }
+        }
+        if (a.dy)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            float t[kE];
+            singles(D[r], t);
+            if (present >> r & 1u) store<VEC>(a.dy + row_of(here, r) * a.ld_dy, j, n, d, t);
+          }
+      }
+    }
+    // padding gives 0 (whatever the arithmetic made of zero rows, NaN parameters included)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if ((present & ~valid) >> r & 1u) {
+        float t[kE];
+#pragma unroll
+        for (int i = 0; i < kE; ++i) t[i] = 0.f;
+        if (a.dx) store<VEC>(a.dx + row_of(here, r) * a.ld_dx, j, n, d, t);
+        if (a.dy) store<VEC>(a.dy + row_of(here, r) * a.ld_dy, j, n, d, t);
+        if (sum_gate && each) store<VEC>(a.d_gate + (long long)row_of(here, r) * d, j, n, d, t);
+      }
+    if (ends) {
+      if (sum_gate) flush(s_gate, a.d_gate + (long long)gate_row * d);
+      if (a.gate && at.more()) gate.set(a.gate + (long long)at.gate * d, j, n, d);
+    }
   }
   float* part = a.part + (long long)blockIdx.x * 4 * d;
   if (a.wanted & 1) flush(s_wpost, part);
@@ -446,46 +801,48 @@ __global__ void __launch_bounds__(MT)
 }
 
 struct FinishArgs {
-  int d, ctas, pieces;
+  int d, ctas, pieces, gates;  // gates: gate rows whose pieces are added here
+  int sums;                    // 4, and the gate row where there is one: sums over all CTAs
   const float* part;
   const float* part_gate;
   float* to[4];   // dw_post, db_post, dw_pre, db_pre
   float* d_gate;
 };
 
-// One CTA per 32 columns of one sum: 32 threads per column add every 32nd
-// CTA's share, a tree adds those.
+// The first CTAs: 32 columns of one of the sums over all CTAs each, 32 threads per
+// column add every 32nd CTA's share and a tree adds those. The others, with several
+// gate rows: a thread per column of a gate row adds its pieces.
 __global__ void __launch_bounds__(1024) finish_kernel(const FinishArgs a) {
   __shared__ float t[32][33];
   grid_dep_wait();
-  const int c = blockIdx.x * 32 + threadIdx.x, k = blockIdx.y;
-  const float* from;
-  float* to;
-  long long step;
-  int count;
-  if (k < 4) {
-    to = a.to[k];
+  const int tiles = (a.d + 31) / 32;
+  if ((int)blockIdx.x < a.sums * tiles) {
+    const int k = blockIdx.x / tiles, c0 = (blockIdx.x - k * tiles) * 32;
+    float* to = k == 0 ? a.to[0] : k == 1 ? a.to[1] : k == 2 ? a.to[2] : k == 3 ? a.to[3] : a.d_gate;
     if (!to) return;
-    from = a.part + (long long)k * a.d;
-    step = 4ll * a.d;
-    count = a.ctas;
-  } else {
-    to = a.d_gate + (long long)(k - 4) * a.d;
-    from = a.part_gate + (long long)(k - 4) * a.pieces * a.d;
-    step = a.d;
-    count = a.pieces;
-  }
-  float s = 0.f;
-  if (c < a.d)
-#pragma unroll 4
-    for (int i = threadIdx.y; i < count; i += 32) s += from[i * step + c];
-  t[threadIdx.y][threadIdx.x] = s;
-  __syncthreads();
-  s = t[threadIdx.x][threadIdx.y];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = c0 + x;
+    const float* from = k < 4 ? a.part + (long long)k * a.d + c : a.part_gate + c;
+    const long long step = k < 4 ? 4ll * a.d : a.d;
+    float s = 0.f;
+    if (c < a.d)
+#pragma unroll 8
+      for (int i = y; i < a.ctas; i += 32) s += from[i * step];
+    t[y][x] = s;
+    __syncthreads();
+    s = t[x][y];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const int cc = blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x == 0 && cc < a.d) to[cc] = s;
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (x == 0 && c0 + y < a.d) to[c0 + y] = s;
+    return;
+  }
+  const long long i = (long long)(blockIdx.x - a.sums * tiles) * 1024 + threadIdx.x;
+  const int g = (int)(i / a.d), c = (int)(i - (long long)g * a.d);
+  if (g >= a.gates) return;
+  const float* from = a.part_gate + (long long)g * a.pieces * a.d + c;
+  float s = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < a.pieces; ++k) s += from[(long long)k * a.d];
+  a.d_gate[i] = s;
 }
 
 // ---- host ----
@@ -505,12 +862,12 @@ struct Plan {
 Plan plan_backward(const unif_moe_block_norm* p, bool gate, int sms) {
   const int warps = cta_threads(p->width) / 32;
   const int groups = group_lanes(p->width) ? kThreads / group_lanes(p->width) : 1;
-  const int slots = sms * (warps >= 16 ? 1 : 16 / warps);
+  const int slots = sms * (warps > 12 ? 1 : 12 / warps);
   const long long T = p->tokens;
   const long long period = gate && p->gate_rows && p->gate_rows < T ? p->gate_rows : T;
   const long long G = (T + period - 1) / period;
   // a run has at least a few rows for each group, so that its column sums are worth writing
-  const long long least = 4ll * groups;
+  const long long least = 8ll * groups;
   long long want = (T + slots - 1) / slots;
   if (want < least) want = least;
   Plan r;
@@ -547,20 +904,30 @@ cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+template <typename TX, typename TB, bool VEC, int GL, int MT>
+cudaError_t launch_bwd_as(const BackwardArgs<TX, TB>& a, int ctas, int threads, cudaStream_t s) {
+  const int smem = VEC ? ring_steps<TX, TB>(MT) * step_rows(true, MT) * row_bytes<TX, TB>() * threads : 0;
+  if (smem > 40 * 1024) {  // with the static part above what needs no leave
+    const cudaError_t e = allow_smem_once(backward_kernel<TX, TB, VEC, GL, MT>, smem);
+    if (e != cudaSuccess) return e;
+  }
+  backward_kernel<TX, TB, VEC, GL, MT><<<ctas, threads, smem, s>>>(a);
+  return cudaGetLastError();
+}
+
 template <typename TX, typename TB, bool VEC>
 cudaError_t launch_bwd(const BackwardArgs<TX, TB>& a, int ctas, cudaStream_t s) {
   const int threads = cta_threads(a.d);
   switch (group_lanes(a.d)) {
-    case 8: backward_kernel<TX, TB, VEC, 8, kThreads><<<ctas, threads, 0, s>>>(a); break;
-    case 16: backward_kernel<TX, TB, VEC, 16, kThreads><<<ctas, threads, 0, s>>>(a); break;
-    case 32: backward_kernel<TX, TB, VEC, 32, kThreads><<<ctas, threads, 0, s>>>(a); break;
-    default:
-      if (threads <= 256) backward_kernel<TX, TB, VEC, 0, 256><<<ctas, threads, 0, s>>>(a);
-      else if (threads <= 512) backward_kernel<TX, TB, VEC, 0, 512><<<ctas, threads, 0, s>>>(a);
-      else backward_kernel<TX, TB, VEC, 0, 1024><<<ctas, threads, 0, s>>>(a);
-      break;
+    case 8: return launch_bwd_as<TX, TB, VEC, 8, kThreads>(a, ctas, threads, s);
+    case 16: return launch_bwd_as<TX, TB, VEC, 16, kThreads>(a, ctas, threads, s);
+    case 32: return launch_bwd_as<TX, TB, VEC, 32, kThreads>(a, ctas, threads, s);
   }
-  return cudaGetLastError();
+  if (threads <= 128) return launch_bwd_as<TX, TB, VEC, 0, 128>(a, ctas, threads, s);
+  if (threads <= 384) return launch_bwd_as<TX, TB, VEC, 0, 384>(a, ctas, threads, s);
+  if (threads <= 512) return launch_bwd_as<TX, TB, VEC, 0, 512>(a, ctas, threads, s);
+  // still wider rows: no room for a ring beside 1,024 threads
+  return launch_bwd_as<TX, TB, false, 0, 1024>(a, ctas, threads, s);
 }
 
 int check_desc(const unif_moe_block_norm* p) {
@@ -653,10 +1020,13 @@ cudaError_t backward_as(const unif_moe_block_norm* p, const Plan& pl, const void
                       : launch_bwd<TX, TB, false>(a, pl.ctas, s);
   const bool gates = d_gate && pl.pieces > 1;
   if (e != cudaSuccess || !((a.wanted & 15) || gates)) return e;
-  FinishArgs f{a.d, pl.ctas, pl.pieces, a.part, a.part_gate, {to[0], to[1], to[2], to[3]}, d_gate};
-  return launch_dependent(finish_kernel,
-                          dim3((a.d + 31) / 32, 4 + (gates ? pl.ctas / pl.pieces : 0)),
-                          dim3(32, 32), 0, s, f);
+  const int gate_rows = gates ? pl.ctas / pl.pieces : 0;
+  const int sums = gate_rows == 1 ? 5 : 4;
+  FinishArgs f{a.d, pl.ctas, pl.pieces, gate_rows, sums, a.part, a.part_gate,
+               {to[0], to[1], to[2], to[3]}, d_gate};
+  const long long more = gate_rows > 1 ? ((long long)gate_rows * a.d + 1023) / 1024 : 0;
+  return launch_dependent(finish_kernel, dim3((unsigned)(sums * ((a.d + 31) / 32) + more)), dim3(1024),
+                          0, s, f);
 }
 
 }  // namespace norm

@@ -398,7 +398,7 @@ template <typename TO, bool GELU>
 cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmA, const Params& p, int grid,
                    cudaStream_t s) {
   const uint32_t smem = smem_bytes(p.G);
-  cudaError_t e = allow_smem(product_kernel<TO, GELU>, smem);
+  cudaError_t e = allow_smem_once(product_kernel<TO, GELU>, smem);
   if (e != cudaSuccess) return e;
   return launch_dependent(product_kernel<TO, GELU>, dim3(grid), dim3(kThreads), smem, s, tmW, tmA, p);
 }

@@ -248,6 +248,13 @@ template <typename... P>
 cudaError_t allow_smem(void (*fn)(P...), size_t need) {
   return allow_smem(reinterpret_cast<const void*>(fn), need);
 }
+// The same for calls without a handle, which would ask at every launch: the
+// device is asked once per kernel and device.
+cudaError_t allow_smem_once(const void* fn, size_t need);
+template <typename... P>
+cudaError_t allow_smem_once(void (*fn)(P...), size_t need) {
+  return allow_smem_once(reinterpret_cast<const void*>(fn), need);
+}
 
 // Load time.
 cudaError_t launch_prototypes(unif_moe_layer* L, const void* w_router, const float* bias,

@@ -11,7 +11,10 @@
 #include <string.h>
 #include <vector>
 
+#include <mutex>
 #include <new>
+#include <set>
+#include <utility>
 
 #include "internal.cuh"
 
@@ -37,6 +40,19 @@ cudaError_t allow_smem(const void* fn, size_t need) {
   most -= (int)at.sharedSizeBytes;
   if (most < 0 || need > (size_t)most) return cudaErrorInvalidValue;
   return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+
+cudaError_t allow_smem_once(const void* fn, size_t need) {
+  static std::mutex lock;
+  static std::set<std::pair<const void*, int>> done;
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> hold(lock);
+  if (done.count({fn, dev})) return cudaSuccess;
+  const cudaError_t r = allow_smem(fn, need);
+  if (r == cudaSuccess) done.insert({fn, dev});
+  return r;
 }
 
 int sm_count(int* n) {
