@@ -392,8 +392,8 @@ struct Param<__nv_bfloat16, true> {
 // (no mean(a), mean(f) terms for rms), and the column sums
 //   dw_pre = sum du o^, db_pre = sum du, dw_post = sum e yn, db_post = sum e,
 //   dg = sum D z over the rows of a gate row.
-// A CTA walks a run of consecutive rows that share a gate row (or holds whole
-// gate rows), keeps the column sums of its columns in registers and writes
+// A CTA walks rows that share a gate row, every pieces-th chunk of them so that
+// padding falls on all CTAs alike, or a run of whole gate rows. It keeps the column sums of its columns in registers and writes
 // them once; finish_kernel adds the CTAs' sums in a fixed order, so results
 // do not change from run to run.
 template <typename TX, typename TB>
@@ -415,7 +415,7 @@ struct BackwardArgs {
   float* part_gate;    // [CTAs][d] where pieces > 1
   int wanted;          // bits 0-3: the sums of part; bit 4: dg
   int pieces;          // CTAs per gate row, or 1
-  int run;             // rows per CTA
+  int run;             // rows per CTA (pieces == 1), or of a chunk
 };
 
 // A step of the backward takes R rows of a group at a time (two, where the threads
@@ -457,18 +457,18 @@ __device__ __forceinline__ void ring_read(const uint4* slot, int, const __nv_bfl
   unpack(slot[0], v);
 }
 
-// The rows of a CTA, `step` at a time. With `cut` a step never holds rows of two
-// gate rows, and `gate` is the one it is in.
+// The rows of a CTA, `step` at a time: chunks of consecutive rows `skip` rows apart,
+// or, with `cut`, one gate row after another (`gate` is the one it is in).
 struct Walk {
-  int base, end, last, period, gate;
+  int base, end, last, size, skip, gate;
   bool cut;
   __device__ __forceinline__ bool more() const { return base < last; }
   __device__ __forceinline__ void next(int step) {
     base += step;
-    if (cut && base >= end) {
-      base = end;
-      end = min(last - end, period) + end;
-      ++gate;
+    if (base >= end) {
+      base = last - end > skip ? end + skip : last;
+      end = min(last - base, size) + base;
+      if (cut) ++gate;
     }
   }
 };
@@ -498,21 +498,26 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   const bool layer_pre = a.pre == UNIF_MOE_NORM_LAYER, layer_post = a.post == UNIF_MOE_NORM_LAYER;
   const bool act = !VEC || j * kE < d;  // VEC: this thread has columns
   const int period = a.gate_rows ? a.gate_rows : a.T;
-  int r0, r1, gate0 = 0;
-  if (a.pieces > 1) {  // piece of a gate row
-    gate0 = blockIdx.x / a.pieces;
-    const int p = blockIdx.x % a.pieces;
-    const long long g0 = (long long)gate0 * period, g1 = min((long long)a.T, g0 + period);
-    r0 = (int)min(g1, g0 + (long long)p * a.run);
-    r1 = (int)min(g1, (long long)r0 + a.run);
-  } else {
-    r0 = (int)min((long long)a.T, (long long)blockIdx.x * a.run);
-    r1 = (int)min((long long)a.T, (long long)r0 + a.run);
-    gate0 = r0 / period;
-  }
   const bool sum_gate = (a.wanted & 16) != 0;
   const bool each = a.gate_rows == 1;  // a gate row for each row
   const bool cut = a.gate && a.pieces == 1 && !each;
+  Walk at;
+  at.cut = cut;
+  if (a.pieces > 1) {  // every pieces-th chunk of a gate row
+    at.gate = blockIdx.x / a.pieces;
+    const int p = blockIdx.x % a.pieces, g0 = at.gate * period;
+    at.last = min(a.T - g0, period) + g0;
+    at.size = a.run;
+    at.skip = (a.pieces - 1) * a.run;
+    at.base = (int)min((long long)at.last, g0 + (long long)p * a.run);
+  } else {
+    at.base = (int)min((long long)a.T, (long long)blockIdx.x * a.run);
+    at.last = min(a.T - at.base, a.run) + at.base;
+    at.gate = at.base / period;
+    at.size = cut ? period : a.run;
+    at.skip = 0;
+  }
+  at.end = min(at.last - at.base, at.size) + at.base;
   const bool with_y = a.dy || (a.wanted & 19);
   F8 s_wpost = zero8(), s_bpost = zero8(), s_wpre = zero8(), s_bpre = zero8(), s_gate = zero8();
 
@@ -540,7 +545,7 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   w_pre.set(a.w_pre, j, n, d);
   w_post.set(a.w_post, j, n, d);
   b_post.set(a.b_post, j, n, d);
-  if (a.gate && !each) gate.set(a.gate + (long long)gate0 * d, j, n, d);
+  if (a.gate && !each) gate.set(a.gate + (long long)at.gate * d, j, n, d);
 
   // planes of dout, out, y, du of each row of a step
   auto slot = [&](int k, int r) { return ring + (k * R + r) * (kPlanes * threads) + threadIdx.x; };
@@ -551,9 +556,6 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   if (!GL && threadIdx.x < 2 * 2 * R * W) red[threadIdx.x] = 0.f;
   if (!GL) __syncthreads();
 
-  Walk at;
-  at.base = r0; at.last = r1; at.period = period; at.gate = gate0; at.cut = cut;
-  at.end = cut ? (int)min((long long)r1, (long long)(gate0 + 1) * period) : r1;
   Walk ahead = at;
   auto row_of = [&](const Walk& w, int r) { return w.base + r * kGroups + grp; };
   // bit r: row r of the step is there and no padding
@@ -572,12 +574,12 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   auto fetch = [&](int k) {  // the step `ahead` stands at, the k-th to be worked on
     if (ahead.more()) {
       valids |= next_valid << (k * R);
-      if (act)
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-          if (next_valid >> r & 1u) {
+      for (int r = 0; r < R; ++r) {
+        uint4* to = slot(put, r);
+        if (next_valid >> r & 1u) {
+          if (act) {
             const long long row = row_of(ahead, r);
-            uint4* to = slot(put, r);
             if (a.dout) ring_copy(to, a.dout + row * a.ld_dout + j * kE, threads);
             if (a.pre) {
               ring_copy(to + kPX * threads, a.o + row * a.ld_o + j * kE, threads);
@@ -585,6 +587,11 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
             }
             if (with_y) ring_copy(to + 2 * kPX * threads, a.y + row * a.ld_y + j * kE, threads);
           }
+        } else if (GL || next_valid) {  // padding beside rows that count
+#pragma unroll
+          for (int i = 0; i < kPlanes; ++i) to[i * threads] = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
       ahead.next(kStep);
       next_valid = validity(ahead);
       if (++put == kRing) put = 0;
@@ -626,14 +633,15 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     const int ring_at = get;
     if (++get == kRing) get = 0;
     float m0[R], q0[R], m1[R], q1[R];
+    if (GL || valid)
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool v = valid >> r & 1u;
-      q0[r] = v ? rp[r] : 0.f;
-      q1[r] = v ? ry[r] : 0.f;
-      m0[r] = -mp[r] * q0[r];
-      m1[r] = -my[r] * q1[r];
-    }
+      for (int r = 0; r < R; ++r) {
+        const bool v = valid >> r & 1u;
+        q0[r] = v ? rp[r] : 0.f;
+        q1[r] = v ? ry[r] : 0.f;
+        m0[r] = v ? -mp[r] * q0[r] : 0.f;
+        m1[r] = v ? -my[r] * q1[r] : 0.f;
+      }
     at.next(kStep);
     statistics(at);
     const bool ends = cut && at.gate != here.gate;  // the last step of a gate row
@@ -642,15 +650,12 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     if (GL || valid) {  // (without groups in warps the whole CTA agrees)
       auto values = [&](auto* base, long long ld, int plane, int r) {
         float v[kE];
-        const bool ok = valid >> r & 1u;
         if (VEC) {
           ring_read(slot(ring_at, r) + plane * threads, threads, base, v);
-#pragma unroll
-          for (int i = 0; i < kE; ++i) v[i] = ok ? v[i] : 0.f;
         } else {
 #pragma unroll
           for (int i = 0; i < kE; ++i) v[i] = 0.f;
-          if (ok) load<false>(base + row_of(here, r) * ld, j, n, d, v);
+          if (valid >> r & 1u) load<false>(base + row_of(here, r) * ld, j, n, d, v);
         }
         return pairs(v);
       };
@@ -856,9 +861,10 @@ struct Plan {
   int run, pieces, ctas;
 };
 
-// How the backward's rows are split: about `slots` runs of rows. Where a gate
-// row's rows are many, every gate row is cut into the same number of pieces;
-// where they are few, a run holds whole gate rows.
+// How the backward's rows are split. Where a gate row's rows are many, they are
+// dealt out in chunks to the same number of CTAs for every gate row; where they
+// are few, a CTA's run holds whole gate rows. About as many CTAs as fit on the
+// SMs, each with enough rows that its column sums are worth writing.
 Plan plan_backward(const unif_moe_block_norm* p, bool gate, int sms) {
   const int warps = cta_threads(p->width) / 32;
   const int groups = group_lanes(p->width) ? kThreads / group_lanes(p->width) : 1;
@@ -866,18 +872,16 @@ Plan plan_backward(const unif_moe_block_norm* p, bool gate, int sms) {
   const long long T = p->tokens;
   const long long period = gate && p->gate_rows && p->gate_rows < T ? p->gate_rows : T;
   const long long G = (T + period - 1) / period;
-  // a run has at least a few rows for each group, so that its column sums are worth writing
-  const long long least = 8ll * groups;
+  const long long chunk = groups < 2 ? 4 : 2ll * groups;  // whole steps of 1 or 2 rows a group
   long long want = (T + slots - 1) / slots;
-  if (want < least) want = least;
+  if (want < 8ll * groups) want = 8ll * groups;
   Plan r;
   if (period > want) {
     long long pieces = slots / G < 1 ? 1 : slots / G;
-    const long long most = (period + least - 1) / least;
+    const long long most = period / want;
     if (pieces > most) pieces = most;
     r.pieces = (int)pieces;
-    r.run = (int)((period + pieces - 1) / pieces);
-    r.pieces = (int)((period + r.run - 1) / r.run);
+    r.run = pieces > 1 ? (int)chunk : (int)period;
     r.ctas = (int)(G * r.pieces);
   } else {
     r.pieces = 1;
