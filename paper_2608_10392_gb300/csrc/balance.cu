@@ -10,7 +10,9 @@
 // first leaves each CTA's sums in the workspace, the second adds them (in the
 // CTAs' order: results do not change from run to run) and writes the gradient
 // from a second reading of the logits, which the first left in L2.
-// A token belongs to L lanes of a warp, which hold E logits each.
+// A token belongs to L lanes of a warp, which hold E logits each. At most one CTA
+// per SM: with two of 256 threads and one token of each group at a time, 65,536
+// tokens of 32 experts took 17 and 21 us.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -18,9 +20,6 @@
 
 namespace unif {
 namespace balance {
-
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 
 struct Args {
   int T, K, n_q;
@@ -34,8 +33,8 @@ struct Args {
   int32_t* counts;  // [K]
   float* prob;      // [K]
   float* dlogits;   // [T][K] or NULL
-  float* part_p;    // [CTAs][K]
-  int32_t* part_c;  // [CTAs][K]
+  float* part_p;    // [K][CTAs]
+  int32_t* part_c;  // [K][CTAs]
   float* part_z;    // [CTAs]
   int32_t* part_n;  // [CTAs]
   int ctas;         // of the first kernel
@@ -57,64 +56,102 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// exp(z - max) of a token's logits in e (0 past K), their sum and the maximum;
-// false for padding and for a token whose logits are all -inf.
-template <typename T, int L, int E>
-__device__ __forceinline__ bool softmax(const Args& a, int t, int lane, float (&e)[E], float& top,
-                                        float& sum) {
-  const bool in = t < a.T && (!a.mask || a.mask[t]);
-  const T* z = static_cast<const T*>(a.logits) + (long long)t * a.ld;
+// Lane `lane` of a token's L lanes holds the columns lane E .. lane E + E - 1.
+template <typename T, int L, int E, bool VEC>
+__device__ __forceinline__ void load(const Args& a, bool in, int t, int lane, float (&z)[E]) {
+  const T* p = static_cast<const T*>(a.logits) + (long long)t * a.ld + lane * E;
+  if (VEC) {  // 16 bytes of fp32 or 8 of bf16 at a time, K a multiple of four
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const bool ok = in && lane * E + i < a.K;
+      if (sizeof(T) == 4) {
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (ok) v = *reinterpret_cast<const float4*>(p + i);
+        z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
+      } else {
+        uint2 v = make_uint2(0xff80ff80u, 0xff80ff80u);  // -inf
+        if (ok) v = *reinterpret_cast<const uint2*>(p + i);
+        z[i] = __uint_as_float(v.x << 16);
+        z[i + 1] = __uint_as_float(v.x & 0xffff0000u);
+        z[i + 2] = __uint_as_float(v.y << 16);
+        z[i + 3] = __uint_as_float(v.y & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) z[i] = in && lane * E + i < a.K ? to_float(p[i]) : -INFINITY;
+  }
+}
+
+// z to exp(z - max) (0 past K), their sum and the maximum; false for padding and for
+// a token whose logits are all -inf.
+template <int L, int E>
+__device__ __forceinline__ bool softmax(bool in, float (&z)[E], float& top, float& sum) {
   top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int c = i * L + lane;
-    e[i] = in && c < a.K ? to_float(z[c]) : -INFINITY;
-    top = fmaxf(top, e[i]);
-  }
+  for (int i = 0; i < E; ++i) top = fmaxf(top, z[i]);
   top = lanes_max<L>(top);
   const float base = top == -INFINITY ? 0.f : top;
   sum = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    e[i] = __expf(e[i] - base);
-    sum += e[i];
+    z[i] = __expf(z[i] - base);
+    sum += z[i];
   }
   sum = lanes_sum<L>(sum);
   return in && (top != -INFINITY || isnan(sum));
 }
 
-template <typename T, int L, int E>
-__global__ void __launch_bounds__(kThreads) sums_kernel(const Args a) {
+// TH threads; U tokens of each group of lanes are loaded before the first is used.
+template <typename T, int L, int E, bool VEC, int TH, int U>
+__global__ void __launch_bounds__(TH) sums_kernel(const Args a) {
+  constexpr int kWarps = TH / 32;
   extern __shared__ float sh[];  // [kWarps][K] probabilities, then [K] counts
   __shared__ float z_sh[kWarps];
   __shared__ int n_sh[kWarps];
   int* cnt = reinterpret_cast<int*>(sh + kWarps * a.K);
-  for (int i = threadIdx.x; i < a.K; i += kThreads) cnt[i] = 0;
+  for (int i = threadIdx.x; i < a.K; i += TH) cnt[i] = 0;
   __syncthreads();
-  constexpr int kTok = kThreads / L;  // tokens of a CTA at a time
+  constexpr int kTok = TH / L;  // tokens of a CTA at a time
   const int lane = threadIdx.x % L, tok = threadIdx.x / L, warp = threadIdx.x / 32;
+  const long long stride = (long long)gridDim.x * kTok;
   float p[E], zs = 0.f;
   int n = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i) p[i] = 0.f;
-  for (long long base = (long long)blockIdx.x * kTok; base < a.T; base += (long long)gridDim.x * kTok) {
-    const long long tt = base + tok;
-    const int t = (int)min(tt, (long long)a.T);
-    float e[E], top, sum;
-    const bool valid = softmax<T, L, E>(a, t, lane, e, top, sum);
-    if (valid) {
-      const float inv = 1.f / sum, lse = top + logf(sum);
+  for (long long base = (long long)blockIdx.x * kTok; base < a.T; base += U * stride) {
+    float z[U][E];
+    int m[U], q0[U];
+    bool in[U];
 #pragma unroll
-      for (int i = 0; i < E; ++i) p[i] = fmaf(e[i], inv, p[i]);
-      if (lane == 0) {
-        zs = fmaf(lse, lse, zs);
-        ++n;
+    for (int u = 0; u < U; ++u) {
+      const long long tt = base + u * stride + tok;
+      in[u] = tt < a.T && (!a.mask || a.mask[tt]);
+      const int t = in[u] ? (int)tt : 0;
+      load<T, L, E, VEC>(a, in[u], t, lane, z[u]);
+      m[u] = a.n_q;
+      q0[u] = -1;
+      if (in[u]) {
+        if (a.k) m[u] = min(m[u], a.k[t]);
+        if (lane < a.n_q) q0[u] = a.q[(long long)t * a.ld_q + lane];
       }
-      int m = a.n_q;
-      if (a.k) m = min(m, a.k[t]);
-      for (int i = lane; i < m; i += L) {
-        const int j = a.q[(long long)t * a.ld_q + i];
-        if (j >= 0 && j < a.K) atomicAdd(&cnt[j], 1);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float top, sum;
+      if (softmax<L, E>(in[u], z[u], top, sum)) {
+        const float inv = 1.f / sum, lse = top + logf(sum);
+#pragma unroll
+        for (int i = 0; i < E; ++i) p[i] = fmaf(z[u][i], inv, p[i]);
+        if (lane == 0) {
+          zs = fmaf(lse, lse, zs);
+          ++n;
+        }
+        int j = q0[u];
+        for (int i = lane; i < m[u]; i += L) {
+          if (i != lane) j = a.q[(base + u * stride + tok) * a.ld_q + i];
+          if (j >= 0 && j < a.K) atomicAdd(&cnt[j], 1);
+        }
       }
     }
   }
@@ -123,7 +160,7 @@ __global__ void __launch_bounds__(kThreads) sums_kernel(const Args a) {
   for (int i = 0; i < E; ++i) {
 #pragma unroll
     for (int o = L; o < 32; o <<= 1) p[i] += __shfl_xor_sync(0xffffffffu, p[i], o);
-    const int c = i * L + lane;
+    const int c = lane * E + i;
     if ((threadIdx.x & 31) < L && c < a.K) sh[warp * a.K + c] = p[i];
   }
 #pragma unroll
@@ -136,147 +173,182 @@ __global__ void __launch_bounds__(kThreads) sums_kernel(const Args a) {
     n_sh[warp] = n;
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < a.K; c += kThreads) {
+  for (int c = threadIdx.x; c < a.K; c += TH) {
     float s = 0.f;
+#pragma unroll 8
     for (int w = 0; w < kWarps; ++w) s += sh[w * a.K + c];
-    a.part_p[(long long)blockIdx.x * a.K + c] = s;
-    a.part_c[(long long)blockIdx.x * a.K + c] = cnt[c];
+    a.part_p[(long long)c * gridDim.x + blockIdx.x] = s;
+    a.part_c[(long long)c * gridDim.x + blockIdx.x] = cnt[c];
   }
-  if (threadIdx.x == 0) {
-    float s = 0.f;
-    int m = 0;
-    for (int w = 0; w < kWarps; ++w) { s += z_sh[w]; m += n_sh[w]; }
-    a.part_z[blockIdx.x] = s;
-    a.part_n[blockIdx.x] = m;
+  if (warp == kWarps - 1) {
+    const int l = threadIdx.x & 31;
+    float s = l < kWarps ? z_sh[l] : 0.f;
+    int m = l < kWarps ? n_sh[l] : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      m += __shfl_xor_sync(0xffffffffu, m, o);
+    }
+    if (l == 0) {
+      a.part_z[blockIdx.x] = s;
+      a.part_n[blockIdx.x] = m;
+    }
   }
 }
 
-template <typename T, int L, int E>
-__global__ void __launch_bounds__(kThreads) gradient_kernel(const Args a) {
-  extern __shared__ float sh[];  // [K] f, then [kWarps][K] shares of the sums
+template <typename T, int L, int E, bool VEC, int TH, int U>
+__global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
+  constexpr int kWarps = TH / 32;
+  extern __shared__ float f[];  // [K] f, then [K] mean probabilities (first CTA)
   __shared__ int all[2];
-  __shared__ float fl[kWarps];
-  float* f = sh;
-  int* share = reinterpret_cast<int*>(sh + a.K);
-  float* share_p = sh + a.K;
+  __shared__ float zsum;
+  float* prob = f + a.K;
   const int lane32 = threadIdx.x & 31, warp = threadIdx.x / 32;
-  if (threadIdx.x < 2) all[threadIdx.x] = 0;
+  const bool first = blockIdx.x == 0;
+  if (threadIdx.x == 0) all[0] = 0;
   grid_dep_wait();
-  // counts: whole numbers, so any order gives the same
-  int sum_c = 0, n = 0;
-  for (int c = lane32; c < a.K; c += 32) {
-    int s = 0;
-    for (int i = warp; i < a.ctas; i += kWarps) s += a.part_c[(long long)i * a.K + c];
-    share[warp * a.K + c] = s;
-    sum_c += s;
-  }
-  for (int i = threadIdx.x; i < a.ctas; i += kThreads) n += a.part_n[i];
   __syncthreads();
-  atomicAdd(&all[0], sum_c);
-  atomicAdd(&all[1], n);
+  // a warp per column adds the CTAs' sums (whole numbers, and in a fixed order)
+  for (int c = warp; c < a.K; c += kWarps) {
+    int m = 0;
+    float q = 0.f;
+    for (int i = lane32; i < a.ctas; i += 32) {
+      m += a.part_c[(long long)c * a.ctas + i];
+      if (first) q += a.part_p[(long long)c * a.ctas + i];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      m += __shfl_xor_sync(0xffffffffu, m, o);
+      q += __shfl_xor_sync(0xffffffffu, q, o);
+    }
+    if (lane32 == 0) {
+      f[c] = __int_as_float(m);
+      atomicAdd(&all[0], m);
+      if (first) {
+        prob[c] = q;
+        a.counts[c] = m;
+      }
+    }
+  }
+  if (warp == kWarps - 1) {
+    int n = 0;
+    float z = 0.f;
+    for (int i = lane32; i < a.ctas; i += 32) {
+      n += a.part_n[i];
+      if (first) z += a.part_z[i];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      n += __shfl_xor_sync(0xffffffffu, n, o);
+      z += __shfl_xor_sync(0xffffffffu, z, o);
+    }
+    if (lane32 == 0) {
+      all[1] = n;
+      zsum = z;
+    }
+  }
   __syncthreads();
   const float inv_c = 1.f / (float)max(all[0], 1), inv_n = 1.f / (float)max(all[1], 1);
-  for (int c = threadIdx.x; c < a.K; c += kThreads) {
-    int s = 0;
-    for (int w = 0; w < kWarps; ++w) s += share[w * a.K + c];
-    f[c] = (float)s * inv_c;
-    if (blockIdx.x == 0) a.counts[c] = s;
-  }
+  for (int c = threadIdx.x; c < a.K; c += TH) f[c] = (float)__float_as_int(f[c]) * inv_c;
   __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int c = lane32; c < a.K; c += 32) {
-      float s = 0.f;
-      for (int i = warp; i < a.ctas; i += kWarps) s += a.part_p[(long long)i * a.K + c];
-      share_p[warp * a.K + c] = s;
-    }
-    __syncthreads();
+  if (first && warp == 0) {
     float b = 0.f;
-    for (int c = threadIdx.x; c < a.K; c += kThreads) {
-      float s = 0.f;
-      for (int w = 0; w < kWarps; ++w) s += share_p[w * a.K + c];
-      s *= inv_n;
-      a.prob[c] = s;
-      b = fmaf(f[c], s, b);
+    for (int c = lane32; c < a.K; c += 32) {
+      const float q = prob[c] * inv_n;
+      a.prob[c] = q;
+      b = fmaf(f[c], q, b);
     }
-    b = lanes_sum<32>(b);
-    if (lane32 == 0) fl[warp] = b;
-    __syncthreads();
-    if (warp == 0) {
-      float z = 0.f;
-      for (int i = lane32; i < a.ctas; i += 32) z += a.part_z[i];
-      z = lanes_sum<32>(z) * inv_n;
-      b = 0.f;
-      for (int w = 0; w < kWarps; ++w) b += fl[w];
-      b *= (float)a.K;
-      if (lane32 == 0) {
-        a.loss[0] = fmaf(a.w_b, b, a.w_z * z);
-        a.loss[1] = b;
-        a.loss[2] = z;
-      }
+    b = lanes_sum<32>(b) * (float)a.K;
+    if (lane32 == 0) {
+      const float z = zsum * inv_n;
+      a.loss[0] = fmaf(a.w_b, b, a.w_z * z);
+      a.loss[1] = b;
+      a.loss[2] = z;
     }
   }
   if (!a.dlogits) return;
-  constexpr int kTok = kThreads / L;
+  constexpr int kTok = TH / L;
   const int lane = threadIdx.x % L, tok = threadIdx.x / L;
   const float wb = a.w_b * (float)a.K, wz = 2.f * a.w_z;
+  const long long stride = (long long)gridDim.x * kTok;
   float fr[E];
 #pragma unroll
-  for (int i = 0; i < E; ++i) fr[i] = i * L + lane < a.K ? f[i * L + lane] : 0.f;
-  for (long long base = (long long)blockIdx.x * kTok; base < a.T; base += (long long)gridDim.x * kTok) {
-    const long long tt = base + tok;
-    const int t = (int)min(tt, (long long)a.T);
-    float e[E], top, sum;
-    const bool valid = softmax<T, L, E>(a, t, lane, e, top, sum);
-    const float inv = 1.f / sum;
-    float fp = 0.f;
+  for (int i = 0; i < E; ++i) fr[i] = lane * E + i < a.K ? f[lane * E + i] : 0.f;
+  for (long long base = (long long)blockIdx.x * kTok; base < a.T; base += U * stride) {
+    float e[U][E];
+    bool in[U];
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      e[i] *= inv;
-      fp = fmaf(fr[i], e[i], fp);
+    for (int u = 0; u < U; ++u) {
+      const long long tt = base + u * stride + tok;
+      in[u] = tt < a.T && (!a.mask || a.mask[tt]);
+      load<T, L, E, VEC>(a, in[u], in[u] ? (int)tt : 0, lane, e[u]);
     }
-    fp = lanes_sum<L>(fp);
-    const float g = fmaf(wz, top + logf(sum), -wb * fp);
-    if (tt < a.T)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long tt = base + u * stride + tok;
+      float top, sum;
+      const bool valid = softmax<L, E>(in[u], e[u], top, sum);
+      const float inv = 1.f / sum;
+      float fp = 0.f;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const int c = i * L + lane;
-        if (c < a.K)
-          a.dlogits[(long long)t * a.K + c] = valid ? e[i] * inv_n * fmaf(wb, fr[i], g) : 0.f;
+        e[u][i] *= inv;
+        fp = fmaf(fr[i], e[u][i], fp);
       }
+      fp = lanes_sum<L>(fp);
+      const float g = fmaf(wz, top + logf(sum), -wb * fp);
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[u][i] = valid ? e[u][i] * inv_n * fmaf(wb, fr[i], g) : 0.f;
+      if (tt < a.T) {
+        float* to = a.dlogits + tt * a.K + lane * E;
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+          if (VEC) {
+            if (lane * E + i < a.K)
+              *reinterpret_cast<float4*>(to + i) =
+                  make_float4(e[u][i], e[u][i + 1], e[u][i + 2], e[u][i + 3]);
+          } else {
+#pragma unroll
+            for (int k = i; k < i + 4; ++k)
+              if (lane * E + k < a.K) to[k] = e[u][k];
+          }
+        }
+      }
+    }
   }
 }
 
-int tokens_per_cta(int K) {
-  const int lanes = K <= 4 ? 1 : K <= 8 ? 2 : K <= 16 ? 4 : K <= 32 ? 8 : K <= 64 ? 16 : 32;
-  return kThreads / lanes;
-}
+constexpr int kWide = 128;  // up to this many experts: CTAs of 1,024 threads
+inline int threads_of(int K) { return K <= kWide ? 1024 : 256; }
 
-// CTAs of both kernels: one per 256 lanes of tokens, at most two per SM.
+// CTAs of both kernels: at most one per SM, so that the second has few sums to add.
 int cta_count(int T, int K, int sms) {
-  const long long want = ((long long)T + tokens_per_cta(K) - 1) / tokens_per_cta(K);
-  return (int)(want < 1 ? 1 : want > 2ll * sms ? 2 * sms : want);
+  const int lanes = K <= 4 ? 1 : K <= 8 ? 2 : K <= 16 ? 4 : K <= 32 ? 8 : K <= 64 ? 16 : 32;
+  const long long tok = threads_of(K) / lanes, want = ((long long)T + tok - 1) / tok;
+  return (int)(want < 1 ? 1 : want > sms ? sms : want);
 }
 
-template <typename T, int L, int E>
+template <typename T, int L, int E, bool VEC, int TH, int U>
 cudaError_t launch_as(const Args& a, cudaStream_t s) {
-  const size_t smem = (size_t)(kWarps + 1) * a.K * sizeof(float);
-  sums_kernel<T, L, E><<<a.ctas, kThreads, smem, s>>>(a);
+  const size_t smem = (size_t)(TH / 32 * a.K + a.K) * sizeof(float);
+  const size_t smem2 = (size_t)(2 * a.K) * sizeof(float);
+  sums_kernel<T, L, E, VEC, TH, U><<<a.ctas, TH, smem, s>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_dependent(gradient_kernel<T, L, E>, dim3(a.dlogits ? a.ctas : 1), dim3(kThreads),
-                          smem, s, a);
+  return launch_dependent(gradient_kernel<T, L, E, VEC, TH, U>, dim3(a.dlogits ? a.ctas : 1), dim3(TH),
+                          smem2, s, a);
 }
 
-template <typename T>
+template <typename T, bool VEC>
 cudaError_t launch(const Args& a, cudaStream_t s) {
-  if (a.K <= 4) return launch_as<T, 1, 4>(a, s);
-  if (a.K <= 8) return launch_as<T, 2, 4>(a, s);
-  if (a.K <= 16) return launch_as<T, 4, 4>(a, s);
-  if (a.K <= 32) return launch_as<T, 8, 4>(a, s);
-  if (a.K <= 64) return launch_as<T, 16, 4>(a, s);
-  if (a.K <= 128) return launch_as<T, 32, 4>(a, s);
-  if (a.K <= 256) return launch_as<T, 32, 8>(a, s);
-  return launch_as<T, 32, 16>(a, s);
+  if (a.K <= 4) return launch_as<T, 1, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 8) return launch_as<T, 2, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 16) return launch_as<T, 4, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 32) return launch_as<T, 8, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 64) return launch_as<T, 16, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 128) return launch_as<T, 32, 4, VEC, 1024, 4>(a, s);
+  if (a.K <= 256) return launch_as<T, 32, 8, VEC, 256, 4>(a, s);
+  return launch_as<T, 32, 16, VEC, 256, 2>(a, s);
 }
 
 // Offsets of the workspace's parts, each at a multiple of 16 bytes.
@@ -364,7 +436,14 @@ int unif_moe_balance_loss(int T, int K, const void* logits, unif_moe_dtype dtype
   a.part_z = reinterpret_cast<float*>(ws + at[2]);
   a.part_n = reinterpret_cast<int32_t*>(ws + at[3]);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dtype == UNIF_MOE_BF16 ? bl::launch<__nv_bfloat16>(a, s) : bl::launch<float>(a, s);
+  const uintptr_t step = dtype == UNIF_MOE_BF16 ? 8 : 16;
+  const bool vec = K % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(logits) % step == 0 &&
+                   reinterpret_cast<uintptr_t>(dlogits) % 16 == 0;
+  cudaError_t e;
+  if (dtype == UNIF_MOE_BF16)
+    e = vec ? bl::launch<__nv_bfloat16, true>(a, s) : bl::launch<__nv_bfloat16, false>(a, s);
+  else
+    e = vec ? bl::launch<float, true>(a, s) : bl::launch<float, false>(a, s);
   if (e != cudaSuccess) {
     set_error("balance loss: %s", cudaGetErrorString(e));
     return UNIF_MOE_ERR_CUDA;
