@@ -552,7 +552,7 @@ UNIF_MOE_API int unif_moe_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
                                            unif_moe_dtype dtype, int64_t ld, void* stream);
 
 enum { UNIF_MOE_ACTIVATION_NONE = 0, UNIF_MOE_ACTIVATION_GELU = 1 };
-#define UNIF_MOE_MXFP4_MAX_GROUPS 1024
+#define UNIF_MOE_MXFP4_MAX_GROUPS 4224 /* above the (64 + 1) * 64 of the largest layer */
 
 /* Product of rows in MXFP4 with the weights of their group, also in MXFP4:
  *   out[r][j] = act(sum_c A[r][c] W[g][j][c]) for the rows r of group g, those in

@@ -25,17 +25,22 @@ using namespace tc;
 
 constexpr int kTN = 192;         // rows of a tile (MMA N)
 constexpr int kStep = 256;       // columns of a step: 128 bytes of codes, 8 scales
-constexpr int kStages = 5;
+// Stages of the ring; fewer where the table of groups (from about 670 on) needs the room.
+constexpr int kMaxStages = 5, kFewStages = 3;
 constexpr uint32_t kBytesW = 128 * 128, kBytesA = kTN * 128;
-constexpr uint32_t kBytesSW = 1024, kBytesSA = 2048;  // scale blocks of a stage
-constexpr uint32_t kStageBytes = kBytesW + kBytesA + kBytesSW + kBytesSA;
+constexpr uint32_t kStageBytes = kBytesW + kBytesA;
+// Scales of two steps: 512-byte blocks [step][128 columns][weights | rows 0-127, rows 128-191].
+constexpr int kScaleBufs = 3;
+constexpr uint32_t kBytesSW = 4 * 512, kBytesSA = 8 * 512, kBytesS = kBytesSW + kBytesSA;
 constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 4;
 constexpr int kThreads = 32 * (kScaleWarp + kScaleWarps);
-constexpr int kBoxRows = 32;     // rows of one TMA box of A
+// Rows of the TMA boxes of A: one box where the tile has at most 16 or 64 rows or
+// more than 128, else two of 64. (Six boxes of 32 took the loader 970 cycles a step.)
+constexpr int kBoxS = 16, kBoxM = 64;
 // TMEM columns: two accumulators, then the scales of each stage.
 constexpr uint32_t kAcc = kTN, kScaleCol = 2 * kTN, kScaleCols = 24, kTmemCols = 512;
-static_assert(kScaleCol + kStages * kScaleCols <= kTmemCols, "TMEM");
-constexpr int kBars = 2 * kStages + 5;
+static_assert(kScaleCol + kMaxStages * kScaleCols <= kTmemCols, "TMEM");
+constexpr int kBars = 2 * kMaxStages + 5 + 2 * kScaleBufs;
 
 struct Params {
   int rows, N, G, num_kb, ch_tiles;
@@ -50,8 +55,8 @@ struct Params {
   long long wait_limit;
 };
 
-__host__ __device__ constexpr uint32_t smem_bytes(int G) {
-  return 1024u + kStages * kStageBytes + (kBars + 1) * 8u + (uint32_t)(2 * G + 1) * 4u + 16u;
+__host__ __device__ constexpr uint32_t smem_bytes(int stages, int G) {
+  return 1024u + stages * kStageBytes + kScaleBufs * kBytesS + (kBars + 1) * 8u + (uint32_t)(3 * G + 1) * 4u + 16u;
 }
 
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
@@ -80,6 +85,9 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int n, int scale_byte) {
   return ((uint32_t)scale_byte << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
          (1u << 23) | (1u << 27) | ((uint32_t)scale_byte << 29);
 }
+
+constexpr uint32_t kSmemMax = 232448;  // shared memory that a CTA can have
+static_assert(smem_bytes(kFewStages, UNIF_MOE_MXFP4_MAX_GROUPS) <= kSmemMax, "shared memory");
 
 __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long long limit) {
   const long long t0 = clock64();
@@ -144,36 +152,46 @@ __device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int
   }
 }
 
-template <typename TO, bool GELU>
+template <typename TO, bool GELU, int kStages>
 __global__ void __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+                   const __grid_constant__ CUtensorMap tmAM, const __grid_constant__ CUtensorMap tmAS,
                    const Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t s0 = smem_u32(smem);
-  // stage s: weight codes, row codes, weight scales, row scales
+  // stage s: weight codes, row codes
   auto stage = [&](int s) { return s0 + (uint32_t)s * kStageBytes; };
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes);
+  uint8_t* scales = smem + kStages * kStageBytes;
+  const uint32_t sc0 = smem_u32(scales);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(scales + kScaleBufs * kBytesS);
   const uint32_t bar0 = smem_u32(bars);
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
   auto accf_bar = [&](int a) { return bar0 + 8u * (2 * kStages + a); };
   auto acce_bar = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); };
   const uint32_t mma_done = bar0 + 8u * (2 * kStages + 4);
+  auto sfull_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 5 + b); };
+  auto sempty_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 5 + kScaleBufs + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int32_t* first_s = reinterpret_cast<int32_t*>(bars + kBars + 1);  // [G + 1]
-  int32_t* len_s = first_s + p.G + 1;                               // [G]
+  int32_t* len_s = first_s + p.G + 1;                               // [G] rows of each group
+  int32_t* start_s = len_s + p.G;                                   // [G] its first row
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(full_bar(s), 2);  // the loader and the scales' warp
+      mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(accf_bar(a), 1);
       mbar_init(acce_bar(a), kEpiWarps);
+    }
+    for (int b = 0; b < kScaleBufs; ++b) {
+      mbar_init(sfull_bar(b), 32 * kScaleWarps);  // each thread for what it wrote
+      mbar_init(sempty_bar(b), 1);
     }
     mbar_init(mma_done, 1);
     *abort_flag = 0;
@@ -195,6 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int lo = p.offsets ? min(max(p.offsets[g], 0), p.rows) : 0;
         const int hi = p.offsets ? min(max(p.offsets[g + 1], 0), p.rows) : p.rows;
         n = max(hi - lo, 0);
+        start_s[g] = lo;
       }
       long long before = n;  // rows of the groups up to this one
 #pragma unroll
@@ -237,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tiles = first_s[lo + 1] - first_s[lo], rows = len_s[lo];
     const int part = ((rows + tiles - 1) / tiles + 15) & ~15;
     const int at = (tile - first_s[lo]) * part;
-    it.row0 = (p.offsets ? min(max(p.offsets[lo], 0), p.rows) : 0) + at;
+    it.row0 = start_s[lo] + at;
     it.rows = min(part, rows - at);
     return it;
   };
@@ -267,55 +286,63 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kTmaWarp) {
     // ---------------- codes of both operands --------------------------------
-    bool ok = true;
-    int s = 0;
-    uint32_t ph = 0;
-    long long issued = 0;
-    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
-      const Item it = item_of(i);
-      const int boxes = (it.rows + kBoxRows - 1) / kBoxRows;
-      for (int kb = 0; kb < p.num_kb; ++kb) {
-        ok = wait_warp(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
-        if (!ok) break;
-        if (lane == 0) {
+    // (One elected lane runs this role and the next from end to end: a branch for
+    // one lane inside the loop costs the warp about 300 cycles to reconverge at every step, and
+    // instructions under one lane's predicate are issued several times slower.)
+    if (elect_one()) {
+      bool ok = true;
+      int s = 0;
+      uint32_t ph = 0;
+      long long issued = 0;
+      for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
+        const Item it = item_of(i);
+        const bool large = it.rows > 2 * kBoxM, small = it.rows <= kBoxS, two = !large && it.rows > kBoxM;
+        const CUtensorMap* map = large ? &tmA : small ? &tmAS : &tmAM;
+        const uint32_t bytes =
+            kBytesW + 128u * (uint32_t)(large ? kTN : small ? kBoxS : two ? 2 * kBoxM : kBoxM);
+        const int w0 = it.g * p.N + it.ch0;
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          ok = wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
           const uint32_t bar = full_bar(s);
-          mbar_expect_tx(bar, kBytesW + (uint32_t)boxes * kBoxRows * 128u);
-          tma_load_2d(stage(s), &tmW, bar, kb * 64, it.g * p.N + it.ch0);
-          for (int b = 0; b < boxes; ++b)
-            tma_load_2d(stage(s) + kBytesW + (uint32_t)b * kBoxRows * 128u, &tmA, bar, kb * 64,
-                        it.row0 + b * kBoxRows);
+          mbar_expect_tx(bar, bytes);
+          tma_load_2d(stage(s), &tmW, bar, kb * 64, w0);
+          tma_load_2d(stage(s) + kBytesW, map, bar, kb * 64, it.row0);
+          if (two) tma_load_2d(stage(s) + kBytesW + kBoxM * 128u, map, bar, kb * 64, it.row0 + kBoxM);
+          ++issued;
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
-        __syncwarp();
-        ++issued;
-        if (++s == kStages) { s = 0; ph ^= 1u; }
       }
-    }
-    // loads still in flight land before the CTA exits
-    if (lane == 0)
+      // loads still in flight land before the CTA exits
       for (long long j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
         wait_settle(full_bar((int)(j % kStages)), (uint32_t)((j / kStages) & 1), p.wait_limit / 16);
+    }
     __syncwarp();
   } else if (warp == kMmaWarp) {
     // ---------------- scales to TMEM, MMAs ----------------------------------
-    int s = 0, acc = 0;
-    uint32_t ph = 0, acc_ph = 0;
-    bool ok = true, any = false;
-    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
-      const Item it = item_of(i);
-      ok = wait_warp(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
-      if (!ok) break;
-      tc_fence_after();
-      const int n = (it.rows + 15) & ~15;
-      const uint32_t d = tmem + acc * kAcc;
-      const uint32_t id0 = idesc_mxf4(n, 0), id2 = idesc_mxf4(n, 2);
-      for (int kb = 0; kb < p.num_kb; ++kb) {
-        ok = wait_warp(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+    if (elect_one()) {
+      int s = 0, acc = 0;
+      uint32_t ph = 0, acc_ph = 0;
+      int sb = 0;  // scale buffer and its phase
+      uint32_t sb_ph = 0;
+      bool ok = true, any = false;
+      for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
+        const Item it = item_of(i);
+        ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
         if (!ok) break;
         tc_fence_after();
-        if (elect_one()) {
-          const uint32_t sc = stage(s) + kBytesW + kBytesA;
+        const int n = (it.rows + 15) & ~15;
+        const uint32_t d = tmem + acc * kAcc;
+        const uint32_t id0 = idesc_mxf4(n, 0), id2 = idesc_mxf4(n, 2);
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if ((kb & 1) == 0)
+            ok = wait_bounded(sfull_bar(sb), sb_ph, abort_flag, p.status, p.wait_limit);
+          ok = ok && wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t sc = sc0 + sb * kBytesS + (kb & 1) * 1024u;
           const uint32_t tw = tmem + kScaleCol + s * kScaleCols, ta = tw + 8;
-          const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW);
+          const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW + (kb & 1) * 1024u);
           copy_scales(tw, dw);
           copy_scales(tw + 4, dw + (512 >> 4));
           copy_scales(ta, da);
@@ -331,59 +358,72 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_mxf4(d, w + 2 * k, a + 2 * k, (k & 1) ? id2 : id0, tw + 4 * (k >> 1),
                      ta + 8 * (k >> 1), (kb | k) != 0 ? 1u : 0u);
           umma_commit(empty_bar(s));
+          if ((kb & 1) || kb == p.num_kb - 1) {
+            umma_commit(sempty_bar(sb));
+            if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
+          }
           if (kb == p.num_kb - 1) umma_commit(accf_bar(acc));
+          any = true;
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
-        __syncwarp();
-        any = true;
-        if (++s == kStages) { s = 0; ph ^= 1u; }
+        if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
       }
-      if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+      // every MMA issued has completed before TMEM is released
+      if (any) {
+        umma_commit(mma_done);
+        wait_settle(mma_done, 0u, p.wait_limit);
+      }
     }
-    // every MMA issued has completed before TMEM is released
-    if (any) {
-      if (elect_one()) umma_commit(mma_done);
-      __syncwarp();
-      wait_settle(mma_done, 0u, p.wait_limit);
-    }
+    __syncwarp();
   } else {
     // ---------------- scales ------------------------------------------------
-    const int mine = warp - kScaleWarp;
-    long long c = 0;  // steps so far
+    // Two steps at a time, two threads a row with eight bytes (a step's scales) each:
+    // with a lane per row and step, every load touched 32 lines and the L1's tags were
+    // taken 320 cycles a step.
+    const int t = threadIdx.x - 32 * kScaleWarp, r0 = t >> 1, h = t & 1;
+    int sb = 0;
+    uint32_t sb_ph = 0;
     bool ok = true;
     for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
       const Item it = item_of(i);
-      const uint8_t* ws = p.w_scales + ((long long)it.g * p.N + it.ch0 + lane) * p.pitch;
-      const uint8_t* as = p.a_scales + ((long long)it.row0 + lane) * p.pitch;
-      for (int kb = 0; kb < p.num_kb; ++kb, ++c) {
-        if ((int)(c % kScaleWarps) != mine) continue;
-        uint2 w[4], a[6];
+      const uint8_t* ws = p.w_scales + ((long long)it.g * p.N + it.ch0 + r0) * p.pitch + 8 * h;
+      const uint8_t* as = p.a_scales + ((long long)it.row0 + r0) * p.pitch + 8 * h;
+      for (int kb = 0; kb < p.num_kb; kb += 2) {
+        const bool in = kb + h < p.num_kb;
+        uint2 w[2], a[3];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < 2; ++r) {
           w[r] = make_uint2(0u, 0u);
-          if (it.ch0 + 32 * r + lane < p.N)
-            w[r] = __ldg(reinterpret_cast<const uint2*>(ws + (long long)(32 * r) * p.pitch + kb * 8));
+          if (in && it.ch0 + 64 * r + r0 < p.N)
+            w[r] = __ldg(reinterpret_cast<const uint2*>(ws + (long long)(64 * r) * p.pitch + kb * 8));
         }
 #pragma unroll
-        for (int r = 0; r < 6; ++r) {
+        for (int r = 0; r < 3; ++r) {
           a[r] = make_uint2(0u, 0u);
-          if (32 * r + lane < it.rows)
-            a[r] = __ldg(reinterpret_cast<const uint2*>(as + (long long)(32 * r) * p.pitch + kb * 8));
+          if (in && 64 * r + r0 < it.rows)
+            a[r] = __ldg(reinterpret_cast<const uint2*>(as + (long long)(64 * r) * p.pitch + kb * 8));
         }
-        const int s = (int)(c % kStages);
-        const uint32_t ph = (uint32_t)((c / kStages) & 1);
-        ok = wait_warp(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
+        ok = wait_warp(sempty_bar(sb), sb_ph ^ 1u, abort_flag, p.status, p.wait_limit);
         if (!ok) break;
-        uint8_t* at = smem + (size_t)s * kStageBytes + kBytesW + kBytesA + lane * 16;
-        *reinterpret_cast<uint4*>(at) = make_uint4(w[0].x, w[1].x, w[2].x, w[3].x);
-        *reinterpret_cast<uint4*>(at + 512) = make_uint4(w[0].y, w[1].y, w[2].y, w[3].y);
-        at += kBytesSW;
-        *reinterpret_cast<uint4*>(at) = make_uint4(a[0].x, a[1].x, a[2].x, a[3].x);
-        *reinterpret_cast<uint4*>(at + 512) = make_uint4(a[4].x, a[5].x, 0u, 0u);
-        *reinterpret_cast<uint4*>(at + 1024) = make_uint4(a[0].y, a[1].y, a[2].y, a[3].y);
-        *reinterpret_cast<uint4*>(at + 1536) = make_uint4(a[4].y, a[5].y, 0u, 0u);
+        // block of (step, 128 columns): byte 16 (row % 32) + 4 (row / 32)
+        uint8_t* at = scales + sb * kBytesS + (r0 & 31) * 16 + h * 1024;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          uint32_t* to = reinterpret_cast<uint32_t*>(at + ((64 * r + r0) >> 5) * 4);
+          to[0] = w[r].x;
+          to[128] = w[r].y;
+        }
+        at += kBytesSW + h * 1024;
+#pragma unroll
+        for (int r = 0; r < 3; ++r) {
+          uint32_t* to =
+              reinterpret_cast<uint32_t*>(at + (r >> 1) * 512 + (((64 * r + r0) & 127) >> 5) * 4);
+          to[0] = a[r].x;
+          to[256] = a[r].y;
+        }
         fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full_bar(s));
+        mbar_arrive(sfull_bar(sb));
+        if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
       }
     }
   }
@@ -394,13 +434,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <typename TO, bool GELU>
-cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmA, const Params& p, int grid,
+template <typename TO, bool GELU, int kStages>
+cudaError_t launch_as(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, int grid,
                    cudaStream_t s) {
-  const uint32_t smem = smem_bytes(p.G);
-  cudaError_t e = allow_smem_once(product_kernel<TO, GELU>, smem);
+  const uint32_t smem = smem_bytes(kStages, p.G);
+  cudaError_t e = allow_smem_once(product_kernel<TO, GELU, kStages>, smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(product_kernel<TO, GELU>, dim3(grid), dim3(kThreads), smem, s, tmW, tmA, p);
+  return launch_dependent(product_kernel<TO, GELU, kStages>, dim3(grid), dim3(kThreads), smem, s, tmW, tmA[0],
+                          tmA[1], tmA[2], p);
+}
+
+template <typename TO, bool GELU>
+cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, int grid,
+                   cudaStream_t s) {
+  if (smem_bytes(kMaxStages, p.G) <= kSmemMax)
+    return launch_as<TO, GELU, kMaxStages>(tmW, tmA, p, grid, s);
+  return launch_as<TO, GELU, kFewStages>(tmW, tmA, p, grid, s);
 }
 
 }  // namespace fp4p
@@ -449,9 +498,11 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   const int rc = unif::sm_count(&sms);
   if (rc != UNIF_MOE_OK) return rc;
   const uint64_t pitch = (uint64_t)(cols + 31) / 32 * 16;
-  CUtensorMap tmW, tmA;  // 128-byte pieces of code rows, counted in 2-byte units
+  CUtensorMap tmW, tmA[3];  // 128-byte pieces of code rows, counted in 2-byte units
   if (!unif::encode_bf16_map(&tmW, w_codes, pitch / 2, (uint64_t)n * groups, 64, 128, 128) ||
-      !unif::encode_bf16_map(&tmA, a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxRows, 128)) {
+      !unif::encode_bf16_map(&tmA[0], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kTN, 128) ||
+      !unif::encode_bf16_map(&tmA[1], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxM, 128) ||
+      !unif::encode_bf16_map(&tmA[2], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxS, 128)) {
     set_error("cuTensorMapEncodeTiled failed for the codes");
     return UNIF_MOE_ERR_CUDA;
   }
