@@ -40,6 +40,9 @@ constexpr int kBoxS = 16, kBoxM = 64;
 // TMEM columns: two accumulators, then the scales of each stage.
 constexpr uint32_t kAcc = kTN, kScaleCol = 2 * kTN, kScaleCols = 24, kTmemCols = 512;
 static_assert(kScaleCol + kMaxStages * kScaleCols <= kTmemCols, "TMEM");
+// Items of a CTA that are looked up once, by all threads together: one thread's
+// search takes some 1,800 cycles, as long as an item of three steps.
+constexpr int kListed = 256;
 constexpr int kBars = 2 * kMaxStages + 5 + 2 * kScaleBufs;
 
 struct Params {
@@ -56,7 +59,8 @@ struct Params {
 };
 
 __host__ __device__ constexpr uint32_t smem_bytes(int stages, int G) {
-  return 1024u + stages * kStageBytes + kScaleBufs * kBytesS + (kBars + 1) * 8u + (uint32_t)(3 * G + 1) * 4u + 16u;
+  return 1024u + stages * kStageBytes + kScaleBufs * kBytesS + (kBars + 1) * 8u + kListed * 16u +
+         (uint32_t)(3 * G + 1) * 4u + 32u;
 }
 
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
@@ -96,8 +100,8 @@ __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long 
 }
 
 // Items of the walk: a run of a group's rows and 128 of its channels.
-struct Item {
-  int g, ch0, row0, rows;  // rows >= 1
+struct __align__(16) Item {
+  int w0, ch0, row0, rows;  // first weight row of the group and channels, first channel; rows >= 1
 };
 
 template <typename TO, bool GELU>
@@ -175,7 +179,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto sempty_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 5 + kScaleBufs + b); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int32_t* first_s = reinterpret_cast<int32_t*>(bars + kBars + 1);  // [G + 1]
+  Item* list_s = reinterpret_cast<Item*>((reinterpret_cast<uintptr_t>(bars + kBars + 1) + 15) & ~(uintptr_t)15);
+  int32_t* first_s = reinterpret_cast<int32_t*>(list_s + kListed);  // [G + 1] row tiles before each group
   int32_t* len_s = first_s + p.G + 1;                               // [G] rows of each group
   int32_t* start_s = len_s + p.G;                                   // [G] its first row
 
@@ -201,49 +206,59 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
   }
+  __shared__ long long rows_sh[kThreads / 32];
+  __shared__ int tiles_sh[kThreads / 32];
   grid_dep_wait();
-  if (warp == 0) {
-    // row tiles before each group; whatever the offsets hold, rows stay in [0, rows)
-    // and the groups have no more than `rows` rows together
-    int sum = 0, left = p.rows;
-    for (int g0 = 0; g0 < p.G; g0 += 32) {
-      const int g = g0 + lane;
-      int n = 0;
+  // Row tiles before each group; whatever the offsets hold, rows stay in [0, rows) and
+  // the groups have no more than `rows` rows together.
+  {
+    long long rows_before = 0;
+    int tiles_before = 0;
+    for (int g0 = 0; g0 < p.G; g0 += kThreads) {
+      const int g = g0 + (int)threadIdx.x;
+      int n = 0, lo = 0;
       if (g < p.G) {
-        const int lo = p.offsets ? min(max(p.offsets[g], 0), p.rows) : 0;
-        const int hi = p.offsets ? min(max(p.offsets[g + 1], 0), p.rows) : p.rows;
-        n = max(hi - lo, 0);
+        lo = p.offsets ? min(max(p.offsets[g], 0), p.rows) : 0;
+        n = max((p.offsets ? min(max(p.offsets[g + 1], 0), p.rows) : p.rows) - lo, 0);
+      }
+      long long upto = n;  // rows of the warp's groups up to this one
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+      }
+      if (lane == 31) rows_sh[warp] = upto;
+      __syncthreads();
+      long long before = rows_before + upto - n;
+      for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) before += rows_sh[w];
+        rows_before += rows_sh[w];
+      }
+      n = (int)max(0ll, min((long long)n, p.rows - before));
+      int tiles = (n + kTN - 1) / kTN, to = tiles;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, to, o);
+        if (lane >= o) to += t;
+      }
+      if (lane == 31) tiles_sh[warp] = to;
+      __syncthreads();
+      int at = tiles_before + to - tiles;
+      for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) at += tiles_sh[w];
+        tiles_before += tiles_sh[w];
+      }
+      if (g < p.G) {
+        first_s[g] = at;
+        len_s[g] = n;
         start_s[g] = lo;
       }
-      long long before = n;  // rows of the groups up to this one
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, before, o);
-        if (lane >= o) before += t;
-      }
-      const long long all = __shfl_sync(0xffffffffu, before, 31);
-      n = (int)max(0ll, min((long long)n, left - (before - n)));
-      left = (int)max(0ll, left - all);
-      if (g < p.G) len_s[g] = n;
-      const int tiles = (n + kTN - 1) / kTN;
-      int inc = tiles;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      if (g < p.G) first_s[g] = sum + inc - tiles;
-      sum += __shfl_sync(0xffffffffu, inc, 31);
     }
-    if (lane == 0) first_s[p.G] = sum;
+    if (threadIdx.x == 0) first_s[p.G] = tiles_before;
   }
-  __syncwarp();
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
   const int n_items = first_s[p.G] * p.ch_tiles;
-  auto item_of = [&](int i) {
+  auto look_up = [&](int i) {
     const int tile = i / p.ch_tiles;
     int lo = 0, hi = p.G - 1;  // the last group whose first tile is <= tile
     while (lo < hi) {
@@ -251,23 +266,35 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (first_s[mid] <= tile) lo = mid; else hi = mid - 1;
     }
     Item it;
-    it.g = lo;
     it.ch0 = (i - tile * p.ch_tiles) * 128;
+    it.w0 = lo * p.N + it.ch0;
     const int tiles = first_s[lo + 1] - first_s[lo], rows = len_s[lo];
+    // the group's rows in equal parts, whole multiples of 16 rows
     const int part = ((rows + tiles - 1) / tiles + 15) & ~15;
     const int at = (tile - first_s[lo]) * part;
     it.row0 = start_s[lo] + at;
     it.rows = min(part, rows - at);
     return it;
   };
+  for (int k = threadIdx.x; k < kListed; k += kThreads) {
+    const long long i = blockIdx.x + (long long)k * gridDim.x;
+    if (i < n_items) list_s[k] = look_up((int)i);
+  }
+  // the k-th item of this CTA, i = blockIdx.x + k gridDim.x
+  auto item_of = [&](int i, int k) { return k < kListed ? list_s[k] : look_up(i); };
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
 
   if (warp < kEpiWarps) {
     // ---------------- accumulators to the output ----------------------------
     const int q = warp & 3, half = warp >> 2;
     int acc = 0;
     uint32_t ph = 0;
-    for (int i = blockIdx.x; i < n_items; i += gridDim.x) {
-      const Item it = item_of(i);
+    for (int i = blockIdx.x, k = 0; i < n_items; i += gridDim.x, ++k) {
+      const Item it = item_of(i, k);
       if (!wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit)) break;
       tc_fence_after();
       const int chunks = (it.rows + 31) / 32;
@@ -294,19 +321,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0;
       uint32_t ph = 0;
       long long issued = 0;
-      for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
-        const Item it = item_of(i);
+      for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+        const Item it = item_of(i, k);
         const bool large = it.rows > 2 * kBoxM, small = it.rows <= kBoxS, two = !large && it.rows > kBoxM;
         const CUtensorMap* map = large ? &tmA : small ? &tmAS : &tmAM;
         const uint32_t bytes =
             kBytesW + 128u * (uint32_t)(large ? kTN : small ? kBoxS : two ? 2 * kBoxM : kBoxM);
-        const int w0 = it.g * p.N + it.ch0;
         for (int kb = 0; kb < p.num_kb; ++kb) {
           ok = wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
           if (!ok) break;
           const uint32_t bar = full_bar(s);
           mbar_expect_tx(bar, bytes);
-          tma_load_2d(stage(s), &tmW, bar, kb * 64, w0);
+          tma_load_2d(stage(s), &tmW, bar, kb * 64, it.w0);
           tma_load_2d(stage(s) + kBytesW, map, bar, kb * 64, it.row0);
           if (two) tma_load_2d(stage(s) + kBytesW + kBoxM * 128u, map, bar, kb * 64, it.row0 + kBoxM);
           ++issued;
@@ -326,23 +352,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       int sb = 0;  // scale buffer and its phase
       uint32_t sb_ph = 0;
       bool ok = true, any = false;
-      for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
-        const Item it = item_of(i);
+      for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+        const Item it = item_of(i, k);
         ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
         if (!ok) break;
         tc_fence_after();
         const int n = (it.rows + 15) & ~15;
         const uint32_t d = tmem + acc * kAcc;
         const uint32_t id0 = idesc_mxf4(n, 0), id2 = idesc_mxf4(n, 2);
-        for (int kb = 0; kb < p.num_kb; ++kb) {
-          if ((kb & 1) == 0)
-            ok = wait_bounded(sfull_bar(sb), sb_ph, abort_flag, p.status, p.wait_limit);
-          ok = ok && wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
-          if (!ok) break;
+        // One step; h: its half of the scale buffer.
+        auto step = [&](const int kb, const uint32_t h) {
+          if (!wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit)) return false;
           tc_fence_after();
-          const uint32_t sc = sc0 + sb * kBytesS + (kb & 1) * 1024u;
+          const uint32_t sc = sc0 + sb * kBytesS + h * 1024u;
           const uint32_t tw = tmem + kScaleCol + s * kScaleCols, ta = tw + 8;
-          const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW + (kb & 1) * 1024u);
+          const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW + h * 1024u);
           copy_scales(tw, dw);
           copy_scales(tw + 4, dw + (512 >> 4));
           copy_scales(ta, da);
@@ -358,14 +382,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_mxf4(d, w + 2 * k, a + 2 * k, (k & 1) ? id2 : id0, tw + 4 * (k >> 1),
                      ta + 8 * (k >> 1), (kb | k) != 0 ? 1u : 0u);
           umma_commit(empty_bar(s));
-          if ((kb & 1) || kb == p.num_kb - 1) {
-            umma_commit(sempty_bar(sb));
-            if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
-          }
-          if (kb == p.num_kb - 1) umma_commit(accf_bar(acc));
           any = true;
           if (++s == kStages) { s = 0; ph ^= 1u; }
+          return true;
+        };
+        for (int kb = 0; kb < p.num_kb; kb += 2) {
+          ok = wait_bounded(sfull_bar(sb), sb_ph, abort_flag, p.status, p.wait_limit) && step(kb, 0);
+          if (ok && kb + 1 < p.num_kb) ok = step(kb + 1, 1);
+          if (!ok) break;
+          umma_commit(sempty_bar(sb));
+          if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
         }
+        if (ok) umma_commit(accf_bar(acc));
         if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
       }
       // every MMA issued has completed before TMEM is released
@@ -384,9 +412,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     int sb = 0;
     uint32_t sb_ph = 0;
     bool ok = true;
-    for (int i = blockIdx.x; i < n_items && ok; i += gridDim.x) {
-      const Item it = item_of(i);
-      const uint8_t* ws = p.w_scales + ((long long)it.g * p.N + it.ch0 + r0) * p.pitch + 8 * h;
+    for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+      const Item it = item_of(i, k);
+      const uint8_t* ws = p.w_scales + ((long long)it.w0 + r0) * p.pitch + 8 * h;
       const uint8_t* as = p.a_scales + ((long long)it.row0 + r0) * p.pitch + 8 * h;
       for (int kb = 0; kb < p.num_kb; kb += 2) {
         const bool in = kb + h < p.num_kb;
