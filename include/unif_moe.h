@@ -419,9 +419,9 @@ UNIF_MOE_API int unif_moe_group_noalloc(int T, int n_experts, int n_blocks,
 /* ---- Operators round the layer ----
  * They need no handle, allocate nothing and keep no state between calls: all
  * memory is the caller's, on the current device. Row strides (ld_*) count
- * elements and are at least the width; rows that are 16-byte aligned and a
- * multiple of 8 elements wide and apart are moved in 16-byte accesses, others
- * element by element. The paper has no counterpart of them; its backbones hold
+ * elements and are at least the width; rows that start at a multiple of 8
+ * elements and are a multiple of 8 elements wide and apart are moved eight
+ * elements at a time, others one by one. The paper has no counterpart of them; its backbones hold
  * the layer in Transformer blocks, which need them beside it. */
 
 enum { UNIF_MOE_NORM_NONE = 0, UNIF_MOE_NORM_LAYER = 1, UNIF_MOE_NORM_RMS = 2 };

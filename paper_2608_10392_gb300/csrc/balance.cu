@@ -6,7 +6,8 @@
 //   loss = w_b balance + w_z zloss
 //   dloss/dz_tj = p_tj / n (w_b K (f_j - sum_i f_i p_ti) + 2 w_z lse(z_t))
 //
-// The gradient needs the counts of all tokens, so there are two kernels: the
+// The gradient needs the counts of all tokens. Where a cluster of CTAs holds all
+// of them at once, one kernel does it; otherwise there are two: the
 // first leaves each CTA's sums in the workspace, the second adds them (in the
 // CTAs' order: results do not change from run to run) and writes the gradient
 // from a second reading of the logits, which the first left in L2.
@@ -80,6 +81,22 @@ __device__ __forceinline__ void load(const Args& a, bool in, int t, int lane, fl
   } else {
 #pragma unroll
     for (int i = 0; i < E; ++i) z[i] = in && lane * E + i < a.K ? to_float(p[i]) : -INFINITY;
+  }
+}
+
+template <int E, bool VEC>
+__device__ __forceinline__ void store(const Args& a, long long t, int lane, const float (&v)[E]) {
+  float* to = a.dlogits + t * a.K + lane * E;
+#pragma unroll
+  for (int i = 0; i < E; i += 4) {
+    if (VEC) {
+      if (lane * E + i < a.K)
+        *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else {
+#pragma unroll
+      for (int k = i; k < i + 4; ++k)
+        if (lane * E + k < a.K) to[k] = v[k];
+    }
   }
 }
 
@@ -299,37 +316,231 @@ __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
       const float g = fmaf(wz, top + logf(sum), -wb * fp);
 #pragma unroll
       for (int i = 0; i < E; ++i) e[u][i] = valid ? e[u][i] * inv_n * fmaf(wb, fr[i], g) : 0.f;
-      if (tt < a.T) {
-        float* to = a.dlogits + tt * a.K + lane * E;
+      if (tt < a.T) store<E, VEC>(a, tt, lane, e[u]);
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t of_rank(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint32_t read_rank(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+                   : "memory");
+}
+
+// The whole call in one kernel, where a cluster of up to eight CTAs holds all
+// tokens' probabilities in its registers (U tokens per group of lanes): the CTAs
+// read one another's column sums from shared memory. Two kernels cost a second
+// launch and a second reading (12,608 tokens of 8 experts: 10.4 us).
+template <typename T, int L, int E, bool VEC, int TH, int U>
+__global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
+  constexpr int kWarps = TH / 32, kTok = TH / L;
+  extern __shared__ float sh[];  // [kWarps][K] shares; then [K] sums, [K] counts, [K] f
+  __shared__ float z_sh[kWarps], zsum;
+  __shared__ int n_sh[kWarps], all[2], mine[2];
+  float* sum_p = sh + kWarps * a.K;
+  int* cnt = reinterpret_cast<int*>(sum_p + a.K);
+  float* f = sum_p + 2 * a.K;
+  const int lane = threadIdx.x % L, tok = threadIdx.x / L, warp = threadIdx.x / 32,
+            lane32 = threadIdx.x & 31;
+  const uint32_t ranks = gridDim.x;  // one cluster
+  for (int i = threadIdx.x; i < a.K; i += TH) cnt[i] = 0;
+  if (threadIdx.x < 2) all[threadIdx.x] = 0;
+  float z[U][E], lse[U];
+  int m[U], q0[U];
+  bool in[U];
 #pragma unroll
-        for (int i = 0; i < E; i += 4) {
-          if (VEC) {
-            if (lane * E + i < a.K)
-              *reinterpret_cast<float4*>(to + i) =
-                  make_float4(e[u][i], e[u][i + 1], e[u][i + 2], e[u][i + 3]);
-          } else {
+  for (int u = 0; u < U; ++u) {
+    const int t0 = (u * (int)ranks + (int)blockIdx.x) * kTok + tok;
+    in[u] = t0 < a.T && (!a.mask || a.mask[t0]);
+    const int t = in[u] ? t0 : 0;
+    load<T, L, E, VEC>(a, in[u], t, lane, z[u]);
+    m[u] = a.n_q;
+    q0[u] = -1;
+    if (in[u]) {
+      if (a.k) m[u] = min(m[u], a.k[t]);
+      if (lane < a.n_q) q0[u] = a.q[(long long)t * a.ld_q + lane];
+    }
+  }
+  __syncthreads();
+  float p[E], zs = 0.f;
+  int n = 0;
 #pragma unroll
-            for (int k = i; k < i + 4; ++k)
-              if (lane * E + k < a.K) to[k] = e[u][k];
-          }
-        }
+  for (int i = 0; i < E; ++i) p[i] = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float top, sum;
+    in[u] = softmax<L, E>(in[u], z[u], top, sum);
+    const float inv = 1.f / sum;
+    lse[u] = top + logf(sum);
+#pragma unroll
+    for (int i = 0; i < E; ++i) z[u][i] *= inv;
+    if (in[u]) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) p[i] += z[u][i];
+      if (lane == 0) {
+        zs = fmaf(lse[u], lse[u], zs);
+        ++n;
+      }
+      const long long t = (u * (int)ranks + (int)blockIdx.x) * kTok + tok;
+      int j = q0[u];
+      for (int i = lane; i < m[u]; i += L) {
+        if (i != lane) j = a.q[t * a.ld_q + i];
+        if (j >= 0 && j < a.K) atomicAdd(&cnt[j], 1);
       }
     }
+  }
+  // the groups of a warp, the warps, then the CTAs, in a fixed order
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+#pragma unroll
+    for (int o = L; o < 32; o <<= 1) p[i] += __shfl_xor_sync(0xffffffffu, p[i], o);
+    const int c = lane * E + i;
+    if (lane32 < L && c < a.K) sh[warp * a.K + c] = p[i];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    zs += __shfl_xor_sync(0xffffffffu, zs, o);
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+  }
+  if (lane32 == 0) {
+    z_sh[warp] = zs;
+    n_sh[warp] = n;
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.K; c += TH) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int w = 0; w < kWarps; ++w) s += sh[w * a.K + c];
+    sum_p[c] = s;
+  }
+  if (warp == kWarps - 1) {
+    float s = lane32 < kWarps ? z_sh[lane32] : 0.f;
+    int k = lane32 < kWarps ? n_sh[lane32] : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      k += __shfl_xor_sync(0xffffffffu, k, o);
+    }
+    if (lane32 == 0) {
+      mine[0] = __float_as_int(s);
+      mine[1] = k;
+    }
+  }
+  cluster_sync();
+  const bool first = blockIdx.x == 0;
+  int total = 0;
+  for (int c = threadIdx.x; c < a.K; c += TH) {
+    int k = 0;
+    float s = 0.f;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      k += (int)read_rank(of_rank(cnt + c, r));
+      if (first) s += __uint_as_float(read_rank(of_rank(sum_p + c, r)));
+    }
+    f[c] = __int_as_float(k);
+    total += k;
+    if (first) {
+      a.counts[c] = k;
+      sh[c] = s;  // (the shares have been added)
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  if (lane32 == 0) atomicAdd(&all[0], total);
+  if (threadIdx.x == TH - 1) {
+    int k = 0;
+    float s = 0.f;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      s += __uint_as_float(read_rank(of_rank(&mine[0], r)));
+      k += (int)read_rank(of_rank(&mine[1], r));
+    }
+    zsum = s;
+    all[1] = k;
+  }
+  cluster_sync();  // nothing is read from another CTA any more; all of this CTA's is written
+  const float inv_c = 1.f / (float)max(all[0], 1), inv_n = 1.f / (float)max(all[1], 1);
+  if (first && warp == 0) {
+    float b = 0.f;
+    for (int c = lane32; c < a.K; c += 32) {
+      const float q = sh[c] * inv_n;
+      a.prob[c] = q;
+      b = fmaf((float)__float_as_int(f[c]) * inv_c, q, b);
+    }
+    b = lanes_sum<32>(b) * (float)a.K;
+    if (lane32 == 0) {
+      const float zl = zsum * inv_n;
+      a.loss[0] = fmaf(a.w_b, b, a.w_z * zl);
+      a.loss[1] = b;
+      a.loss[2] = zl;
+    }
+  }
+  if (!a.dlogits) return;
+  const float wb = a.w_b * (float)a.K, wz = 2.f * a.w_z;
+  float fr[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    fr[i] = lane * E + i < a.K ? (float)__float_as_int(f[lane * E + i]) * inv_c : 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = (u * (int)ranks + (int)blockIdx.x) * kTok + tok;
+    float fp = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) fp = fmaf(fr[i], z[u][i], fp);
+    fp = lanes_sum<L>(fp);
+    const float g = fmaf(wz, lse[u], -wb * fp);
+#pragma unroll
+    for (int i = 0; i < E; ++i) z[u][i] = in[u] ? z[u][i] * inv_n * fmaf(wb, fr[i], g) : 0.f;
+    if (t < a.T) store<E, VEC>(a, t, lane, z[u]);
   }
 }
 
 constexpr int kWide = 128;  // up to this many experts: CTAs of 1,024 threads
 inline int threads_of(int K) { return K <= kWide ? 1024 : 256; }
 
+// Lanes per token, and tokens that a cluster of eight CTAs holds at once (those of
+// cluster_kernel's instances).
+int lanes_of(int K) {
+  return K <= 4 ? 1 : K <= 8 ? 2 : K <= 16 ? 4 : K <= 32 ? 8 : K <= 64 ? 16 : 32;
+}
+bool in_cluster(int T, int K) {
+  return T <= 8ll * (K <= 256 ? 4 : 2) * (threads_of(K) / lanes_of(K));
+}
+
 // CTAs of both kernels: at most one per SM, so that the second has few sums to add.
 int cta_count(int T, int K, int sms) {
-  const int lanes = K <= 4 ? 1 : K <= 8 ? 2 : K <= 16 ? 4 : K <= 32 ? 8 : K <= 64 ? 16 : 32;
-  const long long tok = threads_of(K) / lanes, want = ((long long)T + tok - 1) / tok;
+  const long long tok = threads_of(K) / lanes_of(K), want = ((long long)T + tok - 1) / tok;
   return (int)(want < 1 ? 1 : want > sms ? sms : want);
 }
 
 template <typename T, int L, int E, bool VEC, int TH, int U>
 cudaError_t launch_as(const Args& a, cudaStream_t s) {
+  const long long once = (long long)U * (TH / L);  // tokens that a CTA holds at once
+  if (in_cluster(a.T, a.K)) {
+    unsigned ctas = 1;  // 1, 2, 4 or 8
+    while (ctas * once < a.T) ctas *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(TH);
+    cfg.dynamicSmemBytes = (size_t)(TH / 32 + 3) * a.K * sizeof(float);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, cluster_kernel<T, L, E, VEC, TH, U>, a);
+  }
   const size_t smem = (size_t)(TH / 32 * a.K + a.K) * sizeof(float);
   const size_t smem2 = (size_t)(2 * a.K) * sizeof(float);
   sums_kernel<T, L, E, VEC, TH, U><<<a.ctas, TH, smem, s>>>(a);
@@ -387,7 +598,7 @@ int64_t unif_moe_balance_workspace(int T, int K) {
   int sms = 0;
   if (unif::sm_count(&sms) != UNIF_MOE_OK) return -1;
   int64_t at[4];
-  return bl::layout(K, bl::cta_count(T, K, sms), at);
+  return bl::in_cluster(T, K) ? 0 : bl::layout(K, bl::cta_count(T, K, sms), at);
 }
 
 int unif_moe_balance_loss(int T, int K, const void* logits, unif_moe_dtype dtype, int64_t ld,
@@ -417,9 +628,9 @@ int unif_moe_balance_loss(int T, int K, const void* logits, unif_moe_dtype dtype
   if (rs != UNIF_MOE_OK) return rs;
   bl::Args a{};
   a.ctas = bl::cta_count(T, K, sms);
-  int64_t at[4];
-  const int64_t need = bl::layout(K, a.ctas, at);
-  if (!workspace || workspace_bytes < need) {
+  int64_t at[4] = {};
+  const int64_t need = bl::in_cluster(T, K) ? 0 : bl::layout(K, a.ctas, at);
+  if (workspace_bytes < need || (need && !workspace)) {
     set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
     return UNIF_MOE_ERR_CAPACITY;
   }

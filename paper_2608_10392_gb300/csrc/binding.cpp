@@ -317,15 +317,17 @@ PyObject* balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const uint8_t* mask = mask_of(at, tensor(a[3], "mask"), T);
     const int64_t need = unif_moe_balance_workspace((int)T, (int)K);
     if (need < 0) check(K > UNIF_MOE_BALANCE_MAX_EXPERTS ? UNIF_MOE_ERR_SHAPE : UNIF_MOE_ERR_ARG);
-    const Tensor ws = at.empty({need}, at::kByte), loss = at.empty({3}, at::kFloat),
-                 counts = at.empty({K}, at::kInt), prob = at.empty({K}, at::kFloat);
+    Tensor ws;
+    if (need) ws = at.empty({need}, at::kByte);
+    const Tensor loss = at.empty({3}, at::kFloat), counts = at.empty({K}, at::kInt), prob = at.empty({K}, at::kFloat);
     Tensor d;
     if (a[6] == Py_True) d = at.empty({T, K}, at::kFloat);
     check(unif_moe_balance_loss(
         (int)T, (int)K, pz.p, (unif_moe_dtype)type, pz.ld, static_cast<const int32_t*>(pq.p), (int)n_q,
         pq.ld, static_cast<const int32_t*>(k), mask, (float)as_double(a[4]), (float)as_double(a[5]),
         loss.data_ptr<float>(), counts.data_ptr<int32_t>(), prob.data_ptr<float>(),
-        d.defined() ? d.data_ptr<float>() : nullptr, ws.data_ptr(), need, at.stream(a[7])));
+        d.defined() ? d.data_ptr<float>() : nullptr, need ? ws.data_ptr() : nullptr, need,
+        at.stream(a[7])));
     PyObject* r = PyDict_New();
     if (!r) throw Raised();
     try {

@@ -33,8 +33,8 @@ struct Raw<__nv_bfloat16> {
   uint4 a;
 };
 
-// VEC: thread j of a group holds columns 8 j .. 8 j + 7 (16-byte accesses);
-// otherwise columns j, j + n, j + 2 n, ... of n threads.
+// VEC: thread j of a group holds columns 8 j .. 8 j + 7 (one access of 16 bytes of bf16
+// or 32 of fp32: whole sectors); otherwise columns j, j + n, j + 2 n, ... of n threads.
 template <bool VEC>
 __device__ __forceinline__ int column(int j, int n, int i) {
   return VEC ? j * kE + i : i * n + j;
@@ -57,13 +57,14 @@ __device__ __forceinline__ void unpack(const uint4& r, float (&v)[kE]) {
 template <bool VEC>
 __device__ __forceinline__ void load(const float* p, int j, int n, int d, float (&v)[kE]) {
   if (VEC) {
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-    if (j * kE < d) {
-      a = *reinterpret_cast<const float4*>(p + j * kE);
-      b = *reinterpret_cast<const float4*>(p + j * kE + 4);
-    }
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = 0.f;
+    if (j * kE < d)
+      asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]),
+                     "=f"(v[6]), "=f"(v[7])
+                   : "l"(p + j * kE)
+                   : "memory");
   } else {
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
@@ -89,10 +90,11 @@ __device__ __forceinline__ void load(const __nv_bfloat16* p, int j, int n, int d
 template <bool VEC>
 __device__ __forceinline__ void store(float* p, int j, int n, int d, const float (&v)[kE]) {
   if (VEC) {
-    if (j * kE < d) {
-      *reinterpret_cast<float4*>(p + j * kE) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + j * kE + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    }
+    if (j * kE < d)
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + j * kE),
+                   "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]),
+                   "f"(v[7])
+                   : "memory");
   } else {
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
@@ -893,7 +895,7 @@ Plan plan_backward(const unif_moe_block_norm* p, bool gate, int sms) {
 
 template <typename T>
 bool vec_ok(const T* p, long long ld) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % kE == 0;
+  return reinterpret_cast<uintptr_t>(p) % (kE * sizeof(T)) == 0 && ld % kE == 0;
 }
 
 template <typename TX, typename TB, bool VEC>
@@ -1015,11 +1017,11 @@ cudaError_t backward_as(const unif_moe_block_norm* p, const Plan& pl, const void
   for (int i = 0; i < 4; ++i) a.wanted |= to[i] ? 1 << i : 0;
   a.wanted |= d_gate ? 16 : 0;
   a.pieces = pl.pieces; a.run = pl.run;
-  auto ok = [](const void* q, long long ld) { return !q || vec_ok(static_cast<const char*>(q), ld); };
+  auto ok = [](const auto* q, long long ld) { return !q || vec_ok(q, ld); };
   // d_gate is written a gate row at a time by the CTA that holds it
-  const bool vec = a.d % kE == 0 && ok(o, ld_o) && ok(y, ld_y) && ok(dout, ld_dout) &&
-                   ok(du, ld_du) && ok(dx, ld_dx) && ok(dy, ld_dy) && ok(w_post, 0) &&
-                   ok(b_post, 0) && ok(gate, 0) && ok(w_pre, 0) && ok(d_gate, 0) && ok(ws, 0);
+  const bool vec = a.d % kE == 0 && ok(a.o, ld_o) && ok(a.y, ld_y) && ok(a.dout, ld_dout) &&
+                   ok(a.du, ld_du) && ok(a.dx, ld_dx) && ok(a.dy, ld_dy) && ok(a.w_post, 0) &&
+                   ok(a.b_post, 0) && ok(a.gate, 0) && ok(a.w_pre, 0) && ok(d_gate, 0) && ok(ws, 0);
   cudaError_t e = vec ? launch_bwd<TX, TB, true>(a, pl.ctas, s)
                       : launch_bwd<TX, TB, false>(a, pl.ctas, s);
   const bool gates = d_gate && pl.pieces > 1;
