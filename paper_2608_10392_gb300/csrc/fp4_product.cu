@@ -104,6 +104,7 @@ struct __align__(16) Item {
   int w0, ch0, row0, rows;  // first weight row of the group and channels, first channel; rows >= 1
 };
 
+// The first `rows` (at most 32) rows of a chunk, one channel per lane.
 template <typename TO, bool GELU>
 __device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int row0, int rows, int ch,
                                             int lane) {
@@ -297,7 +298,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Item it = item_of(i, k);
       if (!wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit)) break;
       tc_fence_after();
-      const int chunks = (it.rows + 31) / 32;
+      // (a quarter past the last channel has nothing to store)
+      const int ch = it.ch0 + q * 32, chunks = ch < p.N ? (it.rows + 31) / 32 : 0;
       const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16);
       float v[32];
       for (int c = half; c < chunks; c += 2) {
@@ -306,7 +308,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           if (lane == 0) mbar_arrive(acce_bar(acc));
         }
-        store_chunk<TO, GELU>(p, v, it.row0 + c * 32, it.rows - c * 32, it.ch0 + q * 32 + lane, lane);
+        const int row0 = it.row0 + c * 32, rows = it.rows - c * 32;
+        store_chunk<TO, GELU>(p, v, row0, rows, ch + lane, lane);
       }
       if (half >= chunks && lane == 0) mbar_arrive(acce_bar(acc));
       if (++acc == 2) { acc = 0; ph ^= 1u; }
