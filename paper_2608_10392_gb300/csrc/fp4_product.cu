@@ -27,15 +27,20 @@ constexpr int kTN = 192;         // rows of a tile (MMA N)
 constexpr int kStep = 256;       // columns of a step: 128 bytes of codes, 8 scales
 // Stages of the ring; fewer where the table of groups (from about 670 on) needs the room.
 constexpr int kMaxStages = 5, kFewStages = 3;
-constexpr uint32_t kBytesW = 128 * 128, kBytesA = kTN * 128;
-constexpr uint32_t kStageBytes = kBytesW + kBytesA;
+constexpr uint32_t kBytesW = 128 * 128;
+// Row codes of a stage: the tile's rows, or with PAIR this CTA's half of them.
+__host__ __device__ constexpr int stage_rows(bool pair) { return pair ? kTN / 2 : kTN; }
+__host__ __device__ constexpr uint32_t stage_bytes(bool pair) {
+  return kBytesW + (uint32_t)stage_rows(pair) * 128u;
+}
 // Scales of two steps: 512-byte blocks [step][128 columns][weights | rows 0-127, rows 128-191].
 constexpr int kScaleBufs = 3;
 constexpr uint32_t kBytesSW = 4 * 512, kBytesSA = 8 * 512, kBytesS = kBytesSW + kBytesSA;
 constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 4;
 constexpr int kThreads = 32 * (kScaleWarp + kScaleWarps);
-// Rows of the TMA boxes of A: one box where the tile has at most 16 or 64 rows or
-// more than 128, else two of 64. (Six boxes of 32 took the loader 970 cycles a step.)
+// Rows of the smaller TMA boxes of A (half of these with PAIR): one box where the
+// tile has at most 16 or 64 rows or more than 128, else two of 64. (Six boxes of 32
+// took the loader 970 cycles a step.)
 constexpr int kBoxS = 16, kBoxM = 64;
 // TMEM columns: two accumulators, then the scales of each stage.
 constexpr uint32_t kAcc = kTN, kScaleCol = 2 * kTN, kScaleCols = 24, kTmemCols = 512;
@@ -46,7 +51,7 @@ constexpr int kListed = 256;
 constexpr int kBars = 2 * kMaxStages + 5 + 2 * kScaleBufs;
 
 struct Params {
-  int rows, N, G, num_kb, ch_tiles;
+  int rows, N, G, num_kb;
   const int32_t* offsets;   // [G + 1], or NULL: one group of all rows
   const uint8_t* a_scales;
   const uint8_t* w_scales;
@@ -58,24 +63,37 @@ struct Params {
   long long wait_limit;
 };
 
-__host__ __device__ constexpr uint32_t smem_bytes(int stages, int G) {
-  return 1024u + stages * kStageBytes + kScaleBufs * kBytesS + (kBars + 1) * 8u + kListed * 16u +
+__host__ __device__ constexpr uint32_t smem_bytes(bool pair, int stages, int G) {
+  return 1024u + stages * stage_bytes(pair) + kScaleBufs * kBytesS + (kBars + 1) * 8u + kListed * 16u +
          (uint32_t)(3 * G + 1) * 4u + 32u;
 }
 
+template <bool PAIR>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
                                          uint32_t sa, uint32_t sb, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::
-          "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
-      : "memory");
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::
+            "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::
+            "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
 }
 // A 512-byte block of scales (32 x 16 bytes) to four TMEM columns, in all four
-// lane quarters.
+// lane quarters; with PAIR in both CTAs, each from its own shared memory.
+template <bool PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  if (PAIR)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 // Descriptor of such a block: no swizzle, 8-row groups of 16-byte rows 128 bytes apart.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
@@ -83,15 +101,15 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
          ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
 }
 // Instruction descriptor of kind mxf4: A and B E2M1 (bits 7-9, 10-12 = 1), N >> 3
-// at bits 17-22, scales E8M0 (bit 23), M >> 7 at bits 27-28; bits 4-5 and 29-30
+// at bits 17-22, scales E8M0 (bit 23), M >> 7 (1, or 2 with PAIR) at bits 27-28; bits 4-5 and 29-30
 // pick the byte of a TMEM word at which B's and A's scales start (0 or 2).
-__device__ __forceinline__ uint32_t idesc_mxf4(int n, int scale_byte) {
+__device__ __forceinline__ uint32_t idesc_mxf4(bool pair, int n, int scale_byte) {
   return ((uint32_t)scale_byte << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
-         (1u << 23) | (1u << 27) | ((uint32_t)scale_byte << 29);
+         (1u << 23) | ((pair ? 2u : 1u) << 27) | ((uint32_t)scale_byte << 29);
 }
 
 constexpr uint32_t kSmemMax = 232448;  // shared memory that a CTA can have
-static_assert(smem_bytes(kFewStages, UNIF_MOE_MXFP4_MAX_GROUPS) <= kSmemMax, "shared memory");
+static_assert(smem_bytes(false, kFewStages, UNIF_MOE_MXFP4_MAX_GROUPS) <= kSmemMax, "shared memory");
 
 __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long long limit) {
   const long long t0 = clock64();
@@ -99,7 +117,7 @@ __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long 
     if (clock64() - t0 > limit) return;
 }
 
-// Items of the walk: a run of a group's rows and 128 of its channels.
+// Items of the walk: a run of a group's rows and 128 (PAIR: 256) of its channels.
 struct __align__(16) Item {
   int w0, ch0, row0, rows;  // first weight row of the group and channels, first channel; rows >= 1
 };
@@ -157,11 +175,19 @@ __device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int
   }
 }
 
-template <typename TO, bool GELU, int kStages>
+// PAIR: the CTAs of a cluster of two share an item (tcgen05 cta_group::2): 256 channels,
+// 128 of them and half of the rows' codes in each one's shared memory. The first CTA's
+// barriers take both CTAs' arrivals, its MMA lane issues for both.
+template <typename TO, bool GELU, int kStages, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                    const __grid_constant__ CUtensorMap tmAM, const __grid_constant__ CUtensorMap tmAS,
                    const Params p) {
+  constexpr uint32_t kStageBytes = stage_bytes(PAIR);
+  constexpr int kCtas = PAIR ? 2 : 1, kChannels = 128 * kCtas;
+  const uint32_t rank = PAIR ? cluster_rank() : 0u;
+  const bool leader = rank == 0;
+  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t s0 = smem_u32(smem);
@@ -193,10 +219,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(accf_bar(a), 1);
-      mbar_init(acce_bar(a), kEpiWarps);
+      mbar_init(acce_bar(a), kCtas * kEpiWarps);
     }
     for (int b = 0; b < kScaleBufs; ++b) {
-      mbar_init(sfull_bar(b), 32 * kScaleWarps);  // each thread for what it wrote
+      mbar_init(sfull_bar(b), kCtas * kScaleWarps);
       mbar_init(sempty_bar(b), 1);
     }
     mbar_init(mma_done, 1);
@@ -204,8 +230,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
-    tmem_relinquish();
+    if (PAIR) {
+      tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+      tmem_relinquish();
+    }
   }
   __shared__ long long rows_sh[kThreads / 32];
   __shared__ int tiles_sh[kThreads / 32];
@@ -258,16 +289,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) first_s[p.G] = tiles_before;
   }
   __syncthreads();
-  const int n_items = first_s[p.G] * p.ch_tiles;
+  const int ch_tiles = (p.N + kChannels - 1) / kChannels, n_items = first_s[p.G] * ch_tiles;
   auto look_up = [&](int i) {
-    const int tile = i / p.ch_tiles;
+    const int tile = i / ch_tiles;
     int lo = 0, hi = p.G - 1;  // the last group whose first tile is <= tile
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (first_s[mid] <= tile) lo = mid; else hi = mid - 1;
     }
     Item it;
-    it.ch0 = (i - tile * p.ch_tiles) * 128;
+    it.ch0 = (i - tile * ch_tiles) * kChannels + 128 * (int)rank;  // this CTA's
     it.w0 = lo * p.N + it.ch0;
     const int tiles = first_s[lo + 1] - first_s[lo], rows = len_s[lo];
     // the group's rows in equal parts, whole multiples of 16 rows
@@ -278,23 +309,33 @@ __global__ void __launch_bounds__(kThreads, 1)
     return it;
   };
   for (int k = threadIdx.x; k < kListed; k += kThreads) {
-    const long long i = blockIdx.x + (long long)k * gridDim.x;
+    const long long i = unit + (long long)k * units;
     if (i < n_items) list_s[k] = look_up((int)i);
   }
-  // the k-th item of this CTA, i = blockIdx.x + k gridDim.x
+  // the k-th item of this CTA (pair), i = unit + k units
   auto item_of = [&](int i, int k) { return k < kListed ? list_s[k] : look_up(i); };
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync_all();  // both CTAs' barriers are set before either signals the other
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // Arrives at a barrier of the first CTA.
+  auto arrive_leader = [&](uint32_t bar) {
+    if (!PAIR || leader) mbar_arrive(bar);
+    else mbar_arrive_cluster(mapa_shared(bar, 0));
+  };
+  auto commit = [&](uint32_t bar) {  // at this barrier of the pair's CTAs
+    if (PAIR) umma_commit_pair(bar, 3);
+    else umma_commit(bar);
+  };
 
   if (warp < kEpiWarps) {
     // ---------------- accumulators to the output ----------------------------
     const int q = warp & 3, half = warp >> 2;
     int acc = 0;
     uint32_t ph = 0;
-    for (int i = blockIdx.x, k = 0; i < n_items; i += gridDim.x, ++k) {
+    for (int i = unit, k = 0; i < n_items; i += units, ++k) {
       const Item it = item_of(i, k);
       if (!wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit)) break;
       tc_fence_after();
@@ -306,12 +347,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_ld32(from + c * 32, v);
         if (c + 2 >= chunks) {
           tc_fence_before();
-          if (lane == 0) mbar_arrive(acce_bar(acc));
+          if (lane == 0) arrive_leader(acce_bar(acc));
         }
         const int row0 = it.row0 + c * 32, rows = it.rows - c * 32;
         store_chunk<TO, GELU>(p, v, row0, rows, ch + lane, lane);
       }
-      if (half >= chunks && lane == 0) mbar_arrive(acce_bar(acc));
+      if (half >= chunks && lane == 0) arrive_leader(acce_bar(acc));
       if (++acc == 2) { acc = 0; ph ^= 1u; }
     }
   } else if (warp == kTmaWarp) {
@@ -324,45 +365,52 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0;
       uint32_t ph = 0;
       long long issued = 0;
-      for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+      for (int i = unit, k = 0; i < n_items && ok; i += units, ++k) {
         const Item it = item_of(i, k);
-        const bool large = it.rows > 2 * kBoxM, small = it.rows <= kBoxS, two = !large && it.rows > kBoxM;
+        // this CTA's rows of the tile
+        const int rows = PAIR ? ((it.rows + 15) & ~15) / 2 : it.rows, row0 = it.row0 + (int)rank * rows;
+        constexpr int kM = kBoxM / kCtas, kS = kBoxS / kCtas;
+        const bool large = rows > 2 * kM, small = rows <= kS, two = !large && rows > kM;
         const CUtensorMap* map = large ? &tmA : small ? &tmAS : &tmAM;
         const uint32_t bytes =
-            kBytesW + 128u * (uint32_t)(large ? kTN : small ? kBoxS : two ? 2 * kBoxM : kBoxM);
+            kBytesW + 128u * (uint32_t)(large ? stage_rows(PAIR) : small ? kS : two ? 2 * kM : kM);
+        auto load = [&](uint32_t dst, const CUtensorMap* from, uint32_t bar, int c0, int c1) {
+          if (PAIR) tma_load_2d_pair(dst, from, mapa_shared(bar, 0), c0, c1);
+          else tma_load_2d(dst, from, bar, c0, c1);
+        };
         for (int kb = 0; kb < p.num_kb; ++kb) {
           ok = wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
           if (!ok) break;
           const uint32_t bar = full_bar(s);
-          mbar_expect_tx(bar, bytes);
-          tma_load_2d(stage(s), &tmW, bar, kb * 64, it.w0);
-          tma_load_2d(stage(s) + kBytesW, map, bar, kb * 64, it.row0);
-          if (two) tma_load_2d(stage(s) + kBytesW + kBoxM * 128u, map, bar, kb * 64, it.row0 + kBoxM);
+          if (leader) mbar_expect_tx(bar, kCtas * bytes);
+          load(stage(s), &tmW, bar, kb * 64, it.w0);
+          load(stage(s) + kBytesW, map, bar, kb * 64, row0);
+          if (two) load(stage(s) + kBytesW + kM * 128u, map, bar, kb * 64, row0 + kM);
           ++issued;
           if (++s == kStages) { s = 0; ph ^= 1u; }
         }
       }
-      // loads still in flight land before the CTA exits
-      for (long long j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
+      // loads still in flight land before the CTA (pair) exits
+      for (long long j = issued > kStages ? issued - kStages : 0; leader && j < issued; ++j)
         wait_settle(full_bar((int)(j % kStages)), (uint32_t)((j / kStages) & 1), p.wait_limit / 16);
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
-    // ---------------- scales to TMEM, MMAs ----------------------------------
-    if (elect_one()) {
+    // ---------------- scales to TMEM, MMAs (the first CTA) ------------------
+    if (leader && elect_one()) {
       int s = 0, acc = 0;
       uint32_t ph = 0, acc_ph = 0;
       int sb = 0;  // scale buffer and its phase
       uint32_t sb_ph = 0;
       bool ok = true, any = false;
-      for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+      for (int i = unit, k = 0; i < n_items && ok; i += units, ++k) {
         const Item it = item_of(i, k);
         ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
         if (!ok) break;
         tc_fence_after();
         const int n = (it.rows + 15) & ~15;
         const uint32_t d = tmem + acc * kAcc;
-        const uint32_t id0 = idesc_mxf4(n, 0), id2 = idesc_mxf4(n, 2);
+        const uint32_t id0 = idesc_mxf4(PAIR, n, 0), id2 = idesc_mxf4(PAIR, n, 2);
         // One step; h: its half of the scale buffer.
         auto step = [&](const int kb, const uint32_t h) {
           if (!wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit)) return false;
@@ -370,21 +418,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t sc = sc0 + sb * kBytesS + h * 1024u;
           const uint32_t tw = tmem + kScaleCol + s * kScaleCols, ta = tw + 8;
           const uint64_t dw = scale_desc(sc), da = scale_desc(sc + kBytesSW + h * 1024u);
-          copy_scales(tw, dw);
-          copy_scales(tw + 4, dw + (512 >> 4));
-          copy_scales(ta, da);
-          copy_scales(ta + 8, da + (1024 >> 4));
+          copy_scales<PAIR>(tw, dw);
+          copy_scales<PAIR>(tw + 4, dw + (512 >> 4));
+          copy_scales<PAIR>(ta, da);
+          copy_scales<PAIR>(ta + 8, da + (1024 >> 4));
           if (n > 128) {
-            copy_scales(ta + 4, da + (512 >> 4));
-            copy_scales(ta + 12, da + (1536 >> 4));
+            copy_scales<PAIR>(ta + 4, da + (512 >> 4));
+            copy_scales<PAIR>(ta + 12, da + (1536 >> 4));
           }
           const uint64_t w = sw128_desc(stage(s)), a = sw128_desc(stage(s) + kBytesW);
           // 64 columns (32 bytes, two scales) at a time
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            mma_mxf4(d, w + 2 * k, a + 2 * k, (k & 1) ? id2 : id0, tw + 4 * (k >> 1),
+            mma_mxf4<PAIR>(d, w + 2 * k, a + 2 * k, (k & 1) ? id2 : id0, tw + 4 * (k >> 1),
                      ta + 8 * (k >> 1), (kb | k) != 0 ? 1u : 0u);
-          umma_commit(empty_bar(s));
+          commit(empty_bar(s));
           any = true;
           if (++s == kStages) { s = 0; ph ^= 1u; }
           return true;
@@ -393,15 +441,16 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = wait_bounded(sfull_bar(sb), sb_ph, abort_flag, p.status, p.wait_limit) && step(kb, 0);
           if (ok && kb + 1 < p.num_kb) ok = step(kb + 1, 1);
           if (!ok) break;
-          umma_commit(sempty_bar(sb));
+          commit(sempty_bar(sb));
           if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
         }
-        if (ok) umma_commit(accf_bar(acc));
+        if (ok) commit(accf_bar(acc));
         if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
       }
       // every MMA issued has completed before TMEM is released
       if (any) {
-        umma_commit(mma_done);
+        if (PAIR) umma_commit_pair(mma_done, 1);
+        else umma_commit(mma_done);
         wait_settle(mma_done, 0u, p.wait_limit);
       }
     }
@@ -415,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int sb = 0;
     uint32_t sb_ph = 0;
     bool ok = true;
-    for (int i = blockIdx.x, k = 0; i < n_items && ok; i += gridDim.x, ++k) {
+    for (int i = unit, k = 0; i < n_items && ok; i += units, ++k) {
       const Item it = item_of(i, k);
       const uint8_t* ws = p.w_scales + ((long long)it.w0 + r0) * p.pitch + 8 * h;
       const uint8_t* as = p.a_scales + ((long long)it.row0 + r0) * p.pitch + 8 * h;
@@ -453,7 +502,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           to[256] = a[r].y;
         }
         fence_proxy_async();
-        mbar_arrive(sfull_bar(sb));
+        __syncwarp();
+        if (lane == 0) arrive_leader(sfull_bar(sb));
         if (++sb == kScaleBufs) { sb = 0; sb_ph ^= 1u; }
       }
     }
@@ -462,25 +512,42 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+  if (PAIR) cluster_sync_all();
+  if (warp == kMmaWarp) {
+    if (PAIR) tmem_dealloc_pair(tmem, kTmemCols);
+    else tmem_dealloc(tmem, kTmemCols);
+  }
 }
 
-template <typename TO, bool GELU, int kStages>
+template <typename TO, bool GELU, int kStages, bool PAIR>
 cudaError_t launch_as(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, int grid,
-                   cudaStream_t s) {
-  const uint32_t smem = smem_bytes(kStages, p.G);
-  cudaError_t e = allow_smem_once(product_kernel<TO, GELU, kStages>, smem);
+                      cudaStream_t s) {
+  const uint32_t smem = smem_bytes(PAIR, kStages, p.G);
+  cudaError_t e = allow_smem_once(product_kernel<TO, GELU, kStages, PAIR>, smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(product_kernel<TO, GELU, kStages>, dim3(grid), dim3(kThreads), smem, s, tmW, tmA[0],
-                          tmA[1], tmA[2], p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = PAIR ? 2 : 1;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, product_kernel<TO, GELU, kStages, PAIR>, tmW, tmA[0], tmA[1], tmA[2], p);
 }
 
 template <typename TO, bool GELU>
-cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, int grid,
-                   cudaStream_t s) {
-  if (smem_bytes(kMaxStages, p.G) <= kSmemMax)
-    return launch_as<TO, GELU, kMaxStages>(tmW, tmA, p, grid, s);
-  return launch_as<TO, GELU, kFewStages>(tmW, tmA, p, grid, s);
+cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, bool pair,
+                   int grid, cudaStream_t s) {
+  if (pair) return launch_as<TO, GELU, kMaxStages, true>(tmW, tmA, p, grid, s);
+  if (smem_bytes(false, kMaxStages, p.G) <= kSmemMax)
+    return launch_as<TO, GELU, kMaxStages, false>(tmW, tmA, p, grid, s);
+  return launch_as<TO, GELU, kFewStages, false>(tmW, tmA, p, grid, s);
 }
 
 }  // namespace fp4p
@@ -529,18 +596,21 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   const int rc = unif::sm_count(&sms);
   if (rc != UNIF_MOE_OK) return rc;
   const uint64_t pitch = (uint64_t)(cols + 31) / 32 * 16;
+  const bool pair = n > 128 && rows >= 32ll * groups &&
+                    fpp::smem_bytes(true, fpp::kMaxStages, groups) <= fpp::kSmemMax;
+  const int ctas = pair ? 2 : 1;
   CUtensorMap tmW, tmA[3];  // 128-byte pieces of code rows, counted in 2-byte units
   if (!unif::encode_bf16_map(&tmW, w_codes, pitch / 2, (uint64_t)n * groups, 64, 128, 128) ||
-      !unif::encode_bf16_map(&tmA[0], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kTN, 128) ||
-      !unif::encode_bf16_map(&tmA[1], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxM, 128) ||
-      !unif::encode_bf16_map(&tmA[2], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxS, 128)) {
+      !unif::encode_bf16_map(&tmA[0], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::stage_rows(pair), 128) ||
+      !unif::encode_bf16_map(&tmA[1], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxM / ctas, 128) ||
+      !unif::encode_bf16_map(&tmA[2], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxS / ctas, 128)) {
     set_error("cuTensorMapEncodeTiled failed for the codes");
     return UNIF_MOE_ERR_CUDA;
   }
   fpp::Params p{};
   p.rows = (int)rows; p.N = n; p.G = groups;
   p.num_kb = (cols + fpp::kStep - 1) / fpp::kStep;
-  p.ch_tiles = (n + 127) / 128;
+  const int ch_tiles = (n + 128 * ctas - 1) / (128 * ctas);
   p.offsets = offsets;
   p.a_scales = a_scales; p.w_scales = w_scales;
   p.pitch = (cols + 255) / 256 * 8;
@@ -549,20 +619,20 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   p.status = status;
   p.wait_limit = unif::gemm_wait_limit();
   // at most one part-filled row tile per group beside the full ones
-  const int64_t most = ((int64_t)rows / fpp::kTN + (groups < rows ? groups : rows)) * p.ch_tiles;
+  const int64_t most = ((int64_t)rows / fpp::kTN + (groups < rows ? groups : rows)) * ch_tiles;
   if (most > 0x7fffffff) {
     set_error("too many tiles: rows=%lld n=%d groups=%d", (long long)rows, n, groups);
     return UNIF_MOE_ERR_SHAPE;
   }
-  const int grid = (int)(most < sms ? most : sms);
+  const int grid = ctas * (int)(most < sms / ctas ? most : sms / ctas);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   const bool gelu = activation == UNIF_MOE_ACTIVATION_GELU;
   if (dtype == UNIF_MOE_F32)
-    e = gelu ? fpp::launch<float, true>(tmW, tmA, p, grid, s) : fpp::launch<float, false>(tmW, tmA, p, grid, s);
+    e = gelu ? fpp::launch<float, true>(tmW, tmA, p, pair, grid, s) : fpp::launch<float, false>(tmW, tmA, p, pair, grid, s);
   else
-    e = gelu ? fpp::launch<__nv_bfloat16, true>(tmW, tmA, p, grid, s)
-             : fpp::launch<__nv_bfloat16, false>(tmW, tmA, p, grid, s);
+    e = gelu ? fpp::launch<__nv_bfloat16, true>(tmW, tmA, p, pair, grid, s)
+             : fpp::launch<__nv_bfloat16, false>(tmW, tmA, p, pair, grid, s);
   if (e != cudaSuccess) {
     set_error("mxfp4 product: %s", cudaGetErrorString(e));
     return UNIF_MOE_ERR_CUDA;
