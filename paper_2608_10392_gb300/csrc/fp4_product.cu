@@ -6,9 +6,9 @@
 // channels to a tile, and the rows the N operand, up to 192 to a tile: a tile
 // of few rows then costs few columns, whatever a group's size, and a lane of
 // the accumulator is a channel, so that 32 lanes store consecutive channels of
-// one row.
+// one row. (Where groups are large, rows can be M: see the rule at the launch.)
 //
-// One CTA per SM walks (row tile, channel tile) items, steps of 256 columns
+// One CTA per SM, or a pair of CTAs per two SMs, walks (row tile, channel tile) items, steps of 256 columns
 // through a ring of stages. Roles of the warps: 8 store accumulators, one loads
 // codes by TMA, one issues MMAs, 4 bring the scales: eight bytes a row and step,
 // read from row-major storage into registers and written as the 512-byte blocks
@@ -53,8 +53,8 @@ constexpr int kBars = 2 * kMaxStages + 5 + 2 * kScaleBufs;
 struct Params {
   int rows, N, G, num_kb;
   const int32_t* offsets;   // [G + 1], or NULL: one group of all rows
-  const uint8_t* a_scales;
-  const uint8_t* w_scales;
+  const uint8_t* m_scales;  // of the M operand, of the N operand
+  const uint8_t* n_scales;
   int pitch;                // scale bytes of a row
   void* out;
   long long ld;
@@ -117,10 +117,54 @@ __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long 
     if (clock64() - t0 > limit) return;
 }
 
-// Items of the walk: a run of a group's rows and 128 (PAIR: 256) of its channels.
+// Items of the walk: up to 128 entries of the M operand (for each CTA of a pair) and
+// up to kTN of the N operand; entries are rows or, of the weights, channels.
 struct __align__(16) Item {
-  int w0, ch0, row0, rows;  // first weight row of the group and channels, first channel; rows >= 1
+  int m0, n0;      // first entry of each operand, in its tensor; m0: this CTA's
+  int ch0;         // first output channel of the tile (this CTA's, where channels are M)
+  uint32_t sizes;  // entries: of M for this CTA (0 to 128), of N (1 to kTN) in the upper half
+  __device__ __forceinline__ int m() const { return (int)(sizes & 0xffffu); }
+  __device__ __forceinline__ int n() const { return (int)(sizes >> 16); }
 };
+
+__device__ __forceinline__ float gelu_erf(float y) {
+  return 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
+}
+
+// A row's `count` (at most 32) channels from `ch` on, one row per lane: whole
+// sectors, eight 32-bit words a store. (Sixteen channels that are not all there, at the
+// end of a row of odd width, are stored one by one.)
+template <bool GELU>
+__device__ __forceinline__ void store_row(const Params& p, float (&v)[32], int row, int ch, int count) {
+  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + (long long)row * p.ld + ch;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    uint32_t h[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = v[16 * g + 2 * j], b = v[16 * g + 2 * j + 1];
+      if (GELU) {
+        h[j] = gelu2_bf16x2(a, b);
+      } else {
+        __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+        h[j] = *reinterpret_cast<uint32_t*>(&t);
+      }
+    }
+    if (16 * g + 16 <= count) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o + 16 * g),
+                   "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]), "r"(h[4]), "r"(h[5]), "r"(h[6]),
+                   "r"(h[7])
+                   : "memory");
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const __nv_bfloat162 t = *reinterpret_cast<__nv_bfloat162*>(&h[j]);
+        if (16 * g + 2 * j < count) o[16 * g + 2 * j] = t.x;
+        if (16 * g + 2 * j + 1 < count) o[16 * g + 2 * j + 1] = t.y;
+      }
+    }
+  }
+}
 
 // The first `rows` (at most 32) rows of a chunk, one channel per lane.
 template <typename TO, bool GELU>
@@ -132,9 +176,7 @@ __device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
         if (j < rows) {
-          float y = v[j];
-          if (GELU) y = 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
-          *o = y;
+          *o = GELU ? gelu_erf(v[j]) : v[j];
         }
         o += p.ld;
       }
@@ -178,13 +220,16 @@ __device__ __forceinline__ void store_chunk(const Params& p, float (&v)[32], int
 // PAIR: the CTAs of a cluster of two share an item (tcgen05 cta_group::2): 256 channels,
 // 128 of them and half of the rows' codes in each one's shared memory. The first CTA's
 // barriers take both CTAs' arrivals, its MMA lane issues for both.
-template <typename TO, bool GELU, int kStages, bool PAIR>
+//
+// ROWS_M (bf16 output whose rows take 32-byte stores): the rows are the M operand and
+// the channels N; otherwise the channels are M.
+template <typename TO, bool GELU, int kStages, bool PAIR, bool ROWS_M>
 __global__ void __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                   const __grid_constant__ CUtensorMap tmAM, const __grid_constant__ CUtensorMap tmAS,
+    product_kernel(const __grid_constant__ CUtensorMap tmM, const __grid_constant__ CUtensorMap tmN,
+                   const __grid_constant__ CUtensorMap tmNM, const __grid_constant__ CUtensorMap tmNS,
                    const Params p) {
   constexpr uint32_t kStageBytes = stage_bytes(PAIR);
-  constexpr int kCtas = PAIR ? 2 : 1, kChannels = 128 * kCtas;
+  constexpr int kCtas = PAIR ? 2 : 1, kM = 128 * kCtas, kRowTile = ROWS_M ? kM : kTN;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
   const bool leader = rank == 0;
   const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
@@ -267,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         rows_before += rows_sh[w];
       }
       n = (int)max(0ll, min((long long)n, p.rows - before));
-      int tiles = (n + kTN - 1) / kTN, to = tiles;
+      int tiles = (n + kRowTile - 1) / kRowTile, to = tiles;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int t = __shfl_up_sync(0xffffffffu, to, o);
@@ -289,23 +334,36 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) first_s[p.G] = tiles_before;
   }
   __syncthreads();
-  const int ch_tiles = (p.N + kChannels - 1) / kChannels, n_items = first_s[p.G] * ch_tiles;
+  const int ch_tiles = ROWS_M ? (p.N + kTN - 1) / kTN : (p.N + kM - 1) / kM;
+  const int n_items = first_s[p.G] * ch_tiles;
+  // `total` entries in `parts` equal parts, whole multiples of 16
+  auto part_of = [](int total, int parts) { return ((total + parts - 1) / parts + 15) & ~15; };
   auto look_up = [&](int i) {
-    const int tile = i / ch_tiles;
+    const int tile = i / ch_tiles, ch = i - tile * ch_tiles;
     int lo = 0, hi = p.G - 1;  // the last group whose first tile is <= tile
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (first_s[mid] <= tile) lo = mid; else hi = mid - 1;
     }
+    const int k = tile - first_s[lo], rows = len_s[lo];
     Item it;
-    it.ch0 = (i - tile * ch_tiles) * kChannels + 128 * (int)rank;  // this CTA's
-    it.w0 = lo * p.N + it.ch0;
-    const int tiles = first_s[lo + 1] - first_s[lo], rows = len_s[lo];
-    // the group's rows in equal parts, whole multiples of 16 rows
-    const int part = ((rows + tiles - 1) / tiles + 15) & ~15;
-    const int at = (tile - first_s[lo]) * part;
-    it.row0 = start_s[lo] + at;
-    it.rows = min(part, rows - at);
+    int m, n;
+    if (ROWS_M) {
+      const int part = part_of(p.N, ch_tiles), at = k * kM + 128 * (int)rank;
+      m = min(max(rows - at, 0), 128);
+      it.m0 = start_s[lo] + min(at, rows);
+      it.ch0 = ch * part;
+      n = min(part, p.N - it.ch0);
+      it.n0 = lo * p.N + it.ch0;
+    } else {
+      const int part = part_of(rows, first_s[lo + 1] - first_s[lo]);
+      it.ch0 = ch * kM + 128 * (int)rank;
+      m = min(max(p.N - it.ch0, 0), 128);
+      it.m0 = lo * p.N + it.ch0;
+      it.n0 = start_s[lo] + k * part;
+      n = min(part, rows - k * part);
+    }
+    it.sizes = (uint32_t)m | (uint32_t)n << 16;
     return it;
   };
   for (int k = threadIdx.x; k < kListed; k += kThreads) {
@@ -339,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Item it = item_of(i, k);
       if (!wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit)) break;
       tc_fence_after();
-      // (a quarter past the last channel has nothing to store)
-      const int ch = it.ch0 + q * 32, chunks = ch < p.N ? (it.rows + 31) / 32 : 0;
+      // (a quarter past the last entry of M has nothing to store)
+      const int chunks = q * 32 < it.m() ? (it.n() + 31) / 32 : 0;
       const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16);
       float v[32];
       for (int c = half; c < chunks; c += 2) {
@@ -349,8 +407,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           if (lane == 0) arrive_leader(acce_bar(acc));
         }
-        const int row0 = it.row0 + c * 32, rows = it.rows - c * 32;
-        store_chunk<TO, GELU>(p, v, row0, rows, ch + lane, lane);
+        if (ROWS_M) {
+          if (q * 32 + lane < it.m())
+            store_row<GELU>(p, v, it.m0 + q * 32 + lane, it.ch0 + c * 32, it.n() - c * 32);
+        } else {
+          store_chunk<TO, GELU>(p, v, it.n0 + c * 32, it.n() - c * 32, it.ch0 + q * 32 + lane, lane);
+        }
       }
       if (half >= chunks && lane == 0) arrive_leader(acce_bar(acc));
       if (++acc == 2) { acc = 0; ph ^= 1u; }
@@ -367,13 +429,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       long long issued = 0;
       for (int i = unit, k = 0; i < n_items && ok; i += units, ++k) {
         const Item it = item_of(i, k);
-        // this CTA's rows of the tile
-        const int rows = PAIR ? ((it.rows + 15) & ~15) / 2 : it.rows, row0 = it.row0 + (int)rank * rows;
-        constexpr int kM = kBoxM / kCtas, kS = kBoxS / kCtas;
-        const bool large = rows > 2 * kM, small = rows <= kS, two = !large && rows > kM;
-        const CUtensorMap* map = large ? &tmA : small ? &tmAS : &tmAM;
+        // this CTA's entries of N
+        const int n = PAIR ? ((it.n() + 15) & ~15) / 2 : it.n(), n0 = it.n0 + (int)rank * n;
+        constexpr int kNM = kBoxM / kCtas, kNS = kBoxS / kCtas;
+        const bool large = n > 2 * kNM, small = n <= kNS, two = !large && n > kNM;
+        const CUtensorMap* map = large ? &tmN : small ? &tmNS : &tmNM;
         const uint32_t bytes =
-            kBytesW + 128u * (uint32_t)(large ? stage_rows(PAIR) : small ? kS : two ? 2 * kM : kM);
+            kBytesW + 128u * (uint32_t)(large ? stage_rows(PAIR) : small ? kNS : two ? 2 * kNM : kNM);
         auto load = [&](uint32_t dst, const CUtensorMap* from, uint32_t bar, int c0, int c1) {
           if (PAIR) tma_load_2d_pair(dst, from, mapa_shared(bar, 0), c0, c1);
           else tma_load_2d(dst, from, bar, c0, c1);
@@ -383,9 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           const uint32_t bar = full_bar(s);
           if (leader) mbar_expect_tx(bar, kCtas * bytes);
-          load(stage(s), &tmW, bar, kb * 64, it.w0);
-          load(stage(s) + kBytesW, map, bar, kb * 64, row0);
-          if (two) load(stage(s) + kBytesW + kM * 128u, map, bar, kb * 64, row0 + kM);
+          load(stage(s), &tmM, bar, kb * 64, it.m0);
+          load(stage(s) + kBytesW, map, bar, kb * 64, n0);
+          if (two) load(stage(s) + kBytesW + kNM * 128u, map, bar, kb * 64, n0 + kNM);
           ++issued;
           if (++s == kStages) { s = 0; ph ^= 1u; }
         }
@@ -408,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
         if (!ok) break;
         tc_fence_after();
-        const int n = (it.rows + 15) & ~15;
+        const int n = (it.n() + 15) & ~15;
         const uint32_t d = tmem + acc * kAcc;
         const uint32_t id0 = idesc_mxf4(PAIR, n, 0), id2 = idesc_mxf4(PAIR, n, 2);
         // One step; h: its half of the scale buffer.
@@ -466,21 +528,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int i = unit, k = 0; i < n_items && ok; i += units, ++k) {
       const Item it = item_of(i, k);
-      const uint8_t* ws = p.w_scales + ((long long)it.w0 + r0) * p.pitch + 8 * h;
-      const uint8_t* as = p.a_scales + ((long long)it.row0 + r0) * p.pitch + 8 * h;
+      const uint8_t* ws = p.m_scales + ((long long)it.m0 + r0) * p.pitch + 8 * h;
+      const uint8_t* as = p.n_scales + ((long long)it.n0 + r0) * p.pitch + 8 * h;
       for (int kb = 0; kb < p.num_kb; kb += 2) {
         const bool in = kb + h < p.num_kb;
         uint2 w[2], a[3];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           w[r] = make_uint2(0u, 0u);
-          if (in && it.ch0 + 64 * r + r0 < p.N)
+          if (in && 64 * r + r0 < it.m())
             w[r] = __ldg(reinterpret_cast<const uint2*>(ws + (long long)(64 * r) * p.pitch + kb * 8));
         }
 #pragma unroll
         for (int r = 0; r < 3; ++r) {
           a[r] = make_uint2(0u, 0u);
-          if (in && 64 * r + r0 < it.rows)
+          if (in && 64 * r + r0 < it.n())
             a[r] = __ldg(reinterpret_cast<const uint2*>(as + (long long)(64 * r) * p.pitch + kb * 8));
         }
         ok = wait_warp(sempty_bar(sb), sb_ph ^ 1u, abort_flag, p.status, p.wait_limit);
@@ -519,11 +581,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <typename TO, bool GELU, int kStages, bool PAIR>
-cudaError_t launch_as(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, int grid,
+template <typename TO, bool GELU, int kStages, bool PAIR, bool ROWS_M>
+cudaError_t launch_as(const CUtensorMap& tmM, const CUtensorMap (&tmN)[3], const Params& p, int grid,
                       cudaStream_t s) {
   const uint32_t smem = smem_bytes(PAIR, kStages, p.G);
-  cudaError_t e = allow_smem_once(product_kernel<TO, GELU, kStages, PAIR>, smem);
+  cudaError_t e = allow_smem_once(product_kernel<TO, GELU, kStages, PAIR, ROWS_M>, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
@@ -538,16 +600,19 @@ cudaError_t launch_as(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, product_kernel<TO, GELU, kStages, PAIR>, tmW, tmA[0], tmA[1], tmA[2], p);
+  return cudaLaunchKernelEx(&cfg, product_kernel<TO, GELU, kStages, PAIR, ROWS_M>, tmM, tmN[0], tmN[1],
+                            tmN[2], p);
 }
 
 template <typename TO, bool GELU>
-cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap (&tmA)[3], const Params& p, bool pair,
-                   int grid, cudaStream_t s) {
-  if (pair) return launch_as<TO, GELU, kMaxStages, true>(tmW, tmA, p, grid, s);
-  if (smem_bytes(false, kMaxStages, p.G) <= kSmemMax)
-    return launch_as<TO, GELU, kMaxStages, false>(tmW, tmA, p, grid, s);
-  return launch_as<TO, GELU, kFewStages, false>(tmW, tmA, p, grid, s);
+cudaError_t launch(const CUtensorMap& tmM, const CUtensorMap (&tmN)[3], const Params& p, bool pair,
+                   bool rows_m, int grid, cudaStream_t s) {
+  if (pair) return launch_as<TO, GELU, kMaxStages, true, false>(tmM, tmN, p, grid, s);
+  if (smem_bytes(false, kMaxStages, p.G) > kSmemMax)
+    return launch_as<TO, GELU, kFewStages, false, false>(tmM, tmN, p, grid, s);
+  if constexpr (sizeof(TO) == 2)
+    if (rows_m) return launch_as<TO, GELU, kMaxStages, false, true>(tmM, tmN, p, grid, s);
+  return launch_as<TO, GELU, kMaxStages, false, false>(tmM, tmN, p, grid, s);
 }
 
 }  // namespace fp4p
@@ -596,30 +661,54 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   const int rc = unif::sm_count(&sms);
   if (rc != UNIF_MOE_OK) return rc;
   const uint64_t pitch = (uint64_t)(cols + 31) / 32 * 16;
-  const bool pair = n > 128 && rows >= 32ll * groups &&
-                    fpp::smem_bytes(true, fpp::kMaxStages, groups) <= fpp::kSmemMax;
+  const bool fits = fpp::smem_bytes(false, fpp::kMaxStages, groups) <= fpp::kSmemMax;
+  // Rows as M where tiles of 128 channels would waste a quarter of their work, groups
+  // have rows enough, and the output takes 32-byte stores (us, channels as M and rows
+  // as M: 100,003 rows in 272 groups of 192 x 768 26.1 and 18.9, 30,000 rows 14.0 and 11.0; without
+  // waste, 60,000 rows of 384 x 1,536 24.6 and 26.6; fp32 output, 60,000 of 1,536 x 384
+  // 66.6 and 86.9; rows off 32 bytes, 50,000 of 100 x 500 8.7 and 51.9).
+  const bool wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && ld * (dtype == UNIF_MOE_F32 ? 4 : 2) % 32 == 0;
+  const int parts = (n + fpp::kTN - 1) / fpp::kTN, part = ((n + parts - 1) / parts + 15) / 16 * 16;
+  const int padded = (n + 127) / 128 * 128;
+  const bool rows_m = fits && dtype == UNIF_MOE_BF16 && wide && 3ll * padded >= 4ll * parts * part &&
+                      rows >= 64ll * groups;
+  // CTA pairs, which read half of the rows' codes each, where steps are many enough for
+  // operand traffic to bound the tile and a pair's 256 channels are no more
+  // than two CTAs' 128 (us, single CTAs and pairs: 131,072 rows of 1,024 x 4,096 fp32 261 and 223,
+  // 20,000 rows 49.3 and 43.2, 2,000 rows 15.7 and 14.1, 500 rows 12.4 and 13.0; 100,000
+  // rows of 1,024 x 1,024 77.0 and 69.7, 1,000 rows of 4,096 x 1,024 in 8 groups 9.0 and
+  // 10.0; 100,000 rows of 768 x 768 54.6 and 54.5; of 384 x 1,536 24.6 and 29.1).
+  const bool pair = fits && !rows_m && (n + 255) / 256 * 256 == padded && rows >= 32ll * groups &&
+                    (cols >= 2048 || (cols >= 1024 && rows >= 1024ll * groups));
   const int ctas = pair ? 2 : 1;
-  CUtensorMap tmW, tmA[3];  // 128-byte pieces of code rows, counted in 2-byte units
-  if (!unif::encode_bf16_map(&tmW, w_codes, pitch / 2, (uint64_t)n * groups, 64, 128, 128) ||
-      !unif::encode_bf16_map(&tmA[0], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::stage_rows(pair), 128) ||
-      !unif::encode_bf16_map(&tmA[1], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxM / ctas, 128) ||
-      !unif::encode_bf16_map(&tmA[2], a_codes, pitch / 2, (uint64_t)rows, 64, fpp::kBoxS / ctas, 128)) {
+  // 128-byte pieces of code rows, counted in 2-byte units
+  const uint8_t* const m_codes = rows_m ? a_codes : w_codes;
+  const uint8_t* const n_codes = rows_m ? w_codes : a_codes;
+  const uint64_t w_rows = (uint64_t)n * groups, m_rows = rows_m ? (uint64_t)rows : w_rows,
+                 n_rows = rows_m ? w_rows : (uint64_t)rows;
+  CUtensorMap tmM, tmN[3];
+  if (!unif::encode_bf16_map(&tmM, m_codes, pitch / 2, m_rows, 64, 128, 128) ||
+      !unif::encode_bf16_map(&tmN[0], n_codes, pitch / 2, n_rows, 64, fpp::stage_rows(pair), 128) ||
+      !unif::encode_bf16_map(&tmN[1], n_codes, pitch / 2, n_rows, 64, fpp::kBoxM / ctas, 128) ||
+      !unif::encode_bf16_map(&tmN[2], n_codes, pitch / 2, n_rows, 64, fpp::kBoxS / ctas, 128)) {
     set_error("cuTensorMapEncodeTiled failed for the codes");
     return UNIF_MOE_ERR_CUDA;
   }
   fpp::Params p{};
   p.rows = (int)rows; p.N = n; p.G = groups;
   p.num_kb = (cols + fpp::kStep - 1) / fpp::kStep;
-  const int ch_tiles = (n + 128 * ctas - 1) / (128 * ctas);
+  const int ch_tile = rows_m ? fpp::kTN : 128 * ctas, row_tile = rows_m ? 128 * ctas : fpp::kTN;
+  const int ch_tiles = (n + ch_tile - 1) / ch_tile;
   p.offsets = offsets;
-  p.a_scales = a_scales; p.w_scales = w_scales;
+  p.m_scales = rows_m ? a_scales : w_scales;
+  p.n_scales = rows_m ? w_scales : a_scales;
   p.pitch = (cols + 255) / 256 * 8;
   p.out = out; p.ld = ld;
   p.pairs = (reinterpret_cast<uintptr_t>(out) & 3u) == 0 && ld % 2 == 0 && n % 2 == 0;
   p.status = status;
   p.wait_limit = unif::gemm_wait_limit();
   // at most one part-filled row tile per group beside the full ones
-  const int64_t most = ((int64_t)rows / fpp::kTN + (groups < rows ? groups : rows)) * ch_tiles;
+  const int64_t most = ((int64_t)rows / row_tile + (groups < rows ? groups : rows)) * ch_tiles;
   if (most > 0x7fffffff) {
     set_error("too many tiles: rows=%lld n=%d groups=%d", (long long)rows, n, groups);
     return UNIF_MOE_ERR_SHAPE;
@@ -629,10 +718,10 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   cudaError_t e;
   const bool gelu = activation == UNIF_MOE_ACTIVATION_GELU;
   if (dtype == UNIF_MOE_F32)
-    e = gelu ? fpp::launch<float, true>(tmW, tmA, p, pair, grid, s) : fpp::launch<float, false>(tmW, tmA, p, pair, grid, s);
+    e = gelu ? fpp::launch<float, true>(tmM, tmN, p, pair, rows_m, grid, s) : fpp::launch<float, false>(tmM, tmN, p, pair, rows_m, grid, s);
   else
-    e = gelu ? fpp::launch<__nv_bfloat16, true>(tmW, tmA, p, pair, grid, s)
-             : fpp::launch<__nv_bfloat16, false>(tmW, tmA, p, pair, grid, s);
+    e = gelu ? fpp::launch<__nv_bfloat16, true>(tmM, tmN, p, pair, rows_m, grid, s)
+             : fpp::launch<__nv_bfloat16, false>(tmM, tmN, p, pair, rows_m, grid, s);
   if (e != cudaSuccess) {
     set_error("mxfp4 product: %s", cudaGetErrorString(e));
     return UNIF_MOE_ERR_CUDA;

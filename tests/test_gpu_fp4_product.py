@@ -105,6 +105,20 @@ def test_many_groups(G):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("sizes,n,cols,act,dtype", [
+    # rows as the M operand: channels that 128-channel tiles would waste
+    ([129, 0, 300, 1, 128], 192, 768, "gelu", "bf16"), ([500, 77], 160, 300, "none", "bf16"),
+    ([90] * 20, 144, 512, "gelu", "bf16"), ([1000], 176, 33, "none", "bf16"),
+    ([200, 100], 192, 256, "gelu", "f32"),
+    # pairs of CTAs: many steps, an even number of 128-channel tiles
+    ([385, 0, 3, 192, 193], 512, 2048, "gelu", "bf16"), ([40, 33, 31, 60], 256, 2100, "none", "f32"),
+    ([700], 1000, 4096, "gelu", "f32"), ([2100, 1500], 250, 1024, "none", "bf16"),
+    ([17, 97, 31, 5, 20, 100, 32, 1], 300, 2304, "none", "bf16")])
+def test_other_operand_orders(sizes, n, cols, act, dtype):
+    check(sizes, n, cols, act=act, dtype=dtype, seed=n)
+
+
+@pytest.mark.gpu
 def test_more_items_than_sms():
     """Several items per CTA with few and many steps: the ring and the accumulators
     come round, in groups of unequal size."""
