@@ -1,0 +1,21 @@
+"""The example that runs the operators round the layer together: training steps lower
+the loss, and the 4-bit experts give the layer's output to the accuracy of 4 bits."""
+import os
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [dict(), dict(d=768, d_ff=1536, n_experts=6, n_blocks=8, tokens=777)],
+                         ids=["vit_s", "wider"])
+def test_sublayer_example(sizes, monkeypatch):
+    monkeypatch.syspath_prepend(os.path.join(ROOT, "examples"))
+    import sublayer
+    losses, off = sublayer.main(steps=4, **sizes)
+    assert all(b < a for a, b in zip(losses, losses[1:])), losses
+    # an element of a 4-bit block is off by up to 1/4 of itself (about 0.11 rms over the block,
+    # less for the largest); two operands of each of two products: 0.11 * sqrt(4) = 0.22
+    assert 0.01 < off < 0.25, off
