@@ -426,6 +426,7 @@ UNIF_MOE_API int unif_moe_group_noalloc(int T, int n_experts, int n_blocks,
 
 enum { UNIF_MOE_NORM_NONE = 0, UNIF_MOE_NORM_LAYER = 1, UNIF_MOE_NORM_RMS = 2 };
 #define UNIF_MOE_NORM_MAX_WIDTH 8192
+#define UNIF_MOE_NORM_MAX_TOKENS 0x7fff0000
 
 /* The step between two blocks of a Transformer: the norm after a block, the
  * block's gate, the scaled residual sum and the norm before the next block. For
@@ -439,7 +440,8 @@ enum { UNIF_MOE_NORM_NONE = 0, UNIF_MOE_NORM_LAYER = 1, UNIF_MOE_NORM_RMS = 2 };
  * bf16, or an fp32 stream with a bf16 branch. Arithmetic is fp32, and u is taken
  * from the fp32 sum, not from the rounded out. */
 typedef struct {
-  int tokens, width;              /* T >= 0, 1 <= width <= UNIF_MOE_NORM_MAX_WIDTH */
+  int tokens, width;              /* 0 <= T <= UNIF_MOE_NORM_MAX_TOKENS,
+                                     1 <= width <= UNIF_MOE_NORM_MAX_WIDTH */
   int stream_dtype, branch_dtype; /* unif_moe_dtype */
   int post_norm, pre_norm;        /* UNIF_MOE_NORM_* */
   int gate_rows;                  /* consecutive tokens that share a row of the gate: token t
@@ -459,7 +461,7 @@ typedef struct {
  *     may be y, with the same strides
  *   *_mean_dev, *_rstd_dev [T] fp32 or NULL: mean and 1 / sqrt(...) of y and of
  *     out, which the backward reads
- * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (width), ERR_CUDA. */
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (width, T), ERR_CUDA. */
 UNIF_MOE_API int unif_moe_block_norm_forward(
     const unif_moe_block_norm* p, const void* x_dev, int64_t ld_x, const void* y_dev, int64_t ld_y,
     const uint8_t* token_mask_dev, const void* w_post_dev, const void* b_post_dev,
@@ -565,7 +567,7 @@ enum { UNIF_MOE_ACTIVATION_NONE = 0, UNIF_MOE_ACTIVATION_GELU = 1 };
  *   w_codes_dev, w_scales_dev   [groups][n] rows of cols columns
  *   offsets_dev [groups + 1] int32; NULL with one group: all rows. Offsets outside
  *     [0, rows] are taken as the nearest bound; a group whose end is not above its
- *     start has no rows, and groups that together have more than `rows` rows lose the
+ *     start has no rows, a row of two groups gets one's result, and groups that together have more than `rows` rows lose the
  *     last ones. Rows of no group are not written
  *   activation  UNIF_MOE_ACTIVATION_*: GELU is 0.5 v (1 + erf(v / sqrt 2)), for bf16
  *     output within 3e-4 |v| of it before the rounding

@@ -64,29 +64,32 @@ at::ScalarType type_of(long c, const char* name) {
   return c == UNIF_MOE_F32 ? at::kFloat : at::kBFloat16;
 }
 
-// The device that all tensors of a call are on, current while the call runs.
+// The device that all tensors of a call are on and the call's stream, both current while
+// the call runs: memory taken for outputs and workspaces then belongs to the stream
+// that uses it, and is not given to another before that stream is done with it.
 struct Place {
   c10::Device dev;
   c10::cuda::CUDAGuard guard;
+  c10::cuda::OptionalCUDAStreamGuard on_stream;
   static c10::Device of(const Tensor& t, const char* name) {
     if (!t.defined() || !t.is_cuda()) value_error(std::string(name) + ": need a CUDA tensor");
     return t.device();
   }
-  Place(const Tensor& t, const char* name) : dev(of(t, name)), guard(dev) {}
-  void on(const Tensor& t, const char* name) const {
-    if (t.device() != dev)
-      value_error(std::string(name) + ": on " + t.device().str() + ", need " + dev.str());
-  }
-  void* stream(PyObject* o) const {
-    if (o == Py_None) return c10::cuda::getCurrentCUDAStream(dev.index()).stream();
-    PyObject* h = PyObject_HasAttrString(o, "cuda_stream") ? PyObject_GetAttrString(o, "cuda_stream")
-                                                           : Py_NewRef(o);
+  Place(const Tensor& t, const char* name, PyObject* s) : dev(of(t, name)), guard(dev) {
+    if (s == Py_None) return;
+    PyObject* h = PyObject_HasAttrString(s, "cuda_stream") ? PyObject_GetAttrString(s, "cuda_stream")
+                                                           : Py_NewRef(s);
     if (!h) throw Raised();
     void* p = PyLong_AsVoidPtr(h);
     Py_DECREF(h);
     if (PyErr_Occurred()) throw Raised();
-    return p;
+    on_stream.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(p), dev.index()));
   }
+  void on(const Tensor& t, const char* name) const {
+    if (t.device() != dev)
+      value_error(std::string(name) + ": on " + t.device().str() + ", need " + dev.str());
+  }
+  void* stream() const { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
   Tensor empty(at::IntArrayRef size, at::ScalarType t) const {
     return Tensor(at::detail::empty_cuda(size, t, dev, std::nullopt));
   }
@@ -202,7 +205,7 @@ NormParams norm_params(const Place& at, const unif_moe_block_norm& d, PyObject* 
 PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&]() -> PyObject* {
     const Tensor x = tensor(a[1], "x"), y = tensor(a[2], "y");
-    const Place at(x, "x");
+    const Place at(x, "x", a[12]);
     if (x.dim() != 2) value_error("x: need two dimensions");
     const int64_t T = x.size(0);
     const unif_moe_block_norm d = desc_of(a[0], T);
@@ -225,7 +228,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
     check(unif_moe_block_norm_forward(&d, px.p, px.ld, py.p, py.ld, mask, p.w_post, p.b_post, p.gate,
                                       p.w_pre, b_pre, po.p, po.ld, pu.p, pu.ld, sp[0], sp[1], sp[2],
-                                      sp[3], at.stream(a[12])));
+                                      sp[3], at.stream()));
     PyObject* r = PyDict_New();
     if (!r) throw Raised();
     try {
@@ -250,7 +253,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                  du = tensor(a[8], "du");
     const Tensor& ref = dout.defined() ? dout : du;
     if (!ref.defined()) value_error("dout and du are both None");
-    const Place at(ref, dout.defined() ? "dout" : "du");
+    const Place at(ref, dout.defined() ? "dout" : "du", a[14]);
     if (ref.dim() != 2) value_error("dout and du: need two dimensions");
     const int64_t T = ref.size(0);
     const unif_moe_block_norm d = desc_of(a[0], T);
@@ -283,7 +286,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check(unif_moe_block_norm_backward(
         &d, po.p, po.ld, py.p, py.ld, mask, p.w_post, p.b_post, p.gate, p.w_pre, st[0], st[1], st[2],
         st[3], pdo.p, pdo.ld, pdu.p, pdu.ld, dx.data_ptr(), w, y.defined() ? dy.data_ptr() : nullptr, w,
-        gp[0], gp[1], gp[2], gp[3], gp[4], ws.data_ptr(), need, at.stream(a[14])));
+        gp[0], gp[1], gp[2], gp[3], gp[4], ws.data_ptr(), need, at.stream()));
     PyObject* r = PyDict_New();
     if (!r) throw Raised();
     try {
@@ -305,7 +308,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> PyObject* {
     const Tensor z = tensor(a[0], "logits"), q = tensor(a[1], "q");
-    const Place at(z, "logits");
+    const Place at(z, "logits", a[7]);
     const int type = code(z.scalar_type());
     if (type < 0 || z.dim() != 2) value_error("logits: need [T][K] of fp32 or bf16, got " + shown(z));
     const int64_t T = z.size(0), K = z.size(1);
@@ -327,7 +330,7 @@ PyObject* balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
         pq.ld, static_cast<const int32_t*>(k), mask, (float)as_double(a[4]), (float)as_double(a[5]),
         loss.data_ptr<float>(), counts.data_ptr<int32_t>(), prob.data_ptr<float>(),
         d.defined() ? d.data_ptr<float>() : nullptr, need ? ws.data_ptr() : nullptr, need,
-        at.stream(a[7])));
+        at.stream()));
     PyObject* r = PyDict_New();
     if (!r) throw Raised();
     try {
@@ -375,7 +378,7 @@ Fp4 fp4_of(const Place& at, const Tensor& codes, const Tensor& scales, int64_t c
 PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 5, [&]() -> PyObject* {
     const Tensor x = tensor(a[0], "x");
-    const Place at(x, "x");
+    const Place at(x, "x", a[4]);
     const int type = code(x.scalar_type());
     if (type < 0 || x.dim() < 1) value_error("x: need rows of fp32 or bf16, got " + shown(x));
     const int64_t cols = x.size(-1);
@@ -401,7 +404,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     check(unif_moe_mxfp4_quantize(px.p, (unif_moe_dtype)type, rows, (int)cols, px.ld,
                                   static_cast<uint8_t*>(codes.data_ptr()),
-                                  static_cast<uint8_t*>(scales.data_ptr()), at.stream(a[4])));
+                                  static_cast<uint8_t*>(scales.data_ptr()), at.stream()));
     return Py_BuildValue("(NNL)", THPVariable_Wrap(codes), THPVariable_Wrap(scales), (long long)cols);
   });
 }
@@ -410,7 +413,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject* {
     const Tensor codes = tensor(a[0], "q.codes"), scales = tensor(a[1], "q.scales");
-    const Place at(codes, "q.codes");
+    const Place at(codes, "q.codes", a[5]);
     const int64_t cols = cols_of(a[2], "q");
     const Fp4 q = fp4_of(at, codes, scales, cols, "q");
     const long type = as_long(a[3]);
@@ -427,7 +430,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
       po.ld = cols;
     }
     check(unif_moe_mxfp4_dequantize(q.codes, q.scales, q.rows, (int)cols, po.p, (unif_moe_dtype)type,
-                                    po.ld, at.stream(a[5])));
+                                    po.ld, at.stream()));
     return THPVariable_Wrap(out);
   });
 }
@@ -437,7 +440,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 12, [&]() -> PyObject* {
     const Tensor ac = tensor(a[0], "a.codes"), wc = tensor(a[3], "w.codes");
-    const Place at(ac, "a.codes");
+    const Place at(ac, "a.codes", a[11]);
     const int64_t cols = cols_of(a[2], "a");
     if (as_long(a[5]) != cols) value_error("a and w have different numbers of columns");
     const Fp4 x = fp4_of(at, ac, tensor(a[1], "a.scales"), cols, "a");
@@ -458,7 +461,7 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
         static_cast<const int32_t*>(dense(at, offsets, "offsets", groups + 1, at::kInt)),
         (int)as_long(a[7]), po.p, (unif_moe_dtype)type, po.ld,
         static_cast<int32_t*>(dense(at, tensor(a[10], "status"), "status", 1, at::kInt)),
-        at.stream(a[11])));
+        at.stream()));
     return THPVariable_Wrap(out);
   });
 }

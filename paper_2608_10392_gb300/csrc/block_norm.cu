@@ -942,6 +942,10 @@ int check_desc(const unif_moe_block_norm* p) {
     set_error("bad sizes: tokens=%d width=%d gate_rows=%d", p->tokens, p->width, p->gate_rows);
     return UNIF_MOE_ERR_ARG;
   }
+  if (p->tokens > UNIF_MOE_NORM_MAX_TOKENS) {
+    set_error("tokens=%d above %d", p->tokens, UNIF_MOE_NORM_MAX_TOKENS);
+    return UNIF_MOE_ERR_SHAPE;
+  }
   if (p->width > UNIF_MOE_NORM_MAX_WIDTH) {
     set_error("width=%d above %d", p->width, UNIF_MOE_NORM_MAX_WIDTH);
     return UNIF_MOE_ERR_SHAPE;

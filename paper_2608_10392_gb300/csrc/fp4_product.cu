@@ -709,7 +709,7 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   p.wait_limit = unif::gemm_wait_limit();
   // at most one part-filled row tile per group beside the full ones
   const int64_t most = ((int64_t)rows / row_tile + (groups < rows ? groups : rows)) * ch_tiles;
-  if (most > 0x7fffffff) {
+  if (most > 0x7fff0000) {  // items are counted in 32 bits, beyond the last one by a grid
     set_error("too many tiles: rows=%lld n=%d groups=%d", (long long)rows, n, groups);
     return UNIF_MOE_ERR_SHAPE;
   }

@@ -48,11 +48,15 @@ cudaError_t allow_smem_once(const void* fn, size_t need) {
   int dev = 0;
   const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  std::lock_guard<std::mutex> hold(lock);
-  if (done.count({fn, dev})) return cudaSuccess;
-  const cudaError_t r = allow_smem(fn, need);
-  if (r == cudaSuccess) done.insert({fn, dev});
-  return r;
+  try {
+    std::lock_guard<std::mutex> hold(lock);
+    if (done.count({fn, dev})) return cudaSuccess;
+    const cudaError_t r = allow_smem(fn, need);
+    if (r == cudaSuccess) done.insert({fn, dev});
+    return r;
+  } catch (...) {  // no exception leaves the library
+    return cudaErrorMemoryAllocation;
+  }
 }
 
 int sm_count(int* n) {

@@ -177,6 +177,8 @@ _status_words = {}  # per device: set by a product whose kernel gave up a wait
 def _status_word(device: torch.device) -> torch.Tensor:
     t = _status_words.get(device)
     if t is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first mxfp4_product on a device has to be outside a capture")
         t = _status_words[device] = torch.zeros(1, dtype=torch.int32, device=device)
     return t
 
@@ -204,4 +206,4 @@ def mxfp4_product(a: Mxfp4, w: Mxfp4, offsets: Optional[torch.Tensor] = None, *,
     are not written. activation: "none" or "gelu"."""
     return _b().product(a.codes, a.scales, a.cols, w.codes, w.scales, w.cols, offsets,
                         _ACTIVATIONS[activation], _CODES[DTYPES[dtype]], out,
-                        _status_word(a.codes.device), stream)
+                        _status_word(a.codes.device) if a.codes.is_cuda else None, stream)

@@ -377,6 +377,27 @@ def test_large_values_stay_finite_and_nan_stays_in_its_row():
     assert torch.isfinite(u[~bad]).all() and torch.isnan(u[7]).all() and torch.isnan(u[9, 100])
 
 
+@pytest.mark.gpu
+def test_stream_argument():
+    """Calls on a stream that is not the current one, one after another without
+    waiting: workspaces and outputs of one call are not handed to the next too early."""
+    cfg, v, e = make(3000, 768, "bf16", "bf16", "rms", "rms", 100, False, None, seed=6, dev="cuda")
+    norm = layer_of(cfg, "bf16", "bf16")
+    params = {k: v[k] for k in PARAMS}
+    s = statistics(cfg, e)
+    want = norm.backward(v["x"], v["y"], s, dout=v["dout"], du=v["du"], **params)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = [norm.backward(v["x"], v["y"], s, dout=v["dout"], du=v["du"], stream=side, **params)
+           for _ in range(20)]
+    outs = [norm.forward(v["x"], v["y"], stream=side.cuda_stream, **params) for _ in range(3)]
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(g[k], want[k]) for k in want)
+    first = norm.forward(v["x"], v["y"], **params)
+    assert all(torch.equal(o["u"], first["u"]) for o in outs)
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
@@ -403,6 +424,7 @@ def test_refusals():
                      (7, float("inf")), (8, -1.0), (8, float("nan"))):
         assert fwd(bad(i, value)) == -1, (i, value)
     assert fwd(bad(1, 8193)) == -2 and b"width" in L.unif_moe_last_error()
+    assert fwd(bad(0, 0x7fff0001)) == -2 and b"tokens" in L.unif_moe_last_error()
     assert fwd(D(4, 64, 1, 0, 2, 2, 0, 1.0, 1e-6)) == -1  # bf16 stream, fp32 branch
     assert fwd(D(*good), w_post=None) == -1
     assert fwd(D(*good), w_pre=None) == -1

@@ -213,6 +213,32 @@ def test_graph_capture():
     assert torch.equal(out, got)
 
 
+@pytest.mark.gpu
+def test_stream_argument_and_a_capture_first():
+    from paper_2608_10392_gb300 import mxfp4_product, mxfp4_quantize, operators
+    a, wg, got = check([300, 200], 256, 1024, seed=8)
+    off = torch.tensor([0, 300, 500], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    again = [mxfp4_product(a, wg, off, stream=side) for _ in range(5)]
+    x = torch.randn(64, 96, device="cuda")
+    torch.cuda.synchronize()
+    q = mxfp4_quantize(x, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(got, r) for r in again)
+    assert torch.equal(q.codes, mxfp4_quantize(x).codes)
+    # the word that products report to is not made inside a capture
+    kept = dict(operators._status_words)
+    operators._status_words.clear()
+    try:
+        graph, out = torch.cuda.CUDAGraph(), torch.empty_like(got)
+        with pytest.raises(RuntimeError, match="capture"):
+            with torch.cuda.graph(graph):
+                mxfp4_product(a, wg, off, out=out)
+    finally:
+        operators._status_words.update(kept)
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()
