@@ -17,6 +17,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "internal.cuh"
 
 namespace unif {
@@ -338,10 +340,10 @@ __device__ __forceinline__ void cluster_sync() {
                    : "memory");
 }
 
-// The whole call in one kernel, where a cluster of up to eight CTAs holds all
-// tokens' probabilities in its registers (U tokens per group of lanes): the CTAs
+// The whole call in one kernel, where a cluster of CTAs holds all tokens'
+// probabilities in its registers (up to U tokens per group of lanes): the CTAs
 // read one another's column sums from shared memory. Two kernels cost a second
-// launch and a second reading (12,608 tokens of 8 experts: 10.4 us).
+// launch and a second reading.
 template <typename T, int L, int E, bool VEC, int TH, int U>
 __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   constexpr int kWarps = TH / 32, kTok = TH / L;
@@ -354,6 +356,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   const int lane = threadIdx.x % L, tok = threadIdx.x / L, warp = threadIdx.x / 32,
             lane32 = threadIdx.x & 31;
   const uint32_t ranks = gridDim.x;  // one cluster
+  const int held = (int)((a.T + ranks * kTok - 1) / (ranks * kTok));  // tokens of a group, <= U
   for (int i = threadIdx.x; i < a.K; i += TH) cnt[i] = 0;
   if (threadIdx.x < 2) all[threadIdx.x] = 0;
   float z[U][E], lse[U];
@@ -361,6 +364,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   bool in[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
+    if (u >= held) break;
     const int t0 = (u * (int)ranks + (int)blockIdx.x) * kTok + tok;
     in[u] = t0 < a.T && (!a.mask || a.mask[t0]);
     const int t = in[u] ? t0 : 0;
@@ -379,6 +383,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   for (int i = 0; i < E; ++i) p[i] = 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
+    if (u >= held) break;
     float top, sum;
     in[u] = softmax<L, E>(in[u], z[u], top, sum);
     const float inv = 1.f / sum;
@@ -492,6 +497,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
     fr[i] = lane * E + i < a.K ? (float)__float_as_int(f[lane * E + i]) * inv_c : 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
+    if (u >= held) break;
     const int t = (u * (int)ranks + (int)blockIdx.x) * kTok + tok;
     float fp = 0.f;
 #pragma unroll
@@ -506,6 +512,26 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
 
 constexpr int kWide = 128;  // up to this many experts: CTAs of 1,024 threads
 inline int threads_of(int K) { return K <= kWide ? 1024 : 256; }
+
+// Whether clusters of 16 CTAs of this kernel can run (above the portable eight).
+bool allow_cluster_16(const void* fn, int threads, size_t smem) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+      cudaOccupancyMaxActiveClusters(&clusters, fn, &cfg) == cudaSuccess && clusters > 0)
+    return true;
+  cudaGetLastError();  // a refusal is no error of the call
+  return false;
+}
 
 // Lanes per token, and tokens that a cluster of eight CTAs holds at once (those of
 // cluster_kernel's instances).
@@ -524,10 +550,19 @@ int cta_count(int T, int K, int sms) {
 
 template <typename T, int L, int E, bool VEC, int TH, int U>
 cudaError_t launch_as(const Args& a, cudaStream_t s) {
-  const long long once = (long long)U * (TH / L);  // tokens that a CTA holds at once
   if (in_cluster(a.T, a.K)) {
-    unsigned ctas = 1;  // 1, 2, 4 or 8
-    while (ctas * once < a.T) ctas *= 2;
+    // as many CTAs as have tokens, up to the largest cluster: 16 where the device
+    // takes that many (not every one has to), else 8
+    static std::atomic<unsigned> largest{0};
+    unsigned most = largest.load(std::memory_order_relaxed);
+    if (!most) {
+      most = allow_cluster_16(reinterpret_cast<const void*>(cluster_kernel<T, L, E, VEC, TH, U>), TH,
+                              (size_t)(TH / 32 + 3) * a.K * sizeof(float))
+                 ? 16 : 8;
+      largest.store(most, std::memory_order_relaxed);
+    }
+    unsigned ctas = 1;
+    while (ctas < most && (long long)ctas * (TH / L) < a.T) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(TH);
