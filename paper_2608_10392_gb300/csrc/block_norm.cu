@@ -68,8 +68,8 @@ __device__ __forceinline__ void load(const float* p, int j, int n, int d, float 
   } else {
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
-      const int c = column<false>(j, n, i);
-      v[i] = c < d ? p[c] : 0.f;
+      v[i] = 0.f;
+      if (i * n < d && column<false>(j, n, i) < d) v[i] = p[column<false>(j, n, i)];
     }
   }
 }
@@ -82,8 +82,8 @@ __device__ __forceinline__ void load(const __nv_bfloat16* p, int j, int n, int d
   } else {
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
-      const int c = column<false>(j, n, i);
-      v[i] = c < d ? __bfloat162float(p[c]) : 0.f;
+      v[i] = 0.f;
+      if (i * n < d && column<false>(j, n, i) < d) v[i] = __bfloat162float(p[column<false>(j, n, i)]);
     }
   }
 }
@@ -97,10 +97,8 @@ __device__ __forceinline__ void store(float* p, int j, int n, int d, const float
                    : "memory");
   } else {
 #pragma unroll
-    for (int i = 0; i < kE; ++i) {
-      const int c = column<false>(j, n, i);
-      if (c < d) p[c] = v[i];
-    }
+    for (int i = 0; i < kE; ++i)
+      if (i * n < d && column<false>(j, n, i) < d) p[column<false>(j, n, i)] = v[i];
   }
 }
 template <bool VEC>
@@ -117,10 +115,8 @@ __device__ __forceinline__ void store(__nv_bfloat16* p, int j, int n, int d, con
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kE; ++i) {
-      const int c = column<false>(j, n, i);
-      if (c < d) p[c] = __float2bfloat16_rn(v[i]);
-    }
+    for (int i = 0; i < kE; ++i)
+      if (i * n < d && column<false>(j, n, i) < d) p[column<false>(j, n, i)] = __float2bfloat16_rn(v[i]);
   }
 }
 
@@ -203,12 +199,15 @@ __device__ __forceinline__ void scale_shift(float (&v)[kE], const TB* w, const T
   }
 }
 
-template <typename TX, typename TB, bool VEC, int GL>
-__global__ void __launch_bounds__(GL ? kThreads : 1024)
+// MT: most threads of a CTA; without VEC the threads, so that the columns' offsets are
+// constants (with an offset and a bound worked out per value, a row of 333 took 1,850
+// instructions a warp in the backward).
+template <typename TX, typename TB, bool VEC, int GL, int MT>
+__global__ void __launch_bounds__(MT)
     forward_kernel(const ForwardArgs<TX, TB> a) {
   __shared__ float red[2 * 2 * kMaxWarps];
   int turn = 0;
-  const int n = GL ? GL : (int)blockDim.x;
+  const int n = GL ? GL : VEC ? (int)blockDim.x : MT;
   const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
   const int rows = GL ? kThreads / (GL ? GL : 1) : 1;
   const int d = a.d;
@@ -361,6 +360,64 @@ __device__ __forceinline__ void group_sums(const uint64_t (&s)[R][2], float* red
   for (int r = 0; r < R; ++r) out[r] = upk(t[r]);
 }
 
+// Eight values of a row that is not moved 16 bytes at a time: on their way (Coming: no
+// instruction uses them yet, so nothing waits for them) and held.
+template <typename T>
+struct Coming {
+  T v[kE];
+  __device__ __forceinline__ void read(const T* p, int j, int n, int d) {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      v[i] = (T)0;
+      if (i * n < d && column<false>(j, n, i) < d) v[i] = p[column<false>(j, n, i)];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = (T)0;
+  }
+};
+template <typename T>
+struct Bits {  // what a value is read as
+  using type = float;
+};
+template <>
+struct Bits<__nv_bfloat16> {
+  using type = unsigned short;
+};
+template <typename T>
+struct Row8;
+template <>
+struct Row8<float> {
+  float v[kE];
+  __device__ __forceinline__ void take(const Coming<float>& c) {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = c.v[i];
+  }
+  __device__ __forceinline__ F8 get() const { return pairs(v); }
+};
+template <>
+struct Row8<__nv_bfloat16> {
+  uint4 raw;
+  __device__ __forceinline__ void take(const Coming<unsigned short>& c) {
+    uint32_t h[kE / 2];
+#pragma unroll
+    for (int i = 0; i < kE / 2; ++i) h[i] = (uint32_t)c.v[2 * i] | (uint32_t)c.v[2 * i + 1] << 16;
+    raw = make_uint4(h[0], h[1], h[2], h[3]);
+  }
+  __device__ __forceinline__ void read(const __nv_bfloat16* p, int j, int n, int d) {
+    Coming<unsigned short> c;
+    c.read(reinterpret_cast<const unsigned short*>(p), j, n, d);
+    take(c);
+  }
+  __device__ __forceinline__ void clear() { raw = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ F8 get() const {
+    float v[kE];
+    unpack(raw, v);
+    return pairs(v);
+  }
+};
+
 // A parameter's values of this thread's columns: bf16 ones stay in registers from
 // row to row as they were read, fp32 ones are read again.
 template <typename TB, bool VEC>
@@ -373,6 +430,15 @@ struct Param {
     load<VEC>(p, j, n, d, v);
     return pairs(v);
   }
+};
+template <>
+struct Param<__nv_bfloat16, false> {
+  Row8<__nv_bfloat16> held;
+  __device__ __forceinline__ Param() { held.clear(); }
+  __device__ __forceinline__ void set(const __nv_bfloat16* q, int j, int n, int d) {
+    if (q) held.read(q, j, n, d);
+  }
+  __device__ __forceinline__ F8 get(int, int, int) const { return held.get(); }
 };
 template <>
 struct Param<__nv_bfloat16, true> {
@@ -482,7 +548,9 @@ template <typename TX, typename TB, bool VEC, int GL, int MT>
 __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     backward_kernel(const BackwardArgs<TX, TB> a) {
   constexpr int R = step_rows(VEC, MT), W = MT / 32;
-  constexpr int kRing = ring_steps<TX, TB>(MT);
+  constexpr int kRing = VEC ? ring_steps<TX, TB>(MT) : 2;
+  // without VEC the next row waits in registers, where there are enough
+  constexpr bool kHeld = !VEC && MT <= 512, kAhead = VEC || kHeld;
   constexpr int kPX = kE * sizeof(TX) / 16, kPB = kE * sizeof(TB) / 16;  // planes of an array
   constexpr int kPlanes = 2 * kPX + 2 * kPB;
   constexpr int kGroups = GL ? MT / (GL ? GL : 1) : 1;
@@ -492,7 +560,7 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   __shared__ float fold[GL ? MT * kE : 1];
   const int threads = (int)blockDim.x;
   int turn = 0;
-  const int n = GL ? GL : threads;
+  const int n = GL ? GL : VEC ? threads : MT;
   const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
   const int grp = GL ? (int)threadIdx.x / (GL ? GL : 1) : 0;
   const int d = a.d;
@@ -571,13 +639,26 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     return v;
   };
   uint32_t valids = 0;  // R bits for each step from the current one on
-  uint32_t next_valid = VEC ? validity(ahead) : 0u;
+  uint32_t next_valid = kAhead ? validity(ahead) : 0u;
   int put = 0, get = 0;
+  using BX = typename Bits<TX>::type;
+  using BB = typename Bits<TB>::type;
+  Coming<BX> next_dout, next_o;
+  Coming<BB> next_y, next_du;
   auto fetch = [&](int k) {  // the step `ahead` stands at, the k-th to be worked on
     if (ahead.more()) {
       valids |= next_valid << (k * R);
+      if (kHeld && (next_valid & 1u)) {
+        const long long row = row_of(ahead, 0);
+        if (a.dout) next_dout.read(reinterpret_cast<const BX*>(a.dout + row * a.ld_dout), j, n, d);
+        if (a.pre) {
+          next_o.read(reinterpret_cast<const BX*>(a.o + row * a.ld_o), j, n, d);
+          next_du.read(reinterpret_cast<const BB*>(a.du + row * a.ld_du), j, n, d);
+        }
+        if (with_y) next_y.read(reinterpret_cast<const BB*>(a.y + row * a.ld_y), j, n, d);
+      }
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
+      for (int r = 0; VEC && r < R; ++r) {
         uint4* to = slot(put, r);
         if (next_valid >> r & 1u) {
           if (act) {
@@ -598,9 +679,10 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
       next_valid = validity(ahead);
       if (++put == kRing) put = 0;
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (VEC) asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (VEC)
+  next_dout.clear(); next_o.clear(); next_y.clear(); next_du.clear();
+  if (kAhead)
 #pragma unroll
     for (int k = 0; k < kRing - 1; ++k) fetch(k);
 
@@ -624,11 +706,19 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     const int gate_row = at.gate;
     const Walk here = at;
     uint32_t valid;
-    if (VEC) {
+    Row8<TX> held_dout, held_o;
+    Row8<TB> held_y, held_du;
+    if (kHeld) {
+      held_dout.take(next_dout);
+      held_o.take(next_o);
+      held_y.take(next_y);
+      held_du.take(next_du);
+    }
+    if (kAhead) {
       fetch(kRing - 1);
       valid = valids & ((1u << R) - 1u);
       valids >>= R;
-      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      if (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
     } else {
       valid = validity(at);
     }
@@ -650,7 +740,8 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
     const uint32_t present = (row_of(here, R - 1) < here.end ? 1u << (R - 1) : 0u) |
                              (row_of(here, 0) < here.end ? 1u : 0u);
     if (GL || valid) {  // (without groups in warps the whole CTA agrees)
-      auto values = [&](auto* base, long long ld, int plane, int r) {
+      auto values = [&](auto* base, long long ld, int plane, int r, const auto& held) {
+        if (kHeld) return valid & 1u ? held.get() : zero8();
         float v[kE];
         if (VEC) {
           ring_read(slot(ring_at, r) + plane * threads, threads, base, v);
@@ -663,7 +754,7 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
       };
       F8 D[R];
 #pragma unroll
-      for (int r = 0; r < R; ++r) D[r] = a.dout ? values(a.dout, a.ld_dout, 0, r) : zero8();
+      for (int r = 0; r < R; ++r) D[r] = a.dout ? values(a.dout, a.ld_dout, 0, r, held_dout) : zero8();
       // columns past d hold 0 in every parameter and input, so that no sum sees what
       // the rest of the arithmetic makes of them
       if (a.pre) {
@@ -673,8 +764,8 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
         const F8 wp = w_pre.get(j, n, d);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          oh[r] = values(a.o, a.ld_o, kPX, r);
-          w[r] = values(a.du, a.ld_du, 2 * kPX + kPB, r);
+          oh[r] = values(a.o, a.ld_o, kPX, r, held_o);
+          w[r] = values(a.du, a.ld_du, 2 * kPX + kPB, r, held_du);
           const uint64_t q = pk(q0[r], q0[r]), mq = pk(m0[r], m0[r]);
           s[r][0] = s[r][1] = 0ull;
 #pragma unroll
@@ -714,7 +805,7 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
         if (a.post) w = w_post.get(j, n, d);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          yn[r] = values(a.y, a.ld_y, 2 * kPX, r);
+          yn[r] = values(a.y, a.ld_y, 2 * kPX, r, held_y);
           if (a.post) {
             const uint64_t q = pk(q1[r], q1[r]), mq = pk(m1[r], m1[r]);
 #pragma unroll
@@ -902,10 +993,17 @@ template <typename TX, typename TB, bool VEC>
 cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, cudaStream_t s) {
   const int threads = cta_threads(a.d);
   switch (group_lanes(a.d)) {
-    case 8: forward_kernel<TX, TB, VEC, 8><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
-    case 16: forward_kernel<TX, TB, VEC, 16><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
-    case 32: forward_kernel<TX, TB, VEC, 32><<<(a.T + 3) / 4, threads, 0, s>>>(a); break;
-    default: forward_kernel<TX, TB, VEC, 0><<<a.T, threads, 0, s>>>(a); break;
+    case 8: forward_kernel<TX, TB, VEC, 8, kThreads><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
+    case 16: forward_kernel<TX, TB, VEC, 16, kThreads><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
+    case 32: forward_kernel<TX, TB, VEC, 32, kThreads><<<(a.T + 3) / 4, threads, 0, s>>>(a); break;
+    default:
+      if (VEC) forward_kernel<TX, TB, true, 0, 1024><<<a.T, threads, 0, s>>>(a);
+      else if (threads <= 64) forward_kernel<TX, TB, false, 0, 64><<<a.T, 64, 0, s>>>(a);
+      else if (threads <= 128) forward_kernel<TX, TB, false, 0, 128><<<a.T, 128, 0, s>>>(a);
+      else if (threads <= 256) forward_kernel<TX, TB, false, 0, 256><<<a.T, 256, 0, s>>>(a);
+      else if (threads <= 512) forward_kernel<TX, TB, false, 0, 512><<<a.T, 512, 0, s>>>(a);
+      else forward_kernel<TX, TB, false, 0, 1024><<<a.T, 1024, 0, s>>>(a);
+      break;
   }
   return cudaGetLastError();
 }
@@ -929,11 +1027,16 @@ cudaError_t launch_bwd(const BackwardArgs<TX, TB>& a, int ctas, cudaStream_t s) 
     case 16: return launch_bwd_as<TX, TB, VEC, 16, kThreads>(a, ctas, threads, s);
     case 32: return launch_bwd_as<TX, TB, VEC, 32, kThreads>(a, ctas, threads, s);
   }
-  if (threads <= 128) return launch_bwd_as<TX, TB, VEC, 0, 128>(a, ctas, threads, s);
-  if (threads <= 384) return launch_bwd_as<TX, TB, VEC, 0, 384>(a, ctas, threads, s);
-  if (threads <= 512) return launch_bwd_as<TX, TB, VEC, 0, 512>(a, ctas, threads, s);
+  // (without VEC the kernel counts on all of its threads)
+  if constexpr (!VEC) {
+    if (threads <= 64) return launch_bwd_as<TX, TB, false, 0, 64>(a, ctas, 64, s);
+    if (threads > 128 && threads <= 256) return launch_bwd_as<TX, TB, false, 0, 256>(a, ctas, 256, s);
+  }
+  if (threads <= 128) return launch_bwd_as<TX, TB, VEC, 0, 128>(a, ctas, VEC ? threads : 128, s);
+  if (threads <= 384) return launch_bwd_as<TX, TB, VEC, 0, 384>(a, ctas, VEC ? threads : 384, s);
+  if (threads <= 512) return launch_bwd_as<TX, TB, VEC, 0, 512>(a, ctas, VEC ? threads : 512, s);
   // still wider rows: no room for a ring beside 1,024 threads
-  return launch_bwd_as<TX, TB, false, 0, 1024>(a, ctas, threads, s);
+  return launch_bwd_as<TX, TB, false, 0, 1024>(a, ctas, 1024, s);
 }
 
 int check_desc(const unif_moe_block_norm* p) {
