@@ -11,6 +11,8 @@
 // first leaves each CTA's sums in the workspace, the second adds them (in the
 // CTAs' order: results do not change from run to run) and writes the gradient
 // from a second reading of the logits, which the first left in L2.
+// Latency bounds the call (us on the GPU): 256 tokens of 4 experts 4.7, 12,608 of 8
+// 8.6, both in one kernel; 65,536 of 32 in two 13.7, where the bytes need 2.6.
 // A token belongs to L lanes of a warp, which hold E logits each. At most one CTA
 // per SM: with two of 256 threads and one token of each group at a time, 65,536
 // tokens of 32 experts took 17 and 21 us.
