@@ -11,7 +11,7 @@
 // rounded once, to the type it is stored in.
 //
 // Measured (us; at the copy rate of 6.8 TB/s): forward of 12,608 x 384, fp32 stream,
-// 13.5 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 47 (24); backward of 12,608 x 768
+// 13.5 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 38 (24); backward of 12,608 x 768
 // bf16 with a gate per image 34 (17), of 65,536 x 1,024 padded, fp32 stream, 187 (178
 // for all rows). Widths that are no multiple of eight move value by value: backward
 // of 20,000 x 1,001 bf16 104 (35), forward 65 (24).
@@ -904,6 +904,226 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
   if (sum_gate && a.pieces > 1) flush(s_gate, a.part_gate + (long long)blockIdx.x * d);
 }
 
+// The forward over many rows of bf16, two at a time, the next steps' rows on their way
+// to shared memory as in the backward. A CTA takes every gridDim.x-th chunk of rows. 16
+// warps on an SM: with 20 or 24 and fewer registers 20,000-odd rows took 2 to 19% longer.
+template <typename TX, typename TB>
+__host__ __device__ constexpr int stream_steps() {  // of a ring of 320 bytes a thread
+  return 320 / (2 * kE * (int)(sizeof(TX) + sizeof(TB)));
+}
+
+template <typename TX, typename TB, int GL, int MT>
+__global__ void __launch_bounds__(MT, 512 / MT)
+    forward_stream_kernel(const ForwardArgs<TX, TB> a, const int chunk) {
+  constexpr int R = 2, W = MT / 32, kRing = stream_steps<TX, TB>();
+  constexpr int kPX = kE * sizeof(TX) / 16, kPB = kE * sizeof(TB) / 16, kPlanes = kPX + kPB;
+  constexpr int kGroups = GL ? MT / (GL ? GL : 1) : 1, kStep = kGroups * R;
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float red[GL ? 4 : 2 * 2 * R * W];
+  const int threads = (int)blockDim.x;
+  int turn = 0;
+  const int n = GL ? GL : threads;
+  const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
+  const int grp = GL ? (int)threadIdx.x / (GL ? GL : 1) : 0;
+  const int d = a.d;
+  const float inv = 1.f / (float)d;
+  const bool act = j * kE < d;
+  Param<TB, true> w_post, b_post, w_pre, b_pre, gate[R];
+  w_post.set(a.w_post, j, n, d);
+  b_post.set(a.b_post, j, n, d);
+  w_pre.set(a.w_pre, j, n, d);
+  b_pre.set(a.b_pre, j, n, d);
+  int gate_at[R] = {0, 0};
+  if (a.gate)
+#pragma unroll
+    for (int r = 0; r < R; ++r) gate[r].set(a.gate, j, n, d);
+
+  auto slot = [&](int k, int r) { return ring + (k * R + r) * (kPlanes * threads) + threadIdx.x; };
+  if (!act)  // threads without columns read zeros
+    for (int k = 0; k < kRing * R; ++k)
+#pragma unroll
+      for (int i = 0; i < kPlanes; ++i) slot(0, k)[i * threads] = make_uint4(0u, 0u, 0u, 0u);
+  if (!GL && threadIdx.x < 2 * 2 * R * W) red[threadIdx.x] = 0.f;
+  if (!GL) __syncthreads();
+
+  Walk at;
+  at.cut = false;
+  at.gate = 0;
+  at.last = a.T;
+  at.size = chunk;
+  at.base = (int)min((long long)a.T, (long long)blockIdx.x * chunk);
+  at.skip = (int)min((long long)a.T, (long long)(gridDim.x - 1) * chunk);
+  at.end = min(at.last - at.base, chunk) + at.base;
+  Walk ahead = at;
+  auto row_of = [&](const Walk& w, int r) { return w.base + r * kGroups + grp; };
+  auto validity = [&](const Walk& w) {
+    uint32_t v = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = row_of(w, r);
+      if (w.more() && row < w.end && (!a.mask || a.mask[row])) v |= 1u << r;
+    }
+    return v;
+  };
+  uint32_t valids = 0, next_valid = validity(ahead);
+  int put = 0, get = 0;
+  auto fetch = [&](int k) {
+    if (ahead.more()) {
+      valids |= next_valid << (k * R);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        uint4* to = slot(put, r);
+        if (next_valid >> r & 1u) {
+          if (act) {
+            const long long row = row_of(ahead, r);
+            ring_copy(to, a.x + row * a.ld_x + j * kE, threads);
+            if (a.y) ring_copy(to + kPX * threads, a.y + row * a.ld_y + j * kE, threads);
+          }
+        } else if (GL || next_valid) {
+#pragma unroll
+          for (int i = 0; i < kPlanes; ++i) to[i * threads] = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+      ahead.next(kStep);
+      next_valid = validity(ahead);
+      if (++put == kRing) put = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int k = 0; k < kRing - 1; ++k) fetch(k);
+
+  // v to w (v - mean) rstd + b, for the step's rows together
+  auto norm_rows = [&](F8 (&v)[R], int kind, const Param<TB, true>& w, const Param<TB, true>& b,
+                       const TB* bias, float (&mean)[R], float (&rstd)[R]) {
+    uint64_t s[R][2];
+    float2 c[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = 0.f;
+    if (kind == UNIF_MOE_NORM_LAYER) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        s[r][0] = add2(add2(v[r].p[0], v[r].p[1]), add2(v[r].p[2], v[r].p[3]));
+        s[r][1] = 0ull;
+      }
+      group_sums<GL, R, W>(s, red, turn, c);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        mean[r] = c[r].x * inv;
+        const float m = act ? -mean[r] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kE / 2; ++i) v[r].p[i] = add2(v[r].p[i], pk(m, m));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[r][0] = s[r][1] = 0ull;
+#pragma unroll
+      for (int i = 0; i < kE / 2; ++i) s[r][0] = fma2(v[r].p[i], v[r].p[i], s[r][0]);
+    }
+    group_sums<GL, R, W>(s, red, turn, c);
+    const F8 wv = w.get(j, n, d);
+    F8 bv = zero8();
+    if (bias) bv = b.get(j, n, d);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      rstd[r] = rsqrtf(c[r].x * inv + a.eps);
+#pragma unroll
+      for (int i = 0; i < kE / 2; ++i)
+        v[r].p[i] = fma2(mul2(v[r].p[i], pk(rstd[r], rstd[r])), wv.p[i], bv.p[i]);
+    }
+  };
+  while (at.more()) {
+    const Walk here = at;
+    if (a.gate && a.gate_rows)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int g = min(row_of(here, r), a.T - 1) / a.gate_rows;
+        if (g != gate_at[r]) {
+          gate[r].set(a.gate + (long long)g * d, j, n, d);
+          gate_at[r] = g;
+        }
+      }
+    fetch(kRing - 1);
+    const uint32_t valid = valids & ((1u << R) - 1u);
+    valids >>= R;
+    asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+    const int ring_at = get;
+    if (++get == kRing) get = 0;
+    at.next(kStep);
+    const uint32_t present = (row_of(here, 1) < here.end ? 2u : 0u) | (row_of(here, 0) < here.end ? 1u : 0u);
+    float m1[R], r1[R], m2[R], r2[R];
+    if (GL || valid) {  // (without groups in warps the whole CTA agrees)
+      F8 o[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float t[kE];
+        ring_read(slot(ring_at, r), threads, a.x, t);
+        o[r] = pairs(t);
+      }
+      if (a.y) {
+        F8 z[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float t[kE];
+          ring_read(slot(ring_at, r) + kPX * threads, threads, a.y, t);
+          z[r] = pairs(t);
+        }
+        if (a.post) norm_rows(z, a.post, w_post, b_post, a.b_post, m1, r1);
+        const uint64_t sc = pk(a.scale, a.scale);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (a.gate) {
+            const F8 g = gate[r].get(j, n, d);
+#pragma unroll
+            for (int i = 0; i < kE / 2; ++i) z[r].p[i] = mul2(z[r].p[i], g.p[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < kE / 2; ++i) o[r].p[i] = fma2(o[r].p[i], sc, z[r].p[i]);
+          if (a.out && (valid >> r & 1u)) {
+            float t[kE];
+            singles(o[r], t);
+            store<true>(a.out + row_of(here, r) * a.ld_out, j, n, d, t);
+          }
+        }
+      }
+      if (a.pre) {
+        norm_rows(o, a.pre, w_pre, b_pre, a.b_pre, m2, r2);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (valid >> r & 1u) {
+            float t[kE];
+            singles(o[r], t);
+            store<true>(a.u + row_of(here, r) * a.ld_u, j, n, d, t);
+          }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (!(present >> r & 1u)) continue;
+      const bool v = valid >> r & 1u;
+      const int row = row_of(here, r);
+      if (!v) {  // padding gives 0
+        float t[kE];
+#pragma unroll
+        for (int i = 0; i < kE; ++i) t[i] = 0.f;
+        if (a.y && a.out) store<true>(a.out + row * a.ld_out, j, n, d, t);
+        if (a.pre) store<true>(a.u + row * a.ld_u, j, n, d, t);
+      }
+      if (j == 0) {
+        if (a.y && a.post) {
+          if (a.m_post) a.m_post[row] = v ? m1[r] : 0.f;
+          if (a.r_post) a.r_post[row] = v ? r1[r] : 0.f;
+        }
+        if (a.pre) {
+          if (a.m_pre) a.m_pre[row] = v ? m2[r] : 0.f;
+          if (a.r_pre) a.r_pre[row] = v ? r2[r] : 0.f;
+        }
+      }
+    }
+  }
+}
+
 struct FinishArgs {
   int d, ctas, pieces, gates;  // gates: gate rows whose pieces are added here
   int sums;                    // 4, and the gate row where there is one: sums over all CTAs
@@ -995,9 +1215,40 @@ bool vec_ok(const T* p, long long ld) {
   return reinterpret_cast<uintptr_t>(p) % (kE * sizeof(T)) == 0 && ld % kE == 0;
 }
 
+template <typename TX, typename TB, int GL, int MT>
+cudaError_t launch_stream(const ForwardArgs<TX, TB>& a, int threads, int sms, cudaStream_t s) {
+  const int smem = stream_steps<TX, TB>() * 2 * kE * (int)(sizeof(TX) + sizeof(TB)) * threads;
+  const cudaError_t e = allow_smem_once(forward_stream_kernel<TX, TB, GL, MT>, smem);
+  if (e != cudaSuccess) return e;
+  const int groups = GL ? MT / (GL ? GL : 1) : 1, chunk = 4 * groups;  // two steps
+  const long long chunks = ((long long)a.T + chunk - 1) / chunk;
+  const int most = sms * (512 / threads);
+  forward_stream_kernel<TX, TB, GL, MT>
+      <<<(unsigned)(chunks < most ? chunks : most), threads, smem, s>>>(a, chunk);
+  return cudaGetLastError();
+}
+
 template <typename TX, typename TB, bool VEC>
-cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, cudaStream_t s) {
+cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, int sms, cudaStream_t s) {
   const int threads = cta_threads(a.d);
+  // A bf16 stream: forward_stream_kernel once every SM has 16 rows for each group of a
+  // CTA. us, one row after the other against it: 9,728 x 384 13.6 and 9.9, x 1,024 24.4
+  // and 18.5, x 4,096 91 and 86, 77,824 x 80 20.0 and 16.1; with half as many rows
+  // 9,728 x 80 3.9 and 4.3. An fp32 stream has more bytes for the same work and more
+  // CTAs hide them better: 9,728 x 1,024 over bf16 24.7 and 27.4, over fp32 x 2,048 55
+  // and 86.
+  if constexpr (VEC && sizeof(TX) == 2) {
+    const int groups = group_lanes(a.d) ? kThreads / group_lanes(a.d) : 1;
+    if (threads <= 512 && a.T >= 16ll * groups * sms) {
+      switch (group_lanes(a.d)) {
+        case 8: return launch_stream<TX, TB, 8, kThreads>(a, threads, sms, s);
+        case 16: return launch_stream<TX, TB, 16, kThreads>(a, threads, sms, s);
+        case 32: return launch_stream<TX, TB, 32, kThreads>(a, threads, sms, s);
+      }
+      if (threads <= 128) return launch_stream<TX, TB, 0, 128>(a, threads, sms, s);
+      return launch_stream<TX, TB, 0, 512>(a, threads, sms, s);
+    }
+  }
   switch (group_lanes(a.d)) {
     case 8: forward_kernel<TX, TB, VEC, 8, kThreads><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
     case 16: forward_kernel<TX, TB, VEC, 16, kThreads><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
@@ -1082,7 +1333,7 @@ int check_desc(const unif_moe_block_norm* p) {
 bool ld_bad(const void* p, long long ld, int d) { return p && ld < d; }
 
 template <typename TX, typename TB>
-cudaError_t forward_as(const unif_moe_block_norm* p, const void* x, long long ld_x, const void* y,
+cudaError_t forward_as(const unif_moe_block_norm* p, int sms, const void* x, long long ld_x, const void* y,
                        long long ld_y, const uint8_t* mask, const void* w_post, const void* b_post,
                        const void* gate, const void* w_pre, const void* b_pre, void* out,
                        long long ld_out, void* u, long long ld_u, float* m_post, float* r_post,
@@ -1099,7 +1350,7 @@ cudaError_t forward_as(const unif_moe_block_norm* p, const void* x, long long ld
                    (!out || vec_ok(a.out, ld_out)) && (!u || vec_ok(a.u, ld_u)) &&
                    vec_ok(a.w_post, 0) && vec_ok(a.b_post, 0) && vec_ok(a.gate, 0) &&
                    vec_ok(a.w_pre, 0) && vec_ok(a.b_pre, 0);
-  return vec ? launch_fwd<TX, TB, true>(a, s) : launch_fwd<TX, TB, false>(a, s);
+  return vec ? launch_fwd<TX, TB, true>(a, sms, s) : launch_fwd<TX, TB, false>(a, sms, s);
 }
 
 int64_t workspace_floats(const Plan& pl, int d) {
@@ -1184,9 +1435,12 @@ int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int
     set_error("a row stride is below the width");
     return UNIF_MOE_ERR_ARG;
   }
+  int sms = 0;
+  const int rs = unif::sm_count(&sms);
+  if (rs != UNIF_MOE_OK) return rs;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-#define UNIF_ARGS p, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u, \
+#define UNIF_ARGS p, sms, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u, \
                   ld_u, m_post, r_post, m_pre, r_pre, s
   if (p->branch_dtype == UNIF_MOE_F32) e = nm::forward_as<float, float>(UNIF_ARGS);
   else if (p->stream_dtype == UNIF_MOE_F32) e = nm::forward_as<float, __nv_bfloat16>(UNIF_ARGS);

@@ -341,6 +341,43 @@ def test_in_place_and_repeatable():
     assert all(torch.equal(a[k], b[k]) for k in a)
 
 
+# Forwards over enough rows that a CTA takes several after one another: each width class,
+# rows that are no multiple of a CTA's, gates that change inside a CTA's rows.
+MANY = [
+    (39001, 48, "bf16", "bf16", "rms", "layer", 1, True, "some"),
+    (19999, 128, "bf16", "bf16", "layer", "rms", 7, True, None),
+    (9803, 200, "bf16", "bf16", "none", "layer", 197, False, "some"),
+    (5005, 384, "bf16", "bf16", "rms", "none", 1, True, "some"),
+    (2433, 1000, "bf16", "bf16", "layer", "layer", 0, True, "some"),
+    (2501, 4096, "bf16", "bf16", "rms", "rms", 64, False, None),
+    (3001, 320, "bf16", "bf16", "layer", "rms", 0, True, "all"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(map(str, c)))
+def test_forward_of_many_rows_against_64_bits(case):
+    test_forward_against_64_bits(case)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(5003, 384), (39007, 64)])
+def test_many_rows_in_place_and_without_a_branch(T, d):
+    cfg, v, e = make(T, d, "bf16", "bf16", "rms", "rms", 100, False, "some", seed=6, dev="cuda")
+    norm = layer_of(cfg, "bf16", "bf16")
+    params = {k: v[k] for k in PARAMS}
+    r = norm.forward(v["x"], v["y"], mask=v["mask"], **params)
+    x, y = v["x"].clone(), v["y"].clone()
+    norm.forward(x, y, mask=v["mask"], out=x, u=y, **params)
+    assert torch.equal(x, r["out"]) and torch.equal(y, r["u"])
+    # the stream's rows as they are, normed: what a few rows at a time give
+    norm = layer_of(dict(cfg, post="none", gate_rows=None, scale=1.0), "bf16", "bf16")
+    u = norm.forward(r["out"], pre_weight=v["pre_weight"])["u"]
+    for lo in (0, T // 2, T - 40):
+        part = norm.forward(r["out"][lo:lo + 40], pre_weight=v["pre_weight"])["u"].double().cpu()
+        close(u[lo:lo + 40], part, 2.0 ** -7 * part.abs() + 1e-4, "u")
+
+
 @pytest.mark.gpu
 def test_another_stream_and_no_tokens():
     cfg, v, e = make(500, 768, "f32", "bf16", "layer", "layer", 0, True, None, seed=8, dev="cuda")
