@@ -11,10 +11,10 @@
 // rounded once, to the type it is stored in.
 //
 // Measured (us; at the copy rate of 6.8 TB/s): forward of 12,608 x 384, fp32 stream,
-// 13.5 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 38 (24); backward of 12,608 x 768
+// 12.8 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 38 (24); backward of 12,608 x 768
 // bf16 with a gate per image 34 (17), of 65,536 x 1,024 padded, fp32 stream, 187 (178
 // for all rows). Widths that are no multiple of eight move value by value: backward
-// of 20,000 x 1,001 bf16 104 (35), forward 65 (24).
+// of 20,000 x 1,001 bf16 104 (35), forward 67 (24).
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -166,50 +166,18 @@ struct ForwardArgs {
   float *m_post, *r_post, *m_pre, *r_pre;
 };
 
-// Standardises v (the columns past d hold 0 and stay 0).
-template <bool VEC, int GL>
-__device__ __forceinline__ void standardise(float (&v)[kE], int kind, int j, int n, int d, float eps,
-                                            float* red, int& turn, float& mean, float& rstd) {
-  const float inv = 1.f / (float)d;
-  mean = 0.f;
-  if (kind == UNIF_MOE_NORM_LAYER) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < kE; ++i) s[0] += v[i];
-    group_sum<GL>(s, red, turn);
-    mean = s[0] * inv;
-#pragma unroll
-    for (int i = 0; i < kE; ++i)
-      if (column<VEC>(j, n, i) < d) v[i] -= mean;
-  }
-  float q[1] = {0.f};
-#pragma unroll
-  for (int i = 0; i < kE; ++i) q[0] = fmaf(v[i], v[i], q[0]);
-  group_sum<GL>(q, red, turn);
-  rstd = rsqrtf(q[0] * inv + eps);
-#pragma unroll
-  for (int i = 0; i < kE; ++i) v[i] *= rstd;
+// One row to a group of threads. MT: most threads of a CTA; without VEC the threads, so
+// that the columns' offsets are constants (with an offset and a bound worked out per
+// value, a row of 333 took 1,850 instructions a warp in the backward). With VEC a thread keeps
+// to 32 registers (else 40), so that all 64 warps are on an SM (9,728 x 4,096 fp32 124 us with one CTA, 98
+// with two; bf16 parameters 8,192 wide 218 and 208). Not in groups of fp32 vectors, which would
+// spill (155,648 x 64 27.1 us, 28.2 so).
+template <typename TB, bool VEC, int GL, int MT>
+constexpr int least_ctas() {
+  return !VEC ? 1536 / MT : GL && sizeof(TB) == 4 ? 1 : 2048 / MT;
 }
-
-template <bool VEC, typename TB>
-__device__ __forceinline__ void scale_shift(float (&v)[kE], const TB* w, const TB* b, int j, int n,
-                                            int d) {
-  float t[kE];
-  load<VEC>(w, j, n, d, t);
-#pragma unroll
-  for (int i = 0; i < kE; ++i) v[i] *= t[i];
-  if (b) {
-    load<VEC>(b, j, n, d, t);
-#pragma unroll
-    for (int i = 0; i < kE; ++i) v[i] += t[i];
-  }
-}
-
-// MT: most threads of a CTA; without VEC the threads, so that the columns' offsets are
-// constants (with an offset and a bound worked out per value, a row of 333 took 1,850
-// instructions a warp in the backward).
 template <typename TX, typename TB, bool VEC, int GL, int MT>
-__global__ void __launch_bounds__(MT)
+__global__ void __launch_bounds__(MT, least_ctas<TB, VEC, GL, MT>())
     forward_kernel(const ForwardArgs<TX, TB> a) {
   __shared__ float red[2 * 2 * kMaxWarps];
   int turn = 0;
@@ -219,41 +187,68 @@ __global__ void __launch_bounds__(MT)
   const int d = a.d;
   // every lane of a warp takes part in the shuffles, also past the last row
   const int row = blockIdx.x * rows + (GL ? (int)threadIdx.x / (GL ? GL : 1) : 0);
-  const bool in = row < a.T;
-  const bool valid = in && (!a.mask || a.mask[row]);
+  const bool in = row < a.T, valid = in && (!a.mask || a.mask[row]);
+  const bool act = valid && (!VEC || j * kE < d);  // has columns of a row that counts
   float o[kE], z[kE];
 #pragma unroll
   for (int i = 0; i < kE; ++i) o[i] = z[i] = 0.f;
-  if (valid) load<VEC>(a.x + row * a.ld_x, j, n, d, o);
+  if (act) {
+    load<VEC>(a.x + row * a.ld_x, j, n, d, o);
+    if (a.y) load<VEC>(a.y + row * a.ld_y, j, n, d, z);
+  }
+  float mean = 0.f, rstd = 0.f;
+  const float inv = 1.f / (float)d;
+  auto norm = [&](float (&v)[kE], int kind, const TB* w, const TB* b) {
+    if (!GL && !valid) return;  // (the whole CTA)
+    float s[1] = {0.f}, t[kE];
+    mean = 0.f;
+    if (kind == UNIF_MOE_NORM_LAYER) {
+#pragma unroll
+      for (int i = 0; i < kE; ++i) s[0] += v[i];
+      group_sum<GL>(s, red, turn);
+      mean = s[0] * inv;
+      const float m = act ? mean : 0.f;  // columns past d hold 0 and stay 0
+#pragma unroll
+      for (int i = 0; i < kE; ++i)
+        if (VEC || column<false>(j, n, i) < d) v[i] -= m;
+      s[0] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i) s[0] = fmaf(v[i], v[i], s[0]);
+    group_sum<GL>(s, red, turn);
+    rstd = rsqrtf(s[0] * inv + a.eps);
+    if (!act) return;
+    load<VEC>(w, j, n, d, t);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = v[i] * rstd * t[i];
+    if (b) {
+      load<VEC>(b, j, n, d, t);
+#pragma unroll
+      for (int i = 0; i < kE; ++i) v[i] += t[i];
+    }
+  };
   if (a.y) {
-    if (valid) load<VEC>(a.y + row * a.ld_y, j, n, d, z);
     if (a.post) {
-      float mean, rstd;
-      standardise<VEC, GL>(z, a.post, j, n, d, a.eps, red, turn, mean, rstd);
-      scale_shift<VEC>(z, a.w_post, a.b_post, j, n, d);
+      norm(z, a.post, a.w_post, a.b_post);
       if (j == 0 && in) {
         if (a.m_post) a.m_post[row] = valid ? mean : 0.f;
         if (a.r_post) a.r_post[row] = valid ? rstd : 0.f;
       }
     }
-    if (a.gate && in) {
-      float g[kE];
-      const long long at = a.gate_rows ? row / a.gate_rows : 0;
-      load<VEC>(a.gate + at * d, j, n, d, g);
+    if (act) {
+      if (a.gate) {
+        float g[kE];
+        load<VEC>(a.gate_rows ? a.gate + (long long)(row / a.gate_rows) * d : a.gate, j, n, d, g);
 #pragma unroll
-      for (int i = 0; i < kE; ++i) z[i] *= g[i];
+        for (int i = 0; i < kE; ++i) z[i] *= g[i];
+      }
+#pragma unroll
+      for (int i = 0; i < kE; ++i) o[i] = fmaf(a.scale, o[i], z[i]);
     }
-#pragma unroll
-    for (int i = 0; i < kE; ++i) o[i] = valid ? fmaf(a.scale, o[i], z[i]) : 0.f;
     if (a.out && in) store<VEC>(a.out + row * a.ld_out, j, n, d, o);
   }
   if (a.pre) {
-    float mean, rstd;
-    standardise<VEC, GL>(o, a.pre, j, n, d, a.eps, red, turn, mean, rstd);
-    scale_shift<VEC>(o, a.w_pre, a.b_pre, j, n, d);
-    if (!valid)
-#pragma unroll
-      for (int i = 0; i < kE; ++i) o[i] = 0.f;
+    norm(o, a.pre, a.w_pre, a.b_pre);
     if (in) {
       store<VEC>(a.u + row * a.ld_u, j, n, d, o);
       if (j == 0) {
@@ -912,19 +907,16 @@ __host__ __device__ constexpr int stream_steps() {  // of a ring of 320 bytes a 
   return 320 / (2 * kE * (int)(sizeof(TX) + sizeof(TB)));
 }
 
-template <typename TX, typename TB, int GL, int MT>
-__global__ void __launch_bounds__(MT, 512 / MT)
+template <typename TX, typename TB>
+__global__ void __launch_bounds__(kThreads, 4)
     forward_stream_kernel(const ForwardArgs<TX, TB> a, const int chunk) {
-  constexpr int R = 2, W = MT / 32, kRing = stream_steps<TX, TB>();
+  constexpr int R = 2, W = kThreads / 32, kRing = stream_steps<TX, TB>();
   constexpr int kPX = kE * sizeof(TX) / 16, kPB = kE * sizeof(TB) / 16, kPlanes = kPX + kPB;
-  constexpr int kGroups = GL ? MT / (GL ? GL : 1) : 1, kStep = kGroups * R;
   extern __shared__ uint4 ring[];
-  __shared__ __align__(16) float red[GL ? 4 : 2 * 2 * R * W];
+  __shared__ __align__(16) float red[2 * 2 * R * W];
   const int threads = (int)blockDim.x;
   int turn = 0;
-  const int n = GL ? GL : threads;
-  const int j = GL ? (int)threadIdx.x % (GL ? GL : 1) : (int)threadIdx.x;
-  const int grp = GL ? (int)threadIdx.x / (GL ? GL : 1) : 0;
+  const int n = threads, j = (int)threadIdx.x;
   const int d = a.d;
   const float inv = 1.f / (float)d;
   const bool act = j * kE < d;
@@ -943,8 +935,8 @@ __global__ void __launch_bounds__(MT, 512 / MT)
     for (int k = 0; k < kRing * R; ++k)
 #pragma unroll
       for (int i = 0; i < kPlanes; ++i) slot(0, k)[i * threads] = make_uint4(0u, 0u, 0u, 0u);
-  if (!GL && threadIdx.x < 2 * 2 * R * W) red[threadIdx.x] = 0.f;
-  if (!GL) __syncthreads();
+  if (threadIdx.x < 2 * 2 * R * W) red[threadIdx.x] = 0.f;
+  __syncthreads();
 
   Walk at;
   at.cut = false;
@@ -955,7 +947,7 @@ __global__ void __launch_bounds__(MT, 512 / MT)
   at.skip = (int)min((long long)a.T, (long long)(gridDim.x - 1) * chunk);
   at.end = min(at.last - at.base, chunk) + at.base;
   Walk ahead = at;
-  auto row_of = [&](const Walk& w, int r) { return w.base + r * kGroups + grp; };
+  auto row_of = [&](const Walk& w, int r) { return w.base + r; };
   auto validity = [&](const Walk& w) {
     uint32_t v = 0;
 #pragma unroll
@@ -979,12 +971,12 @@ __global__ void __launch_bounds__(MT, 512 / MT)
             ring_copy(to, a.x + row * a.ld_x + j * kE, threads);
             if (a.y) ring_copy(to + kPX * threads, a.y + row * a.ld_y + j * kE, threads);
           }
-        } else if (GL || next_valid) {
+        } else if (next_valid) {
 #pragma unroll
           for (int i = 0; i < kPlanes; ++i) to[i * threads] = make_uint4(0u, 0u, 0u, 0u);
         }
       }
-      ahead.next(kStep);
+      ahead.next(R);
       next_valid = validity(ahead);
       if (++put == kRing) put = 0;
     }
@@ -1006,7 +998,7 @@ __global__ void __launch_bounds__(MT, 512 / MT)
         s[r][0] = add2(add2(v[r].p[0], v[r].p[1]), add2(v[r].p[2], v[r].p[3]));
         s[r][1] = 0ull;
       }
-      group_sums<GL, R, W>(s, red, turn, c);
+      group_sums<0, R, W>(s, red, turn, c);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         mean[r] = c[r].x * inv;
@@ -1021,7 +1013,7 @@ __global__ void __launch_bounds__(MT, 512 / MT)
 #pragma unroll
       for (int i = 0; i < kE / 2; ++i) s[r][0] = fma2(v[r].p[i], v[r].p[i], s[r][0]);
     }
-    group_sums<GL, R, W>(s, red, turn, c);
+    group_sums<0, R, W>(s, red, turn, c);
     const F8 wv = w.get(j, n, d);
     F8 bv = zero8();
     if (bias) bv = b.get(j, n, d);
@@ -1050,10 +1042,10 @@ __global__ void __launch_bounds__(MT, 512 / MT)
     asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
     const int ring_at = get;
     if (++get == kRing) get = 0;
-    at.next(kStep);
+    at.next(R);
     const uint32_t present = (row_of(here, 1) < here.end ? 2u : 0u) | (row_of(here, 0) < here.end ? 1u : 0u);
     float m1[R], r1[R], m2[R], r2[R];
-    if (GL || valid) {  // (without groups in warps the whole CTA agrees)
+    if (valid) {  // (the whole CTA agrees)
       F8 o[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
@@ -1215,40 +1207,27 @@ bool vec_ok(const T* p, long long ld) {
   return reinterpret_cast<uintptr_t>(p) % (kE * sizeof(T)) == 0 && ld % kE == 0;
 }
 
-template <typename TX, typename TB, int GL, int MT>
+template <typename TX, typename TB>
 cudaError_t launch_stream(const ForwardArgs<TX, TB>& a, int threads, int sms, cudaStream_t s) {
   const int smem = stream_steps<TX, TB>() * 2 * kE * (int)(sizeof(TX) + sizeof(TB)) * threads;
-  const cudaError_t e = allow_smem_once(forward_stream_kernel<TX, TB, GL, MT>, smem);
-  if (e != cudaSuccess) return e;
-  const int groups = GL ? MT / (GL ? GL : 1) : 1, chunk = 4 * groups;  // two steps
+  constexpr int chunk = 4;  // two steps
   const long long chunks = ((long long)a.T + chunk - 1) / chunk;
   const int most = sms * (512 / threads);
-  forward_stream_kernel<TX, TB, GL, MT>
-      <<<(unsigned)(chunks < most ? chunks : most), threads, smem, s>>>(a, chunk);
+  forward_stream_kernel<TX, TB><<<(unsigned)(chunks < most ? chunks : most), threads, smem, s>>>(a, chunk);
   return cudaGetLastError();
 }
 
 template <typename TX, typename TB, bool VEC>
 cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, int sms, cudaStream_t s) {
   const int threads = cta_threads(a.d);
-  // A bf16 stream: forward_stream_kernel once every SM has 16 rows for each group of a
-  // CTA. us, one row after the other against it: 9,728 x 384 13.6 and 9.9, x 1,024 24.4
-  // and 18.5, x 4,096 91 and 86, 77,824 x 80 20.0 and 16.1; with half as many rows
-  // 9,728 x 80 3.9 and 4.3. An fp32 stream has more bytes for the same work and more
-  // CTAs hide them better: 9,728 x 1,024 over bf16 24.7 and 27.4, over fp32 x 2,048 55
-  // and 86.
-  if constexpr (VEC && sizeof(TX) == 2) {
-    const int groups = group_lanes(a.d) ? kThreads / group_lanes(a.d) : 1;
-    if (threads <= 512 && a.T >= 16ll * groups * sms) {
-      switch (group_lanes(a.d)) {
-        case 8: return launch_stream<TX, TB, 8, kThreads>(a, threads, sms, s);
-        case 16: return launch_stream<TX, TB, 16, kThreads>(a, threads, sms, s);
-        case 32: return launch_stream<TX, TB, 32, kThreads>(a, threads, sms, s);
-      }
-      if (threads <= 128) return launch_stream<TX, TB, 0, 128>(a, threads, sms, s);
-      return launch_stream<TX, TB, 0, 512>(a, threads, sms, s);
-    }
-  }
+  // A bf16 stream of 257 to 1,024 columns: forward_stream_kernel once every SM has 16
+  // rows. us, a row to a group of threads against it: 9,728 x 384 12.3 and 10.0, x 1,024 22.0
+  // and 18.5, x 2,048 39.7 and 41.6; 77,824 x 80 16.9 and 16.1, 19,456 x 80 5.1 and 5.5. An fp32
+  // stream has more bytes for the same work and more CTAs hide them better: 9,728 x 1,024
+  // over bf16 23.6 and 27.4.
+  if constexpr (VEC && sizeof(TX) == 2)
+    if (!group_lanes(a.d) && threads <= kThreads && a.T >= 16ll * sms)
+      return launch_stream(a, threads, sms, s);
   switch (group_lanes(a.d)) {
     case 8: forward_kernel<TX, TB, VEC, 8, kThreads><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
     case 16: forward_kernel<TX, TB, VEC, 16, kThreads><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
