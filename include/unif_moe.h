@@ -570,7 +570,7 @@ enum { UNIF_MOE_ACTIVATION_NONE = 0, UNIF_MOE_ACTIVATION_GELU = 1 };
  *     start has no rows, a row of two groups gets one's result, and groups that together have more than `rows` rows lose the
  *     last ones. Rows of no group are not written
  *   activation  UNIF_MOE_ACTIVATION_*: GELU is 0.5 v (1 + erf(v / sqrt 2)), for bf16
- *     output within 3e-4 |v| of it before the rounding
+ *     output within 2^-11 of itself (or 2e-37) before the rounding
  *   out_dev [rows][n] fp32 or bf16, rows ld apart
  *   status_dev [1] int32: a kernel that gives up a wait sets it non-zero (zero it
  *     before the first call); the output is then incomplete
