@@ -31,7 +31,7 @@ using namespace tc;
 
 constexpr int kTN = 192;         // rows of a tile (MMA N)
 constexpr int kStep = 256;       // columns of a step: 128 bytes of codes, 8 scales
-// Stages of the ring; fewer where the table of groups (from about 670 on) needs the room.
+// Stages of the ring; fewer where the table of groups (from 324 on) needs the room.
 constexpr int kMaxStages = 5, kFewStages = 3;
 constexpr uint32_t kBytesW = 128 * 128;
 // Row codes of a stage: the tile's rows, or with PAIR this CTA's half of them.
@@ -114,7 +114,7 @@ __device__ __forceinline__ uint32_t idesc_mxf4(bool pair, int n, int scale_byte)
          (1u << 23) | ((pair ? 2u : 1u) << 27) | ((uint32_t)scale_byte << 29);
 }
 
-constexpr uint32_t kSmemMax = 232448;  // shared memory that a CTA can have
+constexpr uint32_t kSmemMax = 232448;  // shared memory that a CTA can have, all of it dynamic
 static_assert(smem_bytes(false, kFewStages, UNIF_MOE_MXFP4_MAX_GROUPS) <= kSmemMax, "shared memory");
 
 __device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long long limit) {
@@ -325,8 +325,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       tmem_relinquish();
     }
   }
-  __shared__ long long rows_sh[kThreads / 32];
-  __shared__ int tiles_sh[kThreads / 32];
+  // the warps' sums of rows and tiles, where the list of items comes later: no shared
+  // memory beside that of smem_bytes
+  long long* rows_sh = reinterpret_cast<long long*>(list_s);
+  int* tiles_sh = reinterpret_cast<int*>(rows_sh + kThreads / 32);
+  static_assert(kThreads / 32 * 12 <= kListed * sizeof(Item), "the list holds the warps' sums");
   grid_dep_wait();
   // Row tiles before each group; whatever the offsets hold, rows stay in [0, rows) and
   // the groups have no more than `rows` rows together.

@@ -239,6 +239,20 @@ def test_stream_argument_and_a_capture_first():
         operators._status_words.update(kept)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [309, 310, 311, 320, 323, 324, 325])
+def test_group_counts_at_which_the_ring_gets_shorter(G):
+    """The table of groups takes shared memory beside the ring of stages: on both sides
+    of the count from which the ring has fewer."""
+    g = torch.Generator().manual_seed(G)
+    sizes = torch.randint(0, 9, (G,), generator=g).tolist()
+    check(sizes, 64, 128, seed=G)
+    # rows as the M operand: 64 rows a group, channels that 128-channel tiles would waste
+    sizes = torch.randint(40, 90, (G,), generator=g).tolist()
+    sizes[7] += max(0, 64 * G - sum(sizes))
+    check(sizes, 160, 64, act="gelu", seed=G)
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()
