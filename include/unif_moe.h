@@ -512,14 +512,16 @@ UNIF_MOE_API int64_t unif_moe_balance_workspace(int T, int K);
  *     router's product [T][K + 1] are such rows); no alignment needed
  *   q_dev [T][n_q] int32, rows ld_q apart: the experts of a token; k_dev [T] int32 or
  *     NULL: only the first k_t of them count (unif_moe_get_routing's q with the
- *     forward's residual_counts). Entries outside [0, K) are skipped
+ *     forward's residual_counts). Entries outside [0, K) are skipped. Sums
+ *     over all tokens are 64-bit; the tokens that one CTA takes may select up to
+ *     0x7fff0000 experts (T n_q up to that is always accepted)
  *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose logits are not read
  * A token whose logits are all -inf counts as padding. With no token left, losses, counts and prob
  * are 0. Outputs (device, overwritten): loss_dev [3] = loss, balance, zloss;
- * counts_dev [K] = c; prob_dev [K] = P; dlogits_dev [T][K] fp32 or NULL (0 for
+ * counts_dev [K] = c, at most 2^31 - 1; prob_dev [K] = P; dlogits_dev [T][K] fp32 or NULL (0 for
  * padding). Sums over tokens are added in a fixed order.
  * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (K above
- * UNIF_MOE_BALANCE_MAX_EXPERTS), ERR_CAPACITY (workspace), ERR_CUDA. */
+ * UNIF_MOE_BALANCE_MAX_EXPERTS; n_q), ERR_CAPACITY (workspace), ERR_CUDA. */
 UNIF_MOE_API int unif_moe_balance_loss(int T, int K, const void* logits_dev, unif_moe_dtype dtype,
                                        int64_t ld, const int32_t* q_dev, int n_q, int64_t ld_q,
                                        const int32_t* k_dev, const uint8_t* token_mask_dev,

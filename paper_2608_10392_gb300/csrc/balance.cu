@@ -61,6 +61,9 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// A count as it is given to the caller.
+__device__ __forceinline__ int count32(long long c) { return (int)min(c, 0x7fffffffll); }
+
 // Lane `lane` of a token's L lanes holds the columns lane E .. lane E + E - 1.
 template <typename T, int L, int E, bool VEC>
 __device__ __forceinline__ void load(const Args& a, bool in, int t, int lane, float (&z)[E]) {
@@ -221,17 +224,18 @@ template <typename T, int L, int E, bool VEC, int TH, int U>
 __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
   constexpr int kWarps = TH / 32;
   extern __shared__ float f[];  // [K] f, then [K] mean probabilities (first CTA)
-  __shared__ int all[2];
+  __shared__ unsigned long long all_c;  // selections of all tokens: beyond 32 bits
+  __shared__ int all_n;
   __shared__ float zsum;
   float* prob = f + a.K;
   const int lane32 = threadIdx.x & 31, warp = threadIdx.x / 32;
   const bool first = blockIdx.x == 0;
-  if (threadIdx.x == 0) all[0] = 0;
+  if (threadIdx.x == 0) all_c = 0;
   grid_dep_wait();
   __syncthreads();
   // a warp per column adds the CTAs' sums (whole numbers, and in a fixed order)
   for (int c = warp; c < a.K; c += kWarps) {
-    int m = 0;
+    long long m = 0;
     float q = 0.f;
     for (int i = lane32; i < a.ctas; i += 32) {
       m += a.part_c[(long long)c * a.ctas + i];
@@ -243,11 +247,11 @@ __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
       q += __shfl_xor_sync(0xffffffffu, q, o);
     }
     if (lane32 == 0) {
-      f[c] = __int_as_float(m);
-      atomicAdd(&all[0], m);
+      f[c] = (float)m;
+      atomicAdd(&all_c, (unsigned long long)m);
       if (first) {
         prob[c] = q;
-        a.counts[c] = m;
+        a.counts[c] = count32(m);
       }
     }
   }
@@ -264,13 +268,13 @@ __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
       z += __shfl_xor_sync(0xffffffffu, z, o);
     }
     if (lane32 == 0) {
-      all[1] = n;
+      all_n = n;
       zsum = z;
     }
   }
   __syncthreads();
-  const float inv_c = 1.f / (float)max(all[0], 1), inv_n = 1.f / (float)max(all[1], 1);
-  for (int c = threadIdx.x; c < a.K; c += TH) f[c] = (float)__float_as_int(f[c]) * inv_c;
+  const float inv_c = 1.f / (float)max(all_c, 1ull), inv_n = 1.f / (float)max(all_n, 1);
+  for (int c = threadIdx.x; c < a.K; c += TH) f[c] *= inv_c;
   __syncthreads();
   if (first && warp == 0) {
     float b = 0.f;
@@ -351,7 +355,8 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   constexpr int kWarps = TH / 32, kTok = TH / L;
   extern __shared__ float sh[];  // [kWarps][K] shares; then [K] sums, [K] counts, [K] f
   __shared__ float z_sh[kWarps], zsum;
-  __shared__ int n_sh[kWarps], all[2], mine[2];
+  __shared__ int n_sh[kWarps], all_n, mine[2];
+  __shared__ unsigned long long all_c;
   float* sum_p = sh + kWarps * a.K;
   int* cnt = reinterpret_cast<int*>(sum_p + a.K);
   float* f = sum_p + 2 * a.K;
@@ -360,7 +365,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   const uint32_t ranks = gridDim.x;  // one cluster
   const int held = (int)((a.T + ranks * kTok - 1) / (ranks * kTok));  // tokens of a group, <= U
   for (int i = threadIdx.x; i < a.K; i += TH) cnt[i] = 0;
-  if (threadIdx.x < 2) all[threadIdx.x] = 0;
+  if (threadIdx.x == 0) all_c = 0;
   float z[U][E], lse[U];
   int m[U], q0[U];
   bool in[U];
@@ -446,24 +451,24 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   }
   cluster_sync();
   const bool first = blockIdx.x == 0;
-  int total = 0;
+  long long total = 0;
   for (int c = threadIdx.x; c < a.K; c += TH) {
-    int k = 0;
+    long long k = 0;
     float s = 0.f;
     for (uint32_t r = 0; r < ranks; ++r) {
       k += (int)read_rank(of_rank(cnt + c, r));
       if (first) s += __uint_as_float(read_rank(of_rank(sum_p + c, r)));
     }
-    f[c] = __int_as_float(k);
+    f[c] = (float)k;
     total += k;
     if (first) {
-      a.counts[c] = k;
+      a.counts[c] = count32(k);
       sh[c] = s;  // (the shares have been added)
     }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (lane32 == 0) atomicAdd(&all[0], total);
+  if (lane32 == 0) atomicAdd(&all_c, (unsigned long long)total);
   if (threadIdx.x == TH - 1) {
     int k = 0;
     float s = 0.f;
@@ -472,16 +477,16 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
       k += (int)read_rank(of_rank(&mine[1], r));
     }
     zsum = s;
-    all[1] = k;
+    all_n = k;
   }
   cluster_sync();  // nothing is read from another CTA any more; all of this CTA's is written
-  const float inv_c = 1.f / (float)max(all[0], 1), inv_n = 1.f / (float)max(all[1], 1);
+  const float inv_c = 1.f / (float)max(all_c, 1ull), inv_n = 1.f / (float)max(all_n, 1);
   if (first && warp == 0) {
     float b = 0.f;
     for (int c = lane32; c < a.K; c += 32) {
       const float q = sh[c] * inv_n;
       a.prob[c] = q;
-      b = fmaf((float)__float_as_int(f[c]) * inv_c, q, b);
+      b = fmaf(f[c] * inv_c, q, b);
     }
     b = lanes_sum<32>(b) * (float)a.K;
     if (lane32 == 0) {
@@ -496,7 +501,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   float fr[E];
 #pragma unroll
   for (int i = 0; i < E; ++i)
-    fr[i] = lane * E + i < a.K ? (float)__float_as_int(f[lane * E + i]) * inv_c : 0.f;
+    fr[i] = lane * E + i < a.K ? f[lane * E + i] * inv_c : 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (u >= held) break;
@@ -548,6 +553,14 @@ bool in_cluster(int T, int K) {
 int cta_count(int T, int K, int sms) {
   const long long tok = threads_of(K) / lanes_of(K), want = ((long long)T + tok - 1) / tok;
   return (int)(want < 1 ? 1 : want > sms ? sms : want);
+}
+
+// The most tokens that one CTA takes. Its counts are 32-bit, the sums over CTAs are not.
+long long tokens_per_cta(int T, int K, int ctas) {
+  const long long tok = threads_of(K) / lanes_of(K);
+  // (a cluster of eight: up to four tokens of each group of lanes)
+  const long long most = in_cluster(T, K) ? 4 * tok : ((T + tok - 1) / tok + ctas - 1) / ctas * tok;
+  return most < T ? most : T;
 }
 
 template <typename T, int L, int E, bool VEC, int TH, int U>
@@ -660,11 +673,17 @@ int unif_moe_balance_loss(int T, int K, const void* logits, unif_moe_dtype dtype
     set_error("the weights of the losses must be finite");
     return UNIF_MOE_ERR_ARG;
   }
-  int sms = 0;
-  const int rs = unif::sm_count(&sms);
-  if (rs != UNIF_MOE_OK) return rs;
+  int sms = 1;
+  if (!bl::in_cluster(T, K)) {
+    const int rs = unif::sm_count(&sms);
+    if (rs != UNIF_MOE_OK) return rs;
+  }
   bl::Args a{};
   a.ctas = bl::cta_count(T, K, sms);
+  if (bl::tokens_per_cta(T, K, a.ctas) * n_q > 0x7fff0000) {  // (a lane's index goes 32 beyond)
+    set_error("n_q=%d: too many selections for one CTA's tokens", n_q);
+    return UNIF_MOE_ERR_SHAPE;
+  }
   int64_t at[4] = {};
   const int64_t need = bl::in_cluster(T, K) ? 0 : bl::layout(K, a.ctas, at);
   if (workspace_bytes < need || (need && !workspace)) {

@@ -168,6 +168,50 @@ def test_counts_follow_the_layers_routing():
     assert r["counts"].tolist() == want
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4096, 1 << 22], ids=["one_kernel", "two_kernels"])
+def test_selections_beyond_32_bits(T):
+    """2^31 selections in all (8.6 GB of them): their total does not fit in 32 bits. The
+    same for 2^31 of one expert, whose count is then given as 2^31 - 1."""
+    from paper_2608_10392_gb300 import balance_loss
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    K, n_q = 8, (1 << 31) // T
+    pattern = torch.tensor([0, 0, 0, 1, 1, 2, 3, 4, 5, 6, 7, 7, 7, 7, 7, 7], dtype=torch.int32,
+                           device="cuda")
+    q = torch.empty(1 << 31, dtype=torch.int32, device="cuda")
+    q.view(-1, 16).copy_(pattern.expand(1 << 27, 16))
+    z = torch.randn(T, K, generator=torch.Generator("cuda").manual_seed(T), device="cuda")
+    wb, wz = 0.02, 0.003
+    p, lse = torch.softmax(z.double(), 1), torch.logsumexp(z.double(), 1)
+    P, zl = p.mean(0), lse.square().mean()
+    for counts in (torch.bincount(pattern.long(), minlength=K) << 27,
+                   torch.tensor([0, 0, 0, 1 << 31, 0, 0, 0, 0], device="cuda")):
+        if counts[3] == 1 << 31:
+            q.fill_(3)
+        r = balance_loss(z, q.view(T, n_q), balance_weight=wb, z_weight=wz)
+        f = counts.double() / 2.0 ** 31
+        b, fp = K * (f * P).sum(), (p * f).sum(1, keepdim=True)
+        assert torch.equal(r["counts"].long(), counts.clamp(max=(1 << 31) - 1))
+        want = torch.stack([wb * b + wz * zl, b, zl])
+        assert ((r["loss"].double() - want).abs() <= 2e-5 * (want + 1)).all(), (r["loss"], want)
+        d = p / T * (wb * K * (f - fp) + 2 * wz * lse[:, None])
+        size = p / T * (wb * K * (f + fp) + 2 * wz * (lse.abs() + 1)[:, None])
+        assert ((r["dlogits"].double() - d).abs() <= 2e-5 * size).all()
+
+
+def test_more_selections_than_a_cta_counts_are_refused():
+    """2^31 selections in a CTA's tokens, whose counts are 32-bit (no GPU needed)."""
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    L = pkg.lib()
+    p, n_q = C.c_void_p(4096), 1 << 30
+    assert L.unif_moe_balance_loss(4, 8, p, 0, 8, p, n_q, n_q, None, None, 0.1, 0.1, p, p, p, None,
+                                   None, 0, None) == -2
+    assert b"selections" in L.unif_moe_last_error()
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()
