@@ -25,7 +25,7 @@ SOURCES = ["unif_moe.cu", "route_permute.cu", "gemm_simt.cu", "gemm_tc.cu", "gem
            "backward.cu", "diagnostics.cu", "gemm_fused.cu", "gemm_pair.cu",
            "bundles.cu", "block_norm.cu", "balance.cu", "mxfp4.cu",
            "fp4_product.cu"]
-HEADERS = ["internal.cuh", "decide.cuh", "items.cuh", "tc_common.cuh",
+HEADERS = ["internal.cuh", "decide.cuh", "items.cuh", "tc_common.cuh", "per_device.h",
            os.path.join("..", "..", "include", "unif_moe.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

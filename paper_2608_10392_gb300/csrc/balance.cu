@@ -19,9 +19,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
-#include <atomic>
-
 #include "internal.cuh"
+#include "per_device.h"
 
 namespace unif {
 namespace balance {
@@ -520,7 +519,8 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
 constexpr int kWide = 128;  // up to this many experts: CTAs of 1,024 threads
 inline int threads_of(int K) { return K <= kWide ? 1024 : 256; }
 
-// Whether clusters of 16 CTAs of this kernel can run (above the portable eight).
+// Whether clusters of 16 CTAs of this kernel can run on the current device (above the
+// portable eight); lets them be launched there.
 bool allow_cluster_16(const void* fn, int threads, size_t smem) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(16);
@@ -538,6 +538,24 @@ bool allow_cluster_16(const void* fn, int threads, size_t smem) {
     return true;
   cudaGetLastError();  // a refusal is no error of the call
   return false;
+}
+
+// The most CTAs of a cluster of this kernel on the current device: 16 where it takes that
+// many (not every one has to), else 8.
+unsigned largest_cluster(const void* fn, int threads, size_t smem) {
+  static PerDevice<unsigned> kept;
+  int dev = 0;
+  unsigned n = 8;
+  if (cudaGetDevice(&dev) != cudaSuccess) return n;
+  try {
+    kept.get(fn, dev, &n, [&](unsigned* to) {
+      *to = allow_cluster_16(fn, threads, smem) ? 16 : 8;
+      return true;
+    });
+  } catch (...) {  // no exception leaves the library
+    return 8;
+  }
+  return n;
 }
 
 // Lanes per token, and tokens that a cluster of eight CTAs holds at once (those of
@@ -566,16 +584,10 @@ long long tokens_per_cta(int T, int K, int ctas) {
 template <typename T, int L, int E, bool VEC, int TH, int U>
 cudaError_t launch_as(const Args& a, cudaStream_t s) {
   if (in_cluster(a.T, a.K)) {
-    // as many CTAs as have tokens, up to the largest cluster: 16 where the device
-    // takes that many (not every one has to), else 8
-    static std::atomic<unsigned> largest{0};
-    unsigned most = largest.load(std::memory_order_relaxed);
-    if (!most) {
-      most = allow_cluster_16(reinterpret_cast<const void*>(cluster_kernel<T, L, E, VEC, TH, U>), TH,
-                              (size_t)(TH / 32 + 3) * a.K * sizeof(float))
-                 ? 16 : 8;
-      largest.store(most, std::memory_order_relaxed);
-    }
+    // as many CTAs as have tokens, up to the largest cluster
+    const unsigned most = largest_cluster(
+        reinterpret_cast<const void*>(cluster_kernel<T, L, E, VEC, TH, U>), TH,
+        (size_t)(TH / 32 + 3) * a.K * sizeof(float));
     unsigned ctas = 1;
     while (ctas < most && (long long)ctas * (TH / L) < a.T) ctas *= 2;
     cudaLaunchConfig_t cfg = {};

@@ -11,12 +11,10 @@
 #include <string.h>
 #include <vector>
 
-#include <mutex>
 #include <new>
-#include <set>
-#include <utility>
 
 #include "internal.cuh"
+#include "per_device.h"
 
 namespace unif {
 
@@ -43,17 +41,16 @@ cudaError_t allow_smem(const void* fn, size_t need) {
 }
 
 cudaError_t allow_smem_once(const void* fn, size_t need) {
-  static std::mutex lock;
-  static std::set<std::pair<const void*, int>> done;
+  static PerDevice<cudaError_t> kept;
   int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   try {
-    std::lock_guard<std::mutex> hold(lock);
-    if (done.count({fn, dev})) return cudaSuccess;
-    const cudaError_t r = allow_smem(fn, need);
-    if (r == cudaSuccess) done.insert({fn, dev});
-    return r;
+    kept.get(fn, dev, &e, [&](cudaError_t* to) {
+      *to = allow_smem(fn, need);
+      return *to == cudaSuccess;
+    });
+    return e;
   } catch (...) {  // no exception leaves the library
     return cudaErrorMemoryAllocation;
   }
