@@ -419,14 +419,14 @@ struct Row8<__nv_bfloat16> {
   }
 };
 
-// A parameter's values of this thread's columns: bf16 ones stay in registers from
-// row to row as they were read, fp32 ones are read again.
+// A parameter's values of this thread's columns (0 where it is NULL or not `on`): bf16 ones
+// stay in registers from row to row as they were read, fp32 ones are read again.
 template <typename TB, bool VEC>
 struct Param {
   const TB* p = nullptr;
   __device__ __forceinline__ void set(const TB* q, int, int, int) { p = q; }
-  __device__ __forceinline__ F8 get(int j, int n, int d) const {
-    if (!p) return zero8();
+  __device__ __forceinline__ F8 get(int j, int n, int d, bool on = true) const {
+    if (!p || !on) return zero8();
     float v[kE];
     load<VEC>(p, j, n, d, v);
     return pairs(v);
@@ -437,19 +437,23 @@ struct Param<__nv_bfloat16, false> {
   Row8<__nv_bfloat16> held;
   __device__ __forceinline__ Param() { held.clear(); }
   __device__ __forceinline__ void set(const __nv_bfloat16* q, int j, int n, int d) {
+    held.clear();
     if (q) held.read(q, j, n, d);
   }
-  __device__ __forceinline__ F8 get(int, int, int) const { return held.get(); }
+  __device__ __forceinline__ F8 get(int, int, int, bool on = true) const {
+    return on ? held.get() : zero8();
+  }
 };
 template <>
 struct Param<__nv_bfloat16, true> {
   uint4 raw = {0u, 0u, 0u, 0u};
   __device__ __forceinline__ void set(const __nv_bfloat16* q, int j, int, int d) {
+    raw = make_uint4(0u, 0u, 0u, 0u);
     if (q && j * kE < d) raw = *reinterpret_cast<const uint4*>(q + j * kE);
   }
-  __device__ __forceinline__ F8 get(int, int, int) const {
+  __device__ __forceinline__ F8 get(int, int, int, bool on = true) const {
     float v[kE];
-    unpack(raw, v);
+    unpack(on ? raw : make_uint4(0u, 0u, 0u, 0u), v);
     return pairs(v);
   }
 };
@@ -837,8 +841,11 @@ __global__ void __launch_bounds__(MT, MT <= 384 ? 384 / MT : 1)
         if (a.gate)
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            if (each && (present >> r & 1u)) gate.set(a.gate + (long long)row_of(here, r) * d, j, n, d);
-            const F8 t = gate.get(j, n, d);
+            // 0 for padding, whose gate may hold NaN or infinity: these times 0 are NaN. (A
+            // gate row of several tokens is only padding's where no row of a step is valid.)
+            const bool v = valid >> r & 1u;
+            if (each) gate.set(v ? a.gate + (long long)row_of(here, r) * d : nullptr, j, n, d);
+            const F8 t = gate.get(j, n, d, !GL || v);
 #pragma unroll
             for (int i = 0; i < kE / 2; ++i) D[r].p[i] = mul2(D[r].p[i], t.p[i]);
           }

@@ -435,6 +435,58 @@ def test_stream_argument():
     assert all(torch.equal(o["u"], first["u"]) for o in outs)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [
+    # a gate row per token: two rows a step, groups of lanes, other widths, wide rows
+    (300, 384, "bf16", "bf16", "layer", "rms", 1, True, "some"),
+    (301, 1024, "f32", "bf16", "rms", "none", 1, True, "some"),
+    (200, 64, "f32", "f32", "layer", "layer", 1, True, "some"),
+    (211, 200, "bf16", "bf16", "rms", "layer", 1, True, "some"),
+    (90, 37, "bf16", "bf16", "layer", "layer", 1, True, "some"),
+    (60, 333, "f32", "bf16", "rms", "layer", 1, True, "some"),
+    (40, 5000, "bf16", "bf16", "layer", "layer", 1, True, "some"),
+    # gate rows of which all tokens are padding
+    (640, 128, "bf16", "bf16", "layer", "rms", 3, True, "some"),
+    (600, 256, "f32", "f32", "rms", "rms", 4, True, "some"),
+    (500, 384, "bf16", "bf16", "rms", "layer", 2, True, "some"),
+    (400, 50, "f32", "bf16", "layer", "layer", 3, True, "some")],
+    ids=lambda c: "-".join(map(str, c)))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_gates_of_padding_take_no_part(case, value):
+    """Gate rows of padding tokens alone may hold anything (made from their activations)."""
+    T, d, stream, branch = case[:4]
+    cfg, v, e = make(*case, seed=11, dev="cuda")
+    gr = cfg["gate_rows"]
+    used = torch.zeros(len(e["gate"]), dtype=torch.bool)
+    used[torch.arange(T)[e["mask"]] // gr] = True
+    assert not used.all()
+    v["gate"][~used.cuda()] = value
+    norm = layer_of(cfg, stream, branch)
+    r = norm.forward(v["x"], v["y"], mask=v["mask"], pre_bias=v["pre_bias"],
+                     **{k: v[k] for k in PARAMS})
+    assert torch.isfinite(r["out"]).all() and (r["u"] is None or torch.isfinite(r["u"]).all())
+    r = run_backward(cfg, v, e, stream, branch)
+    keep, g, size = backward64(cfg, e)
+    close(r["dy"][keep.cuda()], g["dy"], ROUND[branch] * g["dy"].abs() + 4e-5 * size["dy"], "dy")
+    assert not r["dx"][~keep.cuda()].any() and not r["dy"][~keep.cuda()].any()
+    for n in g:
+        assert torch.isfinite(r[n]).all(), n
+        if n not in ("dx", "dy"):
+            close(r[n], g[n], 1e-4 * size[n] + 1e-30, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", CASES + MANY, ids=lambda c: "-".join(map(str, c)))
+def test_nothing_but_numbers(case):
+    """No NaN or infinity in any result (a comparison with a tolerance lets NaN pass)."""
+    stream, branch = case[2:4]
+    cfg, v, e = make(*case, seed=21, dev="cuda")
+    r = layer_of(cfg, stream, branch).forward(v["x"], v["y"], mask=v["mask"], pre_bias=v["pre_bias"],
+                                              **{k: v[k] for k in PARAMS})
+    r.update(run_backward(cfg, v, e, stream, branch))
+    assert all(torch.isfinite(t).all() for t in r.values() if t is not None)
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
