@@ -186,9 +186,10 @@ def _status_word(device: torch.device) -> torch.Tensor:
 def mxfp4_status(device=None) -> int:
     """Waits for the device and returns ERR_TIMEOUT (-5) if a product's kernel gave up a
     wait since the last call (its output is incomplete), else 0."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None \
-        else torch.device(device)
-    torch.cuda.synchronize(device)
+    device = torch.device("cuda" if device is None else device)
+    torch.cuda.synchronize(device)  # (raises for other devices)
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
     word = _status_word(device)
     bad = int(word.item()) != 0
     word.zero_()

@@ -253,6 +253,54 @@ def test_group_counts_at_which_the_ring_gets_shorter(G):
     check(sizes, 160, 64, act="gelu", seed=G)
 
 
+class Word:
+    """Stands for the word on a device that products report to."""
+
+    def __init__(self, calls, value):
+        self.calls, self.value = calls, value
+
+    def item(self):
+        self.calls.append("read")
+        return self.value
+
+    def zero_(self):
+        self.calls.append("clear")
+        self.value = 0
+        return self
+
+
+@pytest.fixture
+def words(monkeypatch):
+    """Calls that touch the words, without a GPU: device 0 has a word that is set."""
+    from paper_2608_10392_gb300 import operators
+    calls = []
+
+    def made(*args, **kw):
+        calls.append("make")
+        return Word(calls, 0)
+
+    class Stream:
+        def synchronize(self):
+            calls.append("wait")
+
+    monkeypatch.setattr(operators, "_status_words", {torch.device("cuda", 0): Word(calls, 1)})
+    monkeypatch.setattr(torch, "zeros", made)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: calls.append("wait"))
+    return calls
+
+
+@pytest.mark.parametrize("device", ["cuda", "cuda:0", 0, None])
+def test_status_of_a_device_by_any_of_its_names(device, words):
+    """The word that a product reports to is found by every name of its device."""
+    from paper_2608_10392_gb300 import mxfp4_status
+    assert mxfp4_status(device) == -5
+    assert mxfp4_status(device) == 0
+    assert "make" not in words
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()
