@@ -179,7 +179,9 @@ def _status_word(device: torch.device) -> torch.Tensor:
     if t is None:
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("the first mxfp4_product on a device has to be outside a capture")
-        t = _status_words[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        t = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.current_stream(device).synchronize()  # products may be on another stream
+        _status_words[device] = t
     return t
 
 
@@ -193,6 +195,7 @@ def mxfp4_status(device=None) -> int:
     word = _status_word(device)
     bad = int(word.item()) != 0
     word.zero_()
+    torch.cuda.synchronize(device)  # a later product may be on another stream
     return -5 if bad else 0
 
 

@@ -301,6 +301,17 @@ def test_status_of_a_device_by_any_of_its_names(device, words):
     assert "make" not in words
 
 
+def test_status_word_is_cleared_before_a_later_product(words):
+    """Making and clearing the word have ended when the call returns: a product on another
+    stream does not have its report cleared."""
+    from paper_2608_10392_gb300 import mxfp4_status, operators
+    mxfp4_status()
+    assert words == ["wait", "read", "clear", "wait"]
+    del words[:]
+    operators._status_word(torch.device("cuda", 1))
+    assert words == ["make", "wait"]
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()
