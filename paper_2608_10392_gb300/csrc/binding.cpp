@@ -221,8 +221,9 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows po = rows_of(at, out, "out", T, d.width, ts), pu = rows_of(at, u, "u", T, d.width, tb);
     float* sp[4] = {nullptr, nullptr, nullptr, nullptr};
     const bool stats = a[11] == Py_True;
-    if (stats)
-      for (int i = 0; i < 4; ++i) {
+    const bool there[2] = {y.defined() && d.post_norm != 0, d.pre_norm != 0};
+    for (int i = 0; i < 4; ++i)  // of the norms that there are: nothing writes the others
+      if (stats && there[i / 2]) {
         st[i] = at.empty({T}, at::kFloat);
         sp[i] = st[i].data_ptr<float>();
       }
@@ -233,7 +234,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!r) throw Raised();
     try {
       put(r, "out", y.defined() ? out : x);
-      put(r, "u", u);
+      put(r, "u", d.pre_norm ? u : Tensor());
       static const char* names[4] = {"post_mean", "post_rstd", "pre_mean", "pre_rstd"};
       if (stats)
         for (int i = 0; i < 4; ++i) put(r, names[i], st[i]);

@@ -107,8 +107,8 @@ class BlockNorm:
                 stats: bool = False, stream=None) -> dict:
         """dict of out (x itself without y), u (None without pre norm) and, where
         `stats` asks for them, the statistics post_mean, post_rstd, pre_mean,
-        pre_rstd [T] that backward takes. Without y: the norm before a stack's
-        first block."""
+        pre_rstd [T] that backward takes (None for a norm that is not there; means of
+        an rms norm are 0). Without y: the norm before a stack's first block."""
         return _b().norm_forward(self._desc, x, y, post_weight, post_bias, gate, pre_weight,
                                  pre_bias, mask, out, u, stats, stream)
 

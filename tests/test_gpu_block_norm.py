@@ -487,6 +487,29 @@ def test_nothing_but_numbers(case):
     assert all(torch.isfinite(t).all() for t in r.values() if t is not None)
 
 
+@pytest.mark.gpu
+def test_statistics_and_results_of_absent_norms():
+    """None, not memory that nothing has written."""
+    cfg, v, e = make(30, 64, "f32", "f32", "rms", "layer", None, False, None, seed=2, dev="cuda")
+    x, y, w = v["x"], v["y"], v["pre_weight"]
+
+    def run(post, pre, y, **k):
+        return layer_of(dict(cfg, post=post, pre=pre, gate_rows=None), "f32", "f32").forward(
+            x, y, post_weight=w if post != "none" else None, pre_weight=w if pre != "none" else None,
+            stats=True, **k)
+
+    for post, pre, branch in (("none", "layer", y), ("rms", "none", y), ("none", "none", y),
+                              ("layer", "rms", y), ("none", "rms", None)):
+        r = run(post, pre, branch)
+        for name, kind in (("post", post), ("pre", pre)):
+            assert (r[name + "_rstd"] is None) == (kind == "none")
+            assert (r[name + "_mean"] is None) == (kind == "none")
+            if kind == "rms":
+                assert not r[name + "_mean"].any()
+    given = torch.full_like(x, 3.0)
+    assert run("rms", "none", y, u=given)["u"] is None and (given == 3).all()
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
