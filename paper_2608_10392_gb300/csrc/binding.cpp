@@ -145,6 +145,11 @@ long as_long(PyObject* o) {
   if (v == -1 && PyErr_Occurred()) throw Raised();
   return v;
 }
+bool as_bool(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised();
+  return v != 0;
+}
 double as_double(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Raised();
@@ -220,7 +225,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (d.pre_norm && !u.defined()) u = at.empty({T, d.width}, tb);
     const Rows po = rows_of(at, out, "out", T, d.width, ts), pu = rows_of(at, u, "u", T, d.width, tb);
     float* sp[4] = {nullptr, nullptr, nullptr, nullptr};
-    const bool stats = a[11] == Py_True;
+    const bool stats = as_bool(a[11]);
     const bool there[2] = {y.defined() && d.post_norm != 0, d.pre_norm != 0};
     for (int i = 0; i < 4; ++i)  // of the norms that there are: nothing writes the others
       if (stats && there[i / 2]) {
@@ -325,7 +330,7 @@ PyObject* balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (need) ws = at.empty({need}, at::kByte);
     const Tensor loss = at.empty({3}, at::kFloat), counts = at.empty({K}, at::kInt), prob = at.empty({K}, at::kFloat);
     Tensor d;
-    if (a[6] == Py_True) d = at.empty({T, K}, at::kFloat);
+    if (as_bool(a[6])) d = at.empty({T, K}, at::kFloat);
     check(unif_moe_balance_loss(
         (int)T, (int)K, pz.p, (unif_moe_dtype)type, pz.ld, static_cast<const int32_t*>(pq.p), (int)n_q,
         pq.ld, static_cast<const int32_t*>(k), mask, (float)as_double(a[4]), (float)as_double(a[5]),

@@ -510,6 +510,19 @@ def test_statistics_and_results_of_absent_norms():
     assert run("rms", "none", y, u=given)["u"] is None and (given == 3).all()
 
 
+@pytest.mark.gpu
+def test_any_true_value_asks_for_statistics_and_gradients():
+    from paper_2608_10392_gb300 import balance_loss
+    cfg, v, e = make(30, 64, "f32", "f32", "none", "rms", None, False, None, seed=2, dev="cuda")
+    norm = layer_of(cfg, "f32", "f32")
+    for yes, no in ((1, 0), ([1], []), ("yes", None)):
+        assert "pre_rstd" in norm.forward(v["x"], pre_weight=v["pre_weight"], stats=yes)
+        assert "pre_rstd" not in norm.forward(v["x"], pre_weight=v["pre_weight"], stats=no)
+        q = torch.zeros(30, 1, dtype=torch.int32, device="cuda")
+        assert balance_loss(v["x"], q, grad=yes)["dlogits"] is not None
+        assert balance_loss(v["x"], q, grad=no)["dlogits"] is None
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
