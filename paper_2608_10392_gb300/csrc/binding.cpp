@@ -145,6 +145,11 @@ long as_long(PyObject* o) {
   if (v == -1 && PyErr_Occurred()) throw Raised();
   return v;
 }
+int as_int(PyObject* o) {
+  const long v = as_long(o);
+  if (v != (int)v) value_error(std::to_string(v) + " does not fit in 32 bits");
+  return (int)v;
+}
 bool as_bool(PyObject* o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw Raised();
@@ -183,7 +188,7 @@ unif_moe_block_norm desc_of(PyObject* t, int64_t T) {
   if (T > 0x7fffffff) value_error("more than 2^31 - 1 tokens");
   d.tokens = (int)T;
   int* ints[6] = {&d.width, &d.stream_dtype, &d.branch_dtype, &d.post_norm, &d.pre_norm, &d.gate_rows};
-  for (int i = 0; i < 6; ++i) *ints[i] = (int)as_long(PyTuple_GET_ITEM(t, i));
+  for (int i = 0; i < 6; ++i) *ints[i] = as_int(PyTuple_GET_ITEM(t, i));
   d.res_scale = (float)as_double(PyTuple_GET_ITEM(t, 6));
   d.eps = (float)as_double(PyTuple_GET_ITEM(t, 7));
   return d;
@@ -465,7 +470,7 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check(unif_moe_mxfp4_product(
         x.codes, x.scales, x.rows, (int)cols, w.codes, w.scales, (int)N, (int)groups,
         static_cast<const int32_t*>(dense(at, offsets, "offsets", groups + 1, at::kInt)),
-        (int)as_long(a[7]), po.p, (unif_moe_dtype)type, po.ld,
+        as_int(a[7]), po.p, (unif_moe_dtype)type, po.ld,
         static_cast<int32_t*>(dense(at, tensor(a[10], "status"), "status", 1, at::kInt)),
         at.stream()));
     return THPVariable_Wrap(out);

@@ -523,6 +523,16 @@ def test_any_true_value_asks_for_statistics_and_gradients():
         assert balance_loss(v["x"], q, grad=no)["dlogits"] is None
 
 
+@pytest.mark.gpu
+def test_sizes_beyond_32_bits_are_refused():
+    from paper_2608_10392_gb300 import BlockNorm
+    x, w = torch.ones(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    for k in (dict(width=64 + (1 << 32)), dict(width=64, gate_rows=(1 << 32) + 2)):
+        norm = BlockNorm(stream_dtype="f32", branch_dtype="f32", **k)
+        with pytest.raises(ValueError, match="32"):
+            norm.forward(x, x, gate=torch.ones(2, 64, device="cuda"), pre_weight=w)
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
