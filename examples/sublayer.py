@@ -85,20 +85,23 @@ class Sublayer:
 
     def forward_fp4(self, x, experts):
         """The sublayer with 4-bit experts and activations, over the group table of the
-        layer's routing (which the bf16 forward of the same tokens left in the handle)."""
+        layer's routing. That table is in the handle after a bf16 forward of the same tokens
+        and holds those of its last pass, so tokens are taken a pass at a time."""
         up, down = experts
-        opened, _, _, _ = self.forward(x)
-        _, offsets, token, weight = self.layer.groups()
-        token, weight, offsets = token.long().cuda(), weight.cuda(), offsets.cuda()
-        rows = opened["u"][token.clamp(min=0)]  # padding rows have weight 0
-        h = mxfp4_product(mxfp4_quantize(rows), up, offsets, activation="gelu")
-        part = mxfp4_product(mxfp4_quantize(h), down, offsets, dtype="f32")
-        weight = torch.where(token < 0, 0.0, weight)
-        y = torch.zeros(x.shape[0], self.d, device="cuda")
-        y.index_add_(0, token.clamp(min=0), part * weight[:, None])
-        b = self.bf16
-        return y.bfloat16(), self.closing.forward(x, y.bfloat16(), gate=b["scale"],
-                                                  pre_weight=b["next_norm"])
+        T, P = x.shape[0], self.layer.pass_tokens()
+        y = torch.zeros(T, self.d, device="cuda")
+        for lo in range(0, T, P):
+            opened, _, _, _ = self.forward(x[lo:lo + P])
+            _, offsets, token, weight = self.layer.groups()
+            token, weight, offsets = token.long().cuda(), weight.cuda(), offsets.cuda()
+            rows = opened["u"][token.clamp(min=0)]  # padding rows have weight 0
+            h = mxfp4_product(mxfp4_quantize(rows), up, offsets, activation="gelu")
+            part = mxfp4_product(mxfp4_quantize(h), down, offsets, dtype="f32")
+            weight = torch.where(token < 0, 0.0, weight)
+            y[lo:lo + P].index_add_(0, token.clamp(min=0), part * weight[:, None])
+        y = y.bfloat16()
+        return y, self.closing.forward(x, y, gate=self.bf16["scale"],
+                                       pre_weight=self.bf16["next_norm"])
 
 
 def main(tokens=2048, steps=5, **sizes):
