@@ -28,28 +28,12 @@ constexpr int kThreads = 128;    // threads per CTA of the forms with several ro
 constexpr int kMaxWarps = 32;
 
 // ---- eight values of a row ----
-template <typename T>
-struct Raw;
-template <>
-struct Raw<float> {
-  float4 a, b;
-};
-template <>
-struct Raw<__nv_bfloat16> {
-  uint4 a;
-};
-
 // VEC: thread j of a group holds columns 8 j .. 8 j + 7 (one access of 16 bytes of bf16
 // or 32 of fp32: whole sectors); otherwise columns j, j + n, j + 2 n, ... of n threads.
 template <bool VEC>
 __device__ __forceinline__ int column(int j, int n, int i) {
   return VEC ? j * kE + i : i * n + j;
 }
-
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_float(float v, float* p) { *p = v; }
-__device__ __forceinline__ void from_float(float v, __nv_bfloat16* p) { *p = __float2bfloat16_rn(v); }
 
 __device__ __forceinline__ void unpack(const uint4& r, float (&v)[kE]) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
