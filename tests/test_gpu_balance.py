@@ -212,6 +212,33 @@ def test_more_selections_than_a_cta_counts_are_refused():
     assert b"selections" in L.unif_moe_last_error()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,K", [(40001, 3), (9001, 12), (3001, 50), (2100, 100), (700, 200), (333, 400)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_more_tokens_than_a_cluster_holds(T, K, dtype):
+    """Two kernels, in each of their forms; also without a gradient, where the losses are
+    the same."""
+    from paper_2608_10392_gb300 import balance_loss
+    z, q, k, mask = make(T, K, dtype, seed=T + K, n_q=min(K, 6))
+    z[mask == 0] = float("nan")
+    r = check(z, q, k, mask)
+    assert torch.isfinite(r["dlogits"]).all()
+    s = balance_loss(z, q, k, mask=mask, balance_weight=0.02, z_weight=0.003, grad=False)
+    assert s["dlogits"] is None and all(torch.equal(r[n], s[n]) for n in ("loss", "counts", "prob"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,K", [(1, 4), (300, 33), (4099, 32), (31, 512)])
+def test_losses_without_a_gradient(T, K):
+    from paper_2608_10392_gb300 import balance_loss
+    z, q, k, mask = make(T, K, torch.float32, seed=T, n_q=min(K, 6))
+    s = balance_loss(z, q, k, mask=mask, balance_weight=0.02, z_weight=0.003, grad=False)
+    loss, counts, P, _, _ = reference(z, q, k, mask, 0.02, 0.003)
+    assert torch.equal(s["counts"].cpu().long(), counts)
+    assert ((s["prob"].double().cpu() - P).abs() <= 2e-5 * P + 1e-30).all()
+    assert ((s["loss"].double().cpu() - loss).abs() <= 2e-5 * (loss.abs() + 1)).all()
+
+
 def test_refusals():
     from paper_2608_10392_gb300 import build
     build.build()

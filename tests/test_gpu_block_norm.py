@@ -533,6 +533,70 @@ def test_sizes_beyond_32_bits_are_refused():
             norm.forward(x, x, gate=torch.ones(2, 64, device="cuda"), pre_weight=w)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [
+    (700, 384, "bf16", "bf16", "rms", "rms", 64, True, "some"),
+    (400, 1000, "bf16", "bf16", "layer", "layer", 0, True, None),
+    (300, 96, "bf16", "bf16", "layer", "rms", 1, True, "some"),
+    (100, 333, "bf16", "bf16", "rms", "layer", None, False, None),
+    (2500, 768, "bf16", "bf16", "none", "layer", 0, True, "some"),
+    (500, 640, "f32", "bf16", "layer", "rms", 7, True, "some")],
+    ids=lambda c: "-".join(map(str, c)))
+def test_a_training_steps_chain(case):
+    """The forward's own out and statistics into the backward, against the gradient of the
+    whole in 64 bits, and the branch's statistics themselves. The statistics are those of
+    the sum before its rounding to the stream's type, so that o^ = (out - m) r is off by
+    r times a rounding of out (at most 2^-8 of it in bf16), which passes through the
+    formulas."""
+    T, d, stream, branch = case[:4]
+    cfg, v, e = make(*case, seed=13, dev="cuda")
+    keep = keep_of(cfg, e)
+    k, rows = keep.cuda(), torch.arange(T)[keep]
+    norm = layer_of(cfg, stream, branch)
+    params = {n: v[n] for n in PARAMS}
+    f = norm.forward(v["x"], v["y"], mask=v["mask"], pre_bias=v["pre_bias"], stats=True, **params)
+    y = e["y"][keep]
+    yn, ry = y, torch.ones(len(y), 1, dtype=torch.float64)
+    if cfg["post"] != "none":
+        yn, mean, rstd = norm64(y, cfg["post"])
+        ry = rstd[:, None]
+        close(f["post_mean"][k], mean, 2e-5 * (y.abs().mean(1) + 1), "post_mean")
+        close(f["post_rstd"][k], rstd,
+              2e-5 * rstd + 2e-5 * rstd ** 3 * (y.square().mean(1) + 1), "post_rstd")
+        assert not f["post_rstd"][~k].any() and not f["post_mean"][~k].any()
+    r = norm.backward(f["out"], v["y"], f, dout=v["dout"], du=v["du"], mask=v["mask"], **params)
+    out = forward64(cfg, e, rows, e["x"][keep], y, e)[0]
+    whole = torch.zeros(T, d, dtype=torch.float64)
+    whole[keep] = out
+    _, g, size = backward64(cfg, dict(e, x=whole))
+    n, _, rstd = norm64(out, cfg["pre"])
+    a, off = (e["du"][keep] * e["pre_weight"]).abs(), ROUND[stream] * out.abs() * rstd[:, None]
+    more = {"d_pre_weight": (e["du"][keep].abs() * off).sum(0), "d_pre_bias": 0.0}
+    D = rstd[:, None] * (off * (a * (n.abs() + off)).mean(1, keepdim=True)
+                         + n.abs() * (a * off).mean(1, keepdim=True))
+    more["dx"] = abs(cfg["scale"]) * D
+    if e["gate"] is not None:
+        z = yn
+        if cfg["post"] != "none":
+            z = z * e["post_weight"] + (0 if e["post_bias"] is None else e["post_bias"])
+        at = rows // cfg["gate_rows"] if cfg["gate_rows"] else torch.zeros_like(rows)
+        more["d_gate"] = torch.zeros_like(e["gate"]).index_add_(0, at, D * z.abs())
+    D = D * gates(cfg, e["gate"], rows).abs()
+    if cfg["post"] != "none":
+        more["d_post_weight"], more["d_post_bias"] = (D * yn.abs()).sum(0), D.sum(0)
+        D = D * e["post_weight"].abs()
+        D = ry * (D + D.mean(1, keepdim=True) + yn.abs() * (D * yn.abs()).mean(1, keepdim=True))
+    more["dy"] = D
+    close(r["dx"][k], g["dx"], ROUND[stream] * (g["dx"].abs() + more["dx"]) + 2e-5 * size["dx"]
+          + more["dx"], "dx")
+    close(r["dy"][k], g["dy"], ROUND[branch] * (g["dy"].abs() + more["dy"]) + 4e-5 * size["dy"]
+          + more["dy"], "dy")
+    for name in g:
+        assert torch.isfinite(r[name]).all(), name
+        if name not in ("dx", "dy"):
+            close(r[name], g[name], 1e-4 * size[name] + more[name] + 1e-30, name)
+
+
 def test_refusals():
     """Bad descriptions and arguments are refused before anything runs (no GPU needed)."""
     from paper_2608_10392_gb300 import build
