@@ -60,6 +60,22 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// Counts beyond 32 bits are added in two parts, the low 16 bits and the rest (counts
+// below 2^48): shared memory adds no 64-bit numbers but in a loop that compares and tries
+// again (256 tokens of 4 experts 5.0 us with those, 4.7 without).
+struct Total {
+  unsigned low, high;
+  __device__ __forceinline__ void clear() { low = high = 0u; }
+  __device__ __forceinline__ void add(long long c) {  // by any thread, in shared memory
+    atomicAdd(&low, (unsigned)c & 0xffffu);
+    atomicAdd(&high, (unsigned)(c >> 16));
+  }
+  __device__ __forceinline__ long long get() const { return ((long long)high << 16) + low; }
+};
+__device__ __forceinline__ long long warp_total(long long c) {
+  const unsigned low = __reduce_add_sync(0xffffffffu, (unsigned)c & 0xffffu);
+  return ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(c >> 16)) << 16) + low;
+}
 // A count as it is given to the caller.
 __device__ __forceinline__ int count32(long long c) { return (int)min(c, 0x7fffffffll); }
 
@@ -223,13 +239,13 @@ template <typename T, int L, int E, bool VEC, int TH, int U>
 __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
   constexpr int kWarps = TH / 32;
   extern __shared__ float f[];  // [K] f, then [K] mean probabilities (first CTA)
-  __shared__ unsigned long long all_c;  // selections of all tokens: beyond 32 bits
+  __shared__ Total all_c;  // selections of all tokens
   __shared__ int all_n;
   __shared__ float zsum;
   float* prob = f + a.K;
   const int lane32 = threadIdx.x & 31, warp = threadIdx.x / 32;
   const bool first = blockIdx.x == 0;
-  if (threadIdx.x == 0) all_c = 0;
+  if (threadIdx.x == 0) all_c.clear();
   grid_dep_wait();
   __syncthreads();
   // a warp per column adds the CTAs' sums (whole numbers, and in a fixed order)
@@ -240,14 +256,11 @@ __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
       m += a.part_c[(long long)c * a.ctas + i];
       if (first) q += a.part_p[(long long)c * a.ctas + i];
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      m += __shfl_xor_sync(0xffffffffu, m, o);
-      q += __shfl_xor_sync(0xffffffffu, q, o);
-    }
+    m = warp_total(m);
+    q = lanes_sum<32>(q);
     if (lane32 == 0) {
       f[c] = (float)m;
-      atomicAdd(&all_c, (unsigned long long)m);
+      all_c.add(m);
       if (first) {
         prob[c] = q;
         a.counts[c] = count32(m);
@@ -272,7 +285,7 @@ __global__ void __launch_bounds__(TH) gradient_kernel(const Args a) {
     }
   }
   __syncthreads();
-  const float inv_c = 1.f / (float)max(all_c, 1ull), inv_n = 1.f / (float)max(all_n, 1);
+  const float inv_c = 1.f / (float)max(all_c.get(), 1ll), inv_n = 1.f / (float)max(all_n, 1);
   for (int c = threadIdx.x; c < a.K; c += TH) f[c] *= inv_c;
   __syncthreads();
   if (first && warp == 0) {
@@ -355,7 +368,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   extern __shared__ float sh[];  // [kWarps][K] shares; then [K] sums, [K] counts, [K] f
   __shared__ float z_sh[kWarps], zsum;
   __shared__ int n_sh[kWarps], all_n, mine[2];
-  __shared__ unsigned long long all_c;
+  __shared__ Total all_c;
   float* sum_p = sh + kWarps * a.K;
   int* cnt = reinterpret_cast<int*>(sum_p + a.K);
   float* f = sum_p + 2 * a.K;
@@ -364,7 +377,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
   const uint32_t ranks = gridDim.x;  // one cluster
   const int held = (int)((a.T + ranks * kTok - 1) / (ranks * kTok));  // tokens of a group, <= U
   for (int i = threadIdx.x; i < a.K; i += TH) cnt[i] = 0;
-  if (threadIdx.x == 0) all_c = 0;
+  if (threadIdx.x == 0) all_c.clear();
   float z[U][E], lse[U];
   int m[U], q0[U];
   bool in[U];
@@ -465,9 +478,8 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
       sh[c] = s;  // (the shares have been added)
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (lane32 == 0) atomicAdd(&all_c, (unsigned long long)total);
+  total = warp_total(total);
+  if (lane32 == 0) all_c.add(total);
   if (threadIdx.x == TH - 1) {
     int k = 0;
     float s = 0.f;
@@ -479,7 +491,7 @@ __global__ void __launch_bounds__(TH) cluster_kernel(const Args a) {
     all_n = k;
   }
   cluster_sync();  // nothing is read from another CTA any more; all of this CTA's is written
-  const float inv_c = 1.f / (float)max(all_c, 1ull), inv_n = 1.f / (float)max(all_n, 1);
+  const float inv_c = 1.f / (float)max(all_c.get(), 1ll), inv_n = 1.f / (float)max(all_n, 1);
   if (first && warp == 0) {
     float b = 0.f;
     for (int c = lane32; c < a.K; c += 32) {
