@@ -11,9 +11,9 @@
 // rounded once, to the type it is stored in.
 //
 // Measured (us; at the copy rate of 6.8 TB/s): forward of 12,608 x 384, fp32 stream,
-// 12.8 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 38 (24); backward of 12,608 x 768
-// bf16 with a gate per image 34 (17), of 65,536 x 1,024 padded, fp32 stream, 187 (178
-// for all rows). Widths that are no multiple of eight move value by value: backward
+// 12.9 (8.6), of 20,000 x 1,024 bf16 with norms on both sides 38 (24); backward of 12,608 x 768
+// bf16 with a gate per image 34 (17), of 65,536 x 1,024 padded, fp32 stream, 189 (126
+// for the rows that are read, 178 for all). Widths that are no multiple of eight move value by value: backward
 // of 20,000 x 1,001 bf16 104 (35), forward 67 (24).
 #include <cuda_bf16.h>
 #include <math.h>
@@ -1212,9 +1212,11 @@ template <typename TX, typename TB, bool VEC>
 cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, int sms, cudaStream_t s) {
   const int threads = cta_threads(a.d);
   // A bf16 stream of 257 to 1,024 columns: forward_stream_kernel once every SM has 16
-  // rows. us, a row to a group of threads against it: 9,728 x 384 12.3 and 10.0, x 1,024 22.0
-  // and 18.5, x 2,048 39.7 and 41.6; 77,824 x 80 16.9 and 16.1, 19,456 x 80 5.1 and 5.5. An fp32
-  // stream has more bytes for the same work and more CTAs hide them better: 9,728 x 1,024
+  // rows. us, a row to a group of threads against it, both norms: 64 rows an SM, 9,728 x 384
+  // 12.4 and 10.1, x 1,024 22.1 and 18.5; 16 rows an SM, 2,432 x 384 4.8 and 4.7, x 640 5.8 and
+  // 5.2, x 1,024 7.4 and 6.6; 8 rows an SM, 1,216 x 384 4.0 and 4.1, x 640 4.3 and 4.5, x 1,024
+  // 4.5 and 4.6. Other widths: 9,728 x 2,048 39.7 and 41.6; 77,824 x 80 16.9 and 16.1, 19,456 x
+  // 80 5.1 and 5.5. An fp32 stream has more bytes for the same work and more CTAs hide them better: 9,728 x 1,024
   // over bf16 23.6 and 27.4.
   if constexpr (VEC && sizeof(TX) == 2)
     if (!group_lanes(a.d) && threads <= kThreads && a.T >= 16ll * sms)

@@ -2,9 +2,11 @@
 // (unif_moe_mxfp4_product): out[r][n] = act(sum_c A[r][c] W[g(r)][n][c]).
 //
 // What bounds it: with few rows the weights' bytes (24 rows in 33 groups of 4,096 x 1,024:
-// 10.4 us, 5.2 TB/s); with many steps shared memory, which takes a step's operands in and
-// gives them to the MMAs (131,072 rows of 1,024 x 4,096 in 33 groups, fp32 output: 228 us, 4.8
-// PFLOP/s; MMAs alone 106, bytes 131); with few steps the stores and GELU of a tile beside
+// 11.3 us, 4.8 TB/s); with many steps shared memory for the larger part: it takes 28 KB of a
+// step's operands in and gives 28 KB to the MMAs, 448 clocks at 128 bytes a clock, of about 710
+// that a step takes (131,072 rows of 1,024 x 4,096 in 33 groups, fp32 output, 245 us back to back
+// at 1,720 MHz under the power cap: 37 items of 16 steps a pair; 230 us, 4.8 PFLOP/s, with
+// pauses; the bytes need 131); no counter shows the rest; with few steps the stores and GELU of a tile beside
 // the next tile's loads (100,003 rows of 192 x 768 in 272 groups: 23.3 us, 4.2 TB/s).
 //
 // tcgen05 block-scaled MMAs (kind mxf4: products of 4-bit elements and 8-bit
@@ -710,9 +712,12 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
   const bool fits = fpp::smem_bytes(false, fpp::kMaxStages, groups) <= fpp::kSmemMax;
   // Rows as M where tiles of 128 channels would waste a quarter of their work, groups
   // have rows enough, and the output takes 32-byte stores (us, channels as M and rows
-  // as M: 100,003 rows in 272 groups of 192 x 768 26.1 and 18.9, 30,000 rows 14.0 and 11.0; without
-  // waste, 60,000 rows of 384 x 1,536 24.6 and 26.6; fp32 output, 60,000 of 1,536 x 384
-  // 66.6 and 86.9; rows off 32 bytes, 50,000 of 100 x 500 8.7 and 51.9).
+  // as M, bf16 output with GELU and without: 100,003 rows in 272 groups of 192 x 768 29.8 and 23.2,
+  // 22.4 and 22.2; 17,408 rows, 64 a group, 14.5 and 12.7, 11.6 and 11.4; 8,000 rows 11.3 and
+  // 12.0, 10.3 and 9.7; 20,000 rows in 33 groups of 160 x 512 9.9 and 8.9, 7.3 and 7.1;
+  // without waste, 60,000 rows in 33 groups of 384 x 1,536 27.6 and 28.6, 24.1 and 27.7, 100,000 of
+  // 768 x 768 64.0 and 56.7, 44.2 and 56.0. fp32 output, when it had that form: 60,000 of 1,536 x
+  // 384 66.6 and 86.9; rows off 32 bytes: 50,000 of 100 x 500 8.7 and 51.9).
   const bool wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && ld * (dtype == UNIF_MOE_F32 ? 4 : 2) % 32 == 0;
   const int parts = (n + fpp::kTN - 1) / fpp::kTN, part = ((n + parts - 1) / parts + 15) / 16 * 16;
   const int padded = (n + 127) / 128 * 128;
@@ -720,10 +725,11 @@ int unif_moe_mxfp4_product(const uint8_t* a_codes, const uint8_t* a_scales, int6
                       rows >= 64ll * groups;
   // CTA pairs, which read half of the rows' codes each, where steps are many enough for
   // operand traffic to bound the tile and a pair's 256 channels are no more
-  // than two CTAs' 128 (us, single CTAs and pairs: 131,072 rows of 1,024 x 4,096 fp32 261 and 223,
-  // 20,000 rows 49.3 and 43.2, 2,000 rows 15.7 and 14.1, 500 rows 12.4 and 13.0; 100,000
-  // rows of 1,024 x 1,024 77.0 and 69.7, 1,000 rows of 4,096 x 1,024 in 8 groups 9.0 and
-  // 10.0; 100,000 rows of 768 x 768 54.6 and 54.5; of 384 x 1,536 24.6 and 29.1).
+  // than two CTAs' 128 (us, single CTAs and pairs, bf16 output and fp32, 33 groups: 131,072
+  // rows of 1,024 x 4,096 243 and 204, 270 and 237; 20,000 rows 50.2 and 45.9, 52.9 and 48.8;
+  // 2,000 rows 18.1 and 18.6, 19.1 and 19.2; 500 rows 15.9 and 17.1, 16.2 and 17.1; 100,000 rows
+  // of 1,024 x 1,024 63.0 and 60.7, 82.9 and 80.4; of 768 x 768 44.2 and 43.8, 59.1 and 59.3;
+  // 1,000 rows of 4,096 x 1,024 in 8 groups 9.1 and 10.0, 10.1 and 10.8).
   const bool pair = fits && !rows_m && (n + 255) / 256 * 256 == padded && rows >= 32ll * groups &&
                     (cols >= 2048 || (cols >= 1024 && rows >= 1024ll * groups));
   const int ctas = pair ? 2 : 1;

@@ -9,7 +9,7 @@
 // threads of a block find its largest size by two shuffles, so that a warp reads
 // and writes consecutive bytes whatever the width; kUnroll pieces per thread are
 // loaded before the first is used. 135,168 x 1,024 fp32 to 4 bits and back take 184 us, 6.8
-// TB/s; 12,608 x 384 bf16 7.0 us (3.6 at that rate).
+// TB/s; 12,608 x 384 bf16 7.5 us (3.6 at that rate).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

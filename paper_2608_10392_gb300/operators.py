@@ -1,8 +1,13 @@
 """Operators round the layer: the handle-free entry points of include/unif_moe.h on
 torch tensors. A compiled module (csrc/binding.cpp) checks the tensors, allocates
 the outputs and calls; there is no fallback, and without it every call raises.
-Work goes to `stream` (the tensors' device's current one by default); padding
-masks are uint8 or bool.
+Work goes to `stream` (the tensors' device's current one by default): with another
+one the caller orders the streams and keeps the inputs until their use has ended;
+outputs belong to it. Padding masks are uint8 or bool.
+
+Nothing here records for autograd. Results are constants to it, whatever their
+inputs require: gradients are what backward() and balance_loss()["dlogits"] return,
+and balance_loss()["loss"] added to another loss adds a number, no gradient.
 
     norm = BlockNorm(1024, stream_dtype="f32", branch_dtype="bf16", post_norm="rms", pre_norm="rms")
     r = norm.forward(x, y, post_weight=g1, pre_weight=g2, stats=True)   # r["out"], r["u"], ...
