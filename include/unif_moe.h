@@ -585,6 +585,86 @@ UNIF_MOE_API int unif_moe_mxfp4_product(const uint8_t* a_codes_dev, const uint8_
                                         unif_moe_dtype dtype, int64_t ld, int32_t* status_dev,
                                         void* stream);
 
+/* ---- Dense products beside the layer ----
+ * The products of a Transformer block that are no experts (attention's projections, a
+ * dense FFN), with what follows them in the product's epilogue. As the operators above
+ * they need no handle, allocate nothing and keep no state between calls. */
+
+/* in_dtype of rows and weights in 8-bit floating point (E4M3: sign, four exponent bits,
+ * three mantissa bits, values up to 448) with fp32 scales */
+#define UNIF_MOE_E4M3 2
+#define UNIF_MOE_LINEAR_MAX_COLS (1 << 24)
+
+typedef struct {
+  int64_t rows;    /* T >= 0 */
+  int cols, n;     /* columns of a row, output channels; up to UNIF_MOE_LINEAR_MAX_COLS */
+  int in_dtype;    /* of rows and weights: UNIF_MOE_BF16 or UNIF_MOE_E4M3 */
+  int out_dtype;   /* of result and residual: UNIF_MOE_F32 or UNIF_MOE_BF16 */
+  int bias_dtype;  /* UNIF_MOE_F32 or UNIF_MOE_BF16 */
+  int activation;  /* UNIF_MOE_ACTIVATION_* */
+} unif_moe_linear;
+
+/* Bytes of device workspace of unif_moe_linear_forward for these operands (rows that do
+ * not start at multiples of 16 bytes are laid out there first); -1 on a bad
+ * description. */
+UNIF_MOE_API int64_t unif_moe_linear_workspace(const unif_moe_linear* p, const void* x_dev,
+                                               int64_t ld_x, const void* w_dev, int64_t ld_w);
+
+/* Product with bias, activation and residual:
+ *   z[t][j]   = sx[t] sw[j] sum_c x[t][c] w[j][c] + bias[j]
+ *   out[t][j] = residual[t][j] + act(z[t][j])
+ *   x_dev [T][cols], w_dev [n][cols] (the torch nn.Linear layout); rows ld apart, any alignment
+ *   x_scale_dev [T], w_scale_dev [n] fp32: with E4M3; NULL is 1, and both are NULL for BF16
+ *   bias_dev [n] or NULL; residual_dev [T][n] or NULL, may be out_dev with its stride
+ *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose rows give 0 in out and z,
+ *     whatever x and the residual hold there
+ *   out_dev [T][n]; z_dev [T][n] bf16 or NULL: z for unif_moe_linear_backward
+ *   status_dev [1] int32: a kernel that gives up a wait sets it non-zero (zero it
+ *     before the first call); the output is then incomplete
+ * Sums are fp32, taken in an order that depends on the sizes alone; z and out are rounded once each. GELU as in
+ * unif_moe_mxfp4_product, for fp32 results with the accuracy of normcdff.
+ * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (more than 2^31 tiles),
+ * ERR_CAPACITY (workspace), ERR_CUDA. */
+UNIF_MOE_API int unif_moe_linear_forward(const unif_moe_linear* p, const void* x_dev, int64_t ld_x,
+                                         const float* x_scale_dev, const void* w_dev, int64_t ld_w,
+                                         const float* w_scale_dev, const void* bias_dev,
+                                         const void* residual_dev, int64_t ld_residual,
+                                         const uint8_t* token_mask_dev, void* out_dev,
+                                         int64_t ld_out, void* z_dev, int64_t ld_z,
+                                         void* workspace_dev, int64_t workspace_bytes,
+                                         int32_t* status_dev, void* stream);
+
+/* What unif_moe_linear_backward is to compute, for its workspace: the operands as they
+ * will be given (bf16), and which results. */
+typedef struct {
+  const void *x_dev, *w_dev, *dout_dev, *z_dev;
+  int64_t ld_x, ld_w, ld_dout, ld_z;
+  int dout_dtype;            /* UNIF_MOE_F32 or UNIF_MOE_BF16 */
+  int grad_dtype;            /* of dw: UNIF_MOE_F32 or UNIF_MOE_BF16 */
+  const uint8_t* token_mask_dev; /* or NULL */
+  void* dx_dev;              /* [T][cols] bf16 or NULL */
+  int64_t ld_dx;
+  void* dw_dev;              /* [n][cols] grad_dtype or NULL */
+  int64_t ld_dw;
+  float* dbias_dev;          /* [n] or NULL */
+} unif_moe_linear_grad;
+
+UNIF_MOE_API int64_t unif_moe_linear_backward_workspace(const unif_moe_linear* p,
+                                                        const unif_moe_linear_grad* g);
+
+/* Gradients of unif_moe_linear_forward for bf16 rows and weights, from that of the
+ * result (dout_dev [T][n]; the residual's gradient is dout itself):
+ *   dz = dout act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum_t dz
+ * z_dev [T][n] is the forward's; not read (may be NULL) without an activation. Padding rows are not read
+ * (whatever they hold), take no part in the sums and give 0 in dx. dz enters the
+ * products rounded to bf16, their operand type (exact for a bf16 dout without
+ * activation); dbias sums it unrounded. Sums are fp32, in an order that depends on the sizes alone.
+ * in_dtype must be BF16; out_dtype and bias_dtype of p are not used. Enqueued on
+ * `stream`, no sync. Errors as the forward's. */
+UNIF_MOE_API int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g,
+                                          void* workspace_dev, int64_t workspace_bytes,
+                                          int32_t* status_dev, void* stream);
+
 /* Frees the handle and its device memory (synchronises the device first).
  * NULL is ignored. */
 UNIF_MOE_API void unif_moe_destroy(unif_moe_t h);

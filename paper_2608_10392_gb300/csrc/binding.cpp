@@ -477,6 +477,135 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Scales of rows or channels in 8 bits: fp32, one each.
+const float* scales_of(const Place& at, const Tensor& t, const char* name, int64_t count) {
+  if (!t.defined()) value_error(std::string(name) + ": need a tensor");
+  return static_cast<const float*>(dense(at, t, name, count, at::kFloat));
+}
+
+// x, x scales (or None), w, w scales (or None), bias, activation, residual, mask, dtype code, keep,
+// out, status, stream
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const Tensor x = tensor(a[0], "x"), w = tensor(a[2], "w");
+    const Place at(x, "x", a[12]);
+    const bool eight = a[1] != Py_None;
+    const at::ScalarType ti = eight ? at::kFloat8_e4m3fn : at::kBFloat16;
+    if (x.dim() != 2) value_error("x: need two dimensions");
+    if (!w.defined() || w.dim() != 2) value_error("w: need two dimensions");
+    const int64_t T = x.size(0), cols = x.size(1), N = w.size(0);
+    if (cols > UNIF_MOE_LINEAR_MAX_COLS || N > UNIF_MOE_LINEAR_MAX_COLS || cols < 1 || N < 1)
+      value_error("bad sizes: x " + shown(x) + ", w " + shown(w));
+    const Rows px = rows_of(at, x, "x", T, cols, ti), pw = rows_of(at, w, "w", N, cols, ti);
+    const float *sx = nullptr, *sw = nullptr;
+    if (eight) {
+      sx = scales_of(at, tensor(a[1], "x.scales"), "x.scales", T);
+      sw = scales_of(at, tensor(a[3], "w.scales"), "w.scales", N);
+    }
+    const Tensor bias = tensor(a[4], "bias"), res = tensor(a[6], "residual");
+    const long type = as_long(a[8]);
+    const at::ScalarType to = type_of(type, "dtype");
+    unif_moe_linear d{};
+    d.rows = T;
+    d.cols = (int)cols;
+    d.n = (int)N;
+    d.in_dtype = eight ? UNIF_MOE_E4M3 : UNIF_MOE_BF16;
+    d.out_dtype = (int)type;
+    d.bias_dtype = UNIF_MOE_BF16;
+    d.activation = as_int(a[5]);
+    if (bias.defined()) {
+      d.bias_dtype = code(bias.scalar_type());
+      if (d.bias_dtype < 0) value_error("bias: need fp32 or bf16, got " + shown(bias));
+    }
+    const void* pb = bias.defined() ? dense(at, bias, "bias", N, bias.scalar_type()) : nullptr;
+    const Rows pr = rows_of(at, res, "residual", T, N, to);
+    const uint8_t* mask = mask_of(at, tensor(a[7], "mask"), T);
+    const bool keep = as_bool(a[9]);
+    Tensor out = tensor(a[10], "out"), z, ws;
+    if (!out.defined()) out = at.empty({T, N}, to);
+    if (keep) z = at.empty({T, N}, at::kBFloat16);
+    const Rows po = rows_of(at, out, "out", T, N, to);
+    const int64_t need = unif_moe_linear_workspace(&d, px.p, px.ld, pw.p, pw.ld);
+    if (need < 0) check(UNIF_MOE_ERR_ARG);
+    if (need) ws = at.empty({need}, at::kByte);
+    check(unif_moe_linear_forward(
+        &d, px.p, px.ld, sx, pw.p, pw.ld, sw, pb, pr.p, pr.ld, mask, po.p, po.ld,
+        keep ? z.data_ptr() : nullptr, N, need ? ws.data_ptr() : nullptr, need,
+        static_cast<int32_t*>(dense(at, tensor(a[11], "status"), "status", 1, at::kInt)), at.stream()));
+    if (!keep) return THPVariable_Wrap(out);
+    return Py_BuildValue("(NN)", THPVariable_Wrap(out), THPVariable_Wrap(z));
+  });
+}
+
+// x, w, dout, z, activation, mask, want dx, want dw, want dbias, grad dtype code, status, stream
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&]() -> PyObject* {
+    const Tensor x = tensor(a[0], "x"), w = tensor(a[1], "w"), dout = tensor(a[2], "dout"), z = tensor(a[3], "z");
+    const Place at(x, "x", a[11]);
+    if (x.dim() != 2) value_error("x: need two dimensions");
+    if (!w.defined() || w.dim() != 2) value_error("w: need two dimensions");
+    if (!dout.defined()) value_error("dout: need a tensor");
+    const int64_t T = x.size(0), cols = x.size(1), N = w.size(0);
+    if (cols > UNIF_MOE_LINEAR_MAX_COLS || N > UNIF_MOE_LINEAR_MAX_COLS || cols < 1 || N < 1)
+      value_error("bad sizes: x " + shown(x) + ", w " + shown(w));
+    const int type = code(dout.scalar_type());
+    if (type < 0) value_error("dout: need fp32 or bf16, got " + shown(dout));
+    const Rows px = rows_of(at, x, "x", T, cols, at::kBFloat16), pw = rows_of(at, w, "w", N, cols, at::kBFloat16),
+               pd = rows_of(at, dout, "dout", T, N, dout.scalar_type()),
+               pz = rows_of(at, z, "z", T, N, at::kBFloat16);
+    unif_moe_linear d{};
+    d.rows = T;
+    d.cols = (int)cols;
+    d.n = (int)N;
+    d.in_dtype = d.out_dtype = d.bias_dtype = UNIF_MOE_BF16;
+    d.activation = as_int(a[4]);
+    if (d.activation != UNIF_MOE_ACTIVATION_NONE && !z.defined())
+      value_error("z: the gradient of an activation needs the forward's z (keep)");
+    unif_moe_linear_grad g{};
+    g.x_dev = px.p; g.ld_x = px.ld;
+    g.w_dev = pw.p; g.ld_w = pw.ld;
+    g.dout_dev = pd.p; g.ld_dout = pd.ld;
+    g.z_dev = pz.p; g.ld_z = pz.ld;
+    g.dout_dtype = type;
+    g.token_mask_dev = mask_of(at, tensor(a[5], "mask"), T);
+    const long gt = as_long(a[9]);
+    const at::ScalarType tg = type_of(gt, "grad_dtype");
+    g.grad_dtype = (int)gt;
+    Tensor dx, dw, db, ws;
+    if (as_bool(a[6])) {
+      dx = at.empty({T, cols}, at::kBFloat16);
+      g.dx_dev = dx.data_ptr();
+      g.ld_dx = cols;
+    }
+    if (as_bool(a[7])) {
+      dw = at.empty({N, cols}, tg);
+      g.dw_dev = dw.data_ptr();
+      g.ld_dw = cols;
+    }
+    if (as_bool(a[8])) {
+      db = at.empty({N}, at::kFloat);
+      g.dbias_dev = db.data_ptr<float>();
+    }
+    const int64_t need = unif_moe_linear_backward_workspace(&d, &g);
+    if (need < 0) check(UNIF_MOE_ERR_ARG);
+    if (need) ws = at.empty({need}, at::kByte);
+    check(unif_moe_linear_backward(
+        &d, &g, need ? ws.data_ptr() : nullptr, need,
+        static_cast<int32_t*>(dense(at, tensor(a[10], "status"), "status", 1, at::kInt)), at.stream()));
+    PyObject* r = PyDict_New();
+    if (!r) throw Raised();
+    try {
+      put(r, "dx", dx);
+      put(r, "dw", dw);
+      put(r, "dbias", db);
+    } catch (...) {
+      Py_DECREF(r);
+      throw;
+    }
+    return r;
+  });
+}
+
 // The classes that failed calls and failed allocations raise; before any other call.
 PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject* {
@@ -489,6 +618,7 @@ PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define UNIF_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {UNIF_FAST(norm_forward), UNIF_FAST(norm_backward), UNIF_FAST(balance),
                          UNIF_FAST(quantize), UNIF_FAST(dequantize), UNIF_FAST(product),
+                         UNIF_FAST(linear), UNIF_FAST(linear_backward),
                          UNIF_FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

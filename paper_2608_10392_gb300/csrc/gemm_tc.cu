@@ -685,6 +685,22 @@ bool encode_bf16_map(CUtensorMap* map, const void* base, uint64_t cols, uint64_t
   return r == CUDA_SUCCESS;
 }
 
+// 2-D tensor map of rows of bf16 (size 2) or 8-bit elements (size 1), `pitch` bytes
+// apart, with a 128-byte swizzle.
+bool encode_rows_map(CUtensorMap* map, const void* base, int size, uint64_t cols, uint64_t rows,
+                     uint64_t pitch, uint32_t box_cols, uint32_t box_rows) {
+  tc::EncodeTiledFn fn = tc::encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {pitch};
+  cuuint32_t box[2] = {box_cols, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace tc {
 
 // N split into n_sub sub-tiles of bn columns: bn <= 256 and bn % 64 == 0, so

@@ -1,0 +1,1313 @@
+// Dense products with bias, activation and residual in the epilogue, and their gradients
+// (unif_moe_linear_forward / _backward):
+//   z = sx sw (x w^T) + b,  out = r + act(z);   dz = dout act'(z),  dx = dz w,  dw = dz^T x
+//
+// Three kernels multiply.
+// - gemm_kernel: tiles of 128 rows, or of 256 on a CTA pair, by up to 256 columns on tcgen05,
+//   accumulators in TMEM (two, so that one is stored while the next is computed), operands by
+//   TMA through a ring of stages. All three products of a layer are this kernel: an operand
+//   whose reduction index runs along memory is K-major, one whose reduction index is
+//   the row (w in dx; dz and x in dw) MN-major, and neither is transposed in memory.
+// - rows_kernel: few rows, bound by the weights' bytes: a CTA takes 16 output channels, its
+//   warps share the columns, and both operands go from memory to mma.sync fragments without
+//   shared memory (a thread's 16 bytes stand for other columns than the fragment's, the same
+//   ones for both operands, which a sum does not notice).
+// - grad_kernel / finish_kernel: dz and the column sums of dbias; sums over the parts of a
+//   split reduction, in a fixed order.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "gelu_log.cuh"
+#include "tc_common.cuh"
+
+namespace unif {
+namespace lin {
+
+using namespace tc;
+
+enum Kind {
+  kForward = 0,   // bf16, both operands K-major
+  kForward8 = 1,  // E4M3, both K-major
+  kInput = 2,     // dx: dz K-major, w MN-major
+  kWeight = 3     // dw: both MN-major
+};
+
+constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 320;
+constexpr uint32_t kTmemCols = 512, kAcc = 256;
+constexpr int kMaxStages = 8;
+constexpr int kBars = 2 * kMaxStages + 5;
+constexpr uint32_t kSmemMax = 232448;
+constexpr uint32_t kStaging = kEpiWarps * 32 * 33 * 4;  // rows that no 32-byte stores fit
+// Steps of 64 rows that one accumulation of kWeight runs over. The tensor cores
+// truncate the accumulator at every MMA, so the error grows with their number: longer sums
+// are added in fp32 registers.
+constexpr int kSumSteps = 16;
+
+struct Params {
+  int M, N;                        // rows and columns of the result
+  int steps, splits;               // steps of 128 operand bytes; parts of the reduction
+  int tile_n, m_tiles, n_tiles;    // columns of a tile (a multiple of 16)
+  int stages;
+  uint32_t stage_bytes;
+  bool gelu, wide;                 // wide: all row accesses in whole 16- or 32-byte pieces
+  void* out;
+  long long ld_out;
+  const float *sm, *sn;            // scales of rows and columns, or NULL
+  const void* bias;
+  bool bias_f32;
+  const void* residual;
+  long long ld_res;
+  const uint8_t* mask;
+  __nv_bfloat16* z;
+  long long ld_z;
+  float* part;                     // splits > 1: [splits][M][N]
+  int* status;
+  long long wait_limit;
+};
+
+__device__ __forceinline__ void wait_settle(uint32_t bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > limit) return;
+}
+
+template <int KIND, bool PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  if constexpr (KIND != kForward8) {
+    if (PAIR) umma_bf16_pair(d, a, b, idesc, acc);
+    else umma_bf16(d, a, b, idesc, acc);
+  } else if (PAIR) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+  }
+}
+
+// Instruction descriptor: fp32 accumulator (bits 4-5), operand types (bits 7-9 and 10-12: bf16
+// 1, E4M3 0), MN-major A and B (bits 15, 16), N >> 3 and M >> 4.
+template <int KIND, bool PAIR>
+__device__ __forceinline__ uint32_t idesc_of(int n) {
+  return (1u << 4) | (KIND == kForward8 ? 0u : (1u << 7) | (1u << 10)) |
+         (KIND == kWeight ? 1u << 15 : 0u) | (KIND >= kInput ? 1u << 16 : 0u) |
+         ((uint32_t)(n >> 3) << 17) | ((PAIR ? 256u >> 4 : 128u >> 4) << 24);
+}
+
+// Descriptor of an MN-major operand: 128-byte rows of 64 elements of one reduction index, 8-row
+// groups 1,024 bytes apart, blocks of 64 elements one after the other (64 rows of 128 bytes).
+__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) |
+         ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// ---- the epilogue's rows ----
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// Sixteen consecutive values (32-byte aligned bf16 or fp32).
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&v)[16]) {
+  uint32_t r[8];
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                 "=r"(r[7])
+               : "l"(p)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[2 * i] = __uint_as_float(r[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load16(const float* p, float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[8 * i]), "=f"(v[8 * i + 1]), "=f"(v[8 * i + 2]), "=f"(v[8 * i + 3]),
+                   "=f"(v[8 * i + 4]), "=f"(v[8 * i + 5]), "=f"(v[8 * i + 6]), "=f"(v[8 * i + 7])
+                 : "l"(p + 8 * i)
+                 : "memory");
+}
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
+  uint32_t h[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    h[i] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(h[0]), "r"(h[1]),
+               "r"(h[2]), "r"(h[3]), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7])
+               : "memory");
+}
+__device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 8 * i),
+                 "f"(v[8 * i]), "f"(v[8 * i + 1]), "f"(v[8 * i + 2]), "f"(v[8 * i + 3]), "f"(v[8 * i + 4]),
+                 "f"(v[8 * i + 5]), "f"(v[8 * i + 6]), "f"(v[8 * i + 7])
+                 : "memory");
+}
+
+// What becomes of two results: bf16 ones take the packed GELU (2^-12 of the value at most,
+// before a rounding of 2^-9), fp32 ones the library's.
+template <typename TO>
+__device__ __forceinline__ void act2(float& a, float& b) {
+  if constexpr (sizeof(TO) == 4) {
+    a *= normcdff(a);
+    b *= normcdff(b);
+  } else {
+    gelu::gelu2(a, b);
+  }
+}
+
+// Sixteen columns of this thread's row, from column `ch` (a multiple of 16) on, all there.
+template <typename TO>
+__device__ __forceinline__ void finish16(const Params& p, float (&v)[16], long long row, int ch, float scale,
+                                         bool on) {
+  TO* o = static_cast<TO*>(p.out) + row * p.ld_out + ch;
+  float t[16];
+  if (p.sn) {
+    load16(p.sn + ch, t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= scale * t[i];
+  } else if (p.sm) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= scale;
+  }
+  if (p.bias) {
+    if (p.bias_f32) load16(static_cast<const float*>(p.bias) + ch, t);
+    else load16(static_cast<const __nv_bfloat16*>(p.bias) + ch, t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += t[i];
+  }
+  if (p.z) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] = on ? v[i] : 0.f;
+    store16(p.z + row * p.ld_z + ch, t);
+  }
+  if (p.gelu)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) act2<TO>(v[i], v[i + 1]);
+  if (p.residual && on) {
+    load16(static_cast<const TO*>(p.residual) + row * p.ld_res + ch, t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += t[i];
+  }
+  if (!on)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+  store16(o, v);
+}
+
+// One element.
+template <typename TO>
+__device__ __forceinline__ void finish1(const Params& p, float v, long long row, int ch, bool on) {
+  if (p.sm) v *= p.sm[row];
+  if (p.sn) v *= p.sn[ch];
+  if (p.bias)
+    v += p.bias_f32 ? static_cast<const float*>(p.bias)[ch]
+                    : __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[ch]);
+  if (!on) v = 0.f;
+  if (p.z) p.z[row * p.ld_z + ch] = __float2bfloat16_rn(v);
+  if (p.gelu && on) {
+    float u = v;
+    act2<TO>(v, u);
+  }
+  if (p.residual && on) v += to_f32(static_cast<const TO*>(p.residual)[row * p.ld_res + ch]);
+  put(static_cast<TO*>(p.out) + row * p.ld_out + ch, v);
+}
+
+// PAIR: the CTAs of a cluster of two share a tile of 256 rows (tcgen05 cta_group::2), 128 of
+// them and half of the columns' operand in each one's shared memory. The first CTA's
+// barriers take both CTAs' bytes, its MMA lane issues for both.
+template <int KIND, typename TO, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+    gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                const Params p) {
+  constexpr int kCtas = PAIR ? 2 : 1, kTileM = 128 * kCtas;
+  constexpr bool kSum = KIND == kWeight;  // long reductions: sums of accumulations in registers
+  const uint32_t rank = PAIR ? cluster_rank() : 0u;
+  const bool leader = rank == 0;
+  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t s0 = smem_u32(smem);
+  const int n_st = p.stages;
+  auto stage = [&](int s) { return s0 + (uint32_t)s * p.stage_bytes; };
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)n_st * p.stage_bytes);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kMaxStages + s); };
+  auto accf_bar = [&](int a) { return bar0 + 8u * (2 * kMaxStages + a); };
+  auto acce_bar = [&](int a) { return bar0 + 8u * (2 * kMaxStages + 2 + a); };
+  const uint32_t mma_done = bar0 + 8u * (2 * kMaxStages + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* staging = reinterpret_cast<float*>(bars + kBars + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(accf_bar(a), 1);
+      mbar_init(acce_bar(a), kCtas * kEpiWarps);
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    if (PAIR) {
+      tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+      tmem_relinquish();
+    }
+  }
+  grid_dep_wait();
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync_all();  // both CTAs' barriers are set before either signals the other
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto arrive_leader = [&](uint32_t bar) {
+    if (!PAIR || leader) mbar_arrive(bar);
+    else mbar_arrive_cluster(mapa_shared(bar, 0));
+  };
+  auto commit = [&](uint32_t bar) {
+    if (PAIR) umma_commit_pair(bar, 3);
+    else umma_commit(bar);
+  };
+
+  // Items: (part of the reduction, row tile, column tile), the columns of a row tile one after
+  // another so that its rows are read from L2 but once from memory.
+  struct Item {
+    int m0, n0, n;      // this CTA's first row, the tile's first column and columns
+    int from, to;       // steps
+    int part;
+    __device__ __forceinline__ int sums() const {
+      return kSum ? (to - from + kSumSteps - 1) / kSumSteps : 1;
+    }
+    // the first step of its j-th accumulation
+    __device__ __forceinline__ int step(int j) const {
+      return kSum ? from + (int)((long long)(to - from) * j / sums()) : j ? to : from;
+    }
+  };
+  const int tiles = p.m_tiles * p.n_tiles, n_items = tiles * p.splits;
+  auto item_of = [&](int i) {
+    Item it;
+    it.part = kSum ? i / tiles : 0;
+    const int t = kSum ? i - it.part * tiles : i;
+    const int m = t / p.n_tiles;
+    it.m0 = m * kTileM + 128 * (int)rank;
+    it.n0 = (t - m * p.n_tiles) * p.tile_n;
+    it.n = min(p.tile_n, p.N - it.n0);
+    it.from = kSum ? (int)((long long)p.steps * it.part / p.splits) : 0;
+    it.to = kSum ? (int)((long long)p.steps * (it.part + 1) / p.splits) : p.steps;
+    return it;
+  };
+
+  if (warp < kEpiWarps) {
+    // ---------------- accumulators to the result ----------------------------
+    const int q = warp & 3, half = warp >> 2;
+    float* stg = staging + warp * (32 * 33);
+    int acc = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int i = unit; i < n_items && ok; i += units) {
+      const Item it = item_of(i);
+      const long long row = (long long)it.m0 + q * 32 + lane;
+      const bool there = row < p.M;
+      // (a quarter past the last row has nothing to store)
+      const int chunks = it.m0 + q * 32 < p.M ? (it.n + 31) / 32 : 0;
+      bool on = there;
+      float scale = 1.f;
+      if (there && p.mask) on = p.mask[row] != 0;
+      if (there && p.sm) scale = p.sm[row];
+      // 32 columns from column c * 32 of the tile on
+      auto finish = [&](float (&v)[32], int c) {
+        const int ch = it.n0 + c * 32, count = it.n - c * 32;
+        if (kSum && p.splits > 1) {
+          float* o = p.part + ((long long)it.part * p.M + row) * p.N + ch;
+          if (p.wide) {
+            if (there)
+#pragma unroll
+              for (int g = 0; g < 2; ++g)
+                if (16 * g < count) store16(o + 16 * g, *reinterpret_cast<float(*)[16]>(&v[16 * g]));
+            return;
+          }
+        } else if (p.wide) {
+          if (there)
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+              if (16 * g < count)
+                finish16<TO>(p, *reinterpret_cast<float(*)[16]>(&v[16 * g]), row, ch + 16 * g, scale, on);
+          return;
+        }
+        // a lane per column instead: rows of any width and alignment in runs of 32
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) stg[lane * 33 + j] = v[j];
+        __syncwarp();
+        const uint32_t live = __ballot_sync(0xffffffffu, on);
+        const int rows = (int)min(32ll, p.M - (row - lane));
+        if (lane < count)
+          for (int r = 0; r < rows; ++r) {
+            const float x = stg[r * 33 + lane];
+            if (kSum && p.splits > 1)
+              p.part[((long long)it.part * p.M + row - lane + r) * p.N + ch + lane] = x;
+            else
+              finish1<TO>(p, x, row - lane + r, ch + lane, live >> r & 1u);
+          }
+      };
+      if constexpr (kSum) {
+        float sum[4][32];
+        for (int j = 0; j < it.sums(); ++j) {
+          ok = wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16) + half * 32;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (2 * c + half < chunks) {
+#pragma unroll
+              for (int g = 0; g < 2; ++g) {
+                float v[16];
+                tmem_ld16(from + c * 64 + g * 16, v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  float& s = sum[c][16 * g + e];
+                  s = j ? s + v[e] : v[e];
+                }
+              }
+            }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_leader(acce_bar(acc));
+          if (++acc == 2) { acc = 0; ph ^= 1u; }
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (2 * c + half < chunks) finish(sum[c], 2 * c + half);
+      } else {
+        ok = wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16);
+        float v[32];
+        for (int c = half; c < chunks; c += 2) {
+          tmem_ld32(from + c * 32, v);
+          if (c + 2 >= chunks) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_leader(acce_bar(acc));
+          }
+          finish(v, c);
+        }
+        if (half >= chunks) {
+          __syncwarp();
+          if (lane == 0) arrive_leader(acce_bar(acc));
+        }
+        if (++acc == 2) { acc = 0; ph ^= 1u; }
+      }
+    }
+  } else if (warp == kTmaWarp) {
+    // ---------------- operands (one lane runs the role from end to end) -----
+    if (elect_one()) {
+      bool ok = true;
+      int s = 0;
+      uint32_t ph = 0;
+      long long issued = 0;
+      auto load = [&](uint32_t dst, const CUtensorMap* from, uint32_t bar, int c0, int c1) {
+        if (PAIR) tma_load_2d_pair(dst, from, mapa_shared(bar, 0), c0, c1);
+        else tma_load_2d(dst, from, bar, c0, c1);
+      };
+      constexpr int kCols = KIND == kForward8 ? 128 : 64;  // reduction elements of a step
+      for (int i = unit; i < n_items && ok; i += units) {
+        const Item it = item_of(i);
+        // this CTA's share of the columns: whole pieces of 16 of the tile, halved
+        const int n = (((it.n + 15) & ~15)) / kCtas, n0 = it.n0 + (int)rank * n;
+        const int blocks = (n + 63) / 64;  // of an MN-major operand
+        const uint32_t bytes = 16384u + (KIND >= kInput ? blocks * 8192u : (uint32_t)(p.tile_n / kCtas) * 128u);
+        for (int k = it.from; k < it.to; ++k) {
+          ok = wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
+          const uint32_t bar = full_bar(s), a = stage(s), b = a + 16384u;
+          if (leader) mbar_expect_tx(bar, kCtas * bytes);
+          if (KIND == kWeight) {
+            load(a, &tmA, bar, it.m0, k * kCols);
+            load(a + 8192u, &tmA, bar, it.m0 + 64, k * kCols);
+          } else {
+            load(a, &tmA, bar, k * kCols, it.m0);
+          }
+          if (KIND >= kInput)
+            for (int j = 0; j < blocks; ++j) load(b + j * 8192u, &tmB, bar, n0 + 64 * j, k * kCols);
+          else
+            load(b, &tmB, bar, k * kCols, n0);
+          ++issued;
+          if (++s == n_st) { s = 0; ph ^= 1u; }
+        }
+      }
+      // loads still in flight land before the CTA (pair) exits
+      for (long long j = issued > n_st ? issued - n_st : 0; leader && j < issued; ++j)
+        wait_settle(full_bar((int)(j % n_st)), (uint32_t)((j / n_st) & 1), p.wait_limit / 16);
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    // ---------------- MMAs (the first CTA) ----------------------------------
+    if (leader && elect_one()) {
+      int s = 0, acc = 0;
+      uint32_t ph = 0, acc_ph = 0;
+      bool ok = true, any = false;
+      for (int i = unit; i < n_items && ok; i += units) {
+        const Item it = item_of(i);
+        const uint32_t idesc = idesc_of<KIND, PAIR>((it.n + 15) & ~15);
+        for (int j = 0; j < it.sums() && ok; ++j) {
+          ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tmem + acc * kAcc;
+          const int first = it.step(j), last = it.step(j + 1);
+          for (int k = first; k < last; ++k) {
+            ok = wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t sa = stage(s), sb = sa + 16384u;
+            // 32 bytes of the reduction along memory, or 16 rows, at a time
+            const uint64_t a = KIND == kWeight ? mn_desc(sa) : sw128_desc(sa);
+            const uint64_t b = KIND >= kInput ? mn_desc(sb) : sw128_desc(sb);
+            constexpr int kStepA = KIND == kWeight ? 128 : 2, kStepB = KIND >= kInput ? 128 : 2;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              mma<KIND, PAIR>(d, a + kStepA * e, b + kStepB * e, idesc, (k > first || e > 0) ? 1u : 0u);
+            commit(empty_bar(s));
+            any = true;
+            if (++s == n_st) { s = 0; ph ^= 1u; }
+          }
+          if (ok) commit(accf_bar(acc));
+          if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+        }
+      }
+      // every MMA issued has completed before TMEM is released
+      if (any) {
+        if (PAIR) umma_commit_pair(mma_done, 1);
+        else umma_commit(mma_done);
+        wait_settle(mma_done, 0u, p.wait_limit);
+      }
+    }
+    __syncwarp();
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (PAIR) cluster_sync_all();
+  if (warp == kMmaWarp) {
+    if (PAIR) tmem_dealloc_pair(tmem, kTmemCols);
+    else tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ---- few rows ----
+
+struct RowsParams {
+  Params e;             // M, N, epilogue
+  const uint8_t *x, *w; // rows
+  long long ld_x, ld_w; // bytes between rows
+  int bytes;            // of a row
+};
+constexpr int kRowsMax = 32;       // rows of x
+constexpr int kRowsWarps = 16;     // most warps of a CTA
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+      " {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16832(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+      " {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Sixteen bytes of a row, those past its end 0 (`left` bytes are left of it). VEC: rows
+// start at multiples of 16 bytes. SIZE: bytes of an element.
+template <bool VEC, int SIZE>
+__device__ __forceinline__ uint4 piece(const uint8_t* p, int left) {
+  if (VEC && left >= 16) return __ldg(reinterpret_cast<const uint4*>(p));
+  uint32_t r[4] = {0u, 0u, 0u, 0u};
+  if (left > 0) {
+#pragma unroll
+    for (int i = 0; i < 16 / SIZE; ++i)
+      if (i * SIZE < left) {
+        const uint32_t v = SIZE == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + 2 * i) : (uint32_t)p[i];
+        r[i * SIZE / 4] |= v << (8 * (i * SIZE % 4));
+      }
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// NT: pieces of eight rows of x. A warp takes 128-byte blocks of the rows in turn with the
+// CTA's other warps, two pieces of 16 bytes a thread from each of 16 weight rows.
+template <int SIZE, int NT, bool VEC, typename TO>
+__global__ void __launch_bounds__(32 * kRowsWarps) rows_kernel(const RowsParams p) {
+  __shared__ float red[kRowsWarps * 16 * 8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int g = lane >> 2, at = (lane & 3) * 16;
+  const int ch0 = blockIdx.x * 16;
+  grid_dep_wait();
+  const bool two = ch0 + g + 8 < p.e.N, one = ch0 + g < p.e.N;
+  const uint8_t* w0 = p.w + (one ? ch0 + g : 0) * p.ld_w;
+  const uint8_t* w1 = p.w + (two ? ch0 + g + 8 : 0) * p.ld_w;
+  float c[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[t][i] = 0.f;
+  const int blocks = (p.bytes + 127) / 128;
+#pragma unroll 2
+  for (int b = warp; b < blocks; b += warps) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int from = b * 128 + h * 64 + at, left = p.bytes - from;
+      const uint4 a = piece<VEC, SIZE>(w0 + from, one ? left : 0);
+      const uint4 d = piece<VEC, SIZE>(w1 + from, two ? left : 0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int row = t * 8 + g;
+        const uint4 x = piece<VEC, SIZE>(p.x + (row < p.e.M ? row : 0) * p.ld_x + from, row < p.e.M ? left : 0);
+        if (SIZE == 2) {
+          mma_16816(c[t], a.x, d.x, a.y, d.y, x.x, x.y);
+          mma_16816(c[t], a.z, d.z, a.w, d.w, x.z, x.w);
+        } else {
+          mma_16832(c[t], a.x, d.x, a.y, d.y, x.x, x.y);
+          mma_16832(c[t], a.z, d.z, a.w, d.w, x.z, x.w);
+        }
+      }
+    }
+  }
+  // [warp][row of x][channel]; c: channels g, g and g + 8, g + 8, rows 2 (lane % 4), + 1
+  float* mine = red + warp * (16 * 8 * NT);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine[(t * 8 + (lane & 3) * 2 + (i & 1)) * 16 + g + (i >> 1) * 8] = c[t][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * 8 * NT; i += blockDim.x) {
+    const int row = i >> 4, ch = ch0 + (i & 15);
+    if (row >= p.e.M || ch >= p.e.N) continue;
+    float v = 0.f;
+    for (int k = 0; k < warps; ++k) v += red[k * (16 * 8 * NT) + i];
+    finish1<TO>(p.e, v, row, ch, !p.e.mask || p.e.mask[row]);
+  }
+}
+
+// ---- rows laid out for TMA, dz and the bias's gradient ----
+
+// Rows to a pitch of whole 16 bytes; padding rows to 0. A warp to 256 elements of a row.
+template <typename T>
+__global__ void __launch_bounds__(256)
+    layout_kernel(const T* x, long long ld, T* to, long long pitch, long long rows, int cols,
+                  const uint8_t* mask) {
+  grid_dep_wait();
+  const int lane = threadIdx.x & 31;
+  const int pieces = (cols + 255) / 256;
+  const long long total = rows * pieces, step = (long long)gridDim.x * 8;
+  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += step) {
+    const long long row = i / pieces;
+    const int c0 = (int)(i - row * pieces) * 256 + lane;
+    const bool on = !mask || mask[row];
+    T v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = on && c0 + 32 * k < cols ? x[row * ld + c0 + 32 * k] : (T)0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c0 + 32 * k < cols) to[row * pitch + c0 + 32 * k] = v[k];
+  }
+}
+
+struct GradParams {
+  long long rows;
+  int n, per;                // per: rows of a CTA
+  const void* dout;
+  long long ld_dout;
+  const __nv_bfloat16* z;    // or NULL: no activation
+  long long ld_z;
+  const uint8_t* mask;
+  __nv_bfloat16* dz;         // or NULL: dout itself is dz
+  long long ld_dz;
+  float* sums;               // [row blocks][n] or NULL
+};
+constexpr int kGradWarps = 8, kGradRows = 4;  // rows in flight of a warp
+
+// dz = dout act'(z), and the column sums of the CTA's rows: 256 columns by `per` rows, a warp to
+// every eighth row, eight columns a lane (VEC: consecutive ones).
+template <typename TD, bool VEC>
+__global__ void __launch_bounds__(32 * kGradWarps) grad_kernel(const GradParams p) {
+  __shared__ float red[kGradWarps][256];
+  grid_dep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c0 = blockIdx.x * 256;
+  auto column = [&](int k) { return c0 + (VEC ? lane * 8 + k : lane + 32 * k); };
+  const bool on_cols = !VEC || column(0) < p.n;
+  const long long first = (long long)blockIdx.y * p.per, last = min(p.rows, first + p.per);
+  float sum[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+  const TD* dout = static_cast<const TD*>(p.dout);
+  for (long long r0 = first + warp; r0 < last; r0 += kGradWarps * kGradRows) {
+    float d[kGradRows][8], z[kGradRows][8];
+    bool on[kGradRows];
+#pragma unroll
+    for (int u = 0; u < kGradRows; ++u) {
+      const long long r = r0 + u * kGradWarps;
+      on[u] = r < last && on_cols && (!p.mask || p.mask[r]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[u][k] = z[u][k] = 0.f;
+      if (!on[u]) continue;
+      if constexpr (VEC) {
+        if constexpr (sizeof(TD) == 4) {
+          const float4* q = reinterpret_cast<const float4*>(dout + r * p.ld_dout + column(0));
+          const float4 a = __ldcs(q), b = __ldcs(q + 1);
+          d[u][0] = a.x; d[u][1] = a.y; d[u][2] = a.z; d[u][3] = a.w;
+          d[u][4] = b.x; d[u][5] = b.y; d[u][6] = b.z; d[u][7] = b.w;
+        } else {
+          const uint4 a = *reinterpret_cast<const uint4*>(dout + r * p.ld_dout + column(0));
+          const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            d[u][2 * k] = __uint_as_float(w[k] << 16);
+            d[u][2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+          }
+        }
+        if (p.z) {
+          const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p.z + r * p.ld_z + column(0)));
+          const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            z[u][2 * k] = __uint_as_float(w[k] << 16);
+            z[u][2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (column(k) < p.n) {
+            d[u][k] = to_f32(dout[r * p.ld_dout + column(k)]);
+            if (p.z) z[u][k] = __bfloat162float(p.z[r * p.ld_z + column(k)]);
+          }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kGradRows; ++u) {
+      const long long r = r0 + u * kGradWarps;
+      if (r >= last || !on_cols) continue;
+      if (p.z && on[u])
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          float a, b;
+          gelu::gelu_grad2(z[u][k], z[u][k + 1], a, b);
+          d[u][k] *= a;
+          d[u][k + 1] *= b;
+        }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[k] += d[u][k];
+      if (!p.dz) continue;
+      __nv_bfloat16* o = p.dz + r * p.ld_dz;
+      if constexpr (VEC) {
+        uint32_t h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(d[u][2 * k], d[u][2 * k + 1]);
+          h[k] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(o + column(0)) = make_uint4(h[0], h[1], h[2], h[3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (column(k) < p.n) o[column(k)] = __float2bfloat16_rn(d[u][k]);
+      }
+    }
+  }
+  if (!p.sums) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) red[warp][column(k) - c0] = sum[k];
+  __syncthreads();
+  const int c = c0 + (int)threadIdx.x;
+  if (c < p.n) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGradWarps; ++k) v += red[k][threadIdx.x];
+    p.sums[(long long)blockIdx.y * p.n + c] = v;
+  }
+}
+
+struct FinishParams {
+  const float* part;  // [splits][M][N]
+  int splits;
+  long long M;
+  int N;
+  void* dw;
+  long long ld_dw;
+  const float* sums;  // [blocks][n]
+  int blocks, n;
+  float* dbias;
+  int dw_ctas;        // the first CTAs add dw's parts
+};
+
+// Adds the parts of dw (four columns a thread) and, 32 columns a CTA, the blocks of dbias.
+template <typename TG>
+__global__ void __launch_bounds__(256) finish_kernel(const FinishParams p) {
+  __shared__ float red[8][32];
+  grid_dep_wait();
+  if ((int)blockIdx.x < p.dw_ctas) {
+    const long long total = p.M * p.N, pieces = (total + 3) / 4;
+    const bool vec = p.N % 4 == 0;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces;
+         i += (long long)p.dw_ctas * 256) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < p.splits; ++s) {
+        const float* q = p.part + s * total + i * 4;
+        if (vec) {
+          const float4 t = __ldcs(reinterpret_cast<const float4*>(q));
+          v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (i * 4 + k < total) v[k] += q[k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const long long e = i * 4 + k;
+        if (e >= total) break;
+        const long long row = e / p.N;
+        put(static_cast<TG*>(p.dw) + row * p.ld_dw + (e - row * p.N), v[k]);
+      }
+    }
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = ((int)blockIdx.x - p.dw_ctas) * 32 + lane;
+  float v = 0.f;
+  if (c < p.n)
+    for (int b = warp; b < p.blocks; b += 8) v += p.sums[(long long)b * p.n + c];
+  red[warp][lane] = v;
+  __syncthreads();
+  if (warp == 0 && c < p.n) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += red[k][lane];
+    p.dbias[c] = v;
+  }
+}
+
+// ---- host side ----
+
+constexpr int kMostRows = 0x7fffffff - 1024;
+
+uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+// Rows that TMA can read as they are.
+bool tma_rows(const void* p, long long ld, int size) { return bits(p) % 16 == 0 && ld * size % 16 == 0; }
+
+long long pitch_of(int cols, int size) { return ((long long)cols * size + 15) / 16 * 16 / size; }
+
+int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Map of rows [rows][cols] of elements of `size` bytes (bf16, or 8-bit), `ld` apart: boxes of
+// 128 bytes by box_rows, 128-byte swizzle.
+bool map_rows(CUtensorMap* map, const void* base, int size, uint64_t cols, uint64_t rows, uint64_t ld,
+              uint32_t box_rows) {
+  return encode_rows_map(map, base, size, cols, rows, ld * size, 128u / size, box_rows);
+}
+
+// Tiles of the result: columns of a tile and how many tiles there are.
+struct Tiles {
+  bool pair;
+  int tile_n, m_tiles, n_tiles;
+};
+int even_part(int n, int parts) { return ((n + parts - 1) / parts + 15) / 16 * 16; }
+
+Tiles pick_tiles(long long M, int N, int sms) {
+  Tiles t;
+  const long long m256 = (M + 255) / 256, m128 = (M + 127) / 128;
+  const int parts = (N + 255) / 256;
+  t.pair = m256 * parts >= sms / 2;
+  int n_parts = parts;
+  if (!t.pair)  // narrower tiles until every SM has one
+    while (m128 * n_parts < sms && even_part(N, n_parts + 1) >= 32 && m128 * (n_parts + 1) <= sms) ++n_parts;
+  t.tile_n = even_part(N, n_parts);
+  t.m_tiles = (int)(t.pair ? m256 : m128);
+  t.n_tiles = (N + t.tile_n - 1) / t.tile_n;
+  return t;
+}
+
+// Parts of a reduction of `steps` steps over `tiles` tiles on `units` CTAs or pairs: as
+// few as give the least of the steps that a unit runs one after another, counting what
+// writing and adding the parts costs (a tile's partial sums as two steps).
+int pick_splits(int tiles, int steps, int units) {
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 64 && s <= (steps + 3) / 4; ++s) {
+    const long long waves = ((long long)tiles * s + units - 1) / units;
+    const double cost = (double)waves * ((steps + s - 1) / s + 4.0) + (s > 1 ? 4.0 * tiles * s / units + 8.0 : 0.0);
+    if (cost < least * 0.97) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
+template <int KIND, typename TO>
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, int sms,
+                        cudaStream_t s) {
+  const int ctas = t.pair ? 2 : 1;
+  const int n = t.tile_n / ctas;
+  p.tile_n = t.tile_n;
+  p.m_tiles = t.m_tiles;
+  p.n_tiles = t.n_tiles;
+  p.stage_bytes = 16384u + (KIND >= kInput ? (uint32_t)((n + 63) / 64) * 8192u : ((uint32_t)n * 128u + 1023u) / 1024u * 1024u);
+  const uint32_t beside = 1024u + (kBars + 1) * 8u + (p.wide ? 0u : kStaging);
+  p.stages = (int)std::min<uint32_t>(kMaxStages, (kSmemMax - beside) / p.stage_bytes);
+  const uint32_t smem = beside + (uint32_t)p.stages * p.stage_bytes;
+  p.wait_limit = gemm_wait_limit();
+  void (*kernel)(const CUtensorMap, const CUtensorMap, const Params) =
+      t.pair ? gemm_kernel<KIND, TO, true> : gemm_kernel<KIND, TO, false>;
+  const cudaError_t e = allow_smem_once(kernel, smem);
+  if (e != cudaSuccess) return e;
+  const long long items = (long long)t.m_tiles * t.n_tiles * p.splits;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(ctas * std::min<long long>(items, sms / ctas)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = t.pair ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, b, p);
+}
+
+template <int SIZE, int NT, typename TO>
+cudaError_t launch_rows_as(const RowsParams& p, bool vec, cudaStream_t s) {
+  const int blocks = (p.bytes + 127) / 128;
+  const int warps = std::min(kRowsWarps, std::max(4, (blocks + 1) / 2));
+  void (*kernel)(const RowsParams) = vec ? rows_kernel<SIZE, NT, true, TO> : rows_kernel<SIZE, NT, false, TO>;
+  return launch_dependent(kernel, dim3((p.e.N + 15) / 16), dim3(32 * warps), 0, s, p);
+}
+template <int SIZE, typename TO>
+cudaError_t launch_rows(const RowsParams& p, bool vec, cudaStream_t s) {
+  if (p.e.M <= 8) return launch_rows_as<SIZE, 1, TO>(p, vec, s);
+  if (p.e.M <= 16) return launch_rows_as<SIZE, 2, TO>(p, vec, s);
+  return launch_rows_as<SIZE, 4, TO>(p, vec, s);
+}
+
+cudaError_t launch_layout(const void* x, long long ld, void* to, long long pitch, long long rows, int cols,
+                          int size, const uint8_t* mask, int sms, cudaStream_t s) {
+  const long long warps = rows * ((cols + 255) / 256);
+  const int grid = (int)std::min<long long>((warps + 7) / 8, 8ll * sms);
+  if (size == 2)
+    return launch_dependent(layout_kernel<uint16_t>, dim3(grid), dim3(256), 0, s,
+                            static_cast<const uint16_t*>(x), ld, static_cast<uint16_t*>(to), pitch, rows, cols, mask);
+  return launch_dependent(layout_kernel<uint8_t>, dim3(grid), dim3(256), 0, s, static_cast<const uint8_t*>(x),
+                          ld, static_cast<uint8_t*>(to), pitch, rows, cols, mask);
+}
+
+int check(const unif_moe_linear* p) {
+  if (!p) { set_error("the description is NULL"); return UNIF_MOE_ERR_ARG; }
+  if (p->rows < 0 || p->rows > kMostRows || p->cols < 1 || p->n < 1 || p->cols > UNIF_MOE_LINEAR_MAX_COLS ||
+      p->n > UNIF_MOE_LINEAR_MAX_COLS) {
+    set_error("bad sizes: rows=%lld cols=%d n=%d", (long long)p->rows, p->cols, p->n);
+    return UNIF_MOE_ERR_ARG;
+  }
+  auto type = [](int t) { return t == UNIF_MOE_F32 || t == UNIF_MOE_BF16; };
+  if ((p->in_dtype != UNIF_MOE_BF16 && p->in_dtype != UNIF_MOE_E4M3) || !type(p->out_dtype) ||
+      !type(p->bias_dtype) || p->activation < UNIF_MOE_ACTIVATION_NONE ||
+      p->activation > UNIF_MOE_ACTIVATION_GELU) {
+    set_error("bad dtypes (in %d, out %d, bias %d) or activation %d", p->in_dtype, p->out_dtype, p->bias_dtype,
+              p->activation);
+    return UNIF_MOE_ERR_ARG;
+  }
+  return UNIF_MOE_OK;
+}
+
+int in_size(const unif_moe_linear* p) { return p->in_dtype == UNIF_MOE_BF16 ? 2 : 1; }
+
+int64_t forward_bytes(const unif_moe_linear* p, const void* x, long long ld_x, const void* w, long long ld_w) {
+  const int size = in_size(p);
+  if (p->rows <= kRowsMax) return 0;
+  int64_t need = 0;
+  if (!tma_rows(x, ld_x, size)) need += round_up(p->rows * pitch_of(p->cols, size) * size);
+  if (!tma_rows(w, ld_w, size)) need += round_up((int64_t)p->n * pitch_of(p->cols, size) * size);
+  return need;
+}
+
+// The workspace of a backward: where each part begins.
+struct Plan {
+  int sms, splits, blocks, per;
+  bool copy_x, copy_w, make_dz, sums;
+  long long px, pw, pz;  // pitches
+  int64_t x, w, dz, part, bias, total;
+  Tiles in, weight;
+};
+Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int sms) {
+  Plan r{};
+  r.sms = sms;
+  const long long T = p->rows;
+  r.copy_x = g->dw_dev && (g->token_mask_dev || !tma_rows(g->x_dev, g->ld_x, 2));
+  r.copy_w = g->dx_dev && !tma_rows(g->w_dev, g->ld_w, 2);
+  r.make_dz = (g->dx_dev || g->dw_dev) &&
+              (p->activation != UNIF_MOE_ACTIVATION_NONE || g->dout_dtype != UNIF_MOE_BF16 || g->token_mask_dev ||
+               !tma_rows(g->dout_dev, g->ld_dout, 2));
+  r.sums = g->dbias_dev != nullptr;
+  r.px = r.copy_x ? pitch_of(p->cols, 2) : g->ld_x;
+  r.pw = r.copy_w ? pitch_of(p->cols, 2) : g->ld_w;
+  r.pz = r.make_dz ? pitch_of(p->n, 2) : g->ld_dout;
+  // row blocks of grad_kernel: four CTAs an SM
+  const long long cols = (p->n + 255) / 256, most = std::max<long long>(1, 4ll * sms / cols);
+  r.per = (int)std::max<long long>(kGradWarps * kGradRows, (T + most - 1) / most);
+  r.blocks = (int)((T + r.per - 1) / r.per);
+  r.in = pick_tiles(T, p->cols, sms);
+  r.weight = pick_tiles(p->n, p->cols, sms);
+  const long long steps = (T + 63) / 64;
+  // a tile of its own pair as soon as parts of the rows can fill the SMs
+  const long long m256 = (p->n + 255) / 256;
+  const int parts = (p->cols + 255) / 256;
+  if (p->n > 128 && m256 * parts * std::max<long long>(1, steps / 8) >= sms / 2) {
+    r.weight.pair = true;
+    r.weight.tile_n = even_part(p->cols, parts);
+    r.weight.m_tiles = (int)m256;
+    r.weight.n_tiles = (p->cols + r.weight.tile_n - 1) / r.weight.tile_n;
+  }
+  r.splits = pick_splits(r.weight.m_tiles * r.weight.n_tiles, (int)steps, sms / (r.weight.pair ? 2 : 1));
+  int64_t at = 0;
+  auto take = [&](bool want, int64_t bytes) {
+    const int64_t here = at;
+    if (want) at += round_up(bytes);
+    return here;
+  };
+  r.x = take(r.copy_x, T * r.px * 2);
+  r.w = take(r.copy_w, (int64_t)p->n * r.pw * 2);
+  r.dz = take(r.make_dz, T * r.pz * 2);
+  r.part = take(g->dw_dev && r.splits > 1, (int64_t)r.splits * p->n * p->cols * 4);
+  r.bias = take(r.sums, (int64_t)r.blocks * p->n * 4);
+  r.total = at;
+  return r;
+}
+
+int check_grad(const unif_moe_linear* p, const unif_moe_linear_grad* g) {
+  const int rc = check(p);
+  if (rc != UNIF_MOE_OK) return rc;
+  if (!g) { set_error("the gradients' description is NULL"); return UNIF_MOE_ERR_ARG; }
+  auto type = [](int t) { return t == UNIF_MOE_F32 || t == UNIF_MOE_BF16; };
+  if (p->in_dtype != UNIF_MOE_BF16 || !type(g->dout_dtype) || !type(g->grad_dtype)) {
+    set_error("gradients are those of bf16 rows; bad dtypes (in %d, dout %d, gradient %d)", p->in_dtype,
+              g->dout_dtype, g->grad_dtype);
+    return UNIF_MOE_ERR_ARG;
+  }
+  const bool act = p->activation != UNIF_MOE_ACTIVATION_NONE;
+  if (p->rows > 0 && ((!g->x_dev && g->dw_dev) || (!g->w_dev && g->dx_dev) || !g->dout_dev || (act && !g->z_dev))) {
+    set_error("x, w, dout or z is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if ((g->dw_dev && (g->ld_dw < p->cols || (p->rows > 0 && g->ld_x < p->cols))) ||
+      (p->rows > 0 && ((g->dx_dev && (g->ld_w < p->cols || g->ld_dx < p->cols)) || g->ld_dout < p->n ||
+                       (act && g->ld_z < p->n)))) {
+    set_error("a row stride is below the width");
+    return UNIF_MOE_ERR_ARG;
+  }
+  return UNIF_MOE_OK;
+}
+
+bool wide32(const void* p, long long ld, int size) { return bits(p) % 32 == 0 && ld * size % 32 == 0; }
+
+}  // namespace lin
+}  // namespace unif
+
+using unif::set_error;
+namespace ln = unif::lin;
+
+#define UNIF_LAUNCH(call)                                             \
+  do {                                                                \
+    const cudaError_t e_ = (call);                                    \
+    if (e_ != cudaSuccess) {                                          \
+      set_error("linear: %s", cudaGetErrorString(e_));                \
+      return UNIF_MOE_ERR_CUDA;                                       \
+    }                                                                 \
+  } while (0)
+
+extern "C" {
+
+int64_t unif_moe_linear_workspace(const unif_moe_linear* p, const void* x, int64_t ld_x, const void* w,
+                                  int64_t ld_w) {
+  set_error("%s", "");
+  if (ln::check(p) != UNIF_MOE_OK) return -1;
+  return ln::forward_bytes(p, x, ld_x, w, ld_w);
+}
+
+int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_x, const float* x_scale,
+                            const void* w, int64_t ld_w, const float* w_scale, const void* bias,
+                            const void* residual, int64_t ld_res, const uint8_t* mask, void* out, int64_t ld_out,
+                            void* z, int64_t ld_z, void* workspace, int64_t workspace_bytes, int32_t* status,
+                            void* stream) {
+  set_error("%s", "");
+  const int rc = ln::check(p);
+  if (rc != UNIF_MOE_OK || p->rows == 0) return rc;
+  if (!x || !w || !out || !status) {
+    set_error("x, w, out or status is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (p->in_dtype == UNIF_MOE_BF16 && (x_scale || w_scale)) {
+    set_error("bf16 rows take no scales");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (ld_x < p->cols || ld_w < p->cols || ld_out < p->n || (residual && ld_res < p->n) || (z && ld_z < p->n)) {
+    set_error("a row stride is below the width");
+    return UNIF_MOE_ERR_ARG;
+  }
+  const int size = ln::in_size(p), os = p->out_dtype == UNIF_MOE_F32 ? 4 : 2;
+  const int bs = p->bias_dtype == UNIF_MOE_F32 ? 4 : 2;
+  const int64_t need = ln::forward_bytes(p, x, ld_x, w, ld_w);
+  if (need > workspace_bytes || (need && !workspace)) {
+    set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    return UNIF_MOE_ERR_CAPACITY;
+  }
+  if (need && ln::bits(workspace) % 16) {
+    set_error("the workspace must be 16-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  int sms = 0;
+  const int rs = unif::sm_count(&sms);
+  if (rs != UNIF_MOE_OK) return rs;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  ln::Params e{};
+  e.M = (int)p->rows;
+  e.N = p->n;
+  e.splits = 1;
+  e.gelu = p->activation == UNIF_MOE_ACTIVATION_GELU;
+  e.out = out;
+  e.ld_out = ld_out;
+  e.sm = x_scale;
+  e.sn = w_scale;
+  e.bias = bias;
+  e.bias_f32 = p->bias_dtype == UNIF_MOE_F32;
+  e.residual = residual;
+  e.ld_res = ld_res;
+  e.mask = mask;
+  e.z = static_cast<__nv_bfloat16*>(z);
+  e.ld_z = ld_z;
+  e.status = status;
+  if (p->rows <= ln::kRowsMax) {
+    ln::RowsParams r{};
+    r.e = e;
+    r.x = static_cast<const uint8_t*>(x);
+    r.w = static_cast<const uint8_t*>(w);
+    r.ld_x = ld_x * size;
+    r.ld_w = ld_w * size;
+    r.bytes = p->cols * size;
+    const bool vec = ln::tma_rows(x, ld_x, size) && ln::tma_rows(w, ld_w, size);
+    if (size == 2)
+      UNIF_LAUNCH(os == 4 ? (ln::launch_rows<2, float>(r, vec, s)) : (ln::launch_rows<2, __nv_bfloat16>(r, vec, s)));
+    else
+      UNIF_LAUNCH(os == 4 ? (ln::launch_rows<1, float>(r, vec, s)) : (ln::launch_rows<1, __nv_bfloat16>(r, vec, s)));
+    return UNIF_MOE_OK;
+  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  long long px = ld_x, pw = ld_w;
+  if (!ln::tma_rows(x, ld_x, size)) {
+    px = ln::pitch_of(p->cols, size);
+    UNIF_LAUNCH(ln::launch_layout(x, ld_x, ws, px, p->rows, p->cols, size, nullptr, sms, s));
+    x = ws;
+    ws += ln::round_up(p->rows * px * size);
+  }
+  if (!ln::tma_rows(w, ld_w, size)) {
+    pw = ln::pitch_of(p->cols, size);
+    UNIF_LAUNCH(ln::launch_layout(w, ld_w, ws, pw, p->n, p->cols, size, nullptr, sms, s));
+    w = ws;
+  }
+  const ln::Tiles t = ln::pick_tiles(p->rows, p->n, sms);
+  if ((long long)t.m_tiles * t.n_tiles > 0x7fff0000) {
+    set_error("too many tiles: rows=%lld n=%d", (long long)p->rows, p->n);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  e.steps = (int)(((int64_t)p->cols * size + 127) / 128);
+  e.wide = p->n % 16 == 0 && ln::wide32(out, ld_out, os) && (!residual || ln::wide32(residual, ld_res, os)) &&
+           (!z || ln::wide32(z, ld_z, 2)) && (!bias || ln::wide32(bias, 16, bs)) &&
+           (!w_scale || ln::wide32(w_scale, 16, 4));
+  CUtensorMap a, b;
+  if (!ln::map_rows(&a, x, size, p->cols, p->rows, px, 128) ||
+      !ln::map_rows(&b, w, size, p->cols, p->n, pw, t.tile_n / (t.pair ? 2 : 1))) {
+    set_error("cuTensorMapEncodeTiled failed");
+    return UNIF_MOE_ERR_CUDA;
+  }
+  if (size == 2)
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward, float>(a, b, e, t, sms, s))
+                        : (ln::launch_gemm<ln::kForward, __nv_bfloat16>(a, b, e, t, sms, s)));
+  else
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward8, float>(a, b, e, t, sms, s))
+                        : (ln::launch_gemm<ln::kForward8, __nv_bfloat16>(a, b, e, t, sms, s)));
+  return UNIF_MOE_OK;
+}
+
+int64_t unif_moe_linear_backward_workspace(const unif_moe_linear* p, const unif_moe_linear_grad* g) {
+  set_error("%s", "");
+  int sms = 0;
+  if (ln::check_grad(p, g) != UNIF_MOE_OK || unif::sm_count(&sms) != UNIF_MOE_OK) return -1;
+  return p->rows == 0 ? 0 : ln::plan_backward(p, g, sms).total;
+}
+
+int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, void* workspace,
+                             int64_t workspace_bytes, int32_t* status, void* stream) {
+  set_error("%s", "");
+  const int rc = ln::check_grad(p, g);
+  if (rc != UNIF_MOE_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int gs = g->grad_dtype == UNIF_MOE_F32 ? 4 : 2;
+  if (p->rows == 0) {
+    if (g->dw_dev)
+      UNIF_LAUNCH(cudaMemset2DAsync(g->dw_dev, (size_t)g->ld_dw * gs, 0, (size_t)p->cols * gs, p->n, s));
+    if (g->dbias_dev) UNIF_LAUNCH(cudaMemsetAsync(g->dbias_dev, 0, sizeof(float) * p->n, s));
+    return UNIF_MOE_OK;
+  }
+  if (!status) { set_error("status is NULL"); return UNIF_MOE_ERR_ARG; }
+  if (!g->dx_dev && !g->dw_dev && !g->dbias_dev) return UNIF_MOE_OK;
+  int sms = 0;
+  const int rs = unif::sm_count(&sms);
+  if (rs != UNIF_MOE_OK) return rs;
+  const ln::Plan pl = ln::plan_backward(p, g, sms);
+  if (pl.total > workspace_bytes || (pl.total && !workspace)) {
+    set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)pl.total);
+    return UNIF_MOE_ERR_CAPACITY;
+  }
+  if (pl.total && ln::bits(workspace) % 32) {
+    set_error("the workspace must be 32-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if ((long long)pl.in.m_tiles * pl.in.n_tiles > 0x7fff0000 ||
+      (long long)pl.weight.m_tiles * pl.weight.n_tiles * pl.splits > 0x7fff0000) {
+    set_error("too many tiles: rows=%lld cols=%d n=%d", (long long)p->rows, p->cols, p->n);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const void *x = g->x_dev, *w = g->w_dev, *dz = g->dout_dev;
+  if (pl.copy_x) {
+    x = ws + pl.x;
+    UNIF_LAUNCH(ln::launch_layout(g->x_dev, g->ld_x, ws + pl.x, pl.px, p->rows, p->cols, 2, g->token_mask_dev, sms, s));
+  }
+  if (pl.copy_w) {
+    w = ws + pl.w;
+    UNIF_LAUNCH(ln::launch_layout(g->w_dev, g->ld_w, ws + pl.w, pl.pw, p->n, p->cols, 2, nullptr, sms, s));
+  }
+  if (pl.make_dz || pl.sums) {
+    ln::GradParams q{};
+    q.rows = p->rows;
+    q.n = p->n;
+    q.per = pl.per;
+    q.dout = g->dout_dev;
+    q.ld_dout = g->ld_dout;
+    q.z = p->activation != UNIF_MOE_ACTIVATION_NONE ? static_cast<const __nv_bfloat16*>(g->z_dev) : nullptr;
+    q.ld_z = g->ld_z;
+    q.mask = g->token_mask_dev;
+    if (pl.make_dz) {
+      dz = ws + pl.dz;
+      q.dz = reinterpret_cast<__nv_bfloat16*>(ws + pl.dz);
+      q.ld_dz = pl.pz;
+    }
+    q.sums = pl.sums ? reinterpret_cast<float*>(ws + pl.bias) : nullptr;
+    const int ds = g->dout_dtype == UNIF_MOE_F32 ? 4 : 2;
+    const bool vec = p->n % 8 == 0 && ln::bits(g->dout_dev) % 16 == 0 && g->ld_dout * ds % 16 == 0 &&
+                     (!q.z || ln::tma_rows(g->z_dev, g->ld_z, 2));
+    const dim3 grid((p->n + 255) / 256, pl.blocks), block(32 * ln::kGradWarps);
+    void (*kernel)(const ln::GradParams) =
+        ds == 4 ? (vec ? ln::grad_kernel<float, true> : ln::grad_kernel<float, false>)
+                : (vec ? ln::grad_kernel<__nv_bfloat16, true> : ln::grad_kernel<__nv_bfloat16, false>);
+    UNIF_LAUNCH(unif::launch_dependent(kernel, grid, block, 0, s, q));
+  }
+  if (g->dx_dev) {
+    ln::Params e{};
+    e.M = (int)p->rows;
+    e.N = p->cols;
+    e.splits = 1;
+    e.steps = (p->n + 63) / 64;
+    e.out = g->dx_dev;
+    e.ld_out = g->ld_dx;
+    e.status = status;
+    e.wide = p->cols % 16 == 0 && ln::wide32(g->dx_dev, g->ld_dx, 2);
+    CUtensorMap a, b;
+    if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 128) || !ln::map_rows(&b, w, 2, p->cols, p->n, pl.pw, 64)) {
+      set_error("cuTensorMapEncodeTiled failed");
+      return UNIF_MOE_ERR_CUDA;
+    }
+    UNIF_LAUNCH((ln::launch_gemm<ln::kInput, __nv_bfloat16>(a, b, e, pl.in, sms, s)));
+  }
+  if (g->dw_dev) {
+    ln::Params e{};
+    e.M = p->n;
+    e.N = p->cols;
+    e.splits = pl.splits;
+    e.steps = (int)((p->rows + 63) / 64);
+    e.out = g->dw_dev;
+    e.ld_out = g->ld_dw;
+    e.part = reinterpret_cast<float*>(ws + pl.part);
+    e.status = status;
+    e.wide = p->cols % 16 == 0 && (pl.splits > 1 || ln::wide32(g->dw_dev, g->ld_dw, gs));
+    CUtensorMap a, b;
+    if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 64) || !ln::map_rows(&b, x, 2, p->cols, p->rows, pl.px, 64)) {
+      set_error("cuTensorMapEncodeTiled failed");
+      return UNIF_MOE_ERR_CUDA;
+    }
+    UNIF_LAUNCH(gs == 4 ? (ln::launch_gemm<ln::kWeight, float>(a, b, e, pl.weight, sms, s))
+                        : (ln::launch_gemm<ln::kWeight, __nv_bfloat16>(a, b, e, pl.weight, sms, s)));
+  }
+  const bool add = g->dw_dev && pl.splits > 1;
+  if (add || pl.sums) {
+    ln::FinishParams q{};
+    q.part = reinterpret_cast<const float*>(ws + pl.part);
+    q.splits = pl.splits;
+    q.M = p->n;
+    q.N = p->cols;
+    q.dw = g->dw_dev;
+    q.ld_dw = g->ld_dw;
+    q.sums = reinterpret_cast<const float*>(ws + pl.bias);
+    q.blocks = pl.blocks;
+    q.n = p->n;
+    q.dbias = g->dbias_dev;
+    q.dw_ctas = add ? (int)std::min<int64_t>(((int64_t)p->n * p->cols + 1023) / 1024, 8ll * sms) : 0;
+    const unsigned grid = q.dw_ctas + (pl.sums ? (p->n + 31) / 32 : 0);
+    void (*kernel)(const ln::FinishParams) = gs == 4 ? ln::finish_kernel<float> : ln::finish_kernel<__nv_bfloat16>;
+    UNIF_LAUNCH(unif::launch_dependent(kernel, dim3(grid), dim3(256), 0, s, q));
+  }
+  return UNIF_MOE_OK;
+}
+
+}  // extern "C"

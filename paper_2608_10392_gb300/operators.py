@@ -23,7 +23,7 @@ from typing import NamedTuple, Optional
 import torch
 
 __all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize",
-           "mxfp4_product", "mxfp4_status"]
+           "mxfp4_product", "mxfp4_status", "Fp8", "linear", "linear_backward", "linear_status"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
@@ -37,9 +37,24 @@ class _BlockNormDesc(C.Structure):
                 ("gate_rows", C.c_int), ("res_scale", C.c_float), ("eps", C.c_float)]
 
 
+class _LinearDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int), ("n", C.c_int), ("in_dtype", C.c_int),
+                ("out_dtype", C.c_int), ("bias_dtype", C.c_int), ("activation", C.c_int)]
+
+
+class _LinearGrad(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("w", C.c_void_p), ("dout", C.c_void_p), ("z", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_dout", C.c_int64),
+                ("ld_z", C.c_int64), ("dout_dtype", C.c_int), ("grad_dtype", C.c_int),
+                ("mask", C.c_void_p), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dw", C.c_void_p),
+                ("ld_dw", C.c_int64), ("dbias", C.c_void_p)]
+
+
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
            "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss",
-           "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize", "unif_moe_mxfp4_product"]
+           "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize", "unif_moe_mxfp4_product",
+           "unif_moe_linear_workspace", "unif_moe_linear_forward",
+           "unif_moe_linear_backward_workspace", "unif_moe_linear_backward"]
 
 
 def declare(L: C.CDLL) -> None:
@@ -57,6 +72,12 @@ def declare(L: C.CDLL) -> None:
     L.unif_moe_mxfp4_quantize.argtypes = [P, I, I64, I, I64, P, P, P]
     L.unif_moe_mxfp4_dequantize.argtypes = [P, P, I64, I, P, I, I64, P]
     L.unif_moe_mxfp4_product.argtypes = [P, P, I64, I, P, P, I, I, P, I, P, I, I64, P, P]
+    Q, G = C.POINTER(_LinearDesc), C.POINTER(_LinearGrad)
+    L.unif_moe_linear_workspace.argtypes = [Q, P, I64, P, I64]
+    L.unif_moe_linear_forward.argtypes = ([Q, P, I64, P, P, I64, P, P, P, I64, P, P, I64, P, I64, P, I64,
+                                           P, P])
+    L.unif_moe_linear_backward_workspace.argtypes = [Q, G]
+    L.unif_moe_linear_backward.argtypes = [Q, G, P, I64, P, P]
     for name in EXPORTS:
         getattr(L, name).restype = I64 if name.endswith("_workspace") else C.c_int
 
@@ -183,7 +204,7 @@ def _status_word(device: torch.device) -> torch.Tensor:
     t = _status_words.get(device)
     if t is None:
         if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("the first mxfp4_product on a device has to be outside a capture")
+            raise RuntimeError("the first product on a device has to be outside a capture")
         t = torch.zeros(1, dtype=torch.int32, device=device)
         torch.cuda.current_stream(device).synchronize()  # products may be on another stream
         _status_words[device] = t
@@ -191,8 +212,9 @@ def _status_word(device: torch.device) -> torch.Tensor:
 
 
 def mxfp4_status(device=None) -> int:
-    """Waits for the device and returns ERR_TIMEOUT (-5) if a product's kernel gave up a
-    wait since the last call (its output is incomplete), else 0."""
+    """Waits for the device and returns ERR_TIMEOUT (-5) if the kernel of a product (mxfp4_product,
+    linear, linear_backward) gave up a wait since the last call (its output is incomplete),
+    else 0. linear_status is the same."""
     device = torch.device("cuda" if device is None else device)
     torch.cuda.synchronize(device)  # (raises for other devices)
     if device.index is None:
@@ -216,3 +238,48 @@ def mxfp4_product(a: Mxfp4, w: Mxfp4, offsets: Optional[torch.Tensor] = None, *,
     return _b().product(a.codes, a.scales, a.cols, w.codes, w.scales, w.cols, offsets,
                         _ACTIVATIONS[activation], _CODES[DTYPES[dtype]], out,
                         _status_word(a.codes.device) if a.codes.is_cuda else None, stream)
+
+
+linear_status = mxfp4_status
+
+
+class Fp8(NamedTuple):
+    """Rows in 8-bit floating point (E4M3) under a scale each: a value is its code times the
+    scale of its row. codes [...][cols] float8_e4m3fn with dense rows (those of a 2-d tensor may be
+    strided), scales [...] fp32, contiguous."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _status_of(x):
+    return _status_word(x.device) if isinstance(x, torch.Tensor) and x.is_cuda else None
+
+
+def linear(x, w, bias: Optional[torch.Tensor] = None, *, activation: str = "none",
+           residual: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+           dtype: str = "bf16", keep: bool = False, out: Optional[torch.Tensor] = None, stream=None):
+    """out = residual + act(x w^T + bias), [T][n] ("bf16" or "f32"): one kernel, the sum rounded
+    once.
+
+    x [T][cols] and w [n][cols] both bf16 or both Fp8 (rows under a scale each); rows of all
+    2-d tensors may be strided, with any alignment. bias [n] fp32 or bf16; residual [T][n] of
+    the result's dtype (out may be it); activation "none" or "gelu"; mask [T]: 0 marks padding,
+    whose rows give 0. keep: also z = x w^T + bias in bf16, (out, z), for linear_backward."""
+    if isinstance(x, Fp8) != isinstance(w, Fp8):
+        raise ValueError("x and w: need both in 8 bits or neither")
+    xc, xs, wc, ws = (x.codes, x.scales, w.codes, w.scales) if isinstance(x, Fp8) else (x, None, w, None)
+    return _b().linear(xc, xs, wc, ws, bias, _ACTIVATIONS[activation], residual, mask,
+                       _CODES[DTYPES[dtype]], keep, out, _status_of(xc), stream)
+
+
+def linear_backward(x: torch.Tensor, w: torch.Tensor, dout: torch.Tensor,
+                    z: Optional[torch.Tensor] = None, *, activation: str = "none",
+                    mask: Optional[torch.Tensor] = None, bias: bool = False, dx: bool = True,
+                    dw: bool = True, grad_dtype: str = "f32", stream=None) -> dict:
+    """Gradients of linear for bf16 x and w, from that of its result (dout [T][n], fp32 or bf16)
+    and its z (with an activation): dict of dx [T][cols] (bf16), dw [n][cols] (grad_dtype),
+    dbias [n] (fp32); None for what `dx`, `dw`, `bias` do not ask for. The residual's gradient
+    is dout. Padding rows (mask 0) give 0 in dx and take no part in the sums. dz = dout act'(z)
+    is rounded to bf16 for the two products."""
+    return _b().linear_backward(x, w, dout, z, _ACTIVATIONS[activation], mask, dx, dw, bias,
+                                _CODES[DTYPES[grad_dtype]], _status_of(x), stream)

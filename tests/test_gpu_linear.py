@@ -1,0 +1,417 @@
+"""The dense products (linear, linear_backward) against 64 bits: sizes from one row to many,
+odd widths, strides, masks, 8-bit rows, in-place residuals, gradients against the formula's
+and against differences; refusals.
+
+Tolerances. Products of two bf16 (or two 8-bit) values are exact in fp32. The tensor cores add
+16 (32) of them to an fp32 sum and cut it: with S the sum of the terms' absolute values a
+step loses at most 2^-22 S, so a sum over c columns is within (c / 16 + 2) 2^-22 S (the two:
+sums of warps or parts). Scales, bias and residual are fp32 operations, 2^-23 of what they
+give each: 4 in all. GELU has a slope of at most 1.13 and its own 2^-11 of the value in bf16
+results, 2^-20 (normcdff and a product) in fp32 ones. A result is rounded once: 2^-8 in bf16."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+F64 = torch.float64
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def gelu(z):
+    return z * torch.special.ndtr(z)
+
+
+def operand(rows, cols, g, pad=0, shift=0, scale=1.0):
+    """bf16 rows, `pad` elements apart, `shift` elements into their buffer."""
+    wide = torch.randn(rows, cols + pad + shift, generator=g, device="cuda").mul_(scale).bfloat16()
+    return wide[:, shift:shift + cols]
+
+
+def eight(rows, cols, g, pad=0, scale=1.0):
+    from paper_2608_10392_gb300 import Fp8
+    v = (torch.randn(rows, cols + pad, generator=g, device="cuda") * 60).clamp(-448, 448)
+    return Fp8(v.to(torch.float8_e4m3fn)[:, :cols],
+               scale / 60 * (0.5 + torch.rand(rows, generator=g, device="cuda")))
+
+
+def value(x):
+    if isinstance(x, torch.Tensor):
+        return x.to(F64)
+    return x.codes.to(F64) * x.scales.to(F64)[:, None]
+
+
+def check(x, w, bias=None, act="none", residual=None, mask=None, dtype="bf16", keep=False, out=None, **kw):
+    from paper_2608_10392_gb300 import linear, linear_status
+    before = None if residual is None else residual.to(F64)
+    got = linear(x, w, bias, activation=act, residual=residual, mask=mask, dtype=dtype, keep=keep, out=out, **kw)
+    assert linear_status() == 0
+    got, z_got = got if keep else (got, None)
+    xv, wv = value(x), value(w)
+    on = torch.ones(len(xv), dtype=torch.bool, device="cuda") if mask is None else mask != 0
+    xv = torch.where(on[:, None], xv, 0.0)
+    z = xv @ wv.T
+    size = xv.abs() @ wv.abs().T
+    step = 16 if isinstance(x, torch.Tensor) else 32
+    tol = (xv.shape[1] / step + 2) * 2.0 ** -22 * size
+    if bias is not None:
+        z = z + bias.to(F64)
+    tol = tol + 4 * 2.0 ** -23 * (size + z.abs())
+    z_tol = tol + 2.0 ** -8 * z.abs()
+    y = z
+    if act == "gelu":
+        y = gelu(z)
+        tol = 1.13 * tol + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -20) * y.abs() + 2e-37
+    if residual is not None:
+        y = y + torch.where(on[:, None], before, 0.0)
+        tol = tol + 2.0 ** -23 * (y.abs() + before.abs().nan_to_num())
+    tol = tol + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * y.abs()
+    assert got.shape == y.shape and got.dtype == TYPES[dtype]
+    y, z = torch.where(on[:, None], y, 0.0), torch.where(on[:, None], z, 0.0)
+    err = (got.to(F64) - y).abs()
+    bad = ~(err <= torch.where(on[:, None], tol, 0.0))
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist(), float(err.nan_to_num(1e9).max()))
+    if keep:
+        bad = ~((z_got.to(F64) - z).abs() <= torch.where(on[:, None], z_tol, 0.0))
+        assert z_got.dtype == torch.bfloat16 and not bad.any(), int(bad.sum())
+    return got
+
+
+def inputs(T, cols, n, seed, kind="bf16", bias=None, residual=None, masked=False, dtype="bf16"):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    make = operand if kind == "bf16" else eight
+    r = dict(x=make(T, cols, g), w=make(n, cols, g, scale=cols ** -0.5))
+    if bias:
+        r["bias"] = torch.randn(n, generator=g, device="cuda").to(TYPES[bias])
+    if residual:
+        r["residual"] = (2 * torch.randn(T, n, generator=g, device="cuda")).to(TYPES[dtype])
+    if masked:
+        r["mask"] = torch.rand(T, generator=g, device="cuda") < 0.6
+        if kind == "bf16":
+            r["x"][~r["mask"]] = float("nan")
+        else:
+            r["x"].codes.view(torch.uint8)[~r["mask"]] = 0x7f  # NaN
+        if residual:
+            r["residual"][~r["mask"]] = float("nan")
+    return r
+
+
+SIZES = [(1, 1, 1), (1, 64, 16), (3, 7, 5), (7, 1024, 4096), (8, 4096, 1024), (9, 333, 77), (16, 384, 1536),
+         (17, 100, 40), (32, 2000, 130), (33, 1, 1), (33, 64, 16), (64, 1023, 47), (100, 4096, 1024),
+         (127, 768, 768), (128, 128, 256), (129, 65, 257), (300, 384, 1536), (1000, 1000, 1000), (2049, 72, 264),
+         (5003, 1001, 777), (12608, 384, 1536), (9000, 520, 2064)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,cols,n", SIZES)
+def test_against_64_bits(T, cols, n, kind):
+    check(**inputs(T, cols, n, T + cols + n, kind))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,cols,n", [(5, 200, 33), (30, 512, 96), (70, 512, 96), (70, 200, 33), (700, 320, 528),
+                                      (4000, 136, 600), (4000, 160, 608)])
+@pytest.mark.parametrize("bias,act,residual,dtype,keep,masked", [
+    ("bf16", "gelu", False, "bf16", True, False), ("f32", "none", True, "f32", False, True),
+    ("bf16", "none", True, "bf16", False, True), (None, "gelu", True, "f32", True, True),
+    ("f32", "gelu", True, "bf16", False, False)])
+def test_epilogue(T, cols, n, kind, bias, act, residual, dtype, keep, masked):
+    check(**inputs(T, cols, n, n + T, kind, bias, residual, masked, dtype), act=act, dtype=dtype, keep=keep)
+
+
+@pytest.mark.gpu
+def test_every_row_padding_and_no_rows():
+    from paper_2608_10392_gb300 import linear
+    for T in (4, 200):
+        k = inputs(T, 64, 48, 1, bias="f32", residual=True, masked=True)
+        k["mask"][:] = False
+        k["x"][:] = float("nan")
+        k["residual"][:] = float("inf")
+        assert (check(**k, act="gelu", keep=True) == 0).all()
+    w = torch.ones(48, 64, device="cuda").bfloat16()
+    assert linear(torch.empty(0, 64, device="cuda").bfloat16(), w).shape == (0, 48)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 40, 900])
+@pytest.mark.parametrize("cols,n,pad,shift", [(128, 64, 8, 0), (128, 64, 8, 8), (128, 64, 3, 1), (100, 36, 4, 0),
+                                              (64, 48, 1, 0), (96, 80, 0, 2)])
+def test_strides(T, cols, n, pad, shift):
+    g = torch.Generator(device="cuda").manual_seed(T + cols)
+    x, w = operand(T, cols, g, pad, shift), operand(n, cols, g, pad, shift)
+    for dtype in ("bf16", "f32"):
+        wide = torch.full((T, n + pad + shift), 3.0, device="cuda", dtype=TYPES[dtype])
+        res = torch.randn(T, n + pad + shift, generator=g, device="cuda").to(TYPES[dtype])[:, shift:shift + n]
+        check(x, w, dtype=dtype, residual=res, out=wide[:, shift:shift + n])
+        assert (wide[:, :shift] == 3).all() and (wide[:, shift + n:] == 3).all()
+    q = eight(T, cols, g, pad=5)
+    check(q, eight(n, cols, g, pad=3))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n", [(6, 48), (50, 48), (600, 77), (3000, 512)])
+def test_result_in_place_of_the_residual(T, n):
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x, w = operand(T, 96, g), operand(n, 96, g, scale=0.1)
+    res = torch.randn(T, n, generator=g, device="cuda")
+    want = check(x, w, residual=res.clone(), dtype="f32", act="gelu")
+    got = check(x, w, residual=res, dtype="f32", act="gelu", out=res)
+    assert got.data_ptr() == res.data_ptr() and torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements of result: the last rows are as right as the first."""
+    from paper_2608_10392_gb300 import linear
+    g = torch.Generator(device="cuda").manual_seed(3)
+    T, n = 70000, 32768
+    x, w = operand(T, 64, g), operand(n, 64, g, scale=0.125)
+    out = linear(x, w)
+    for rows in (slice(0, 300), slice(T - 300, T)):
+        z = x[rows].to(F64) @ w.to(F64).T
+        assert ((out[rows].to(F64) - z).abs() <= 2.0 ** -8 * z.abs() + 1e-5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [6, 50, 3000])
+def test_other_streams_and_graphs(T):
+    from paper_2608_10392_gb300 import linear, linear_backward
+    k = inputs(T, 200, 120, 2, bias="bf16")
+    dout = torch.randn(T, 120, device="cuda").bfloat16()
+
+    def both(**s):
+        y, z = linear(k["x"], k["w"], k["bias"], activation="gelu", keep=True, **s)
+        r = linear_backward(k["x"], k["w"], dout, z, activation="gelu", bias=True, **s)
+        return y, r["dx"], r["dw"], r["dbias"]
+
+    want = both()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = both(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    k["x"].copy_(k["x"].flip(0))
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    again = both()
+    assert all(torch.equal(a, b) for a, b in zip(held, again)) and not torch.equal(held[0], want[0])
+
+
+# ------------------------------------------------------------------ gradients
+
+def check_backward(x, w, dout, z=None, act="none", mask=None, grad_dtype="f32", **kw):
+    """dz is exact to 2^-20 (GELU's derivative, at most 1.13: 2e-6 of dout), rounded by 2^-8
+    where it is not dout itself; sums as above over n columns (dx) or T rows (dw)."""
+    from paper_2608_10392_gb300 import linear_backward, linear_status
+    r = linear_backward(x, w, dout, z, activation=act, mask=mask, bias=True, grad_dtype=grad_dtype, **kw)
+    assert linear_status() == 0
+    on = torch.ones(len(x), dtype=torch.bool, device="cuda") if mask is None else mask != 0
+    xv, d, wv = (torch.where(on[:, None], x.to(F64), 0.0), torch.where(on[:, None], dout.to(F64), 0.0), w.to(F64))
+    dz, off = d, torch.zeros_like(d)
+    if act == "gelu":
+        zv = torch.where(on[:, None], z.to(F64), 0.0)
+        dz = d * (torch.special.ndtr(zv) + zv * torch.exp(-zv * zv / 2) / math.sqrt(2 * math.pi))
+        off = 2e-6 * d.abs()
+    rounded = act != "none" or dout.dtype == torch.float32
+    unit = 2.0 ** -8 * dz.abs() + off if rounded else off
+    T, n = d.shape
+
+    def close(got, want, tol, kind):
+        assert got.dtype == TYPES[kind] and got.shape == want.shape
+        tol = tol + (2.0 ** -8 if kind == "bf16" else 2.0 ** -23) * want.abs()
+        bad = ~((got.to(F64) - want).abs() <= tol)
+        assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+    size = dz.abs() @ wv.abs()
+    close(r["dx"], dz @ wv, unit @ wv.abs() + (n / 16 + 2) * 2.0 ** -22 * size, "bf16")
+    size = dz.abs().T @ xv.abs()
+    # an accumulation runs over at most 1,024 rows; those are added in fp32
+    close(r["dw"], dz.T @ xv, unit.T @ xv.abs() + (min(T, 1024) / 16 + T / 1024 + 66) * 2.0 ** -22 * size, grad_dtype)
+    close(r["dbias"], dz.sum(0), off.sum(0) + (T / 32 + 64) * 2.0 ** -24 * dz.abs().sum(0), "f32")
+    return r
+
+
+def grads(T, cols, n, seed, act="none", masked=False, dtype="bf16", pad=0, shift=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    k = dict(x=operand(T, cols, g, pad, shift), w=operand(n, cols, g, pad, shift, scale=cols ** -0.5), act=act)
+    k["dout"] = (0.1 * torch.randn(T, n + pad, generator=g, device="cuda")).to(TYPES[dtype])[:, :n]
+    if act != "none":
+        k["z"] = operand(T, n, g, pad, shift, scale=2.0)
+    if masked:
+        k["mask"] = torch.rand(T, generator=g, device="cuda") < 0.6
+        for name in ("x", "dout", "z"):
+            if name in k:
+                k[name][~k["mask"]] = float("nan")
+    return k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,cols,n", [(1, 1, 1), (1, 64, 64), (5, 33, 7), (63, 128, 256), (64, 200, 120), (65, 65, 65),
+                                      (300, 384, 1536), (1000, 768, 130), (1025, 72, 264), (5003, 333, 129),
+                                      (12608, 384, 1536), (20000, 1024, 512), (40000, 128, 128)])
+@pytest.mark.parametrize("act,masked,grad_dtype", [("none", False, "f32"), ("gelu", True, "bf16"),
+                                                   ("gelu", False, "f32"), ("none", True, "f32")])
+def test_gradients(T, cols, n, act, masked, grad_dtype):
+    check_backward(**grads(T, cols, n, T + n, act, masked), grad_dtype=grad_dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 1), (1, 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_strided_rows(pad, shift, dtype):
+    check_backward(**grads(300, 96, 80, 1, "gelu", False, dtype, pad, shift))
+    check_backward(**grads(300, 96, 80, 1, "none", True, dtype, pad, shift))
+
+
+@pytest.mark.gpu
+def test_gradients_of_extreme_z():
+    k = grads(70, 32, 48, 1, "gelu")
+    k["z"][:, :8] = torch.tensor([0.0, -0.0, 13.0, -13.0, 40.0, -40.0, 1e30, -1e30], device="cuda").bfloat16()
+    check_backward(**k)
+    k["z"][:, 0], k["z"][:, 1] = float("inf"), -float("inf")
+    from paper_2608_10392_gb300 import linear_backward
+    r = linear_backward(k["x"], k["w"], k["dout"], k["z"], activation="gelu", bias=True)
+    assert torch.isfinite(r["dx"]).all() and torch.isfinite(r["dw"]).all()
+    # -inf is taken as -13, where the derivative is Phi - 13 phi > -13 0.4 e^-84.5 > -2e-36;
+    # 70 rows of |x| < 6 and |dout| < 1 make less than 1e-33 of it
+    assert (r["dw"][1].abs() < 1e-33).all() and torch.allclose(r["dbias"][0], k["dout"][:, 0].float().sum(), rtol=1e-5)
+
+
+@pytest.mark.gpu
+def test_no_rows_and_all_padding():
+    from paper_2608_10392_gb300 import linear_backward
+    w = torch.ones(48, 64, device="cuda").bfloat16()
+    r = linear_backward(torch.empty(0, 64, device="cuda").bfloat16(), w, torch.empty(0, 48, device="cuda").bfloat16(),
+                        bias=True)
+    assert r["dx"].shape == (0, 64) and (r["dw"] == 0).all() and (r["dbias"] == 0).all()
+    k = grads(90, 64, 48, 3, "gelu", True)
+    k["mask"][:] = False
+    r = check_backward(**k)
+    assert all((r[name] == 0).all() for name in r)
+
+
+@pytest.mark.gpu
+def test_only_what_is_asked_for():
+    from paper_2608_10392_gb300 import linear_backward
+    k = grads(200, 96, 80, 5)
+    whole = check_backward(**k)
+    for ask in (dict(dw=False), dict(dx=False), dict(dx=False, dw=False, bias=True), dict(dx=False, dw=False)):
+        r = linear_backward(k["x"], k["w"], k["dout"], **ask)
+        for name, default in (("dx", True), ("dw", True), ("bias", False)):
+            got = r["dbias" if name == "bias" else name]
+            if ask.get(name, default):
+                assert torch.equal(got, whole["dbias" if name == "bias" else name])
+            else:
+                assert got is None
+
+
+@pytest.mark.gpu
+def test_gradients_against_differences():
+    """sum(out * c) for small changes of x and w, in 64 bits: the forward and the backward
+    belong together. The difference quotient of step h is off by h^2 f''' / 6, far below the
+    2^-8 that dz is rounded by."""
+    from paper_2608_10392_gb300 import linear, linear_backward
+    g = torch.Generator(device="cuda").manual_seed(11)
+    T, cols, n = 50, 40, 24
+    x, w, b = operand(T, cols, g), operand(n, cols, g, scale=0.2), torch.randn(n, generator=g, device="cuda")
+    c = torch.randn(T, n, generator=g, device="cuda").bfloat16()
+    _, z = linear(x, w, b, activation="gelu", keep=True)
+    r = linear_backward(x, w, c, z, activation="gelu", bias=True)
+
+    def f(xv, wv, bv):
+        return (gelu(xv @ wv.T + bv) * c.to(F64)).sum()
+
+    xv, wv, bv = x.to(F64), w.to(F64), b.to(F64)
+    h = 1e-4
+    for name, ref, at in (("dx", xv, (3, 7)), ("dx", xv, (49, 0)), ("dw", wv, (5, 39)), ("dbias", bv, (23,))):
+        d = torch.zeros_like(ref)
+        d[at] = h
+        args = {"dx": [d, 0, 0], "dw": [0, d, 0], "dbias": [0, 0, d]}[name]
+        num = (f(xv + args[0], wv + args[1], bv + args[2]) - f(xv - args[0], wv - args[1], bv - args[2])) / (2 * h)
+        # z and dz rounded by 2^-8, each term of the sum at most |c| 1.13 times its factor
+        size = {"dx": (c.to(F64).abs() @ wv.abs()), "dw": (c.to(F64).abs().T @ xv.abs()),
+                "dbias": c.to(F64).abs().sum(0)}[name][at]
+        assert abs(float(r[name][at]) - float(num)) <= 2.0 ** -6 * float(size)
+
+
+@pytest.mark.gpu
+def test_results_repeat():
+    k = grads(9000, 520, 264, 9, "gelu")
+    a, b = check_backward(**k), check_backward(**k)
+    assert all(torch.equal(a[name], b[name]) for name in a)
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_refusals():
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+    p = C.c_void_p(4096)
+
+    def call(**k):
+        v = dict(rows=4, cols=64, n=8, i=1, o=1, bt=1, act=0, x=p, ld_x=64, sx=None, w=p, ld_w=64, sw=None, res=None,
+                 ld_r=8, out=p, ld=8, z=None, ld_z=8, ws=None, wb=0, status=p)
+        v.update(k)
+        d = ops._LinearDesc(v["rows"], v["cols"], v["n"], v["i"], v["o"], v["bt"], v["act"])
+        return L.unif_moe_linear_forward(C.byref(d), v["x"], v["ld_x"], v["sx"], v["w"], v["ld_w"], v["sw"], None,
+                                         v["res"], v["ld_r"], None, v["out"], v["ld"], v["z"], v["ld_z"], v["ws"],
+                                         v["wb"], v["status"], None)
+
+    for k in (dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(n=0), dict(cols=(1 << 24) + 1), dict(i=0),
+              dict(i=3), dict(o=2), dict(bt=2), dict(act=2), dict(act=-1), dict(x=None), dict(w=None),
+              dict(out=None), dict(status=None), dict(sx=p), dict(sw=p), dict(ld_x=63), dict(ld_w=63), dict(ld=7),
+              dict(res=p, ld_r=7), dict(z=p, ld_z=7)):
+        assert call(**k) == -1, k
+    # rows that start off 16 bytes need a workspace
+    odd = dict(rows=100, cols=63, ld_x=63)
+    assert call(**odd) == -3 and call(**odd, ws=C.c_void_p(4100), wb=1 << 20) == -1
+    assert call(rows=0, x=None) == 0
+    d = ops._LinearDesc(100, 63, 8, 1, 1, 1, 0)
+    assert L.unif_moe_linear_workspace(C.byref(d), p, 63, p, 64) >= 100 * 64 * 2
+    assert L.unif_moe_linear_workspace(C.byref(d), p, 64, p, 64) == 0
+    assert L.unif_moe_linear_workspace(None, p, 64, p, 64) == -1
+
+    def back(**k):
+        v = dict(i=1, rows=4, act=0, x=p, w=p, dout=p, z=None, ld_x=64, ld_w=64, ld_dout=8, ld_z=8, dt=1, gt=0, dx=p,
+                 ld_dx=64, dw=p, ld_dw=64)
+        v.update(k)
+        d = ops._LinearDesc(v["rows"], 64, 8, v["i"], 1, 1, v["act"])
+        g = ops._LinearGrad(v["x"], v["w"], v["dout"], v["z"], v["ld_x"], v["ld_w"], v["ld_dout"], v["ld_z"], v["dt"],
+                            v["gt"], None, v["dx"], v["ld_dx"], v["dw"], v["ld_dw"], None)
+        return L.unif_moe_linear_backward(C.byref(d), C.byref(g), None, 0, None, None)
+
+    for k in (dict(i=2), dict(act=1), dict(x=None), dict(w=None), dict(dout=None), dict(dt=2), dict(gt=2),
+              dict(ld_x=63), dict(ld_w=63), dict(ld_dout=7), dict(act=1, z=p, ld_z=7), dict(ld_dx=63),
+              dict(ld_dw=63), dict(rows=-1), dict()):  # (the last: no status word)
+        assert back(**k) == -1, k
+    x = torch.zeros(4, 64).bfloat16()
+    with pytest.raises(ValueError, match="x: need a CUDA tensor"):
+        pkg.linear(x, x)
+    with pytest.raises(ValueError, match="both in 8 bits"):
+        pkg.linear(x, pkg.Fp8(x, x))
+    with pytest.raises(KeyError):
+        pkg.linear(x, x, activation="tanh")
+
+
+@pytest.mark.gpu
+def test_refusals_of_tensors():
+    import paper_2608_10392_gb300 as pkg
+    x, w = torch.zeros(4, 64, device="cuda").bfloat16(), torch.zeros(8, 64, device="cuda").bfloat16()
+    for bad in (dict(bias=torch.zeros(7, device="cuda")), dict(bias=torch.zeros(8, device="cuda").half()),
+                dict(residual=torch.zeros(4, 8, device="cuda")), dict(mask=torch.ones(3, device="cuda") > 0),
+                dict(out=torch.zeros(4, 8, device="cuda")), dict(bias=torch.zeros(8))):
+        with pytest.raises(ValueError):
+            pkg.linear(x, w, **bad)
+    with pytest.raises(ValueError, match="w:"):
+        pkg.linear(x, w[:, :63])
+    with pytest.raises(ValueError, match="z: the gradient"):
+        pkg.linear_backward(x, w, torch.zeros(4, 8, device="cuda").bfloat16(), activation="gelu")
