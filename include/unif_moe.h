@@ -494,6 +494,17 @@ UNIF_MOE_API int unif_moe_block_norm_backward(
     float* d_gate_dev, float* dw_pre_dev, float* db_pre_dev, void* workspace_dev,
     int64_t workspace_bytes, void* stream);
 
+/* The forward with u in 8 bits, as unif_moe_fp8_quantize gives it from the fp32 u (not from a
+ * rounded one): u_codes_dev [T][width] E4M3, rows ld_u bytes apart, u_scales_dev [T]. Padding
+ * rows have codes 0. Needs a pre norm; u_codes overlaps no input. The backward takes the gradient of u as if nothing
+ * had been rounded. Everything else as unif_moe_block_norm_forward. */
+UNIF_MOE_API int unif_moe_block_norm_forward_fp8(
+    const unif_moe_block_norm* p, const void* x_dev, int64_t ld_x, const void* y_dev, int64_t ld_y,
+    const uint8_t* token_mask_dev, const void* w_post_dev, const void* b_post_dev,
+    const void* gate_dev, const void* w_pre_dev, const void* b_pre_dev, void* out_dev,
+    int64_t ld_out, uint8_t* u_codes_dev, int64_t ld_u, float* u_scales_dev, float* post_mean_dev,
+    float* post_rstd_dev, float* pre_mean_dev, float* pre_rstd_dev, void* stream);
+
 #define UNIF_MOE_BALANCE_MAX_EXPERTS 512
 
 /* Bytes of device workspace of unif_moe_balance_loss; -1 on bad sizes. */
@@ -585,13 +596,29 @@ UNIF_MOE_API int unif_moe_mxfp4_product(const uint8_t* a_codes_dev, const uint8_
                                         unif_moe_dtype dtype, int64_t ld, int32_t* status_dev,
                                         void* stream);
 
+/* Rows to 8-bit floating point (E4M3: sign, four exponent bits, three mantissa bits, values
+ * up to 448) under a scale each: the scale of a row is 2^e with the smallest e, at least -126, for
+ * which no value is above 448 2^e (2^-126 for a row of zeros), a code x 2^-e rounded to nearest
+ * even. A row with a NaN or an infinity gets the scale NaN and codes 0.
+ *   x_dev [rows][cols] fp32 or bf16, rows ld apart
+ *   codes_dev [rows][cols], rows ld_codes bytes apart; scales_dev [rows] fp32
+ * Up to 2^24 columns. Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_CUDA. */
+UNIF_MOE_API int unif_moe_fp8_quantize(const void* x_dev, unif_moe_dtype dtype, int64_t rows, int cols,
+                                       int64_t ld, uint8_t* codes_dev, int64_t ld_codes,
+                                       float* scales_dev, void* stream);
+
+/* Codes times the scale of their row (any fp32 scale, any E4M3 code; 0x7f and 0xff are NaN),
+ * rounded once to fp32 or bf16, rows ld apart. Enqueued on `stream`, no sync. Errors as above. */
+UNIF_MOE_API int unif_moe_fp8_dequantize(const uint8_t* codes_dev, int64_t ld_codes,
+                                         const float* scales_dev, int64_t rows, int cols, void* x_dev,
+                                         unif_moe_dtype dtype, int64_t ld, void* stream);
+
 /* ---- Dense products beside the layer ----
  * The products of a Transformer block that are no experts (attention's projections, a
  * dense FFN), with what follows them in the product's epilogue. As the operators above
  * they need no handle, allocate nothing and keep no state between calls. */
 
-/* in_dtype of rows and weights in 8-bit floating point (E4M3: sign, four exponent bits,
- * three mantissa bits, values up to 448) with fp32 scales */
+/* in_dtype of rows and weights in 8-bit floating point (E4M3) with fp32 scales */
 #define UNIF_MOE_E4M3 2
 #define UNIF_MOE_LINEAR_MAX_COLS (1 << 24)
 

@@ -20,14 +20,15 @@ from typing import Optional
 import torch
 
 from . import operators as _operators
-from .operators import (BlockNorm, Fp8, Mxfp4, balance_loss, linear, linear_backward,
+from .operators import (BlockNorm, Fp8, Mxfp4, balance_loss, fp8_dequantize, fp8_quantize, linear, linear_backward,
                         linear_status, mxfp4_dequantize, mxfp4_product, mxfp4_quantize,
                         mxfp4_status)
 
 __all__ = ["Layer", "lib", "UnifMoeError", "ERR", "EXPORTS", "Options", "FEATURE_NORM_FIRST",
            "FEATURE_HOST_IO", "FEATURE_BACKWARD", "FEATURE_DIAGNOSTICS", "FEATURES_DEFAULT",
            "FEATURES_ALL", "BlockNorm", "balance_loss", "Mxfp4",
-           "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_product", "mxfp4_status", "Fp8", "linear",
+           "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_product", "mxfp4_status", "Fp8",
+           "fp8_quantize", "fp8_dequantize", "linear",
            "linear_backward", "linear_status"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))

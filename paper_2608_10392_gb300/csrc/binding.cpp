@@ -211,9 +211,19 @@ NormParams norm_params(const Place& at, const unif_moe_block_norm& d, PyObject* 
   return p;
 }
 
-// desc, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, mask, out, u, stats, stream
-PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 13, [&]() -> PyObject* {
+// Codes [rows][cols] of 8 bits, their rows' pitch a multiple of 16 bytes (so that a product reads them
+// where they are); for more dimensions the last one is cols.
+Tensor empty_codes(const Place& at, at::IntArrayRef size) {
+  std::vector<int64_t> wide(size.begin(), size.end());
+  wide.back() = (wide.back() + 15) / 16 * 16;
+  const Tensor t = at.empty(wide, at::kFloat8_e4m3fn);
+  return wide.back() == size.back() ? t : t.narrow(-1, 0, size.back());
+}
+
+// desc, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, mask, out, u, stats, stream; u in
+// 8 bits: its codes, and after the stream its scales (None: new ones)
+PyObject* norm_forward_as(PyObject* const* a, Py_ssize_t n, bool eight) {
+  return guarded(n, eight ? 14 : 13, [&]() -> PyObject* {
     const Tensor x = tensor(a[1], "x"), y = tensor(a[2], "y");
     const Place at(x, "x", a[12]);
     if (x.dim() != 2) value_error("x: need two dimensions");
@@ -227,8 +237,21 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const uint8_t* mask = mask_of(at, tensor(a[8], "mask"), T);
     Tensor out = tensor(a[9], "out"), u = tensor(a[10], "u"), st[4];
     if (y.defined() && !out.defined()) out = at.empty({T, d.width}, ts);
-    if (d.pre_norm && !u.defined()) u = at.empty({T, d.width}, tb);
-    const Rows po = rows_of(at, out, "out", T, d.width, ts), pu = rows_of(at, u, "u", T, d.width, tb);
+    Tensor scales;
+    if (eight) {
+      if (!d.pre_norm) value_error("u in 8 bits needs a pre norm");
+      scales = tensor(a[13], "u.scales");
+      if (u.defined() != scales.defined()) value_error("u: need codes and scales");
+      if (!u.defined()) {
+        u = empty_codes(at, {T, d.width});
+        scales = at.empty({T}, at::kFloat);
+      }
+    } else if (d.pre_norm && !u.defined()) {
+      u = at.empty({T, d.width}, tb);
+    }
+    const Rows po = rows_of(at, out, "out", T, d.width, ts),
+               pu = rows_of(at, u, "u", T, d.width, eight ? at::kFloat8_e4m3fn : tb);
+    float* su = static_cast<float*>(dense(at, scales, "u.scales", T, at::kFloat));
     float* sp[4] = {nullptr, nullptr, nullptr, nullptr};
     const bool stats = as_bool(a[11]);
     const bool there[2] = {y.defined() && d.post_norm != 0, d.pre_norm != 0};
@@ -237,14 +260,20 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         st[i] = at.empty({T}, at::kFloat);
         sp[i] = st[i].data_ptr<float>();
       }
-    check(unif_moe_block_norm_forward(&d, px.p, px.ld, py.p, py.ld, mask, p.w_post, p.b_post, p.gate,
-                                      p.w_pre, b_pre, po.p, po.ld, pu.p, pu.ld, sp[0], sp[1], sp[2],
-                                      sp[3], at.stream()));
+    if (eight)
+      check(unif_moe_block_norm_forward_fp8(&d, px.p, px.ld, py.p, py.ld, mask, p.w_post, p.b_post, p.gate,
+                                            p.w_pre, b_pre, po.p, po.ld, static_cast<uint8_t*>(pu.p), pu.ld, su,
+                                            sp[0], sp[1], sp[2], sp[3], at.stream()));
+    else
+      check(unif_moe_block_norm_forward(&d, px.p, px.ld, py.p, py.ld, mask, p.w_post, p.b_post, p.gate,
+                                        p.w_pre, b_pre, po.p, po.ld, pu.p, pu.ld, sp[0], sp[1], sp[2],
+                                        sp[3], at.stream()));
     PyObject* r = PyDict_New();
     if (!r) throw Raised();
     try {
       put(r, "out", y.defined() ? out : x);
       put(r, "u", d.pre_norm ? u : Tensor());
+      if (eight) put(r, "u_scales", scales);
       static const char* names[4] = {"post_mean", "post_rstd", "pre_mean", "pre_rstd"};
       if (stats)
         for (int i = 0; i < 4; ++i) put(r, names[i], st[i]);
@@ -255,6 +284,8 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return r;
   });
 }
+PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) { return norm_forward_as(a, n, false); }
+PyObject* norm_forward_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) { return norm_forward_as(a, n, true); }
 
 // desc, out, y, (post_mean, post_rstd, pre_mean, pre_rstd), dout, du, post_weight, post_bias,
 // gate, pre_weight, mask, stream
@@ -477,6 +508,89 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Codes of rows in 8 bits, [...][cols] with dense rows at one distance from each other.
+Rows codes_of(const Place& at, const Tensor& t, const char* name, int64_t& rows, int64_t& cols) {
+  if (!t.defined() || t.scalar_type() != at::kFloat8_e4m3fn || t.dim() < 1)
+    value_error(std::string(name) + ": need a tensor of float8_e4m3fn");
+  at.on(t, name);
+  cols = t.size(-1);
+  if (cols < 1 || cols > UNIF_MOE_LINEAR_MAX_COLS || (cols > 1 && t.stride(-1) != 1))
+    value_error(std::string(name) + ": need dense rows, got " + shown(t));
+  rows = 1;
+  Rows r;
+  r.p = t.data_ptr();
+  r.ld = 0;
+  for (int64_t i = t.dim() - 2; i >= 0; --i) {
+    if (t.size(i) > 1) {
+      if (!r.ld) r.ld = t.stride(i) / std::max<int64_t>(rows, 1);
+      if (t.stride(i) != r.ld * rows) value_error(std::string(name) + ": need rows at one distance, got " + shown(t));
+    }
+    rows *= t.size(i);
+  }
+  if (rows <= 1 || !r.ld) r.ld = std::max(r.ld, cols);
+  return r;
+}
+
+// x, out codes, out scales (or None), stream
+PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> PyObject* {
+    const Tensor x = tensor(a[0], "x");
+    const Place at(x, "x", a[3]);
+    const int type = code(x.scalar_type());
+    if (type < 0 || x.dim() < 1) value_error("x: need rows of fp32 or bf16, got " + shown(x));
+    const int64_t cols = x.size(-1);
+    if (cols < 1 || cols > UNIF_MOE_LINEAR_MAX_COLS) value_error("x: " + std::to_string(cols) + " columns");
+    const int64_t rows = x.numel() / cols;
+    Rows px;
+    if (x.dim() == 2) {
+      px = rows_of(at, x, "x", rows, cols, x.scalar_type());
+    } else {
+      px.p = dense(at, x, "x", rows * cols, x.scalar_type());
+      px.ld = cols;
+    }
+    Tensor codes = tensor(a[1], "out.codes"), scales = tensor(a[2], "out.scales");
+    if (codes.defined() != scales.defined()) value_error("out: need codes and scales");
+    if (!codes.defined()) {
+      codes = empty_codes(at, x.sizes());
+      scales = at.empty(x.sizes().slice(0, x.dim() - 1), at::kFloat);
+    }
+    int64_t got = 0, wide = 0;
+    const Rows pc = codes_of(at, codes, "out.codes", got, wide);
+    if (got != rows || wide != cols)
+      value_error("out: need " + std::to_string(rows) + " rows of " + std::to_string(cols) + " columns");
+    check(unif_moe_fp8_quantize(px.p, (unif_moe_dtype)type, rows, (int)cols, px.ld, static_cast<uint8_t*>(pc.p),
+                                pc.ld, static_cast<float*>(dense(at, scales, "out.scales", rows, at::kFloat)),
+                                at.stream()));
+    return Py_BuildValue("(NN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales));
+  });
+}
+
+// codes, scales, dtype code, out, stream
+PyObject* fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const Tensor codes = tensor(a[0], "q.codes"), scales = tensor(a[1], "q.scales");
+    const Place at(codes, "q.codes", a[4]);
+    int64_t rows = 0, cols = 0;
+    const Rows pc = codes_of(at, codes, "q.codes", rows, cols);
+    if (!scales.defined()) value_error("q.scales: need a tensor");
+    const void* ps = dense(at, scales, "q.scales", rows, at::kFloat);
+    const long type = as_long(a[2]);
+    const at::ScalarType t = type_of(type, "dtype");
+    Tensor out = tensor(a[3], "out");
+    Rows po;
+    if (out.defined()) {
+      po = rows_of(at, out, "out", rows, cols, t);
+    } else {
+      out = at.empty(codes.sizes(), t);
+      po.p = out.data_ptr();
+      po.ld = cols;
+    }
+    check(unif_moe_fp8_dequantize(static_cast<const uint8_t*>(pc.p), pc.ld, static_cast<const float*>(ps), rows,
+                                  (int)cols, po.p, (unif_moe_dtype)type, po.ld, at.stream()));
+    return THPVariable_Wrap(out);
+  });
+}
+
 // Scales of rows or channels in 8 bits: fp32, one each.
 const float* scales_of(const Place& at, const Tensor& t, const char* name, int64_t count) {
   if (!t.defined()) value_error(std::string(name) + ": need a tensor");
@@ -618,7 +732,8 @@ PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define UNIF_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {UNIF_FAST(norm_forward), UNIF_FAST(norm_backward), UNIF_FAST(balance),
                          UNIF_FAST(quantize), UNIF_FAST(dequantize), UNIF_FAST(product),
-                         UNIF_FAST(linear), UNIF_FAST(linear_backward),
+                         UNIF_FAST(linear), UNIF_FAST(linear_backward), UNIF_FAST(norm_forward_fp8),
+                         UNIF_FAST(fp8_quantize), UNIF_FAST(fp8_dequantize),
                          UNIF_FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -18,6 +18,7 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include "fp8.cuh"
 #include "internal.cuh"
 
 namespace unif {
@@ -148,19 +149,58 @@ struct ForwardArgs {
   TX* out;
   TB* u;
   float *m_post, *r_post, *m_pre, *r_pre;
+  uint8_t* u8 = nullptr;     // u in 8 bits in the place of u, its rows ld_u bytes apart
+  float* u_scale = nullptr;  // [T]
 };
+
+// The largest of a value's bits over the threads of a row's group (as group_sum).
+template <int GL>
+__device__ __forceinline__ uint32_t group_max(uint32_t v, float* red, int& turn) {
+#pragma unroll
+  for (int o = (GL ? GL : 32) / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if (GL) return v;
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return v;
+  uint32_t* buf = reinterpret_cast<uint32_t*>(red + (turn & 1) * (2 * kMaxWarps));
+  turn ^= 1;
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  for (int w = 0; w < warps; ++w) v = max(v, buf[w]);
+  return v;
+}
+
+__device__ __forceinline__ uint32_t largest(const float (&v)[kE]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kE; ++i) most = max(most, fp8::magnitude(v[i]));
+  return most;
+}
+
+// Eight values as codes of 8 bits.
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, int j, int n, int d, const float (&v)[kE], float by) {
+  const uint2 q = fp8::codes8(v, by);
+  if (VEC) {
+    if (j * kE < d) *reinterpret_cast<uint2*>(p + j * kE) = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (i * n < d && column<false>(j, n, i) < d)
+        p[column<false>(j, n, i)] = (uint8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+  }
+}
 
 // One row to a group of threads. MT: most threads of a CTA; without VEC the threads, so
 // that the columns' offsets are constants (with an offset and a bound worked out per
 // value, a row of 333 took 1,850 instructions a warp in the backward). With VEC a thread keeps
 // to 32 registers (else 40), so that all 64 warps are on an SM (9,728 x 4,096 fp32 124 us with one CTA, 98
 // with two; bf16 parameters 8,192 wide 218 and 208). Not in groups of fp32 vectors, which would
-// spill (155,648 x 64 27.1 us, 28.2 so).
+// spill (155,648 x 64 27.1 us, 28.2 so). Q8: u as codes of 8 bits under a scale of its row.
 template <typename TB, bool VEC, int GL, int MT>
 constexpr int least_ctas() {
   return !VEC ? 1536 / MT : GL && sizeof(TB) == 4 ? 1 : 2048 / MT;
 }
-template <typename TX, typename TB, bool VEC, int GL, int MT>
+template <typename TX, typename TB, bool VEC, int GL, int MT, bool Q8>
 __global__ void __launch_bounds__(MT, least_ctas<TB, VEC, GL, MT>())
     forward_kernel(const ForwardArgs<TX, TB> a) {
   __shared__ float red[2 * 2 * kMaxWarps];
@@ -233,8 +273,18 @@ __global__ void __launch_bounds__(MT, least_ctas<TB, VEC, GL, MT>())
   }
   if (a.pre) {
     norm(o, a.pre, a.w_pre, a.b_pre);
+    if constexpr (Q8) {
+      float by = 1.f, scale = __uint_as_float(1u << 23);
+      uint32_t most = 0;
+      if (GL || valid) most = group_max<GL>(act ? largest(o) : 0u, red, turn);
+      if (valid) scale = fp8::row_scale(most, by);
+      if (in) {
+        store_codes<VEC>(a.u8 + row * a.ld_u, j, n, d, o, by);
+        if (j == 0) a.u_scale[row] = scale;
+      }
+    }
     if (in) {
-      store<VEC>(a.u + row * a.ld_u, j, n, d, o);
+      if constexpr (!Q8) store<VEC>(a.u + row * a.ld_u, j, n, d, o);
       if (j == 0) {
         if (a.m_pre) a.m_pre[row] = valid ? mean : 0.f;
         if (a.r_pre) a.r_pre[row] = valid ? rstd : 0.f;
@@ -898,7 +948,7 @@ __host__ __device__ constexpr int stream_steps() {  // of a ring of 320 bytes a 
   return 320 / (2 * kE * (int)(sizeof(TX) + sizeof(TB)));
 }
 
-template <typename TX, typename TB>
+template <typename TX, typename TB, bool Q8>
 __global__ void __launch_bounds__(kThreads, 4)
     forward_stream_kernel(const ForwardArgs<TX, TB> a, const int chunk) {
   constexpr int R = 2, W = kThreads / 32, kRing = stream_steps<TX, TB>();
@@ -1072,13 +1122,40 @@ __global__ void __launch_bounds__(kThreads, 4)
       }
       if (a.pre) {
         norm_rows(o, a.pre, w_pre, b_pre, a.b_pre, m2, r2);
+        if constexpr (Q8) {
+          uint32_t most[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-          if (valid >> r & 1u) {
+          for (int r = 0; r < R; ++r) {
             float t[kE];
             singles(o[r], t);
-            store<true>(a.u + row_of(here, r) * a.ld_u, j, n, d, t);
+            most[r] = __reduce_max_sync(0xffffffffu, act ? largest(t) : 0u);
           }
+          uint32_t* buf = reinterpret_cast<uint32_t*>(red + (turn & 1) * (2 * R * W));
+          turn ^= 1;
+          if ((threadIdx.x & 31) == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r) buf[(threadIdx.x >> 5) * R + r] = most[r];
+          __syncthreads();
+          const int warps = threads >> 5;
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            for (int w = 0; w < warps; ++w) most[r] = max(most[r], buf[w * R + r]);
+            if (!(valid >> r & 1u)) continue;
+            float t[kE], by;
+            singles(o[r], t);
+            const float scale = fp8::row_scale(most[r], by);
+            store_codes<true>(a.u8 + row_of(here, r) * a.ld_u, j, n, d, t, by);
+            if (j == 0) a.u_scale[row_of(here, r)] = scale;
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (valid >> r & 1u) {
+              float t[kE];
+              singles(o[r], t);
+              store<true>(a.u + row_of(here, r) * a.ld_u, j, n, d, t);
+            }
+        }
       }
     }
 #pragma unroll
@@ -1091,7 +1168,12 @@ __global__ void __launch_bounds__(kThreads, 4)
 #pragma unroll
         for (int i = 0; i < kE; ++i) t[i] = 0.f;
         if (a.y && a.out) store<true>(a.out + row * a.ld_out, j, n, d, t);
-        if (a.pre) store<true>(a.u + row * a.ld_u, j, n, d, t);
+        if constexpr (Q8) {
+          store_codes<true>(a.u8 + row * a.ld_u, j, n, d, t, 1.f);
+          if (j == 0) a.u_scale[row] = __uint_as_float(1u << 23);
+        } else if (a.pre) {
+          store<true>(a.u + row * a.ld_u, j, n, d, t);
+        }
       }
       if (j == 0) {
         if (a.y && a.post) {
@@ -1198,17 +1280,17 @@ bool vec_ok(const T* p, long long ld) {
   return reinterpret_cast<uintptr_t>(p) % (kE * sizeof(T)) == 0 && ld % kE == 0;
 }
 
-template <typename TX, typename TB>
+template <typename TX, typename TB, bool Q8>
 cudaError_t launch_stream(const ForwardArgs<TX, TB>& a, int threads, int sms, cudaStream_t s) {
   const int smem = stream_steps<TX, TB>() * 2 * kE * (int)(sizeof(TX) + sizeof(TB)) * threads;
   constexpr int chunk = 4;  // two steps
   const long long chunks = ((long long)a.T + chunk - 1) / chunk;
   const int most = sms * (512 / threads);
-  forward_stream_kernel<TX, TB><<<(unsigned)(chunks < most ? chunks : most), threads, smem, s>>>(a, chunk);
+  forward_stream_kernel<TX, TB, Q8><<<(unsigned)(chunks < most ? chunks : most), threads, smem, s>>>(a, chunk);
   return cudaGetLastError();
 }
 
-template <typename TX, typename TB, bool VEC>
+template <typename TX, typename TB, bool VEC, bool Q8>
 cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, int sms, cudaStream_t s) {
   const int threads = cta_threads(a.d);
   // A bf16 stream of 257 to 1,024 columns: forward_stream_kernel once every SM has 16
@@ -1220,19 +1302,19 @@ cudaError_t launch_fwd(const ForwardArgs<TX, TB>& a, int sms, cudaStream_t s) {
   // over bf16 23.6 and 27.4.
   if constexpr (VEC && sizeof(TX) == 2)
     if (!group_lanes(a.d) && threads <= kThreads && a.T >= 16ll * sms)
-      return launch_stream(a, threads, sms, s);
+      return launch_stream<TX, TB, Q8>(a, threads, sms, s);
   switch (group_lanes(a.d)) {
-    case 8: forward_kernel<TX, TB, VEC, 8, kThreads><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
-    case 16: forward_kernel<TX, TB, VEC, 16, kThreads><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
-    case 32: forward_kernel<TX, TB, VEC, 32, kThreads><<<(a.T + 3) / 4, threads, 0, s>>>(a); break;
+    case 8: forward_kernel<TX, TB, VEC, 8, kThreads, Q8><<<(a.T + 15) / 16, threads, 0, s>>>(a); break;
+    case 16: forward_kernel<TX, TB, VEC, 16, kThreads, Q8><<<(a.T + 7) / 8, threads, 0, s>>>(a); break;
+    case 32: forward_kernel<TX, TB, VEC, 32, kThreads, Q8><<<(a.T + 3) / 4, threads, 0, s>>>(a); break;
     default:
-      if (VEC) forward_kernel<TX, TB, true, 0, 1024><<<a.T, threads, 0, s>>>(a);
-      else if (threads <= 64) forward_kernel<TX, TB, false, 0, 64><<<a.T, 64, 0, s>>>(a);
-      else if (threads <= 128) forward_kernel<TX, TB, false, 0, 128><<<a.T, 128, 0, s>>>(a);
-      else if (threads <= 256) forward_kernel<TX, TB, false, 0, 256><<<a.T, 256, 0, s>>>(a);
-      else if (threads <= 384) forward_kernel<TX, TB, false, 0, 384><<<a.T, 384, 0, s>>>(a);
-      else if (threads <= 512) forward_kernel<TX, TB, false, 0, 512><<<a.T, 512, 0, s>>>(a);
-      else forward_kernel<TX, TB, false, 0, 1024><<<a.T, 1024, 0, s>>>(a);
+      if (VEC) forward_kernel<TX, TB, true, 0, 1024, Q8><<<a.T, threads, 0, s>>>(a);
+      else if (threads <= 64) forward_kernel<TX, TB, false, 0, 64, Q8><<<a.T, 64, 0, s>>>(a);
+      else if (threads <= 128) forward_kernel<TX, TB, false, 0, 128, Q8><<<a.T, 128, 0, s>>>(a);
+      else if (threads <= 256) forward_kernel<TX, TB, false, 0, 256, Q8><<<a.T, 256, 0, s>>>(a);
+      else if (threads <= 384) forward_kernel<TX, TB, false, 0, 384, Q8><<<a.T, 384, 0, s>>>(a);
+      else if (threads <= 512) forward_kernel<TX, TB, false, 0, 512, Q8><<<a.T, 512, 0, s>>>(a);
+      else forward_kernel<TX, TB, false, 0, 1024, Q8><<<a.T, 1024, 0, s>>>(a);
       break;
   }
   return cudaGetLastError();
@@ -1309,7 +1391,7 @@ cudaError_t forward_as(const unif_moe_block_norm* p, int sms, const void* x, lon
                        long long ld_y, const uint8_t* mask, const void* w_post, const void* b_post,
                        const void* gate, const void* w_pre, const void* b_pre, void* out,
                        long long ld_out, void* u, long long ld_u, float* m_post, float* r_post,
-                       float* m_pre, float* r_pre, cudaStream_t s) {
+                       float* m_pre, float* r_pre, float* u_scale, cudaStream_t s) {
   ForwardArgs<TX, TB> a{p->tokens, p->width, p->post_norm, p->pre_norm, p->gate_rows,
                         p->res_scale, p->eps,
                         static_cast<const TX*>(x), static_cast<const TB*>(y),
@@ -1319,10 +1401,18 @@ cudaError_t forward_as(const unif_moe_block_norm* p, int sms, const void* x, lon
                         static_cast<const TB*>(b_pre), static_cast<TX*>(out),
                         static_cast<TB*>(u), m_post, r_post, m_pre, r_pre};
   const bool vec = p->width % kE == 0 && vec_ok(a.x, ld_x) && (!y || vec_ok(a.y, ld_y)) &&
-                   (!out || vec_ok(a.out, ld_out)) && (!u || vec_ok(a.u, ld_u)) &&
+                   (!out || vec_ok(a.out, ld_out)) &&
                    vec_ok(a.w_post, 0) && vec_ok(a.b_post, 0) && vec_ok(a.gate, 0) &&
                    vec_ok(a.w_pre, 0) && vec_ok(a.b_pre, 0);
-  return vec ? launch_fwd<TX, TB, true>(a, sms, s) : launch_fwd<TX, TB, false>(a, sms, s);
+  if (u_scale) {
+    a.u8 = static_cast<uint8_t*>(u);
+    a.u_scale = u_scale;
+    a.u = nullptr;
+    return vec && vec_ok(a.u8, ld_u) ? launch_fwd<TX, TB, true, true>(a, sms, s)
+                                     : launch_fwd<TX, TB, false, true>(a, sms, s);
+  }
+  return vec && (!u || vec_ok(a.u, ld_u)) ? launch_fwd<TX, TB, true, false>(a, sms, s)
+                                          : launch_fwd<TX, TB, false, false>(a, sms, s);
 }
 
 int64_t workspace_floats(const Plan& pl, int d) {
@@ -1380,12 +1470,11 @@ namespace nm = unif::norm;
 
 extern "C" {
 
-int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
-                                const void* y, int64_t ld_y, const uint8_t* mask,
-                                const void* w_post, const void* b_post, const void* gate,
-                                const void* w_pre, const void* b_pre, void* out, int64_t ld_out,
-                                void* u, int64_t ld_u, float* m_post, float* r_post, float* m_pre,
-                                float* r_pre, void* stream) {
+static int norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
+                        const void* y, int64_t ld_y, const uint8_t* mask,
+                        const void* w_post, const void* b_post, const void* gate, const void* w_pre,
+                        const void* b_pre, void* out, int64_t ld_out, void* u, int64_t ld_u,
+                        float* m_post, float* r_post, float* m_pre, float* r_pre, float* u_scale, void* stream) {
   set_error("%s", "");
   const int rc = nm::check_desc(p);
   if (rc != UNIF_MOE_OK) return rc;
@@ -1413,7 +1502,7 @@ int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
 #define UNIF_ARGS p, sms, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u, \
-                  ld_u, m_post, r_post, m_pre, r_pre, s
+                  ld_u, m_post, r_post, m_pre, r_pre, u_scale, s
   if (p->branch_dtype == UNIF_MOE_F32) e = nm::forward_as<float, float>(UNIF_ARGS);
   else if (p->stream_dtype == UNIF_MOE_F32) e = nm::forward_as<float, __nv_bfloat16>(UNIF_ARGS);
   else e = nm::forward_as<__nv_bfloat16, __nv_bfloat16>(UNIF_ARGS);
@@ -1423,6 +1512,31 @@ int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int
     return UNIF_MOE_ERR_CUDA;
   }
   return UNIF_MOE_OK;
+}
+
+int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
+                                const void* y, int64_t ld_y, const uint8_t* mask,
+                                const void* w_post, const void* b_post, const void* gate,
+                                const void* w_pre, const void* b_pre, void* out, int64_t ld_out,
+                                void* u, int64_t ld_u, float* m_post, float* r_post, float* m_pre,
+                                float* r_pre, void* stream) {
+  return norm_forward(p, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u, ld_u,
+                      m_post, r_post, m_pre, r_pre, nullptr, stream);
+}
+
+int unif_moe_block_norm_forward_fp8(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
+                                    const void* y, int64_t ld_y, const uint8_t* mask,
+                                    const void* w_post, const void* b_post, const void* gate,
+                                    const void* w_pre, const void* b_pre, void* out, int64_t ld_out,
+                                    uint8_t* u_codes, int64_t ld_u, float* u_scales, float* m_post,
+                                    float* r_post, float* m_pre, float* r_pre, void* stream) {
+  set_error("%s", "");
+  if (p && p->tokens != 0 && (!p->pre_norm || !u_scales)) {
+    set_error("u in 8 bits needs a pre norm and scales");
+    return UNIF_MOE_ERR_ARG;
+  }
+  return norm_forward(p, x, ld_x, y, ld_y, mask, w_post, b_post, gate, w_pre, b_pre, out, ld_out, u_codes,
+                      ld_u, m_post, r_post, m_pre, r_pre, u_scales, stream);
 }
 
 int64_t unif_moe_block_norm_workspace(const unif_moe_block_norm* p, int gate) {

@@ -23,7 +23,8 @@ from typing import NamedTuple, Optional
 import torch
 
 __all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize",
-           "mxfp4_product", "mxfp4_status", "Fp8", "linear", "linear_backward", "linear_status"]
+           "mxfp4_product", "mxfp4_status", "Fp8", "fp8_quantize",
+           "fp8_dequantize", "linear", "linear_backward", "linear_status"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
@@ -53,6 +54,7 @@ class _LinearGrad(C.Structure):
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
            "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss",
            "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize", "unif_moe_mxfp4_product",
+           "unif_moe_block_norm_forward_fp8", "unif_moe_fp8_quantize", "unif_moe_fp8_dequantize",
            "unif_moe_linear_workspace", "unif_moe_linear_forward",
            "unif_moe_linear_backward_workspace", "unif_moe_linear_backward"]
 
@@ -72,6 +74,10 @@ def declare(L: C.CDLL) -> None:
     L.unif_moe_mxfp4_quantize.argtypes = [P, I, I64, I, I64, P, P, P]
     L.unif_moe_mxfp4_dequantize.argtypes = [P, P, I64, I, P, I, I64, P]
     L.unif_moe_mxfp4_product.argtypes = [P, P, I64, I, P, P, I, I, P, I, P, I, I64, P, P]
+    L.unif_moe_block_norm_forward_fp8.argtypes = ([D, P, I64, P, I64] + [P] * 6 + [P, I64, P, I64, P]
+                                                  + [P] * 5)
+    L.unif_moe_fp8_quantize.argtypes = [P, I, I64, I, I64, P, I64, P, P]
+    L.unif_moe_fp8_dequantize.argtypes = [P, I64, P, I64, I, P, I, I64, P]
     Q, G = C.POINTER(_LinearDesc), C.POINTER(_LinearGrad)
     L.unif_moe_linear_workspace.argtypes = [Q, P, I64, P, I64]
     L.unif_moe_linear_forward.argtypes = ([Q, P, I64, P, P, I64, P, P, P, I64, P, P, I64, P, I64, P, I64,
@@ -114,11 +120,15 @@ class BlockNorm:
     all parameters: branch_dtype. post_norm and pre_norm: "none", "layer" or
     "rms". gate_rows consecutive tokens share a row of the gate (0: all of them).
     Rows of the tensors may be strided; masked rows (mask 0) are not read and
-    give 0."""
+    give 0. u_format "fp8": u in 8 bits (an Fp8, from the unrounded sum), for linear;
+    the backward is the same, as if nothing had been rounded."""
 
     def __init__(self, width: int, stream_dtype: str = "bf16", branch_dtype: str = "bf16",
                  post_norm: str = "none", pre_norm: str = "rms", gate_rows: int = 0,
-                 res_scale: float = 1.0, eps: float = 1e-6):
+                 res_scale: float = 1.0, eps: float = 1e-6, u_format: str = "branch"):
+        if u_format not in ("branch", "fp8"):
+            raise ValueError("u_format: %r (branch or fp8)" % (u_format,))
+        self.eight = u_format == "fp8"
         self.width, self.gate_rows = width, gate_rows
         self.post, self.pre = _NORMS[post_norm], _NORMS[pre_norm]
         self._desc = (width, _CODES[DTYPES[stream_dtype]], _CODES[DTYPES[branch_dtype]], self.post,
@@ -129,12 +139,18 @@ class BlockNorm:
                 post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                 pre_weight: Optional[torch.Tensor] = None,
                 pre_bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
-                out: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, u=None,
                 stats: bool = False, stream=None) -> dict:
         """dict of out (x itself without y), u (None without pre norm) and, where
         `stats` asks for them, the statistics post_mean, post_rstd, pre_mean,
         pre_rstd [T] that backward takes (None for a norm that is not there; means of
         an rms norm are 0). Without y: the norm before a stack's first block."""
+        if self.eight:
+            codes, scales = (None, None) if u is None else (u.codes, u.scales)
+            r = _b().norm_forward_fp8(self._desc, x, y, post_weight, post_bias, gate, pre_weight,
+                                      pre_bias, mask, out, codes, stats, stream, scales)
+            r["u"] = Fp8(r["u"], r.pop("u_scales"))
+            return r
         return _b().norm_forward(self._desc, x, y, post_weight, post_bias, gate, pre_weight,
                                  pre_bias, mask, out, u, stats, stream)
 
@@ -249,6 +265,23 @@ class Fp8(NamedTuple):
     strided), scales [...] fp32, contiguous."""
     codes: torch.Tensor
     scales: torch.Tensor
+
+
+def fp8_quantize(x: torch.Tensor, out: Optional[Fp8] = None, stream=None) -> Fp8:
+    """Rows x [...][cols] (fp32 or bf16; a 2-d x may have strided rows) to 8 bits: a row's scale is
+    2^e, the smallest for which no value is above 448 2^e, codes round to nearest even. New
+    codes have rows a multiple of 16 bytes apart, which linear reads as they are."""
+    if out is None:
+        return Fp8(*_b().fp8_quantize(x, None, None, stream))
+    _b().fp8_quantize(x, out.codes, out.scales, stream)
+    return out
+
+
+def fp8_dequantize(q: Fp8, dtype: str = "bf16", out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The values of rows in 8 bits, [...][cols] ("bf16" or "f32"); an out [rows][cols] may
+    have strided rows."""
+    return _b().fp8_dequantize(q.codes, q.scales, _CODES[DTYPES[dtype]], out, stream)
 
 
 def _status_of(x):
