@@ -596,6 +596,56 @@ UNIF_MOE_API int unif_moe_mxfp4_product(const uint8_t* a_codes_dev, const uint8_
                                         unif_moe_dtype dtype, int64_t ld, int32_t* status_dev,
                                         void* stream);
 
+/* ---- The layer for a few tokens ----
+ * A bf16 layer's forward (Eqs. 17-30) of up to UNIF_MOE_FEW_TOKENS tokens, as a server takes them
+ * one step after another: two kernels (three above 8 tokens) that read the weights of each
+ * (expert, block) pair in use once. Decisions are those of unif_moe_forward but for near-ties (the
+ * logits' sums have another order); h and y are rounded as there, h after its weight. No atomics:
+ * results repeat bit for bit. */
+#define UNIF_MOE_FEW_TOKENS 64
+
+typedef struct {
+  int tokens;                               /* 0 <= T <= UNIF_MOE_FEW_TOKENS */
+  int d_model, d_ff, n_experts, n_blocks;   /* limits of a bf16 unif_moe_create */
+  unif_moe_thresholds th;
+} unif_moe_few;
+
+/* The router's rows for unif_moe_few_forward, made once for a layer's weights: table_dev
+ * [1 + K + B][d] bf16 = W_shr, W_g, then mu_b, the mean key of each block of the shared expert
+ * (Eq. 20; fp64 sums, rounded once), from w_router_dev [d][K+1] and w_up_dev as
+ * unif_moe_load_weights takes them. Enqueued on `stream`, no sync. */
+UNIF_MOE_API int unif_moe_router_table(int d_model, int d_ff, int n_experts, int n_blocks,
+                                       const void* w_router_dev, const void* w_up_dev,
+                                       void* table_dev, void* stream);
+
+/* Bytes of device workspace of unif_moe_few_forward; -1 on a bad description. */
+UNIF_MOE_API int64_t unif_moe_few_workspace(const unif_moe_few* p);
+
+/* The forward from the caller's weights, without a handle; no state between calls.
+ *   x_dev [T][d], out_dev [T][d] bf16, rows ld apart (x: multiples of 16 bytes)
+ *   router_dev as unif_moe_router_table gives it; router_bias_dev [K+1] float or NULL
+ *   w_up_dev [K+1][H][d], w_down_dev [K+1][d][H] bf16, 32-byte aligned
+ *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose rows are not used and give 0
+ *   shared_counts_dev, residual_counts_dev [T] int32 or NULL: b(x) and k(x), 0 for padding
+ *   workspace_dev: of one call at a time
+ * out may be x, with its stride. Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE, ERR_CAPACITY (T above
+ * UNIF_MOE_FEW_TOKENS, workspace), ERR_CUDA. */
+UNIF_MOE_API int unif_moe_few_forward(const unif_moe_few* p, const void* x_dev, int64_t ld_x,
+                                      const void* router_dev, const float* router_bias_dev,
+                                      const void* w_up_dev, const void* w_down_dev,
+                                      const uint8_t* token_mask_dev, void* out_dev, int64_t ld_out,
+                                      int32_t* shared_counts_dev, int32_t* residual_counts_dev,
+                                      void* workspace_dev, int64_t workspace_bytes, void* stream);
+
+/* The same with the weights and thresholds of a bf16 layer (T also above its max_tokens). The
+ * handle is only read: the records of its last forward stay, and calls with workspaces of their own
+ * may overlap. Errors as above, and ERR_STATE (no weights), ERR_SHAPE (an fp32 layer). */
+UNIF_MOE_API int64_t unif_moe_forward_few_workspace(unif_moe_t h, int T);
+UNIF_MOE_API int unif_moe_forward_few(unif_moe_t h, const void* x_dev, int64_t ld_x, int T,
+                                      const uint8_t* token_mask_dev, void* out_dev, int64_t ld_out,
+                                      int32_t* shared_counts_dev, int32_t* residual_counts_dev,
+                                      void* workspace_dev, int64_t workspace_bytes, void* stream);
+
 /* Rows to 8-bit floating point (E4M3: sign, four exponent bits, three mantissa bits, values
  * up to 448) under a scale each: the scale of a row is 2^e with the smallest e, at least -126, for
  * which no value is above 448 2^e (2^-126 for a row of zeros), a code x 2^-e rounded to nearest

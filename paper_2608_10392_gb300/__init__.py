@@ -20,16 +20,17 @@ from typing import Optional
 import torch
 
 from . import operators as _operators
-from .operators import (BlockNorm, Fp8, Mxfp4, balance_loss, fp8_dequantize, fp8_quantize, linear, linear_backward,
-                        linear_status, mxfp4_dequantize, mxfp4_product, mxfp4_quantize,
-                        mxfp4_status)
+from .operators import (FEW_TOKENS, BlockNorm, Fp8, Mxfp4, balance_loss, few_tokens,
+                        fp8_dequantize, fp8_quantize, linear, linear_backward, linear_status,
+                        mxfp4_dequantize, mxfp4_product, mxfp4_quantize, mxfp4_status,
+                        router_table)
 
 __all__ = ["Layer", "lib", "UnifMoeError", "ERR", "EXPORTS", "Options", "FEATURE_NORM_FIRST",
            "FEATURE_HOST_IO", "FEATURE_BACKWARD", "FEATURE_DIAGNOSTICS", "FEATURES_DEFAULT",
            "FEATURES_ALL", "BlockNorm", "balance_loss", "Mxfp4",
            "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_product", "mxfp4_status", "Fp8",
-           "fp8_quantize", "fp8_dequantize", "linear",
-           "linear_backward", "linear_status"]
+           "fp8_quantize", "fp8_dequantize", "linear", "linear_backward",
+           "linear_status", "router_table", "few_tokens", "FEW_TOKENS"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libunif_moe.so")
@@ -229,6 +230,16 @@ class Layer:
                                       _stream(stream)))
         self.last_T = T
         return out
+
+    def forward_few(self, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+                    mask: Optional[torch.Tensor] = None,
+                    shared_counts: Optional[torch.Tensor] = None,
+                    residual_counts: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """forward for up to FEW_TOKENS tokens (bf16 layers), in two or three kernels that read
+        each weight in use once; x and out may have strided rows. It leaves the records of the last
+        forward (routing, groups, what backward needs) as they are."""
+        return _operators._b().forward_few(self._h.value, self.d, x, mask, shared_counts,
+                                           residual_counts, out, stream)
 
     def backward(self, x: torch.Tensor, dy: torch.Tensor, mask: Optional[torch.Tensor] = None,
                  lambda_div: float = 0.0, want_bias: bool = False, out: Optional[dict] = None,

@@ -24,7 +24,7 @@ BINDING = os.path.join(LIBDIR, "_binding.so")
 SOURCES = ["unif_moe.cu", "route_permute.cu", "gemm_simt.cu", "gemm_tc.cu", "gemm_ws.cu",
            "backward.cu", "diagnostics.cu", "gemm_fused.cu", "gemm_pair.cu",
            "bundles.cu", "block_norm.cu", "balance.cu", "mxfp4.cu",
-           "fp4_product.cu", "linear.cu", "fp8.cu"]
+           "fp4_product.cu", "linear.cu", "fp8.cu", "few.cu"]
 HEADERS = ["internal.cuh", "decide.cuh", "items.cuh", "tc_common.cuh", "per_device.h", "gelu_log.cuh",
            "fp8.cuh",
            os.path.join("..", "..", "include", "unif_moe.h")]

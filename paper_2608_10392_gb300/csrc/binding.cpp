@@ -720,6 +720,104 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+int32_t* counts_of(const Place& at, PyObject* o, const char* name, int64_t T) {
+  return static_cast<int32_t*>(dense(at, tensor(o, name), name, T, at::kInt));
+}
+
+// w_router, w_up, n_blocks, stream
+PyObject* router_table(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> PyObject* {
+    const Tensor wr = tensor(a[0], "w_router"), up = tensor(a[1], "w_up");
+    const Place at(up, "w_up", a[3]);
+    if (up.dim() != 3) value_error("w_up: need [K + 1][H][d], got " + shown(up));
+    const int64_t E = up.size(0), H = up.size(1), d = up.size(2);
+    const int B = as_int(a[2]);
+    if (E < 2 || E > 65 || H > 0x7fffffff || d > 0x7fffffff || B < 2 || B > 64)
+      value_error("bad sizes: w_up " + shown(up) + ", " + std::to_string(B) + " blocks");
+    const void* pu = dense(at, up, "w_up", E * H * d, at::kBFloat16);
+    if (!wr.defined()) value_error("w_router: need a tensor");
+    const void* pr = dense(at, wr, "w_router", d * E, at::kBFloat16);
+    const Tensor table = at.empty({E + B, d}, at::kBFloat16);
+    check(unif_moe_router_table((int)d, (int)H, (int)E - 1, B, pr, pu, table.data_ptr(), at.stream()));
+    return THPVariable_Wrap(table);
+  });
+}
+
+// A token's rows of the few-token calls: 64 at most, so that T fits everything.
+struct FewRows {
+  int T = 0, d = 0;
+  Rows x, out;
+  Tensor to;
+};
+FewRows few_rows(const Place& at, const Tensor& x, PyObject* out) {
+  FewRows r;
+  if (x.dim() != 2 || x.size(0) > 0x7fffffff || x.size(1) > 0x7fffffff) value_error("x: need [T][d], got " + shown(x));
+  r.T = (int)x.size(0);
+  r.d = (int)x.size(1);
+  r.x = rows_of(at, x, "x", r.T, r.d, at::kBFloat16);
+  r.to = tensor(out, "out");
+  if (!r.to.defined()) r.to = at.empty({r.T, r.d}, at::kBFloat16);
+  r.out = rows_of(at, r.to, "out", r.T, r.d, at::kBFloat16);
+  return r;
+}
+
+// x, router, w_up, w_down, n_blocks, router_bias, mask, (tau, alpha, beta, topk, prefix), shared_counts,
+// residual_counts, out, stream
+PyObject* few_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&]() -> PyObject* {
+    const Tensor x = tensor(a[0], "x"), router = tensor(a[1], "router"), up = tensor(a[2], "w_up"),
+                 down = tensor(a[3], "w_down");
+    const Place at(x, "x", a[11]);
+    const FewRows r = few_rows(at, x, a[10]);
+    if (!up.defined() || up.dim() != 3 || up.size(2) != r.d) value_error("w_up: need [K + 1][H][d]");
+    if (!router.defined() || !down.defined()) value_error("router and w_down: need tensors");
+    const int64_t E = up.size(0), H = up.size(1);
+    const int B = as_int(a[4]);
+    if (E < 2 || E > 65 || H > 0x7fffffff || B < 2 || B > 64)
+      value_error("bad sizes: w_up " + shown(up) + ", " + std::to_string(B) + " blocks");
+    unif_moe_few d{r.T, r.d, (int)H, (int)E - 1, B, {}};
+    if (!PyTuple_Check(a[7]) || PyTuple_GET_SIZE(a[7]) != 5) value_error("bad thresholds");
+    d.th.tau = (float)as_double(PyTuple_GET_ITEM(a[7], 0));
+    d.th.alpha_fixed = (float)as_double(PyTuple_GET_ITEM(a[7], 1));
+    d.th.beta_fixed = (float)as_double(PyTuple_GET_ITEM(a[7], 2));
+    d.th.topk_fixed = as_int(PyTuple_GET_ITEM(a[7], 3));
+    d.th.prefix_blocks = as_bool(PyTuple_GET_ITEM(a[7], 4));
+    const void *pr = dense(at, router, "router", (E + B) * r.d, at::kBFloat16),
+               *pu = dense(at, up, "w_up", E * H * r.d, at::kBFloat16),
+               *pd = dense(at, down, "w_down", E * H * r.d, at::kBFloat16);
+    const float* bias = static_cast<const float*>(dense(at, tensor(a[5], "router_bias"), "router_bias", E, at::kFloat));
+    const uint8_t* mask = mask_of(at, tensor(a[6], "mask"), r.T);
+    int32_t *bc = counts_of(at, a[8], "shared_counts", r.T), *kc = counts_of(at, a[9], "residual_counts", r.T);
+    const int64_t need = unif_moe_few_workspace(&d);
+    if (need < 0) check(r.T > UNIF_MOE_FEW_TOKENS ? UNIF_MOE_ERR_CAPACITY : UNIF_MOE_ERR_ARG);
+    const Tensor ws = at.empty({need}, at::kByte);
+    check(unif_moe_few_forward(&d, r.x.p, r.x.ld, pr, bias, pu, pd, mask, r.out.p, r.out.ld, bc, kc, ws.data_ptr(),
+                               need, at.stream()));
+    return THPVariable_Wrap(r.to);
+  });
+}
+
+// handle, d, x, mask, shared_counts, residual_counts, out, stream
+PyObject* forward_few(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    void* h = PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) throw Raised();
+    const Tensor x = tensor(a[2], "x");
+    const Place at(x, "x", a[7]);
+    const FewRows r = few_rows(at, x, a[6]);
+    if (r.d != as_long(a[1])) value_error("x: need rows of " + std::to_string(as_long(a[1])) + ", got " + shown(x));
+    const uint8_t* mask = mask_of(at, tensor(a[3], "mask"), r.T);
+    int32_t *bc = counts_of(at, a[4], "shared_counts", r.T), *kc = counts_of(at, a[5], "residual_counts", r.T);
+    const int64_t need = unif_moe_forward_few_workspace(static_cast<unif_moe_t>(h), r.T);
+    Tensor ws;
+    if (need > 0) ws = at.empty({need}, at::kByte);
+    // (where there is none, the call says why)
+    check(unif_moe_forward_few(static_cast<unif_moe_t>(h), r.x.p, r.x.ld, r.T, mask, r.out.p, r.out.ld, bc, kc,
+                               need > 0 ? ws.data_ptr() : nullptr, need, at.stream()));
+    return THPVariable_Wrap(r.to);
+  });
+}
+
 // The classes that failed calls and failed allocations raise; before any other call.
 PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject* {
@@ -733,7 +831,8 @@ PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {UNIF_FAST(norm_forward), UNIF_FAST(norm_backward), UNIF_FAST(balance),
                          UNIF_FAST(quantize), UNIF_FAST(dequantize), UNIF_FAST(product),
                          UNIF_FAST(linear), UNIF_FAST(linear_backward), UNIF_FAST(norm_forward_fp8),
-                         UNIF_FAST(fp8_quantize), UNIF_FAST(fp8_dequantize),
+                         UNIF_FAST(fp8_quantize), UNIF_FAST(fp8_dequantize), UNIF_FAST(router_table),
+                         UNIF_FAST(few_tokens), UNIF_FAST(forward_few),
                          UNIF_FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,792 @@
+// The whole layer for a few tokens (unif_moe_few_forward, unif_moe_forward_few): decisions,
+// h = w GeLU(x K_e[:, H_b]) and y = sum h V_e[H_b, :] over the (expert, block) pairs that some
+// token runs, in two kernels (three above 8 tokens).
+//
+// Bound by the weights' bytes: those of a pair are read once, whichever and however many tokens
+// run it, and nothing else is large. No tiles of 128 rows are laid out for a token or two, no
+// group table, no fp32 accumulator and no atomics: results repeat bit for bit.
+//
+// - up_kernel: every CTA takes the tokens' decisions for itself (up to 8 tokens; more are
+//   decided by route_kernel, a CTA a token), lists the pairs in use, and its warps take tiles of
+//   16 keys of a pair: x and keys go from memory to mma.sync fragments, a thread's 32
+//   bytes standing for other features than the fragment's, the same ones for both operands. The
+//   tokens of a pair are gathered: columns of the product are those that run it.
+// - down_kernel: a cluster of CTAs takes 16 or 32 output features, its warps chunks of 64 channels
+//   of the pairs in use in turn; the warps' sums meet in shared memory, the CTAs' in the cluster's,
+//   added in a fixed order.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "gelu_log.cuh"
+#include "internal.cuh"
+
+namespace unif {
+namespace few {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMost = UNIF_MOE_FEW_TOKENS;
+constexpr int kTogether = 8;  // most tokens that every CTA decides for itself
+
+struct Params {
+  int T, d, H, K, B, M, C;        // C = 1 + K + B: rows of the router
+  float tau, alpha_fixed, beta_fixed;
+  int topk_fixed, prefix;
+  const __nv_bfloat16* x;
+  long long ld_x;
+  const __nv_bfloat16* router;    // [C][d]
+  const float* bias;              // [K + 1] or NULL
+  const __nv_bfloat16 *up, *down; // [K + 1][H][d], [K + 1][d][H]
+  const uint8_t* mask;
+  __nv_bfloat16* out;
+  long long ld_out;
+  int32_t *b_out, *k_out;
+  // workspace
+  uint64_t *shr, *em;             // [T] blocks of the shared expert, residual experts
+  float* alpha;                   // [T]
+  float* s;                       // [T][K] affinities
+  int* n_pairs;                   // pairs in use, in the order of (expert, block)
+  uint16_t* pair;                 // [G]
+  uint64_t* members;              // [G] tokens of each
+  __nv_bfloat16* h;               // [K + 1][T][H], of the pairs' tokens
+};
+
+// Thirty-two bytes: sixteen bf16 values as eight operand registers.
+struct Piece {
+  uint32_t r[8];
+};
+__device__ __forceinline__ void clear(Piece& p) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p.r[i] = 0u;
+}
+// Weights: read once, kept out of the way of x in L1 (32-byte aligned).
+__device__ __forceinline__ void read_weights(Piece& p, const __nv_bfloat16* from) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(p.r[0]), "=r"(p.r[1]), "=r"(p.r[2]), "=r"(p.r[3]), "=r"(p.r[4]), "=r"(p.r[5]), "=r"(p.r[6]),
+                 "=r"(p.r[7])
+               : "l"(from));
+}
+// Tokens (16-byte aligned).
+__device__ __forceinline__ void read_token(Piece& p, const __nv_bfloat16* from) {
+  const uint4 a = *reinterpret_cast<const uint4*>(from), b = *(reinterpret_cast<const uint4*>(from) + 1);
+  p.r[0] = a.x; p.r[1] = a.y; p.r[2] = a.z; p.r[3] = a.w;
+  p.r[4] = b.x; p.r[5] = b.y; p.r[6] = b.z; p.r[7] = b.w;
+}
+// c += rows (g: lo, g + 8: hi) x columns (token g) over 64 features of four threads.
+__device__ __forceinline__ void multiply(float (&c)[4], const Piece& lo, const Piece& hi, const Piece& x) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+        " {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(lo.r[i]), "r"(hi.r[i]), "r"(lo.r[i + 1]), "r"(hi.r[i + 1]), "r"(x.r[i]), "r"(x.r[i + 1]));
+}
+
+// ---- decisions ----
+
+// Those of token t by one warp, from its row z of the router's product (Eqs. 18-27): the orders
+// are ranks (larger first, ties to the lower index), as in decide.cuh. Each lane holds
+// entries lane and lane + 32 of the experts and of the blocks.
+__device__ __forceinline__ void decide(const Params& p, int t, bool valid, const float* z, int lane, uint64_t& shr,
+                                       uint64_t& em, float& alpha, float* s, int& count, int& taken) {
+  const int K = p.K, B = p.B;
+  shr = em = 0ull;
+  alpha = 0.f;
+  count = taken = 0;
+  float l[2], e[2], u[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int j = lane + 32 * i;
+    l[i] = valid && j < K ? z[1 + j] + (p.bias ? p.bias[1 + j] : 0.f) : -INFINITY;
+    u[i] = valid && j < B ? z[1 + K + j] : -INFINITY;
+  }
+  if (valid) {
+    float most = fmaxf(l[0], l[1]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float den = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      e[i] = lane + 32 * i < K ? expf(l[i] - most) : 0.f;
+      den += e[i];
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+    const float z0 = z[0] + (p.bias ? p.bias[0] : 0.f);
+    alpha = isnan(p.alpha_fixed) ? p.tau + (1.f - 2.f * p.tau) * (1.f / (1.f + expf(-z0))) : p.alpha_fixed;
+    count = min(max(__float2int_rn((float)B * alpha), 0), B);
+    const float inv = 1.f / den;
+    e[0] *= inv;
+    e[1] *= inv;
+    // ranks of the blocks, ranks of the experts and the mass up to each
+    int rb[2] = {0, 0}, re[2] = {0, 0};
+    float mass[2] = {0.f, 0.f};
+    for (int i = 0; i < B && !p.prefix; ++i) {
+      const float v = __shfl_sync(0xffffffffu, i < 32 ? u[0] : u[1], i & 31);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) rb[k] += v > u[k] || (v == u[k] && i < lane + 32 * k);
+    }
+    for (int i = 0; i < K; ++i) {
+      const float v = __shfl_sync(0xffffffffu, i < 32 ? l[0] : l[1], i & 31);
+      const float w = __shfl_sync(0xffffffffu, i < 32 ? e[0] : e[1], i & 31);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int j = lane + 32 * k;
+        const bool before = v > l[k] || (v == l[k] && i < j);
+        re[k] += before;
+        mass[k] += before || i == j ? w : 0.f;
+      }
+    }
+    const float beta = isnan(p.beta_fixed) ? 1.f - alpha : p.beta_fixed;
+    int k = K;  // (where rounding leaves every sum below beta)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (lane + 32 * i < K && mass[i] >= beta) k = min(k, re[i] + 1);
+    taken = p.topk_fixed > 0 ? p.topk_fixed : __reduce_min_sync(0xffffffffu, k);
+    uint32_t bits[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = lane + 32 * i;
+      bits[i] = __ballot_sync(0xffffffffu, j < B && (p.prefix ? j : rb[i]) < count);
+      bits[2 + i] = __ballot_sync(0xffffffffu, j < K && re[i] < taken);
+      if (j < K) s[j] = e[i];
+    }
+    shr = (uint64_t)bits[1] << 32 | bits[0];
+    em = (uint64_t)bits[3] << 32 | bits[2];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (lane + 32 * i < K) s[lane + 32 * i] = 0.f;
+  }
+}
+
+// Shared memory of the router's product: [warps][rows of the router, in 16s][8 tokens], then [8][C].
+__host__ __device__ inline int router_rows(int C) { return (C + 15) / 16 * 16; }
+__host__ __device__ inline int route_floats(int C) { return kWarps * router_rows(C) * 8 + 8 * C; }
+
+// z [8][C] of the tokens from t0 on (up to 8): the warps share the features.
+__device__ __forceinline__ float* route_products(const Params& p, int t0, int count, float* sm) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, at = (lane & 3) * 16;
+  const int R = router_rows(p.C);
+  float* mine = sm + warp * R * 8;
+  const bool there = g < count;
+  const __nv_bfloat16* x = p.x + (long long)(t0 + (there ? g : 0)) * p.ld_x + at;
+  for (int r0 = 0; r0 < R; r0 += 64) {  // four tiles of 16 rows at a time
+    float c[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[k][i] = 0.f;
+    for (int f = warp * 64; f < p.d; f += kWarps * 64) {
+      Piece v, lo[4], hi[4];
+      clear(v);
+      if (there) read_token(v, x + f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = r0 + 16 * k + g;
+        clear(lo[k]);
+        clear(hi[k]);
+        if (r < p.C) read_token(lo[k], p.router + (long long)r * p.d + f + at);
+        if (r + 8 < p.C) read_token(hi[k], p.router + (long long)(r + 8) * p.d + f + at);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) multiply(c[k], lo[k], hi[k], v);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + 16 * k + g, n = (lane & 3) * 2;
+      if (r0 + 16 * k >= R) continue;
+      mine[r * 8 + n] = c[k][0];
+      mine[r * 8 + n + 1] = c[k][1];
+      mine[(r + 8) * 8 + n] = c[k][2];
+      mine[(r + 8) * 8 + n + 1] = c[k][3];
+    }
+  }
+  __syncthreads();
+  float* z = sm + kWarps * R * 8;
+  for (int i = threadIdx.x; i < 8 * p.C; i += kThreads) {
+    const int n = i & 7, r = i >> 3;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) v += sm[w * R * 8 + r * 8 + n];
+    z[n * p.C + r] = v;
+  }
+  __syncthreads();
+  return z;
+}
+
+// A token to a CTA (more than kTogether tokens).
+__global__ void __launch_bounds__(kThreads) route_kernel(const Params p) {
+  extern __shared__ float sm[];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int t = blockIdx.x;
+  const bool valid = !p.mask || p.mask[t];
+  const float* z = route_products(p, t, 1, sm);
+  if (threadIdx.x >= 32) return;
+  uint64_t shr, em;
+  float alpha;
+  int count, taken;
+  const int lane = threadIdx.x;
+  decide(p, t, valid, z, lane, shr, em, alpha, p.s + (long long)t * p.K, count, taken);
+  if (lane == 0) {
+    p.shr[t] = shr;
+    p.em[t] = em;
+    p.alpha[t] = alpha;
+    if (p.b_out) p.b_out[t] = count;
+    if (p.k_out) p.k_out[t] = taken;
+  }
+}
+
+// ---- h ----
+
+struct UpShared {
+  uint64_t shr[kMost], em[kMost];
+  uint64_t in_block[64], in_expert[64];  // tokens whose shared set has a block; that take an expert
+  float alpha[kMost];
+  int found[kWarps + 1];
+  uint8_t slots[kWarps][kMost];          // a warp's tokens of its pair
+};
+// after it: [G] pairs in use, then (kTogether tokens) the affinities [8][K] and the router's product
+__host__ __device__ inline size_t up_smem(int G, int K, int C, bool routes) {
+  size_t n = (sizeof(UpShared) + 15) / 16 * 16 + ((size_t)G * 2 + 15) / 16 * 16;
+  if (routes) n += 4 * ((size_t)8 * K + route_floats(C));
+  return n;
+}
+
+// NT: pieces of eight tokens. ROUTES: the decisions are taken here.
+template <int NT, bool ROUTES>
+__global__ void __launch_bounds__(kThreads, NT <= 4 ? 2 : 1) up_kernel(const Params p) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  UpShared& sh = *reinterpret_cast<UpShared*>(raw);
+  uint16_t* list = reinterpret_cast<uint16_t*>(raw + (sizeof(UpShared) + 15) / 16 * 16);
+  const int G = (p.K + 1) * p.B;
+  float* s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(list) + ((size_t)G * 2 + 15) / 16 * 16);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool first = blockIdx.x == 0;
+  grid_dep_wait();
+  grid_dep_launch();
+  if constexpr (ROUTES) {
+    const float* z = route_products(p, 0, p.T, s + 8 * p.K);
+    if (warp < p.T) {
+      uint64_t shr, em;
+      float alpha;
+      int count, taken;
+      decide(p, warp, !p.mask || p.mask[warp], z + warp * p.C, lane, shr, em, alpha, s + warp * p.K, count, taken);
+      if (lane == 0) {
+        sh.shr[warp] = shr;
+        sh.em[warp] = em;
+        sh.alpha[warp] = alpha;
+        if (first) {
+          if (p.b_out) p.b_out[warp] = count;
+          if (p.k_out) p.k_out[warp] = taken;
+        }
+      }
+    }
+  } else {
+    for (int t = threadIdx.x; t < p.T; t += kThreads) {
+      sh.shr[t] = p.shr[t];
+      sh.em[t] = p.em[t];
+      sh.alpha[t] = p.alpha[t];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.B + p.K; i += kThreads) {
+    uint64_t v = 0ull;
+    for (int t = 0; t < p.T; ++t) v |= ((i < p.B ? sh.shr[t] >> i : sh.em[t] >> (i - p.B)) & 1ull) << t;
+    if (i < p.B) sh.in_block[i] = v;
+    else sh.in_expert[i - p.B] = v;
+  }
+  __syncthreads();
+  auto members = [&](int pair) {
+    const int e = pair / p.B, b = pair - e * p.B;
+    return e == 0 ? sh.in_block[b] : sh.in_expert[e - 1] & ~sh.in_block[b];
+  };
+  // pairs in use, in order: a run of them to each thread
+  const int each = (G + kThreads - 1) / kThreads, from = threadIdx.x * each, to = min(G, from + each);
+  int n = 0;
+  for (int i = from; i < to; ++i) n += members(i) != 0ull;
+  int before = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += t;
+  }
+  if (lane == 31) sh.found[warp] = before;
+  __syncthreads();
+  int at = before - n, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) at += sh.found[w];
+    all += sh.found[w];
+  }
+  for (int i = from; i < to; ++i) {
+    const uint64_t m = members(i);
+    if (m == 0ull) continue;
+    list[at] = (uint16_t)i;
+    if (first) {
+      p.pair[at] = (uint16_t)i;
+      p.members[at] = m;
+    }
+    ++at;
+  }
+  if (first && threadIdx.x == 0) *p.n_pairs = all;
+  __syncthreads();
+
+  // tiles of 16 keys
+  const int tiles = p.M / 16;
+  const long long items = (long long)all * tiles;
+  const int g = lane >> 2, k0 = (lane & 3) * 16;
+  uint8_t* slots = sh.slots[warp];
+  for (long long i = (long long)warp * gridDim.x + blockIdx.x; i < items; i += (long long)gridDim.x * kWarps) {
+    const int pair = list[i / tiles], row = (int)(i % tiles) * 16;
+    const int e = pair / p.B, b = pair - e * p.B;
+    const uint64_t m = members(pair);
+    const int tokens = __popcll(m), pieces = (tokens + 7) / 8;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < (NT + 3) / 4; ++k) {
+      const int t = lane + 32 * k;
+      if (m >> t & 1ull) slots[__popcll(m & ((1ull << t) - 1ull))] = (uint8_t)t;
+    }
+    __syncwarp();
+    const __nv_bfloat16* w0 = p.up + ((long long)e * p.H + b * p.M + row + g) * p.d + k0;
+    const __nv_bfloat16* w1 = w0 + 8ll * p.d;
+    const __nv_bfloat16* x[NT];
+    float c[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int slot = t * 8 + g;
+      x[t] = p.x + (long long)(slot < tokens ? slots[slot] : slots[0]) * p.ld_x + k0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
+    }
+    constexpr int U = 4;  // weights of 64 features in flight
+    int f = 0;
+    for (; f + 64 * U <= p.d; f += 64 * U) {
+      Piece lo[U], hi[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        read_weights(lo[u], w0 + f + 64 * u);
+        read_weights(hi[u], w1 + f + 64 * u);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          if (t < pieces) {
+            Piece v;
+            read_token(v, x[t] + f + 64 * u);
+            multiply(c[t], lo[u], hi[u], v);
+          }
+    }
+    for (; f < p.d; f += 64) {
+      Piece lo, hi;
+      read_weights(lo, w0 + f);
+      read_weights(hi, w1 + f);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (t < pieces) {
+          Piece v;
+          read_token(v, x[t] + f);
+          multiply(c[t], lo, hi, v);
+        }
+    }
+    // h = w GeLU, rounded once: the weight comes before the rounding, so that the down projection
+    // adds up what is held
+    __nv_bfloat16* h = p.h + (long long)e * p.T * p.H + b * p.M + row + g;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (t >= pieces) continue;
+      gelu::gelu2(c[t][0], c[t][1]);
+      gelu::gelu2(c[t][2], c[t][3]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int slot = t * 8 + (lane & 3) * 2 + j;
+        if (slot >= tokens) continue;
+        const int tok = slots[slot];
+        const float w = e == 0 ? sh.alpha[tok]
+                               : ROUTES ? s[tok * p.K + e - 1] : __ldg(p.s + (long long)tok * p.K + e - 1);
+        h[(long long)tok * p.H] = __float2bfloat16_rn(w * c[t][j]);
+        h[(long long)tok * p.H + 8] = __float2bfloat16_rn(w * c[t][2 + j]);
+      }
+    }
+  }
+}
+
+// ---- y ----
+
+// MT: tiles of 16 output features of a cluster. Shared memory: the warps' sums [warps][16 MT][8 NT],
+// then the CTA's [16 MT][8 NT].
+template <int NT, int MT>
+constexpr size_t down_smem() { return 4u * (kWarps + 1) * 16 * MT * 8 * NT; }
+
+template <int NT, int MT>
+__global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) down_kernel(const Params p, const int ctas) {
+  extern __shared__ __align__(16) float red[];
+  constexpr int kSums = 16 * MT * 8 * NT;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x % ctas, j0 = blockIdx.x / ctas * (16 * MT);
+  const int g = lane >> 2, k0 = (lane & 3) * 16;
+  float c[MT][NT][4];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[i][t][j] = 0.f;
+  grid_dep_wait();
+  const int per = p.M / 64, chunks = *p.n_pairs * per, step = ctas * kWarps;
+  constexpr int U = 4 / MT;  // chunks whose weights are in flight
+  for (int i0 = warp * ctas + rank; i0 < chunks; i0 += step * U) {
+    Piece lo[U][MT], hi[U][MT];
+    const __nv_bfloat16* h[U];
+    uint64_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * step;
+      m[u] = 0ull;
+      if (i >= chunks) continue;
+      const int at = i / per, pair = p.pair[at];
+      const int e = pair / p.B, ch = (pair - e * p.B) * p.M + (i - at * per) * 64 + k0;
+      m[u] = p.members[at];
+      const __nv_bfloat16* w = p.down + ((long long)e * p.d + j0 + g) * p.H + ch;
+#pragma unroll
+      for (int k = 0; k < MT; ++k) {
+        read_weights(lo[u][k], w + (long long)(16 * k) * p.H);
+        read_weights(hi[u][k], w + (long long)(16 * k + 8) * p.H);
+      }
+      h[u] = p.h + (long long)e * p.T * p.H + ch;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (m[u] == 0ull) continue;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if ((m[u] >> (8 * t) & 255ull) == 0ull) continue;
+        Piece v;
+        clear(v);
+        const int tok = t * 8 + g;
+        if (m[u] >> tok & 1ull) read_token(v, h[u] + (long long)tok * p.H);
+#pragma unroll
+        for (int k = 0; k < MT; ++k) multiply(c[k][t], lo[u][k], hi[u][k], v);
+      }
+    }
+  }
+  // [feature][token]
+  float* mine = red + warp * kSums;
+#pragma unroll
+  for (int k = 0; k < MT; ++k)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        mine[(16 * k + g + (j >> 1) * 8) * (8 * NT) + t * 8 + (lane & 3) * 2 + (j & 1)] = c[k][t][j];
+  __syncthreads();
+  float* sums = red + kWarps * kSums;
+  for (int i = threadIdx.x; i < kSums; i += kThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) v += red[w * kSums + i];
+    sums[i] = v;
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  // each CTA adds a share of the cluster's sums
+  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(sums));
+  for (int i = rank * kThreads + threadIdx.x; i < kSums; i += ctas * kThreads) {
+    const int f = i % (16 * MT), t = i / (16 * MT);  // consecutive features to consecutive threads
+    if (t >= p.T) continue;
+    float v = 0.f;
+    for (int r = 0; r < ctas; ++r) {
+      uint32_t there;
+      float a;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(base + 4u * (f * (8 * NT) + t)), "r"(r));
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a) : "r"(there) : "memory");
+      v += a;
+    }
+    p.out[t * p.ld_out + j0 + f] = __float2bfloat16_rn(v);
+  }
+  // no CTA leaves while another reads its sums
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// ---- the router's rows ----
+
+// Row c of [1 + K + B][d]: column c of w_router [d][K + 1], or the mean key of block c - K - 1 of the
+// shared expert, summed in fp64 and rounded once.
+__global__ void __launch_bounds__(256)
+    table_kernel(int d, int K, int B, int M, const __nv_bfloat16* w_router, const __nv_bfloat16* up,
+                 __nv_bfloat16* table) {
+  grid_dep_wait();
+  const int i = blockIdx.x * 256 + threadIdx.x, c = blockIdx.y;
+  if (i >= d) return;
+  if (c <= K) {
+    table[(long long)c * d + i] = w_router[(long long)i * (K + 1) + c];
+    return;
+  }
+  double sum = 0.0;
+  const __nv_bfloat16* key = up + (long long)(c - K - 1) * M * d + i;
+  for (int h = 0; h < M; ++h) sum += (double)__bfloat162float(key[(long long)h * d]);
+  const double mean = sum / (double)M;
+  // towards zero with the last bit set where that was not exact: the second rounding is then right
+  float f = __double2float_rz(mean);
+  if ((double)f != mean) f = __uint_as_float(__float_as_uint(f) | 1u);
+  table[(long long)c * d + i] = __float2bfloat16_rn(f);
+}
+
+// ---- host side ----
+
+int check(const unif_moe_few* p) {
+  if (!p) { set_error("the description is NULL"); return UNIF_MOE_ERR_ARG; }
+  if (p->tokens < 0 || p->d_model < 1 || p->d_ff < 1 || p->n_experts < 1 || p->n_experts > 64 || p->n_blocks < 2 ||
+      p->n_blocks > 64) {
+    set_error("bad sizes: tokens=%d d_model=%d d_ff=%d n_experts=%d n_blocks=%d", p->tokens, p->d_model, p->d_ff,
+              p->n_experts, p->n_blocks);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (p->tokens > kMost) {
+    set_error("tokens=%d above %d", p->tokens, kMost);
+    return UNIF_MOE_ERR_CAPACITY;
+  }
+  if (p->d_ff % p->n_blocks || p->d_model % 64 || p->d_ff / p->n_blocks % 64) {
+    set_error("d_model=%d and d_ff / n_blocks=%d / %d must be multiples of 64", p->d_model, p->d_ff, p->n_blocks);
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  const unif_moe_thresholds& th = p->th;
+  if (th.topk_fixed < 0 || th.topk_fixed > p->n_experts || isinf(th.tau) || isinf(th.alpha_fixed) ||
+      isinf(th.beta_fixed) || (!isnan(th.alpha_fixed) && !(th.alpha_fixed >= 0.f && th.alpha_fixed <= 1.f))) {
+    set_error("bad thresholds (topk_fixed=%d, alpha_fixed=%g)", th.topk_fixed, th.alpha_fixed);
+    return UNIF_MOE_ERR_ARG;
+  }
+  return UNIF_MOE_OK;
+}
+
+// The parts of the workspace, each at a multiple of 256 bytes.
+struct Parts {
+  int64_t shr, em, alpha, s, n_pairs, pair, members, h, total;
+};
+Parts parts_of(const unif_moe_few* p) {
+  const int64_t T = p->tokens, G = (int64_t)(p->n_experts + 1) * p->n_blocks;
+  Parts r{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  r.shr = take(8 * T);
+  r.em = take(8 * T);
+  r.alpha = take(4 * T);
+  r.s = take(4 * T * p->n_experts);
+  r.n_pairs = take(4);
+  r.pair = take(2 * G);
+  r.members = take(8 * G);
+  r.h = take(2 * (p->n_experts + 1) * T * p->d_ff);
+  r.total = at;
+  return r;
+}
+
+cudaError_t launch_cluster(void (*kernel)(const Params, const int), int grid, int ctas, size_t smem, cudaStream_t s,
+                           const Params& p) {
+  const cudaError_t e = allow_smem_once(kernel, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid * ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, p, ctas);
+}
+
+template <int NT>
+cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
+  const int G = (p.K + 1) * p.B;
+  const bool routes = p.T <= kTogether;
+  const size_t smem = up_smem(G, p.K, p.C, routes);
+  cudaError_t e;
+  if (!routes) {
+    const size_t bytes = 4 * (size_t)route_floats(p.C);
+    e = allow_smem_once(route_kernel, bytes);
+    if (e == cudaSuccess) e = launch_dependent(route_kernel, dim3(p.T), dim3(kThreads), bytes, s, p);
+    if (e != cudaSuccess) return e;
+  }
+  void (*up)(const Params);
+  if constexpr (NT == 1) up = up_kernel<1, true>;
+  else up = up_kernel<NT, false>;
+  e = allow_smem_once(up, smem);
+  if (e == cudaSuccess) e = launch_dependent(up, dim3((NT <= 4 ? 2 : 1) * sms), dim3(kThreads), smem, s, p);
+  if (e != cudaSuccess) return e;
+  // clusters of 32 output features, as many CTAs in each as the SMs hold at once
+  constexpr int MT = 2;
+  const int groups = p.d / (16 * MT), slots = (NT <= 2 ? 2 : 1) * sms;
+  const int ctas = std::max(1, std::min(8, slots / groups));
+  return launch_cluster(down_kernel<NT, MT>, groups, ctas, down_smem<NT, MT>(), s, p);
+}
+
+cudaError_t launch(const Params& p, int sms, cudaStream_t s) {
+  if (p.T <= 8) return launch_as<1>(p, sms, s);
+  if (p.T <= 16) return launch_as<2>(p, sms, s);
+  if (p.T <= 32) return launch_as<4>(p, sms, s);
+  return launch_as<8>(p, sms, s);
+}
+
+bool off(const void* p, uintptr_t by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }
+
+int run(const unif_moe_few* d, const void* x, int64_t ld_x, const void* router, const float* bias, const void* up,
+        const void* down, const uint8_t* mask, void* out, int64_t ld_out, int32_t* b_out, int32_t* k_out,
+        void* workspace, int64_t workspace_bytes, cudaStream_t s) {
+  if (d->tokens == 0) return UNIF_MOE_OK;
+  if (!x || !router || !up || !down || !out) {
+    set_error("x, router, weights or out is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (ld_x < d->d_model || ld_out < d->d_model) {
+    set_error("a row stride is below d_model=%d", d->d_model);
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (off(x, 16) || ld_x % 8 || off(router, 16) || off(up, 32) || off(down, 32)) {
+    set_error("rows of x and the router must start at multiples of 16 bytes, the weights at one of 32");
+    return UNIF_MOE_ERR_ARG;
+  }
+  const Parts at = parts_of(d);
+  if (!workspace || workspace_bytes < at.total) {
+    set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)at.total);
+    return UNIF_MOE_ERR_CAPACITY;
+  }
+  if (off(workspace, 16)) {
+    set_error("the workspace must be 16-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc != UNIF_MOE_OK) return rc;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  Params p{};
+  p.T = d->tokens; p.d = d->d_model; p.H = d->d_ff; p.K = d->n_experts; p.B = d->n_blocks;
+  p.M = p.H / p.B;
+  p.C = 1 + p.K + p.B;
+  p.tau = isnan(d->th.tau) ? (float)((double)(p.B - 1) / ((double)p.B * p.B)) : d->th.tau;
+  p.alpha_fixed = d->th.alpha_fixed;
+  p.beta_fixed = d->th.beta_fixed;
+  p.topk_fixed = d->th.topk_fixed;
+  p.prefix = d->th.prefix_blocks;
+  p.x = static_cast<const __nv_bfloat16*>(x);
+  p.ld_x = ld_x;
+  p.router = static_cast<const __nv_bfloat16*>(router);
+  p.bias = bias;
+  p.up = static_cast<const __nv_bfloat16*>(up);
+  p.down = static_cast<const __nv_bfloat16*>(down);
+  p.mask = mask;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.ld_out = ld_out;
+  p.b_out = b_out;
+  p.k_out = k_out;
+  p.shr = reinterpret_cast<uint64_t*>(ws + at.shr);
+  p.em = reinterpret_cast<uint64_t*>(ws + at.em);
+  p.alpha = reinterpret_cast<float*>(ws + at.alpha);
+  p.s = reinterpret_cast<float*>(ws + at.s);
+  p.n_pairs = reinterpret_cast<int*>(ws + at.n_pairs);
+  p.pair = reinterpret_cast<uint16_t*>(ws + at.pair);
+  p.members = reinterpret_cast<uint64_t*>(ws + at.members);
+  p.h = reinterpret_cast<__nv_bfloat16*>(ws + at.h);
+  const cudaError_t e = launch(p, sms, s);
+  if (e != cudaSuccess) {
+    set_error("few tokens: %s", cudaGetErrorString(e));
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+// The description of a layer's forward of T tokens.
+int of_layer(const unif_moe_layer* L, int T, unif_moe_few* d) {
+  if (!L) { set_error("NULL handle"); return UNIF_MOE_ERR_ARG; }
+  if (L->dtype != UNIF_MOE_BF16) {
+    set_error("few tokens: the layer must be bf16");
+    return UNIF_MOE_ERR_SHAPE;
+  }
+  if (!L->loaded) { set_error("forward before load_weights"); return UNIF_MOE_ERR_STATE; }
+  *d = unif_moe_few{T, L->d, L->H, L->K, L->B, L->th};
+  d->th.tau = L->tau;
+  return check(d);
+}
+
+}  // namespace few
+}  // namespace unif
+
+using unif::set_error;
+namespace fw = unif::few;
+
+extern "C" {
+
+int unif_moe_router_table(int d_model, int d_ff, int n_experts, int n_blocks, const void* w_router, const void* w_up,
+                          void* table, void* stream) {
+  set_error("%s", "");
+  const unif_moe_few d{1, d_model, d_ff, n_experts, n_blocks, {NAN, NAN, NAN, 0, 0}};
+  const int rc = fw::check(&d);
+  if (rc != UNIF_MOE_OK) return rc;
+  if (!w_router || !w_up || !table) {
+    set_error("w_router, w_up or table is NULL");
+    return UNIF_MOE_ERR_ARG;
+  }
+  const cudaError_t e = unif::launch_dependent(
+      fw::table_kernel, dim3((d_model + 255) / 256, 1 + n_experts + n_blocks), dim3(256), 0,
+      static_cast<cudaStream_t>(stream), d_model, n_experts, n_blocks, d_ff / n_blocks,
+      static_cast<const __nv_bfloat16*>(w_router), static_cast<const __nv_bfloat16*>(w_up),
+      static_cast<__nv_bfloat16*>(table));
+  if (e != cudaSuccess) {
+    set_error("router table: %s", cudaGetErrorString(e));
+    return UNIF_MOE_ERR_CUDA;
+  }
+  return UNIF_MOE_OK;
+}
+
+int64_t unif_moe_few_workspace(const unif_moe_few* p) {
+  set_error("%s", "");
+  return fw::check(p) == UNIF_MOE_OK ? fw::parts_of(p).total : -1;
+}
+
+int unif_moe_few_forward(const unif_moe_few* p, const void* x, int64_t ld_x, const void* router, const float* bias,
+                         const void* w_up, const void* w_down, const uint8_t* mask, void* out, int64_t ld_out,
+                         int32_t* b_out, int32_t* k_out, void* workspace, int64_t workspace_bytes, void* stream) {
+  set_error("%s", "");
+  const int rc = fw::check(p);
+  if (rc != UNIF_MOE_OK) return rc;
+  return fw::run(p, x, ld_x, router, bias, w_up, w_down, mask, out, ld_out, b_out, k_out, workspace, workspace_bytes,
+                 static_cast<cudaStream_t>(stream));
+}
+
+int64_t unif_moe_forward_few_workspace(unif_moe_t L, int T) {
+  set_error("%s", "");
+  unif_moe_few d;
+  return fw::of_layer(L, T, &d) == UNIF_MOE_OK ? fw::parts_of(&d).total : -1;
+}
+
+int unif_moe_forward_few(unif_moe_t L, const void* x, int64_t ld_x, int T, const uint8_t* mask, void* out,
+                         int64_t ld_out, int32_t* b_out, int32_t* k_out, void* workspace, int64_t workspace_bytes,
+                         void* stream) {
+  set_error("%s", "");
+  unif_moe_few d;
+  const int rc = fw::of_layer(L, T, &d);
+  if (rc != UNIF_MOE_OK) return rc;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || (dev != L->device && cudaSetDevice(L->device) != cudaSuccess)) {
+    set_error("no CUDA device");
+    return UNIF_MOE_ERR_CUDA;
+  }
+  const int r = fw::run(&d, x, ld_x, L->wr_bf, L->bias, L->w_up, L->w_down, mask, out, ld_out, b_out, k_out,
+                        workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+  if (dev != L->device) cudaSetDevice(dev);
+  return r;
+}
+
+}  // extern "C"

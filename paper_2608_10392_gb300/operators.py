@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import math
 import os
 from typing import NamedTuple, Optional
 
@@ -24,7 +25,8 @@ import torch
 
 __all__ = ["BlockNorm", "balance_loss", "Mxfp4", "mxfp4_quantize", "mxfp4_dequantize",
            "mxfp4_product", "mxfp4_status", "Fp8", "fp8_quantize",
-           "fp8_dequantize", "linear", "linear_backward", "linear_status"]
+           "fp8_dequantize", "linear", "linear_backward", "linear_status", "router_table", "few_tokens",
+           "FEW_TOKENS"]
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _CODES = {torch.float32: 0, torch.bfloat16: 1}
@@ -51,12 +53,22 @@ class _LinearGrad(C.Structure):
                 ("ld_dw", C.c_int64), ("dbias", C.c_void_p)]
 
 
+class _FewDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("d_model", C.c_int), ("d_ff", C.c_int),
+                ("n_experts", C.c_int), ("n_blocks", C.c_int), ("tau", C.c_float),
+                ("alpha_fixed", C.c_float), ("beta_fixed", C.c_float), ("topk_fixed", C.c_int),
+                ("prefix_blocks", C.c_int)]
+
+
 EXPORTS = ["unif_moe_block_norm_forward", "unif_moe_block_norm_workspace",
            "unif_moe_block_norm_backward", "unif_moe_balance_workspace", "unif_moe_balance_loss",
            "unif_moe_mxfp4_quantize", "unif_moe_mxfp4_dequantize", "unif_moe_mxfp4_product",
            "unif_moe_block_norm_forward_fp8", "unif_moe_fp8_quantize", "unif_moe_fp8_dequantize",
            "unif_moe_linear_workspace", "unif_moe_linear_forward",
-           "unif_moe_linear_backward_workspace", "unif_moe_linear_backward"]
+           "unif_moe_linear_backward_workspace", "unif_moe_linear_backward",
+           "unif_moe_router_table", "unif_moe_few_workspace", "unif_moe_few_forward",
+           "unif_moe_forward_few_workspace", "unif_moe_forward_few"]
+FEW_TOKENS = 64
 
 
 def declare(L: C.CDLL) -> None:
@@ -84,6 +96,12 @@ def declare(L: C.CDLL) -> None:
                                            P, P])
     L.unif_moe_linear_backward_workspace.argtypes = [Q, G]
     L.unif_moe_linear_backward.argtypes = [Q, G, P, I64, P, P]
+    F = C.POINTER(_FewDesc)
+    L.unif_moe_router_table.argtypes = [I, I, I, I, P, P, P, P]
+    L.unif_moe_few_workspace.argtypes = [F]
+    L.unif_moe_few_forward.argtypes = [F, P, I64] + [P] * 6 + [I64, P, P, P, I64, P]
+    L.unif_moe_forward_few_workspace.argtypes = [P, I]
+    L.unif_moe_forward_few.argtypes = [P, P, I64, I, P, P, I64, P, P, P, I64, P]
     for name in EXPORTS:
         getattr(L, name).restype = I64 if name.endswith("_workspace") else C.c_int
 
@@ -316,3 +334,27 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dout: torch.Tensor,
     is rounded to bf16 for the two products."""
     return _b().linear_backward(x, w, dout, z, _ACTIVATIONS[activation], mask, dx, dw, bias,
                                 _CODES[DTYPES[grad_dtype]], _status_of(x), stream)
+
+
+def router_table(w_router: torch.Tensor, w_up: torch.Tensor, n_blocks: int, stream=None) -> torch.Tensor:
+    """The router's rows [1 + K + B][d] for few_tokens, made once for a layer's weights: W_shr, W_g
+    (w_router [d][K + 1]) and the mean key of each of the n_blocks blocks of the shared expert
+    (w_up [K + 1][H][d]); bf16."""
+    return _b().router_table(w_router, w_up, n_blocks, stream)
+
+
+def few_tokens(x: torch.Tensor, router: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+               n_blocks: int, *, router_bias: Optional[torch.Tensor] = None,
+               mask: Optional[torch.Tensor] = None, tau: float = math.nan,
+               alpha_fixed: float = math.nan, beta_fixed: float = math.nan, topk_fixed: int = 0,
+               prefix_blocks: bool = False, shared_counts: Optional[torch.Tensor] = None,
+               residual_counts: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """The whole layer for up to FEW_TOKENS tokens x [T][d] (bf16), from the caller's weights: router
+    from router_table, w_up [K + 1][H][d], w_down [K + 1][d][H] (contiguous bf16), router_bias
+    [K + 1] fp32; thresholds as Layer's. A server's step: two or three kernels that read each weight
+    in use once. mask [T]: 0 marks padding, which gives 0. shared_counts, residual_counts [T]
+    int32 receive b(x) and k(x). Layer.forward_few does the same with a layer's weights."""
+    return _b().few_tokens(x, router, w_up, w_down, n_blocks, router_bias, mask,
+                           (tau, alpha_fixed, beta_fixed, topk_fixed, prefix_blocks), shared_counts,
+                           residual_counts, out, stream)
