@@ -34,25 +34,29 @@ enum Kind {
   kWeight = 3     // dw: both MN-major
 };
 
-constexpr int kEpiWarps = 8, kTmaWarp = 8, kMmaWarp = 9;
-constexpr int kThreads = 320;
+constexpr int kEpiWarps = 16, kTmaWarp = 16, kMmaWarp = 17;
+constexpr int kEpiThreads = 32 * kEpiWarps;
+constexpr int kThreads = kEpiThreads + 64;
 constexpr uint32_t kTmemCols = 512, kAcc = 256;
 constexpr int kMaxStages = 8;
 constexpr int kBars = 2 * kMaxStages + 5;
 constexpr uint32_t kSmemMax = 232448;
-constexpr uint32_t kStaging = kEpiWarps * 32 * 33 * 4;  // rows that no 32-byte stores fit
-// Steps of 64 rows that one accumulation of kWeight runs over. The tensor cores
-// truncate the accumulator at every MMA, so the error grows with their number: longer sums
-// are added in fp32 registers.
+constexpr uint32_t kStaging = kEpiWarps * 32 * 17 * 4;  // rows that no 32-byte stores fit
+constexpr uint32_t kColumns = 2 * 2 * 256 * 4;          // bias and scales of two tiles
+// Steps that one accumulation for an fp32 result runs over. The tensor cores
+// truncate the accumulator at every MMA, so the error grows with their number: the sums of
+// longer reductions are added in fp32 (65,536 x 4,096 to 1,024 onto an fp32 residual: 2.5e-6 of the
+// result's norm off in one accumulation, 6e-7 so).
 constexpr int kSumSteps = 16;
 
 struct Params {
   int M, N;                        // rows and columns of the result
   int steps, splits;               // steps of 128 operand bytes; parts of the reduction
-  int tile_n, m_tiles, n_tiles;    // columns of a tile (a multiple of 16)
+  int sum_steps;                   // most steps of an accumulation
+  int tile_n, m_tiles, n_tiles;    // columns of a tile (a multiple of 16, on pairs of 32)
   int stages;
   uint32_t stage_bytes;
-  bool gelu, wide;                 // wide: all row accesses in whole 16- or 32-byte pieces
+  bool gelu;
   void* out;
   long long ld_out;
   const float *sm, *sn;            // scales of rows and columns, or NULL
@@ -110,6 +114,16 @@ __device__ __forceinline__ uint32_t idesc_of(int n) {
 __device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) |
          ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// 16 consecutive TMEM columns of 32 lanes from registers (complete after tmem_wait_st).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0],"
+      " {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]),
+      "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+      : "memory");
 }
 
 // ---- the epilogue's rows ----
@@ -173,72 +187,84 @@ __device__ __forceinline__ void act2(float& a, float& b) {
   }
 }
 
-// Sixteen columns of this thread's row, from column `ch` (a multiple of 16) on, all there.
+// Sixteen columns of this thread's row, from column `ch` (a multiple of 16) on, all there. bias, sn:
+// their values for these columns in shared memory (read where p has them).
 template <typename TO>
 __device__ __forceinline__ void finish16(const Params& p, float (&v)[16], long long row, int ch, float scale,
-                                         bool on) {
+                                         bool on, const float* bias, const float* sn) {
   TO* o = static_cast<TO*>(p.out) + row * p.ld_out + ch;
-  float t[16];
   if (p.sn) {
-    load16(p.sn + ch, t);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] *= scale * t[i];
+    for (int i = 0; i < 16; i += 4) {
+      const float4 c = *reinterpret_cast<const float4*>(sn + i);
+      v[i] *= scale * c.x;
+      v[i + 1] *= scale * c.y;
+      v[i + 2] *= scale * c.z;
+      v[i + 3] *= scale * c.w;
+    }
   } else if (p.sm) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] *= scale;
   }
-  if (p.bias) {
-    if (p.bias_f32) load16(static_cast<const float*>(p.bias) + ch, t);
-    else load16(static_cast<const __nv_bfloat16*>(p.bias) + ch, t);
+  if (p.bias)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += t[i];
-  }
-  if (p.z) {
+    for (int i = 0; i < 16; i += 4) {
+      const float4 c = *reinterpret_cast<const float4*>(bias + i);
+      v[i] += c.x;
+      v[i + 1] += c.y;
+      v[i + 2] += c.z;
+      v[i + 3] += c.w;
+    }
+  if (!on)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = on ? v[i] : 0.f;
-    store16(p.z + row * p.ld_z + ch, t);
-  }
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+  if (p.z) store16(p.z + row * p.ld_z + ch, v);
   if (p.gelu)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) act2<TO>(v[i], v[i + 1]);
   if (p.residual && on) {
+    float t[16];
     load16(static_cast<const TO*>(p.residual) + row * p.ld_res + ch, t);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] += t[i];
   }
-  if (!on)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.f;
   store16(o, v);
 }
 
 // One element.
 template <typename TO>
-__device__ __forceinline__ void finish1(const Params& p, float v, long long row, int ch, bool on) {
-  if (p.sm) v *= p.sm[row];
-  if (p.sn) v *= p.sn[ch];
-  if (p.bias)
-    v += p.bias_f32 ? static_cast<const float*>(p.bias)[ch]
-                    : __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[ch]);
+__device__ __forceinline__ void finish1(const Params& p, float v, long long row, int ch, bool on, float sm,
+                                        float sn, float bias, float residual) {
+  if (p.sm || p.sn) v *= sm * sn;
+  v += bias;
   if (!on) v = 0.f;
   if (p.z) p.z[row * p.ld_z + ch] = __float2bfloat16_rn(v);
-  if (p.gelu && on) {
+  if (p.gelu) {
     float u = v;
     act2<TO>(v, u);
   }
-  if (p.residual && on) v += to_f32(static_cast<const TO*>(p.residual)[row * p.ld_res + ch]);
-  put(static_cast<TO*>(p.out) + row * p.ld_out + ch, v);
+  put(static_cast<TO*>(p.out) + row * p.ld_out + ch, on ? v + residual : 0.f);
+}
+__device__ __forceinline__ float bias_of(const Params& p, int ch) {
+  return !p.bias ? 0.f
+         : p.bias_f32 ? static_cast<const float*>(p.bias)[ch]
+                      : __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[ch]);
+}
+template <typename TO>
+__device__ __forceinline__ float residual_of(const Params& p, long long row, int ch) {
+  return to_f32(static_cast<const TO*>(p.residual)[row * p.ld_res + ch]);
 }
 
 // PAIR: the CTAs of a cluster of two share a tile of 256 rows (tcgen05 cta_group::2), 128 of
 // them and half of the columns' operand in each one's shared memory. The first CTA's
 // barriers take both CTAs' bytes, its MMA lane issues for both.
-template <int KIND, typename TO, bool PAIR>
+// WIDE: all row accesses in whole pieces of 16 values.
+template <int KIND, typename TO, bool PAIR, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const Params p) {
-  constexpr int kCtas = PAIR ? 2 : 1, kTileM = 128 * kCtas;
-  constexpr bool kSum = KIND == kWeight;  // long reductions: sums of accumulations in registers
+  constexpr int kCtas = PAIR ? 2 : 1, kTileM = 128 * kCtas, kUnit = 16 * kCtas;  // columns of an MMA: whole units
+  constexpr bool kParts = KIND == kWeight;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
   const bool leader = rank == 0;
   const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
@@ -256,7 +282,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t mma_done = bar0 + 8u * (2 * kMaxStages + 4);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* staging = reinterpret_cast<float*>(bars + kBars + 1);
+  float* columns = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(bars + kBars + 1) + 15) & ~(uintptr_t)15);
+  float* staging = columns + kColumns / 4;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -303,132 +330,145 @@ __global__ void __launch_bounds__(kThreads, 1)
     int m0, n0, n;      // this CTA's first row, the tile's first column and columns
     int from, to;       // steps
     int part;
-    __device__ __forceinline__ int sums() const {
-      return kSum ? (to - from + kSumSteps - 1) / kSumSteps : 1;
-    }
-    // the first step of its j-th accumulation
-    __device__ __forceinline__ int step(int j) const {
-      return kSum ? from + (int)((long long)(to - from) * j / sums()) : j ? to : from;
-    }
+  };
+  // accumulations of an item; the first step of its j-th
+  auto sums = [&](const Item& it) { return (it.to - it.from + p.sum_steps - 1) / p.sum_steps; };
+  auto first_step = [&](const Item& it, int n, int j) {
+    return it.from + (int)((long long)(it.to - it.from) * j / n);
   };
   const int tiles = p.m_tiles * p.n_tiles, n_items = tiles * p.splits;
   auto item_of = [&](int i) {
     Item it;
-    it.part = kSum ? i / tiles : 0;
-    const int t = kSum ? i - it.part * tiles : i;
+    it.part = kParts ? i / tiles : 0;
+    const int t = kParts ? i - it.part * tiles : i;
     const int m = t / p.n_tiles;
     it.m0 = m * kTileM + 128 * (int)rank;
     it.n0 = (t - m * p.n_tiles) * p.tile_n;
     it.n = min(p.tile_n, p.N - it.n0);
-    it.from = kSum ? (int)((long long)p.steps * it.part / p.splits) : 0;
-    it.to = kSum ? (int)((long long)p.steps * (it.part + 1) / p.splits) : p.steps;
+    it.from = kParts ? (int)((long long)p.steps * it.part / p.splits) : 0;
+    it.to = kParts ? (int)((long long)p.steps * (it.part + 1) / p.splits) : p.steps;
     return it;
   };
 
   if (warp < kEpiWarps) {
     // ---------------- accumulators to the result ----------------------------
-    const int q = warp & 3, half = warp >> 2;
-    float* stg = staging + warp * (32 * 33);
-    int acc = 0;
-    uint32_t ph = 0;
+    // Four warps to a quarter of the rows, 16 columns at a time. (A wait given up is not the end
+    // of the loop: the warps meet at a barrier.)
+    const int q = warp & 3, part = warp >> 2;
+    float* stg = staging + warp * (32 * 17);
+    int acc = 0;       // the accumulator of the item's sum
+    uint32_t ph = 0;   // a phase bit per accumulator
     bool ok = true;
-    for (int i = unit; i < n_items && ok; i += units) {
+    auto wait_acc = [&](int a) {
+      ok = ok && wait_warp(accf_bar(a), ph >> a & 1u, abort_flag, p.status, p.wait_limit);
+      ph ^= 1u << a;
+      tc_fence_after();
+    };
+    auto release = [&](int a) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_leader(acce_bar(a));
+    };
+    const bool per_column = p.bias || p.sn;
+    // the columns' bias (the first 256 threads) and scales (the others), on their way a tile ahead
+    auto column = [&](int i) {
       const Item it = item_of(i);
+      const int c = it.n0 + (int)(threadIdx.x & 255u);
+      if ((int)(threadIdx.x & 255u) >= it.n) return 0.f;
+      if (threadIdx.x < 256) return bias_of(p, c);
+      return p.sn ? p.sn[c] : 1.f;
+    };
+    float ahead = per_column && unit < n_items ? column(unit) : 0.f;
+    int turn = 0;
+    for (int i = unit; i < n_items; i += units, turn ^= 1) {
+      const Item it = item_of(i);
+      float* bias = columns + turn * 512;
+      if (per_column) {
+        bias[threadIdx.x] = ahead;
+        asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
+        if (i + units < n_items) ahead = column(i + units);
+      }
       const long long row = (long long)it.m0 + q * 32 + lane;
       const bool there = row < p.M;
       // (a quarter past the last row has nothing to store)
-      const int chunks = it.m0 + q * 32 < p.M ? (it.n + 31) / 32 : 0;
+      const int chunks = it.m0 + q * 32 < p.M ? (it.n + 15) / 16 : 0;
       bool on = there;
       float scale = 1.f;
       if (there && p.mask) on = p.mask[row] != 0;
       if (there && p.sm) scale = p.sm[row];
-      // 32 columns from column c * 32 of the tile on
-      auto finish = [&](float (&v)[32], int c) {
-        const int ch = it.n0 + c * 32, count = it.n - c * 32;
-        if (kSum && p.splits > 1) {
-          float* o = p.part + ((long long)it.part * p.M + row) * p.N + ch;
-          if (p.wide) {
-            if (there)
-#pragma unroll
-              for (int g = 0; g < 2; ++g)
-                if (16 * g < count) store16(o + 16 * g, *reinterpret_cast<float(*)[16]>(&v[16 * g]));
-            return;
-          }
-        } else if (p.wide) {
-          if (there)
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-              if (16 * g < count)
-                finish16<TO>(p, *reinterpret_cast<float(*)[16]>(&v[16 * g]), row, ch + 16 * g, scale, on);
+      // 16 columns from column c * 16 of the tile on
+      auto finish = [&](float (&v)[16], int c) {
+        const int ch = it.n0 + c * 16, count = it.n - c * 16;
+        const bool parts = kParts && p.splits > 1;
+        if constexpr (WIDE) {
+          if (!there) return;
+          if (parts) store16(p.part + ((long long)it.part * p.M + row) * p.N + ch, v);
+          else if constexpr (KIND >= kInput) store16(static_cast<TO*>(p.out) + row * p.ld_out + ch, v);
+          else finish16<TO>(p, v, row, ch, scale, on, bias + c * 16, bias + 256 + c * 16);
           return;
         }
-        // a lane per column instead: rows of any width and alignment in runs of 32
+        // a lane per column instead, two rows at a time: rows of any width and alignment
+        if constexpr (!WIDE) {
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) stg[lane * 33 + j] = v[j];
+        for (int j = 0; j < 16; ++j) stg[lane * 17 + j] = v[j];
         __syncwarp();
         const uint32_t live = __ballot_sync(0xffffffffu, on);
-        const int rows = (int)min(32ll, p.M - (row - lane));
-        if (lane < count)
-          for (int r = 0; r < rows; ++r) {
-            const float x = stg[r * 33 + lane];
-            if (kSum && p.splits > 1)
-              p.part[((long long)it.part * p.M + row - lane + r) * p.N + ch + lane] = x;
-            else
-              finish1<TO>(p, x, row - lane + r, ch + lane, live >> r & 1u);
+        const int col = lane & 15;
+        const float sn = per_column ? bias[256 + c * 16 + col] : 1.f, b = per_column ? bias[c * 16 + col] : 0.f;
+#pragma unroll 1
+        for (int r0 = lane >> 4; r0 < 32; r0 += 16) {
+          float res[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int r = r0 + 2 * k;
+            res[k] = 0.f;
+            if (p.residual && (live >> r & 1u) && col < count) res[k] = residual_of<TO>(p, row - lane + r, ch + col);
           }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int r = r0 + 2 * k;
+            const float sm = __shfl_sync(0xffffffffu, scale, r);
+            if (row - lane + r >= p.M || col >= count) continue;
+            const float x = stg[r * 17 + col];
+            if (parts) p.part[((long long)it.part * p.M + row - lane + r) * p.N + ch + col] = x;
+            else if constexpr (KIND >= kInput) put(static_cast<TO*>(p.out) + (row - lane + r) * p.ld_out + ch + col, x);
+            else finish1<TO>(p, x, row - lane + r, ch + col, live >> r & 1u, sm, sn, b, res[k]);
+          }
+        }
+        }
       };
-      if constexpr (kSum) {
-        float sum[4][32];
-        for (int j = 0; j < it.sums(); ++j) {
-          ok = wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16) + half * 32;
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (2 * c + half < chunks) {
-#pragma unroll
-              for (int g = 0; g < 2; ++g) {
-                float v[16];
-                tmem_ld16(from + c * 64 + g * 16, v);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  float& s = sum[c][16 * g + e];
-                  s = j ? s + v[e] : v[e];
-                }
-              }
-            }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) arrive_leader(acce_bar(acc));
-          if (++acc == 2) { acc = 0; ph ^= 1u; }
-        }
+      if constexpr (WIDE)  // the residual's rows, on their way to L2 while the sums are taken
+        if (KIND < kInput && p.residual && on)
+          for (int c = part; c < chunks; c += 4)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const TO*>(p.residual) + row * p.ld_res +
+                                                          it.n0 + c * 16));
+      const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + part * 16;
+      const int n_sums = sums(it);
+      wait_acc(acc);
+      for (int j = 1; j < n_sums; ++j) {  // further accumulations, added to the first
+        wait_acc(acc ^ 1);
         if (!ok) break;
+        for (int c = 0; 4 * c + part < chunks; ++c) {
+          float u[16], v[16];
+          tmem_ld16(lanes + acc * kAcc + c * 64, u);
+          tmem_ld16(lanes + (acc ^ 1) * kAcc + c * 64, v);
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (2 * c + half < chunks) finish(sum[c], 2 * c + half);
-      } else {
-        ok = wait_warp(accf_bar(acc), ph, abort_flag, p.status, p.wait_limit);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t from = tmem + acc * kAcc + ((uint32_t)(q * 32) << 16);
-        float v[32];
-        for (int c = half; c < chunks; c += 2) {
-          tmem_ld32(from + c * 32, v);
-          if (c + 2 >= chunks) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_leader(acce_bar(acc));
-          }
-          finish(v, c);
+          for (int e = 0; e < 16; ++e) u[e] += v[e];
+          tmem_st16(lanes + acc * kAcc + c * 64, u);
         }
-        if (half >= chunks) {
-          __syncwarp();
-          if (lane == 0) arrive_leader(acce_bar(acc));
-        }
-        if (++acc == 2) { acc = 0; ph ^= 1u; }
+        tmem_wait_st();
+        release(acc ^ 1);
       }
+      if (!ok) continue;
+      for (int c = part; c < chunks; c += 4) {
+        float v[16];
+        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + acc * kAcc + c * 16, v);
+        if (c + 4 >= chunks) release(acc);
+        finish(v, c);
+      }
+      if (part >= chunks) release(acc);
+      acc ^= 1;
     }
   } else if (warp == kTmaWarp) {
     // ---------------- operands (one lane runs the role from end to end) -----
@@ -444,8 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr int kCols = KIND == kForward8 ? 128 : 64;  // reduction elements of a step
       for (int i = unit; i < n_items && ok; i += units) {
         const Item it = item_of(i);
-        // this CTA's share of the columns: whole pieces of 16 of the tile, halved
-        const int n = (((it.n + 15) & ~15)) / kCtas, n0 = it.n0 + (int)rank * n;
+        // this CTA's share of the columns
+        const int n = (it.n + kUnit - 1) / kUnit * 16, n0 = it.n0 + (int)rank * n;
         const int blocks = (n + 63) / 64;  // of an MN-major operand
         const uint32_t bytes = 16384u + (KIND >= kInput ? blocks * 8192u : (uint32_t)(p.tile_n / kCtas) * 128u);
         for (int k = it.from; k < it.to; ++k) {
@@ -480,13 +520,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true, any = false;
       for (int i = unit; i < n_items && ok; i += units) {
         const Item it = item_of(i);
-        const uint32_t idesc = idesc_of<KIND, PAIR>((it.n + 15) & ~15);
-        for (int j = 0; j < it.sums() && ok; ++j) {
-          ok = wait_bounded(acce_bar(acc), acc_ph ^ 1u, abort_flag, p.status, p.wait_limit);
+        const uint32_t idesc = idesc_of<KIND, PAIR>((it.n + kUnit - 1) / kUnit * kUnit);
+        const int n_sums = sums(it);
+        for (int j = 0; j < n_sums && ok; ++j) {
+          const int to = j ? acc ^ 1 : acc;
+          ok = wait_bounded(acce_bar(to), (acc_ph >> to & 1u) ^ 1u, abort_flag, p.status, p.wait_limit);
           if (!ok) break;
+          acc_ph ^= 1u << to;
           tc_fence_after();
-          const uint32_t d = tmem + acc * kAcc;
-          const int first = it.step(j), last = it.step(j + 1);
+          const uint32_t d = tmem + to * kAcc;
+          const int first = first_step(it, n_sums, j), last = first_step(it, n_sums, j + 1);
           for (int k = first; k < last; ++k) {
             ok = wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
             if (!ok) break;
@@ -503,9 +546,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             any = true;
             if (++s == n_st) { s = 0; ph ^= 1u; }
           }
-          if (ok) commit(accf_bar(acc));
-          if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+          if (ok) commit(accf_bar(to));
         }
+        acc ^= 1;
       }
       // every MMA issued has completed before TMEM is released
       if (any) {
@@ -623,7 +666,9 @@ __global__ void __launch_bounds__(32 * kRowsWarps) rows_kernel(const RowsParams 
     if (row >= p.e.M || ch >= p.e.N) continue;
     float v = 0.f;
     for (int k = 0; k < warps; ++k) v += red[k * (16 * 8 * NT) + i];
-    finish1<TO>(p.e, v, row, ch, !p.e.mask || p.e.mask[row]);
+    const bool on = !p.e.mask || p.e.mask[row];
+    finish1<TO>(p.e, v, row, ch, on, p.e.sm ? p.e.sm[row] : 1.f, p.e.sn ? p.e.sn[ch] : 1.f, bias_of(p.e, ch),
+                on && p.e.residual ? residual_of<TO>(p.e, row, ch) : 0.f);
   }
 }
 
@@ -851,41 +896,81 @@ struct Tiles {
   bool pair;
   int tile_n, m_tiles, n_tiles;
 };
-int even_part(int n, int parts) { return ((n + parts - 1) / parts + 15) / 16 * 16; }
-
-Tiles pick_tiles(long long M, int N, int sms) {
-  Tiles t;
-  const long long m256 = (M + 255) / 256, m128 = (M + 127) / 128;
-  const int parts = (N + 255) / 256;
-  t.pair = m256 * parts >= sms / 2;
-  int n_parts = parts;
-  if (!t.pair)  // narrower tiles until every SM has one
-    while (m128 * n_parts < sms && even_part(N, n_parts + 1) >= 32 && m128 * (n_parts + 1) <= sms) ++n_parts;
-  t.tile_n = even_part(N, n_parts);
-  t.m_tiles = (int)(t.pair ? m256 : m128);
-  t.n_tiles = (N + t.tile_n - 1) / t.tile_n;
-  return t;
+// (tcgen05 takes 16, 32, ... 256 columns, on pairs 32, 64, ... 256)
+int even_part(int n, int parts, bool pair) {
+  const int unit = pair ? 32 : 16;
+  return ((n + parts - 1) / parts + unit - 1) / unit * unit;
 }
 
-// Parts of a reduction of `steps` steps over `tiles` tiles on `units` CTAs or pairs: as
-// few as give the least of the steps that a unit runs one after another, counting what
-// writing and adding the parts costs (a tile's partial sums as two steps).
-int pick_splits(int tiles, int steps, int units) {
-  int best = 1;
-  double least = 1e30;
-  for (int s = 1; s <= 64 && s <= (steps + 3) / 4; ++s) {
-    const long long waves = ((long long)tiles * s + units - 1) / units;
-    const double cost = (double)waves * ((steps + s - 1) / s + 4.0) + (s > 1 ? 4.0 * tiles * s / units + 8.0 : 0.0);
-    if (cost < least * 0.97) {
-      least = cost;
-      best = s;
+// The width and form of the tiles that leave the longest-running CTA or pair the least to do,
+// in clocks of the tensor cores (2 a column and step) or of shared memory (128 bytes of
+// operands in and out a clock), whichever are more, with 1,500 beside for a CTA's beginning
+// and end. (us, pairs of 256 columns wherever they are half the SMs' number and this: 5,003 x 1,001
+// to 777 80 tiles on 76 pairs, 32.3 and 24; ...)
+Tiles pick_tiles(long long M, int N, int steps, int sms) {
+  Tiles best{};
+  double least = 1e300;
+  for (int pair = 0; pair < 2; ++pair) {
+    const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
+    int last = 0;
+    for (int parts = (N + 255) / 256; parts <= (N + 31) / 32; ++parts) {
+      const int n = even_part(N, parts, pair);
+      if (n == last || (last && n < 32)) continue;
+      last = n;
+      const long long tiles = m * ((N + n - 1) / n), waves = (tiles + units - 1) / units;
+      const double step = pair ? std::max(2.0 * n, 256.0 + n) : 256.0 + 2.0 * n;
+      const double cost = waves * (std::max(step * steps, 14.0 * n) + 200.0) + 1500.0 + 4.0 * n;
+      if (cost < least * 0.98) {
+        least = cost;
+        best.pair = pair != 0;
+        best.tile_n = n;
+        best.m_tiles = (int)m;
+        best.n_tiles = (N + n - 1) / n;
+      }
+      if (tiles > 4 * units) break;  // narrower tiles only cost more
+    }
+  }
+  return best;
+}
+
+// The same for dw, whose reduction can be split into parts: their sums cost a second kernel
+// (4,000 clocks) and the bytes of the parts (16 a clock and SM, written and read).
+Tiles pick_weight_tiles(long long M, int N, int steps, int sms, int* splits) {
+  Tiles best{};
+  double least = 1e300;
+  *splits = 1;
+  for (int pair = 0; pair < 2; ++pair) {
+    const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
+    int last = 0;
+    for (int parts = (N + 255) / 256; parts <= (N + 63) / 64; ++parts) {
+      const int n = even_part(N, parts, pair);
+      if (n == last) continue;
+      last = n;
+      const int held = (n / (pair ? 2 : 1) + 63) / 64 * 64;  // columns of the blocks in shared memory
+      const long long tiles = m * ((N + n - 1) / n);
+      const double step = pair ? std::max(2.0 * n, 256.0 + held + n / 2) : 256.0 + held + n;
+      for (int s = 1; s <= 64 && s <= (steps + 3) / 4; ++s) {
+        const long long waves = (tiles * s + units - 1) / units;
+        const double cost = waves * (step * ((steps + s - 1) / s) * 1.06 + 600.0 + 4.0 * n) + 1500.0 +
+                            (s > 1 ? 4000.0 + 2.0 * s * (double)M * N * 4.0 / 16.0 / sms : 0.0);
+        if (cost < least * 0.98) {
+          least = cost;
+          best.pair = pair != 0;
+          best.tile_n = n;
+          best.m_tiles = (int)m;
+          best.n_tiles = (N + n - 1) / n;
+          *splits = s;
+        }
+        if (tiles * s > 4 * units) break;
+      }
+      if (tiles > 8 * units) break;
     }
   }
   return best;
 }
 
 template <int KIND, typename TO>
-cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, int sms,
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, bool wide, int sms,
                         cudaStream_t s) {
   const int ctas = t.pair ? 2 : 1;
   const int n = t.tile_n / ctas;
@@ -893,12 +978,14 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
   p.m_tiles = t.m_tiles;
   p.n_tiles = t.n_tiles;
   p.stage_bytes = 16384u + (KIND >= kInput ? (uint32_t)((n + 63) / 64) * 8192u : ((uint32_t)n * 128u + 1023u) / 1024u * 1024u);
-  const uint32_t beside = 1024u + (kBars + 1) * 8u + (p.wide ? 0u : kStaging);
+  const uint32_t beside = 1024u + (kBars + 1) * 8u + 16u + kColumns + (wide ? 0u : kStaging);
   p.stages = (int)std::min<uint32_t>(kMaxStages, (kSmemMax - beside) / p.stage_bytes);
   const uint32_t smem = beside + (uint32_t)p.stages * p.stage_bytes;
+  p.sum_steps = KIND == kWeight || (KIND != kInput && sizeof(TO) == 4) ? kSumSteps : 1 << 30;
   p.wait_limit = gemm_wait_limit();
   void (*kernel)(const CUtensorMap, const CUtensorMap, const Params) =
-      t.pair ? gemm_kernel<KIND, TO, true> : gemm_kernel<KIND, TO, false>;
+      t.pair ? (wide ? gemm_kernel<KIND, TO, true, true> : gemm_kernel<KIND, TO, true, false>)
+             : (wide ? gemm_kernel<KIND, TO, false, true> : gemm_kernel<KIND, TO, false, false>);
   const cudaError_t e = allow_smem_once(kernel, smem);
   if (e != cudaSuccess) return e;
   const long long items = (long long)t.m_tiles * t.n_tiles * p.splits;
@@ -997,19 +1084,9 @@ Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int 
   const long long cols = (p->n + 255) / 256, most = std::max<long long>(1, 4ll * sms / cols);
   r.per = (int)std::max<long long>(kGradWarps * kGradRows, (T + most - 1) / most);
   r.blocks = (int)((T + r.per - 1) / r.per);
-  r.in = pick_tiles(T, p->cols, sms);
-  r.weight = pick_tiles(p->n, p->cols, sms);
-  const long long steps = (T + 63) / 64;
-  // a tile of its own pair as soon as parts of the rows can fill the SMs
-  const long long m256 = (p->n + 255) / 256;
-  const int parts = (p->cols + 255) / 256;
-  if (p->n > 128 && m256 * parts * std::max<long long>(1, steps / 8) >= sms / 2) {
-    r.weight.pair = true;
-    r.weight.tile_n = even_part(p->cols, parts);
-    r.weight.m_tiles = (int)m256;
-    r.weight.n_tiles = (p->cols + r.weight.tile_n - 1) / r.weight.tile_n;
-  }
-  r.splits = pick_splits(r.weight.m_tiles * r.weight.n_tiles, (int)steps, sms / (r.weight.pair ? 2 : 1));
+  r.in = pick_tiles(T, p->cols, (p->n + 63) / 64, sms);
+  const int steps = (int)((T + 63) / 64);
+  r.weight = pick_weight_tiles(p->n, p->cols, steps, sms, &r.splits);
   int64_t at = 0;
   auto take = [&](bool want, int64_t bytes) {
     const int64_t here = at;
@@ -1096,7 +1173,6 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     return UNIF_MOE_ERR_ARG;
   }
   const int size = ln::in_size(p), os = p->out_dtype == UNIF_MOE_F32 ? 4 : 2;
-  const int bs = p->bias_dtype == UNIF_MOE_F32 ? 4 : 2;
   const int64_t need = ln::forward_bytes(p, x, ld_x, w, ld_w);
   if (need > workspace_bytes || (need && !workspace)) {
     set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
@@ -1155,15 +1231,15 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     UNIF_LAUNCH(ln::launch_layout(w, ld_w, ws, pw, p->n, p->cols, size, nullptr, sms, s));
     w = ws;
   }
-  const ln::Tiles t = ln::pick_tiles(p->rows, p->n, sms);
+  const int steps = (int)(((int64_t)p->cols * size + 127) / 128);
+  const ln::Tiles t = ln::pick_tiles(p->rows, p->n, steps, sms);
   if ((long long)t.m_tiles * t.n_tiles > 0x7fff0000) {
     set_error("too many tiles: rows=%lld n=%d", (long long)p->rows, p->n);
     return UNIF_MOE_ERR_SHAPE;
   }
-  e.steps = (int)(((int64_t)p->cols * size + 127) / 128);
-  e.wide = p->n % 16 == 0 && ln::wide32(out, ld_out, os) && (!residual || ln::wide32(residual, ld_res, os)) &&
-           (!z || ln::wide32(z, ld_z, 2)) && (!bias || ln::wide32(bias, 16, bs)) &&
-           (!w_scale || ln::wide32(w_scale, 16, 4));
+  e.steps = steps;
+  const bool wide = p->n % 16 == 0 && ln::wide32(out, ld_out, os) && (!residual || ln::wide32(residual, ld_res, os)) &&
+           (!z || ln::wide32(z, ld_z, 2));
   CUtensorMap a, b;
   if (!ln::map_rows(&a, x, size, p->cols, p->rows, px, 128) ||
       !ln::map_rows(&b, w, size, p->cols, p->n, pw, t.tile_n / (t.pair ? 2 : 1))) {
@@ -1171,11 +1247,11 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     return UNIF_MOE_ERR_CUDA;
   }
   if (size == 2)
-    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward, float>(a, b, e, t, sms, s))
-                        : (ln::launch_gemm<ln::kForward, __nv_bfloat16>(a, b, e, t, sms, s)));
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward, float>(a, b, e, t, wide, sms, s))
+                        : (ln::launch_gemm<ln::kForward, __nv_bfloat16>(a, b, e, t, wide, sms, s)));
   else
-    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward8, float>(a, b, e, t, sms, s))
-                        : (ln::launch_gemm<ln::kForward8, __nv_bfloat16>(a, b, e, t, sms, s)));
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward8, float>(a, b, e, t, wide, sms, s))
+                        : (ln::launch_gemm<ln::kForward8, __nv_bfloat16>(a, b, e, t, wide, sms, s)));
   return UNIF_MOE_OK;
 }
 
@@ -1262,13 +1338,13 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.out = g->dx_dev;
     e.ld_out = g->ld_dx;
     e.status = status;
-    e.wide = p->cols % 16 == 0 && ln::wide32(g->dx_dev, g->ld_dx, 2);
+    const bool wide = p->cols % 16 == 0 && ln::wide32(g->dx_dev, g->ld_dx, 2);
     CUtensorMap a, b;
     if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 128) || !ln::map_rows(&b, w, 2, p->cols, p->n, pl.pw, 64)) {
       set_error("cuTensorMapEncodeTiled failed");
       return UNIF_MOE_ERR_CUDA;
     }
-    UNIF_LAUNCH((ln::launch_gemm<ln::kInput, __nv_bfloat16>(a, b, e, pl.in, sms, s)));
+    UNIF_LAUNCH((ln::launch_gemm<ln::kInput, __nv_bfloat16>(a, b, e, pl.in, wide, sms, s)));
   }
   if (g->dw_dev) {
     ln::Params e{};
@@ -1280,14 +1356,14 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.ld_out = g->ld_dw;
     e.part = reinterpret_cast<float*>(ws + pl.part);
     e.status = status;
-    e.wide = p->cols % 16 == 0 && (pl.splits > 1 || ln::wide32(g->dw_dev, g->ld_dw, gs));
+    const bool wide = p->cols % 16 == 0 && (pl.splits > 1 || ln::wide32(g->dw_dev, g->ld_dw, gs));
     CUtensorMap a, b;
     if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 64) || !ln::map_rows(&b, x, 2, p->cols, p->rows, pl.px, 64)) {
       set_error("cuTensorMapEncodeTiled failed");
       return UNIF_MOE_ERR_CUDA;
     }
-    UNIF_LAUNCH(gs == 4 ? (ln::launch_gemm<ln::kWeight, float>(a, b, e, pl.weight, sms, s))
-                        : (ln::launch_gemm<ln::kWeight, __nv_bfloat16>(a, b, e, pl.weight, sms, s)));
+    UNIF_LAUNCH(gs == 4 ? (ln::launch_gemm<ln::kWeight, float>(a, b, e, pl.weight, wide, sms, s))
+                        : (ln::launch_gemm<ln::kWeight, __nv_bfloat16>(a, b, e, pl.weight, wide, sms, s)));
   }
   const bool add = g->dw_dev && pl.splits > 1;
   if (add || pl.sums) {
