@@ -701,6 +701,22 @@ bool encode_rows_map(CUtensorMap* map, const void* base, int size, uint64_t cols
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 3-D tensor map of planes of rows of bf16 or fp32 (size 2 or 4), rows `pitch` and planes `plane` bytes
+// apart, in boxes of 32 rows by box_cols, with a 64-byte swizzle or (0) none.
+bool encode_box_map(CUtensorMap* map, const void* base, int size, uint64_t cols, uint64_t rows, uint64_t planes,
+                    uint64_t pitch, uint64_t plane, uint32_t box_cols, int swizzle_bytes) {
+  tc::EncodeTiledFn fn = tc::encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {cols, rows, planes};
+  cuuint64_t strides[2] = {pitch, plane};
+  cuuint32_t box[3] = {box_cols, 32, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swizzle_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace tc {
 
 // N split into n_sub sub-tiles of bn columns: bn <= 256 and bn % 64 == 0, so

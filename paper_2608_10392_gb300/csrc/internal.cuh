@@ -322,6 +322,9 @@ bool encode_bf16_map(CUtensorMap* map, const void* base, uint64_t cols, uint64_t
                      uint32_t box_cols, uint32_t box_rows, int swizzle_bytes);  // clock cycles before a bounded wait gives up
 bool encode_rows_map(CUtensorMap* map, const void* base, int size, uint64_t cols, uint64_t rows,
                      uint64_t pitch, uint32_t box_cols, uint32_t box_rows);
+bool encode_box_map(CUtensorMap* map, const void* base, int size, uint64_t cols, uint64_t rows,
+                    uint64_t planes, uint64_t pitch, uint64_t plane, uint32_t box_cols,
+                    int swizzle_bytes);
 int router_tc_setup(unif_moe_layer* L);
 // Whether the tensor-core router's shared memory holds the grouping's
 // counters (and at least one tile of staged rows) for these sizes.

@@ -39,26 +39,33 @@ constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = kEpiThreads + 64;
 constexpr uint32_t kTmemCols = 512, kAcc = 256;
 constexpr int kMaxStages = 8;
-constexpr int kBars = 2 * kMaxStages + 5;
+constexpr int kBars = 2 * kMaxStages + 5 + 2 * kEpiWarps;
 constexpr uint32_t kSmemMax = 232448;
-constexpr uint32_t kStaging = kEpiWarps * 32 * 17 * 4;  // rows that no 32-byte stores fit
+// Staging of a storing warp: a box of 32 rows by 64 bytes, or two, and one for z; or, for rows that
+// TMA cannot write, 32 rows by 16 fp32 values. Two boxes with a residual, which comes there first,
+// and where a tile has few steps for its stores to hide behind (us, one box and two: 12,608 x 384 to
+// 1,536 19.3 and 18.2; 65,536 x 1,024 to 4,096 with GELU 360 and 335); they leave the ring a stage
+// less (the same without GELU 310 and 338).
+constexpr uint32_t kBox = 2048, kStagingOdd = kEpiWarps * 32 * 17 * 4;
 constexpr uint32_t kColumns = 2 * 2 * 256 * 4;          // bias and scales of two tiles
 // Steps that one accumulation for an fp32 result runs over. The tensor cores
 // truncate the accumulator at every MMA, so the error grows with their number: the sums of
 // longer reductions are added in fp32 (65,536 x 4,096 to 1,024 onto an fp32 residual: 2.5e-6 of the
 // result's norm off in one accumulation, 6e-7 so).
-constexpr int kSumSteps = 16;
+constexpr int kSumSteps = 22;
 
 struct Params {
   int M, N;                        // rows and columns of the result
   int steps, splits;               // steps of 128 operand bytes; parts of the reduction
   int sum_steps;                   // most steps of an accumulation
-  int tile_n, m_tiles, n_tiles;    // columns of a tile (a multiple of 16, on pairs of 32)
+  int tile_n, m_tiles, n_tiles;    // columns of a tile (a multiple of 32)
   int stages;
-  uint32_t stage_bytes;
+  uint32_t stage_bytes, boxes;     // boxes staged by a warp, of them `two` in turn for the result
+  bool two;
   bool gelu;
-  void* out;
+  void* out;                       // (through the tensor map where the rows allow that)
   long long ld_out;
+  bool own_rows;                   // what is between the rows of out belongs to the call too
   const float *sm, *sn;            // scales of rows and columns, or NULL
   const void* bias;
   bool bias_f32;
@@ -67,7 +74,6 @@ struct Params {
   const uint8_t* mask;
   __nv_bfloat16* z;
   long long ld_z;
-  float* part;                     // splits > 1: [splits][M][N]
   int* status;
   long long wait_limit;
 };
@@ -126,54 +132,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) 
       : "memory");
 }
 
+// 32 lanes x 16 columns without the wait: the registers are valid after tmem_wait_ld.
+__device__ __forceinline__ void tmem_ld16_async(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32"
+      " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+
 // ---- the epilogue's rows ----
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// Sixteen consecutive values (32-byte aligned bf16 or fp32).
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&v)[16]) {
-  uint32_t r[8];
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-                 "=r"(r[7])
-               : "l"(p)
-               : "memory");
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[2 * i] = __uint_as_float(r[i] << 16);
-    v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load16(const float* p, float (&v)[16]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=f"(v[8 * i]), "=f"(v[8 * i + 1]), "=f"(v[8 * i + 2]), "=f"(v[8 * i + 3]),
-                   "=f"(v[8 * i + 4]), "=f"(v[8 * i + 5]), "=f"(v[8 * i + 6]), "=f"(v[8 * i + 7])
-                 : "l"(p + 8 * i)
-                 : "memory");
-}
-__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
-  uint32_t h[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    h[i] = *reinterpret_cast<const uint32_t*>(&t);
-  }
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(h[0]), "r"(h[1]),
-               "r"(h[2]), "r"(h[3]), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7])
-               : "memory");
-}
-__device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 8 * i),
-                 "f"(v[8 * i]), "f"(v[8 * i + 1]), "f"(v[8 * i + 2]), "f"(v[8 * i + 3]), "f"(v[8 * i + 4]),
-                 "f"(v[8 * i + 5]), "f"(v[8 * i + 6]), "f"(v[8 * i + 7])
-                 : "memory");
-}
 
 // What becomes of two results: bf16 ones take the packed GELU (2^-12 of the value at most,
 // before a rounding of 2^-9), fp32 ones the library's.
@@ -187,48 +160,100 @@ __device__ __forceinline__ void act2(float& a, float& b) {
   }
 }
 
-// Sixteen columns of this thread's row, from column `ch` (a multiple of 16) on, all there. bias, sn:
-// their values for these columns in shared memory (read where p has them).
-template <typename TO>
-__device__ __forceinline__ void finish16(const Params& p, float (&v)[16], long long row, int ch, float scale,
-                                         bool on, const float* bias, const float* sn) {
-  TO* o = static_cast<TO*>(p.out) + row * p.ld_out + ch;
-  if (p.sn) {
+// Scales and bias on W columns of this thread's row (0 in padding rows), two at a time; `bias` and `sn`
+// of the columns are in shared memory.
+template <int W>
+__device__ __forceinline__ void finish_row(const Params& p, float (&v)[W], float scale, bool on, const float* bias,
+                                           const float* sn) {
+  const uint64_t s2 = pk2(scale, scale);
+  if (p.sm || p.sn || p.bias)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float4 c = *reinterpret_cast<const float4*>(sn + i);
-      v[i] *= scale * c.x;
-      v[i + 1] *= scale * c.y;
-      v[i + 2] *= scale * c.z;
-      v[i + 3] *= scale * c.w;
-    }
-  } else if (p.sm) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] *= scale;
-  }
-  if (p.bias)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float4 c = *reinterpret_cast<const float4*>(bias + i);
-      v[i] += c.x;
-      v[i + 1] += c.y;
-      v[i + 2] += c.z;
-      v[i + 3] += c.w;
+    for (int i = 0; i < W; i += 4) {
+      const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(sn + i);
+      const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(bias + i);
+      upk2(fma2(pk2(v[i], v[i + 1]), mul2(s2, c.x), b.x), v[i], v[i + 1]);
+      upk2(fma2(pk2(v[i + 2], v[i + 3]), mul2(s2, c.y), b.y), v[i + 2], v[i + 3]);
     }
   if (!on)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.f;
-  if (p.z) store16(p.z + row * p.ld_z + ch, v);
-  if (p.gelu)
+    for (int i = 0; i < W; ++i) v[i] = 0.f;
+}
+
+// This thread's row (64 bytes) of a staged box, 16 bytes at a time: TMA's 64-byte swizzle.
+__device__ __forceinline__ uint32_t box_at(uint32_t box, int row, int piece) {
+  return box + row * 64 + ((piece ^ (row >> 1 & 3)) << 4);
+}
+__device__ __forceinline__ void put4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ void put_row(uint32_t box, int row, const float (&v)[32]) {  // bf16
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) act2<TO>(v[i], v[i + 1]);
-  if (p.residual && on) {
-    float t[16];
-    load16(static_cast<const TO*>(p.residual) + row * p.ld_res + ch, t);
+  for (int i = 0; i < 4; ++i)
+    put4(box_at(box, row, i), pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
+         pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7]));
+}
+__device__ __forceinline__ void put_row(uint32_t box, int row, const float (&v)[16]) {  // fp32
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += t[i];
+  for (int i = 0; i < 4; ++i)
+    put4(box_at(box, row, i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+         __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+}
+__device__ __forceinline__ void put_z(uint32_t box, int row, const float (&v)[32]) { put_row(box, row, v); }
+__device__ __forceinline__ void put_z(uint32_t box, int row, const float (&v)[16]) {  // 32 bytes a row, no swizzle
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    put4(box + row * 32 + i * 16, pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
+         pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7]));
+}
+__device__ __forceinline__ void get4(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void add_row(uint32_t box, int row, float (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t r[4];
+    get4(box_at(box, row, i), r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[8 * i + 2 * k] += __uint_as_float(r[k] << 16);
+      v[8 * i + 2 * k + 1] += __uint_as_float(r[k] & 0xffff0000u);
+    }
   }
-  store16(o, v);
+}
+__device__ __forceinline__ void add_row(uint32_t box, int row, float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t r[4];
+    get4(box_at(box, row, i), r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[4 * i + k] += __uint_as_float(r[k]);
+  }
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(src), "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1,
+                                            int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+// The sources of all of this thread's bulk stores but the last N have been read.
+template <int N>
+__device__ __forceinline__ void bulk_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
 
 // One element.
@@ -258,11 +283,15 @@ __device__ __forceinline__ float residual_of(const Params& p, long long row, int
 // PAIR: the CTAs of a cluster of two share a tile of 256 rows (tcgen05 cta_group::2), 128 of
 // them and half of the columns' operand in each one's shared memory. The first CTA's
 // barriers take both CTAs' bytes, its MMA lane issues for both.
-// WIDE: all row accesses in whole pieces of 16 values.
+// WIDE: the rows of the result (and of z and the residual) are written and read by TMA, from and to
+// staged boxes of 32 rows by 64 bytes, which also cuts them off at the result's ends. (Written by the
+// threads, a row each, a store touches 32 lines and the storing warps are bound by that:
+// 12,608 x 384 to 1,536 with GELU and z 26 us ...)
 template <int KIND, typename TO, bool PAIR, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                const Params p) {
+                const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmRes,
+                const __grid_constant__ CUtensorMap tmZ, const Params p) {
   constexpr int kCtas = PAIR ? 2 : 1, kTileM = 128 * kCtas, kUnit = 16 * kCtas;  // columns of an MMA: whole units
   constexpr bool kParts = KIND == kWeight;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
@@ -273,17 +302,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t s0 = smem_u32(smem);
   const int n_st = p.stages;
   auto stage = [&](int s) { return s0 + (uint32_t)s * p.stage_bytes; };
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)n_st * p.stage_bytes);
+  // the ring, the staged boxes (512-byte aligned), barriers
+  uint8_t* staged = smem + (size_t)n_st * p.stage_bytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + (WIDE ? kEpiWarps * p.boxes * kBox : kStagingOdd));
   const uint32_t bar0 = smem_u32(bars);
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kMaxStages + s); };
   auto accf_bar = [&](int a) { return bar0 + 8u * (2 * kMaxStages + a); };
   auto acce_bar = [&](int a) { return bar0 + 8u * (2 * kMaxStages + 2 + a); };
   const uint32_t mma_done = bar0 + 8u * (2 * kMaxStages + 4);
+  auto box_bar = [&](int w, uint32_t k) { return bar0 + 8u * (2 * kMaxStages + 5 + 2 * w + (k & 1u)); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* columns = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(bars + kBars + 1) + 15) & ~(uintptr_t)15);
-  float* staging = columns + kColumns / 4;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -296,6 +327,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(acce_bar(a), kCtas * kEpiWarps);
     }
     mbar_init(mma_done, 1);
+    for (int w = 0; w < kEpiWarps; ++w) {
+      mbar_init(box_bar(w, 0), 1);
+      mbar_init(box_bar(w, 1), 1);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -336,14 +371,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto first_step = [&](const Item& it, int n, int j) {
     return it.from + (int)((long long)(it.to - it.from) * j / n);
   };
-  const int tiles = p.m_tiles * p.n_tiles, n_items = tiles * p.splits;
-  auto item_of = [&](int i) {
+  // The items of this CTA or pair one after another, i = unit + k units, without a division for each.
+  struct Walk {
+    int i, m, n, part;
+  };
+  const int n_items = p.m_tiles * p.n_tiles * p.splits;
+  const int by_m = units / p.n_tiles, by_n = units - by_m * p.n_tiles;
+  auto start = [&]() {
+    Walk w;
+    w.i = unit;
+    w.m = unit / p.n_tiles;
+    w.n = unit - w.m * p.n_tiles;
+    w.part = kParts ? w.m / p.m_tiles : 0;
+    w.m -= w.part * p.m_tiles;
+    return w;
+  };
+  auto next = [&](Walk& w) {
+    w.i += units;
+    w.m += by_m;
+    w.n += by_n;
+    if (w.n >= p.n_tiles) {
+      w.n -= p.n_tiles;
+      ++w.m;
+    }
+    if (kParts)
+      for (; w.m >= p.m_tiles; w.m -= p.m_tiles) ++w.part;
+  };
+  auto item_of = [&](const Walk& w) {
     Item it;
-    it.part = kParts ? i / tiles : 0;
-    const int t = kParts ? i - it.part * tiles : i;
-    const int m = t / p.n_tiles;
-    it.m0 = m * kTileM + 128 * (int)rank;
-    it.n0 = (t - m * p.n_tiles) * p.tile_n;
+    it.part = w.part;
+    it.m0 = w.m * kTileM + 128 * (int)rank;
+    it.n0 = w.n * p.tile_n;
     it.n = min(p.tile_n, p.N - it.n0);
     it.from = kParts ? (int)((long long)p.steps * it.part / p.splits) : 0;
     it.to = kParts ? (int)((long long)p.steps * (it.part + 1) / p.splits) : p.steps;
@@ -352,10 +410,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp < kEpiWarps) {
     // ---------------- accumulators to the result ----------------------------
-    // Four warps to a quarter of the rows, 16 columns at a time. (A wait given up is not the end
+    // Four warps to a quarter of the rows, W columns at a time. (A wait given up is not the end
     // of the loop: the warps meet at a barrier.)
+    constexpr int W = WIDE ? 64 / (int)sizeof(TO) : 16;
     const int q = warp & 3, part = warp >> 2;
-    float* stg = staging + warp * (32 * 17);
     int acc = 0;       // the accumulator of the item's sum
     uint32_t ph = 0;   // a phase bit per accumulator
     bool ok = true;
@@ -369,107 +427,190 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) arrive_leader(acce_bar(a));
     };
-    const bool per_column = p.bias || p.sn;
-    // the columns' bias (the first 256 threads) and scales (the others), on their way a tile ahead
-    auto column = [&](int i) {
-      const Item it = item_of(i);
-      const int c = it.n0 + (int)(threadIdx.x & 255u);
-      if ((int)(threadIdx.x & 255u) >= it.n) return 0.f;
-      if (threadIdx.x < 256) return bias_of(p, c);
-      return p.sn ? p.sn[c] : 1.f;
+    // pieces of W columns of an item in this warp's rows (a quarter past the last row has none)
+    auto pieces = [&](const Item& it) { return it.m0 + q * 32 < p.M ? (it.n + W - 1) / W : 0; };
+    // The pieces of this warp one after another, over the items.
+    struct Piece {
+      Walk at;
+      int c, n0, m0, of;  // of its item: first column and row, pieces
     };
-    float ahead = per_column && unit < n_items ? column(unit) : 0.f;
+    auto enter = [&](Piece& e) {
+      const Item it = item_of(e.at);
+      e.c = part;
+      e.n0 = it.n0;
+      e.m0 = it.m0;
+      e.of = e.at.i < n_items ? pieces(it) : 0;
+    };
+    auto first_piece = [&]() {
+      Piece e;
+      e.at = start();
+      enter(e);
+      return e;
+    };
+    auto settle = [&](Piece& e) {  // the piece, or the next one there is; false after the last
+      while (e.c >= e.of) {
+        if (e.at.i >= n_items) return false;
+        next(e.at);
+        enter(e);
+      }
+      return true;
+    };
+    const bool per_column = KIND < kInput && (p.bias || p.sn || p.sm);
+    // The columns' bias (the first 256 threads) and scales (the others), on their way a tile ahead. (Each
+    // warp its own columns, without the barrier: 12,608 x 384 to 1,536 16.3 us and 18.7.)
+    auto column = [&](const Walk& w) {
+      const int c = (int)(threadIdx.x & 255u), n0 = w.n * p.tile_n;
+      if (c >= min(p.tile_n, p.N - n0)) return 0.f;
+      if (threadIdx.x < 256) return bias_of(p, n0 + c);
+      return p.sn ? p.sn[n0 + c] : 1.f;
+    };
+    Walk ahead = start();
+    float in_columns = per_column && ahead.i < n_items ? column(ahead) : 0.f;
     int turn = 0;
-    for (int i = unit; i < n_items; i += units, turn ^= 1) {
-      const Item it = item_of(i);
-      float* bias = columns + turn * 512;
+    // WIDE: boxes this warp has staged, and the residual's boxes on their way (two ahead)
+    const bool with_res = WIDE && KIND < kInput && p.residual;
+    const uint32_t box0 = smem_u32(staged) + warp * p.boxes * kBox, two = p.two ? kBox : 0u;
+    uint32_t k = 0, fetched = 0;
+    Piece coming = first_piece();
+    auto fetch = [&]() {  // the residual of the next piece, to the box that will hold its result
+      if (!settle(coming)) return;
+      if (lane == 0) {
+        mbar_expect_tx(box_bar(warp, fetched), kBox);
+        tma_load_3d(box0 + (fetched & 1u) * two, &tmRes, box_bar(warp, fetched),
+                    coming.n0 + coming.c * W, coming.m0 + q * 32, 0);
+      }
+      ++fetched;
+      coming.c += 4;
+    };
+    if (with_res) {
+      fetch();
+      fetch();
+    }
+    for (Walk at = start(); at.i < n_items; next(at), turn ^= 512) {
+      const Item it = item_of(at);
+      const float* cols = columns + turn;
       if (per_column) {
-        bias[threadIdx.x] = ahead;
+        columns[turn + threadIdx.x] = in_columns;
         asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
-        if (i + units < n_items) ahead = column(i + units);
+        next(ahead);
+        if (ahead.i < n_items) in_columns = column(ahead);
       }
       const long long row = (long long)it.m0 + q * 32 + lane;
       const bool there = row < p.M;
-      // (a quarter past the last row has nothing to store)
-      const int chunks = it.m0 + q * 32 < p.M ? (it.n + 15) / 16 : 0;
+      const int n_pieces = pieces(it);
       bool on = there;
       float scale = 1.f;
-      if (there && p.mask) on = p.mask[row] != 0;
-      if (there && p.sm) scale = p.sm[row];
-      // 16 columns from column c * 16 of the tile on
-      auto finish = [&](float (&v)[16], int c) {
-        const int ch = it.n0 + c * 16, count = it.n - c * 16;
-        const bool parts = kParts && p.splits > 1;
-        if constexpr (WIDE) {
-          if (!there) return;
-          if (parts) store16(p.part + ((long long)it.part * p.M + row) * p.N + ch, v);
-          else if constexpr (KIND >= kInput) store16(static_cast<TO*>(p.out) + row * p.ld_out + ch, v);
-          else finish16<TO>(p, v, row, ch, scale, on, bias + c * 16, bias + 256 + c * 16);
-          return;
-        }
-        // a lane per column instead, two rows at a time: rows of any width and alignment
-        if constexpr (!WIDE) {
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 16; ++j) stg[lane * 17 + j] = v[j];
-        __syncwarp();
-        const uint32_t live = __ballot_sync(0xffffffffu, on);
-        const int col = lane & 15;
-        const float sn = per_column ? bias[256 + c * 16 + col] : 1.f, b = per_column ? bias[c * 16 + col] : 0.f;
-#pragma unroll 1
-        for (int r0 = lane >> 4; r0 < 32; r0 += 16) {
-          float res[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int r = r0 + 2 * k;
-            res[k] = 0.f;
-            if (p.residual && (live >> r & 1u) && col < count) res[k] = residual_of<TO>(p, row - lane + r, ch + col);
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int r = r0 + 2 * k;
-            const float sm = __shfl_sync(0xffffffffu, scale, r);
-            if (row - lane + r >= p.M || col >= count) continue;
-            const float x = stg[r * 17 + col];
-            if (parts) p.part[((long long)it.part * p.M + row - lane + r) * p.N + ch + col] = x;
-            else if constexpr (KIND >= kInput) put(static_cast<TO*>(p.out) + (row - lane + r) * p.ld_out + ch + col, x);
-            else finish1<TO>(p, x, row - lane + r, ch + col, live >> r & 1u, sm, sn, b, res[k]);
-          }
-        }
-        }
-      };
-      if constexpr (WIDE)  // the residual's rows, on their way to L2 while the sums are taken
-        if (KIND < kInput && p.residual && on)
-          for (int c = part; c < chunks; c += 4)
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const TO*>(p.residual) + row * p.ld_res +
-                                                          it.n0 + c * 16));
-      const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + part * 16;
+      if (KIND < kInput && there && p.mask) on = p.mask[row] != 0;
+      if (KIND < kInput && there && p.sm) scale = p.sm[row];
+      const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
       const int n_sums = sums(it);
       wait_acc(acc);
       for (int j = 1; j < n_sums; ++j) {  // further accumulations, added to the first
         wait_acc(acc ^ 1);
         if (!ok) break;
-        for (int c = 0; 4 * c + part < chunks; ++c) {
-          float u[16], v[16];
-          tmem_ld16(lanes + acc * kAcc + c * 64, u);
-          tmem_ld16(lanes + (acc ^ 1) * kAcc + c * 64, v);
+        for (int c = part; c < n_pieces; c += 4)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] += v[e];
-          tmem_st16(lanes + acc * kAcc + c * 64, u);
-        }
+          for (int h = 0; h < W; h += 16) {
+            uint32_t u[16], v[16];
+            tmem_ld16_async(lanes + acc * kAcc + c * W + h, u);
+            tmem_ld16_async(lanes + (acc ^ 1) * kAcc + c * W + h, v);
+            tmem_wait_ld();
+            float w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(u[e]) + __uint_as_float(v[e]);
+            tmem_st16(lanes + acc * kAcc + c * W + h, w);
+          }
         tmem_wait_st();
         release(acc ^ 1);
       }
       if (!ok) continue;
-      for (int c = part; c < chunks; c += 4) {
-        float v[16];
-        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + acc * kAcc + c * 16, v);
-        if (c + 4 >= chunks) release(acc);
-        finish(v, c);
+      for (int c = part; c < n_pieces; c += 4) {
+        float v[W];
+        if constexpr (W == 32) tmem_ld32(lanes + acc * kAcc + c * W, v);
+        else tmem_ld16(lanes + acc * kAcc + c * W, v);
+        if (c + 4 >= n_pieces) release(acc);
+        const int ch = it.n0 + c * W;
+        if constexpr (WIDE) {
+          if constexpr (KIND < kInput) finish_row<W>(p, v, scale, on, cols + c * W, cols + 256 + c * W);
+          const uint32_t box = box0 + (k & 1u) * two, z_box = box0 + two + kBox;
+          if (with_res) {
+            ok = wait_warp(box_bar(warp, k), k >> 1 & 1u, abort_flag, p.status, p.wait_limit);
+            if (!ok) break;
+          } else {
+            if (lane == 0) {  // the box's last piece has gone out (and z's)
+              if (p.two) bulk_read<1>();
+              else bulk_read<0>();
+            }
+            __syncwarp();
+          }
+          if constexpr (KIND < kInput) {
+            if (p.z) {
+              put_z(z_box, lane, v);
+              fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&tmZ, z_box, ch, it.m0 + q * 32, 0);
+                bulk_commit();
+              }
+            }
+            if (p.gelu)
+#pragma unroll
+              for (int e = 0; e < W; e += 2) act2<TO>(v[e], v[e + 1]);
+            if (with_res && on) add_row(box, lane, v);
+          }
+          put_row(box, lane, v);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_3d(&tmOut, box, ch, it.m0 + q * 32, it.part);
+            bulk_commit();
+          }
+          ++k;
+          if (with_res) {
+            if (lane == 0) bulk_read<0>();
+            fetch();
+          }
+        } else {
+          // a lane per column, two rows at a time: rows of any width and alignment
+          float* stg = reinterpret_cast<float*>(staged) + warp * (32 * 17);
+          const int count = it.n - c * W;
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) stg[lane * 17 + j] = v[j];
+          __syncwarp();
+          const uint32_t live = __ballot_sync(0xffffffffu, on);
+          const int col = lane & 15;
+          const float sn = per_column ? cols[256 + c * W + col] : 1.f, b = per_column ? cols[c * W + col] : 0.f;
+#pragma unroll 1
+          for (int r0 = lane >> 4; r0 < 32; r0 += 16) {
+            float res[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int r = r0 + 2 * e;
+              res[e] = 0.f;
+              if (KIND < kInput && p.residual && (live >> r & 1u) && col < count)
+                res[e] = residual_of<TO>(p, row - lane + r, ch + col);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int r = r0 + 2 * e;
+              const float sm = __shfl_sync(0xffffffffu, scale, r);
+              if (row - lane + r >= p.M || col >= count) continue;
+              const float x = stg[r * 17 + col];
+              if constexpr (KIND >= kInput) put(static_cast<TO*>(p.out) + (row - lane + r) * p.ld_out + ch + col, x);
+              else finish1<TO>(p, x, row - lane + r, ch + col, live >> r & 1u, sm, sn, b, res[e]);
+            }
+          }
+        }
       }
-      if (part >= chunks) release(acc);
+      if (part >= n_pieces) release(acc);
       acc ^= 1;
     }
+    if (WIDE && lane == 0) {
+      for (; k < fetched; ++k) wait_settle(box_bar(warp, k), k >> 1 & 1u, p.wait_limit / 16);  // (after a wait given up)
+      bulk_wait_all();
+    }
+    __syncwarp();
   } else if (warp == kTmaWarp) {
     // ---------------- operands (one lane runs the role from end to end) -----
     if (elect_one()) {
@@ -482,8 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         else tma_load_2d(dst, from, bar, c0, c1);
       };
       constexpr int kCols = KIND == kForward8 ? 128 : 64;  // reduction elements of a step
-      for (int i = unit; i < n_items && ok; i += units) {
-        const Item it = item_of(i);
+      for (Walk at = start(); at.i < n_items && ok; next(at)) {
+        const Item it = item_of(at);
         // this CTA's share of the columns
         const int n = (it.n + kUnit - 1) / kUnit * 16, n0 = it.n0 + (int)rank * n;
         const int blocks = (n + 63) / 64;  // of an MN-major operand
@@ -518,8 +659,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0, acc = 0;
       uint32_t ph = 0, acc_ph = 0;
       bool ok = true, any = false;
-      for (int i = unit; i < n_items && ok; i += units) {
-        const Item it = item_of(i);
+      for (Walk at = start(); at.i < n_items && ok; next(at)) {
+        const Item it = item_of(at);
         const uint32_t idesc = idesc_of<KIND, PAIR>((it.n + kUnit - 1) / kUnit * kUnit);
         const int n_sums = sums(it);
         for (int j = 0; j < n_sums && ok; ++j) {
@@ -710,92 +851,87 @@ struct GradParams {
 };
 constexpr int kGradWarps = 8, kGradRows = 4;  // rows in flight of a warp
 
+// Eight values as they are read: consecutive ones (VEC), or every 32nd.
+template <typename T, bool VEC>
+struct Eight {
+  uint32_t r[VEC ? 8 * sizeof(T) / 4 : 8];
+  __device__ __forceinline__ void read(const T* p, int left) {  // left: values up to the row's end from p on
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+        r[4 * i] = a.x; r[4 * i + 1] = a.y; r[4 * i + 2] = a.z; r[4 * i + 3] = a.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] = 32 * k < left ? __float_as_uint(to_f32(p[32 * k])) : 0u;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(r) / 4); ++k) r[k] = 0u;
+  }
+  __device__ __forceinline__ float get(int k) const {
+    if constexpr (VEC && sizeof(T) == 2) return __uint_as_float(k & 1 ? r[k / 2] & 0xffff0000u : r[k / 2] << 16);
+    else return __uint_as_float(r[k]);
+  }
+};
+
 // dz = dout act'(z), and the column sums of the CTA's rows: 256 columns by `per` rows, a warp to
 // every eighth row, eight columns a lane (VEC: consecutive ones).
 template <typename TD, bool VEC>
-__global__ void __launch_bounds__(32 * kGradWarps) grad_kernel(const GradParams p) {
+__global__ void __launch_bounds__(32 * kGradWarps, VEC ? 3 : 2) grad_kernel(const GradParams p) {
   __shared__ float red[kGradWarps][256];
   grid_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int c0 = blockIdx.x * 256;
   auto column = [&](int k) { return c0 + (VEC ? lane * 8 + k : lane + 32 * k); };
-  const bool on_cols = !VEC || column(0) < p.n;
+  const bool on_cols = column(0) < p.n;
   const long long first = (long long)blockIdx.y * p.per, last = min(p.rows, first + p.per);
   float sum[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum[k] = 0.f;
   const TD* dout = static_cast<const TD*>(p.dout);
   for (long long r0 = first + warp; r0 < last; r0 += kGradWarps * kGradRows) {
-    float d[kGradRows][8], z[kGradRows][8];
-    bool on[kGradRows];
+    Eight<TD, VEC> d[kGradRows];
+    Eight<__nv_bfloat16, VEC> z[kGradRows];
 #pragma unroll
     for (int u = 0; u < kGradRows; ++u) {
       const long long r = r0 + u * kGradWarps;
-      on[u] = r < last && on_cols && (!p.mask || p.mask[r]);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) d[u][k] = z[u][k] = 0.f;
-      if (!on[u]) continue;
-      if constexpr (VEC) {
-        if constexpr (sizeof(TD) == 4) {
-          const float4* q = reinterpret_cast<const float4*>(dout + r * p.ld_dout + column(0));
-          const float4 a = __ldcs(q), b = __ldcs(q + 1);
-          d[u][0] = a.x; d[u][1] = a.y; d[u][2] = a.z; d[u][3] = a.w;
-          d[u][4] = b.x; d[u][5] = b.y; d[u][6] = b.z; d[u][7] = b.w;
-        } else {
-          const uint4 a = *reinterpret_cast<const uint4*>(dout + r * p.ld_dout + column(0));
-          const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            d[u][2 * k] = __uint_as_float(w[k] << 16);
-            d[u][2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-          }
-        }
-        if (p.z) {
-          const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p.z + r * p.ld_z + column(0)));
-          const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            z[u][2 * k] = __uint_as_float(w[k] << 16);
-            z[u][2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (column(k) < p.n) {
-            d[u][k] = to_f32(dout[r * p.ld_dout + column(k)]);
-            if (p.z) z[u][k] = __bfloat162float(p.z[r * p.ld_z + column(k)]);
-          }
+      if (r < last && on_cols && (!p.mask || p.mask[r])) {
+        d[u].read(dout + r * p.ld_dout + column(0), p.n - column(0));
+        if (p.z) z[u].read(p.z + r * p.ld_z + column(0), p.n - column(0));
+      } else {  // (GELU's derivative of 0 is finite: padding rows give 0)
+        d[u].clear();
+        z[u].clear();
       }
     }
 #pragma unroll
     for (int u = 0; u < kGradRows; ++u) {
       const long long r = r0 + u * kGradWarps;
       if (r >= last || !on_cols) continue;
-      if (p.z && on[u])
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = d[u].get(k);
+      if (p.z)
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
           float a, b;
-          gelu::gelu_grad2(z[u][k], z[u][k + 1], a, b);
-          d[u][k] *= a;
-          d[u][k + 1] *= b;
+          gelu::gelu_grad2(z[u].get(k), z[u].get(k + 1), a, b);
+          v[k] *= a;
+          v[k + 1] *= b;
         }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum[k] += d[u][k];
+      for (int k = 0; k < 8; ++k) sum[k] += v[k];
       if (!p.dz) continue;
       __nv_bfloat16* o = p.dz + r * p.ld_dz;
       if constexpr (VEC) {
-        uint32_t h[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const __nv_bfloat162 t = __floats2bfloat162_rn(d[u][2 * k], d[u][2 * k + 1]);
-          h[k] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        *reinterpret_cast<uint4*>(o + column(0)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(o + column(0)) =
+            make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if (column(k) < p.n) o[column(k)] = __float2bfloat16_rn(d[u][k]);
+          if (column(k) < p.n) o[column(k)] = __float2bfloat16_rn(v[k]);
       }
     }
   }
@@ -813,10 +949,10 @@ __global__ void __launch_bounds__(32 * kGradWarps) grad_kernel(const GradParams 
 }
 
 struct FinishParams {
-  const float* part;  // [splits][M][N]
+  const float* part;  // [splits][M][pitch]
   int splits;
   long long M;
-  int N;
+  int N, pitch;
   void* dw;
   long long ld_dw;
   const float* sums;  // [blocks][n]
@@ -831,28 +967,27 @@ __global__ void __launch_bounds__(256) finish_kernel(const FinishParams p) {
   __shared__ float red[8][32];
   grid_dep_wait();
   if ((int)blockIdx.x < p.dw_ctas) {
-    const long long total = p.M * p.N, pieces = (total + 3) / 4;
-    const bool vec = p.N % 4 == 0;
+    const int per_row = p.pitch / 4;
+    const long long plane = p.M * p.pitch, pieces = p.M * per_row;
+    const bool vec = sizeof(TG) == 4 && p.N % 4 == 0 && p.ld_dw % 4 == 0 && reinterpret_cast<uintptr_t>(p.dw) % 16 == 0;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces;
          i += (long long)p.dw_ctas * 256) {
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
       for (int s = 0; s < p.splits; ++s) {
-        const float* q = p.part + s * total + i * 4;
-        if (vec) {
-          const float4 t = __ldcs(reinterpret_cast<const float4*>(q));
-          v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (i * 4 + k < total) v[k] += q[k];
-        }
+        const float4 t = __ldcs(reinterpret_cast<const float4*>(p.part + s * plane + i * 4));
+        v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
       }
+      const long long row = i / per_row;
+      const int c = (int)(i - row * per_row) * 4;
+      TG* to = static_cast<TG*>(p.dw) + row * p.ld_dw + c;
+      if (vec) {
+        *reinterpret_cast<float4*>(to) = v;
+      } else {
+        const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const long long e = i * 4 + k;
-        if (e >= total) break;
-        const long long row = e / p.N;
-        put(static_cast<TG*>(p.dw) + row * p.ld_dw + (e - row * p.N), v[k]);
+        for (int k = 0; k < 4; ++k)
+          if (c + k < p.N) put(to + k, e[k]);
       }
     }
     return;
@@ -882,6 +1017,8 @@ bool tma_rows(const void* p, long long ld, int size) { return bits(p) % 16 == 0 
 
 long long pitch_of(int cols, int size) { return ((long long)cols * size + 15) / 16 * 16 / size; }
 
+long long part_pitch(int cols) { return (cols + 3) / 4 * 4; }  // fp32 values between rows of parts
+
 int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Map of rows [rows][cols] of elements of `size` bytes (bf16, or 8-bit), `ld` apart: boxes of
@@ -896,11 +1033,8 @@ struct Tiles {
   bool pair;
   int tile_n, m_tiles, n_tiles;
 };
-// (tcgen05 takes 16, 32, ... 256 columns, on pairs 32, 64, ... 256)
-int even_part(int n, int parts, bool pair) {
-  const int unit = pair ? 32 : 16;
-  return ((n + parts - 1) / parts + unit - 1) / unit * unit;
-}
+// (whole boxes of 32 columns; on pairs tcgen05 takes 32, 64, ... 256)
+int even_part(int n, int parts) { return ((n + parts - 1) / parts + 31) / 32 * 32; }
 
 // The width and form of the tiles that leave the longest-running CTA or pair the least to do,
 // in clocks of the tensor cores (2 a column and step) or of shared memory (128 bytes of
@@ -914,7 +1048,7 @@ Tiles pick_tiles(long long M, int N, int steps, int sms) {
     const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
     int last = 0;
     for (int parts = (N + 255) / 256; parts <= (N + 31) / 32; ++parts) {
-      const int n = even_part(N, parts, pair);
+      const int n = even_part(N, parts);
       if (n == last || (last && n < 32)) continue;
       last = n;
       const long long tiles = m * ((N + n - 1) / n), waves = (tiles + units - 1) / units;
@@ -943,7 +1077,7 @@ Tiles pick_weight_tiles(long long M, int N, int steps, int sms, int* splits) {
     const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
     int last = 0;
     for (int parts = (N + 255) / 256; parts <= (N + 63) / 64; ++parts) {
-      const int n = even_part(N, parts, pair);
+      const int n = even_part(N, parts);
       if (n == last) continue;
       last = n;
       const int held = (n / (pair ? 2 : 1) + 63) / 64 * 64;  // columns of the blocks in shared memory
@@ -969,21 +1103,51 @@ Tiles pick_weight_tiles(long long M, int N, int steps, int sms, int* splits) {
   return best;
 }
 
+// The result's side of a launch: maps of its rows, the residual's and z's where TMA can take
+// all of them.
+struct Out {
+  bool wide;
+  CUtensorMap out, res, z;
+};
+template <typename TO>
+bool map_out(Out* o, const Params& p) {
+  constexpr int size = sizeof(TO), box = 64 / size;
+  // (a store is cut off at whole 16 bytes: what is behind a row's end must be nobody's else)
+  auto fits = [&](const void* q, long long ld, int bytes) {
+    return !q || (bits(q) % 16 == 0 && ld * bytes % 16 == 0 && (p.own_rows || (long long)p.N * bytes % 16 == 0));
+  };
+  o->wide = fits(p.out, p.ld_out, size) && fits(p.residual, p.ld_res, size) && fits(p.z, p.ld_z, 2);
+  if (!o->wide) return true;
+  const uint64_t plane = (uint64_t)p.M * p.ld_out * size;
+  if (!encode_box_map(&o->out, p.out, size, p.N, p.M, p.splits, p.ld_out * size, plane, box, 64)) return false;
+  o->res = o->z = o->out;
+  if (p.residual && !encode_box_map(&o->res, p.residual, size, p.N, p.M, 1, p.ld_res * size, p.ld_res * size * (uint64_t)p.M, box, 64))
+    return false;
+  return !p.z || encode_box_map(&o->z, p.z, 2, p.N, p.M, 1, p.ld_z * 2, p.ld_z * 2 * (uint64_t)p.M, box, size == 2 ? 64 : 0);
+}
+
 template <int KIND, typename TO>
-cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, bool wide, int sms,
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, int sms,
                         cudaStream_t s) {
+  Out o{};
+  if (!map_out<TO>(&o, p)) return cudaErrorInvalidValue;
+  const bool wide = o.wide;
   const int ctas = t.pair ? 2 : 1;
   const int n = t.tile_n / ctas;
   p.tile_n = t.tile_n;
   p.m_tiles = t.m_tiles;
   p.n_tiles = t.n_tiles;
   p.stage_bytes = 16384u + (KIND >= kInput ? (uint32_t)((n + 63) / 64) * 8192u : ((uint32_t)n * 128u + 1023u) / 1024u * 1024u);
-  const uint32_t beside = 1024u + (kBars + 1) * 8u + 16u + kColumns + (wide ? 0u : kStaging);
+  p.two = p.residual || p.steps <= 8 || (p.gelu && p.steps < 32);
+  p.boxes = (p.two ? 2u : 1u) + (p.z ? 1u : 0u);
+  const uint32_t beside =
+      1024u + (kBars + 1) * 8u + 16u + kColumns + (wide ? kEpiWarps * p.boxes * kBox : kStagingOdd);
   p.stages = (int)std::min<uint32_t>(kMaxStages, (kSmemMax - beside) / p.stage_bytes);
   const uint32_t smem = beside + (uint32_t)p.stages * p.stage_bytes;
   p.sum_steps = KIND == kWeight || (KIND != kInput && sizeof(TO) == 4) ? kSumSteps : 1 << 30;
   p.wait_limit = gemm_wait_limit();
-  void (*kernel)(const CUtensorMap, const CUtensorMap, const Params) =
+  void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                 const Params) =
       t.pair ? (wide ? gemm_kernel<KIND, TO, true, true> : gemm_kernel<KIND, TO, true, false>)
              : (wide ? gemm_kernel<KIND, TO, false, true> : gemm_kernel<KIND, TO, false, false>);
   const cudaError_t e = allow_smem_once(kernel, smem);
@@ -1002,7 +1166,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = t.pair ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a, b, p);
+  return cudaLaunchKernelEx(&cfg, kernel, a, b, o.out, o.res, o.z, p);
 }
 
 template <int SIZE, int NT, typename TO>
@@ -1096,7 +1260,7 @@ Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int 
   r.x = take(r.copy_x, T * r.px * 2);
   r.w = take(r.copy_w, (int64_t)p->n * r.pw * 2);
   r.dz = take(r.make_dz, T * r.pz * 2);
-  r.part = take(g->dw_dev && r.splits > 1, (int64_t)r.splits * p->n * p->cols * 4);
+  r.part = take(g->dw_dev && r.splits > 1, (int64_t)r.splits * p->n * part_pitch(p->cols) * 4);
   r.bias = take(r.sums, (int64_t)r.blocks * p->n * 4);
   r.total = at;
   return r;
@@ -1125,8 +1289,6 @@ int check_grad(const unif_moe_linear* p, const unif_moe_linear_grad* g) {
   }
   return UNIF_MOE_OK;
 }
-
-bool wide32(const void* p, long long ld, int size) { return bits(p) % 32 == 0 && ld * size % 32 == 0; }
 
 }  // namespace lin
 }  // namespace unif
@@ -1238,8 +1400,6 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     return UNIF_MOE_ERR_SHAPE;
   }
   e.steps = steps;
-  const bool wide = p->n % 16 == 0 && ln::wide32(out, ld_out, os) && (!residual || ln::wide32(residual, ld_res, os)) &&
-           (!z || ln::wide32(z, ld_z, 2));
   CUtensorMap a, b;
   if (!ln::map_rows(&a, x, size, p->cols, p->rows, px, 128) ||
       !ln::map_rows(&b, w, size, p->cols, p->n, pw, t.tile_n / (t.pair ? 2 : 1))) {
@@ -1247,11 +1407,11 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     return UNIF_MOE_ERR_CUDA;
   }
   if (size == 2)
-    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward, float>(a, b, e, t, wide, sms, s))
-                        : (ln::launch_gemm<ln::kForward, __nv_bfloat16>(a, b, e, t, wide, sms, s)));
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward, float>(a, b, e, t, sms, s))
+                        : (ln::launch_gemm<ln::kForward, __nv_bfloat16>(a, b, e, t, sms, s)));
   else
-    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward8, float>(a, b, e, t, wide, sms, s))
-                        : (ln::launch_gemm<ln::kForward8, __nv_bfloat16>(a, b, e, t, wide, sms, s)));
+    UNIF_LAUNCH(os == 4 ? (ln::launch_gemm<ln::kForward8, float>(a, b, e, t, sms, s))
+                        : (ln::launch_gemm<ln::kForward8, __nv_bfloat16>(a, b, e, t, sms, s)));
   return UNIF_MOE_OK;
 }
 
@@ -1338,13 +1498,12 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.out = g->dx_dev;
     e.ld_out = g->ld_dx;
     e.status = status;
-    const bool wide = p->cols % 16 == 0 && ln::wide32(g->dx_dev, g->ld_dx, 2);
     CUtensorMap a, b;
     if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 128) || !ln::map_rows(&b, w, 2, p->cols, p->n, pl.pw, 64)) {
       set_error("cuTensorMapEncodeTiled failed");
       return UNIF_MOE_ERR_CUDA;
     }
-    UNIF_LAUNCH((ln::launch_gemm<ln::kInput, __nv_bfloat16>(a, b, e, pl.in, wide, sms, s)));
+    UNIF_LAUNCH((ln::launch_gemm<ln::kInput, __nv_bfloat16>(a, b, e, pl.in, sms, s)));
   }
   if (g->dw_dev) {
     ln::Params e{};
@@ -1352,18 +1511,18 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.N = p->cols;
     e.splits = pl.splits;
     e.steps = (int)((p->rows + 63) / 64);
-    e.out = g->dw_dev;
-    e.ld_out = g->ld_dw;
-    e.part = reinterpret_cast<float*>(ws + pl.part);
+    // parts of the sum go to the workspace
+    e.out = pl.splits > 1 ? ws + pl.part : g->dw_dev;
+    e.ld_out = pl.splits > 1 ? ln::part_pitch(p->cols) : g->ld_dw;
+    e.own_rows = pl.splits > 1;
     e.status = status;
-    const bool wide = p->cols % 16 == 0 && (pl.splits > 1 || ln::wide32(g->dw_dev, g->ld_dw, gs));
     CUtensorMap a, b;
     if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 64) || !ln::map_rows(&b, x, 2, p->cols, p->rows, pl.px, 64)) {
       set_error("cuTensorMapEncodeTiled failed");
       return UNIF_MOE_ERR_CUDA;
     }
-    UNIF_LAUNCH(gs == 4 ? (ln::launch_gemm<ln::kWeight, float>(a, b, e, pl.weight, wide, sms, s))
-                        : (ln::launch_gemm<ln::kWeight, __nv_bfloat16>(a, b, e, pl.weight, wide, sms, s)));
+    UNIF_LAUNCH(gs == 4 || pl.splits > 1 ? (ln::launch_gemm<ln::kWeight, float>(a, b, e, pl.weight, sms, s))
+                                         : (ln::launch_gemm<ln::kWeight, __nv_bfloat16>(a, b, e, pl.weight, sms, s)));
   }
   const bool add = g->dw_dev && pl.splits > 1;
   if (add || pl.sums) {
@@ -1372,6 +1531,7 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     q.splits = pl.splits;
     q.M = p->n;
     q.N = p->cols;
+    q.pitch = (int)ln::part_pitch(p->cols);
     q.dw = g->dw_dev;
     q.ld_dw = g->ld_dw;
     q.sums = reinterpret_cast<const float*>(ws + pl.bias);
