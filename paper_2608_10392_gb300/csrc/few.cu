@@ -8,12 +8,17 @@
 //
 // - up_kernel: every CTA takes the tokens' decisions for itself (up to 8 tokens; more are
 //   decided by route_kernel, a CTA a token), lists the pairs in use, and its warps take tiles of
-//   16 keys of a pair: x and keys go from memory to mma.sync fragments, a thread's 32
-//   bytes standing for other features than the fragment's, the same ones for both operands. The
-//   tokens of a pair are gathered: columns of the product are those that run it.
-// - down_kernel: a cluster of CTAs takes 16 or 32 output features, its warps chunks of 64 channels
-//   of the pairs in use in turn; the warps' sums meet in shared memory, the CTAs' in the cluster's,
-//   added in a fixed order.
+//   16 keys of a pair. The tokens of a pair are gathered: columns of the product are those that run it.
+// - down_kernel: a cluster of CTAs takes 16 output features, its warps the pairs in turn, or 64 channels
+//   of them where pairs are few. Columns are again a pair's tokens; a warp adds them to its sums of
+//   all tokens in shared memory. The warps' sums meet there, the CTAs' in the cluster's, in a fixed
+//   order.
+//
+// Weights stream through a ring of a warp's own in shared memory (cp.async, 2 KB a stage), so that what
+// is on its way does not depend on registers; the products are mma.sync, a thread's 32 bytes of a row
+// standing for other positions than the fragment's, the same ones for both operands, which a sum
+// does not notice. (Weights straight into registers: 24 tokens of the 33-expert layer 67 and 118 us
+// in the two kernels, of 277 MB each.)
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -48,7 +53,7 @@ struct Params {
   float* s;                       // [T][K] affinities
   int* n_pairs;                   // pairs in use, in the order of (expert, block)
   uint16_t* pair;                 // [G]
-  uint64_t* members;              // [G] tokens of each
+  uint64_t* members;              // [B + K] tokens whose shared set has a block, that take an expert
   __nv_bfloat16* h;               // [K + 1][T][H], of the pairs' tokens
 };
 
@@ -60,13 +65,52 @@ __device__ __forceinline__ void clear(Piece& p) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) p.r[i] = 0u;
 }
-// Weights: read once, kept out of the way of x in L1 (32-byte aligned).
-__device__ __forceinline__ void read_weights(Piece& p, const __nv_bfloat16* from) {
-  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(p.r[0]), "=r"(p.r[1]), "=r"(p.r[2]), "=r"(p.r[3]), "=r"(p.r[4]), "=r"(p.r[5]), "=r"(p.r[6]),
-                 "=r"(p.r[7])
-               : "l"(from));
-}
+// A warp's ring of weights: stages of 16 rows by 128 bytes, 16 bytes of a row at the place that the
+// row's number mixes (so that fragments are read without bank conflicts).
+constexpr uint32_t kStage = 2048;
+template <int S>
+struct Ring {
+  uint32_t base;
+  int lane, put = 0, get = 0;
+  __device__ __forceinline__ Ring(uint32_t base_, int lane_) : base(base_), lane(lane_) {}
+  // 16 rows `ld` elements apart from `from` on, on their way to the next stage (nothing where `on` is
+  // false); the stage read last must not be in use any more
+  __device__ __forceinline__ void fetch(bool on, const __nv_bfloat16* from, long long ld) {
+    __syncwarp();
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = (lane >> 3) + 4 * i, piece = lane & 7;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + put * kStage + row * 128 +
+                                                                      ((piece ^ (row & 7)) << 4)),
+                     "l"(from + row * ld + piece * 8)
+                     : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    put = put + 1 == S ? 0 : put + 1;
+  }
+  // The oldest stage's fragments: rows g and g + 8 of this thread.
+  __device__ __forceinline__ void read(Piece& lo, Piece& hi) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+    __syncwarp();
+    const int g = lane >> 2, c = (lane & 3) * 2;
+    const uint32_t row = base + get * kStage + g * 128;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t at = row + (((c + h) ^ g) << 4);
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(lo.r[4 * h]), "=r"(lo.r[4 * h + 1]), "=r"(lo.r[4 * h + 2]), "=r"(lo.r[4 * h + 3])
+                   : "r"(at)
+                   : "memory");
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(hi.r[4 * h]), "=r"(hi.r[4 * h + 1]), "=r"(hi.r[4 * h + 2]), "=r"(hi.r[4 * h + 3])
+                   : "r"(at + 1024)
+                   : "memory");
+    }
+    get = get + 1 == S ? 0 : get + 1;
+  }
+};
 // Tokens (16-byte aligned).
 __device__ __forceinline__ void read_token(Piece& p, const __nv_bfloat16* from) {
   const uint4 a = *reinterpret_cast<const uint4*>(from), b = *(reinterpret_cast<const uint4*>(from) + 1);
@@ -123,11 +167,13 @@ __device__ __forceinline__ void decide(const Params& p, int t, bool valid, const
     // ranks of the blocks, ranks of the experts and the mass up to each
     int rb[2] = {0, 0}, re[2] = {0, 0};
     float mass[2] = {0.f, 0.f};
-    for (int i = 0; i < B && !p.prefix; ++i) {
+#pragma unroll 8
+    for (int i = 0; i < (p.prefix ? 0 : B); ++i) {
       const float v = __shfl_sync(0xffffffffu, i < 32 ? u[0] : u[1], i & 31);
 #pragma unroll
       for (int k = 0; k < 2; ++k) rb[k] += v > u[k] || (v == u[k] && i < lane + 32 * k);
     }
+#pragma unroll 8
     for (int i = 0; i < K; ++i) {
       const float v = __shfl_sync(0xffffffffu, i < 32 ? l[0] : l[1], i & 31);
       const float w = __shfl_sync(0xffffffffu, i < 32 ? e[0] : e[1], i & 31);
@@ -249,27 +295,35 @@ struct UpShared {
   int found[kWarps + 1];
   uint8_t slots[kWarps][kMost];          // a warp's tokens of its pair
 };
-// after it: [G] pairs in use, then (kTogether tokens) the affinities [8][K] and the router's product
+constexpr int kUpStages = 6;
+// After it: the affinities [8][K] where the decisions are taken here, [G] pairs in use, then the rings
+// (before they are in use, the router's product in their place).
+__host__ __device__ inline size_t up_fixed(int G, int K, bool routes) {
+  return ((sizeof(UpShared) + (size_t)G * 2 + (routes ? 32 * (size_t)K : 0)) + 127) / 128 * 128 + 128;
+}
 __host__ __device__ inline size_t up_smem(int G, int K, int C, bool routes) {
-  size_t n = (sizeof(UpShared) + 15) / 16 * 16 + ((size_t)G * 2 + 15) / 16 * 16;
-  if (routes) n += 4 * ((size_t)8 * K + route_floats(C));
-  return n;
+  const size_t rings = (size_t)kWarps * kUpStages * kStage, product = routes ? 4 * (size_t)route_floats(C) : 0;
+  return up_fixed(G, K, routes) + (rings > product ? rings : product);
 }
 
-// NT: pieces of eight tokens. ROUTES: the decisions are taken here.
+// NT: pieces of eight tokens that are taken at once; a pair that more tokens run is gone through again.
+// ROUTES: the decisions are taken here.
 template <int NT, bool ROUTES>
-__global__ void __launch_bounds__(kThreads, NT <= 4 ? 2 : 1) up_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
   extern __shared__ __align__(16) uint8_t raw[];
   UpShared& sh = *reinterpret_cast<UpShared*>(raw);
-  uint16_t* list = reinterpret_cast<uint16_t*>(raw + (sizeof(UpShared) + 15) / 16 * 16);
   const int G = (p.K + 1) * p.B;
-  float* s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(list) + ((size_t)G * 2 + 15) / 16 * 16);
+  float* s = reinterpret_cast<float*>(raw + sizeof(UpShared));               // [8][K]
+  uint16_t* list = reinterpret_cast<uint16_t*>(s + (ROUTES ? 8 * p.K : 0));  // [G]
+  static_assert(sizeof(UpShared) % 8 == 0, "what follows is aligned");
+  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(raw));
+  const uint32_t rings = (base + (uint32_t)up_fixed(G, p.K, ROUTES) - 1u) & ~127u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool first = blockIdx.x == 0;
   grid_dep_wait();
   grid_dep_launch();
   if constexpr (ROUTES) {
-    const float* z = route_products(p, 0, p.T, s + 8 * p.K);
+    const float* z = route_products(p, 0, p.T, reinterpret_cast<float*>(raw + (rings - base)));
     if (warp < p.T) {
       uint64_t shr, em;
       float alpha;
@@ -326,34 +380,63 @@ __global__ void __launch_bounds__(kThreads, NT <= 4 ? 2 : 1) up_kernel(const Par
     const uint64_t m = members(i);
     if (m == 0ull) continue;
     list[at] = (uint16_t)i;
-    if (first) {
-      p.pair[at] = (uint16_t)i;
-      p.members[at] = m;
-    }
+    if (first) p.pair[at] = (uint16_t)i;
     ++at;
   }
   if (first && threadIdx.x == 0) *p.n_pairs = all;
   __syncthreads();
 
-  // tiles of 16 keys
-  const int tiles = p.M / 16;
-  const long long items = (long long)all * tiles;
+  if (first)
+    for (int i = threadIdx.x; i < p.B + p.K; i += kThreads)
+      p.members[i] = i < p.B ? sh.in_block[i] : sh.in_expert[i - p.B];
+
+  // tiles of 16 keys, in blocks of 64 features
+  const int tiles = p.M / 16, blocks = p.d / 64;
+  const long long items = (long long)all * tiles, step = (long long)gridDim.x * kWarps;
   const int g = lane >> 2, k0 = (lane & 3) * 16;
-  uint8_t* slots = sh.slots[warp];
-  for (long long i = (long long)warp * gridDim.x + blockIdx.x; i < items; i += (long long)gridDim.x * kWarps) {
+  uint8_t* slots_all = sh.slots[warp];
+  auto keys_of = [&](long long i) {
+    const int pair = list[i / tiles], row = (int)(i % tiles) * 16;
+    const int e = pair / p.B, b = pair - e * p.B;
+    return p.up + ((long long)e * p.H + b * p.M + row) * p.d;
+  };
+  Ring<kUpStages> ring(rings + (uint32_t)warp * kUpStages * kStage, lane);
+  long long next = (long long)warp * gridDim.x + blockIdx.x;  // of the blocks on their way
+  int next_f = 0, again = 0;  // times that the item's blocks are needed once more
+  const __nv_bfloat16* keys = nullptr;
+  auto enter = [&]() {
+    if (next >= items) return;
+    keys = keys_of(next);
+    again = p.T <= 8 * NT ? 0 : (__popcll(members(list[next / tiles])) - 1) / (8 * NT);
+  };
+  enter();
+  auto fetch = [&]() {
+    ring.fetch(next < items, keys + next_f, p.d);
+    if ((next_f += 64) == p.d) {
+      next_f = 0;
+      if (--again < 0) {
+        next += step;
+        enter();
+      }
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kUpStages - 1; ++k) fetch();
+  for (long long i = (long long)warp * gridDim.x + blockIdx.x; i < items; i += step) {
     const int pair = list[i / tiles], row = (int)(i % tiles) * 16;
     const int e = pair / p.B, b = pair - e * p.B;
     const uint64_t m = members(pair);
-    const int tokens = __popcll(m), pieces = (tokens + 7) / 8;
+    const int all_tokens = __popcll(m);
     __syncwarp();
 #pragma unroll
-    for (int k = 0; k < (NT + 3) / 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       const int t = lane + 32 * k;
-      if (m >> t & 1ull) slots[__popcll(m & ((1ull << t) - 1ull))] = (uint8_t)t;
+      if (m >> t & 1ull) slots_all[__popcll(m & ((1ull << t) - 1ull))] = (uint8_t)t;
     }
     __syncwarp();
-    const __nv_bfloat16* w0 = p.up + ((long long)e * p.H + b * p.M + row + g) * p.d + k0;
-    const __nv_bfloat16* w1 = w0 + 8ll * p.d;
+    for (int s0 = 0; s0 < all_tokens; s0 += 8 * NT) {
+    const uint8_t* slots = slots_all + s0;
+    const int tokens = min(all_tokens - s0, 8 * NT), pieces = (tokens + 7) / 8;
     const __nv_bfloat16* x[NT];
     float c[NT][4];
 #pragma unroll
@@ -363,36 +446,20 @@ __global__ void __launch_bounds__(kThreads, NT <= 4 ? 2 : 1) up_kernel(const Par
 #pragma unroll
       for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
     }
-    constexpr int U = 4;  // weights of 64 features in flight
-    int f = 0;
-    for (; f + 64 * U <= p.d; f += 64 * U) {
-      Piece lo[U], hi[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        read_weights(lo[u], w0 + f + 64 * u);
-        read_weights(hi[u], w1 + f + 64 * u);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          if (t < pieces) {
-            Piece v;
-            read_token(v, x[t] + f + 64 * u);
-            multiply(c[t], lo[u], hi[u], v);
-          }
-    }
-    for (; f < p.d; f += 64) {
+    Piece v;
+    read_token(v, x[0]);
+    for (int f = 0; f < blocks; ++f) {
       Piece lo, hi;
-      read_weights(lo, w0 + f);
-      read_weights(hi, w1 + f);
+      fetch();
+      ring.read(lo, hi);
+      multiply(c[0], lo, hi, v);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int t = 1; t < NT; ++t)
         if (t < pieces) {
-          Piece v;
-          read_token(v, x[t] + f);
+          read_token(v, x[t] + 64 * f);
           multiply(c[t], lo, hi, v);
         }
+      if (f + 1 < blocks) read_token(v, x[0] + 64 * (f + 1));
     }
     // h = w GeLU, rounded once: the weight comes before the rounding, so that the down projection
     // adds up what is held
@@ -413,77 +480,133 @@ __global__ void __launch_bounds__(kThreads, NT <= 4 ? 2 : 1) up_kernel(const Par
         h[(long long)tok * p.H + 8] = __float2bfloat16_rn(w * c[t][2 + j]);
       }
     }
+    }
   }
 }
 
 // ---- y ----
 
-// MT: tiles of 16 output features of a cluster. Shared memory: the warps' sums [warps][16 MT][8 NT],
-// then the CTA's [16 MT][8 NT].
-template <int NT, int MT>
-constexpr size_t down_smem() { return 4u * (kWarps + 1) * 16 * MT * 8 * NT; }
+// Stages such that two CTAs are on an SM. Shared memory: the masks, the pairs in use [G], the warps'
+// sums [warps][TOK tokens][16], the CTA's, the rings.
+__host__ __device__ constexpr int down_stages(int TOK) { return TOK <= 32 ? 5 : 4; }
+template <int TOK>
+constexpr size_t down_smem(int G) {
+  return 128 * 8 + ((size_t)G * 2 + 15) / 16 * 16 + 4u * (kWarps + 1) * 16 * TOK + 128 +
+         (size_t)kWarps * down_stages(TOK) * kStage;
+}
 
-template <int NT, int MT>
-__global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) down_kernel(const Params p, const int ctas) {
-  extern __shared__ __align__(16) float red[];
-  constexpr int kSums = 16 * MT * 8 * NT;
+// NT as in up_kernel; TOK: most tokens.
+template <int NT, int TOK>
+__global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const int ctas) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  __shared__ uint8_t slots_of[kWarps][kMost];
+  constexpr int kSums = 16 * TOK, S = down_stages(TOK);
+  const int G = (p.K + 1) * p.B;
+  uint64_t* masks = reinterpret_cast<uint64_t*>(raw);
+  uint16_t* list = reinterpret_cast<uint16_t*>(masks + 128);
+  float* red = reinterpret_cast<float*>(raw + 128 * 8 + ((size_t)G * 2 + 15) / 16 * 16);
+  const uint32_t rings = ((uint32_t)__cvta_generic_to_shared(red + (kWarps + 1) * kSums) + 127u) & ~127u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x % ctas, j0 = blockIdx.x / ctas * (16 * MT);
+  const int rank = blockIdx.x % ctas, j0 = blockIdx.x / ctas * 16;
   const int g = lane >> 2, k0 = (lane & 3) * 16;
-  float c[MT][NT][4];
+  float* mine = red + warp * kSums;  // [token][feature]
+  for (int i = lane; i < kSums; i += 32) mine[i] = 0.f;
+  uint8_t* slots_all = slots_of[warp];
+  grid_dep_wait();
+  const int pairs = *p.n_pairs;
+  for (int i = threadIdx.x; i < p.B + p.K; i += kThreads) masks[i] = p.members[i];
+  for (int i = threadIdx.x; i < pairs; i += kThreads) list[i] = p.pair[i];
+  __syncthreads();
+  // items: whole pairs where every warp of the cluster has several, else their chunks of 64 channels
+  const int per = p.M / 64, units = ctas * kWarps;
+  const int length = pairs >= 8 * units ? per : 1, cuts = per / length, items = pairs * cuts;
+  const __nv_bfloat16* rows = p.down + (long long)j0 * p.H;
+  struct At {
+    int i, k, again, e, b, ch;  // item, chunk of it, times that it is needed once more; expert, block,
+  };                            // first channel of the chunk
+  auto members = [&](const At& a) {
+    return a.e == 0 ? masks[a.b] : masks[p.B + a.e - 1] & ~masks[a.b];
+  };
+  auto enter = [&](At& a) {
+    const int at = a.i / cuts, pair = list[at];
+    a.k = 0;
+    a.e = pair / p.B;
+    a.b = pair - a.e * p.B;
+    a.ch = a.b * p.M + (a.i - at * cuts) * length * 64;
+    a.again = TOK <= 8 * NT ? 0 : (__popcll(members(a)) - 1) / (8 * NT);
+  };
+  At next{warp * ctas + rank, 0, 0, 0, 0, 0};
+  if (next.i < items) enter(next);
+  Ring<S> ring(rings + (uint32_t)warp * S * kStage, lane);
+  auto fetch = [&]() {
+    const bool on = next.i < items;
+    ring.fetch(on, rows + (long long)next.e * p.d * p.H + next.ch, p.H);
+    if (!on) return;
+    next.ch += 64;
+    if (++next.k == length) {
+      if (--next.again >= 0) {
+        next.k = 0;
+        next.ch -= 64 * length;
+      } else {
+        next.i += units;
+        if (next.i < items) enter(next);
+      }
+    }
+  };
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+  for (int k = 0; k < S - 1; ++k) fetch();
+  constexpr int P = NT < 2 ? NT : 2;  // pieces of h that are read a chunk ahead
+  for (At at{warp * ctas + rank, 0, 0, 0, 0, 0}; at.i < items; at.i += units) {
+    enter(at);
+    const uint64_t m = members(at);
+    const int all_tokens = __popcll(m);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < (TOK + 31) / 32; ++k) {
+      const int t = lane + 32 * k;
+      if (m >> t & 1ull) slots_all[__popcll(m & ((1ull << t) - 1ull))] = (uint8_t)t;
+    }
+    __syncwarp();
+    for (int s0 = 0; s0 < all_tokens; s0 += 8 * NT) {
+    const uint8_t* slots = slots_all + s0;
+    const int tokens = min(all_tokens - s0, 8 * NT), pieces = (tokens + 7) / 8;
+    const __nv_bfloat16* h[NT];  // (columns past the pair's tokens repeat its first one)
+    float c[NT][4];
+    Piece v[P];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int slot = t * 8 + g;
+      h[t] = p.h + ((long long)at.e * p.T + slots[slot < tokens ? slot : 0]) * p.H + at.ch + k0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
+      if (t < P && t < pieces) read_token(v[t < P ? t : 0], h[t]);
+    }
+    for (int k = 0; k < length; ++k) {
+      Piece lo, hi;
+      fetch();
+      ring.read(lo, hi);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (t < pieces) {
+          if (t < P) {
+            multiply(c[t], lo, hi, v[t < P ? t : 0]);
+            if (k + 1 < length) read_token(v[t < P ? t : 0], h[t] + (k + 1) * 64);
+          } else {
+            Piece w;
+            read_token(w, h[t] + k * 64);
+            multiply(c[t], lo, hi, w);
+          }
+        }
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c[i][t][j] = 0.f;
-  grid_dep_wait();
-  const int per = p.M / 64, chunks = *p.n_pairs * per, step = ctas * kWarps;
-  constexpr int U = 4 / MT;  // chunks whose weights are in flight
-  for (int i0 = warp * ctas + rank; i0 < chunks; i0 += step * U) {
-    Piece lo[U][MT], hi[U][MT];
-    const __nv_bfloat16* h[U];
-    uint64_t m[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * step;
-      m[u] = 0ull;
-      if (i >= chunks) continue;
-      const int at = i / per, pair = p.pair[at];
-      const int e = pair / p.B, ch = (pair - e * p.B) * p.M + (i - at * per) * 64 + k0;
-      m[u] = p.members[at];
-      const __nv_bfloat16* w = p.down + ((long long)e * p.d + j0 + g) * p.H + ch;
-#pragma unroll
-      for (int k = 0; k < MT; ++k) {
-        read_weights(lo[u][k], w + (long long)(16 * k) * p.H);
-        read_weights(hi[u][k], w + (long long)(16 * k + 8) * p.H);
-      }
-      h[u] = p.h + (long long)e * p.T * p.H + ch;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (m[u] == 0ull) continue;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if ((m[u] >> (8 * t) & 255ull) == 0ull) continue;
-        Piece v;
-        clear(v);
-        const int tok = t * 8 + g;
-        if (m[u] >> tok & 1ull) read_token(v, h[u] + (long long)tok * p.H);
-#pragma unroll
-        for (int k = 0; k < MT; ++k) multiply(c[k][t], lo[u][k], hi[u][k], v);
+      for (int j = 0; j < 4; ++j) {
+        const int slot = t * 8 + (lane & 3) * 2 + (j & 1);
+        if (slot < tokens) mine[slots[slot] * 16 + g + (j >> 1) * 8] += c[t][j];
       }
     }
   }
-  // [feature][token]
-  float* mine = red + warp * kSums;
-#pragma unroll
-  for (int k = 0; k < MT; ++k)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        mine[(16 * k + g + (j >> 1) * 8) * (8 * NT) + t * 8 + (lane & 3) * 2 + (j & 1)] = c[k][t][j];
   __syncthreads();
   float* sums = red + kWarps * kSums;
   for (int i = threadIdx.x; i < kSums; i += kThreads) {
@@ -494,19 +617,17 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) down_kernel(const P
   }
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   // each CTA adds a share of the cluster's sums
-  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(sums));
-  for (int i = rank * kThreads + threadIdx.x; i < kSums; i += ctas * kThreads) {
-    const int f = i % (16 * MT), t = i / (16 * MT);  // consecutive features to consecutive threads
-    if (t >= p.T) continue;
+  const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(sums));
+  for (int i = rank * kThreads + threadIdx.x; i < 16 * p.T; i += ctas * kThreads) {
     float v = 0.f;
     for (int r = 0; r < ctas; ++r) {
       uint32_t there;
       float a;
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(base + 4u * (f * (8 * NT) + t)), "r"(r));
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here + 4u * i), "r"(r));
       asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a) : "r"(there) : "memory");
       v += a;
     }
-    p.out[t * p.ld_out + j0 + f] = __float2bfloat16_rn(v);
+    p.out[(i >> 4) * p.ld_out + j0 + (i & 15)] = __float2bfloat16_rn(v);
   }
   // no CTA leaves while another reads its sums
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -582,7 +703,7 @@ Parts parts_of(const unif_moe_few* p) {
   r.s = take(4 * T * p->n_experts);
   r.n_pairs = take(4);
   r.pair = take(2 * G);
-  r.members = take(8 * G);
+  r.members = take(8 * (p->n_blocks + p->n_experts));
   r.h = take(2 * (p->n_experts + 1) * T * p->d_ff);
   r.total = at;
   return r;
@@ -608,7 +729,7 @@ cudaError_t launch_cluster(void (*kernel)(const Params, const int), int grid, in
   return cudaLaunchKernelEx(&cfg, kernel, p, ctas);
 }
 
-template <int NT>
+template <int NT, int TOK>
 cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
   const int G = (p.K + 1) * p.B;
   const bool routes = p.T <= kTogether;
@@ -624,20 +745,20 @@ cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
   if constexpr (NT == 1) up = up_kernel<1, true>;
   else up = up_kernel<NT, false>;
   e = allow_smem_once(up, smem);
-  if (e == cudaSuccess) e = launch_dependent(up, dim3((NT <= 4 ? 2 : 1) * sms), dim3(kThreads), smem, s, p);
+  if (e == cudaSuccess) e = launch_dependent(up, dim3(2 * sms), dim3(kThreads), smem, s, p);
   if (e != cudaSuccess) return e;
-  // clusters of 32 output features, as many CTAs in each as the SMs hold at once
-  constexpr int MT = 2;
-  const int groups = p.d / (16 * MT), slots = (NT <= 2 ? 2 : 1) * sms;
-  const int ctas = std::max(1, std::min(8, slots / groups));
-  return launch_cluster(down_kernel<NT, MT>, groups, ctas, down_smem<NT, MT>(), s, p);
+  // a cluster to 16 output features, of as many CTAs as the SMs hold at once
+  const int groups = p.d / 16, slots = 2 * sms;
+  int ctas = 8;
+  while (ctas > 1 && groups * ctas > slots) ctas /= 2;
+  return launch_cluster(down_kernel<NT, TOK>, groups, ctas, down_smem<TOK>(G), s, p);
 }
 
 cudaError_t launch(const Params& p, int sms, cudaStream_t s) {
-  if (p.T <= 8) return launch_as<1>(p, sms, s);
-  if (p.T <= 16) return launch_as<2>(p, sms, s);
-  if (p.T <= 32) return launch_as<4>(p, sms, s);
-  return launch_as<8>(p, sms, s);
+  if (p.T <= 8) return launch_as<1, 8>(p, sms, s);
+  if (p.T <= 16) return launch_as<2, 16>(p, sms, s);
+  if (p.T <= 32) return launch_as<4, 32>(p, sms, s);
+  return launch_as<4, 64>(p, sms, s);
 }
 
 bool off(const void* p, uintptr_t by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }
