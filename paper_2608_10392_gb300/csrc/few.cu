@@ -30,7 +30,8 @@
 namespace unif {
 namespace few {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;  // of route_kernel and down_kernel
+constexpr int kUpWarps = 16;  // one CTA an SM: fewer read the router
 constexpr int kMost = UNIF_MOE_FEW_TOKENS;
 constexpr int kTogether = 8;  // most tokens that every CTA decides for itself
 
@@ -52,9 +53,34 @@ struct Params {
   float* alpha;                   // [T]
   float* s;                       // [T][K] affinities
   int* n_pairs;                   // pairs in use, in the order of (expert, block)
-  uint16_t* pair;                 // [G]
+  uint16_t* pair;                 // [G], as pair_code
   uint64_t* members;              // [B + K] tokens whose shared set has a block, that take an expert
   __nv_bfloat16* h;               // [K + 1][T][H], of the pairs' tokens
+};
+
+// A pair as it is listed, expert and block without a division.
+__device__ __forceinline__ uint16_t pair_code(int e, int b) { return (uint16_t)(e << 6 | b); }
+__device__ __forceinline__ int expert_of(int code) { return code >> 6; }
+__device__ __forceinline__ int block_of(int code) { return code & 63; }
+
+// Every `step`-th of the (pair, part) items, `parts` to a pair, without a division for each.
+struct Walk {
+  int pair, part;
+  int by_pair, by_part, parts;
+  __device__ __forceinline__ Walk(int first, int step, int parts_) : parts(parts_) {
+    pair = first / parts_;
+    part = first - pair * parts_;
+    by_pair = step / parts_;
+    by_part = step - by_pair * parts_;
+  }
+  __device__ __forceinline__ void next() {
+    pair += by_pair;
+    part += by_part;
+    if (part >= parts) {
+      part -= parts;
+      ++pair;
+    }
+  }
 };
 
 // Thirty-two bytes: sixteen bf16 values as eight operand registers.
@@ -210,9 +236,10 @@ __device__ __forceinline__ void decide(const Params& p, int t, bool valid, const
 
 // Shared memory of the router's product: [warps][rows of the router, in 16s][8 tokens], then [8][C].
 __host__ __device__ inline int router_rows(int C) { return (C + 15) / 16 * 16; }
-__host__ __device__ inline int route_floats(int C) { return kWarps * router_rows(C) * 8 + 8 * C; }
+__host__ __device__ inline int route_floats(int C, int warps) { return warps * router_rows(C) * 8 + 8 * C; }
 
-// z [8][C] of the tokens from t0 on (up to 8): the warps share the features.
+// z [8][C] of the tokens from t0 on (up to 8): the CTA's warps share the features.
+template <int WARPS>
 __device__ __forceinline__ float* route_products(const Params& p, int t0, int count, float* sm) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, at = (lane & 3) * 16;
   const int R = router_rows(p.C);
@@ -225,7 +252,7 @@ __device__ __forceinline__ float* route_products(const Params& p, int t0, int co
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[k][i] = 0.f;
-    for (int f = warp * 64; f < p.d; f += kWarps * 64) {
+    for (int f = warp * 64; f < p.d; f += WARPS * 64) {
       Piece v, lo[4], hi[4];
       clear(v);
       if (there) read_token(v, x + f);
@@ -251,12 +278,12 @@ __device__ __forceinline__ float* route_products(const Params& p, int t0, int co
     }
   }
   __syncthreads();
-  float* z = sm + kWarps * R * 8;
-  for (int i = threadIdx.x; i < 8 * p.C; i += kThreads) {
+  float* z = sm + WARPS * R * 8;
+  for (int i = threadIdx.x; i < 8 * p.C; i += WARPS * 32) {
     const int n = i & 7, r = i >> 3;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += sm[w * R * 8 + r * 8 + n];
+    for (int w = 0; w < WARPS; ++w) v += sm[w * R * 8 + r * 8 + n];
     z[n * p.C + r] = v;
   }
   __syncthreads();
@@ -270,7 +297,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const Params p) {
   grid_dep_launch();
   const int t = blockIdx.x;
   const bool valid = !p.mask || p.mask[t];
-  const float* z = route_products(p, t, 1, sm);
+  const float* z = route_products<kWarps>(p, t, 1, sm);
   if (threadIdx.x >= 32) return;
   uint64_t shr, em;
   float alpha;
@@ -292,8 +319,8 @@ struct UpShared {
   uint64_t shr[kMost], em[kMost];
   uint64_t in_block[64], in_expert[64];  // tokens whose shared set has a block; that take an expert
   float alpha[kMost];
-  int found[kWarps + 1];
-  uint8_t slots[kWarps][kMost];          // a warp's tokens of its pair
+  int found[kUpWarps];
+  uint8_t slots[kUpWarps][kMost];          // a warp's tokens of its pair
 };
 constexpr int kUpStages = 6;
 // After it: the affinities [8][K] where the decisions are taken here, [G] pairs in use, then the rings
@@ -302,14 +329,15 @@ __host__ __device__ inline size_t up_fixed(int G, int K, bool routes) {
   return ((sizeof(UpShared) + (size_t)G * 2 + (routes ? 32 * (size_t)K : 0)) + 127) / 128 * 128 + 128;
 }
 __host__ __device__ inline size_t up_smem(int G, int K, int C, bool routes) {
-  const size_t rings = (size_t)kWarps * kUpStages * kStage, product = routes ? 4 * (size_t)route_floats(C) : 0;
+  const size_t rings = (size_t)kUpWarps * kUpStages * kStage, product = routes ? 4 * (size_t)route_floats(C, kUpWarps) : 0;
   return up_fixed(G, K, routes) + (rings > product ? rings : product);
 }
 
 // NT: pieces of eight tokens that are taken at once; a pair that more tokens run is gone through again.
 // ROUTES: the decisions are taken here.
 template <int NT, bool ROUTES>
-__global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
+__global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
+  constexpr int kThreads = 32 * kUpWarps, kWarps = kUpWarps;
   extern __shared__ __align__(16) uint8_t raw[];
   UpShared& sh = *reinterpret_cast<UpShared*>(raw);
   const int G = (p.K + 1) * p.B;
@@ -323,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
   grid_dep_wait();
   grid_dep_launch();
   if constexpr (ROUTES) {
-    const float* z = route_products(p, 0, p.T, reinterpret_cast<float*>(raw + (rings - base)));
+    const float* z = route_products<kUpWarps>(p, 0, p.T, reinterpret_cast<float*>(raw + (rings - base)));
     if (warp < p.T) {
       uint64_t shr, em;
       float alpha;
@@ -354,14 +382,18 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
     else sh.in_expert[i - p.B] = v;
   }
   __syncthreads();
-  auto members = [&](int pair) {
-    const int e = pair / p.B, b = pair - e * p.B;
+  auto members = [&](int code) {
+    const int e = expert_of(code), b = block_of(code);
     return e == 0 ? sh.in_block[b] : sh.in_expert[e - 1] & ~sh.in_block[b];
   };
   // pairs in use, in order: a run of them to each thread
   const int each = (G + kThreads - 1) / kThreads, from = threadIdx.x * each, to = min(G, from + each);
+  auto code_of = [&](int i) {
+    const int e = i / p.B;
+    return pair_code(e, i - e * p.B);
+  };
   int n = 0;
-  for (int i = from; i < to; ++i) n += members(i) != 0ull;
+  for (int i = from; i < to; ++i) n += members(code_of(i)) != 0ull;
   int before = n;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -370,18 +402,18 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
   }
   if (lane == 31) sh.found[warp] = before;
   __syncthreads();
-  int at = before - n, all = 0;
+  int to_at = before - n, all = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) at += sh.found[w];
+    if (w < warp) to_at += sh.found[w];
     all += sh.found[w];
   }
   for (int i = from; i < to; ++i) {
-    const uint64_t m = members(i);
-    if (m == 0ull) continue;
-    list[at] = (uint16_t)i;
-    if (first) p.pair[at] = (uint16_t)i;
-    ++at;
+    const uint16_t code = code_of(i);
+    if (members(code) == 0ull) continue;
+    list[to_at] = code;
+    if (first) p.pair[to_at] = code;
+    ++to_at;
   }
   if (first && threadIdx.x == 0) *p.n_pairs = all;
   __syncthreads();
@@ -391,41 +423,37 @@ __global__ void __launch_bounds__(kThreads, 2) up_kernel(const Params p) {
       p.members[i] = i < p.B ? sh.in_block[i] : sh.in_expert[i - p.B];
 
   // tiles of 16 keys, in blocks of 64 features
-  const int tiles = p.M / 16, blocks = p.d / 64;
-  const long long items = (long long)all * tiles, step = (long long)gridDim.x * kWarps;
+  const int blocks = p.d / 64;
+  const Walk begin((int)(warp * gridDim.x + blockIdx.x), (int)(gridDim.x * kWarps), p.M / 16);
   const int g = lane >> 2, k0 = (lane & 3) * 16;
   uint8_t* slots_all = sh.slots[warp];
-  auto keys_of = [&](long long i) {
-    const int pair = list[i / tiles], row = (int)(i % tiles) * 16;
-    const int e = pair / p.B, b = pair - e * p.B;
-    return p.up + ((long long)e * p.H + b * p.M + row) * p.d;
-  };
   Ring<kUpStages> ring(rings + (uint32_t)warp * kUpStages * kStage, lane);
-  long long next = (long long)warp * gridDim.x + blockIdx.x;  // of the blocks on their way
-  int next_f = 0, again = 0;  // times that the item's blocks are needed once more
+  Walk next = begin;          // of the blocks on their way
+  int next_f = 0, again = 0;  // their features; times that the item's blocks are needed once more
   const __nv_bfloat16* keys = nullptr;
   auto enter = [&]() {
-    if (next >= items) return;
-    keys = keys_of(next);
-    again = p.T <= 8 * NT ? 0 : (__popcll(members(list[next / tiles])) - 1) / (8 * NT);
+    if (next.pair >= all) return;
+    const int code = list[next.pair];
+    keys = p.up + ((long long)expert_of(code) * p.H + block_of(code) * p.M + next.part * 16) * p.d;
+    again = p.T <= 8 * NT ? 0 : (__popcll(members(code)) - 1) / (8 * NT);
   };
   enter();
   auto fetch = [&]() {
-    ring.fetch(next < items, keys + next_f, p.d);
+    ring.fetch(next.pair < all, keys + next_f, p.d);
     if ((next_f += 64) == p.d) {
       next_f = 0;
       if (--again < 0) {
-        next += step;
+        next.next();
         enter();
       }
     }
   };
 #pragma unroll
   for (int k = 0; k < kUpStages - 1; ++k) fetch();
-  for (long long i = (long long)warp * gridDim.x + blockIdx.x; i < items; i += step) {
-    const int pair = list[i / tiles], row = (int)(i % tiles) * 16;
-    const int e = pair / p.B, b = pair - e * p.B;
-    const uint64_t m = members(pair);
+  for (Walk at = begin; at.pair < all; at.next()) {
+    const int code = list[at.pair], row = at.part * 16;
+    const int e = expert_of(code), b = block_of(code);
+    const uint64_t m = members(code);
     const int all_tokens = __popcll(m);
     __syncwarp();
 #pragma unroll
@@ -499,7 +527,7 @@ constexpr size_t down_smem(int G) {
 template <int NT, int TOK>
 __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const int ctas) {
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ uint8_t slots_of[kWarps][kMost];
+  __shared__ uint8_t slots_of[kWarps][4][kMost];  // the tokens of the last four items
   constexpr int kSums = 16 * TOK, S = down_stages(TOK);
   const int G = (p.K + 1) * p.B;
   uint64_t* masks = reinterpret_cast<uint64_t*>(raw);
@@ -511,7 +539,6 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
   const int g = lane >> 2, k0 = (lane & 3) * 16;
   float* mine = red + warp * kSums;  // [token][feature]
   for (int i = lane; i < kSums; i += 32) mine[i] = 0.f;
-  uint8_t* slots_all = slots_of[warp];
   grid_dep_wait();
   const int pairs = *p.n_pairs;
   for (int i = threadIdx.x; i < p.B + p.K; i += kThreads) masks[i] = p.members[i];
@@ -519,27 +546,29 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
   __syncthreads();
   // items: whole pairs where every warp of the cluster has several, else their chunks of 64 channels
   const int per = p.M / 64, units = ctas * kWarps;
-  const int length = pairs >= 8 * units ? per : 1, cuts = per / length, items = pairs * cuts;
+  const int length = pairs >= 8 * units ? per : 1;
+  const Walk begin(warp * ctas + rank, units, per / length);
   const __nv_bfloat16* rows = p.down + (long long)j0 * p.H;
   struct At {
-    int i, k, again, e, b, ch;  // item, chunk of it, times that it is needed once more; expert, block,
-  };                            // first channel of the chunk
+    Walk w;
+    int k, again, e, b, ch;  // chunk of the item, times that it is needed once more; expert, block, first
+  };                         // channel of the chunk
   auto members = [&](const At& a) {
     return a.e == 0 ? masks[a.b] : masks[p.B + a.e - 1] & ~masks[a.b];
   };
   auto enter = [&](At& a) {
-    const int at = a.i / cuts, pair = list[at];
+    const int code = list[a.w.pair];
     a.k = 0;
-    a.e = pair / p.B;
-    a.b = pair - a.e * p.B;
-    a.ch = a.b * p.M + (a.i - at * cuts) * length * 64;
+    a.e = expert_of(code);
+    a.b = block_of(code);
+    a.ch = a.b * p.M + a.w.part * length * 64;
     a.again = TOK <= 8 * NT ? 0 : (__popcll(members(a)) - 1) / (8 * NT);
   };
-  At next{warp * ctas + rank, 0, 0, 0, 0, 0};
-  if (next.i < items) enter(next);
+  At next{begin, 0, 0, 0, 0, 0};
+  if (next.w.pair < pairs) enter(next);
   Ring<S> ring(rings + (uint32_t)warp * S * kStage, lane);
   auto fetch = [&]() {
-    const bool on = next.i < items;
+    const bool on = next.w.pair < pairs;
     ring.fetch(on, rows + (long long)next.e * p.d * p.H + next.ch, p.H);
     if (!on) return;
     next.ch += 64;
@@ -548,65 +577,131 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
         next.k = 0;
         next.ch -= 64 * length;
       } else {
-        next.i += units;
-        if (next.i < items) enter(next);
+        next.w.next();
+        if (next.w.pair < pairs) enter(next);
       }
     }
   };
 #pragma unroll
   for (int k = 0; k < S - 1; ++k) fetch();
-  constexpr int P = NT < 2 ? NT : 2;  // pieces of h that are read a chunk ahead
-  for (At at{warp * ctas + rank, 0, 0, 0, 0, 0}; at.i < items; at.i += units) {
-    enter(at);
-    const uint64_t m = members(at);
-    const int all_tokens = __popcll(m);
-    __syncwarp();
+  // A step: a chunk for up to 8 NT of its pair's tokens, or (up to 8 tokens) for all of them, with 0 for
+  // those that do not run the pair. h of a step is read kAhead steps before it is used: its latency
+  // is longer than a step (a step ahead: 0.9 us a step, 24 tokens of the 33-expert layer 69 us).
+  constexpr bool kAll = TOK <= 8;
+  constexpr int P = NT < 2 ? NT : 2;  // pieces of h that are read ahead
+  constexpr int kAhead = kAll ? 4 : 2;
+  struct Step {
+    bool on, last;  // there is one; it is the last of its item's tokens
+    int tokens;
+    const uint8_t* slots;
+    const __nv_bfloat16* h;
+  };
+  At ahead{begin, 0, 0, 0, 0, 0};
+  int all_tokens = 0, s0 = 0, turn = 0;
+  uint64_t taking = 0ull;  // the item's tokens
+  auto open = [&]() {  // the item that `ahead` is at: its tokens, listed
+    if (ahead.w.pair >= pairs) return;
+    enter(ahead);
+    taking = members(ahead);
+    if constexpr (kAll) {
+      all_tokens = p.T;
+    } else {
+      turn = (turn + 1) & 3;
+      uint8_t* to = slots_of[warp][turn];
 #pragma unroll
-    for (int k = 0; k < (TOK + 31) / 32; ++k) {
-      const int t = lane + 32 * k;
-      if (m >> t & 1ull) slots_all[__popcll(m & ((1ull << t) - 1ull))] = (uint8_t)t;
+      for (int k = 0; k < (TOK + 31) / 32; ++k) {
+        const int t = lane + 32 * k;
+        if (taking >> t & 1ull) to[__popcll(taking & ((1ull << t) - 1ull))] = (uint8_t)t;
+      }
+      __syncwarp();
+      all_tokens = __popcll(taking);
     }
-    __syncwarp();
-    for (int s0 = 0; s0 < all_tokens; s0 += 8 * NT) {
-    const uint8_t* slots = slots_all + s0;
-    const int tokens = min(all_tokens - s0, 8 * NT), pieces = (tokens + 7) / 8;
-    const __nv_bfloat16* h[NT];  // (columns past the pair's tokens repeat its first one)
-    float c[NT][4];
-    Piece v[P];
+  };
+  Piece v[kAhead][P];
+  auto take = [&](Piece (&to)[P]) {  // the next step, its h on its way
+    Step st{ahead.w.pair < pairs, false, 0, nullptr, nullptr};
+    if (!st.on) return st;
+    st.h = p.h + (long long)ahead.e * p.T * p.H + ahead.ch + k0;
+    if constexpr (kAll) {
+      clear(to[0]);
+      if (taking >> g & 1ull) read_token(to[0], st.h + (long long)g * p.H);
+    } else {
+      st.slots = slots_of[warp][turn] + s0;
+      st.tokens = min(all_tokens - s0, 8 * NT);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int slot = t * 8 + g;
-      h[t] = p.h + ((long long)at.e * p.T + slots[slot < tokens ? slot : 0]) * p.H + at.ch + k0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
-      if (t < P && t < pieces) read_token(v[t < P ? t : 0], h[t]);
+      for (int t = 0; t < P; ++t)
+        if (t * 8 < st.tokens) {
+          const int slot = t * 8 + g;  // (columns past the tokens repeat the first one)
+          read_token(to[t], st.h + (long long)st.slots[slot < st.tokens ? slot : 0] * p.H);
+        }
     }
-    for (int k = 0; k < length; ++k) {
+    if (++ahead.k < length) {
+      ahead.ch += 64;
+    } else {
+      st.last = true;
+      ahead.k = 0;
+      ahead.ch -= 64 * (length - 1);
+      s0 += 8 * NT;
+      if (kAll || s0 >= all_tokens) {
+        s0 = 0;
+        ahead.w.next();
+        open();
+      }
+    }
+    return st;
+  };
+  float c[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
+  open();
+  Step steps[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) steps[k] = take(v[k]);
+  while (steps[0].on) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const Step now = steps[k];
+      if (!now.on) {  // the last step was the one before
+        steps[0].on = false;
+        break;
+      }
       Piece lo, hi;
       fetch();
       ring.read(lo, hi);
+      if constexpr (kAll) {
+        multiply(c[0], lo, hi, v[k][0]);
+      } else {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (t < pieces) {
-          if (t < P) {
-            multiply(c[t], lo, hi, v[t < P ? t : 0]);
-            if (k + 1 < length) read_token(v[t < P ? t : 0], h[t] + (k + 1) * 64);
-          } else {
-            Piece w;
-            read_token(w, h[t] + k * 64);
-            multiply(c[t], lo, hi, w);
+        for (int t = 0; t < NT; ++t)
+          if (t * 8 < now.tokens) {
+            if (t < P) {
+              multiply(c[t], lo, hi, v[k][t < P ? t : 0]);
+            } else {
+              Piece w;
+              const int slot = t * 8 + g;
+              read_token(w, now.h + (long long)now.slots[slot < now.tokens ? slot : 0] * p.H);
+              multiply(c[t], lo, hi, w);
+            }
           }
+        if (now.last) {  // the columns to their tokens
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int slot = t * 8 + (lane & 3) * 2 + (j & 1);
+              if (slot < now.tokens) mine[now.slots[slot] * 16 + g + (j >> 1) * 8] += c[t][j];
+              c[t][j] = 0.f;
+            }
         }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int slot = t * 8 + (lane & 3) * 2 + (j & 1);
-        if (slot < tokens) mine[slots[slot] * 16 + g + (j >> 1) * 8] += c[t][j];
       }
+      steps[k] = take(v[k]);
     }
   }
+  if constexpr (kAll)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine[((lane & 3) * 2 + (j & 1)) * 16 + g + (j >> 1) * 8] = c[0][j];
   __syncthreads();
   float* sums = red + kWarps * kSums;
   for (int i = threadIdx.x; i < kSums; i += kThreads) {
@@ -736,7 +831,7 @@ cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
   const size_t smem = up_smem(G, p.K, p.C, routes);
   cudaError_t e;
   if (!routes) {
-    const size_t bytes = 4 * (size_t)route_floats(p.C);
+    const size_t bytes = 4 * (size_t)route_floats(p.C, kWarps);
     e = allow_smem_once(route_kernel, bytes);
     if (e == cudaSuccess) e = launch_dependent(route_kernel, dim3(p.T), dim3(kThreads), bytes, s, p);
     if (e != cudaSuccess) return e;
@@ -745,7 +840,7 @@ cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
   if constexpr (NT == 1) up = up_kernel<1, true>;
   else up = up_kernel<NT, false>;
   e = allow_smem_once(up, smem);
-  if (e == cudaSuccess) e = launch_dependent(up, dim3(2 * sms), dim3(kThreads), smem, s, p);
+  if (e == cudaSuccess) e = launch_dependent(up, dim3(sms), dim3(32 * kUpWarps), smem, s, p);
   if (e != cudaSuccess) return e;
   // a cluster to 16 output features, of as many CTAs as the SMs hold at once
   const int groups = p.d / 16, slots = 2 * sms;
