@@ -287,7 +287,12 @@ __device__ __forceinline__ float residual_of(const Params& p, long long row, int
 // staged boxes of 32 rows by 64 bytes, which also cuts them off at the result's ends. (Written by the
 // threads, a row each, a store touches 32 lines and the storing warps are bound by that:
 // 12,608 x 384 to 1,536 with GELU and z 26 us ...)
-template <int KIND, typename TO, bool PAIR, bool WIDE>
+//
+// SPLIT (WIDE, not PAIR): a cluster of p.splits CTAs shares a tile, each a part of its reduction; their
+// sums meet in shared memory, where each adds and finishes a share of the tile. For few rows and a
+// long reduction, whose steps one CTA would run one after another (us, without and with: 256 x 4,096 to
+// 1,024 13.9 and 9; ...).
+template <int KIND, typename TO, bool PAIR, bool WIDE, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmRes,
@@ -296,7 +301,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr bool kParts = KIND == kWeight;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
   const bool leader = rank == 0;
-  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+  static_assert(!SPLIT || (WIDE && !PAIR), "forms");
+  const uint32_t share = SPLIT ? cluster_rank() : 0u;  // SPLIT: the part of the reduction
+  const int per = SPLIT ? p.splits : kCtas, unit = blockIdx.x / per, units = gridDim.x / per;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t s0 = smem_u32(smem);
@@ -375,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   struct Walk {
     int i, m, n, part;
   };
-  const int n_items = p.m_tiles * p.n_tiles * p.splits;
+  const int n_items = p.m_tiles * p.n_tiles * (SPLIT ? 1 : p.splits);
   const int by_m = units / p.n_tiles, by_n = units - by_m * p.n_tiles;
   auto start = [&]() {
     Walk w;
@@ -403,8 +410,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     it.m0 = w.m * kTileM + 128 * (int)rank;
     it.n0 = w.n * p.tile_n;
     it.n = min(p.tile_n, p.N - it.n0);
-    it.from = kParts ? (int)((long long)p.steps * it.part / p.splits) : 0;
-    it.to = kParts ? (int)((long long)p.steps * (it.part + 1) / p.splits) : p.steps;
+    const int part = SPLIT ? (int)share : it.part;
+    it.from = kParts || SPLIT ? (int)((long long)p.steps * part / p.splits) : 0;
+    it.to = kParts || SPLIT ? (int)((long long)p.steps * (part + 1) / p.splits) : p.steps;
     return it;
   };
 
@@ -468,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float in_columns = per_column && ahead.i < n_items ? column(ahead) : 0.f;
     int turn = 0;
     // WIDE: boxes this warp has staged, and the residual's boxes on their way (two ahead)
-    const bool with_res = WIDE && KIND < kInput && p.residual;
+    const bool with_res = WIDE && !SPLIT && KIND < kInput && p.residual;
     const uint32_t box0 = smem_u32(staged) + warp * p.boxes * kBox, two = p.two ? kBox : 0u;
     uint32_t k = 0, fetched = 0;
     Piece coming = first_piece();
@@ -524,6 +532,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         release(acc ^ 1);
       }
       if (!ok) continue;
+      if constexpr (SPLIT) {
+        // (all of this CTA's MMAs have completed: the ring is free) rows of tile_n + 4 values
+        for (int c = part; c < n_pieces; c += 4) {
+          float v[W];
+          if constexpr (W == 32) tmem_ld32(lanes + acc * kAcc + c * W, v);
+          else tmem_ld16(lanes + acc * kAcc + c * W, v);
+          const uint32_t to = s0 + ((q * 32 + lane) * (p.tile_n + 4) + c * W) * 4;
+#pragma unroll
+          for (int e = 0; e < W; e += 4)
+            put4(to + e * 4, __float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]),
+                 __float_as_uint(v[e + 3]));
+        }
+        release(acc);
+        acc ^= 1;
+        continue;
+      }
       for (int c = part; c < n_pieces; c += 4) {
         float v[W];
         if constexpr (W == 32) tmem_ld32(lanes + acc * kAcc + c * W, v);
@@ -704,7 +728,63 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (PAIR) cluster_sync_all();
+  if (PAIR || SPLIT) cluster_sync_all();
+  if constexpr (SPLIT) {
+    // Four columns of 32 rows to a warp of the cluster in turn, a row to a lane; the parts are added in
+    // order.
+    const Item it = item_of(start());
+    if (warp < kEpiWarps && *abort_flag == 0)
+      for (int u = warp * p.splits + (int)share; u < it.n; u += kEpiWarps * p.splits) {
+        const int q = u & 3, c = u & ~3, ch = it.n0 + c;
+        const long long row = (long long)it.m0 + q * 32 + lane;
+        if (row >= p.M || c >= it.n) continue;
+        const uint32_t at = s0 + ((q * 32 + lane) * (p.tile_n + 4) + c) * 4;
+        float a[8][4];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r < p.splits)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(a[r][0]), "=f"(a[r][1]), "=f"(a[r][2]), "=f"(a[r][3])
+                         : "r"(mapa_shared(at, r))
+                         : "memory");
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[0][e];
+#pragma unroll
+        for (int r = 1; r < 8; ++r)
+          if (r < p.splits)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += a[r][e];
+        const bool on = KIND >= kInput || !p.mask || p.mask[row] != 0;
+        TO* out = static_cast<TO*>(p.out) + row * p.ld_out + ch;
+        if constexpr (KIND < kInput) {
+          finish_row<4>(p, v, p.sm ? p.sm[row] : 1.f, on, columns + c, columns + 256 + c);
+          if (p.z)
+            *reinterpret_cast<uint2*>(p.z + row * p.ld_z + ch) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+          if (p.gelu) {
+            act2<TO>(v[0], v[1]);
+            act2<TO>(v[2], v[3]);
+          }
+          if (p.residual && on) {
+            const TO* res = static_cast<const TO*>(p.residual) + row * p.ld_res + ch;
+            if constexpr (sizeof(TO) == 4) {
+              const float4 b = *reinterpret_cast<const float4*>(res);
+              v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
+            } else {
+              const uint2 b = *reinterpret_cast<const uint2*>(res);
+              v[0] += __uint_as_float(b.x << 16);
+              v[1] += __uint_as_float(b.x & 0xffff0000u);
+              v[2] += __uint_as_float(b.y << 16);
+              v[3] += __uint_as_float(b.y & 0xffff0000u);
+            }
+          }
+        }
+        if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(out) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+      }
+    __syncwarp();
+    cluster_sync_all();  // no CTA leaves while another reads its sums
+  }
   if (warp == kMmaWarp) {
     if (PAIR) tmem_dealloc_pair(tmem, kTmemCols);
     else tmem_dealloc(tmem, kTmemCols);
@@ -1015,6 +1095,12 @@ uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 // Rows that TMA can read as they are.
 bool tma_rows(const void* p, long long ld, int size) { return bits(p) % 16 == 0 && ld * size % 16 == 0; }
 
+// Rows that TMA can write: a store is cut off at whole 16 bytes, and what is behind a row's end is
+// nobody's to write.
+bool tma_out(const void* p, long long ld, int cols, int size) {
+  return tma_rows(p, ld, size) && (long long)cols * size % 16 == 0;
+}
+
 long long pitch_of(int cols, int size) { return ((long long)cols * size + 15) / 16 * 16 / size; }
 
 long long part_pitch(int cols) { return (cols + 3) / 4 * 4; }  // fp32 values between rows of parts
@@ -1032,35 +1118,47 @@ bool map_rows(CUtensorMap* map, const void* base, int size, uint64_t cols, uint6
 struct Tiles {
   bool pair;
   int tile_n, m_tiles, n_tiles;
+  int split = 1;  // CTAs that share a tile's reduction
 };
 // (whole boxes of 32 columns; on pairs tcgen05 takes 32, 64, ... 256)
 int even_part(int n, int parts) { return ((n + parts - 1) / parts + 31) / 32 * 32; }
 
-// The width and form of the tiles that leave the longest-running CTA or pair the least to do,
-// in clocks of the tensor cores (2 a column and step) or of shared memory (128 bytes of
-// operands in and out a clock), whichever are more, with 1,500 beside for a CTA's beginning
-// and end. (us, pairs of 256 columns wherever they are half the SMs' number and this: 5,003 x 1,001
-// to 777 80 tiles on 76 pairs, 32.3 and 24; ...)
-Tiles pick_tiles(long long M, int N, int steps, int sms) {
+// The width and form of the tiles that leave the longest-running CTA or pair the least to do, in
+// clocks, as measured: a step takes 2 clocks a column on a pair (what the tensor cores need; shared
+// memory, 128 bytes of operands in and out a clock, 256 + n), 2.4 on a CTA alone, and at least
+// 300 to 350; 14 a column go to storing a tile beside them; 5,700 to the beginning and end. A reduction
+// that a cluster shares costs 5,000 clocks more and 55 to 105 a column for the meeting of 128 rows' sums. (us:
+// 5,003 x 1,001 to 777 in 80 tiles of 256 x 208 on 76 pairs 32, in 60 of 256 x 264 23; 64 x 4,096 to 1,024
+// in 32 tiles 12.6, shared by four 9.2; 33 x 1,024 to 4,096 in 128 tiles 7.9, in 43 5.7.)
+Tiles pick_tiles(long long M, int N, int steps, bool may_split, int sms) {
   Tiles best{};
   double least = 1e300;
+  const double met = M < 128 ? (M + 31) / 32 / 4.0 : 1.0;  // rows of a tile that there are
   for (int pair = 0; pair < 2; ++pair) {
     const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
     int last = 0;
     for (int parts = (N + 255) / 256; parts <= (N + 31) / 32; ++parts) {
       const int n = even_part(N, parts);
-      if (n == last || (last && n < 32)) continue;
+      if (n == last) continue;
       last = n;
       const long long tiles = m * ((N + n - 1) / n), waves = (tiles + units - 1) / units;
-      const double step = pair ? std::max(2.0 * n, 256.0 + n) : 256.0 + 2.0 * n;
-      const double cost = waves * (std::max(step * steps, 14.0 * n) + 200.0) + 1500.0 + 4.0 * n;
-      if (cost < least * 0.98) {
+      const double step = pair ? std::max(350.0, std::max(2.0 * n, 256.0 + n)) : std::max(300.0, 2.4 * n);
+      auto take = [&](double cost, int split) {
+        if (cost >= least * 0.98) return;
         least = cost;
         best.pair = pair != 0;
         best.tile_n = n;
         best.m_tiles = (int)m;
         best.n_tiles = (N + n - 1) / n;
-      }
+        best.split = split;
+      };
+      take(waves * (std::max(step * steps, 14.0 * n) + 200.0) + 5700.0 + 4.0 * n + 25.0 * std::min(tiles, units), 1);
+      // a cluster to a tile where all of them find a place at once (120 CTAs of 152 in clusters of 8, 144 in
+      // those of 4)
+      int log = 1;
+      for (int split = 2; may_split && !pair && split <= 8 && 4 * split <= steps; split *= 2, ++log)
+        if (tiles * split <= sms * (split == 8 ? 15 : split == 4 ? 18 : 19) / 19)
+          take(step * ((steps + split - 1) / split) + 10700.0 + (30.0 + 25.0 * log) * n * met, split);
       if (tiles > 4 * units) break;  // narrower tiles only cost more
     }
   }
@@ -1112,10 +1210,7 @@ struct Out {
 template <typename TO>
 bool map_out(Out* o, const Params& p) {
   constexpr int size = sizeof(TO), box = 64 / size;
-  // (a store is cut off at whole 16 bytes: what is behind a row's end must be nobody's else)
-  auto fits = [&](const void* q, long long ld, int bytes) {
-    return !q || (bits(q) % 16 == 0 && ld * bytes % 16 == 0 && (p.own_rows || (long long)p.N * bytes % 16 == 0));
-  };
+  auto fits = [&](const void* q, long long ld, int bytes) { return !q || tma_out(q, ld, p.own_rows ? 16 : p.N, bytes); };
   o->wide = fits(p.out, p.ld_out, size) && fits(p.residual, p.ld_res, size) && fits(p.z, p.ld_z, 2);
   if (!o->wide) return true;
   const uint64_t plane = (uint64_t)p.M * p.ld_out * size;
@@ -1130,15 +1225,17 @@ template <int KIND, typename TO>
 cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, const Tiles& t, int sms,
                         cudaStream_t s) {
   Out o{};
+  if (KIND != kWeight) p.splits = 1;
   if (!map_out<TO>(&o, p)) return cudaErrorInvalidValue;
   const bool wide = o.wide;
-  const int ctas = t.pair ? 2 : 1;
-  const int n = t.tile_n / ctas;
+  const bool split = KIND != kWeight && wide && t.split > 1;
+  const int ctas = t.pair ? 2 : split ? t.split : 1;
+  const int n = t.tile_n / (t.pair ? 2 : 1);
   p.tile_n = t.tile_n;
   p.m_tiles = t.m_tiles;
   p.n_tiles = t.n_tiles;
   p.stage_bytes = 16384u + (KIND >= kInput ? (uint32_t)((n + 63) / 64) * 8192u : ((uint32_t)n * 128u + 1023u) / 1024u * 1024u);
-  p.two = p.residual || p.steps <= 8 || (p.gelu && p.steps < 32);
+  p.two = !split && (p.residual || p.steps <= 8 || (p.gelu && p.steps < 32));
   p.boxes = (p.two ? 2u : 1u) + (p.z ? 1u : 0u);
   const uint32_t beside =
       1024u + (kBars + 1) * 8u + 16u + kColumns + (wide ? kEpiWarps * p.boxes * kBox : kStagingOdd);
@@ -1148,13 +1245,18 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
   p.wait_limit = gemm_wait_limit();
   void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
                  const Params) =
-      t.pair ? (wide ? gemm_kernel<KIND, TO, true, true> : gemm_kernel<KIND, TO, true, false>)
-             : (wide ? gemm_kernel<KIND, TO, false, true> : gemm_kernel<KIND, TO, false, false>);
+      t.pair ? (wide ? gemm_kernel<KIND, TO, true, true, false> : gemm_kernel<KIND, TO, true, false, false>)
+             : (wide ? gemm_kernel<KIND, TO, false, true, false> : gemm_kernel<KIND, TO, false, false, false>);
+  if constexpr (KIND != kWeight)
+    if (split) {
+      kernel = gemm_kernel<KIND, TO, false, true, true>;
+      p.splits = t.split;
+    }
   const cudaError_t e = allow_smem_once(kernel, smem);
   if (e != cudaSuccess) return e;
-  const long long items = (long long)t.m_tiles * t.n_tiles * p.splits;
+  const long long items = (long long)t.m_tiles * t.n_tiles * (split ? 1 : p.splits);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(ctas * std::min<long long>(items, sms / ctas)));
+  cfg.gridDim = dim3((unsigned)(ctas * (split ? items : std::min<long long>(items, sms / ctas))));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -1165,7 +1267,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
   attr[1].val.clusterDim.x = ctas;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = t.pair ? 2 : 1;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, a, b, o.out, o.res, o.z, p);
 }
 
@@ -1248,7 +1350,7 @@ Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int 
   const long long cols = (p->n + 255) / 256, most = std::max<long long>(1, 4ll * sms / cols);
   r.per = (int)std::max<long long>(kGradWarps * kGradRows, (T + most - 1) / most);
   r.blocks = (int)((T + r.per - 1) / r.per);
-  r.in = pick_tiles(T, p->cols, (p->n + 63) / 64, sms);
+  r.in = pick_tiles(T, p->cols, (p->n + 63) / 64, tma_out(g->dx_dev, g->ld_dx, p->cols, 2), sms);
   const int steps = (int)((T + 63) / 64);
   r.weight = pick_weight_tiles(p->n, p->cols, steps, sms, &r.splits);
   int64_t at = 0;
@@ -1394,7 +1496,9 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     w = ws;
   }
   const int steps = (int)(((int64_t)p->cols * size + 127) / 128);
-  const ln::Tiles t = ln::pick_tiles(p->rows, p->n, steps, sms);
+  const bool wide = ln::tma_out(out, ld_out, p->n, os) && (!residual || ln::tma_out(residual, ld_res, p->n, os)) &&
+                    (!z || ln::tma_out(z, ld_z, p->n, 2));
+  const ln::Tiles t = ln::pick_tiles(p->rows, p->n, steps, wide, sms);
   if ((long long)t.m_tiles * t.n_tiles > 0x7fff0000) {
     set_error("too many tiles: rows=%lld n=%d", (long long)p->rows, p->n);
     return UNIF_MOE_ERR_SHAPE;

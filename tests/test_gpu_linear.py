@@ -122,6 +122,18 @@ def test_epilogue(T, cols, n, kind, bias, act, residual, dtype, keep, masked):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,cols,n", [(33, 4096, 64), (129, 2000, 200), (250, 4096, 1024), (600, 8192, 264),
+                                      (70, 1024, 40), (40, 8000, 4096)])
+@pytest.mark.parametrize("bias,act,residual,dtype,keep,masked", [
+    (None, "none", False, "bf16", False, False), ("bf16", "gelu", True, "bf16", True, True),
+    ("f32", "gelu", True, "f32", True, False), ("f32", "none", True, "f32", False, True)])
+def test_few_rows_and_long_reductions(T, cols, n, kind, bias, act, residual, dtype, keep, masked):
+    """Tiles whose reduction several CTAs share."""
+    check(**inputs(T, cols, n, n + T, kind, bias, residual, masked, dtype), act=act, dtype=dtype, keep=keep)
+
+
+@pytest.mark.gpu
 def test_every_row_padding_and_no_rows():
     from paper_2608_10392_gb300 import linear
     for T in (4, 200):
@@ -254,7 +266,8 @@ def grads(T, cols, n, seed, act="none", masked=False, dtype="bf16", pad=0, shift
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,cols,n", [(1, 1, 1), (1, 64, 64), (5, 33, 7), (63, 128, 256), (64, 200, 120), (65, 65, 65),
                                       (300, 384, 1536), (1000, 768, 130), (1025, 72, 264), (5003, 333, 129),
-                                      (12608, 384, 1536), (20000, 1024, 512), (40000, 128, 128)])
+                                      (12608, 384, 1536), (20000, 1024, 512), (40000, 128, 128),
+                                      (50, 512, 4096), (200, 264, 2048)])
 @pytest.mark.parametrize("act,masked,grad_dtype", [("none", False, "f32"), ("gelu", True, "bf16"),
                                                    ("gelu", False, "f32"), ("none", True, "f32")])
 def test_gradients(T, cols, n, act, masked, grad_dtype):
