@@ -1468,13 +1468,13 @@ cudaError_t backward_as(const unif_moe_block_norm* p, const Plan& pl, const void
 using unif::set_error;
 namespace nm = unif::norm;
 
-extern "C" {
+namespace {
 
-static int norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
-                        const void* y, int64_t ld_y, const uint8_t* mask,
-                        const void* w_post, const void* b_post, const void* gate, const void* w_pre,
-                        const void* b_pre, void* out, int64_t ld_out, void* u, int64_t ld_u,
-                        float* m_post, float* r_post, float* m_pre, float* r_pre, float* u_scale, void* stream) {
+// Checks and launch of both forwards; u_scale: u in 8 bits.
+int norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x, const void* y, int64_t ld_y,
+                 const uint8_t* mask, const void* w_post, const void* b_post, const void* gate, const void* w_pre,
+                 const void* b_pre, void* out, int64_t ld_out, void* u, int64_t ld_u, float* m_post,
+                 float* r_post, float* m_pre, float* r_pre, float* u_scale, void* stream) {
   set_error("%s", "");
   const int rc = nm::check_desc(p);
   if (rc != UNIF_MOE_OK) return rc;
@@ -1513,6 +1513,10 @@ static int norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_
   }
   return UNIF_MOE_OK;
 }
+
+}  // namespace
+
+extern "C" {
 
 int unif_moe_block_norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x,
                                 const void* y, int64_t ld_y, const uint8_t* mask,
