@@ -605,24 +605,37 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t live = __ballot_sync(0xffffffffu, on);
           const int col = lane & 15;
           const float sn = per_column ? cols[256 + c * W + col] : 1.f, b = per_column ? cols[c * W + col] : 0.f;
-#pragma unroll 1
-          for (int r0 = lane >> 4; r0 < 32; r0 += 16) {
-            float res[8];
+          // this lane's rows, every other one: what they take of the residual first, all on its way at once
+          const int r0 = lane >> 4, rows = (int)min(32ll, p.M - (row - lane));
+          TO res[16];
+          if (KIND < kInput && p.residual) {
+            const TO* from = static_cast<const TO*>(p.residual) + (row - lane + r0) * p.ld_res + ch + col;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int r = r0 + 2 * e;
-              res[e] = 0.f;
-              if (KIND < kInput && p.residual && (live >> r & 1u) && col < count)
-                res[e] = residual_of<TO>(p, row - lane + r, ch + col);
+            for (int e = 0; e < 16; ++e)
+              if ((live >> (r0 + 2 * e) & 1u) && col < count) res[e] = from[2 * e * p.ld_res];
+          }
+          const bool scaled = KIND < kInput && p.sm;
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            float y[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int r = r0 + 2 * (e + h);
+              y[h] = stg[r * 17 + col];
+              if constexpr (KIND < kInput) {
+                const float sm = scaled ? __shfl_sync(0xffffffffu, scale, r) : 1.f;
+                y[h] = live >> r & 1u ? fmaf(y[h], sm * sn, b) : 0.f;
+                if (p.z && r < rows && col < count)
+                  p.z[(row - lane + r) * p.ld_z + ch + col] = __float2bfloat16_rn(y[h]);
+              }
             }
+            if (KIND < kInput && p.gelu) act2<TO>(y[0], y[1]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int r = r0 + 2 * e;
-              const float sm = __shfl_sync(0xffffffffu, scale, r);
-              if (row - lane + r >= p.M || col >= count) continue;
-              const float x = stg[r * 17 + col];
-              if constexpr (KIND >= kInput) put(static_cast<TO*>(p.out) + (row - lane + r) * p.ld_out + ch + col, x);
-              else finish1<TO>(p, x, row - lane + r, ch + col, live >> r & 1u, sm, sn, b, res[e]);
+            for (int h = 0; h < 2; ++h) {
+              const int r = r0 + 2 * (e + h);
+              if (KIND < kInput && p.residual && (live >> r & 1u)) y[h] += to_f32(res[e + h]);
+              if (r < rows && col < count)
+                put(static_cast<TO*>(p.out) + (row - lane + r) * p.ld_out + ch + col, y[h]);
             }
           }
         }
@@ -1346,8 +1359,8 @@ Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int 
   r.px = r.copy_x ? pitch_of(p->cols, 2) : g->ld_x;
   r.pw = r.copy_w ? pitch_of(p->cols, 2) : g->ld_w;
   r.pz = r.make_dz ? pitch_of(p->n, 2) : g->ld_dout;
-  // row blocks of grad_kernel: four CTAs an SM
-  const long long cols = (p->n + 255) / 256, most = std::max<long long>(1, 4ll * sms / cols);
+  // row blocks of grad_kernel: the three CTAs that an SM holds at once
+  const long long cols = (p->n + 255) / 256, most = std::max<long long>(1, 3ll * sms / cols);
   r.per = (int)std::max<long long>(kGradWarps * kGradRows, (T + most - 1) / most);
   r.blocks = (int)((T + r.per - 1) / r.per);
   r.in = pick_tiles(T, p->cols, (p->n + 63) / 64, tma_out(g->dx_dev, g->ld_dx, p->cols, 2), sms);
