@@ -908,25 +908,37 @@ __global__ void __launch_bounds__(32 * kRowsWarps) rows_kernel(const RowsParams 
 
 // ---- rows laid out for TMA, dz and the bias's gradient ----
 
-// Rows to a pitch of whole 16 bytes; padding rows to 0. A warp to 256 elements of a row.
+// Rows to a pitch of whole 16 bytes, one or two arrays of them; padding rows to 0. A warp to 256
+// elements of a row.
+struct Rows {
+  const void* x;
+  long long ld;
+  void* to;
+  long long pitch, rows;
+  int cols;
+  const uint8_t* mask;
+  __host__ __device__ long long warps() const { return rows * ((cols + 255) / 256); }
+};
 template <typename T>
-__global__ void __launch_bounds__(256)
-    layout_kernel(const T* x, long long ld, T* to, long long pitch, long long rows, int cols,
-                  const uint8_t* mask) {
+__global__ void __launch_bounds__(256) layout_kernel(const Rows a, const Rows b) {
   grid_dep_wait();
   const int lane = threadIdx.x & 31;
-  const int pieces = (cols + 255) / 256;
-  const long long total = rows * pieces, step = (long long)gridDim.x * 8;
-  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += step) {
+  const long long of_a = a.warps(), total = of_a + b.warps(), step = (long long)gridDim.x * 8;
+  for (long long k = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); k < total; k += step) {
+    const Rows& j = k < of_a ? a : b;
+    const long long i = k < of_a ? k : k - of_a;
+    const int pieces = (j.cols + 255) / 256;
     const long long row = i / pieces;
     const int c0 = (int)(i - row * pieces) * 256 + lane;
-    const bool on = !mask || mask[row];
+    const bool on = !j.mask || j.mask[row];
+    const T* from = static_cast<const T*>(j.x) + row * j.ld + c0;
+    T* to = static_cast<T*>(j.to) + row * j.pitch + c0;
     T v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = on && c0 + 32 * k < cols ? x[row * ld + c0 + 32 * k] : (T)0;
+    for (int e = 0; e < 8; ++e) v[e] = on && c0 + 32 * e < j.cols ? from[32 * e] : (T)0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (c0 + 32 * k < cols) to[row * pitch + c0 + 32 * k] = v[k];
+    for (int e = 0; e < 8; ++e)
+      if (c0 + 32 * e < j.cols) to[32 * e] = v[e];
   }
 }
 
@@ -1298,15 +1310,12 @@ cudaError_t launch_rows(const RowsParams& p, bool vec, cudaStream_t s) {
   return launch_rows_as<SIZE, 4, TO>(p, vec, s);
 }
 
-cudaError_t launch_layout(const void* x, long long ld, void* to, long long pitch, long long rows, int cols,
-                          int size, const uint8_t* mask, int sms, cudaStream_t s) {
-  const long long warps = rows * ((cols + 255) / 256);
+cudaError_t launch_layout(const Rows& a, const Rows& b, int size, int sms, cudaStream_t s) {
+  const long long warps = a.warps() + b.warps();
+  if (warps == 0) return cudaSuccess;
   const int grid = (int)std::min<long long>((warps + 7) / 8, 8ll * sms);
-  if (size == 2)
-    return launch_dependent(layout_kernel<uint16_t>, dim3(grid), dim3(256), 0, s,
-                            static_cast<const uint16_t*>(x), ld, static_cast<uint16_t*>(to), pitch, rows, cols, mask);
-  return launch_dependent(layout_kernel<uint8_t>, dim3(grid), dim3(256), 0, s, static_cast<const uint8_t*>(x),
-                          ld, static_cast<uint8_t*>(to), pitch, rows, cols, mask);
+  return launch_dependent(size == 2 ? layout_kernel<uint16_t> : layout_kernel<uint8_t>, dim3(grid), dim3(256), 0, s,
+                          a, b);
 }
 
 int check(const unif_moe_linear* p) {
@@ -1497,17 +1506,19 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
   }
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   long long px = ld_x, pw = ld_w;
+  ln::Rows copies[2] = {};
   if (!ln::tma_rows(x, ld_x, size)) {
     px = ln::pitch_of(p->cols, size);
-    UNIF_LAUNCH(ln::launch_layout(x, ld_x, ws, px, p->rows, p->cols, size, nullptr, sms, s));
+    copies[0] = {x, ld_x, ws, px, p->rows, p->cols, nullptr};
     x = ws;
     ws += ln::round_up(p->rows * px * size);
   }
   if (!ln::tma_rows(w, ld_w, size)) {
     pw = ln::pitch_of(p->cols, size);
-    UNIF_LAUNCH(ln::launch_layout(w, ld_w, ws, pw, p->n, p->cols, size, nullptr, sms, s));
+    copies[1] = {w, ld_w, ws, pw, p->n, p->cols, nullptr};
     w = ws;
   }
+  UNIF_LAUNCH(ln::launch_layout(copies[0], copies[1], size, sms, s));
   const int steps = (int)(((int64_t)p->cols * size + 127) / 128);
   const bool wide = ln::tma_out(out, ld_out, p->n, os) && (!residual || ln::tma_out(residual, ld_res, p->n, os)) &&
                     (!z || ln::tma_out(z, ld_z, p->n, 2));
@@ -1573,14 +1584,16 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
   }
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const void *x = g->x_dev, *w = g->w_dev, *dz = g->dout_dev;
+  ln::Rows copies[2] = {};
   if (pl.copy_x) {
     x = ws + pl.x;
-    UNIF_LAUNCH(ln::launch_layout(g->x_dev, g->ld_x, ws + pl.x, pl.px, p->rows, p->cols, 2, g->token_mask_dev, sms, s));
+    copies[0] = {g->x_dev, g->ld_x, ws + pl.x, pl.px, p->rows, p->cols, g->token_mask_dev};
   }
   if (pl.copy_w) {
     w = ws + pl.w;
-    UNIF_LAUNCH(ln::launch_layout(g->w_dev, g->ld_w, ws + pl.w, pl.pw, p->n, p->cols, 2, nullptr, sms, s));
+    copies[1] = {g->w_dev, g->ld_w, ws + pl.w, pl.pw, p->n, p->cols, nullptr};
   }
+  UNIF_LAUNCH(ln::launch_layout(copies[0], copies[1], 2, sms, s));
   if (pl.make_dz || pl.sums) {
     ln::GradParams q{};
     q.rows = p->rows;
