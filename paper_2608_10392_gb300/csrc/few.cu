@@ -593,6 +593,7 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
   struct Step {
     bool on, last;  // there is one; it is the last of its item's tokens
     int tokens;
+    uint32_t taking;  // (kAll) the tokens that run the pair
     const uint8_t* slots;
     const __nv_bfloat16* h;
   };
@@ -619,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
   };
   Piece v[kAhead][P];
   auto take = [&](Piece (&to)[P]) {  // the next step, its h on its way
-    Step st{ahead.w.pair < pairs, false, 0, nullptr, nullptr};
+    Step st{ahead.w.pair < pairs, false, 0, (uint32_t)taking, nullptr, nullptr};
     if (!st.on) return st;
     st.h = p.h + (long long)ahead.e * p.T * p.H + ahead.ch + k0;
     if constexpr (kAll) {
@@ -671,7 +672,12 @@ __global__ void __launch_bounds__(kThreads, 2) down_kernel(const Params p, const
       fetch();
       ring.read(lo, hi);
       if constexpr (kAll) {
-        multiply(c[0], lo, hi, v[k][0]);
+        // (what does not run the pair adds nothing of it, not 0 times an infinity either)
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        multiply(y, lo, hi, v[k][0]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (now.taking >> ((lane & 3) * 2 + (j & 1)) & 1u) c[0][j] += y[j];
       } else {
 #pragma unroll
         for (int t = 0; t < NT; ++t)

@@ -123,6 +123,33 @@ def test_thresholds_masks_and_bias(T, th):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 8, 9, 40])
+def test_weights_that_are_not_finite(T):
+    """An expert's infinities and NaN reach the tokens that take it and no others."""
+    from paper_2608_10392_gb300 import few_tokens, router_table
+    d, H, K, B = 64, 256, 4, 4
+    w, g = layer(d, H, K, B, 3)
+    x = torch.randn(T, d, generator=g).bfloat16().cuda()
+    on = {k: v.cuda() for k, v in w.items() if v is not None}
+    table = router_table(on["router"], on["up"], B)
+    k = dict(alpha_fixed=0.5, topk_fixed=1, prefix_blocks=True)
+    want = few_tokens(x, table, on["up"], on["down"], B, **k)
+    first = (x.to(F64) @ on["router"].to(F64))[:, 1:].argmax(1)
+    e = int(first[0])
+    takes = first == e
+    if bool(takes.all()):
+        x[1] = -x[0]
+        want = few_tokens(x, table, on["up"], on["down"], B, **k)
+        takes = (x.to(F64) @ on["router"].to(F64))[:, 1:].argmax(1) == e
+    for name, value in (("up", math.nan), ("down", math.inf), ("down", math.nan)):
+        bad = {n: on[n].clone() for n in ("up", "down")}
+        bad[name][1 + e] = value
+        y = few_tokens(x, table, bad["up"], bad["down"], B, **k)
+        assert not takes.all() and torch.equal(y[~takes], want[~takes])
+        assert not y[takes].isfinite().any()
+
+
+@pytest.mark.gpu
 def test_no_tokens_and_all_padding():
     from paper_2608_10392_gb300 import few_tokens, router_table
     w, g = layer(64, 256, 3, 4, 1)
