@@ -1161,11 +1161,8 @@ Tiles pick_tiles(long long M, int N, int steps, bool may_split, int sms) {
   const double met = M < 128 ? (M + 31) / 32 / 4.0 : 1.0;  // rows of a tile that there are
   for (int pair = 0; pair < 2; ++pair) {
     const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
-    int last = 0;
-    for (int parts = (N + 255) / 256; parts <= (N + 31) / 32; ++parts) {
-      const int n = even_part(N, parts);
-      if (n == last) continue;
-      last = n;
+    for (int n = 256; n > 0; n -= 32) {
+      if (n != even_part(N, (N + n - 1) / n)) continue;  // as many tiles fit narrower ones
       const long long tiles = m * ((N + n - 1) / n), waves = (tiles + units - 1) / units;
       const double step = pair ? std::max(350.0, std::max(2.0 * n, 256.0 + n)) : std::max(300.0, 2.4 * n);
       auto take = [&](double cost, int split) {
@@ -1198,11 +1195,8 @@ Tiles pick_weight_tiles(long long M, int N, int steps, int sms, int* splits) {
   *splits = 1;
   for (int pair = 0; pair < 2; ++pair) {
     const long long rows = pair ? 256 : 128, m = (M + rows - 1) / rows, units = pair ? sms / 2 : sms;
-    int last = 0;
-    for (int parts = (N + 255) / 256; parts <= (N + 63) / 64; ++parts) {
-      const int n = even_part(N, parts);
-      if (n == last) continue;
-      last = n;
+    for (int n = 256; n > 0; n -= 32) {
+      if (n != even_part(N, (N + n - 1) / n)) continue;
       const int held = (n / (pair ? 2 : 1) + 63) / 64 * 64;  // columns of the blocks in shared memory
       const long long tiles = m * ((N + n - 1) / n);
       const double step = pair ? std::max(2.0 * n, 256.0 + held + n / 2) : 256.0 + held + n;
@@ -1238,12 +1232,12 @@ bool map_out(Out* o, const Params& p) {
   auto fits = [&](const void* q, long long ld, int bytes) { return !q || tma_out(q, ld, p.own_rows ? 16 : p.N, bytes); };
   o->wide = fits(p.out, p.ld_out, size) && fits(p.residual, p.ld_res, size) && fits(p.z, p.ld_z, 2);
   if (!o->wide) return true;
-  const uint64_t plane = (uint64_t)p.M * p.ld_out * size;
+  const uint64_t plane = (uint64_t)(p.splits > 1 ? p.M : 1) * p.ld_out * size;
   if (!encode_box_map(&o->out, p.out, size, p.N, p.M, p.splits, p.ld_out * size, plane, box, 64)) return false;
   o->res = o->z = o->out;
-  if (p.residual && !encode_box_map(&o->res, p.residual, size, p.N, p.M, 1, p.ld_res * size, p.ld_res * size * (uint64_t)p.M, box, 64))
+  if (p.residual && !encode_box_map(&o->res, p.residual, size, p.N, p.M, 1, p.ld_res * size, p.ld_res * size, box, 64))
     return false;
-  return !p.z || encode_box_map(&o->z, p.z, 2, p.N, p.M, 1, p.ld_z * 2, p.ld_z * 2 * (uint64_t)p.M, box, size == 2 ? 64 : 0);
+  return !p.z || encode_box_map(&o->z, p.z, 2, p.N, p.M, 1, p.ld_z * 2, p.ld_z * 2, box, size == 2 ? 64 : 0);
 }
 
 template <int KIND, typename TO>
@@ -1334,6 +1328,17 @@ int check(const unif_moe_linear* p) {
     return UNIF_MOE_ERR_ARG;
   }
   return UNIF_MOE_OK;
+}
+
+// Whether two arrays of rows share memory (columns of one wider array, each its own, do not). Bytes.
+bool overlap(const void* a, int64_t ld_a, int64_t width_a, int64_t rows_a, const void* b, int64_t ld_b,
+             int64_t width_b, int64_t rows_b) {
+  if (!a || !b || rows_a < 1 || rows_b < 1) return false;
+  const uintptr_t pa = bits(a), pb = bits(b);
+  if (pa + (rows_a - 1) * ld_a + width_a <= pb || pb + (rows_b - 1) * ld_b + width_b <= pa) return false;
+  if (ld_a != ld_b) return true;
+  const int64_t apart = (int64_t)((pa > pb ? pa - pb : pb - pa) % (uint64_t)ld_a);  // of the later one, in a row
+  return apart < (pa > pb ? width_b : width_a) || apart + (pa > pb ? width_a : width_b) > ld_a;
 }
 
 int in_size(const unif_moe_linear* p) { return p->in_dtype == UNIF_MOE_BF16 ? 2 : 1; }
@@ -1466,6 +1471,14 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
   }
   if (need && ln::bits(workspace) % 16) {
     set_error("the workspace must be 16-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  auto over = [&](const void* q, int64_t ld, int64_t width, int64_t rows, int bytes) {
+    return ln::overlap(out, ld_out * os, (int64_t)p->n * os, p->rows, q, ld * bytes, width * bytes, rows);
+  };
+  if (over(x, ld_x, p->cols, p->rows, size) || over(w, ld_w, p->cols, p->n, size) || over(z, ld_z, p->n, p->rows, 2) ||
+      ((out != residual || (ld_out != ld_res && p->rows > 1)) && over(residual, ld_res, p->n, p->rows, os))) {
+    set_error("out overlaps x, w, z or another residual than itself");
     return UNIF_MOE_ERR_ARG;
   }
   int sms = 0;

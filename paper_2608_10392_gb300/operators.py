@@ -164,6 +164,8 @@ class BlockNorm:
         pre_rstd [T] that backward takes (None for a norm that is not there; means of
         an rms norm are 0). Without y: the norm before a stack's first block."""
         if self.eight:
+            if u is not None and not isinstance(u, Fp8):
+                raise ValueError("u: need an Fp8, got %s" % type(u).__name__)
             codes, scales = (None, None) if u is None else (u.codes, u.scales)
             r = _b().norm_forward_fp8(self._desc, x, y, post_weight, post_bias, gate, pre_weight,
                                       pre_bias, mask, out, codes, stats, stream, scales)
@@ -314,7 +316,7 @@ def linear(x, w, bias: Optional[torch.Tensor] = None, *, activation: str = "none
 
     x [T][cols] and w [n][cols] both bf16 or both Fp8 (rows under a scale each); rows of all
     2-d tensors may be strided, with any alignment. bias [n] fp32 or bf16; residual [T][n] of
-    the result's dtype (out may be it); activation "none" or "gelu"; mask [T]: 0 marks padding,
+    the result's dtype (out may be it, and shares memory with nothing else); activation "none" or "gelu"; mask [T]: 0 marks padding,
     whose rows give 0. keep: also z = x w^T + bias in bf16, (out, z), for linear_backward."""
     if isinstance(x, Fp8) != isinstance(w, Fp8):
         raise ValueError("x and w: need both in 8 bits or neither")

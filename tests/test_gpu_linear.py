@@ -174,6 +174,28 @@ def test_result_in_place_of_the_residual(T, n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [6, 50, 300])
+def test_one_array_for_operands_and_result(T):
+    """Columns of one array side by side; what would be written while it is read is refused."""
+    from paper_2608_10392_gb300 import UnifMoeError, linear
+    g = torch.Generator(device="cuda").manual_seed(T)
+    wide = torch.randn(T, 64 + 48 + 48, generator=g, device="cuda").bfloat16()
+    w = operand(48, 64, g)
+    x, res, out = wide[:, :64], wide[:, 64:112], wide[:, 112:]
+    before = wide[:, :112].clone()
+    want = check(x.clone(), w, residual=res.clone())
+    assert torch.equal(check(x, w, residual=res, out=out), want) and torch.equal(wide[:, :112], before)
+    square = operand(64, 64, g)
+    for k in (dict(x=x, w=square, out=x), dict(x=x, w=square, out=wide[:, 32:96]),
+              dict(x=x[1:], w=w, out=wide[:-1, 60:108]), dict(x=x, w=w, residual=wide[:, 80:128], out=out),
+              dict(x=x[1:], w=w, residual=out[1:], out=out[:-1]),
+              dict(x=wide[:, :32], w=wide[:4, 64:96], out=wide[:, 66:70])):
+        with pytest.raises(UnifMoeError, match="overlaps"):
+            linear(**k)
+    assert torch.equal(wide[:, :112], before)
+
+
+@pytest.mark.gpu
 def test_offsets_beyond_32_bits():
     """More than 2^31 elements of result: the last rows are as right as the first."""
     from paper_2608_10392_gb300 import linear
