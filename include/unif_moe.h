@@ -733,8 +733,8 @@ UNIF_MOE_API int64_t unif_moe_linear_backward_workspace(const unif_moe_linear* p
 /* Gradients of unif_moe_linear_forward for bf16 rows and weights, from that of the
  * result (dout_dev [T][n]; the residual's gradient is dout itself):
  *   dz = dout act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum_t dz
- * z_dev [T][n] is the forward's; not read (may be NULL) without an activation. Padding rows are not read
- * (whatever they hold), take no part in the sums and give 0 in dx. dz enters the
+ * z_dev [T][n] is the forward's; not read (may be NULL) without an activation. Padding rows (whatever
+ * they hold) take no part in the sums and give 0 in dx. dz enters the
  * products rounded to bf16, their operand type (exact for a bf16 dout without
  * activation); dbias sums it unrounded. Sums are fp32, in an order that depends on the sizes alone.
  * in_dtype must be BF16; out_dtype and bias_dtype of p are not used. Enqueued on

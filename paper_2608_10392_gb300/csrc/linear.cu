@@ -36,10 +36,11 @@ enum Kind {
 
 constexpr int kEpiWarps = 16, kTmaWarp = 16, kMmaWarp = 17;
 constexpr int kEpiThreads = 32 * kEpiWarps;
+constexpr int kCleanWarps = 8;  // of them, where padding rows are set to 0
 constexpr int kThreads = kEpiThreads + 64;
 constexpr uint32_t kTmemCols = 512, kAcc = 256;
 constexpr int kMaxStages = 8;
-constexpr int kBars = 2 * kMaxStages + 5 + 2 * kEpiWarps;
+constexpr int kBars = 3 * kMaxStages + 5 + 2 * kEpiWarps;
 constexpr uint32_t kSmemMax = 232448;
 // Staging of a storing warp: a box of 32 rows by 64 bytes, or two, and one for z; or, for rows that
 // TMA cannot write, 32 rows by 16 fp32 values. Two boxes with a residual, which comes there first,
@@ -72,6 +73,9 @@ struct Params {
   const void* residual;
   long long ld_res;
   const uint8_t* mask;
+  bool clean_a, clean_b;           // ... the operands that may hold anything in padding rows
+  const int* live;                 // kWeight with padding: how many steps have a row that is none, and which
+  const unsigned long long* dead;  // a bit for each row of these steps, padding 1
   __nv_bfloat16* z;
   long long ld_z;
   int* status;
@@ -288,17 +292,24 @@ __device__ __forceinline__ float residual_of(const Params& p, long long row, int
 // threads, a row each, a store touches 32 lines and the storing warps are bound by that:
 // 12,608 x 384 to 1,536 with GELU and z 26 us ...)
 //
-// SPLIT (WIDE, not PAIR): a cluster of p.splits CTAs shares a tile, each a part of its reduction; their
+// FORM (forward and dx; WIDE, not PAIR): a cluster of p.splits CTAs shares a tile, each a part of its reduction; their
 // sums meet in shared memory, where each adds and finishes a share of the tile. For few rows and a
 // long reduction, whose steps one CTA would run one after another (us, without and with: 256 x 4,096 to
 // 1,024 13.9 and 9; ...).
-template <int KIND, typename TO, bool PAIR, bool WIDE, bool SPLIT>
+//
+// FORM (dw): some rows are padding. Steps of none but such rows are not taken (Params::live), the others'
+// padding rows set to 0 in shared memory before the MMAs read them, by half of the warps that store; a CTA of a
+// pair then waits for its own bytes. (Against rows copied first, padding 0, all gradients, us: 32,768 x 4,096
+// and 1,024, sequences of 100 to 512 of 512 434 and 320, every fourth row at random padding 446 and 387; 12,608 x
+// 1,536 and 384 61 and 50, 62 and 54. Warps that take turns at the steps would have to wait on every one all the
+// same: loads land out of order, and a barrier's parity tells only the last use from the one before.)
+template <int KIND, typename TO, bool PAIR, bool WIDE, bool FORM>
 __global__ void __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmRes,
                 const __grid_constant__ CUtensorMap tmZ, const Params p) {
   constexpr int kCtas = PAIR ? 2 : 1, kTileM = 128 * kCtas, kUnit = 16 * kCtas;  // columns of an MMA: whole units
-  constexpr bool kParts = KIND == kWeight;
+  constexpr bool kParts = KIND == kWeight, clean = kParts && FORM, SPLIT = !kParts && FORM;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
   const bool leader = rank == 0;
   static_assert(!SPLIT || (WIDE && !PAIR), "forms");
@@ -319,19 +330,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto acce_bar = [&](int a) { return bar0 + 8u * (2 * kMaxStages + 2 + a); };
   const uint32_t mma_done = bar0 + 8u * (2 * kMaxStages + 4);
   auto box_bar = [&](int w, uint32_t k) { return bar0 + 8u * (2 * kMaxStages + 5 + 2 * w + (k & 1u)); };
+  auto clean_bar = [&](int s) { return bar0 + 8u * (2 * kMaxStages + 5 + 2 * kEpiWarps + s); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* columns = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(bars + kBars + 1) + 15) & ~(uintptr_t)15);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int epi_warps = clean ? kEpiWarps - kCleanWarps : kEpiWarps;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
+      mbar_init(clean_bar(s), kCtas * kCleanWarps);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(accf_bar(a), 1);
-      mbar_init(acce_bar(a), kCtas * kEpiWarps);
+      mbar_init(acce_bar(a), kCtas * epi_warps);
     }
     mbar_init(mma_done, 1);
     for (int w = 0; w < kEpiWarps; ++w) {
@@ -404,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (kParts)
       for (; w.m >= p.m_tiles; w.m -= p.m_tiles) ++w.part;
   };
+  const int all_steps = clean ? *p.live : p.steps;
   auto item_of = [&](const Walk& w) {
     Item it;
     it.part = w.part;
@@ -411,16 +426,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     it.n0 = w.n * p.tile_n;
     it.n = min(p.tile_n, p.N - it.n0);
     const int part = SPLIT ? (int)share : it.part;
-    it.from = kParts || SPLIT ? (int)((long long)p.steps * part / p.splits) : 0;
-    it.to = kParts || SPLIT ? (int)((long long)p.steps * (part + 1) / p.splits) : p.steps;
+    it.from = kParts || SPLIT ? (int)((long long)all_steps * part / p.splits) : 0;
+    it.to = kParts || SPLIT ? (int)((long long)all_steps * (part + 1) / p.splits) : p.steps;
     return it;
   };
 
-  if (warp < kEpiWarps) {
+  if (warp < epi_warps) {
     // ---------------- accumulators to the result ----------------------------
-    // Four warps to a quarter of the rows, W columns at a time. (A wait given up is not the end
+    // Four warps (two beside those that clean) to a quarter of the rows, W columns at a time. (A wait given up is not the end
     // of the loop: the warps meet at a barrier.)
     constexpr int W = WIDE ? 64 / (int)sizeof(TO) : 16;
+    constexpr int parts = epi_warps / 4;
     const int q = warp & 3, part = warp >> 2;
     int acc = 0;       // the accumulator of the item's sum
     uint32_t ph = 0;   // a phase bit per accumulator
@@ -508,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int n_pieces = pieces(it);
       bool on = there;
       float scale = 1.f;
-      if (KIND < kInput && there && p.mask) on = p.mask[row] != 0;
+      if (KIND != kWeight && there && p.mask) on = p.mask[row] != 0;
       if (KIND < kInput && there && p.sm) scale = p.sm[row];
       const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
       const int n_sums = sums(it);
@@ -516,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 1; j < n_sums; ++j) {  // further accumulations, added to the first
         wait_acc(acc ^ 1);
         if (!ok) break;
-        for (int c = part; c < n_pieces; c += 4)
+        for (int c = part; c < n_pieces; c += parts)
 #pragma unroll
           for (int h = 0; h < W; h += 16) {
             uint32_t u[16], v[16];
@@ -534,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) continue;
       if constexpr (SPLIT) {
         // (all of this CTA's MMAs have completed: the ring is free) rows of tile_n + 4 values
-        for (int c = part; c < n_pieces; c += 4) {
+        for (int c = part; c < n_pieces; c += parts) {
           float v[W];
           if constexpr (W == 32) tmem_ld32(lanes + acc * kAcc + c * W, v);
           else tmem_ld16(lanes + acc * kAcc + c * W, v);
@@ -548,14 +564,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         acc ^= 1;
         continue;
       }
-      for (int c = part; c < n_pieces; c += 4) {
+      for (int c = part; c < n_pieces; c += parts) {
         float v[W];
         if constexpr (W == 32) tmem_ld32(lanes + acc * kAcc + c * W, v);
         else tmem_ld16(lanes + acc * kAcc + c * W, v);
-        if (c + 4 >= n_pieces) release(acc);
+        if (c + parts >= n_pieces) release(acc);
         const int ch = it.n0 + c * W;
         if constexpr (WIDE) {
           if constexpr (KIND < kInput) finish_row<W>(p, v, scale, on, cols + c * W, cols + 256 + c * W);
+          else if (KIND == kInput && !on)
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[e] = 0.f;
           const uint32_t box = box0 + (k & 1u) * two, z_box = box0 + two + kBox;
           if (with_res) {
             ok = wait_warp(box_bar(warp, k), k >> 1 & 1u, abort_flag, p.status, p.wait_limit);
@@ -621,7 +640,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int r = r0 + 2 * (e + h);
-              y[h] = stg[r * 17 + col];
+              y[h] = KIND == kWeight || (live >> r & 1u) ? stg[r * 17 + col] : 0.f;
               if constexpr (KIND < kInput) {
                 const float sm = scaled ? __shfl_sync(0xffffffffu, scale, r) : 1.f;
                 y[h] = live >> r & 1u ? fmaf(y[h], sm * sn, b) : 0.f;
@@ -648,6 +667,46 @@ __global__ void __launch_bounds__(kThreads, 1)
       bulk_wait_all();
     }
     __syncwarp();
+  } else if (clean && warp < kEpiWarps) {
+    // ---------------- padding rows to 0 (kWeight): eight of a step's 64 rows to a warp ----
+    const int r0 = (warp - epi_warps) * (64 / kCleanWarps);
+    static_assert(kCleanWarps == 8, "a byte of padding bits");
+    int s = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (Walk at = start(); at.i < n_items && ok; next(at)) {
+      const Item it = item_of(at);
+      const int blocks = ((it.n + kUnit - 1) / kUnit * 16 + 63) / 64;
+      uint32_t bits = 0;  // of a lane's step of the next 32: this warp's rows that are padding; bit 8: all 64 are
+      for (int k = it.from; k < it.to; ++k) {
+        const int of32 = (k - it.from) & 31;
+        if (of32 == 0) {
+          const unsigned long long d = k + lane < it.to ? p.dead[k + lane] : 0ull;
+          bits = ((uint32_t)(d >> r0) & 255u) | (d == ~0ull ? 256u : 0u);
+        }
+        ok = wait_warp(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        const uint32_t dead = __shfl_sync(0xffffffffu, bits, of32);
+        if (dead) {
+          const uint32_t a = stage(s) + r0 * 128 + lane * 16, b = a + 16384u;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {  // 128 bytes of four rows at a time
+            if (!(dead >> (h * 4 + (lane >> 3)) & 1u)) continue;
+            if (p.clean_a || dead >> 8) {
+              put4(a + h * 512u, 0u, 0u, 0u, 0u);
+              put4(a + h * 512u + 8192u, 0u, 0u, 0u, 0u);
+            }
+            if (p.clean_b || dead >> 8)
+              for (int j = 0; j < blocks; ++j) put4(b + h * 512u + j * 8192u, 0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+        }
+        __syncwarp();
+        if (lane == 0) arrive_leader(clean_bar(s));
+        if (++s == n_st) { s = 0; ph ^= 1u; }
+      }
+    }
+    __syncwarp();
   } else if (warp == kTmaWarp) {
     // ---------------- operands (one lane runs the role from end to end) -----
     if (elect_one()) {
@@ -656,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t ph = 0;
       long long issued = 0;
       auto load = [&](uint32_t dst, const CUtensorMap* from, uint32_t bar, int c0, int c1) {
-        if (PAIR) tma_load_2d_pair(dst, from, mapa_shared(bar, 0), c0, c1);
+        if (PAIR) tma_load_2d_pair(dst, from, mapa_shared(bar, clean ? rank : 0), c0, c1);
         else tma_load_2d(dst, from, bar, c0, c1);
       };
       constexpr int kCols = KIND == kForward8 ? 128 : 64;  // reduction elements of a step
@@ -666,11 +725,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n = (it.n + kUnit - 1) / kUnit * 16, n0 = it.n0 + (int)rank * n;
         const int blocks = (n + 63) / 64;  // of an MN-major operand
         const uint32_t bytes = 16384u + (KIND >= kInput ? blocks * 8192u : (uint32_t)(p.tile_n / kCtas) * 128u);
-        for (int k = it.from; k < it.to; ++k) {
+        int coming = clean && it.from < it.to ? p.live[1 + it.from] : 0;  // (a step ahead)
+        for (int i = it.from; i < it.to; ++i) {
+          const int k = clean ? coming : i;
+          if (clean && i + 1 < it.to) coming = p.live[2 + i];
           ok = wait_bounded(empty_bar(s), ph ^ 1u, abort_flag, p.status, p.wait_limit);
           if (!ok) break;
           const uint32_t bar = full_bar(s), a = stage(s), b = a + 16384u;
-          if (leader) mbar_expect_tx(bar, kCtas * bytes);
+          if (clean) mbar_expect_tx(bar, bytes);
+          else if (leader) mbar_expect_tx(bar, kCtas * bytes);
           if (KIND == kWeight) {
             load(a, &tmA, bar, it.m0, k * kCols);
             load(a + 8192u, &tmA, bar, it.m0 + 64, k * kCols);
@@ -686,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       // loads still in flight land before the CTA (pair) exits
-      for (long long j = issued > n_st ? issued - n_st : 0; leader && j < issued; ++j)
+      for (long long j = issued > n_st ? issued - n_st : 0; (leader || clean) && j < issued; ++j)
         wait_settle(full_bar((int)(j % n_st)), (uint32_t)((j / n_st) & 1), p.wait_limit / 16);
     }
     __syncwarp();
@@ -709,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t d = tmem + to * kAcc;
           const int first = first_step(it, n_sums, j), last = first_step(it, n_sums, j + 1);
           for (int k = first; k < last; ++k) {
-            ok = wait_bounded(full_bar(s), ph, abort_flag, p.status, p.wait_limit);
+            ok = wait_bounded(clean ? clean_bar(s) : full_bar(s), ph, abort_flag, p.status, p.wait_limit);
             if (!ok) break;
             tc_fence_after();
             const uint32_t sa = stage(s), sb = sa + 16384u;
@@ -768,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (r < p.splits)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += a[r][e];
-        const bool on = KIND >= kInput || !p.mask || p.mask[row] != 0;
+        const bool on = !p.mask || p.mask[row] != 0;
         TO* out = static_cast<TO*>(p.out) + row * p.ld_out + ch;
         if constexpr (KIND < kInput) {
           finish_row<4>(p, v, p.sm ? p.sm[row] : 1.f, on, columns + c, columns + 256 + c);
@@ -792,6 +855,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
+        if (KIND == kInput && !on) v[0] = v[1] = v[2] = v[3] = 0.f;
         if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
         else *reinterpret_cast<uint2*>(out) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
       }
@@ -940,6 +1004,56 @@ __global__ void __launch_bounds__(256) layout_kernel(const Rows a, const Rows b)
     for (int e = 0; e < 8; ++e)
       if (c0 + 32 * e < j.cols) to[32 * e] = v[e];
   }
+}
+
+// The steps of 64 rows that are not all padding, in order: how many, which, and their padding rows' bits. At least
+// `least` (and no more than there are): the list is filled up with steps all of whose bits are set. One CTA.
+constexpr int kListThreads = 1024;
+__global__ void __launch_bounds__(kListThreads) steps_kernel(const uint8_t* mask, long long rows, int least, int* live,
+                                                             unsigned long long* dead) {
+  __shared__ int found[kListThreads / 32];
+  grid_dep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int steps = (int)((rows + 63) / 64);
+  const bool aligned = reinterpret_cast<uintptr_t>(mask) % 16 == 0;
+  int before = 0;
+  for (int from = 0; from < steps; from += kListThreads) {
+    const int step = from + (int)threadIdx.x;
+    const long long row0 = (long long)step * 64;
+    unsigned long long d = 0ull;
+    if (aligned && row0 + 64 <= rows) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 m = *(reinterpret_cast<const uint4*>(mask + row0) + i);
+        const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)  // bit 0 of each byte to four bits side by side
+          d |= (unsigned long long)((__vcmpeq4(w[e], 0u) & 0x01010101u) * 0x10204080u >> 28) << (16 * i + 4 * e);
+      }
+    } else {
+      for (int i = 0; i < 64; ++i) d |= (unsigned long long)(row0 + i >= rows || mask[row0 + i] == 0) << i;
+    }
+    const bool on = step < steps && d != ~0ull;
+    const uint32_t b = __ballot_sync(0xffffffffu, on);
+    if (lane == 0) found[warp] = __popc(b);
+    __syncthreads();
+    int at = before + __popc(b & ((1u << lane) - 1u));
+#pragma unroll
+    for (int w = 0; w < kListThreads / 32; ++w) {
+      if (w < warp) at += found[w];
+      before += found[w];
+    }
+    if (on) {
+      live[1 + at] = step;
+      dead[at] = d;
+    }
+    __syncthreads();
+  }
+  for (int i = before + (int)threadIdx.x; i < min(least, steps); i += kListThreads) {
+    live[1 + i] = 0;
+    dead[i] = ~0ull;
+  }
+  if (threadIdx.x == 0) *live = max(before, min(least, steps));
 }
 
 struct GradParams {
@@ -1266,11 +1380,15 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
                  const Params) =
       t.pair ? (wide ? gemm_kernel<KIND, TO, true, true, false> : gemm_kernel<KIND, TO, true, false, false>)
              : (wide ? gemm_kernel<KIND, TO, false, true, false> : gemm_kernel<KIND, TO, false, false, false>);
-  if constexpr (KIND != kWeight)
+  if constexpr (KIND != kWeight) {
     if (split) {
       kernel = gemm_kernel<KIND, TO, false, true, true>;
       p.splits = t.split;
     }
+  } else if (p.live) {
+    kernel = t.pair ? (wide ? gemm_kernel<KIND, TO, true, true, true> : gemm_kernel<KIND, TO, true, false, true>)
+                    : (wide ? gemm_kernel<KIND, TO, false, true, true> : gemm_kernel<KIND, TO, false, false, true>);
+  }
   const cudaError_t e = allow_smem_once(kernel, smem);
   if (e != cudaSuccess) return e;
   const long long items = (long long)t.m_tiles * t.n_tiles * (split ? 1 : p.splits);
@@ -1355,19 +1473,19 @@ int64_t forward_bytes(const unif_moe_linear* p, const void* x, long long ld_x, c
 // The workspace of a backward: where each part begins.
 struct Plan {
   int sms, splits, blocks, per;
-  bool copy_x, copy_w, make_dz, sums;
+  bool copy_x, copy_w, make_dz, sums, list;
   long long px, pw, pz;  // pitches
-  int64_t x, w, dz, part, bias, total;
+  int64_t x, w, dz, part, bias, live, dead, total;
   Tiles in, weight;
 };
 Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int sms) {
   Plan r{};
   r.sms = sms;
   const long long T = p->rows;
-  r.copy_x = g->dw_dev && (g->token_mask_dev || !tma_rows(g->x_dev, g->ld_x, 2));
+  r.copy_x = g->dw_dev && !tma_rows(g->x_dev, g->ld_x, 2);
   r.copy_w = g->dx_dev && !tma_rows(g->w_dev, g->ld_w, 2);
   r.make_dz = (g->dx_dev || g->dw_dev) &&
-              (p->activation != UNIF_MOE_ACTIVATION_NONE || g->dout_dtype != UNIF_MOE_BF16 || g->token_mask_dev ||
+              (p->activation != UNIF_MOE_ACTIVATION_NONE || g->dout_dtype != UNIF_MOE_BF16 ||
                !tma_rows(g->dout_dev, g->ld_dout, 2));
   r.sums = g->dbias_dev != nullptr;
   r.px = r.copy_x ? pitch_of(p->cols, 2) : g->ld_x;
@@ -1391,6 +1509,9 @@ Plan plan_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g, int 
   r.dz = take(r.make_dz, T * r.pz * 2);
   r.part = take(g->dw_dev && r.splits > 1, (int64_t)r.splits * p->n * part_pitch(p->cols) * 4);
   r.bias = take(r.sums, (int64_t)r.blocks * p->n * 4);
+  r.list = g->dw_dev && g->token_mask_dev;
+  r.live = take(r.list, 4 * (int64_t)(steps + 1));
+  r.dead = take(r.list, 8 * (int64_t)steps);
   r.total = at;
   return r;
 }
@@ -1607,6 +1728,10 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     copies[1] = {g->w_dev, g->ld_w, ws + pl.w, pl.pw, p->n, p->cols, nullptr};
   }
   UNIF_LAUNCH(ln::launch_layout(copies[0], copies[1], 2, sms, s));
+  if (pl.list)
+    UNIF_LAUNCH(unif::launch_dependent(ln::steps_kernel, dim3(1), dim3(ln::kListThreads), 0, s, g->token_mask_dev,
+                                       (long long)p->rows, pl.splits, reinterpret_cast<int*>(ws + pl.live),
+                                       reinterpret_cast<unsigned long long*>(ws + pl.dead)));
   if (pl.make_dz || pl.sums) {
     ln::GradParams q{};
     q.rows = p->rows;
@@ -1638,6 +1763,7 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.N = p->cols;
     e.splits = 1;
     e.steps = (p->n + 63) / 64;
+    e.mask = pl.make_dz ? nullptr : g->token_mask_dev;  // (dz's own padding rows are 0)
     e.out = g->dx_dev;
     e.ld_out = g->ld_dx;
     e.status = status;
@@ -1658,6 +1784,12 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.out = pl.splits > 1 ? ws + pl.part : g->dw_dev;
     e.ld_out = pl.splits > 1 ? ln::part_pitch(p->cols) : g->ld_dw;
     e.own_rows = pl.splits > 1;
+    e.clean_a = !pl.make_dz;
+    e.clean_b = !pl.copy_x;
+    if (pl.list) {
+      e.live = reinterpret_cast<const int*>(ws + pl.live);
+      e.dead = reinterpret_cast<const unsigned long long*>(ws + pl.dead);
+    }
     e.status = status;
     CUtensorMap a, b;
     if (!ln::map_rows(&a, dz, 2, p->n, p->rows, pl.pz, 64) || !ln::map_rows(&b, x, 2, p->cols, p->rows, pl.px, 64)) {

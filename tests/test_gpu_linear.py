@@ -297,6 +297,28 @@ def test_gradients(T, cols, n, act, masked, grad_dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,cols,n,act", [(64, 64, 64, "none"), (1300, 200, 136, "none"), (1300, 77, 130, "gelu"),
+                                          (30001, 264, 200, "none"), (70000, 64, 72, "gelu")])
+def test_gradients_of_long_padding(T, cols, n, act):
+    """Runs of padding that are longer than a step of the reduction, at the ends and in between; all but
+    one row; masks at any address."""
+    k = grads(T, cols, n, T, act, True)
+    for name in ("x", "dout", "z"):
+        if name in k:
+            k[name].copy_(torch.randn(k[name].shape, device="cuda"))
+    row = torch.arange(T, device="cuda")
+    for mask in (row >= T // 2, row < T // 3, (row // 100) % 3 == 1, row == T - 1, row == 0, row % 64 == 63):
+        wide = torch.zeros(T + 1, dtype=torch.bool, device="cuda")
+        wide[1:] = mask
+        for m in (mask, wide[1:]):
+            b = dict(k, mask=m, **{name: k[name].clone() for name in ("x", "dout", "z") if name in k})
+            for name in ("x", "dout", "z"):
+                if name in b:
+                    b[name][~m] = float("nan")
+            check_backward(**b)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("pad,shift", [(8, 0), (3, 1), (1, 0)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gradients_of_strided_rows(pad, shift, dtype):
