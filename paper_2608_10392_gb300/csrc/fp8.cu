@@ -2,7 +2,9 @@
 // _dequantize; fp8.cuh has the rule).
 //
 // Bound by memory: a row is read once and held in registers while its largest value is
-// found, by a warp up to 1,024 columns, by a CTA up to 8,192; wider rows are read twice.
+// found, by a warp up to 1,024 columns, by a CTA up to 8,192; wider rows are read twice. (us, at the floor
+// of the bytes in brackets: 65,536 x 1,024 fp32 47.2 (49.4: some of them stay in L2), bf16 29.7 (29.7), 12,608 x
+// 4,096 fp32 39.7 (38.0), bf16 31.8 (22.8); back to bf16 65,536 x 1,024 36.0 (29.7).)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -52,7 +52,10 @@ constexpr uint32_t kColumns = 2 * 2 * 256 * 4;          // bias and scales of tw
 // Steps that one accumulation for an fp32 result runs over. The tensor cores
 // truncate the accumulator at every MMA, so the error grows with their number: the sums of
 // longer reductions are added in fp32 (65,536 x 4,096 to 1,024 onto an fp32 residual: 2.5e-6 of the
-// result's norm off in one accumulation, 6e-7 so).
+// result's norm off in one accumulation, 8e-7 so). That costs a wait for the
+// addition each time (370 us against 293 with a bf16 result, whose own rounding is far above it; half of that
+// are the result's bytes). A warp's 64 columns in registers, the accumulator given back at once, spill:
+// 65,536 x 1,024 to 4,096 388 and 560 us.
 constexpr int kSumSteps = 22;
 
 struct Params {
@@ -144,6 +147,12 @@ __device__ __forceinline__ void tmem_ld16_async(uint32_t taddr, uint32_t (&r)[16
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
+}
+
+// (after tmem_wait_ld: nothing that uses the registers may be moved before it)
+__device__ __forceinline__ void arrived(uint32_t (&r)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
 }
 
 // ---- the epilogue's rows ----
@@ -288,14 +297,14 @@ __device__ __forceinline__ float residual_of(const Params& p, long long row, int
 // them and half of the columns' operand in each one's shared memory. The first CTA's
 // barriers take both CTAs' bytes, its MMA lane issues for both.
 // WIDE: the rows of the result (and of z and the residual) are written and read by TMA, from and to
-// staged boxes of 32 rows by 64 bytes, which also cuts them off at the result's ends. (Written by the
-// threads, a row each, a store touches 32 lines and the storing warps are bound by that:
-// 12,608 x 384 to 1,536 with GELU and z 26 us ...)
+// staged boxes of 32 rows by 64 bytes, which also cuts them off at the result's ends. Rows that TMA
+// cannot write go through shared memory and the threads, a lane to a column (us, by TMA and so: 12,608 x 384 to
+// 1,536 17.4 and 45.3, with GELU and z 24.2 and 55.7; 65,536 x 1,024 to 4,096 299 and 575).
 //
 // FORM (forward and dx; WIDE, not PAIR): a cluster of p.splits CTAs shares a tile, each a part of its reduction; their
 // sums meet in shared memory, where each adds and finishes a share of the tile. For few rows and a
 // long reduction, whose steps one CTA would run one after another (us, without and with: 256 x 4,096 to
-// 1,024 13.9 and 9; ...).
+// 1,024 17.4 and 13.1, with GELU and z 21.6 and 13.1; 64 x 4,096 to 1,024 16.3 and 10.5).
 //
 // FORM (dw): some rows are padding. Steps of none but such rows are not taken (Params::live), the others'
 // padding rows set to 0 in shared memory before the MMAs read them, by half of the warps that store; a CTA of a
@@ -539,6 +548,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld16_async(lanes + acc * kAcc + c * W + h, u);
             tmem_ld16_async(lanes + (acc ^ 1) * kAcc + c * W + h, v);
             tmem_wait_ld();
+            arrived(u);
+            arrived(v);
             float w[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(u[e]) + __uint_as_float(v[e]);
