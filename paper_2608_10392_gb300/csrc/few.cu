@@ -17,8 +17,9 @@
 // Weights stream through a ring of a warp's own in shared memory (cp.async, 2 KB a stage), so that what
 // is on its way does not depend on registers; the products are mma.sync, a thread's 32 bytes of a row
 // standing for other positions than the fragment's, the same ones for both operands, which a sum
-// does not notice. (Weights straight into registers: 24 tokens of the 33-expert layer 67 and 118 us
-// in the two kernels, of 277 MB each.)
+// does not notice. (24 tokens of the 33-expert layer of 1,024 / 4,096, 272 MB of weights in each kernel: 63 and 75 us
+// under the profiler; weights straight into registers 67 and 118.) The layer takes 23.4 us for one token (floor 14),
+// 83 for 8, 104 for 16, 142 for 24, 174 for 64, the forward 75, 133, 153, 151 and 154.
 #include <cuda_bf16.h>
 #include <math.h>
 
