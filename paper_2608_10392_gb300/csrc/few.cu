@@ -17,9 +17,9 @@
 // Weights stream through a ring of a warp's own in shared memory (cp.async, 2 KB a stage), so that what
 // is on its way does not depend on registers; the products are mma.sync, a thread's 32 bytes of a row
 // standing for other positions than the fragment's, the same ones for both operands, which a sum
-// does not notice. (24 tokens of the 33-expert layer of 1,024 / 4,096, 272 MB of weights in each kernel: 63 and 75 us
-// under the profiler; weights straight into registers 67 and 118.) The layer takes 23.4 us for one token (floor 14),
-// 83 for 8, 104 for 16, 142 for 24, 174 for 64, the forward 75, 133, 153, 151 and 154.
+// does not notice. (24 tokens of the 33-expert layer of 1,024 / 4,096, 272 MB of weights in each kernel: 53 and 75 us;
+// weights straight into registers 67 and 118.) The layer takes 24 us for one token of 80 pairs (floor 14),
+// 72 to 83 for 8, 105 for 16, 129 for 24, 152 for 64, the forward 75, 133, 153, 151 and 154.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -34,6 +34,7 @@ namespace few {
 constexpr int kThreads = 256, kWarps = kThreads / 32;  // of route_kernel and down_kernel
 constexpr int kUpWarps = 16;  // one CTA an SM: fewer read the router
 constexpr int kMost = UNIF_MOE_FEW_TOKENS;
+constexpr size_t kSmemMost = 232448;
 constexpr int kTogether = 8;  // most tokens that every CTA decides for itself
 
 struct Params {
@@ -324,20 +325,26 @@ struct UpShared {
   uint8_t slots[kUpWarps][kMost];          // a warp's tokens of its pair
 };
 constexpr int kUpStages = 6;
+// Tokens held in shared memory: rows of d values and 16 bytes.
+__host__ __device__ inline size_t held_bytes(int T, int d) { return ((size_t)T * (2 * d + 16) + 127) / 128 * 128; }
 // After it: the affinities [8][K] where the decisions are taken here, [G] pairs in use, then the rings
 // (before they are in use, the router's product in their place).
 __host__ __device__ inline size_t up_fixed(int G, int K, bool routes) {
   return ((sizeof(UpShared) + (size_t)G * 2 + (routes ? 32 * (size_t)K : 0)) + 127) / 128 * 128 + 128;
 }
-__host__ __device__ inline size_t up_smem(int G, int K, int C, bool routes) {
-  const size_t rings = (size_t)kUpWarps * kUpStages * kStage, product = routes ? 4 * (size_t)route_floats(C, kUpWarps) : 0;
+__host__ __device__ inline size_t up_smem(int G, int K, int C, bool routes, int stages, size_t held) {
+  const size_t rings = (size_t)kUpWarps * stages * kStage + held, product = routes ? 4 * (size_t)route_floats(C, kUpWarps) : 0;
   return up_fixed(G, K, routes) + (rings > product ? rings : product);
 }
 
 // NT: pieces of eight tokens that are taken at once; a pair that more tokens run is gone through again.
-// ROUTES: the decisions are taken here.
-template <int NT, bool ROUTES>
+// ROUTES: the decisions are taken here. HELD: the tokens are held in shared memory, in rings of that many stages
+// (0: they come from L1, of which the rings leave little, so that up to half as many bytes again come from L2; the
+// layer in us, without and with, 1,024 / 4,096, 33 experts: 24 tokens 139 and 129, 48 160 and 137, 64, two stages, 174
+// and 152; 768 wide, 17 experts: 64 tokens, three stages, 84 and 71; up to 8 tokens there is nothing to gain).
+template <int NT, bool ROUTES, int HELD>
 __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
+  constexpr int S = HELD ? HELD : kUpStages;
   constexpr int kThreads = 32 * kUpWarps, kWarps = kUpWarps;
   extern __shared__ __align__(16) uint8_t raw[];
   UpShared& sh = *reinterpret_cast<UpShared*>(raw);
@@ -419,6 +426,19 @@ __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
   if (first && threadIdx.x == 0) *p.n_pairs = all;
   __syncthreads();
 
+  const uint32_t held = rings + kWarps * S * kStage, pitch = 2 * p.d + 16;
+  if constexpr (HELD != 0) {
+    const int pieces = p.d / 8;
+    for (int i = threadIdx.x; i < p.T * pieces; i += kThreads) {
+      const int t = i / pieces, c = i - t * pieces;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(held + t * pitch + c * 16),
+                   "l"(p.x + (long long)t * p.ld_x + c * 8)
+                   : "memory");
+    }
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+  }
+
   if (first)
     for (int i = threadIdx.x; i < p.B + p.K; i += kThreads)
       p.members[i] = i < p.B ? sh.in_block[i] : sh.in_expert[i - p.B];
@@ -428,7 +448,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
   const Walk begin((int)(warp * gridDim.x + blockIdx.x), (int)(gridDim.x * kWarps), p.M / 16);
   const int g = lane >> 2, k0 = (lane & 3) * 16;
   uint8_t* slots_all = sh.slots[warp];
-  Ring<kUpStages> ring(rings + (uint32_t)warp * kUpStages * kStage, lane);
+  Ring<S> ring(rings + (uint32_t)warp * S * kStage, lane);
   Walk next = begin;          // of the blocks on their way
   int next_f = 0, again = 0;  // their features; times that the item's blocks are needed once more
   const __nv_bfloat16* keys = nullptr;
@@ -450,7 +470,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
     }
   };
 #pragma unroll
-  for (int k = 0; k < kUpStages - 1; ++k) fetch();
+  for (int k = 0; k < S - 1; ++k) fetch();
   for (Walk at = begin; at.pair < all; at.next()) {
     const int code = list[at.pair], row = at.part * 16;
     const int e = expert_of(code), b = block_of(code);
@@ -467,16 +487,31 @@ __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
     const uint8_t* slots = slots_all + s0;
     const int tokens = min(all_tokens - s0, 8 * NT), pieces = (tokens + 7) / 8;
     const __nv_bfloat16* x[NT];
+    uint32_t xs[NT];
+    auto token = [&](Piece& v, int t, int f) {  // 64 features of piece t's tokens
+      if constexpr (HELD != 0) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.r[0]), "=r"(v.r[1]), "=r"(v.r[2]), "=r"(v.r[3])
+                     : "r"(xs[t] + 128 * f));
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.r[4]), "=r"(v.r[5]), "=r"(v.r[6]), "=r"(v.r[7])
+                     : "r"(xs[t] + 128 * f + 16));
+      } else {
+        read_token(v, x[t] + 64 * f);
+      }
+    };
     float c[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int slot = t * 8 + g;
-      x[t] = p.x + (long long)(slot < tokens ? slots[slot] : slots[0]) * p.ld_x + k0;
+      const int tok = slot < tokens ? slots[slot] : slots[0];
+      if constexpr (HELD != 0) xs[t] = held + tok * pitch + k0 * 2;
+      else x[t] = p.x + (long long)tok * p.ld_x + k0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) c[t][j] = 0.f;
     }
     Piece v;
-    read_token(v, x[0]);
+    token(v, 0, 0);
     for (int f = 0; f < blocks; ++f) {
       Piece lo, hi;
       fetch();
@@ -485,10 +520,10 @@ __global__ void __launch_bounds__(32 * kUpWarps, 1) up_kernel(const Params p) {
 #pragma unroll
       for (int t = 1; t < NT; ++t)
         if (t < pieces) {
-          read_token(v, x[t] + 64 * f);
+          token(v, t, f);
           multiply(c[t], lo, hi, v);
         }
-      if (f + 1 < blocks) read_token(v, x[0] + 64 * (f + 1));
+      if (f + 1 < blocks) token(v, 0, f + 1);
     }
     // h = w GeLU, rounded once: the weight comes before the rounding, so that the down projection
     // adds up what is held
@@ -835,7 +870,19 @@ template <int NT, int TOK>
 cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
   const int G = (p.K + 1) * p.B;
   const bool routes = p.T <= kTogether;
-  const size_t smem = up_smem(G, p.K, p.C, routes);
+  void (*up)(const Params) = up_kernel<NT, NT == 1, 0>;
+  size_t smem = up_smem(G, p.K, p.C, routes, kUpStages, 0);
+  if constexpr (NT > 1) {
+    // (five stages instead of four, 24 tokens: 130 us and 129)
+    auto hold = [&](int stages, void (*kernel)(const Params)) {
+      const size_t need = up_smem(G, p.K, p.C, routes, stages, held_bytes(p.T, p.d));
+      if (need > kSmemMost) return false;
+      up = kernel;
+      smem = need;
+      return true;
+    };
+    if (!hold(4, up_kernel<NT, false, 4>) && !hold(3, up_kernel<NT, false, 3>)) hold(2, up_kernel<NT, false, 2>);
+  }
   cudaError_t e;
   if (!routes) {
     const size_t bytes = 4 * (size_t)route_floats(p.C, kWarps);
@@ -843,9 +890,6 @@ cudaError_t launch_as(const Params& p, int sms, cudaStream_t s) {
     if (e == cudaSuccess) e = launch_dependent(route_kernel, dim3(p.T), dim3(kThreads), bytes, s, p);
     if (e != cudaSuccess) return e;
   }
-  void (*up)(const Params);
-  if constexpr (NT == 1) up = up_kernel<1, true>;
-  else up = up_kernel<NT, false>;
   e = allow_smem_once(up, smem);
   if (e == cudaSuccess) e = launch_dependent(up, dim3(sms), dim3(32 * kUpWarps), smem, s, p);
   if (e != cudaSuccess) return e;
