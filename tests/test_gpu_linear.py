@@ -404,6 +404,99 @@ def test_results_repeat():
     assert all(torch.equal(a[name], b[name]) for name in a)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,H,masked", [(1, 64, 128, False), (130, 64, 136, True), (1000, 384, 1536, True)])
+def test_a_dense_ffn_in_training(T, d, H, masked):
+    """Norm, two products, and back, against 64 bits from end to end. Tolerances: every tensor's own,
+    from those of what it is made of by absolute values (a product's error |da| |b| + |a| |db|), sums
+    2^-18 of their terms (1,000 rows or 1,536 columns, cut at every 16, stay below 100 2^-22), bf16 2^-8, GELU's slope
+    1.13, that of its derivative 0.8, the derivative's own 2^-16; products of two errors, each below 2^-5 of its tensor
+    where that counts: 2^-4 more in all."""
+    from paper_2608_10392_gb300 import BlockNorm, linear, linear_backward, linear_status
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, d, generator=g, device="cuda")
+    w0 = (1 + 0.1 * torch.randn(d, generator=g, device="cuda")).bfloat16()
+    w1, w2 = operand(H, d, g, scale=d ** -0.5), operand(d, H, g, scale=H ** -0.5)
+    b1, b2 = (0.3 * torch.randn(n, generator=g, device="cuda") for n in (H, d))
+    dy = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    mask = torch.rand(T, generator=g, device="cuda") < 0.7 if masked else None
+    on = torch.ones(T, 1, device="cuda", dtype=F64) if mask is None else mask[:, None].to(F64)
+    if masked:
+        x[~mask], dy[~mask] = float("nan"), float("nan")
+    norm = BlockNorm(d, "f32", pre_norm="rms")
+    f = norm.forward(x, pre_weight=w0, mask=mask, stats=True)
+    h, z = linear(f["u"], w1, b1, activation="gelu", mask=mask, keep=True)
+    y = linear(h, w2, b2, residual=x, mask=mask, dtype="f32")
+    r2 = linear_backward(h, w2, dy, mask=mask, bias=True)
+    r1 = linear_backward(f["u"], w1, r2["dx"], z, activation="gelu", mask=mask, bias=True)
+    r0 = norm.backward(x, None, f, dout=dy.float(), du=r1["dx"], pre_weight=w0, mask=mask)
+    assert linear_status() == 0
+
+    e, cut = 2.0 ** -8, 2.0 ** -18
+    X, D = torch.where(on > 0, x.to(F64), 0.0), torch.where(on > 0, dy.to(F64), 0.0)
+    W0, W1, W2 = (t.to(F64) for t in (w0, w1, w2))
+    rstd = (X.square().mean(1, keepdim=True) + 1e-6).rsqrt()
+    u = X * rstd * W0
+    u_off = (e + cut) * u.abs()
+    Z = (u @ W1.T + b1.to(F64)) * on
+    S = (u.abs() @ W1.abs().T + b1.abs().to(F64)) * on
+    z_off = u_off @ W1.abs().T + cut * S          # before it is rounded, as GELU takes it
+    phi = torch.exp(-Z * Z / 2) / math.sqrt(2 * math.pi)
+    G = torch.special.ndtr(Z) + Z * phi
+    Hh = gelu(Z) * on
+    h_off = 1.13 * z_off + (e + 2.0 ** -11) * Hh.abs()
+    Y = (Hh @ W2.T + b2.to(F64) + X) * on
+    y_off = h_off @ W2.abs().T + cut * (Hh.abs() @ W2.abs().T + b2.abs() + X.abs())
+    dh = D @ W2
+    dh_off = e * dh.abs() + cut * (D.abs() @ W2.abs())
+    dz = dh * G * on
+    dz_off = (1.13 * dh_off + dh.abs() * (0.8 * (z_off + e * Z.abs()) + 2.0 ** -16)) * on
+    dz_as = dz_off + e * dz.abs()                 # as the products take it
+    du = dz @ W1
+    du_off = dz_as @ W1.abs() + e * du.abs() + cut * (dz.abs() @ W1.abs())
+    n = X * rstd
+    back = lambda v: rstd * (v * W0 - n * (v * W0 * n).mean(1, keepdim=True)) * on
+    size = lambda v: rstd * (v * W0.abs() + n.abs() * (v * W0.abs() * n.abs()).mean(1, keepdim=True)) * on
+    dx = D + back(du)
+    for got, want, off in ((y, Y, y_off), (r2["dw"], D.T @ Hh, D.abs().T @ h_off + cut * (D.abs().T @ Hh.abs())),
+                           (r2["dbias"], D.sum(0), cut * D.abs().sum(0)), (r2["dx"], dh, dh_off),
+                           (r1["dbias"], dz.sum(0), dz_off.sum(0) + cut * dz.abs().sum(0)),
+                           (r1["dw"], dz.T @ u, dz_as.T @ u.abs() + dz.abs().T @ u_off + cut * (dz.abs().T @ u.abs())),
+                           (r1["dx"], du, du_off), (r0["dx"], dx, size(du_off + cut * du.abs()) + cut * D.abs()),
+                           (r0["d_pre_weight"], (du * n).sum(0), ((du_off + cut * du.abs()) * n.abs()).sum(0))):
+        off = off * (1 + 2.0 ** -4) + 1e-12
+        bad = ~((got.to(F64) - want).abs() <= off)
+        assert not bad.any(), (int(bad.sum()), float(((got.to(F64) - want).abs() / off).max()))
+
+
+@pytest.mark.gpu
+def test_gradients_on_streams_and_in_graphs():
+    from paper_2608_10392_gb300 import linear_backward
+    k = grads(1500, 200, 136, 4, "gelu", True)
+    args = (k["x"], k["w"], k["dout"], k["z"])
+
+    def run(**s):
+        return linear_backward(*args, activation="gelu", mask=k["mask"], bias=True, **s)
+
+    want = run()
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [run(stream=s) for s in (first, second, first)]  # two at once, each with its own workspace
+    torch.cuda.synchronize()
+    assert all(torch.equal(r[n], want[n]) for r in got for n in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    flip = torch.rand(1500, device="cuda") < 0.5  # another batch and another mask in the same places
+    for t in (k["x"], k["dout"], k["z"]):
+        t.copy_(torch.where(flip[:, None], torch.randn(t.shape, device="cuda"), float("nan")))
+    k["mask"].copy_(flip)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = run()
+    assert all(torch.equal(held[n], want[n]) and torch.isfinite(held[n]).all() for n in want)
+
+
 # ------------------------------------------------------------------ refusals
 
 def test_refusals():
