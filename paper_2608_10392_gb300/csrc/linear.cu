@@ -57,6 +57,8 @@ constexpr uint32_t kColumns = 2 * 2 * 256 * 4;          // bias and scales of tw
 // are the result's bytes). A warp's 64 columns in registers, the accumulator given back at once, spill:
 // 65,536 x 1,024 to 4,096 388 and 560 us.
 constexpr int kSumSteps = 22;
+// The same for a bf16 result: cut 2,048 times, 2^-12 of it at most, a sixteenth of its rounding.
+constexpr int kSumSteps16 = 512;
 
 struct Params {
   int M, N;                        // rows and columns of the result
@@ -889,6 +891,7 @@ struct RowsParams {
 };
 constexpr int kRowsMax = 32;       // rows of x
 constexpr int kRowsWarps = 16;     // most warps of a CTA
+constexpr int kRowsBytes = 65536;  // of a row: 32 blocks of 128 bytes for an accumulator (as kSumSteps; longer rows: tiles)
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                           uint32_t b0, uint32_t b1) {
@@ -1385,7 +1388,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, Params p, co
       1024u + (kBars + 1) * 8u + 16u + kColumns + (wide ? kEpiWarps * p.boxes * kBox : kStagingOdd);
   p.stages = (int)std::min<uint32_t>(kMaxStages, (kSmemMax - beside) / p.stage_bytes);
   const uint32_t smem = beside + (uint32_t)p.stages * p.stage_bytes;
-  p.sum_steps = KIND == kWeight || (KIND != kInput && sizeof(TO) == 4) ? kSumSteps : 1 << 30;
+  p.sum_steps = KIND == kWeight || (KIND != kInput && sizeof(TO) == 4) ? kSumSteps : kSumSteps16;
   p.wait_limit = gemm_wait_limit();
   void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
                  const Params) =
@@ -1470,11 +1473,15 @@ bool overlap(const void* a, int64_t ld_a, int64_t width_a, int64_t rows_a, const
   return apart < (pa > pb ? width_b : width_a) || apart + (pa > pb ? width_a : width_b) > ld_a;
 }
 
+bool few_rows(const unif_moe_linear* p) {
+  return p->rows <= kRowsMax && (int64_t)p->cols * (p->in_dtype == UNIF_MOE_BF16 ? 2 : 1) <= kRowsBytes;
+}
+
 int in_size(const unif_moe_linear* p) { return p->in_dtype == UNIF_MOE_BF16 ? 2 : 1; }
 
 int64_t forward_bytes(const unif_moe_linear* p, const void* x, long long ld_x, const void* w, long long ld_w) {
   const int size = in_size(p);
-  if (p->rows <= kRowsMax) return 0;
+  if (few_rows(p)) return 0;
   int64_t need = 0;
   if (!tma_rows(x, ld_x, size)) need += round_up(p->rows * pitch_of(p->cols, size) * size);
   if (!tma_rows(w, ld_w, size)) need += round_up((int64_t)p->n * pitch_of(p->cols, size) * size);
@@ -1634,7 +1641,7 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
   e.z = static_cast<__nv_bfloat16*>(z);
   e.ld_z = ld_z;
   e.status = status;
-  if (p->rows <= ln::kRowsMax) {
+  if (ln::few_rows(p)) {
     ln::RowsParams r{};
     r.e = e;
     r.x = static_cast<const uint8_t*>(x);

@@ -134,6 +134,30 @@ def test_few_rows_and_long_reductions(T, cols, n, kind, bias, act, residual, dty
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,cols,n", [(3, 300000, 20), (3, 32768, 20), (20, 32769, 40), (50, 200000, 24), (300, 100001, 48),
+                                      (2000, 70000, 264)])
+def test_very_long_reductions(T, cols, n, dtype, kind):
+    """All terms positive, so that what an accumulator is cut by adds up: 2^-22 of what it holds each time (as
+    above), half of it on average over the accumulation. These are short, whatever the length: 512 steps of
+    four 32-byte sums for a bf16 result, 2^11 cuts, 2^-12; 22 steps for fp32 ones, or 32 of the few-row kernel, 2^7 cuts,
+    2^-16; an fp32 addition each, 2^-24."""
+    from paper_2608_10392_gb300 import linear, linear_status
+    k = inputs(T, cols, n, n, kind)
+    if kind == "bf16":
+        k["x"].abs_(), k["w"].abs_()
+    else:
+        for q in (k["x"], k["w"]):
+            q.codes.view(torch.uint8).bitwise_and_(0x7f)
+    got = linear(k["x"], k["w"], dtype=dtype)
+    assert linear_status() == 0
+    want = value(k["x"]) @ value(k["w"]).T
+    bound = 2.0 ** -12 + 2.0 ** -8 if dtype == "bf16" else 2.0 ** -16 + cols / (22 * 64) * 2.0 ** -24 + 2.0 ** -20
+    assert float((got.to(F64) / want - 1).abs().max()) < bound
+
+
+@pytest.mark.gpu
 def test_every_row_padding_and_no_rows():
     from paper_2608_10392_gb300 import linear
     for T in (4, 200):
