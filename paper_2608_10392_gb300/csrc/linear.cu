@@ -2,7 +2,7 @@
 // (unif_moe_linear_forward / _backward):
 //   z = sx sw (x w^T) + b,  out = r + act(z);   dz = dout act'(z),  dx = dz w,  dw = dz^T x
 //
-// Three kernels multiply.
+// Two kernels multiply, four prepare or finish (us: 65,536 x 4,096 to 1,024 291, the library's product 290).
 // - gemm_kernel: tiles of 128 rows, or of 256 on a CTA pair, by up to 256 columns on tcgen05,
 //   accumulators in TMEM (two, so that one is stored while the next is computed), operands by
 //   TMA through a ring of stages. All three products of a layer are this kernel: an operand
@@ -11,9 +11,11 @@
 // - rows_kernel: few rows, bound by the weights' bytes: a CTA takes 16 output channels, its
 //   warps share the columns, and both operands go from memory to mma.sync fragments without
 //   shared memory (a thread's 16 bytes stand for other columns than the fragment's, the same
-//   ones for both operands, which a sum does not notice).
-// - grad_kernel / finish_kernel: dz and the column sums of dbias; sums over the parts of a
-//   split reduction, in a fixed order.
+//   ones for both operands, which a sum does not notice). (4 x 1,024 to 4,096 3.3 us, at the floor of the bytes
+//   1.2; 16 rows 3.9, 32 6.3.)
+// - grad_kernel / finish_kernel: dz and the column sums of dbias (12,608 x 1,536 21 us; its bytes 17); sums over
+//   the parts of a split reduction, in a fixed order.
+// - layout_kernel / steps_kernel: rows that TMA cannot read, laid out; the steps of dw that are not all padding.
 #include <cuda_bf16.h>
 #include <math.h>
 
