@@ -28,6 +28,7 @@ SOURCES = ["unif_moe.cu", "route_permute.cu", "gemm_simt.cu", "gemm_tc.cu", "gem
 HEADERS = ["internal.cuh", "decide.cuh", "items.cuh", "tc_common.cuh", "per_device.h", "gelu_log.cuh",
            "fp8.cuh",
            os.path.join("..", "..", "include", "unif_moe.h")]
+BINDING_HEADERS = [os.path.join(CSRC, "row_distance.h"), os.path.join(CSRC, HEADERS[-1])]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -77,7 +78,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
             jobs.append(cmd)
 
     binding_compile, binding_link = _binding_cmd()
-    if force or _stale(BINDING_OBJ, [BINDING_SRC, headers[-1]]):
+    if force or _stale(BINDING_OBJ, [BINDING_SRC] + BINDING_HEADERS):
         jobs.append(binding_compile)
 
     def run(cmd):

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/unif_moe.h"
+#include "row_distance.h"
 
 namespace {
 
@@ -516,18 +517,10 @@ Rows codes_of(const Place& at, const Tensor& t, const char* name, int64_t& rows,
   cols = t.size(-1);
   if (cols < 1 || cols > UNIF_MOE_LINEAR_MAX_COLS || (cols > 1 && t.stride(-1) != 1))
     value_error(std::string(name) + ": need dense rows, got " + shown(t));
-  rows = 1;
   Rows r;
   r.p = t.data_ptr();
-  r.ld = 0;
-  for (int64_t i = t.dim() - 2; i >= 0; --i) {
-    if (t.size(i) > 1) {
-      if (!r.ld) r.ld = t.stride(i) / std::max<int64_t>(rows, 1);
-      if (t.stride(i) != r.ld * rows) value_error(std::string(name) + ": need rows at one distance, got " + shown(t));
-    }
-    rows *= t.size(i);
-  }
-  if (rows <= 1 || !r.ld) r.ld = std::max(r.ld, cols);
+  if (!unif::rows_at_one_distance(t.sizes().data(), t.strides().data(), (int)t.dim() - 1, cols, &rows, &r.ld))
+    value_error(std::string(name) + ": need rows at one distance, got " + shown(t));
   return r;
 }
 
