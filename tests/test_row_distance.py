@@ -67,6 +67,12 @@ def test_rows_that_are_one_row(rows_of):
     assert rows_of(torch.empty(900).as_strided((4, 64), (64, 1))) == (4, 64)
 
 
+def test_no_rows(rows_of):
+    for shape in ((0, 64), (3, 0, 64), (0, 3, 64), (2, 0, 3, 64), (2, 3, 0, 64)):
+        assert rows_of(torch.empty(shape)) == (0, 64)
+    assert rows_of(torch.empty(3, 0, 80)[..., :64]) == (0, 64)
+
+
 @pytest.mark.gpu
 def test_expanded_codes_are_refused():
     import paper_2608_10392_gb300 as pkg
@@ -90,3 +96,14 @@ def test_expanded_codes_are_refused():
     assert (buffer.view(torch.uint8) == 0).all()
     # one row stays what it was: dense, wherever it lies
     assert torch.equal(pkg.fp8_dequantize(pkg.Fp8(q.codes[:1].expand(1, 64), q.scales[:1])), x[:1].bfloat16())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(0, 50), (3, 0, 50), (0, 3, 50), (2, 3, 0, 64), (2, 0, 3, 64)])
+def test_no_rows_of_any_dimensions(shape):
+    from paper_2608_10392_gb300 import fp8_dequantize, fp8_quantize
+    for dtype in (torch.float32, torch.bfloat16):
+        q = fp8_quantize(torch.empty(shape, device="cuda", dtype=dtype))
+        assert q.codes.shape == shape and q.scales.shape == shape[:-1]
+        assert fp8_dequantize(q, dtype="f32").shape == shape
+        assert fp8_quantize(torch.empty(shape, device="cuda", dtype=dtype), out=q) is q
