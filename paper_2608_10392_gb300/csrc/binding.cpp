@@ -127,6 +127,16 @@ void* dense(const Place& at, const Tensor& t, const char* name, int64_t count, a
   return t.data_ptr();
 }
 
+// The same with the sizes given: a layout mistake is not taken for the right one.
+void* shaped(const Place& at, const Tensor& t, const char* name, at::IntArrayRef sizes, at::ScalarType type) {
+  if (!t.defined() || t.sizes() != sizes) {
+    std::string need;
+    for (const int64_t n : sizes) need += "[" + std::to_string(n) + "]";
+    value_error(std::string(name) + ": need " + need + (t.defined() ? ", got " + shown(t) : ""));
+  }
+  return dense(at, t, name, t.numel(), type);
+}
+
 const uint8_t* mask_of(const Place& at, const Tensor& t, int64_t T) {
   if (!t.defined()) return nullptr;
   return static_cast<const uint8_t*>(
@@ -727,9 +737,8 @@ PyObject* router_table(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int B = as_int(a[2]);
     if (E < 2 || E > 65 || H > 0x7fffffff || d > 0x7fffffff || B < 2 || B > 64)
       value_error("bad sizes: w_up " + shown(up) + ", " + std::to_string(B) + " blocks");
-    const void* pu = dense(at, up, "w_up", E * H * d, at::kBFloat16);
-    if (!wr.defined()) value_error("w_router: need a tensor");
-    const void* pr = dense(at, wr, "w_router", d * E, at::kBFloat16);
+    const void *pu = dense(at, up, "w_up", E * H * d, at::kBFloat16),
+               *pr = shaped(at, wr, "w_router", {d, E}, at::kBFloat16);
     const Tensor table = at.empty({E + B, d}, at::kBFloat16);
     check(unif_moe_router_table((int)d, (int)H, (int)E - 1, B, pr, pu, table.data_ptr(), at.stream()));
     return THPVariable_Wrap(table);
@@ -763,7 +772,6 @@ PyObject* few_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Place at(x, "x", a[11]);
     const FewRows r = few_rows(at, x, a[10]);
     if (!up.defined() || up.dim() != 3 || up.size(2) != r.d) value_error("w_up: need [K + 1][H][d]");
-    if (!router.defined() || !down.defined()) value_error("router and w_down: need tensors");
     const int64_t E = up.size(0), H = up.size(1);
     const int B = as_int(a[4]);
     if (E < 2 || E > 65 || H > 0x7fffffff || B < 2 || B > 64)
@@ -775,9 +783,9 @@ PyObject* few_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     d.th.beta_fixed = (float)as_double(PyTuple_GET_ITEM(a[7], 2));
     d.th.topk_fixed = as_int(PyTuple_GET_ITEM(a[7], 3));
     d.th.prefix_blocks = as_bool(PyTuple_GET_ITEM(a[7], 4));
-    const void *pr = dense(at, router, "router", (E + B) * r.d, at::kBFloat16),
+    const void *pr = shaped(at, router, "router", {E + B, r.d}, at::kBFloat16),
                *pu = dense(at, up, "w_up", E * H * r.d, at::kBFloat16),
-               *pd = dense(at, down, "w_down", E * H * r.d, at::kBFloat16);
+               *pd = shaped(at, down, "w_down", {E, r.d, H}, at::kBFloat16);
     const float* bias = static_cast<const float*>(dense(at, tensor(a[5], "router_bias"), "router_bias", E, at::kFloat));
     const uint8_t* mask = mask_of(at, tensor(a[6], "mask"), r.T);
     int32_t *bc = counts_of(at, a[8], "shared_counts", r.T), *kc = counts_of(at, a[9], "residual_counts", r.T);

@@ -321,3 +321,30 @@ def test_refusals_of_tensors_and_handles():
     L.load_weights(on["router"], on["up"], on["down"])
     with pytest.raises(ValueError):
         L.forward_few(torch.zeros(4, 128, device="cuda").bfloat16())
+
+
+@pytest.mark.gpu
+def test_weights_in_another_layout_are_refused():
+    """As many elements in another order: a router as columns, w_down as w_up's layout."""
+    import paper_2608_10392_gb300 as pkg
+    d, H, K, B = 64, 256, 3, 4
+    w, g = layer(d, H, K, B, 1)
+    on = {k: v.cuda() for k, v in w.items() if v is not None}
+    with pytest.raises(ValueError, match=r"w_router: need \[64\]\[4\]"):
+        pkg.router_table(on["router"].T.contiguous(), on["up"], B)
+    with pytest.raises(ValueError, match="w_router"):
+        pkg.router_table(on["router"].flatten(), on["up"], B)
+    with pytest.raises(ValueError, match="contiguous"):
+        pkg.router_table(on["router"].T.contiguous().T, on["up"], B)
+    table = pkg.router_table(on["router"], on["up"], B)
+    x = torch.zeros(4, d, device="cuda").bfloat16()
+    for down in (on["down"].transpose(1, 2).contiguous(), on["down"].transpose(0, 1).contiguous(), on["down"].flatten(0, 1)):
+        with pytest.raises(ValueError, match=r"w_down: need \[4\]\[64\]\[256\]"):
+            pkg.few_tokens(x, table, on["up"], down, B)
+    with pytest.raises(ValueError, match="contiguous"):
+        pkg.few_tokens(x, table, on["up"], on["down"].transpose(1, 2).contiguous().transpose(1, 2), B)
+    with pytest.raises(ValueError, match=r"router: need \[8\]\[64\]"):
+        pkg.few_tokens(x, table.T.contiguous(), on["up"], on["down"], B)
+    with pytest.raises(ValueError, match="router"):
+        pkg.few_tokens(x, None, on["up"], on["down"], B)
+    assert (pkg.few_tokens(x, table, on["up"], on["down"], B) == 0).all()
