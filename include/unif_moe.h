@@ -696,7 +696,7 @@ UNIF_MOE_API int64_t unif_moe_linear_workspace(const unif_moe_linear* p, const v
  *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose rows give 0 in out and z,
  *     whatever x and the residual hold there
  *   out_dev [T][n]; z_dev [T][n] bf16 or NULL: z for unif_moe_linear_backward
- *     (out shares memory with nothing else: ERR_ARG)
+ *     (out, but for the residual, and z share memory with nothing else: ERR_ARG)
  *   status_dev [1] int32: a kernel that gives up a wait sets it non-zero (zero it
  *     before the first call); the output is then incomplete
  * Sums are fp32, taken in an order that depends on the sizes alone; z and out are rounded once each. GELU as in

@@ -26,7 +26,7 @@ SOURCES = ["unif_moe.cu", "route_permute.cu", "gemm_simt.cu", "gemm_tc.cu", "gem
            "bundles.cu", "block_norm.cu", "balance.cu", "mxfp4.cu",
            "fp4_product.cu", "linear.cu", "fp8.cu", "few.cu"]
 HEADERS = ["internal.cuh", "decide.cuh", "items.cuh", "tc_common.cuh", "per_device.h", "gelu_log.cuh",
-           "fp8.cuh",
+           "fp8.cuh", "overlap.h",
            os.path.join("..", "..", "include", "unif_moe.h")]
 BINDING_HEADERS = [os.path.join(CSRC, "row_distance.h"), os.path.join(CSRC, HEADERS[-1])]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

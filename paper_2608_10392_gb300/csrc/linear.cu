@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "gelu_log.cuh"
+#include "overlap.h"
 #include "tc_common.cuh"
 
 namespace unif {
@@ -1464,17 +1465,6 @@ int check(const unif_moe_linear* p) {
   return UNIF_MOE_OK;
 }
 
-// Whether two arrays of rows share memory (columns of one wider array, each its own, do not). Bytes.
-bool overlap(const void* a, int64_t ld_a, int64_t width_a, int64_t rows_a, const void* b, int64_t ld_b,
-             int64_t width_b, int64_t rows_b) {
-  if (!a || !b || rows_a < 1 || rows_b < 1) return false;
-  const uintptr_t pa = bits(a), pb = bits(b);
-  if (pa + (rows_a - 1) * ld_a + width_a <= pb || pb + (rows_b - 1) * ld_b + width_b <= pa) return false;
-  if (ld_a != ld_b) return true;
-  const int64_t apart = (int64_t)((pa > pb ? pa - pb : pb - pa) % (uint64_t)ld_a);  // of the later one, in a row
-  return apart < (pa > pb ? width_b : width_a) || apart + (pa > pb ? width_a : width_b) > ld_a;
-}
-
 bool few_rows(const unif_moe_linear* p) {
   return p->rows <= kRowsMax && (int64_t)p->cols * (p->in_dtype == UNIF_MOE_BF16 ? 2 : 1) <= kRowsBytes;
 }
@@ -1614,12 +1604,19 @@ int unif_moe_linear_forward(const unif_moe_linear* p, const void* x, int64_t ld_
     set_error("the workspace must be 16-byte aligned");
     return UNIF_MOE_ERR_ARG;
   }
-  auto over = [&](const void* q, int64_t ld, int64_t width, int64_t rows, int bytes) {
-    return ln::overlap(out, ld_out * os, (int64_t)p->n * os, p->rows, q, ld * bytes, width * bytes, rows);
+  auto rows_of = [&](const void* q, int64_t ld, int64_t cols, int64_t rows, int bytes) {
+    return unif::Block{q, ld * bytes, cols * bytes, rows};
   };
-  if (over(x, ld_x, p->cols, p->rows, size) || over(w, ld_w, p->cols, p->n, size) || over(z, ld_z, p->n, p->rows, 2) ||
-      ((out != residual || (ld_out != ld_res && p->rows > 1)) && over(residual, ld_res, p->n, p->rows, os))) {
-    set_error("out overlaps x, w, z or another residual than itself");
+  const unif::Block to = rows_of(out, ld_out, p->n, p->rows, os), res = rows_of(residual, ld_res, p->n, p->rows, os),
+                    kept = rows_of(z, ld_z, p->n, p->rows, 2), bx = rows_of(x, ld_x, p->cols, p->rows, size),
+                    bw = rows_of(w, ld_w, p->cols, p->n, size),
+                    bb = unif::flat(bias, p->n * (p->bias_dtype == UNIF_MOE_F32 ? 4ll : 2ll)),
+                    bsx = unif::flat(x_scale, p->rows * 4), bsw = unif::flat(w_scale, p->n * 4ll),
+                    bm = unif::flat(mask, p->rows), ws_used = unif::flat(workspace, need), st = unif::flat(status, 4);
+  const bool in_place = out == residual && (ld_out == ld_res || p->rows == 1);
+  if (unif::overlap_any(to, {bx, bw, kept, bb, bsx, bsw, bm, ws_used, st}) || (!in_place && unif::overlap(to, res)) ||
+      unif::overlap_any(kept, {bx, bw, res, bb, bsx, bsw, bm, ws_used, st})) {
+    set_error("out or z overlaps another array of the call (the residual in out's place excepted)");
     return UNIF_MOE_ERR_ARG;
   }
   int sms = 0;

@@ -589,3 +589,64 @@ def test_refusals_of_tensors():
         pkg.linear(x, w[:, :63])
     with pytest.raises(ValueError, match="z: the gradient"):
         pkg.linear_backward(x, w, torch.zeros(4, 8, device="cuda").bfloat16(), activation="gelu")
+
+
+PLACES = {name: (i + 1) << 28 for i, name in enumerate(("x", "w", "sx", "sw", "bias", "res", "mask", "out", "z", "ws",
+                                                          "status"))}
+
+
+def test_results_over_operands_are_refused():
+    """out and z over each other and over everything else of the call, whole or by their ends. (Made-up
+    addresses: each call is refused before anything is launched.)"""
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+
+    def refused(eight=False, cols=64, ld_x=64, ld_res=64, bytes_=0, **moved):
+        at = {**PLACES, **moved}
+        d = ops._LinearDesc(100, cols, 64, 2 if eight else 1, 1, 0, 1)
+        rc = L.unif_moe_linear_forward(
+            C.byref(d), at["x"], ld_x, at["sx"] if eight else None, at["w"], 64, at["sw"] if eight else None, at["bias"],
+            at["res"], ld_res, at["mask"], at["out"], 64, at["z"], 64, at["ws"] if bytes_ else None, bytes_, at["status"],
+            None)
+        return rc == -1 and b"overlaps" in L.unif_moe_last_error()
+
+    size = dict(x=12800, w=8192, sx=400, sw=256, bias=256, res=12800, mask=100, out=12800, z=12800, status=4)
+    for result in ("out", "z"):
+        for name in size:
+            eight = name in ("sx", "sw")
+            for shift in (0, -12800 + 2, (size[name] - 1) // 2 * 2):
+                if name != result and not (result == "out" and name == "res" and shift == 0):  # (in its place)
+                    assert refused(eight, **{result: PLACES[name] + shift}), (result, name, shift)
+        # the workspace of rows that are laid out first
+        assert refused(cols=63, ld_x=63, bytes_=1 << 20, **{result: PLACES["ws"] + 6400})
+    assert refused(out=PLACES["res"], ld_res=72)  # the residual's place, with another stride
+
+
+@pytest.mark.gpu
+def test_columns_of_one_array_for_all_of_a_call():
+    """What lies side by side is not refused: x, residual, out and z as columns of one array."""
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    g = torch.Generator(device="cuda").manual_seed(8)
+    T = 200
+    wide = torch.randn(T, 64 + 48 * 3, generator=g, device="cuda").bfloat16()
+    x, res, out, z = wide[:, :64], wide[:, 64:112], wide[:, 112:160], wide[:, 160:]
+    w, status = operand(48, 64, g), torch.zeros(1, dtype=torch.int32, device="cuda")
+    want, z_want = pkg.linear(x.clone(), w, residual=res.clone(), activation="gelu", keep=True)
+    before = wide[:, :112].clone()
+    d = ops._LinearDesc(T, 64, 48, 1, 1, 1, 1)
+    p = lambda t: t.data_ptr()  # noqa: E731
+    need = pkg.lib().unif_moe_linear_workspace(C.byref(d), p(x), 208, p(w), 64)
+    assert need == 0
+    for to in (out, res):  # (the last: in place of the residual)
+        assert pkg.lib().unif_moe_linear_forward(
+            C.byref(d), p(x), 208, None, p(w), 64, None, None, p(res), 208, None, p(to), 208, p(z), 208, None, 0,
+            p(status), torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(to, want) and torch.equal(z, z_want) and int(status) == 0
+        assert torch.equal(wide[:, :64], before[:, :64])
+        if to is out:
+            assert torch.equal(res, before[:, 64:])
