@@ -737,6 +737,8 @@ UNIF_MOE_API int64_t unif_moe_linear_backward_workspace(const unif_moe_linear* p
  * they hold) take no part in the sums and give 0 in dx. dz enters the
  * products rounded to bf16, their operand type (exact for a bf16 dout without
  * activation); dbias sums it unrounded. Sums are fp32, in an order that depends on the sizes alone.
+ * dx, dw and dbias share memory with nothing that the call reads or writes besides (ERR_ARG); x without
+ * dw, w without dx and z without an activation are not read.
  * in_dtype must be BF16; out_dtype and bias_dtype of p are not used. Enqueued on
  * `stream`, no sync. Errors as the forward's. */
 UNIF_MOE_API int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_grad* g,

@@ -1716,6 +1716,23 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
   }
   if (!status) { set_error("status is NULL"); return UNIF_MOE_ERR_ARG; }
   if (!g->dx_dev && !g->dw_dev && !g->dbias_dev) return UNIF_MOE_OK;
+  // what is not read (x without dw, w without dx, z without an activation) may lie anywhere
+  auto rows_of = [](const void* q, int64_t ld, int64_t cols, int64_t rows, int64_t bytes) {
+    return unif::Block{q, ld * bytes, cols * bytes, rows};
+  };
+  const unif::Block bx = rows_of(g->dw_dev ? g->x_dev : nullptr, g->ld_x, p->cols, p->rows, 2),
+                    bw = rows_of(g->dx_dev ? g->w_dev : nullptr, g->ld_w, p->cols, p->n, 2),
+                    bd = rows_of(g->dout_dev, g->ld_dout, p->n, p->rows, g->dout_dtype == UNIF_MOE_F32 ? 4 : 2),
+                    bz = rows_of(p->activation != UNIF_MOE_ACTIVATION_NONE ? g->z_dev : nullptr, g->ld_z, p->n, p->rows, 2),
+                    bm = unif::flat(g->token_mask_dev, p->rows), st = unif::flat(status, 4),
+                    dx = rows_of(g->dx_dev, g->ld_dx, p->cols, p->rows, 2),
+                    dw = rows_of(g->dw_dev, g->ld_dw, p->cols, p->n, gs), db = unif::flat(g->dbias_dev, p->n * 4ll);
+  if (unif::overlap_any(dx, {bx, bw, bd, bz, bm, st, dw, db}) ||
+      unif::overlap_any(dw, {bx, bw, bd, bz, bm, st, db}) ||
+      unif::overlap_any(db, {bx, bw, bd, bz, bm, st})) {
+    set_error("dx, dw or dbias overlaps another array of the call");
+    return UNIF_MOE_ERR_ARG;
+  }
   int sms = 0;
   const int rs = unif::sm_count(&sms);
   if (rs != UNIF_MOE_OK) return rs;
@@ -1726,6 +1743,10 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
   }
   if (pl.total && ln::bits(workspace) % 32) {
     set_error("the workspace must be 32-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  if (unif::overlap_any(unif::flat(workspace, pl.total), {dx, dw, db})) {
+    set_error("dx, dw or dbias overlaps the workspace");
     return UNIF_MOE_ERR_ARG;
   }
   if ((long long)pl.in.m_tiles * pl.in.n_tiles > 0x7fff0000 ||

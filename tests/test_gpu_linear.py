@@ -625,6 +625,68 @@ def test_results_over_operands_are_refused():
     assert refused(out=PLACES["res"], ld_res=72)  # the residual's place, with another stride
 
 
+def backward_description(ops, at, act=1, rows=100, cols=64, n=64, gt=0, ld_x=64, **ask):
+    """(descriptions of a backward of the arrays `at`; with ask[name] False that result is not asked for)"""
+    d = ops._LinearDesc(rows, cols, n, 1, 1, 0, act)
+    want = {name: at[name] if ask.get(name, True) else None for name in ("dx", "dw", "dbias")}
+    return d, ops._LinearGrad(at["x"], at["w"], at["dout"], at["z"], ld_x, 64, 64, 64, 1, gt, at["mask"], want["dx"], 64,
+                              want["dw"], 64, want["dbias"])
+
+
+def test_gradients_over_operands_are_refused():
+    """dx, dw and dbias over each other and over all that the call reads, whole or by their ends. (Made-up
+    addresses: each call is refused before anything is launched.)"""
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+    size = dict(x=12800, w=8192, dout=12800, z=12800, mask=100, dx=12800, dw=16384, dbias=256, status=4)
+    places = {name: (i + 1) << 28 for i, name in enumerate(size)}
+    for result in ("dx", "dw", "dbias"):
+        for name in size:
+            for shift in (0, -size[result] + 4, (size[name] - 1) // 4 * 4):
+                if name == result:
+                    continue
+                at = {**places, result: places[name] + shift}
+                d, g = backward_description(ops, at)
+                assert L.unif_moe_linear_backward(C.byref(d), C.byref(g), None, 0, at["status"], None) == -1
+                assert b"overlaps" in L.unif_moe_last_error(), (result, name, shift)
+
+
+@pytest.mark.gpu
+def test_gradients_over_what_is_not_read():
+    """dx in the place of x without dw, dw in that of w without dx, dbias in that of z without an activation; over
+    the workspace they are refused."""
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+    k = grads(100, 64, 64, 3)
+    x, w, dout = k["x"].contiguous(), k["w"].contiguous(), k["dout"].contiguous()
+    want = pkg.linear_backward(x, w, dout, grad_dtype="bf16", bias=True)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for ask in (dict(dw=False), dict(dx=False), dict(dx=False, dw=False)):
+        to = dict(x=x.clone(), w=w.clone(), dout=dout, z=torch.zeros(100, 64, device="cuda").bfloat16())
+        place = dict(dx=to["x"], dw=to["w"], dbias=to["z"])
+        at = {n: t.data_ptr() for n, t in to.items()}
+        at.update({n: t.data_ptr() for n, t in place.items()}, mask=None)
+        d, gr = backward_description(ops, at, act=0, gt=1, **ask)
+        need = L.unif_moe_linear_backward_workspace(C.byref(d), C.byref(gr))
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        assert L.unif_moe_linear_backward(C.byref(d), C.byref(gr), ws.data_ptr(), need, status.data_ptr(),
+                                          torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        for name in ("dx", "dw"):
+            if ask.get(name, True):
+                assert torch.equal(place[name], want[name])
+        assert torch.equal(place["dbias"].view(torch.float32).flatten()[:64], want["dbias"])
+        d, gr = backward_description(ops, {**at, "dbias": ws.data_ptr()}, act=0, gt=1, **ask)
+        assert need > 0 and L.unif_moe_linear_backward(C.byref(d), C.byref(gr), ws.data_ptr(), need, status.data_ptr(),
+                                                       None) == -1
+        assert b"overlaps" in L.unif_moe_last_error()
+
+
 @pytest.mark.gpu
 def test_columns_of_one_array_for_all_of_a_call():
     """What lies side by side is not refused: x, residual, out and z as columns of one array."""
