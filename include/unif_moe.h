@@ -628,7 +628,8 @@ UNIF_MOE_API int64_t unif_moe_few_workspace(const unif_moe_few* p);
  *   token_mask_dev [T] uint8 or NULL: 0 marks padding, whose rows are not used and give 0
  *   shared_counts_dev, residual_counts_dev [T] int32 or NULL: b(x) and k(x), 0 for padding
  *   workspace_dev: of one call at a time
- * out may be x, with its stride. Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE, ERR_CAPACITY (T above
+ * out may lie over x; out, the counts and the workspace share memory with nothing else (ERR_ARG). Enqueued on
+ * `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE, ERR_CAPACITY (T above
  * UNIF_MOE_FEW_TOKENS, workspace), ERR_CUDA. */
 UNIF_MOE_API int unif_moe_few_forward(const unif_moe_few* p, const void* x_dev, int64_t ld_x,
                                       const void* router_dev, const float* router_bias_dev,

@@ -27,6 +27,7 @@
 
 #include "gelu_log.cuh"
 #include "internal.cuh"
+#include "overlap.h"
 
 namespace unif {
 namespace few {
@@ -932,6 +933,17 @@ int run(const unif_moe_few* d, const void* x, int64_t ld_x, const void* router, 
   }
   if (off(workspace, 16)) {
     set_error("the workspace must be 16-byte aligned");
+    return UNIF_MOE_ERR_ARG;
+  }
+  // (x's rows are read before the first of out's is written)
+  const int64_t T = d->tokens, weight_bytes = ((int64_t)d->n_experts + 1) * d->d_ff * d->d_model * 2;
+  const Block to{out, ld_out * 2, d->d_model * 2ll, T}, used = flat(workspace, at.total),
+      bx{x, ld_x * 2, d->d_model * 2ll, T}, br = flat(router, (1ll + d->n_experts + d->n_blocks) * d->d_model * 2),
+      bb = flat(bias, 4ll * (d->n_experts + 1)), bu = flat(up, weight_bytes), bd = flat(down, weight_bytes), bm = flat(mask, T),
+      nb = flat(b_out, 4 * T), nk = flat(k_out, 4 * T);
+  if (overlap_any(to, {br, bb, bu, bd, bm, nb, nk, used}) || overlap_any(used, {bx, br, bb, bu, bd, bm, nb, nk}) ||
+      overlap_any(nb, {bx, br, bb, bu, bd, bm, nk}) || overlap_any(nk, {bx, br, bb, bu, bd, bm})) {
+    set_error("out, the counts or the workspace overlaps another array of the call (x under out excepted)");
     return UNIF_MOE_ERR_ARG;
   }
   int sms = 0;

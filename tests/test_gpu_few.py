@@ -348,3 +348,43 @@ def test_weights_in_another_layout_are_refused():
     with pytest.raises(ValueError, match="router"):
         pkg.few_tokens(x, None, on["up"], on["down"], B)
     assert (pkg.few_tokens(x, table, on["up"], on["down"], B) == 0).all()
+
+
+def test_results_over_operands_are_refused():
+    """out, the counts and the workspace over each other and over all that the call reads, but for out over x. (Made-up
+    addresses: each call is refused before anything is launched.)"""
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+    T, d, H, K, B = 30, 64, 256, 3, 4
+    desc = ops._FewDesc(T, d, H, K, B, math.nan, math.nan, math.nan, 0, 0)
+    need = L.unif_moe_few_workspace(C.byref(desc))
+    weights = (K + 1) * H * d * 2
+    size = dict(x=T * d * 2, router=(1 + K + B) * d * 2, bias=4 * (K + 1), up=weights, down=weights, mask=T, out=T * d * 2,
+                b=4 * T, k=4 * T, ws=need)
+    places = {name: (i + 1) << 28 for i, name in enumerate(size)}
+    for result in ("out", "b", "k", "ws"):
+        for name in size:
+            for shift in (0, -((size[result] - 1) // 16 * 16), (size[name] - 1) // 16 * 16):
+                if name == result or (result, name) == ("out", "x"):
+                    continue
+                at = {**places, result: places[name] + shift}
+                rc = L.unif_moe_few_forward(C.byref(desc), at["x"], d, at["router"], at["bias"], at["up"], at["down"],
+                                            at["mask"], at["out"], d, at["b"], at["k"], at["ws"], need, None)
+                assert rc == -1 and b"overlaps" in L.unif_moe_last_error(), (result, name, shift)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4, 30])
+def test_out_over_x_a_row_further(T):
+    from paper_2608_10392_gb300 import few_tokens, router_table
+    w, g = layer(256, 512, 4, 4, 2)
+    on = {k: None if v is None else v.cuda() for k, v in w.items()}
+    table = router_table(on["router"], on["up"], 4)
+    both = torch.randn(T + 1, 256, generator=g).bfloat16().cuda()
+    x = both[:T].clone()
+    want = few_tokens(x, table, on["up"], on["down"], 4)
+    few_tokens(both[:T], table, on["up"], on["down"], 4, out=both[1:])
+    assert torch.equal(both[1:], want) and torch.equal(both[0], x[0])
