@@ -496,8 +496,8 @@ UNIF_MOE_API int unif_moe_block_norm_backward(
 
 /* The forward with u in 8 bits, as unif_moe_fp8_quantize gives it from the fp32 u (not from a
  * rounded one): u_codes_dev [T][width] E4M3, rows ld_u bytes apart, u_scales_dev [T]. Padding
- * rows have codes 0. Needs a pre norm; u_codes overlaps no input. The backward takes the gradient of u as if nothing
- * had been rounded. Everything else as unif_moe_block_norm_forward. */
+ * rows have codes 0. Needs a pre norm; u_codes and u_scales share memory with no other rows of the call (ERR_ARG).
+ * The backward takes the gradient of u as if nothing had been rounded. Everything else as unif_moe_block_norm_forward. */
 UNIF_MOE_API int unif_moe_block_norm_forward_fp8(
     const unif_moe_block_norm* p, const void* x_dev, int64_t ld_x, const void* y_dev, int64_t ld_y,
     const uint8_t* token_mask_dev, const void* w_post_dev, const void* b_post_dev,
@@ -653,7 +653,7 @@ UNIF_MOE_API int unif_moe_forward_few(unif_moe_t h, const void* x_dev, int64_t l
  * even. A row with a NaN or an infinity gets the scale NaN and codes 0.
  *   x_dev [rows][cols] fp32 or bf16, rows ld apart
  *   codes_dev [rows][cols], rows ld_codes bytes apart; scales_dev [rows] fp32
- * Up to 2^24 columns. Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_CUDA. */
+ * Up to 2^24 columns; the three share no memory (ERR_ARG). Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_CUDA. */
 UNIF_MOE_API int unif_moe_fp8_quantize(const void* x_dev, unif_moe_dtype dtype, int64_t rows, int cols,
                                        int64_t ld, uint8_t* codes_dev, int64_t ld_codes,
                                        float* scales_dev, void* stream);

@@ -20,6 +20,7 @@
 
 #include "fp8.cuh"
 #include "internal.cuh"
+#include "overlap.h"
 
 namespace unif {
 namespace norm {
@@ -1495,6 +1496,16 @@ int norm_forward(const unif_moe_block_norm* p, const void* x, int64_t ld_x, cons
       nm::ld_bad(out, ld_out, p->width) || nm::ld_bad(p->pre_norm ? u : nullptr, ld_u, p->width)) {
     set_error("a row stride is below the width");
     return UNIF_MOE_ERR_ARG;
+  }
+  if (u_scale) {  // (a row's codes lie in another row's place: not even over y)
+    const int64_t T = p->tokens, width = p->width, sx = p->stream_dtype == UNIF_MOE_F32 ? 4 : 2,
+                  sy = p->branch_dtype == UNIF_MOE_F32 ? 4 : 2;
+    const unif::Block bx{x, ld_x * sx, width * sx, T}, by{y, ld_y * sy, width * sy, T}, bo{out, ld_out * sx, width * sx, T},
+        bu{u, ld_u, width, T}, bs = unif::flat(u_scale, T * 4), bm = unif::flat(mask, T);
+    if (unif::overlap_any(bu, {bx, by, bo, bs, bm}) || unif::overlap_any(bs, {bx, by, bo, bm})) {
+      set_error("u's codes or scales overlap another array of the call");
+      return UNIF_MOE_ERR_ARG;
+    }
   }
   int sms = 0;
   const int rs = unif::sm_count(&sms);

@@ -12,6 +12,7 @@
 
 #include "fp8.cuh"
 #include "internal.cuh"
+#include "overlap.h"
 
 namespace unif {
 namespace fp8 {
@@ -207,6 +208,13 @@ int check(const void* x, int dtype, int64_t rows, int cols, int64_t ld, const vo
   }
   if (ld < cols || ld_c < cols) {
     set_error("a row stride is below cols=%d", cols);
+    return UNIF_MOE_ERR_ARG;
+  }
+  // (rows of other CTAs, or later pieces of a row, are still to be read when the first result is written)
+  const int64_t size = dtype == UNIF_MOE_F32 ? 4 : 2;
+  const Block bx{x, ld * size, cols * size, rows}, bc{codes, ld_c, cols, rows}, bs = flat(scales, rows * 4);
+  if (overlap_any(bx, {bc, bs}) || overlap(bc, bs)) {
+    set_error("x, codes and scales overlap");
     return UNIF_MOE_ERR_ARG;
   }
   return UNIF_MOE_OK;

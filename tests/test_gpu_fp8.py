@@ -350,3 +350,52 @@ def test_refusals_of_tensors():
             x, x.bfloat16(), post_weight=torch.ones(64, device="cuda").bfloat16())
     with pytest.raises(ValueError):
         pkg.linear(q, pkg.Fp8(q.codes, None))
+
+
+def test_arrays_that_overlap_are_refused():
+    """Codes or scales over the rows, whole or by their ends, in all three calls. (Made-up addresses: each
+    call is refused before anything is launched.)"""
+    from paper_2608_10392_gb300 import build
+    build.build()
+    import paper_2608_10392_gb300 as pkg
+    from paper_2608_10392_gb300 import operators as ops
+    L = pkg.lib()
+    T, d = 100, 64
+    places = {name: (i + 1) << 28 for i, name in enumerate(("x", "y", "out", "codes", "scales", "mask"))}
+
+    def calls(at, dt, norm):
+        if not norm:
+            yield L.unif_moe_fp8_quantize(at["x"], dt, T, d, d, at["codes"], d, at["scales"], None)
+            yield L.unif_moe_fp8_dequantize(at["codes"], d, at["scales"], T, d, at["x"], dt, d, None)
+        desc = ops._BlockNormDesc(T, d, dt, dt, 0, 2, 0, 1.0, 1e-6)
+        yield L.unif_moe_block_norm_forward_fp8(C.byref(desc), at["x"], d, at["y"], d, at["mask"], None, None, None,
+                                                0x70000000, None, at["out"], d, at["codes"], d, at["scales"], None, None,
+                                                None, None, None)
+
+    for dt, rows in ((0, T * d * 4), (1, T * d * 2)):
+        size = dict(x=rows, y=rows, out=rows, codes=T * d, scales=4 * T, mask=T)
+        for result in ("codes", "scales"):
+            for name in size:
+                for shift in (0, -((size[result] - 1) // 4 * 4), (size[name] - 1) // 4 * 4):
+                    if name == result:
+                        continue
+                    at = {**places, result: places[name] + shift}
+                    for rc in calls(at, dt, name in ("y", "out", "mask")):
+                        assert rc == -1 and b"overlap" in L.unif_moe_last_error(), (dt, result, name, shift)
+
+
+@pytest.mark.gpu
+def test_codes_and_rows_side_by_side():
+    """Rows and their codes as columns of one array."""
+    from paper_2608_10392_gb300 import Fp8, UnifMoeError, fp8_dequantize, fp8_quantize
+    wide = torch.zeros(50, 3 * 64, device="cuda").bfloat16()
+    wide[:, :64] = data(50, 64, torch.bfloat16)
+    x, want = wide[:, :64], check(wide[:, :64].contiguous())
+    codes = wide.view(torch.float8_e4m3fn)[:, 128:192]
+    out = fp8_quantize(x, out=Fp8(codes, torch.empty(50, device="cuda")))
+    assert same(out.codes, want.codes) and same(out.scales, want.scales)
+    back = fp8_dequantize(out, out=wide[:, 128:])
+    assert same(back, fp8_dequantize(want)) and same(wide[:, :64], x)
+    for bad in (wide.view(torch.float8_e4m3fn)[:, :64], wide.view(torch.float8_e4m3fn)[:, 127:191]):
+        with pytest.raises(UnifMoeError, match="overlap"):
+            fp8_quantize(x, out=Fp8(bad, out.scales))
