@@ -1801,7 +1801,7 @@ int unif_moe_linear_backward(const unif_moe_linear* p, const unif_moe_linear_gra
     e.N = p->cols;
     e.splits = 1;
     e.steps = (p->n + 63) / 64;
-    e.mask = pl.make_dz ? nullptr : g->token_mask_dev;  // (dz's own padding rows are 0)
+    e.mask = g->token_mask_dev;  // (dz's padding rows are 0, but 0 times an infinite weight is not)
     e.out = g->dx_dev;
     e.ld_out = g->ld_dx;
     e.status = status;

@@ -712,3 +712,32 @@ def test_columns_of_one_array_for_all_of_a_call():
         assert torch.equal(wide[:, :64], before[:, :64])
         if to is out:
             assert torch.equal(res, before[:, 64:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,cols,n", [(5, 64, 64), (70, 64, 48), (300, 200, 136), (300, 77, 130), (3000, 512, 256),
+                                      (64, 64, 4096)])
+@pytest.mark.parametrize("act,dtype", [("none", "bf16"), ("none", "f32"), ("gelu", "bf16")])
+def test_padding_rows_under_weights_that_are_not_finite(T, cols, n, act, dtype):
+    """An infinity or NaN of the weights reaches dx of every row but padding, whose dx is 0 whether or not dz
+    is laid out first; dw and dbias do not read the weights."""
+    from paper_2608_10392_gb300 import linear, linear_backward, linear_status
+    k = grads(T, cols, n, T + n, act, True, dtype)
+    k["mask"][0], k["mask"][-1] = False, True
+    for name in ("x", "dout", "z"):
+        if name in k:
+            k[name][0], k[name][-1] = float("nan"), 0.5
+    ask = dict(activation=act, mask=k["mask"], bias=True)
+    want = linear_backward(k["x"].nan_to_num(), k["w"], k["dout"].nan_to_num(), k["z"].nan_to_num() if "z" in k else None, **ask)
+    w = k["w"].clone()
+    w[3, 2], w[n // 2, cols - 1], w[n - 1, 0] = float("inf"), -float("inf"), float("nan")
+    r = linear_backward(k["x"], w, k["dout"], k.get("z"), **ask)
+    out = linear(k["x"], w, mask=k["mask"], dtype="f32")
+    assert linear_status() == 0
+    pad = ~k["mask"]
+    assert (r["dx"][pad] == 0).all() and (out[pad] == 0).all()
+    assert torch.equal(r["dw"], want["dw"]) and torch.equal(r["dbias"], want["dbias"])
+    assert r["dx"][k["mask"]][:, 0].isnan().all()
+    same = torch.ones(cols, dtype=torch.bool, device="cuda")
+    same[[0, 2, cols - 1]] = False
+    assert torch.equal(r["dx"][:, same], want["dx"][:, same])
