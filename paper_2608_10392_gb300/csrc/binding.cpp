@@ -790,10 +790,11 @@ PyObject* few_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const uint8_t* mask = mask_of(at, tensor(a[6], "mask"), r.T);
     int32_t *bc = counts_of(at, a[8], "shared_counts", r.T), *kc = counts_of(at, a[9], "residual_counts", r.T);
     const int64_t need = unif_moe_few_workspace(&d);
-    if (need < 0) check(r.T > UNIF_MOE_FEW_TOKENS ? UNIF_MOE_ERR_CAPACITY : UNIF_MOE_ERR_ARG);
-    const Tensor ws = at.empty({need}, at::kByte);
-    check(unif_moe_few_forward(&d, r.x.p, r.x.ld, pr, bias, pu, pd, mask, r.out.p, r.out.ld, bc, kc, ws.data_ptr(),
-                               need, at.stream()));
+    Tensor ws;
+    if (need > 0) ws = at.empty({need}, at::kByte);
+    // (where there is none, the call says why)
+    check(unif_moe_few_forward(&d, r.x.p, r.x.ld, pr, bias, pu, pd, mask, r.out.p, r.out.ld, bc, kc,
+                               need > 0 ? ws.data_ptr() : nullptr, need, at.stream()));
     return THPVariable_Wrap(r.to);
   });
 }

@@ -388,3 +388,15 @@ def test_out_over_x_a_row_further(T):
     want = few_tokens(x, table, on["up"], on["down"], 4)
     few_tokens(both[:T], table, on["up"], on["down"], 4, out=both[1:])
     assert torch.equal(both[1:], want) and torch.equal(both[0], x[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,H,K,B,code", [(4, 96, 256, 3, 4, "ERR_SHAPE"), (4, 64, 128, 3, 4, "ERR_SHAPE"),
+                                            (65, 64, 256, 3, 4, "ERR_CAPACITY"), (65, 96, 256, 3, 4, "ERR_CAPACITY")])
+def test_refusals_have_the_code_of_the_call(T, d, H, K, B, code):
+    import paper_2608_10392_gb300 as pkg
+    t = lambda *s: torch.zeros(*s, device="cuda").bfloat16()  # noqa: E731
+    with pytest.raises(pkg.UnifMoeError, match=code):
+        pkg.few_tokens(t(T, d), t(1 + K + B, d), t(K + 1, H, d), t(K + 1, d, H), B)
+    with pytest.raises(pkg.UnifMoeError, match="ERR_ARG"):
+        pkg.few_tokens(t(4, 64), t(8, 64), t(4, 256, 64), t(4, 64, 256), 4, alpha_fixed=2.0)
