@@ -746,30 +746,34 @@ def test_padding_rows_under_weights_that_are_not_finite(T, cols, n, act, dtype):
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "dx"])
 def test_what_accumulations_lose_on_average(kind):
-    """2^20 positive terms a sum, into bf16. Rounding is as often up as down, the cuts of an accumulator all go one
-    way: the mean of the signed errors shows them. A cut loses 2^-22 of what is held at most, half of that on
-    average, and over an accumulation half of its sum is held on average: 2^11 cuts (512 steps of four) leave
-    2^11 2^-23 / 2 = 2^-13. 2^20 columns in one accumulation, 2^16 cuts (8 bits: 2^15), would be 32 (16) times that. Of
-    128 x 128 results, spread over their binade by the scales of rows and channels, the mean of roundings by 2^-8
-    at most (2^-8 / sqrt(3) each) stays within five of its deviations, 2^-8 / sqrt(3) / 128."""
+    """2^20 positive terms a sum, into bf16, in tiles whose reduction no CTAs share. Rounding is as often up as
+    down, the cuts of an accumulator all go one way: the mean of the signed errors shows them. A cut loses at most
+    2^-22 of what is held (as above), over an accumulation half of its sum is held on average: 2^11 cuts (512 steps
+    of four) lose at most 2^11 2^-22 / 2 = 2^-12. In one unbroken accumulation there are 2^16 cuts (8 bits: 2^15), 32 (16)
+    times as many. Of 128 x 128 results, spread over their binade by the scales of rows and channels, the mean of
+    roundings by 2^-8 at most (2^-8 / sqrt(3) each) stays within five of its deviations, 2^-8 / sqrt(3) / 128."""
     from paper_2608_10392_gb300 import linear, linear_backward, linear_status
     g = torch.Generator(device="cuda").manual_seed(20)
-    long, few = 1 << 20, 128
-    if kind == "e4m3":
-        x, w = eight(few, long, g), eight(few, long, g)
-        for q in (x, w):
+    long, T, n, few = 1 << 20, 1280, 2048, 128
+
+    def rows(count):
+        if kind == "e4m3":
+            q = eight(count, long, g)
             q.codes.view(torch.uint8).bitwise_and_(0x7f)
-    else:
-        x, w = (torch.randn(few, long, generator=g, device="cuda").abs_() * (1 + torch.rand(few, 1, generator=g, device="cuda"))
-                for _ in range(2))
-        x, w = x.bfloat16(), w.bfloat16()
-    want = value(x) @ value(w).T
+            return q
+        r = torch.randn(count, long, generator=g, device="cuda").abs_()
+        return r.mul_(1 + torch.rand(count, 1, generator=g, device="cuda")).bfloat16()
+
+    def some(q, step):
+        return value(type(q)(q.codes[::step], q.scales[::step]) if kind == "e4m3" else q[::step])
+
+    x, w = rows(T), rows(n)
+    want = some(x, T // few) @ some(w, n // few).T
     if kind == "dx":
-        w = w.T.contiguous()
-        got = linear_backward(torch.empty(few, few, device="cuda").bfloat16(), w, x, dw=False)["dx"]
+        got = linear_backward(torch.empty(T, n, device="cuda").bfloat16(), w.T.contiguous(), x, dw=False)["dx"]
     else:
         got = linear(x, w)
     assert linear_status() == 0
-    loss = 1 - got.to(F64) / want
-    assert float(loss.abs().max()) < 2.0 ** -8 + 2.0 ** -11
-    assert abs(float(loss.mean())) < 2.0 ** -13 + 5 * 2.0 ** -8 / 3 ** 0.5 / few, float(loss.mean())
+    loss = 1 - got[::T // few, ::n // few].to(F64) / want
+    assert loss.shape == (few, few) and float(loss.abs().max()) < 2.0 ** -8 + 2.0 ** -11
+    assert abs(float(loss.mean())) < 2.0 ** -12 + 5 * 2.0 ** -8 / 3 ** 0.5 / few, float(loss.mean())
