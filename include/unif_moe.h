@@ -601,7 +601,7 @@ UNIF_MOE_API int unif_moe_mxfp4_product(const uint8_t* a_codes_dev, const uint8_
  * one step after another: two kernels (three above 8 tokens) that read the weights of each
  * (expert, block) pair in use once. Decisions are those of unif_moe_forward but for near-ties (the
  * logits' sums have another order); h and y are rounded as there, h after its weight. No atomics:
- * results repeat bit for bit. */
+ * a call repeats bit for bit; the order of a token's sums depends on the pairs that all its tokens take. */
 #define UNIF_MOE_FEW_TOKENS 64
 
 typedef struct {
@@ -700,7 +700,9 @@ UNIF_MOE_API int64_t unif_moe_linear_workspace(const unif_moe_linear* p, const v
  *     (out, but for the residual, and z share memory with nothing else: ERR_ARG)
  *   status_dev [1] int32: a kernel that gives up a wait sets it non-zero (zero it
  *     before the first call); the output is then incomplete
- * Sums are fp32, taken in an order that depends on the sizes alone; z and out are rounded once each. GELU as in
+ * Sums are fp32; z and out are rounded once each. A call repeats bit for bit: the order of its sums depends on the
+ * sizes, the arrays' strides and alignment, whether z is kept, and the device. x_scale x w_scale is formed first, in
+ * fp32 (rows and channels whose scales' product leaves its range lose their results). GELU as in
  * unif_moe_mxfp4_product, for fp32 results with the accuracy of normcdff.
  * Enqueued on `stream`, no sync. Errors: ERR_ARG, ERR_SHAPE (more than 2^31 tiles),
  * ERR_CAPACITY (workspace), ERR_CUDA. */
@@ -737,7 +739,8 @@ UNIF_MOE_API int64_t unif_moe_linear_backward_workspace(const unif_moe_linear* p
  * z_dev [T][n] is the forward's; not read (may be NULL) without an activation. Padding rows (whatever
  * they hold) take no part in the sums and give 0 in dx. dz enters the
  * products rounded to bf16, their operand type (exact for a bf16 dout without
- * activation); dbias sums it unrounded. Sums are fp32, in an order that depends on the sizes alone.
+ * activation); dbias sums it unrounded. Sums are fp32; a call repeats bit for bit: their order depends on the sizes, the
+ * arrays' strides and alignment, the mask's contents (dw leaves out steps of nothing but padding) and the device.
  * dx, dw and dbias share memory with nothing that the call reads or writes besides (ERR_ARG); x without
  * dw, w without dx and z without an activation are not read.
  * in_dtype must be BF16; out_dtype and bias_dtype of p are not used. Enqueued on

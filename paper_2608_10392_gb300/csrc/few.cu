@@ -18,8 +18,9 @@
 // is on its way does not depend on registers; the products are mma.sync, a thread's 32 bytes of a row
 // standing for other positions than the fragment's, the same ones for both operands, which a sum
 // does not notice. (24 tokens of the 33-expert layer of 1,024 / 4,096, 272 MB of weights in each kernel: 53 and 75 us;
-// weights straight into registers 67 and 118.) The layer takes 24 us for one token of 80 pairs (floor 14),
-// 72 to 83 for 8, 105 for 16, 129 for 24, 152 for 64, the forward 75, 133, 153, 151 and 154.
+// weights straight into registers 67 and 118.) One token takes 16 us (launches, decisions, the drain of two
+// kernels) and the time of its pairs' bytes, 1.05 MB each: 16 pairs 18.8 us (floor 2.5), 48 23.1 (7.4), 80 26.9 (12.4), 168
+// 42.4 (25.9); the forward 75. 8 tokens take 72 to 83 us, 16 105, 24 129, 64 152, the forward 133, 153, 151 and 154.
 #include <cuda_bf16.h>
 #include <math.h>
 

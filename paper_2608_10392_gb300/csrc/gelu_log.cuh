@@ -25,9 +25,9 @@ __device__ __forceinline__ void two_to(uint64_t q, float& p0, float& p1) {
 }
 
 // GELU of two values, max(v, 0) + x Phi(x), for results that are rounded to bf16: Q of degree 8, its
-// error the same everywhere, leaves Phi within 2^-12.8 of itself. (The storing warps of a product
-// are bound by these multiply-adds: 65,536 x 1,024 to 4,096 in 8 bits takes 250 us, with degree 11 275,
-// without GELU 190; 12,608 x 384 to 1,536 in bf16 22.8, 24.2 and 17.3.)
+// error the same everywhere, leaves Phi within 2^-12.8 of itself, a twenty-eighth of the result's rounding by 2^-8.
+// (A product's storing warps run this chain between the load and the store of a piece: 65,536 x 1,024 to 4,096 in 8
+// bits takes 250 us, with degree 11 275, without GELU 190; 12,608 x 384 to 1,536 in bf16 22.8, 24.2 and 17.3.)
 __device__ __forceinline__ void gelu2(float& v0, float& v1) {
   const uint64_t x = negative2(v0, v1);
   uint64_t q = UNIF_K2(0x32ed9bf9);         // g8

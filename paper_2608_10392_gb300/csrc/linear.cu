@@ -11,8 +11,9 @@
 // - rows_kernel: few rows, bound by the weights' bytes: a CTA takes 16 output channels, its
 //   warps share the columns, and both operands go from memory to mma.sync fragments without
 //   shared memory (a thread's 16 bytes stand for other columns than the fragment's, the same
-//   ones for both operands, which a sum does not notice). (4 x 1,024 to 4,096 3.3 us, at the floor of the bytes
-//   1.2; 16 rows 3.9, 32 6.3.)
+//   ones for both operands, which a sum does not notice). (1,024 to 4,096, weights from memory: 1 to 8 rows 4.3 us, at
+//   the floor of the bytes 1.2, the library's product 4.4; 16 rows 5.0 and 3.6, 32 7.2 and 3.7. Weights in L2: 4 rows
+//   3.3, 16 3.9, 32 6.3.)
 // - grad_kernel / finish_kernel: dz and the column sums of dbias (12,608 x 1,536 21 us; its bytes 17); sums over
 //   the parts of a split reduction, in a fixed order.
 // - layout_kernel / steps_kernel: rows that TMA cannot read, laid out; the steps of dw that are not all padding.
@@ -60,7 +61,9 @@ constexpr uint32_t kColumns = 2 * 2 * 256 * 4;          // bias and scales of tw
 // are the result's bytes). A warp's 64 columns in registers, the accumulator given back at once, spill:
 // 65,536 x 1,024 to 4,096 388 and 560 us.
 constexpr int kSumSteps = 22;
-// The same for a bf16 result: cut 2,048 times, 2^-12 of it at most, a sixteenth of its rounding.
+// The same for a bf16 result: cut 2,048 times, by 2^-22 of what the accumulator holds at most, so by 2^-11 of its terms'
+// absolute values together, and 2^-12 where they are of one sign (measured on average, 2^20 such columns: 1.7e-4 of
+// the result in bf16, 5e-5 in 8 bits); its own rounding is 2^-8 at most.
 constexpr int kSumSteps16 = 512;
 
 struct Params {
@@ -166,8 +169,8 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162flo
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// What becomes of two results: bf16 ones take the packed GELU (2^-12 of the value at most,
-// before a rounding of 2^-9), fp32 ones the library's.
+// What becomes of two results: bf16 ones take the packed GELU (2^-12.5 of the value at most,
+// before a rounding of 2^-8), fp32 ones the library's.
 template <typename TO>
 __device__ __forceinline__ void act2(float& a, float& b) {
   if constexpr (sizeof(TO) == 4) {
